@@ -268,6 +268,123 @@ int fgd_js_distance(int device, int K, int64_t U, int64_t V, int top_k, const fl
                     const float* avg_logits, int32_t* top_idx, double* d_js, double* cd_worker,
                     void* stream);
 
+/* ---- operators of the inner step ---------------------------------------------------------
+ * The round starts from theta_local, the result of H optimizer steps of a Llama-style decoder on
+ * every worker (Sec. 4.1, Algorithm 1's inner loop; Sec. 5 for the models).  These are the decoder
+ * block's operators that a plain matrix-product library does not have.  Activations are fp32, bf16
+ * or fp16 (one type per call); sums, softmax statistics and norms are held in fp32, and every result is rounded
+ * once.  As everywhere: asynchronous on `stream`, no allocation, deterministic (no floating-point
+ * atomics), no caller pointer kept after the call.  Errors: reason via fgd_last_error(NULL). */
+typedef enum { FGD_F32 = 0, FGD_BF16 = 1, FGD_F16 = 2 } fgd_dtype;
+
+/* A [tokens, heads, head_dim] tensor: element (t, h, c) at p[t * token_stride + h * head_stride + c];
+ * strides in elements.  Slices of a fused projection and head-major tensors are both of this form. */
+typedef struct {
+  void* p;
+  int64_t token_stride;
+  int64_t head_stride;
+} fgd_heads;
+
+/* Causal attention over packed sequences with grouped heads.
+ *   S_ij = scale q_i . k_j for the keys j <= i of the same sequence,  P = softmax_j(S),
+ *   o_i = sum_j P_ij v_j,   lse_i = log sum_j exp(S_ij)
+ * n_q_heads is a multiple of n_kv_heads; query head h reads key head h / (n_q_heads / n_kv_heads).
+ * What stands in another sequence's rows (infinities, NaN) never reaches a result; inside a sequence a
+ * query sees no score of a later key, but a non-finite v of a later row of the same 128-row
+ * block can reach it (0 x inf), on the tensor-core path. */
+typedef struct {
+  int32_t dtype; /* fgd_dtype of every fgd_heads tensor */
+  int32_t n_q_heads, n_kv_heads, head_dim;
+  fgd_heads q, k, v; /* inputs */
+  fgd_heads o;       /* forward: output; backward: input */
+  float* lse;        /* [n_q_heads, tokens]; forward: output; backward: input */
+  double scale;
+  /* backward only: */
+  fgd_heads dout;       /* gradient of o */
+  float* delta;         /* [n_q_heads, tokens] scratch: sum over the width of o * dout */
+  fgd_heads dq, dk, dv; /* outputs; dk, dv summed over the query heads that share them */
+} fgd_attn_args;
+
+/* A packing: sequence i holds the tokens [cu_seqlens[i], cu_seqlens[i+1]) (HOST memory, n_seqs + 1 values,
+ * cu_seqlens[0] = 0, not decreasing; empty sequences are fine).  The plan keeps the work list of the
+ * kernels on the device (a few bytes per 128 tokens), so create it once per batch and use it for every
+ * layer, forward and backward, on any head count and width.  Creating it allocates and copies (not inside
+ * a stream capture); the calls that use it do neither and can be captured.  A plan is used by one
+ * host thread at a time; kernels of one plan may run on several streams at once. */
+typedef struct fgd_attn_plan fgd_attn_plan;
+int fgd_attn_plan_create(fgd_attn_plan** out, int device, int n_seqs, const int64_t* cu_seqlens);
+int fgd_attn_plan_destroy(fgd_attn_plan* plan);
+/* head_dim <= 256.  bf16 and fp16 with head_dim a multiple of 8 up to 128, 16-byte aligned bases and strides that
+ * are multiples of 8 elements run on the tensor cores; everything else on the CUDA cores (slower, not an error).
+ * Outputs may not overlap any other tensor. */
+int fgd_attn_forward(fgd_attn_plan* plan, const fgd_attn_args* args, void* stream);
+int fgd_attn_backward(fgd_attn_plan* plan, const fgd_attn_args* args, void* stream);
+/* As fgd_device_status, for the kernels that used this plan: synchronises `stream`, reports
+ * FGD_ERR_TIMEOUT if a bounded device-side wait gave up since the last check, and clears the flag. */
+int fgd_attn_status(fgd_attn_plan* plan, void* stream);
+
+/* A [rows, width] matrix, `ld` elements between rows; p == NULL: absent. */
+typedef struct {
+  void* p;
+  int64_t ld;
+} fgd_mat;
+typedef enum { FGD_GATE_NONE = 0, FGD_GATE_CHANNEL = 1, FGD_GATE_ELEMENT = 2 } fgd_gate_kind;
+
+/* The norms after and before a block, fused with the block's gate and the scaled residual add, for
+ * `workers` workers at once (worker m owns the rows [m rows, (m+1) rows) of every activation and row m of every
+ * per-channel tensor, e.g. a column range of the flat [K, ld] parameter matrix):
+ *   u = y r_y w_post, r_y = 1/sqrt(mean(y^2) + eps)   (w_post absent: u = y)
+ *   x_new = x + res_scale * gate o u                  (y absent: x_new = x, which is then written only
+ *                                                      where x_new is given and is not x itself)
+ *   n = x_new r_x w_pre, r_x = 1/sqrt(mean(x_new^2) + eps)   (n absent: no norm; n is formed from the
+ *                                                      fp32 x_new, before it is rounded to its type)
+ * x_new may be x itself.  Gradients (x_new and y as they were stored; dres = gradient of x_new from
+ * elsewhere, absent = 0; dn absent: n was not formed):
+ *   dx (of x, and of x_new's other readers' sum), dy, dgate, dw_post, dw_pre; dx may be dres itself.
+ * Per-channel tensors (w_post, w_pre, a CHANNEL gate and their gradients) are fp32 [workers, width]; activations
+ * and an ELEMENT gate are of `dtype`.  Outputs may not overlap anything else.  width <= 16384,
+ * workers <= FGD_MAX_K.  Full speed: 16-byte aligned rows and width a multiple of 16 bytes; otherwise an element-wise kernel. */
+typedef struct {
+  int32_t dtype, workers;
+  int64_t rows; /* per worker */
+  int64_t width;
+  int32_t gate_kind;
+  double eps, res_scale;
+  fgd_mat x, y, gate, w_post, w_pre;           /* inputs */
+  fgd_mat x_new, n;                            /* forward: outputs; backward: x_new is an input */
+  fgd_mat dn, dres;                            /* backward: inputs */
+  fgd_mat dx, dy, dgate, dw_post, dw_pre;      /* backward: outputs */
+  void* workspace;                             /* backward: device scratch */
+  int64_t workspace_bytes;
+} fgd_block_norm_args;
+int fgd_block_norm_forward(int device, const fgd_block_norm_args* args, void* stream);
+int fgd_block_norm_backward(int device, const fgd_block_norm_args* args, void* stream);
+/* Bytes of scratch fgd_block_norm_backward needs (>= 0), or a negative status. */
+int64_t fgd_block_norm_workspace(int device, int dtype, int workers, int64_t rows, int64_t width);
+
+/* Activation checkpoints in 8 bits: groups of 32 consecutive values of a row (the last one may be shorter)
+ * share a power-of-two step.  e8 = max(biased exponent of the group's largest magnitude - 6, 1),
+ * q8 = round-to-even(x 2^(127 - e8)) held to [-127, 127], value = q8 2^(e8 - 127); e8 = 255 marks a
+ * group with an infinity or a NaN, which reads back as NaN.  Error: half a step, at most 1/128 of the
+ * group's largest magnitude (one step for an fp32 or fp16 value in the topmost 1/256 below a power of two).  bf16 values read back
+ * are exact.
+ *   x, out: device [rows, width] of `dtype`;  q8: int8 [rows, width];  e8: uint8 [rows, ceil(width / 32)]. */
+int fgd_act_save8(int device, int dtype, int64_t rows, int64_t width, const void* x, int64_t ld_x, int8_t* q8, int64_t ld_q,
+                  uint8_t* e8, int64_t ld_e, void* stream);
+int fgd_act_load8(int device, int dtype, int64_t rows, int64_t width, const int8_t* q8, int64_t ld_q, const uint8_t* e8,
+                  int64_t ld_e, void* out, int64_t ld_out, void* stream);
+/* SwiGLU with its inputs kept as an 8-bit checkpoint.  gu: [rows, 2 width], the gate half g first, then u.
+ *   forward:  h = g sigmoid(g) u, and the checkpoint of g and u: q8 [rows, 2 width], e8 [rows, 2 ceil(width / 32)]
+ *             (the groups of g, then those of u);
+ *   backward: from dh and the checkpoint alone (g^, u^ the values it stands for, s = sigmoid(g^)):
+ *             dgu = (dh u^ s (1 + g^ (1 - s)),  dh g^ s), and where h is given h = g^ s u^ again,
+ *             which the gradient of the following projection's weights needs. */
+int fgd_swiglu8_forward(int device, int dtype, int64_t rows, int64_t width, const void* gu, int64_t ld_gu, void* h, int64_t ld_h,
+                        int8_t* q8, int64_t ld_q, uint8_t* e8, int64_t ld_e, void* stream);
+int fgd_swiglu8_backward(int device, int dtype, int64_t rows, int64_t width, const void* dh, int64_t ld_dh, const int8_t* q8,
+                         int64_t ld_q, const uint8_t* e8, int64_t ld_e, void* dgu, int64_t ld_dgu, void* h, int64_t ld_h,
+                         void* stream);
+
 /* (No counterpart in the paper: a packaging variant of fgd_consensus_distance.)
  * Same result as fgd_consensus_distance, for callers that cannot allocate GPU memory and so
  * cannot create a context: it needs no fgd_ctx and calls no cudaMalloc / cudaFree or any other

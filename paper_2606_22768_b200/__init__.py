@@ -50,6 +50,27 @@ class _CMixDesc(ctypes.Structure):
                 ("w_self", ctypes.c_void_p), ("edge_mask", ctypes.c_void_p), ("W", ctypes.c_void_p)]
 
 
+class _CHeads(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class _CAttnArgs(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("q", _CHeads), ("k", _CHeads), ("v", _CHeads), ("o", _CHeads), ("lse", ctypes.c_void_p), ("scale", ctypes.c_double),
+                ("dout", _CHeads), ("delta", ctypes.c_void_p), ("dq", _CHeads), ("dk", _CHeads), ("dv", _CHeads)]
+
+
+class _CMat(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("ld", ctypes.c_int64)]
+
+
+class _CBlockNormArgs(ctypes.Structure):
+    _fields_ = ([("dtype", ctypes.c_int32), ("workers", ctypes.c_int32), ("rows", ctypes.c_int64), ("width", ctypes.c_int64),
+                 ("gate_kind", ctypes.c_int32), ("eps", ctypes.c_double), ("res_scale", ctypes.c_double)]
+                + [(n, _CMat) for n in ("x", "y", "gate", "w_post", "w_pre", "x_new", "n", "dn", "dres", "dx", "dy", "dgate", "dw_post", "dw_pre")]
+                + [("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64)])
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with `python paper_2606_22768_b200/build.py` "
@@ -75,6 +96,18 @@ def _load():
         "fgd_consensus_distance": (i32, [vp, vp, vp, vp]),
         "fgd_consensus_distance_noalloc": (i32, [i32, i32, i64, i64, vp, vp, vp]),
         "fgd_js_distance": (i32, [i32, i32, i64, i64, i32, vp, vp, vp, vp, vp, vp]),
+        "fgd_attn_plan_create": (i32, [ctypes.POINTER(vp), i32, i32, vp]),
+        "fgd_attn_plan_destroy": (i32, [vp]),
+        "fgd_attn_forward": (i32, [vp, ctypes.POINTER(_CAttnArgs), vp]),
+        "fgd_attn_backward": (i32, [vp, ctypes.POINTER(_CAttnArgs), vp]),
+        "fgd_attn_status": (i32, [vp, vp]),
+        "fgd_block_norm_forward": (i32, [i32, ctypes.POINTER(_CBlockNormArgs), vp]),
+        "fgd_block_norm_backward": (i32, [i32, ctypes.POINTER(_CBlockNormArgs), vp]),
+        "fgd_block_norm_workspace": (i64, [i32, i32, i32, i64, i64]),
+        "fgd_act_save8": (i32, [i32, i32, i64, i64, vp, i64, vp, i64, vp, i64, vp]),
+        "fgd_act_load8": (i32, [i32, i32, i64, i64, vp, i64, vp, i64, vp, i64, vp]),
+        "fgd_swiglu8_forward": (i32, [i32, i32, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp]),
+        "fgd_swiglu8_backward": (i32, [i32, i32, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp]),
         "fgd_topo_ring": (i32, [i32, vp, vp, vp]),
         "fgd_topo_onepeer_xor": (i32, [i32, i64, vp, vp, vp]),
         "fgd_topo_hypercube": (i32, [i32, vp, vp, vp]),
@@ -404,3 +437,245 @@ def fgd_js_distance(worker_logits, avg_logits, top_idx, d_js, cd_worker, top_k: 
                               _dev_ptr(cd_worker, "cd_worker", "torch.float64"), _stream(stream))
     if rc != 0:
         raise FgdError(rc, fgd_last_error(None))
+
+
+# ------------------------------------------------------------------ operators of the inner step
+FGD_F32, FGD_BF16, FGD_F16 = 0, 1, 2
+FGD_GATE_NONE, FGD_GATE_CHANNEL, FGD_GATE_ELEMENT = 0, 1, 2
+ACT8_GROUP = 32      # values that share one step in an 8-bit checkpoint
+_DTYPES = {"torch.float32": FGD_F32, "torch.bfloat16": FGD_BF16, "torch.float16": FGD_F16}
+
+
+def _dtype_of(t, name: str) -> int:
+    code = _DTYPES.get(str(t.dtype))
+    if code is None:
+        raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+    return code
+
+
+def _op_check(rc: int) -> None:
+    if rc != 0:
+        raise FgdError(rc, fgd_last_error(None))
+
+
+def _like(t, name: str, dtype, shape, device) -> None:
+    """Shape, type and device of a tensor argument."""
+    if not getattr(t, "is_cuda", False):
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+
+
+def _stream_on(stream, device):
+    if stream is None:
+        import torch
+        return torch.cuda.current_stream(device).cuda_stream
+    return getattr(stream, "cuda_stream", stream)
+
+
+class AttnPlan:
+    """A packing of sequences: sequence i holds the tokens cu_seqlens[i] .. cu_seqlens[i+1] - 1 (host values).
+    Create one per batch; every layer's forward and backward use it."""
+
+    def __init__(self, cu_seqlens, device: int = 0):
+        cu = np.ascontiguousarray(cu_seqlens, dtype=np.int64)
+        if cu.ndim != 1 or cu.size < 1:
+            raise ValueError("cu_seqlens must hold n_seqs + 1 values")
+        h = ctypes.c_void_p()
+        self._h = None
+        _op_check(_lib.fgd_attn_plan_create(ctypes.byref(h), int(device), int(cu.size) - 1, cu.ctypes.data))
+        self._h, self.device, self.tokens, self.n_seqs = h, int(device), int(cu[-1]), int(cu.size) - 1
+
+    def close(self):
+        if getattr(self, "_h", None):
+            _lib.fgd_attn_plan_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def fgd_attn_status(plan: AttnPlan, stream=None) -> None:
+    """Synchronises the stream; raises FgdError(FGD_ERR_TIMEOUT) if a device-side wait of a kernel of this plan gave up."""
+    _op_check(_lib.fgd_attn_status(plan._h, _stream(stream)))
+
+
+def _heads(t, name: str, dtype, shape, device) -> _CHeads:
+    _like(t, name, dtype, shape, device)
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError(f"{name} must be contiguous along the head width")
+    return _CHeads(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _attn_args(plan, q, k, v, o, lse, scale):
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q and k must be [tokens, heads, width]")
+    import torch
+    dev, (T, hq, d), hk = q.device, q.shape, k.shape[1]
+    if T != plan.tokens:
+        raise ValueError(f"q has {T} tokens, the plan {plan.tokens}")
+    if dev.type != "cuda" or dev.index != plan.device:
+        raise ValueError(f"q is on {dev}, the plan on cuda:{plan.device}")
+    a = _CAttnArgs(_dtype_of(q, "q"), hq, hk, d, _heads(q, "q", q.dtype, (T, hq, d), dev), _heads(k, "k", q.dtype, (T, hk, d), dev),
+                   _heads(v, "v", q.dtype, (T, hk, d), dev), _heads(o, "o", q.dtype, (T, hq, d), dev))
+    _like(lse, "lse", torch.float32, (hq, T), dev)
+    if not lse.is_contiguous():
+        raise ValueError("lse must be contiguous")
+    a.lse, a.scale = lse.data_ptr(), float(d) ** -0.5 if scale is None else float(scale)
+    return a
+
+
+def fgd_attn_forward(plan: AttnPlan, q, k, v, o, lse, scale: Optional[float] = None, stream=None) -> None:
+    """Causal attention over the plan's packed sequences: q [T, Hq, d], k and v [T, Hk, d] -> o [T, Hq, d], lse [Hq, T] (fp32).
+    Any token and head strides (slices of a fused projection); ``scale`` defaults to d ** -0.5."""
+    a = _attn_args(plan, q, k, v, o, lse, scale)
+    _op_check(_lib.fgd_attn_forward(plan._h, ctypes.byref(a), _stream_on(stream, q.device)))
+
+
+def fgd_attn_backward(plan: AttnPlan, q, k, v, o, dout, lse, delta, dq, dk, dv, scale: Optional[float] = None, stream=None) -> None:
+    """Gradients of :func:`fgd_attn_forward` from its inputs, o and lse.  ``delta`` [Hq, T] (fp32) is scratch; dk and dv are summed
+    over the query heads that share a key head."""
+    import torch
+    a = _attn_args(plan, q, k, v, o, lse, scale)
+    dev = q.device
+    _like(delta, "delta", torch.float32, lse.shape, dev)
+    if not delta.is_contiguous():
+        raise ValueError("delta must be contiguous")
+    a.delta = delta.data_ptr()
+    a.dout, a.dq = _heads(dout, "dout", q.dtype, q.shape, dev), _heads(dq, "dq", q.dtype, q.shape, dev)
+    a.dk, a.dv = _heads(dk, "dk", q.dtype, k.shape, dev), _heads(dv, "dv", q.dtype, k.shape, dev)
+    _op_check(_lib.fgd_attn_backward(plan._h, ctypes.byref(a), _stream_on(stream, dev)))
+
+
+def _mat(t, name: str, dtype, shape, device) -> _CMat:
+    if t is None:
+        return _CMat(None, 0)
+    _like(t, name, dtype, shape, device)
+    if shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must be contiguous along a row")
+    return _CMat(t.data_ptr(), t.stride(0) if shape[0] > 1 else max(t.stride(0), shape[1]))
+
+
+def _block_norm_args(first, x_new, y, gate, w_post, w_pre, eps, res_scale):
+    """The part of the arguments that forward and backward share; ``first`` gives shape and type."""
+    if first is None or first.dim() != 2:
+        raise ValueError("activations must be [tokens, width]")
+    import torch
+    dev, (T, H) = first.device, first.shape
+    channel = w_pre if w_pre is not None else w_post
+    if channel is None and gate is not None and gate.dtype == torch.float32 and gate.shape != first.shape:
+        channel = gate
+    K = 1 if channel is None else channel.shape[0]
+    if T % K != 0:
+        raise ValueError(f"{T} rows do not split over {K} workers")
+    a = _CBlockNormArgs(_dtype_of(first, "activations"), K, T // K, H)
+    # [K, width] is a gate per channel, [T, width] one per element (one row per worker: the fp32 one counts as per channel)
+    by_channel = gate is not None and gate.shape[0] == K and (K != T or gate.dtype == torch.float32)
+    a.gate_kind = FGD_GATE_NONE if gate is None else FGD_GATE_CHANNEL if by_channel else FGD_GATE_ELEMENT
+    a.eps, a.res_scale = float(eps), float(res_scale)
+    f32 = torch.float32
+    a.x_new, a.y = _mat(x_new, "x_new", first.dtype, (T, H), dev), _mat(y, "y", first.dtype, (T, H), dev)
+    a.gate = _mat(gate, "gate", f32 if by_channel else first.dtype, (K if by_channel else T, H), dev)
+    a.w_post, a.w_pre = _mat(w_post, "w_post", f32, (K, H), dev), _mat(w_pre, "w_pre", f32, (K, H), dev)
+    return a, dev, T, H, K, by_channel
+
+
+def fgd_block_norm_forward(x, y, gate, w_post, w_pre, x_new, n, eps: float = 1e-5, res_scale: float = 1.0, stream=None) -> None:
+    """x_new = x + res_scale * gate * norm(y) * w_post and n = norm(x_new) * w_pre, in one pass.  Activations [T, H]; w_post, w_pre
+    [K, H] fp32 for K workers with T / K rows each; gate None, [K, H] fp32 (per channel) or [T, H] (per element).  w_post, y, n (with
+    w_pre), x_new and gate may be None, see ``include/fgd.h``; x_new may be x."""
+    a, dev, T, H, K, _ = _block_norm_args(x, x_new, y, gate, w_post, w_pre, eps, res_scale)
+    if T == 0:
+        return
+    a.x, a.n = _mat(x, "x", x.dtype, (T, H), dev), _mat(n, "n", x.dtype, (T, H), dev)
+    _op_check(_lib.fgd_block_norm_forward(dev.index, ctypes.byref(a), _stream_on(stream, dev)))
+
+
+def fgd_block_norm_workspace(dtype: int, workers: int, rows: int, width: int, device: int = 0) -> int:
+    """Bytes of scratch that :func:`fgd_block_norm_backward` needs for ``rows`` rows per worker."""
+    n = int(_lib.fgd_block_norm_workspace(int(device), int(dtype), int(workers), int(rows), int(width)))
+    if n < 0:
+        raise FgdError(n, "fgd_block_norm_workspace: argument out of range")
+    return n
+
+
+def fgd_block_norm_backward(dn, dres, x_new, y, gate, w_post, w_pre, dx, dy, dgate, dw_post, dw_pre, eps: float = 1e-5, res_scale: float = 1.0,
+                            workspace=None, stream=None) -> None:
+    """Gradients of :func:`fgd_block_norm_forward` from x_new and y as stored; dn is the gradient of n, dres that of x_new from elsewhere
+    (None: zero), dx may be dres.  ``workspace``: a uint8 CUDA tensor of :func:`fgd_block_norm_workspace` bytes (None: allocated here)."""
+    import torch
+    first = dn if dn is not None else dres
+    a, dev, T, H, K, by_channel = _block_norm_args(first, x_new, y, gate, w_post, w_pre, eps, res_scale)
+    f32 = torch.float32
+    a.dw_post, a.dw_pre = _mat(dw_post, "dw_post", f32, (K, H), dev), _mat(dw_pre, "dw_pre", f32, (K, H), dev)
+    a.dgate = _mat(dgate, "dgate", f32 if by_channel else first.dtype, (K if by_channel else T, H), dev)
+    if T == 0:
+        with torch.cuda.stream(stream) if isinstance(stream, torch.cuda.Stream) else torch.cuda.device(dev):
+            for g in (dw_post, dw_pre, dgate):
+                if g is not None:
+                    g.zero_()
+        return
+    for name, t in (("dn", dn), ("dres", dres), ("dx", dx), ("dy", dy)):
+        setattr(a, name, _mat(t, name, first.dtype, (T, H), dev))
+    need = fgd_block_norm_workspace(a.dtype, K, T // K, H, dev.index)
+    handle = _stream_on(stream, dev)
+    if workspace is None:
+        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+        if handle != torch.cuda.current_stream(dev).cuda_stream:   # the caching allocator must not hand it out again before the call has run
+            workspace.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(handle, device=dev))
+    a.workspace, a.workspace_bytes = _dev_ptr(workspace, "workspace", "torch.uint8"), workspace.numel()
+    _op_check(_lib.fgd_block_norm_backward(dev.index, ctypes.byref(a), handle))
+
+
+def _act8(t, name: str, dtype, rows: int, width: int, device):
+    m = _mat(t, name, dtype, (rows, width), device)
+    return m.p, m.ld
+
+
+def fgd_act_save8(x, q8, e8, stream=None) -> None:
+    """x [rows, width] -> its 8-bit checkpoint q8 (int8 [rows, width]) and e8 (uint8 [rows, ceil(width / 32)])."""
+    import torch
+    if x.dim() != 2:
+        raise ValueError("x must be [rows, width]")
+    (R, W), dev = x.shape, x.device
+    _op_check(_lib.fgd_act_save8(dev.index or 0, _dtype_of(x, "x"), R, W, *_act8(x, "x", x.dtype, R, W, dev), *_act8(q8, "q8", torch.int8, R, W, dev),
+                                 *_act8(e8, "e8", torch.uint8, R, -(-W // ACT8_GROUP), dev), _stream_on(stream, dev)))
+
+
+def fgd_act_load8(q8, e8, out, stream=None) -> None:
+    """The values an 8-bit checkpoint stands for, in out's type."""
+    import torch
+    if out.dim() != 2:
+        raise ValueError("out must be [rows, width]")
+    (R, W), dev = out.shape, out.device
+    _op_check(_lib.fgd_act_load8(dev.index or 0, _dtype_of(out, "out"), R, W, *_act8(q8, "q8", torch.int8, R, W, dev),
+                                 *_act8(e8, "e8", torch.uint8, R, -(-W // ACT8_GROUP), dev), *_act8(out, "out", out.dtype, R, W, dev), _stream_on(stream, dev)))
+
+
+def fgd_swiglu8_forward(gu, h, q8, e8, stream=None) -> None:
+    """h = silu(g) * u for gu = [g | u] ([rows, 2 width]) and the checkpoint of gu: q8 int8 [rows, 2 width], e8 uint8 [rows, 2 ceil(width / 32)]."""
+    import torch
+    if h.dim() != 2:
+        raise ValueError("h must be [rows, width]")
+    (R, W), dev = h.shape, h.device
+    _op_check(_lib.fgd_swiglu8_forward(dev.index or 0, _dtype_of(h, "h"), R, W, *_act8(gu, "gu", h.dtype, R, 2 * W, dev), *_act8(h, "h", h.dtype, R, W, dev),
+                                       *_act8(q8, "q8", torch.int8, R, 2 * W, dev), *_act8(e8, "e8", torch.uint8, R, 2 * -(-W // ACT8_GROUP), dev),
+                                       _stream_on(stream, dev)))
+
+
+def fgd_swiglu8_backward(dh, q8, e8, dgu, h=None, stream=None) -> None:
+    """Gradient of :func:`fgd_swiglu8_forward` from the checkpoint alone; ``h``, where given, receives the recomputed h."""
+    import torch
+    if dh.dim() != 2:
+        raise ValueError("dh must be [rows, width]")
+    (R, W), dev = dh.shape, dh.device
+    _op_check(_lib.fgd_swiglu8_backward(dev.index or 0, _dtype_of(dh, "dh"), R, W, *_act8(dh, "dh", dh.dtype, R, W, dev),
+                                        *_act8(q8, "q8", torch.int8, R, 2 * W, dev), *_act8(e8, "e8", torch.uint8, R, 2 * -(-W // ACT8_GROUP), dev),
+                                        *_act8(dgu, "dgu", dh.dtype, R, 2 * W, dev), *_act8(h, "h", dh.dtype, R, W, dev), _stream_on(stream, dev)))
