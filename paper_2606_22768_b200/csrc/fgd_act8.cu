@@ -57,7 +57,7 @@ __device__ __forceinline__ void load8(const T* p, float (&f)[8]) {
   constexpr int N = 16 / sizeof(T);
 #pragma unroll
   for (int j = 0; j < 8; j += N) {
-    const Pack<T, N> r = load_stream<T, N>(p + j);
+    const ActPack<T, N> r = load_stream<T, N>(p + j);
 #pragma unroll
     for (int i = 0; i < N; ++i) f[j + i] = to_f32<T>(r.v[i]);
   }
@@ -67,7 +67,7 @@ __device__ __forceinline__ void store8(T* p, const float (&f)[8]) {
   constexpr int N = 16 / sizeof(T);
 #pragma unroll
   for (int j = 0; j < 8; j += N) {
-    Pack<T, N> r;
+    ActPack<T, N> r;
 #pragma unroll
     for (int i = 0; i < N; ++i) r.v[i] = from_f32<T>(f[j + i]);
     store_stream<T, N>(p + j, r);

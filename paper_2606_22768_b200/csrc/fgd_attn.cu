@@ -6,6 +6,7 @@
 #include <vector>
 
 #include "fgd_attn.h"
+#include "fgd_attn_tc.cuh"
 #include "fgd_dtype.cuh"
 #include "fgd_nvtx.h"
 
@@ -57,6 +58,15 @@ AttnArgs kernel_args(const fgd_attn_plan* plan, const fgd_attn_args* b) {
   a.hq = b->n_q_heads; a.hk = b->n_kv_heads; a.d = b->head_dim; a.scale = (float)b->scale;
   a.status = plan->status;
   return a;
+}
+
+// The tensor-core kernels read their inputs by TMA (16-byte rows) and need a positive scale (the maximum of the scores is
+// found before they are scaled; a masked score is -inf).
+bool on_tensor_cores(const fgd_attn_plan* plan, const fgd_attn_args* b, const HeadsArg* all, int n) {
+  if (!plan->encode_tiled || dtype_bytes(b->dtype) != 2 || b->head_dim % 8 != 0 || b->head_dim > 128 || !(b->scale >= 1e-20)) return false;
+  for (int i = 0; i < n; ++i)
+    if (!attn_tc_heads(heads_of(*all[i].t), plan->tokens, all[i].heads)) return false;
+  return true;
 }
 
 }  // namespace
@@ -154,7 +164,9 @@ extern "C" int fgd_attn_forward(fgd_attn_plan* plan, const fgd_attn_args* b, voi
   if (so.overlaps(sl)) return op_fail(FGD_ERR_ALIAS, "%s: o and lse overlap", who);
   DeviceScope dev(plan->device);
   if (!dev.ok()) return op_fail(FGD_ERR_CUDA, "cannot select device %d", plan->device);
-  return attn_forward_elem(plan, b->dtype, kernel_args(plan, b), static_cast<cudaStream_t>(stream));
+  const AttnArgs a = kernel_args(plan, b);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return on_tensor_cores(plan, b, all, 4) ? attn_forward_tc(plan, b->dtype, a, st) : attn_forward_elem(plan, b->dtype, a, st);
 }
 
 extern "C" int fgd_attn_backward(fgd_attn_plan* plan, const fgd_attn_args* b, void* stream) {
@@ -182,5 +194,5 @@ extern "C" int fgd_attn_backward(fgd_attn_plan* plan, const fgd_attn_args* b, vo
   const AttnArgs a = kernel_args(plan, b);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (int rc = attn_delta(b->dtype, a, st)) return rc;
-  return attn_backward_elem(plan, b->dtype, a, st);
+  return on_tensor_cores(plan, b, all, 8) ? attn_backward_tc(plan, b->dtype, a, st) : attn_backward_elem(plan, b->dtype, a, st);
 }

@@ -1,0 +1,328 @@
+// Causal attention forward on the tensor cores (mathematics: fgd_attn_elem.cu).
+//
+// A CTA (one per SM) takes two tiles of 128 query rows that read the same key head -- two query heads that share it, or
+// two neighbouring row tiles of one head -- so that every key / value tile that comes from L2 feeds 256 query rows.
+// Ten warps:
+//     0-3, 4-7  softmax of tile 0 and of tile 1: one thread per row.  It reads its 128 scores from tensor memory, keeps
+//               the running maximum and sum, and writes P (16 bit) back over the scores;
+//     8         loads: Q, then K and V tiles by TMA into a ring, from the diagonal block down to block 0;
+//     9         MMAs: S = Q K^T, O += P V.
+// Tensor memory (512 columns): S0 | S1 | O0 | O1, P over its own S.  While one tile's softmax runs, the other tile's
+// O += P V and its next S run on the tensor cores.
+//
+// The running maximum only moves O when it has grown by more than 2^8 since O was last scaled: P and the row sum use the
+// same stale maximum, so the quotient is exact, and the 16-bit P keeps its relative precision below 2^8 too.
+// Only the block on the diagonal is masked; rows of V beyond the sequence's end are zeroed in shared memory, so nothing of the
+// next sequence (0 x inf) reaches a result.
+#include "fgd_attn_tc.cuh"
+
+using namespace fgd;
+
+namespace {
+
+constexpr int kFwdThreads = 320;
+template <int DP> constexpr int kFwdStages = DP == 128 ? 4 : 8;
+constexpr float kRescale = 8.f;   // log2
+
+template <int DP>
+constexpr size_t fwd_smem() { return 1024 + (size_t)(2 + kFwdStages<DP>) * attn_tile_bytes<DP>(); }
+
+struct FwdItem {
+  int start, len, kvh, nmax;
+  int head[2], row[2], n[2];   // n: key blocks of the tile (0: no tile)
+};
+// pair_heads: heads 2 h and 2 h + 1 of one 128-row tile; otherwise rows [r, r + 256) of head h.
+__device__ __forceinline__ FwdItem fwd_item(const AttnArgs& a, int pair_heads, int per_tile, int64_t w) {
+  const int tile = (int)(w / per_tile), h = (int)(w - (int64_t)tile * per_tile);
+  const AttnTile t = a.tiles[tile];
+  FwdItem it;
+  it.start = t.start; it.len = t.len;
+  it.head[0] = pair_heads ? 2 * h : h;
+  it.head[1] = pair_heads ? 2 * h + 1 : h;
+  it.row[0] = t.row;
+  it.row[1] = pair_heads ? t.row : t.row + kAttnRows;
+  it.n[0] = t.row / kAttnRows + 1;
+  it.n[1] = it.row[1] < t.len ? it.row[1] / kAttnRows + 1 : 0;
+  it.nmax = max(it.n[0], it.n[1]);
+  it.kvh = it.head[0] / (a.hq / a.hk);
+  return it;
+}
+
+template <int DP, bool BF16>
+__global__ void __launch_bounds__(kFwdThreads, 1)
+attn_forward_tc_kernel(const AttnArgs a, int pair_heads, int per_tile, int64_t items, const __grid_constant__ CUtensorMap mq,
+                       const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv) {
+  constexpr int ST = kFwdStages<DP>;
+  constexpr uint32_t TILE = attn_tile_bytes<DP>();
+  extern __shared__ unsigned char smem_raw[];
+  // q_full, q_empty, raw, done | full[ST], empty[ST] | s_full[2], p_full[2], pv_done[2], o_free[2]
+  __shared__ __align__(8) unsigned long long bars[4 + 2 * ST + 8];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_flag;
+  unsigned char* base = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  const uint32_t sq = smem_u32(base), skv = sq + 2 * TILE;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t b0 = smem_u32(bars);
+  const uint32_t q_full = b0, q_empty = b0 + 8, raw = b0 + 16, done = b0 + 24, full = b0 + 32, empty = full + 8 * ST, s_full = empty + 8 * ST, p_full = s_full + 16,
+                 pv_done = s_full + 32, o_free = s_full + 48;
+  if (tid == 0) {
+    abort_flag = 0;
+    mbar_init(q_full, 1); mbar_init(q_empty, 1); mbar_init(raw, 1); mbar_init(done, 1);
+    for (int s = 0; s < ST; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(s_full + 8 * t, 1); mbar_init(p_full + 8 * t, 128); mbar_init(pv_done + 8 * t, 1); mbar_init(o_free + 8 * t, 128);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 9) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  const AttnWait wait{&abort_flag, a.status};
+  // tensor memory columns
+  auto s_col = [](int t) { return (uint32_t)(128 * t); };
+  auto o_col = [](int t) { return (uint32_t)(256 + 128 * t); };
+
+  if (warp == 8) {
+    // ================================================================= loads
+    uint32_t u = 0, n_raw = 0;     // ring uses, repaired tiles
+    int round = 0;
+    bool ok = true;
+    for (; ok; ++round) {
+      const int64_t w = work_item(round);
+      if ((int64_t)round * gridDim.x >= items) break;
+      if (w >= items) continue;
+      const FwdItem it = fwd_item(a, pair_heads, per_tile, w);
+      static_assert(kAttnRows == 128, "TMA boxes are 128 rows");
+      ok = wait(q_empty, (round & 1) ^ 1);
+      if (!ok) break;
+      if (lane == 0) {
+        mbar_expect_tx(q_full, it.n[1] ? 2 * TILE : TILE);
+        load_tile<DP>(sq, &mq, it.head[0], it.start + it.row[0], q_full);
+        if (it.n[1]) load_tile<DP>(sq + TILE, &mq, it.head[1], it.start + it.row[1], q_full);
+      }
+      for (int jb = it.nmax - 1; ok && jb >= 0; --jb) {
+        const int token = it.start + jb * 128, rows = it.len - jb * 128;
+        for (int v = 0; v < 2; ++v, ++u) {
+          const uint32_t s = u % ST, bar = full + 8 * s, dst = skv + s * TILE;
+          ok = wait(empty + 8 * s, ((u / ST) & 1) ^ 1);
+          if (!ok) break;
+          if (v == 0 || rows >= 128) {
+            if (lane == 0) {
+              mbar_expect_tx(bar, TILE);
+              load_tile<DP>(dst, v ? &mv : &mk, it.kvh, token, bar);
+            }
+          } else {     // the sequence ends inside this tile
+            if (lane == 0) {
+              mbar_expect_tx(raw, TILE);
+              load_tile<DP>(dst, &mv, it.kvh, token, raw);
+            }
+            ok = wait(raw, n_raw & 1);
+            ++n_raw;
+            if (!ok) { drain_wait(raw, (n_raw - 1) & 1); break; }
+            zero_rows<DP>(base + 2 * TILE + s * TILE, rows, lane);
+            if (lane == 0) mbar_arrive(bar);
+          }
+        }
+      }
+    }
+    // a CTA that gave up still waits for its own copies
+    if (wait.given_up()) {
+      const int r = round > 0 && !ok ? round : round - 1;
+      if (r >= 0) drain_wait(q_full, r & 1);
+      for (uint32_t k = u > (uint32_t)ST ? u - ST : 0; k < u; ++k) drain_wait(full + 8 * (k % ST), (k / ST) & 1);
+    }
+  } else if (warp == 9) {
+    // ================================================================= MMAs
+    uint32_t u = 0;
+    uint32_t n_p[2] = {0, 0}, n_o[2] = {0, 0};
+    bool ok = true;
+    auto score = [&](int t, uint32_t stage) {
+      if (lane == 0) {
+        mma_columns<BF16, DP>(tmem + s_col(t), sq + t * TILE, skv + stage * TILE);
+        umma_commit(s_full + 8 * t);
+      }
+    };
+    auto release = [&](uint32_t use) { if (lane == 0) umma_commit(empty + 8 * (use % ST)); };
+    auto arrived = [&](uint32_t use) { return wait(full + 8 * (use % ST), (use / ST) & 1); };
+    for (int round = 0; ok; ++round) {
+      const int64_t w = work_item(round);
+      if ((int64_t)round * gridDim.x >= items) break;
+      if (w >= items) continue;
+      const FwdItem it = fwd_item(a, pair_heads, per_tile, w);
+      if (!(ok = wait(q_full, round & 1))) break;
+      uint32_t uk = u++;
+      if (!(ok = arrived(uk))) break;
+      tc_fence_after();
+      for (int t = 0; t < 2; ++t)
+        if (it.nmax - 1 < it.n[t]) score(t, uk % ST);
+      release(uk);
+      if (it.nmax == 1 && lane == 0) umma_commit(q_empty);
+      for (int jb = it.nmax - 1; ok && jb >= 0; --jb) {
+        const uint32_t uv = u++;
+        uk = u;
+        bool k_here = false;
+        if (!(ok = arrived(uv))) break;
+        for (int t = 0; ok && t < 2; ++t) {
+          if (jb < it.n[t]) {
+            ok = wait(p_full + 8 * t, n_p[t] & 1);
+            ++n_p[t];
+            if (ok && jb == it.n[t] - 1) {      // the tile's previous output has been read
+              ok = wait(o_free + 8 * t, (n_o[t] & 1) ^ 1);
+              ++n_o[t];
+            }
+            if (!ok) break;
+            tc_fence_after();
+            if (lane == 0) {
+              mma_rows<BF16, DP>(tmem + o_col(t), tmem + s_col(t), 32, skv + (uv % ST) * TILE, jb != it.n[t] - 1);
+              umma_commit(pv_done + 8 * t);
+            }
+          }
+          if (t == 1) release(uv);
+          if (jb > 0 && jb - 1 < it.n[t]) {
+            if (!k_here && !(ok = arrived(uk))) break;
+            k_here = true;
+            tc_fence_after();
+            score(t, uk % ST);
+          }
+        }
+        if (ok && jb > 0) { release(uk); ++u; }
+        if (ok && jb == 1 && lane == 0) umma_commit(q_empty);     // the last scores of this item are on their way
+      }
+      __syncwarp();
+    }
+    // tensor memory is not released under a running MMA
+    if (lane == 0) umma_commit(done);
+    drain_wait(done, 0);
+  } else {
+    // ================================================================= softmax
+    const int t = warp >> 2, r = (warp & 3) * 32 + lane;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t ts = tmem + s_col(t) + lanes, to = tmem + o_col(t) + lanes;
+    const float c = a.scale * kLog2e;
+    uint32_t n_s = 0, n_pv = 0;
+    bool ok = true;
+    for (int round = 0; ok; ++round) {
+      const int64_t w = work_item(round);
+      if ((int64_t)round * gridDim.x >= items) break;
+      if (w >= items) continue;
+      const FwdItem it = fwd_item(a, pair_heads, per_tile, w);
+      const int n = it.n[t];
+      if (n == 0) continue;
+      float m = 0.f, l0 = 0.f, l1 = 0.f;
+      for (int jb = n - 1; jb >= 0; --jb) {
+        if (!(ok = wait(s_full + 8 * t, n_s & 1))) break;
+        ++n_s;
+        tc_fence_after();
+        uint32_t s[128];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) tmem_ld_32(ts + 32 * k, s + 32 * k);
+        tmem_ld_done<128>(s);
+        if (jb == n - 1) {     // the block on the diagonal
+#pragma unroll
+          for (int k = 0; k < 128; ++k)
+            if (k > r) s[k] = 0xFF800000u;
+        }
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int k = 0; k < 128; ++k) mx[k & 3] = fmaxf(mx[k & 3], __uint_as_float(s[k]));
+        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
+        if (jb == n - 1) {
+          m = top == -INFINITY ? 0.f : top;
+        } else if (__any_sync(0xffffffffu, top > m + kRescale)) {
+          const float mn = fmaxf(m, top), f = exp2_fast(m - mn);
+          if (!(ok = wait(pv_done + 8 * t, (n_pv - 1) & 1))) break;
+          tc_fence_after();
+#pragma unroll
+          for (int k = 0; k < DP; k += 32) {
+            uint32_t o[32];
+            tmem_ld_32(to + k, o);
+            tmem_ld_done<32>(o);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+            tmem_st_32(to + k, o);
+          }
+          l0 *= f;
+          l1 *= f;
+          m = mn;
+        }
+        // p = 2^(c s - m)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t p[32];
+#pragma unroll
+          for (int k = 0; k < 32; ++k) {
+            const float x = exp2_fast(fmaf(__uint_as_float(s[64 * h + 2 * k]), c, -m)), y = exp2_fast(fmaf(__uint_as_float(s[64 * h + 2 * k + 1]), c, -m));
+            l0 += x;
+            l1 += y;
+            p[k] = pack2<BF16>(x, y);
+          }
+          tmem_st_32(ts + 32 * h, p);
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        mbar_arrive(p_full + 8 * t);
+        ++n_pv;
+      }
+      if (!ok || !(ok = wait(pv_done + 8 * t, (n_pv - 1) & 1))) break;
+      tc_fence_after();
+      const float l = l0 + l1, f = 1.f / l;
+      const int64_t row = it.row[t] + r;
+      const bool real = row < it.len;
+      char* out = a.o.p + 2 * ((it.start + row) * a.o.token + it.head[t] * a.o.head);
+#pragma unroll
+      for (int k = 0; k < DP; k += 32) {
+        uint32_t o[32];
+        tmem_ld_32(to + k, o);
+        tmem_ld_done<32>(o);
+        if (real) store_columns<BF16, 32>(out, o, f, k, a.d);
+      }
+      tc_fence_before();
+      mbar_arrive(o_free + 8 * t);
+      if (real) a.lse[it.head[t] * a.tokens + it.start + row] = (m + log2f(l)) * kLn2;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+  }
+}
+
+template <int DP, bool BF16>
+int launch(const fgd_attn_plan* plan, AttnArgs a, cudaStream_t st) {
+  const char* who = "fgd_attn_forward";
+  const bool pair_heads = (a.hq / a.hk) % 2 == 0;
+  a.tiles = pair_heads ? plan->q_tiles : plan->q2_tiles;
+  a.n_tiles = pair_heads ? plan->n_q : plan->n_q2;
+  const int per_tile = pair_heads ? a.hq / 2 : a.hq;
+  const int64_t items = (int64_t)a.n_tiles * per_tile;
+  CUtensorMap mq, mk, mv;
+  if (!attn_tensor_map(plan->encode_tiled, &mq, BF16, a.q, a.tokens, a.hq, a.d) || !attn_tensor_map(plan->encode_tiled, &mk, BF16, a.k, a.tokens, a.hk, a.d) ||
+      !attn_tensor_map(plan->encode_tiled, &mv, BF16, a.v, a.tokens, a.hk, a.d))
+    return op_fail(FGD_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed", who);
+  auto kern = attn_forward_tc_kernel<DP, BF16>;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)fwd_smem<DP>());
+  if (e == cudaSuccess) {
+    const int sms = sm_count();
+    kern<<<(unsigned)(items < sms ? items : sms), kFwdThreads, fwd_smem<DP>(), st>>>(a, pair_heads, per_tile, items, mq, mk, mv);
+    e = cudaGetLastError();
+  }
+  return e == cudaSuccess ? FGD_OK : op_fail(FGD_ERR_CUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
+}
+
+}  // namespace
+
+namespace fgd {
+
+int attn_forward_tc(const fgd_attn_plan* plan, int dtype, const AttnArgs& a, cudaStream_t st) {
+  if (a.d <= 64) return dtype == FGD_BF16 ? launch<64, true>(plan, a, st) : launch<64, false>(plan, a, st);
+  return dtype == FGD_BF16 ? launch<128, true>(plan, a, st) : launch<128, false>(plan, a, st);
+}
+
+}  // namespace fgd

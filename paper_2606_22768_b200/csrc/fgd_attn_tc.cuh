@@ -1,0 +1,203 @@
+// What the tensor-core attention kernels share: bounded waits, TMA loads of head tiles, tensor-memory
+// access, operand descriptors and MMA issue.
+//
+// A tile is 128 rows of one head, DP (64 or 128) columns wide, zero-filled beyond the head's width.  In shared memory it
+// is one or two boxes of 128 rows x 64 columns, 128 bytes per row, written by TMA with the 128-byte swizzle.  The same
+// box serves the MMAs in both directions: with the columns as the contraction (K-major: scores, dP) and with the
+// rows as the contraction (MN-major: P V, dS K, P^T dO, dS^T Q).
+#ifndef FGD_ATTN_TC_CUH_
+#define FGD_ATTN_TC_CUH_
+
+#include <cuda.h>
+
+#include "fgd_attn.h"
+#include "fgd_dtype.cuh"
+#include "fgd_step_dense_tc.cuh"   // mbarrier, descriptor and commit helpers
+
+namespace fgd {
+
+constexpr uint32_t kAttnBox = 128 * 128;           // bytes of a 128 x 64 box of 16-bit values
+constexpr uint32_t kAttnSpin = 1u << 22;           // polls before a wait gives up
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+template <int DP>
+__host__ __device__ constexpr uint32_t attn_tile_bytes() { return kAttnBox * (DP / 64); }
+
+// A wait that ends: after kAttnSpin polls, or once another thread of the CTA has given up.  Called by whole warps; all
+// lanes get the same answer, so that a warp that gives up leaves together (tensor-memory access is warp-wide).
+struct AttnWait {
+  int* abort_flag;   // shared memory
+  int* status;       // the plan's status word
+  __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const {
+    bool here = false;
+    for (uint32_t it = 0; it < kAttnSpin && !here; ++it) {
+      uint32_t ok;
+      asm volatile(
+          "{\n\t.reg .pred p;\n\t"
+          "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+          "selp.u32 %0, 1, 0, p;\n\t}"
+          : "=r"(ok)
+          : "r"(bar), "r"(parity)
+          : "memory");
+      here = ok != 0;
+      if (!here && (it & 31u) == 31u && *(volatile int*)abort_flag) break;
+    }
+    if (__all_sync(0xffffffffu, here)) return true;
+    *(volatile int*)abort_flag = 1;
+    *(volatile int*)status = FGD_ERR_TIMEOUT;
+    return false;
+  }
+  __device__ __forceinline__ bool given_up() const { return *(volatile int*)abort_flag != 0; }
+};
+// Only for the end of a CTA that gave up: wait whatever the flag says, still bounded.
+__device__ __forceinline__ void drain_wait(uint32_t bar, uint32_t parity) { mbar_wait(bar, parity, kAttnSpin); }
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int c, int head, int token, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+      ::"r"(dst), "l"(map), "r"(c), "r"(head), "r"(token), "r"(bar)
+      : "memory");
+}
+// One tile: DP / 64 boxes, issued by one thread.
+template <int DP>
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, int head, int token, uint32_t bar) {
+#pragma unroll
+  for (int b = 0; b < DP / 64; ++b) tma_load_3d(dst + b * kAttnBox, map, b * 64, head, token, bar);
+}
+// Rows [first, 128) of a tile become zero (a row of a box is 128 contiguous bytes, the swizzle stays inside it), for the
+// asynchronous proxy to read.  One warp.
+template <int DP>
+__device__ __forceinline__ void zero_rows(unsigned char* tile, int first, int lane) {
+  for (int b = 0; b < DP / 64; ++b)
+    for (int i = first * 8 + lane; i < 128 * 8; i += 32) reinterpret_cast<uint4*>(tile + b * kAttnBox)[i] = make_uint4(0u, 0u, 0u, 0u);
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  __syncwarp();
+}
+
+// ---- tensor memory: 32 (16) columns of this thread's lane
+__device__ __forceinline__ void tmem_ld_32(uint32_t addr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, "
+      "%21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+        "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(addr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_32(uint32_t addr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, "
+      "%21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(addr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+      "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
+      "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+// Ends the loads into r[0 .. N): afterwards, and not before, the compiler may use the values.
+template <int N>
+__device__ __forceinline__ void tmem_ld_done(uint32_t* r) {
+  tmem_ld_wait();
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+r"(r[i]));
+}
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// ---- MMA issue (one thread).  M = 128 everywhere.
+template <bool BF16, int N, bool B_ROWS>   // B_ROWS: B's contraction runs over its rows (MN-major)
+__host__ __device__ constexpr uint32_t attn_idesc() {
+  return (1u << 4) | ((BF16 ? 1u : 0u) << 7) | ((BF16 ? 1u : 0u) << 10) | ((B_ROWS ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | (8u << 24);
+}
+__device__ __forceinline__ void umma_f16_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}"
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(0u)
+      : "memory");
+}
+__device__ __forceinline__ void umma_f16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %5, %5, %5}, p;\n\t}"
+      ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(0u)
+      : "memory");
+}
+// D[128 x 128] = A B^T over the tiles' columns (both K-major): 16 columns per step, 32 bytes inside a swizzled row.
+template <bool BF16, int DP>
+__device__ __forceinline__ void mma_columns(uint32_t d, uint32_t a_tile, uint32_t b_tile) {
+#pragma unroll
+  for (int k = 0; k < DP / 16; ++k) {
+    const uint32_t off = (k / 4) * kAttnBox + (k % 4) * 32;
+    umma_f16_ss(d, umma_desc(a_tile + off, 16, 1024, 2), umma_desc(b_tile + off, 16, 1024, 2), attn_idesc<BF16, 128, false>(), k > 0 ? 1u : 0u);
+  }
+}
+// D[128 x DP] (+)= A B over B's 128 rows: A is 128 x 128 16-bit values in tensor memory, packed two to a column, its
+// first 64 k at columns [a, a + 32), the others at [a + a_half, a + a_half + 32); 16 rows of B per step.
+template <bool BF16, int DP>
+__device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a, uint32_t a_half, uint32_t b_tile, bool accumulate) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    umma_f16_ts(d, a + (k / 4) * a_half + (k % 4) * 8, umma_desc(b_tile + k * 2048, kAttnBox, 1024, 2), attn_idesc<BF16, DP, true>(),
+                (accumulate || k > 0) ? 1u : 0u);
+}
+
+// ---- arithmetic
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  uint32_t r;
+  if constexpr (BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// N columns [c0, c0 + N) of one row, times f, as 16-bit values to `out` (the row's first column); columns at or beyond d are not the row's.
+template <bool BF16, int N>
+__device__ __forceinline__ void store_columns(char* out, const uint32_t* r, float f, int c0, int d) {
+#pragma unroll
+  for (int c = 0; c < N; c += 8) {
+    if (c0 + c >= d) continue;
+    uint4 w;
+    w.x = pack2<BF16>(__uint_as_float(r[c]) * f, __uint_as_float(r[c + 1]) * f);
+    w.y = pack2<BF16>(__uint_as_float(r[c + 2]) * f, __uint_as_float(r[c + 3]) * f);
+    w.z = pack2<BF16>(__uint_as_float(r[c + 4]) * f, __uint_as_float(r[c + 5]) * f);
+    w.w = pack2<BF16>(__uint_as_float(r[c + 6]) * f, __uint_as_float(r[c + 7]) * f);
+    *reinterpret_cast<uint4*>(out + 2 * (c0 + c)) = w;
+  }
+}
+
+// The order in which a persistent CTA takes the work items, which are sorted by descending work: forwards and backwards by
+// turns, so that a CTA that got a large item gets a small one next.
+__device__ __forceinline__ int64_t work_item(int round) {
+  return (int64_t)round * gridDim.x + ((round & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+}
+
+// ---- host side
+typedef CUresult (*AttnEncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// Tensor map of a [tokens, heads, d] tensor: boxes of 64 columns x 1 head x 128 tokens; columns beyond d and tokens beyond the
+// last read as zero.
+inline bool attn_tensor_map(void* encode, CUtensorMap* map, bool bf16, const AttnHeads& t, int64_t tokens, int heads, int d) {
+  const cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)heads, (cuuint64_t)tokens};
+  // the stride of an axis of one is never used, but has to be a valid one
+  const cuuint64_t strides[2] = {heads > 1 ? (cuuint64_t)t.head * 2 : (cuuint64_t)d * 2, tokens > 1 ? (cuuint64_t)t.token * 2 : (cuuint64_t)d * 2};
+  const cuuint32_t box[3] = {64, 1, 128}, estr[3] = {1, 1, 1};
+  return reinterpret_cast<AttnEncodeFn>(encode)(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, t.p, dims, strides, box, estr,
+                                                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// Can a tensor be read (and written) by the tensor-core kernels?
+inline bool attn_tc_heads(const AttnHeads& t, int64_t tokens, int heads) {
+  auto ok = [](int64_t s) { return s > 0 && s % 8 == 0 && s < ((int64_t)1 << 38); };
+  return (reinterpret_cast<uintptr_t>(t.p) & 15u) == 0 && (heads == 1 || ok(t.head)) && (tokens == 1 || ok(t.token));
+}
+
+}  // namespace fgd
+#endif

@@ -63,7 +63,7 @@ __global__ void __launch_bounds__(NT) norm_forward_kernel(const NormArgs a) {
 #pragma unroll
       for (int j = 0; j < VPT; ++j)
         if (real[j]) {
-          Pack<T, VEC> o;
+          ActPack<T, VEC> o;
 #pragma unroll
           for (int i = 0; i < VEC; ++i) o.v[i] = from_f32<T>(v[j][i]);
           store_stream<T, VEC>(reinterpret_cast<T*>(a.x_new.p) + row * a.x_new.ld + c[j], o);
@@ -82,7 +82,7 @@ __global__ void __launch_bounds__(NT) norm_forward_kernel(const NormArgs a) {
         if (real[j]) {
           float w[VEC];
           load_channel<VEC>(a.w_pre, worker, c[j], true, 1.f, w);
-          Pack<T, VEC> o;
+          ActPack<T, VEC> o;
 #pragma unroll
           for (int i = 0; i < VEC; ++i) o.v[i] = from_f32<T>(v[j][i] * rx * w[i]);
           store_stream<T, VEC>(reinterpret_cast<T*>(a.n.p) + row * a.n.ld + c[j], o);
@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(NT) norm_backward_kernel(const NormArgs a) {
       load_channel<VEC>(a.w_pre, worker, c[j], true, 1.f, wn);
       load_channel<VEC>(a.w_post, worker, c[j], true, 1.f, wp);
       if (a.gate_kind == GATE_ROW) load_channel<VEC>(a.gate, worker, c[j], true, 1.f, gr);
-      Pack<T, VEC> ox, oy, og;
+      ActPack<T, VEC> ox, oy, og;
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
         const float xv = x[j][i], yv = y[j][i], nv = n[j][i];

@@ -44,7 +44,7 @@ struct NormArgs {
 
 template <typename T, int VEC>
 struct RowVec {
-  Pack<T, VEC> r;
+  ActPack<T, VEC> r;
   __device__ __forceinline__ void load(const NormMat& m, int64_t row, int c, bool real) {
     if (real) r = load_stream<T, VEC>(reinterpret_cast<const T*>(m.p) + row * m.ld + c);
     else {

@@ -26,13 +26,13 @@ template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return
 
 // N consecutive activations as they lie in memory; 16 bytes (or one element on the element-wise paths).
 template <typename T, int N>
-struct alignas(sizeof(T) * N) Pack {
+struct alignas(sizeof(T) * N) ActPack {
   T v[N];
 };
 // Streaming access: activations are read once and written once per call, so they leave L1 alone.
 template <typename T, int N>
-__device__ __forceinline__ Pack<T, N> load_stream(const T* p) {
-  Pack<T, N> r;
+__device__ __forceinline__ ActPack<T, N> load_stream(const T* p) {
+  ActPack<T, N> r;
   if constexpr (sizeof(T) * N == 16) {
     *reinterpret_cast<uint4*>(&r) = __ldcs(reinterpret_cast<const uint4*>(p));
   } else {
@@ -42,7 +42,7 @@ __device__ __forceinline__ Pack<T, N> load_stream(const T* p) {
   return r;
 }
 template <typename T, int N>
-__device__ __forceinline__ void store_stream(T* p, const Pack<T, N>& r) {
+__device__ __forceinline__ void store_stream(T* p, const ActPack<T, N>& r) {
   if constexpr (sizeof(T) * N == 16) {
     __stcs(reinterpret_cast<uint4*>(p), *reinterpret_cast<const uint4*>(&r));
   } else {
