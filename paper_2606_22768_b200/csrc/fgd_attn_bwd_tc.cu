@@ -88,7 +88,7 @@ attn_dq_tc_kernel(const AttnArgs a, int64_t items, const __grid_constant__ CUten
       int head, n;
       item(w, t, head, n);
       if (!(ok = wait(q_empty, (round & 1) ^ 1))) break;
-      if (lane == 0) {
+      if (elect_one()) {
         mbar_expect_tx(q_full, 2 * TILE);
         load_tile<DP>(sq, &mq, head, t.start + t.row, q_full);
         load_tile<DP>(sdo, &mdo, head, t.start + t.row, q_full);
@@ -98,12 +98,12 @@ attn_dq_tc_kernel(const AttnArgs a, int64_t items, const __grid_constant__ CUten
         const uint32_t ik = u % SK, iv = u % SV, kb = k_full + 8 * ik, vb = v_full + 8 * iv;
         if (!(ok = wait(k_empty + 8 * ik, ((u / SK) & 1) ^ 1))) break;
         if (rows >= 128) {
-          if (lane == 0) {
+          if (elect_one()) {
             mbar_expect_tx(kb, TILE);
             load_tile<DP>(sk + ik * TILE, &mk, head / group, token, kb);
           }
         } else {     // dQ = dS K must not meet the next sequence's keys
-          if (lane == 0) {
+          if (elect_one()) {
             mbar_expect_tx(raw, TILE);
             load_tile<DP>(sk + ik * TILE, &mk, head / group, token, raw);
           }
@@ -111,10 +111,10 @@ attn_dq_tc_kernel(const AttnArgs a, int64_t items, const __grid_constant__ CUten
           ++n_raw;
           if (!ok) { drain_wait(raw, (n_raw - 1) & 1); break; }
           zero_rows<DP>(base + 2 * TILE + ik * TILE, rows, lane);
-          if (lane == 0) mbar_arrive(kb);
+          if (elect_one()) mbar_arrive(kb);
         }
         if (!(ok = wait(v_empty + 8 * iv, ((u / SV) & 1) ^ 1))) break;
-        if (lane == 0) {
+        if (elect_one()) {
           mbar_expect_tx(vb, TILE);
           load_tile<DP>(sv + iv * TILE, &mv, head / group, token, vb);
         }
@@ -134,7 +134,7 @@ attn_dq_tc_kernel(const AttnArgs a, int64_t items, const __grid_constant__ CUten
     auto score = [&](uint32_t k) {      // S of block k into buffer k & 1
       if (!wait(k_full + 8 * (k % SK), (k / SK) & 1)) return false;
       tc_fence_after();
-      if (lane == 0) {
+      if (elect_one()) {
         mma_columns<BF16, DP>(tmem + 128 * (k & 1), sq, sk + (k % SK) * TILE);
         umma_commit(s_full + 8 * (k & 1));
       }
@@ -143,7 +143,7 @@ attn_dq_tc_kernel(const AttnArgs a, int64_t items, const __grid_constant__ CUten
     auto dprob = [&](uint32_t k) {
       if (!wait(v_full + 8 * (k % SV), (k / SV) & 1)) return false;
       tc_fence_after();
-      if (lane == 0) {
+      if (elect_one()) {
         mma_columns<BF16, DP>(tmem + c_dp, sdo, sv + (k % SV) * TILE);
         umma_commit(dp_full);
         umma_commit(v_empty + 8 * (k % SV));
@@ -160,24 +160,24 @@ attn_dq_tc_kernel(const AttnArgs a, int64_t items, const __grid_constant__ CUten
       item(w, t, head, n);
       if (!(ok = wait(q_full, round & 1))) break;
       if (!(ok = score(u) && dprob(u) && (n == 1 || score(u + 1)))) break;
-      if (n == 1 && lane == 0) umma_commit(q_empty);
+      if (n == 1 && elect_one()) umma_commit(q_empty);
       for (int i = 0; i < n; ++i, ++u) {
         if (!(ok = wait(ds_full, n_ds & 1))) break;
         ++n_ds;
         if (i == 0 && !(ok = wait(dq_free, (done_items & 1) ^ 1))) break;
         tc_fence_after();
-        if (lane == 0) {
+        if (elect_one()) {
           mma_rows<BF16, DP>(tmem + c_dq, tmem + c_dp, 64, sk + (u % SK) * TILE, i > 0);
           if (i == n - 1) umma_commit(dq_done);
           umma_commit(k_empty + 8 * (u % SK));
         }
         if (i + 1 < n && !(ok = dprob(u + 1))) break;
         if (i + 2 < n && !(ok = score(u + 2))) break;
-        if (i + 2 == n && lane == 0) umma_commit(q_empty);      // the item's last product with Q and dO is on its way
+        if (i + 2 == n && elect_one()) umma_commit(q_empty);      // the item's last product with Q and dO is on its way
       }
       ++done_items;
     }
-    if (lane == 0) umma_commit(done);
+    if (elect_one()) umma_commit(done);
     drain_wait(done, 0);
   } else {
     // ================================================================= P, dS, and dQ's way out
@@ -309,13 +309,13 @@ attn_dkv_tc_kernel(const AttnArgs a, int64_t items, const __grid_constant__ CUte
     // one tile of queries or output gradients; rows beyond the sequence become zero (P^T dO and dS^T Q run over them)
     auto rows_tile = [&](const CUtensorMap* map, uint32_t tile, uint32_t bar, int head, int token, int rows) {
       if (rows >= 128) {
-        if (lane == 0) {
+        if (elect_one()) {
           mbar_expect_tx(bar, TILE);
           load_tile<DP>(sk + tile * TILE, map, head, token, bar);
         }
         return true;
       }
-      if (lane == 0) {
+      if (elect_one()) {
         mbar_expect_tx(raw, TILE);
         load_tile<DP>(sk + tile * TILE, map, head, token, raw);
       }
@@ -323,7 +323,7 @@ attn_dkv_tc_kernel(const AttnArgs a, int64_t items, const __grid_constant__ CUte
       ++n_raw;
       if (!here) { drain_wait(raw, (n_raw - 1) & 1); return false; }
       zero_rows<DP>(base + tile * TILE, rows, lane);
-      if (lane == 0) mbar_arrive(bar);
+      if (elect_one()) mbar_arrive(bar);
       return true;
     };
     for (; ok; ++round) {
@@ -334,7 +334,7 @@ attn_dkv_tc_kernel(const AttnArgs a, int64_t items, const __grid_constant__ CUte
       int kvh, first, per_head;
       item(w, t, kvh, first, per_head);
       if (!(ok = wait(kv_empty, (round & 1) ^ 1))) break;
-      if (lane == 0) {
+      if (elect_one()) {
         mbar_expect_tx(kv_full, 2 * TILE);
         load_tile<DP>(sk, &mk, kvh, t.start + t.row, kv_full);
         load_tile<DP>(sv, &mv, kvh, t.start + t.row, kv_full);
@@ -373,7 +373,7 @@ attn_dkv_tc_kernel(const AttnArgs a, int64_t items, const __grid_constant__ CUte
     auto score = [&](uint32_t k) {
       if (!wait(q_full + 8 * (k & 1), (k >> 1) & 1)) return false;
       tc_fence_after();
-      if (lane == 0) {
+      if (elect_one()) {
         mma_columns<BF16, DP>(tmem + c_s, sk, sq + (k & 1) * TILE);
         umma_commit(s_full);
       }
@@ -382,7 +382,7 @@ attn_dkv_tc_kernel(const AttnArgs a, int64_t items, const __grid_constant__ CUte
     auto dprob = [&](uint32_t k) {
       if (!wait(do_full + 8 * (k & 1), (k >> 1) & 1)) return false;
       tc_fence_after();
-      if (lane == 0) {
+      if (elect_one()) {
         mma_columns<BF16, DP>(tmem + c_dp, sv, sdo + (k & 1) * TILE);
         umma_commit(dp_full);
       }
@@ -402,14 +402,14 @@ attn_dkv_tc_kernel(const AttnArgs a, int64_t items, const __grid_constant__ CUte
         if (!(ok = wait(p_full, u & 1))) break;
         if (i == 0 && !(ok = wait(out_free, (n_items & 1) ^ 1))) break;
         tc_fence_after();
-        if (lane == 0) {
+        if (elect_one()) {
           mma_rows<BF16, DP>(tmem + c_dv, tmem + c_s, 64, sdo + (u & 1) * TILE, i > 0);
           umma_commit(do_empty + 8 * (u & 1));
         }
         if (i + 1 < n && !(ok = score(u + 1))) break;
         if (!(ok = wait(ds_full, u & 1))) break;
         tc_fence_after();
-        if (lane == 0) {
+        if (elect_one()) {
           mma_rows<BF16, DP>(tmem + c_dk, tmem + c_dp, 64, sq + (u & 1) * TILE, i > 0);
           umma_commit(q_empty + 8 * (u & 1));
           if (i == n - 1) { umma_commit(out_done); umma_commit(kv_empty); }
@@ -418,7 +418,7 @@ attn_dkv_tc_kernel(const AttnArgs a, int64_t items, const __grid_constant__ CUte
       }
       ++n_items;
     }
-    if (lane == 0) umma_commit(done);
+    if (elect_one()) umma_commit(done);
     drain_wait(done, 0);
   } else {
     // ================================================================= P^T, dS^T, and the gradients' way out

@@ -55,22 +55,23 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, int per_tile, int64_t i
   constexpr int ST = kFwdStages<DP>;
   constexpr uint32_t TILE = attn_tile_bytes<DP>();
   extern __shared__ unsigned char smem_raw[];
-  // q_full, q_empty, raw, done | full[ST], empty[ST] | s_full[2], p_full[2], pv_done[2], o_free[2]
-  __shared__ __align__(8) unsigned long long bars[4 + 2 * ST + 8];
+  // q_full, q_empty, raw, done | full[ST], empty[ST] | s_full[2], pv_done[2], o_free[2], p_full[2][2]
+  __shared__ __align__(8) unsigned long long bars[4 + 2 * ST + 10];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
   unsigned char* base = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   const uint32_t sq = smem_u32(base), skv = sq + 2 * TILE;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t b0 = smem_u32(bars);
-  const uint32_t q_full = b0, q_empty = b0 + 8, raw = b0 + 16, done = b0 + 24, full = b0 + 32, empty = full + 8 * ST, s_full = empty + 8 * ST, p_full = s_full + 16,
-                 pv_done = s_full + 32, o_free = s_full + 48;
+  const uint32_t q_full = b0, q_empty = b0 + 8, raw = b0 + 16, done = b0 + 24, full = b0 + 32, empty = full + 8 * ST, s_full = empty + 8 * ST,
+                 pv_done = s_full + 16, o_free = s_full + 32, p_full = s_full + 48;   // p_full + 16 t + 8 half: 64 columns of P each
   if (tid == 0) {
     abort_flag = 0;
     mbar_init(q_full, 1); mbar_init(q_empty, 1); mbar_init(raw, 1); mbar_init(done, 1);
     for (int s = 0; s < ST; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
     for (int t = 0; t < 2; ++t) {
-      mbar_init(s_full + 8 * t, 1); mbar_init(p_full + 8 * t, 128); mbar_init(pv_done + 8 * t, 1); mbar_init(o_free + 8 * t, 128);
+      mbar_init(s_full + 8 * t, 1); mbar_init(pv_done + 8 * t, 1); mbar_init(o_free + 8 * t, 128);
+      mbar_init(p_full + 16 * t, 128); mbar_init(p_full + 16 * t + 8, 128);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -100,7 +101,7 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, int per_tile, int64_t i
       static_assert(kAttnRows == 128, "TMA boxes are 128 rows");
       ok = wait(q_empty, (round & 1) ^ 1);
       if (!ok) break;
-      if (lane == 0) {
+      if (elect_one()) {
         mbar_expect_tx(q_full, it.n[1] ? 2 * TILE : TILE);
         load_tile<DP>(sq, &mq, it.head[0], it.start + it.row[0], q_full);
         if (it.n[1]) load_tile<DP>(sq + TILE, &mq, it.head[1], it.start + it.row[1], q_full);
@@ -112,12 +113,12 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, int per_tile, int64_t i
           ok = wait(empty + 8 * s, ((u / ST) & 1) ^ 1);
           if (!ok) break;
           if (v == 0 || rows >= 128) {
-            if (lane == 0) {
+            if (elect_one()) {
               mbar_expect_tx(bar, TILE);
               load_tile<DP>(dst, v ? &mv : &mk, it.kvh, token, bar);
             }
           } else {     // the sequence ends inside this tile
-            if (lane == 0) {
+            if (elect_one()) {
               mbar_expect_tx(raw, TILE);
               load_tile<DP>(dst, &mv, it.kvh, token, raw);
             }
@@ -125,7 +126,7 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, int per_tile, int64_t i
             ++n_raw;
             if (!ok) { drain_wait(raw, (n_raw - 1) & 1); break; }
             zero_rows<DP>(base + 2 * TILE + s * TILE, rows, lane);
-            if (lane == 0) mbar_arrive(bar);
+            if (elect_one()) mbar_arrive(bar);
           }
         }
       }
@@ -142,12 +143,12 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, int per_tile, int64_t i
     uint32_t n_p[2] = {0, 0}, n_o[2] = {0, 0};
     bool ok = true;
     auto score = [&](int t, uint32_t stage) {
-      if (lane == 0) {
+      if (elect_one()) {
         mma_columns<BF16, DP>(tmem + s_col(t), sq + t * TILE, skv + stage * TILE);
         umma_commit(s_full + 8 * t);
       }
     };
-    auto release = [&](uint32_t use) { if (lane == 0) umma_commit(empty + 8 * (use % ST)); };
+    auto release = [&](uint32_t use) { if (elect_one()) umma_commit(empty + 8 * (use % ST)); };
     auto arrived = [&](uint32_t use) { return wait(full + 8 * (use % ST), (use / ST) & 1); };
     for (int round = 0; ok; ++round) {
       const int64_t w = work_item(round);
@@ -161,7 +162,7 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, int per_tile, int64_t i
       for (int t = 0; t < 2; ++t)
         if (it.nmax - 1 < it.n[t]) score(t, uk % ST);
       release(uk);
-      if (it.nmax == 1 && lane == 0) umma_commit(q_empty);
+      if (it.nmax == 1 && elect_one()) umma_commit(q_empty);
       for (int jb = it.nmax - 1; ok && jb >= 0; --jb) {
         const uint32_t uv = u++;
         uk = u;
@@ -169,18 +170,20 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, int per_tile, int64_t i
         if (!(ok = arrived(uv))) break;
         for (int t = 0; ok && t < 2; ++t) {
           if (jb < it.n[t]) {
-            ok = wait(p_full + 8 * t, n_p[t] & 1);
+            const bool first = jb == it.n[t] - 1;
+            for (int half = 0; ok && half < 2; ++half) {
+              ok = wait(p_full + 16 * t + 8 * half, n_p[t] & 1);
+              if (ok && first && half == 0) {      // the tile's previous output has been read
+                ok = wait(o_free + 8 * t, (n_o[t] & 1) ^ 1);
+                ++n_o[t];
+              }
+              if (!ok) break;
+              tc_fence_after();
+              if (elect_one()) mma_half_rows<BF16, DP>(tmem + o_col(t), tmem + s_col(t) + 32 * half, skv + (uv % ST) * TILE, half, !first || half == 1);
+            }
             ++n_p[t];
-            if (ok && jb == it.n[t] - 1) {      // the tile's previous output has been read
-              ok = wait(o_free + 8 * t, (n_o[t] & 1) ^ 1);
-              ++n_o[t];
-            }
             if (!ok) break;
-            tc_fence_after();
-            if (lane == 0) {
-              mma_rows<BF16, DP>(tmem + o_col(t), tmem + s_col(t), 32, skv + (uv % ST) * TILE, jb != it.n[t] - 1);
-              umma_commit(pv_done + 8 * t);
-            }
+            if (elect_one()) umma_commit(pv_done + 8 * t);
           }
           if (t == 1) release(uv);
           if (jb > 0 && jb - 1 < it.n[t]) {
@@ -191,12 +194,12 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, int per_tile, int64_t i
           }
         }
         if (ok && jb > 0) { release(uk); ++u; }
-        if (ok && jb == 1 && lane == 0) umma_commit(q_empty);     // the last scores of this item are on their way
+        if (ok && jb == 1 && elect_one()) umma_commit(q_empty);     // the last scores of this item are on their way
       }
       __syncwarp();
     }
     // tensor memory is not released under a running MMA
-    if (lane == 0) umma_commit(done);
+    if (elect_one()) umma_commit(done);
     drain_wait(done, 0);
   } else {
     // ================================================================= softmax
@@ -213,64 +216,78 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, int per_tile, int64_t i
       const FwdItem it = fwd_item(a, pair_heads, per_tile, w);
       const int n = it.n[t];
       if (n == 0) continue;
-      float m = 0.f, l0 = 0.f, l1 = 0.f;
+      float m = 0.f;
+      float2 l = make_float2(0.f, 0.f);
       for (int jb = n - 1; jb >= 0; --jb) {
         if (!(ok = wait(s_full + 8 * t, n_s & 1))) break;
         ++n_s;
         tc_fence_after();
         uint32_t s[128];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) tmem_ld_32(ts + 32 * k, s + 32 * k);
-        tmem_ld_done<128>(s);
-        if (jb == n - 1) {     // the block on the diagonal
-#pragma unroll
-          for (int k = 0; k < 128; ++k)
-            if (k > r) s[k] = 0xFF800000u;
-        }
+        tmem_ld_32(ts, s);
+        tmem_ld_32(ts + 32, s + 32);
+        tmem_ld_done<64>(s);
+        tmem_ld_32(ts + 64, s + 64);          // on their way while the first half's maximum is found
+        tmem_ld_32(ts + 96, s + 96);
+        const bool diagonal = jb == n - 1;
         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        auto half_max = [&](int from) {
+          if (diagonal) {
 #pragma unroll
-        for (int k = 0; k < 128; ++k) mx[k & 3] = fmaxf(mx[k & 3], __uint_as_float(s[k]));
-        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
-        if (jb == n - 1) {
+            for (int k = 0; k < 64; ++k)
+              if (from + k > r) s[from + k] = 0xFF800000u;
+          }
+#pragma unroll
+          for (int k = 0; k < 64; k += 2) mx[(k >> 1) & 3] = max3(mx[(k >> 1) & 3], __uint_as_float(s[from + k]), __uint_as_float(s[from + k + 1]));
+        };
+        half_max(0);
+        tmem_ld_done<64>(s + 64);
+        half_max(64);
+        const float top = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * c;
+        if (diagonal) {
           m = top == -INFINITY ? 0.f : top;
         } else if (__any_sync(0xffffffffu, top > m + kRescale)) {
           const float mn = fmaxf(m, top), f = exp2_fast(m - mn);
           if (!(ok = wait(pv_done + 8 * t, (n_pv - 1) & 1))) break;
           tc_fence_after();
 #pragma unroll
-          for (int k = 0; k < DP; k += 32) {
-            uint32_t o[32];
-            tmem_ld_32(to + k, o);
-            tmem_ld_done<32>(o);
+          for (int k = 0; k < DP; k += 16) {
+            uint32_t o[16];
+            tmem_ld_8(to + k, reinterpret_cast<float*>(o));
+            tmem_ld_8(to + k + 8, reinterpret_cast<float*>(o + 8));
+            tmem_ld_done<16>(o);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-            tmem_st_32(to + k, o);
+            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+            tmem_st_16(to + k, o);
           }
-          l0 *= f;
-          l1 *= f;
+          l.x *= f;
+          l.y *= f;
           m = mn;
         }
-        // p = 2^(c s - m)
+        // p = 2^(c s - m), 32 columns at a time
+        const float2 c2 = make_float2(c, c), m2 = make_float2(-m, -m);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t p[32];
+        for (int q = 0; q < 4; ++q) {
+          uint32_t p[16];
 #pragma unroll
-          for (int k = 0; k < 32; ++k) {
-            const float x = exp2_fast(fmaf(__uint_as_float(s[64 * h + 2 * k]), c, -m)), y = exp2_fast(fmaf(__uint_as_float(s[64 * h + 2 * k + 1]), c, -m));
-            l0 += x;
-            l1 += y;
-            p[k] = pack2<BF16>(x, y);
+          for (int k = 0; k < 16; ++k) {
+            float2 x = fma2(two(s + 32 * q + 2 * k), c2, m2);
+            x.x = exp2_fast(x.x);
+            x.y = exp2_fast(x.y);
+            l = add2(l, x);
+            p[k] = pack2<BF16>(x.x, x.y);
           }
-          tmem_st_32(ts + 32 * h, p);
+          tmem_st_16(ts + 16 * q, p);
+          if (q & 1) {                        // half of P: its product can start
+            tmem_st_wait();
+            tc_fence_before();
+            mbar_arrive(p_full + 16 * t + 8 * (q >> 1));
+          }
         }
-        tmem_st_wait();
-        tc_fence_before();
-        mbar_arrive(p_full + 8 * t);
         ++n_pv;
       }
       if (!ok || !(ok = wait(pv_done + 8 * t, (n_pv - 1) & 1))) break;
       tc_fence_after();
-      const float l = l0 + l1, f = 1.f / l;
+      const float sum = l.x + l.y, f = 1.f / sum;
       const int64_t row = it.row[t] + r;
       const bool real = row < it.len;
       char* out = a.o.p + 2 * ((it.start + row) * a.o.token + it.head[t] * a.o.head);
@@ -283,7 +300,7 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, int per_tile, int64_t i
       }
       tc_fence_before();
       mbar_arrive(o_free + 8 * t);
-      if (real) a.lse[it.head[t] * a.tokens + it.start + row] = (m + log2f(l)) * kLn2;
+      if (real) a.lse[it.head[t] * a.tokens + it.start + row] = (m + log2f(sum)) * kLn2;
     }
   }
   tc_fence_before();

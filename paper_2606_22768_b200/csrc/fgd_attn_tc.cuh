@@ -94,6 +94,13 @@ __device__ __forceinline__ void tmem_st_32(uint32_t addr, const uint32_t* r) {
       "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
       : "memory");
 }
+__device__ __forceinline__ void tmem_st_16(uint32_t addr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(addr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+      "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
 // Ends the loads into r[0 .. N): afterwards, and not before, the compiler may use the values.
 template <int N>
 __device__ __forceinline__ void tmem_ld_done(uint32_t* r) {
@@ -109,39 +116,58 @@ template <bool BF16, int N, bool B_ROWS>   // B_ROWS: B's contraction runs over 
 __host__ __device__ constexpr uint32_t attn_idesc() {
   return (1u << 4) | ((BF16 ? 1u : 0u) << 7) | ((BF16 ? 1u : 0u) << 10) | ((B_ROWS ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | (8u << 24);
 }
-__device__ __forceinline__ void umma_f16_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+// One lane of a converged warp.  (A branch on this tells the compiler that a single thread issues, and so that the operands are
+// uniform; behind `lane == 0` it guards every MMA and copy against operands that differ between lanes.)
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0;
+}
+// Low word of the matrix descriptor (address and leading offset in 16-byte units); the high word is a constant: 1024 bytes between
+// groups of eight rows, descriptor version, 128-byte swizzle.  Steps along the contraction add to the address alone.
+__device__ __forceinline__ uint32_t desc_low(uint32_t tile, uint32_t lead) { return ((tile >> 4) & 0x3FFFu) | ((lead >> 4) << 16); }
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ void umma_f16_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
+      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+      "mov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}"
-      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(0u)
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}"
+      ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "n"(kDescHigh)
       : "memory");
 }
-__device__ __forceinline__ void umma_f16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ void umma_f16_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
+      "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\t"
+      "mov.b64 db, {%2, %5};\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %5, %5, %5}, p;\n\t}"
-      ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(0u)
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
+      ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "n"(kDescHigh)
       : "memory");
 }
 // D[128 x 128] = A B^T over the tiles' columns (both K-major): 16 columns per step, 32 bytes inside a swizzled row.
 template <bool BF16, int DP>
 __device__ __forceinline__ void mma_columns(uint32_t d, uint32_t a_tile, uint32_t b_tile) {
+  const uint32_t a = desc_low(a_tile, 16), b = desc_low(b_tile, 16);
 #pragma unroll
   for (int k = 0; k < DP / 16; ++k) {
-    const uint32_t off = (k / 4) * kAttnBox + (k % 4) * 32;
-    umma_f16_ss(d, umma_desc(a_tile + off, 16, 1024, 2), umma_desc(b_tile + off, 16, 1024, 2), attn_idesc<BF16, 128, false>(), k > 0 ? 1u : 0u);
+    const uint32_t off = ((k / 4) * kAttnBox + (k % 4) * 32) >> 4;
+    umma_f16_ss(d, a + off, b + off, attn_idesc<BF16, 128, false>(), k > 0 ? 1u : 0u);
   }
 }
-// D[128 x DP] (+)= A B over B's 128 rows: A is 128 x 128 16-bit values in tensor memory, packed two to a column, its
-// first 64 k at columns [a, a + 32), the others at [a + a_half, a + a_half + 32); 16 rows of B per step.
+// D[128 x DP] (+)= A B over 64 of B's 128 rows (half 0 or 1): A's 64 columns are 16-bit values in tensor memory, packed two
+// to a column, at [a, a + 32); 16 rows of B per step.
+template <bool BF16, int DP>
+__device__ __forceinline__ void mma_half_rows(uint32_t d, uint32_t a, uint32_t b_tile, int half, bool accumulate) {
+  const uint32_t b = desc_low(b_tile, kAttnBox) + half * (64 * 128 >> 4);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) umma_f16_ts(d, a + k * 8, b + k * (2048 >> 4), attn_idesc<BF16, DP, true>(), (accumulate || k > 0) ? 1u : 0u);
+}
+// All 128 rows: A's second half stands `a_half` columns after the first.
 template <bool BF16, int DP>
 __device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a, uint32_t a_half, uint32_t b_tile, bool accumulate) {
-#pragma unroll
-  for (int k = 0; k < 8; ++k)
-    umma_f16_ts(d, a + (k / 4) * a_half + (k % 4) * 8, umma_desc(b_tile + k * 2048, kAttnBox, 1024, 2), attn_idesc<BF16, DP, true>(),
-                (accumulate || k > 0) ? 1u : 0u);
+  mma_half_rows<BF16, DP>(d, a, b_tile, 0, accumulate);
+  mma_half_rows<BF16, DP>(d, a + a_half, b_tile, 1, true);
 }
 
 // ---- arithmetic
@@ -150,6 +176,34 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// Two fp32 operations per instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\tfma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ float2 two(const uint32_t* r) { return make_float2(__uint_as_float(r[0]), __uint_as_float(r[1])); }
 template <bool BF16>
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   uint32_t r;
