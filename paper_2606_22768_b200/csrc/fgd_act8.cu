@@ -57,9 +57,9 @@ __device__ __forceinline__ void load8(const T* p, float (&f)[8]) {
   constexpr int N = 16 / sizeof(T);
 #pragma unroll
   for (int j = 0; j < 8; j += N) {
-    const ActPack<T, N> r = load_stream<T, N>(p + j);
+    const Vals<N> r = unpack<T, N>(load_stream<T, N>(p + j));
 #pragma unroll
-    for (int i = 0; i < N; ++i) f[j + i] = to_f32<T>(r.v[i]);
+    for (int i = 0; i < N; ++i) f[j + i] = r.v[i];
   }
 }
 template <typename T>
@@ -67,10 +67,10 @@ __device__ __forceinline__ void store8(T* p, const float (&f)[8]) {
   constexpr int N = 16 / sizeof(T);
 #pragma unroll
   for (int j = 0; j < 8; j += N) {
-    ActPack<T, N> r;
+    Vals<N> r;
 #pragma unroll
-    for (int i = 0; i < N; ++i) r.v[i] = from_f32<T>(f[j + i]);
-    store_stream<T, N>(p + j, r);
+    for (int i = 0; i < N; ++i) r.v[i] = f[j + i];
+    store_stream<T, N>(p + j, round_to<T, N>(r));
   }
 }
 __device__ __forceinline__ uint2 quantise8(const float (&f)[8], float inv) {

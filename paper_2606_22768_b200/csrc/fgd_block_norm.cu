@@ -6,179 +6,182 @@ using namespace fgd;
 
 namespace {
 
-template <typename T, int VEC, int NT, int VPT>
-__global__ void __launch_bounds__(NT) norm_forward_kernel(const NormArgs a) {
-  __shared__ float buf[2][1][NT / 32 > 0 ? NT / 32 : 1];
-  const int64_t worker = blockIdx.x / a.ctas, row0 = worker * a.rows, end = row0 + a.rows;
-  int64_t row = row0 + blockIdx.x % a.ctas;
-  const bool has_y = a.y.p != nullptr, full = a.gate_kind == GATE_FULL, post = a.w_post.p != nullptr;
+// A thread with at most 8 elements of a row keeps the per-channel factors in registers for all its rows; with more it reads them again
+// (from L1) in every row.  Arithmetic runs on pairs of fp32 values: with 16-bit activations a scalar version is bound by its
+// instructions, not by HBM.
+template <typename T, int VEC, int NT, int VPT, int STAGES, bool FULL>
+__global__ void __launch_bounds__(NT, NT * VPT <= 1024 ? 1024 / NT > 16 ? 16 : 1024 / NT : 1) norm_forward_kernel(const NormArgs a) {
+  constexpr bool HOLD = VEC * VPT <= 8;
+  constexpr int P = pairs_of<VEC>;
+  enum { X, Y, G, N = FULL ? 3 : 2 };
+  extern __shared__ __align__(16) unsigned char ring[];
+  __shared__ __align__(16) float buf[2][1][NT / 32];
+  const int64_t worker = blockIdx.x / a.ctas, row0 = worker * a.rows, end = row0 + a.rows, first = row0 + blockIdx.x % a.ctas;
+  const bool post = a.w_post.p != nullptr;
+  NormMat in[N] = {a.x, a.y};
+  if constexpr (FULL) in[G] = a.gate;
   int c[VPT];
-  bool real[VPT];
 #pragma unroll
-  for (int j = 0; j < VPT; ++j) { c[j] = (threadIdx.x + j * NT) * VEC; real[j] = c[j] < a.width; }
-  RowVec<T, VEC> x[VPT], y[VPT], g[VPT];
-  auto fetch = [&](int64_t r) {
-#pragma unroll
-    for (int j = 0; j < VPT; ++j) {
-      x[j].load(a.x, r, c[j], real[j]);
-      if (has_y) y[j].load(a.y, r, c[j], real[j]);
-      if (full) g[j].load(a.gate, r, c[j], real[j]);
-    }
-  };
-  if (row < end) fetch(row);
-  for (int slot = 0; row < end; row += a.ctas) {
-    float v[VPT][VEC], ss[1] = {0.f};
-    if (has_y) {
-      float ry = 1.f;
-      if (post) {
-#pragma unroll
-        for (int j = 0; j < VPT; ++j)
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) ss[0] = fmaf(y[j][i], y[j][i], ss[0]);
-        cta_sum<1, NT>(ss, buf, slot); slot ^= 1;
-        ry = rsqrtf(fmaf(ss[0], a.inv_width, a.eps));
-      }
-      ry *= a.scale;
+  for (int j = 0; j < VPT; ++j) c[j] = (threadIdx.x + j * NT) * VEC;
+  Vals<VEC> wt[VPT], wn[VPT];
+  if constexpr (HOLD) {
+    post_factors<VEC, VPT>(a, worker, c, wt);
+    load_channel<VEC, VPT>(a.w_pre, worker, c, a.width, wn);
+  }
+  RowFeed<T, VEC, NT, VPT, N, STAGES> feed;
+  feed.start(in, a.width, ring, first, a.ctas, end);
+  int slot = 0;
+  for (int64_t row = first; row < end; row += a.ctas) {
+    feed.next(in, row, a.ctas, end, row == first);
+    Vals<VEC> v[VPT];
+    float ss[1], ry = 1.f;
+    float2 sum = both(0.f);
+    if (post) {
 #pragma unroll
       for (int j = 0; j < VPT; ++j) {
-        float w[VEC], gr[VEC];
-        load_channel<VEC>(a.w_post, worker, c[j], real[j], 1.f, w);
-        if (a.gate_kind == GATE_ROW) load_channel<VEC>(a.gate, worker, c[j], real[j], 1.f, gr);
+        const Vals<VEC> y = feed.get(Y, j);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          float u = y[j][i] * ry * w[i];
-          if (full) u *= g[j][i];
-          else if (a.gate_kind == GATE_ROW) u *= gr[i];
-          v[j][i] = x[j][i] + u;
-        }
+        for (int i = 0; i < P; ++i) sum = fma2(get2(y, i), get2(y, i), sum);
       }
-    } else {
-#pragma unroll
-      for (int j = 0; j < VPT; ++j)
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) v[j][i] = x[j][i];
+      ss[0] = sum.x + sum.y;
+      cta_sum<1, NT>(ss, buf, slot); slot ^= 1;
+      ry = rsqrtf(fmaf(ss[0], a.inv_width, a.eps));
     }
-    if (row + a.ctas < end) fetch(row + a.ctas);
-    if (a.x_new.p) {
+    if constexpr (!HOLD) post_factors<VEC, VPT>(a, worker, c, wt);
+    sum = both(0.f);
 #pragma unroll
-      for (int j = 0; j < VPT; ++j)
-        if (real[j]) {
-          ActPack<T, VEC> o;
+    for (int j = 0; j < VPT; ++j) {
+      v[j] = feed.get(X, j);
+      const Vals<VEC> y = feed.get(Y, j);
+      Vals<VEC> g;
+      if constexpr (FULL) g = feed.get(G, j);
 #pragma unroll
-          for (int i = 0; i < VEC; ++i) o.v[i] = from_f32<T>(v[j][i]);
-          store_stream<T, VEC>(reinterpret_cast<T*>(a.x_new.p) + row * a.x_new.ld + c[j], o);
-        }
+      for (int i = 0; i < P; ++i) {
+        float2 u = mul2(get2(y, i), both(ry));
+        if constexpr (FULL) u = mul2(u, get2(g, i));
+        const float2 x = fma2(u, get2(wt[j], i), get2(v[j], i));
+        put2(v[j], i, x);
+        sum = fma2(x, x, sum);
+      }
+      if (a.x_new.p && c[j] < a.width) store_vec<T, VEC>(a.x_new, row, c[j], v[j]);
     }
     if (a.n.p) {
-      ss[0] = 0.f;
-#pragma unroll
-      for (int j = 0; j < VPT; ++j)
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) ss[0] = fmaf(v[j][i], v[j][i], ss[0]);
+      ss[0] = sum.x + sum.y;
       cta_sum<1, NT>(ss, buf, slot); slot ^= 1;
-      const float rx = rsqrtf(fmaf(ss[0], a.inv_width, a.eps));
+      const float2 rx = both(rsqrtf(fmaf(ss[0], a.inv_width, a.eps)));
+      if constexpr (!HOLD) load_channel<VEC, VPT>(a.w_pre, worker, c, a.width, wn);
 #pragma unroll
-      for (int j = 0; j < VPT; ++j)
-        if (real[j]) {
-          float w[VEC];
-          load_channel<VEC>(a.w_pre, worker, c[j], true, 1.f, w);
-          ActPack<T, VEC> o;
+      for (int j = 0; j < VPT; ++j) {
 #pragma unroll
-          for (int i = 0; i < VEC; ++i) o.v[i] = from_f32<T>(v[j][i] * rx * w[i]);
-          store_stream<T, VEC>(reinterpret_cast<T*>(a.n.p) + row * a.n.ld + c[j], o);
-        }
+        for (int i = 0; i < P; ++i) put2(v[j], i, mul2(mul2(get2(v[j], i), rx), get2(wn[j], i)));
+        if (c[j] < a.width) store_vec<T, VEC>(a.n, row, c[j], v[j]);
+      }
     }
   }
 }
 
-template <typename T, int VEC, int NT, int VPT>
-__global__ void __launch_bounds__(NT) norm_backward_kernel(const NormArgs a) {
-  __shared__ float buf[2][6][NT / 32 > 0 ? NT / 32 : 1];
-  const int64_t worker = blockIdx.x / a.ctas, row0 = worker * a.rows, end = row0 + a.rows;
-  int64_t row = row0 + blockIdx.x % a.ctas;
-  const bool has_y = a.y.p != nullptr, full = a.gate_kind == GATE_FULL, post = a.w_post.p != nullptr, pre = a.dn.p != nullptr, dres = a.dres.p != nullptr;
+template <typename T, int VEC, int NT, int VPT, int STAGES, bool FULL>
+__global__ void __launch_bounds__(NT, NT <= 512 ? 512 / NT : 1) norm_backward_kernel(const NormArgs a) {
+  constexpr bool HOLD = VEC * VPT <= 8;
+  constexpr int P = pairs_of<VEC>;
+  enum { X, Y, DN, DR, G, N = FULL ? 5 : 4 };
+  extern __shared__ __align__(16) unsigned char ring[];
+  __shared__ __align__(16) float buf[2][6][NT / 32];
+  const int64_t worker = blockIdx.x / a.ctas, row0 = worker * a.rows, end = row0 + a.rows, first = row0 + blockIdx.x % a.ctas;
+  const bool has_y = a.y.p != nullptr, post = a.w_post.p != nullptr, pre = a.dn.p != nullptr;
+  NormMat in[N] = {a.x_new, a.y, a.dn, a.dres};
+  if constexpr (FULL) in[G] = a.gate;
   int c[VPT];
-  bool real[VPT];
 #pragma unroll
-  for (int j = 0; j < VPT; ++j) { c[j] = (threadIdx.x + j * NT) * VEC; real[j] = c[j] < a.width; }
-  RowVec<T, VEC> x[VPT], y[VPT], g[VPT], n[VPT], d[VPT];
-  auto fetch = [&](int64_t r) {
-#pragma unroll
-    for (int j = 0; j < VPT; ++j) {
-      x[j].load(a.x_new, r, c[j], real[j] && pre);
-      y[j].load(a.y, r, c[j], real[j] && has_y);
-      n[j].load(a.dn, r, c[j], real[j] && pre);
-      d[j].load(a.dres, r, c[j], real[j] && dres);
-      if (full) g[j].load(a.gate, r, c[j], real[j]);
-    }
-  };
-  float acc_pre[VPT][VEC], acc_post[VPT][VEC];
+  for (int j = 0; j < VPT; ++j) c[j] = (threadIdx.x + j * NT) * VEC;
+  Vals<VEC> acc_pre[VPT], acc_post[VPT], wt[VPT], wn[VPT];
 #pragma unroll
   for (int j = 0; j < VPT; ++j)
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) acc_pre[j][i] = acc_post[j][i] = 0.f;
-  for (int slot = 0; row < end; row += a.ctas) {
-    fetch(row);
-    // t0 = s g w_post y; the six sums
-    float s[6] = {};
+    for (int i = 0; i < VEC; ++i) acc_pre[j].v[i] = acc_post[j].v[i] = 0.f;
+  if constexpr (HOLD) {
+    post_factors<VEC, VPT>(a, worker, c, wt);
+    load_channel<VEC, VPT>(a.w_pre, worker, c, a.width, wn);
+  }
+  RowFeed<T, VEC, NT, VPT, N, STAGES> feed;
+  feed.start(in, a.width, ring, first, a.ctas, end);
+  int slot = 0;
+  for (int64_t row = first; row < end; row += a.ctas) {
+    feed.next(in, row, a.ctas, end, row == first);
+    if constexpr (!HOLD) {
+      post_factors<VEC, VPT>(a, worker, c, wt);
+      load_channel<VEC, VPT>(a.w_pre, worker, c, a.width, wn);
+    }
+    // the six sums; t0 = s g w_post y
+    float2 s2[6];
+#pragma unroll
+    for (int k = 0; k < 6; ++k) s2[k] = both(0.f);
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
-      float wn[VEC], wp[VEC], gr[VEC];
-      load_channel<VEC>(a.w_pre, worker, c[j], real[j], 1.f, wn);
-      load_channel<VEC>(a.w_post, worker, c[j], real[j], 1.f, wp);
-      if (a.gate_kind == GATE_ROW) load_channel<VEC>(a.gate, worker, c[j], real[j], 1.f, gr);
+      const Vals<VEC> x = feed.get(X, j), y = feed.get(Y, j), n = feed.get(DN, j), d = feed.get(DR, j);
+      Vals<VEC> g;
+      if constexpr (FULL) g = feed.get(G, j);
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        const float xv = x[j][i], yv = y[j][i], av = n[j][i] * wn[i], dv = d[j][i];
-        float t0 = a.scale * wp[i] * yv;
-        if (full) t0 *= g[j][i];
-        else if (a.gate_kind == GATE_ROW) t0 *= gr[i];
-        s[0] = fmaf(xv, xv, s[0]);
-        s[1] = fmaf(yv, yv, s[1]);
-        s[2] = fmaf(av, xv, s[2]);
-        s[3] = fmaf(t0, dv, s[3]);
-        s[4] = fmaf(t0, av, s[4]);
-        s[5] = fmaf(t0, xv, s[5]);
+      for (int i = 0; i < P; ++i) {
+        const float2 xv = get2(x, i), yv = get2(y, i), av = mul2(get2(n, i), get2(wn[j], i));
+        float2 t0 = mul2(get2(wt[j], i), yv);
+        if constexpr (FULL) t0 = mul2(t0, get2(g, i));
+        s2[0] = fma2(xv, xv, s2[0]);
+        s2[1] = fma2(yv, yv, s2[1]);
+        s2[2] = fma2(av, xv, s2[2]);
+        s2[3] = fma2(t0, get2(d, i), s2[3]);
+        s2[4] = fma2(t0, av, s2[4]);
+        s2[5] = fma2(t0, xv, s2[5]);
       }
     }
+    float s[6];
+#pragma unroll
+    for (int k = 0; k < 6; ++k) s[k] = s2[k].x + s2[k].y;
     cta_sum<6, NT>(s, buf, slot); slot ^= 1;
     const float rx = pre ? rsqrtf(fmaf(s[0], a.inv_width, a.eps)) : 0.f;
     const float ry = post ? rsqrtf(fmaf(s[1], a.inv_width, a.eps)) : 1.f;
     const float k = rx * rx * (rx * s[2] * a.inv_width);                       // dX = dres + rx a - k x'
     const float m = post ? ry * ry * a.inv_width * (s[3] + rx * s[4] - k * s[5]) : 0.f;   // dy = ry (b - m y)
+    const float2 rx2 = both(rx), mk2 = both(-k), ry2 = both(ry), mr2 = both(-m * ry), sry2 = both(a.scale * ry);
+    if constexpr (!HOLD) {
+      post_factors<VEC, VPT>(a, worker, c, wt);
+      load_channel<VEC, VPT>(a.w_pre, worker, c, a.width, wn);
+    }
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
-      if (!real[j]) continue;
-      float wn[VEC], wp[VEC], gr[VEC];
-      load_channel<VEC>(a.w_pre, worker, c[j], true, 1.f, wn);
-      load_channel<VEC>(a.w_post, worker, c[j], true, 1.f, wp);
-      if (a.gate_kind == GATE_ROW) load_channel<VEC>(a.gate, worker, c[j], true, 1.f, gr);
-      ActPack<T, VEC> ox, oy, og;
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        const float xv = x[j][i], yv = y[j][i], nv = n[j][i];
-        const float dX = fmaf(-k, xv, fmaf(rx, nv * wn[i], d[j][i]));
-        const float gv = full ? g[j][i] : a.gate_kind == GATE_ROW ? gr[i] : 1.f;
-        const float sd = a.scale * dX, yh = yv * ry;
-        ox.v[i] = from_f32<T>(dX);
-        oy.v[i] = from_f32<T>(ry * fmaf(-m, yv, sd * gv * wp[i]));
-        acc_pre[j][i] = fmaf(nv, xv * rx, acc_pre[j][i]);
-        acc_post[j][i] = fmaf(full ? sd * gv : sd, yh, acc_post[j][i]);
-        if (full) og.v[i] = from_f32<T>(sd * yh * wp[i]);
+      const Vals<VEC> x = feed.get(X, j), y = feed.get(Y, j), n = feed.get(DN, j), d = feed.get(DR, j);
+      Vals<VEC> wp[1], g, ox, oy, og;
+      if constexpr (FULL) {
+        const int cj[1] = {c[j]};
+        load_channel<VEC, 1>(a.w_post, worker, cj, a.width, wp);
+        g = feed.get(G, j);
       }
-      store_stream<T, VEC>(reinterpret_cast<T*>(a.dx.p) + row * a.dx.ld + c[j], ox);
-      if (has_y) store_stream<T, VEC>(reinterpret_cast<T*>(a.dy.p) + row * a.dy.ld + c[j], oy);
-      if (full) store_stream<T, VEC>(reinterpret_cast<T*>(a.dgate.p) + row * a.dgate.ld + c[j], og);
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        const float2 xv = get2(x, i), yv = get2(y, i), nv = get2(n, i), xr = mul2(xv, rx2);
+        put2(acc_pre[j], i, fma2(nv, xr, get2(acc_pre[j], i)));
+        const float2 dX = fma2(mk2, xv, fma2(rx2, mul2(nv, get2(wn[j], i)), get2(d, i)));
+        const float2 syh = mul2(yv, sry2), dg = FULL ? mul2(dX, get2(g, i)) : dX;          // syh = s yh
+        put2(ox, i, dX);
+        put2(oy, i, fma2(mr2, yv, mul2(mul2(dg, get2(wt[j], i)), ry2)));
+        put2(acc_post[j], i, fma2(dg, syh, get2(acc_post[j], i)));
+        if constexpr (FULL) put2(og, i, mul2(mul2(dX, syh), get2(wp[0], i)));
+      }
+      if (c[j] < a.width) {
+        store_vec<T, VEC>(a.dx, row, c[j], ox);
+        if (has_y) store_vec<T, VEC>(a.dy, row, c[j], oy);
+        if constexpr (FULL) store_vec<T, VEC>(a.dgate, row, c[j], og);
+      }
     }
   }
   float* out = a.partial + (size_t)blockIdx.x * 2 * a.width;
 #pragma unroll
   for (int j = 0; j < VPT; ++j)
-    if (real[j])
+    if (c[j] < a.width)
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
-        out[c[j] + i] = acc_pre[j][i];
-        out[a.width + c[j] + i] = acc_post[j][i];
+        out[c[j] + i] = acc_pre[j].v[i];
+        out[a.width + c[j] + i] = acc_post[j].v[i];
       }
 }
 
@@ -210,48 +213,71 @@ __global__ void __launch_bounds__(256) norm_columns_kernel(const NormArgs a) {
 constexpr int kMaxWidth = 16384;
 struct Shape { int nt, vpt; };
 // Threads per row x vectors per thread: one vector while a row fits 512 threads of them.
-Shape shape_for(int width, int vec) {
+Shape shape_for(int width, int vec, bool backward) {
   const int vecs = (width + vec - 1) / vec;
   if (vec > 1) {
     if (vecs <= 32) return {32, 1};
+    if (vecs <= 64) return {64, 1};
     if (vecs <= 128) return {128, 1};
     if (vecs <= 256) return {256, 1};
-    if (vecs <= 512) return {512, 1};
+    if (vecs <= 512) return backward ? Shape{256, 2} : Shape{512, 1};
     if (vecs <= 1024) return {512, 2};
-    return {1024, 4};
+    if (vecs <= 2048) return {512, 4};
+    return {1024, 4};      // fp32 above 8192 columns
   }
   if (vecs <= 128) return {128, 1};
   if (vecs <= 1024) return {256, 4};
-  if (vecs <= 4096) return {512, 8};
+  if (vecs <= 2048) return {512, 4};
+  if (vecs <= 4096) return {1024, 4};
+  if (vecs <= 8192) return {1024, 8};
   return {1024, 16};
 }
-int ctas_per_worker(int64_t workers, int64_t rows, int nt) {
-  int64_t c = ((int64_t)sm_count() * (nt >= 1024 ? 1 : 1024 / nt > 16 ? 16 : 1024 / nt) + workers - 1) / workers;
+// CTAs that share an SM (the kernels' launch bounds leave registers for them).
+int ctas_per_sm(int nt, bool backward) {
+  const int c = (backward ? 512 : 1024) / nt;
+  return c < 1 ? 1 : c > 16 ? 16 : c;
+}
+int ctas_per_worker(int64_t workers, int64_t rows, int nt, bool backward) {
+  int64_t c = ((int64_t)sm_count() * ctas_per_sm(nt, backward) + workers - 1) / workers;
   if (c > rows) c = rows;
   return (int)(c < 1 ? 1 : c);
 }
 
-template <typename T, int VEC, int NT, int VPT>
-void launch_norm(const NormArgs& a, unsigned grid, bool backward, cudaStream_t st) {
-  if (backward) norm_backward_kernel<T, VEC, NT, VPT><<<grid, NT, 0, st>>>(a);
-  else norm_forward_kernel<T, VEC, NT, VPT><<<grid, NT, 0, st>>>(a);
+template <typename T, int VEC, int NT, int VPT, int SF, int SB>
+cudaError_t launch_norm(const NormArgs& a, unsigned grid, bool backward, cudaStream_t st) {
+  const bool full = a.gate_kind == GATE_FULL;
+  auto kern = backward ? (full ? norm_backward_kernel<T, VEC, NT, VPT, SB, true> : norm_backward_kernel<T, VEC, NT, VPT, SB, false>)
+                       : (full ? norm_forward_kernel<T, VEC, NT, VPT, SF, true> : norm_forward_kernel<T, VEC, NT, VPT, SF, false>);
+  const size_t smem = (size_t)(backward ? SB * (full ? 5 : 4) : SF * (full ? 3 : 2)) * VPT * NT * 16;
+  cudaError_t e = smem > 32 * 1024 ? cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
+  if (e == cudaSuccess) {
+    kern<<<grid, NT, smem, st>>>(a);
+    e = cudaGetLastError();
+  }
+  return e;
 }
 template <typename T>
-void launch_norm_shape(const NormArgs& a, Shape s, bool vec, unsigned grid, bool backward, cudaStream_t st) {
+cudaError_t launch_norm_shape(const NormArgs& a, Shape s, bool vec, unsigned grid, bool backward, cudaStream_t st) {
   constexpr int V = 16 / sizeof(T);
   if (vec) {
-    if (s.nt == 32) launch_norm<T, V, 32, 1>(a, grid, backward, st);
-    else if (s.nt == 128) launch_norm<T, V, 128, 1>(a, grid, backward, st);
-    else if (s.nt == 256) launch_norm<T, V, 256, 1>(a, grid, backward, st);
-    else if (s.nt == 512 && s.vpt == 1) launch_norm<T, V, 512, 1>(a, grid, backward, st);
-    else if (s.nt == 512) launch_norm<T, V, 512, 2>(a, grid, backward, st);
-    else launch_norm<T, V, 1024, 4>(a, grid, backward, st);
-  } else {
-    if (s.nt == 128) launch_norm<T, 1, 128, 1>(a, grid, backward, st);
-    else if (s.nt == 256) launch_norm<T, 1, 256, 4>(a, grid, backward, st);
-    else if (s.nt == 512) launch_norm<T, 1, 512, 8>(a, grid, backward, st);
-    else launch_norm<T, 1, 1024, 16>(a, grid, backward, st);
+    // rows in flight: forward 3 x 8 to 24 KB, backward 2 x 16 to 20 KB per 256 threads; two vectors per thread leave room for one
+    if (s.nt == 32) return launch_norm<T, V, 32, 1, 4, 3>(a, grid, backward, st);
+    if (s.nt == 64) return launch_norm<T, V, 64, 1, 4, 3>(a, grid, backward, st);
+    if (s.nt == 128) return launch_norm<T, V, 128, 1, 4, 3>(a, grid, backward, st);
+    if (s.nt == 256 && s.vpt == 1) return launch_norm<T, V, 256, 1, 4, 3>(a, grid, backward, st);
+    if (s.nt == 256) return launch_norm<T, V, 256, 2, 2, 2>(a, grid, backward, st);
+    if (s.vpt == 1) return launch_norm<T, V, 512, 1, 4, 3>(a, grid, backward, st);
+    if (s.vpt == 2) return launch_norm<T, V, 512, 2, 2, 2>(a, grid, backward, st);
+    if (s.nt == 512) return launch_norm<T, V, 512, 4, 1, 1>(a, grid, backward, st);
+    if constexpr (sizeof(T) == 4) return launch_norm<T, V, 1024, 4, 0, 0>(a, grid, backward, st);
+    return cudaErrorInvalidValue;
   }
+  if (s.nt == 128) return launch_norm<T, 1, 128, 1, 0, 0>(a, grid, backward, st);
+  if (s.nt == 256) return launch_norm<T, 1, 256, 4, 0, 0>(a, grid, backward, st);
+  if (s.nt == 512) return launch_norm<T, 1, 512, 4, 0, 0>(a, grid, backward, st);
+  if (s.vpt == 4) return launch_norm<T, 1, 1024, 4, 0, 0>(a, grid, backward, st);
+  if (s.vpt == 8) return launch_norm<T, 1, 1024, 8, 0, 0>(a, grid, backward, st);
+  return launch_norm<T, 1, 1024, 16, 0, 0>(a, grid, backward, st);
 }
 
 struct Named { const char* name; const fgd_mat* m; bool wanted, present_needed, channel; };
@@ -318,7 +344,7 @@ int run_norm(const fgd_block_norm_args* b, bool backward, int device, void* stre
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool columns = backward && (pre || post || b->gate_kind == GATE_ROW);
   if (T == 0 && !columns) return FGD_OK;
-  const Shape s = shape_for((int)b->width, aligned ? vec : 1);
+  const Shape s = shape_for((int)b->width, aligned ? vec : 1, backward);
   NormArgs a = {};
   auto mat = [](const fgd_mat& m, bool use) { return NormMat{use ? static_cast<char*>(m.p) : nullptr, m.ld}; };
   a.x = mat(b->x, !backward); a.y = mat(b->y, y); a.gate = mat(b->gate, gate); a.w_post = mat(b->w_post, post); a.w_pre = mat(b->w_pre, pre);
@@ -326,7 +352,7 @@ int run_norm(const fgd_block_norm_args* b, bool backward, int device, void* stre
   a.dn = mat(b->dn, backward && pre); a.dres = mat(b->dres, backward); a.dx = mat(b->dx, backward); a.dy = mat(b->dy, backward && y);
   a.dgate = mat(b->dgate, backward && gate); a.dw_post = mat(b->dw_post, backward && post); a.dw_pre = mat(b->dw_pre, backward && pre);
   a.rows = b->rows; a.width = (int)b->width; a.gate_kind = b->gate_kind;
-  a.ctas = ctas_per_worker(b->workers, b->rows, s.nt);
+  a.ctas = ctas_per_worker(b->workers, b->rows, s.nt, backward);
   a.eps = (float)b->eps; a.scale = (float)b->res_scale; a.inv_width = 1.f / (float)b->width;
   const int64_t grid = (int64_t)b->workers * a.ctas;
   if (grid > 0x7fffffff) return op_fail(FGD_ERR_INVALID_ARG, "%s: too many workers", who);
@@ -336,13 +362,16 @@ int run_norm(const fgd_block_norm_args* b, bool backward, int device, void* stre
       return op_fail(FGD_ERR_INVALID_ARG, "%s: needs a workspace of %lld bytes (fgd_block_norm_workspace)", who, (long long)need);
     a.partial = static_cast<float*>(b->workspace);
   }
+  cudaError_t e;
   switch (b->dtype) {
-    case FGD_F32: launch_norm_shape<float>(a, s, aligned, (unsigned)grid, backward, st); break;
-    case FGD_BF16: launch_norm_shape<__nv_bfloat16>(a, s, aligned, (unsigned)grid, backward, st); break;
-    default: launch_norm_shape<__half>(a, s, aligned, (unsigned)grid, backward, st); break;
+    case FGD_F32: e = launch_norm_shape<float>(a, s, aligned, (unsigned)grid, backward, st); break;
+    case FGD_BF16: e = launch_norm_shape<__nv_bfloat16>(a, s, aligned, (unsigned)grid, backward, st); break;
+    default: e = launch_norm_shape<__half>(a, s, aligned, (unsigned)grid, backward, st); break;
   }
-  if (columns) norm_columns_kernel<<<dim3((unsigned)((b->width + 31) / 32), (unsigned)b->workers), 256, 0, st>>>(a);
-  const cudaError_t e = cudaGetLastError();
+  if (e == cudaSuccess && columns) {
+    norm_columns_kernel<<<dim3((unsigned)((b->width + 31) / 32), (unsigned)b->workers), 256, 0, st>>>(a);
+    e = cudaGetLastError();
+  }
   if (e != cudaSuccess) return op_fail(FGD_ERR_CUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
   return FGD_OK;
 }
@@ -354,7 +383,7 @@ extern "C" int64_t fgd_block_norm_workspace(int device, int dtype, int workers, 
   if (bytes == 0 || workers < 1 || workers > FGD_MAX_K || rows < 0 || rows > 0x7fffffff || width < 1 || width > kMaxWidth) return FGD_ERR_INVALID_ARG;
   DeviceScope dev(device);
   // the element-wise shapes have no fewer threads per row than the vector shapes, so no more CTAs
-  return (int64_t)workers * ctas_per_worker(workers, rows, shape_for((int)width, 16 / bytes).nt) * 2 * width * (int64_t)sizeof(float);
+  return (int64_t)workers * ctas_per_worker(workers, rows, shape_for((int)width, 16 / bytes, true).nt, true) * 2 * width * (int64_t)sizeof(float);
 }
 extern "C" int fgd_block_norm_forward(int device, const fgd_block_norm_args* args, void* stream) {
   FGD_NVTX_RANGE("fgd_block_norm_forward");

@@ -12,9 +12,9 @@
 // pass but the activations themselves.
 //
 // HBM-bound: forward 4 activations' bytes per element, backward 6 (8 with an element-wise gate).  One CTA takes whole
-// rows, every element stays in registers between its load and its store, and the next row is loaded
-// before this row's sums are reduced.  The backward pass needs ONE reduction per row for all its means: with
-// t0 = s g o w_post o y,
+// rows.  On the 16-byte path a thread copies its vectors of the next rows into shared memory asynchronously (cp.async: a ring of
+// rows that only this thread reads, so it needs no barrier and costs no registers) while it works on the current row.  The
+// backward pass needs ONE reduction per row for all its means: with t0 = s g o w_post o y,
 //     sum b o yh = r_y sum t0 o dX = r_y (sum t0 o dres + r_x sum t0 o a - r_x^2 mean(a o xh) sum t0 o x'),
 // so the six sums of x'^2, y^2, a x', t0 dres, t0 a, t0 x' settle everything at once.  Gradients of weights and of a
 // per-channel gate are column sums: every CTA keeps its own in registers over its rows and writes them
@@ -43,64 +43,192 @@ struct NormArgs {
 };
 
 template <typename T, int VEC>
-struct RowVec {
-  ActPack<T, VEC> r;
-  __device__ __forceinline__ void load(const NormMat& m, int64_t row, int c, bool real) {
-    if (real) r = load_stream<T, VEC>(reinterpret_cast<const T*>(m.p) + row * m.ld + c);
-    else {
+__device__ __forceinline__ void store_vec(const NormMat& m, int64_t row, int c, const Vals<VEC>& v) {
+  store_stream<T, VEC>(reinterpret_cast<T*>(m.p) + row * m.ld + c, round_to<T, VEC>(v));
+}
+
+// VPT vectors of per-channel fp32 values (1 where the tensor is absent), c[j] the first column of vector j; a column beyond the
+// width reads the row's first vector instead, which is never used.
+template <int VEC, int VPT>
+__device__ __forceinline__ void load_channel(const NormMat& m, int64_t worker, const int (&c)[VPT], int width, Vals<VEC> (&w)[VPT]) {
+  if (m.p == nullptr) {
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) r.v[i] = from_f32<T>(0.f);
+    for (int j = 0; j < VPT; ++j)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) w[j].v[i] = 1.f;
+    return;
+  }
+  const float* p = reinterpret_cast<const float*>(m.p) + worker * m.ld;
+#pragma unroll
+  for (int j = 0; j < VPT; ++j) {
+    const float* q = p + (c[j] < width ? c[j] : 0);
+    if constexpr (VEC % 4 == 0) {
+#pragma unroll
+      for (int i = 0; i < VEC; i += 4) {
+        const float4 t = __ldg(reinterpret_cast<const float4*>(q + i));
+        w[j].v[i] = t.x; w[j].v[i + 1] = t.y; w[j].v[i + 2] = t.z; w[j].v[i + 3] = t.w;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) w[j].v[i] = __ldg(q + i);
     }
   }
-  __device__ __forceinline__ float operator[](int i) const { return to_f32<T>(r.v[i]); }
+}
+// What multiplies y r_y per channel: res_scale, w_post, and the gate where it is per channel.
+template <int VEC, int VPT>
+__device__ __forceinline__ void post_factors(const NormArgs& a, int64_t worker, const int (&c)[VPT], Vals<VEC> (&w)[VPT]) {
+  load_channel<VEC, VPT>(a.w_post, worker, c, a.width, w);
+  if (a.gate_kind == GATE_ROW) {
+    Vals<VEC> g[VPT];
+    load_channel<VEC, VPT>(a.gate, worker, c, a.width, g);
+#pragma unroll
+    for (int j = 0; j < VPT; ++j)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) w[j].v[i] *= g[j].v[i];
+  }
+#pragma unroll
+  for (int j = 0; j < VPT; ++j)
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) w[j].v[i] *= a.scale;
+}
+
+// The rows of up to N tensors that a thread is going to work on: a ring of STAGES rows in shared memory filled with cp.async
+// (16-byte vectors), or, with STAGES = 0, the current row in registers.  Absent tensors and columns beyond the width read as zero.
+template <typename T, int VEC, int NT, int VPT, int N, int STAGES>
+struct RowFeed {
+  unsigned char* ring;
+  uint32_t use;               // bit k: tensor k is present
+  int width, stage;
+  ActPack<T, VEC> cur[STAGES ? 1 : N][STAGES ? 1 : VPT];
+
+  __device__ __forceinline__ size_t slot(int s, int k, int j) const { return ((size_t)((s * N + k) * VPT + j) * NT + threadIdx.x) * 16; }
+  __device__ __forceinline__ void ask(int s, int64_t row, const NormMat (&t)[N]) {
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (use >> k & 1) {
+        const T* p = reinterpret_cast<const T*>(t[k].p) + row * t[k].ld;
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+          const int c = (threadIdx.x + j * NT) * VEC;
+          if (c < width) {
+            const uint32_t dst = (uint32_t)__cvta_generic_to_shared(ring + slot(s, k, j));
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(p + c) : "memory");
+          }
+        }
+      }
+  }
+  // Rows first, first + step, ... below end.
+  __device__ __forceinline__ void start(const NormMat (&t)[N], int width_, unsigned char* ring_, int64_t first, int64_t step, int64_t end) {
+    ring = ring_; width = width_; stage = 0; use = 0;
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (t[k].p != nullptr) use |= 1u << k;
+    if constexpr (STAGES > 0) {
+#pragma unroll
+      for (int s = 0; s < STAGES; ++s)
+        for (int k = 0; k < N; ++k)
+          for (int j = 0; j < VPT; ++j)
+            if (!(use >> k & 1) || (int)(threadIdx.x + j * NT) * VEC >= width) *reinterpret_cast<uint4*>(ring + slot(s, k, j)) = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+      for (int s = 0; s < STAGES - 1; ++s) {
+        if (first + s * step < end) ask(s, first + s * step, t);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+      }
+    }
+  }
+  // Makes row `row` the current one and asks for the row STAGES - 1 further on.
+  __device__ __forceinline__ void next(const NormMat (&t)[N], int64_t row, int64_t step, int64_t end, bool first) {
+    if constexpr (STAGES == 1) {
+      ask(0, row, t);
+      asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
+    } else if constexpr (STAGES > 1) {
+      if (!first) stage = stage + 1 == STAGES ? 0 : stage + 1;
+      asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+      const int64_t far = row + (STAGES - 1) * step;
+      const int into = stage == 0 ? STAGES - 1 : stage - 1;
+      if (far < end) ask(into, far, t);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    } else {
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+          const int c = (threadIdx.x + j * NT) * VEC;
+          if ((use >> k & 1) && c < width) cur[k][j] = load_stream<T, VEC>(reinterpret_cast<const T*>(t[k].p) + row * t[k].ld + c);
+          else zero(cur[k][j]);
+        }
+    }
+  }
+  __device__ __forceinline__ Vals<VEC> get(int k, int j) const {
+    if constexpr (STAGES > 0) {
+      ActPack<T, VEC> p;
+      if constexpr (ActPack<T, VEC>::kVector) p.w = *reinterpret_cast<const uint4*>(ring + slot(stage, k, j));
+      return unpack<T, VEC>(p);
+    } else {
+      return unpack<T, VEC>(cur[k][j]);
+    }
+  }
 };
 
-// VEC per-channel fp32 values (weights are read by every row: through the read-only cache).
-template <int VEC>
-__device__ __forceinline__ void load_channel(const NormMat& m, int64_t worker, int c, bool real, float fill, float (&w)[VEC]) {
-#pragma unroll
-  for (int i = 0; i < VEC; ++i) w[i] = fill;
-  if (m.p == nullptr || !real) return;
-  const float* p = reinterpret_cast<const float*>(m.p) + worker * m.ld + c;
-  if constexpr (VEC % 4 == 0) {
-#pragma unroll
-    for (int i = 0; i < VEC; i += 4) {
-      const float4 t = __ldg(reinterpret_cast<const float4*>(p + i));
-      w[i] = t.x; w[i + 1] = t.y; w[i + 2] = t.z; w[i + 3] = t.w;
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) w[i] = __ldg(p + i);
-  }
-}
-
 // Sums of N values over the CTA, in a fixed order, given to every thread.  `slot` alternates between calls, so
-// one barrier per reduction is enough.
+// one barrier per reduction is enough.  Inside a warp the lanes trade values as they add: after the first step a lane carries half of
+// the N sums, after the third one of eight, so that six sums cost 9 shuffles instead of 30.
 template <int N, int NT>
 __device__ __forceinline__ void cta_sum(float (&v)[N], float (*buf)[N][NT / 32], int slot) {
+  static_assert(N == 1 || N == 6, "one sum or six");
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if constexpr (N == 1) {
 #pragma unroll
-  for (int k = 0; k < N; ++k)
+    for (int off = 16; off > 0; off >>= 1) v[0] += __shfl_xor_sync(0xffffffffu, v[0], off);
+    if constexpr (NT > 32) {
+      if (lane == 0) buf[slot][0][warp] = v[0];
+    }
+  } else {
+    // bit 4, 3, 2 of the lane choose the upper half of what is left
+    const bool up16 = lane & 16, up8 = lane & 8, up4 = lane & 4;
+    float a[4], b[2], c;
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], off);
+    for (int i = 0; i < 4; ++i) {
+      const float hi = i < 2 ? v[i + 4] : 0.f;
+      a[i] = (up16 ? hi : v[i]) + __shfl_xor_sync(0xffffffffu, up16 ? v[i] : hi, 16);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) b[i] = (up8 ? a[i + 2] : a[i]) + __shfl_xor_sync(0xffffffffu, up8 ? a[i] : a[i + 2], 8);
+    c = (up4 ? b[1] : b[0]) + __shfl_xor_sync(0xffffffffu, up4 ? b[0] : b[1], 4);
+    c += __shfl_xor_sync(0xffffffffu, c, 2);
+    c += __shfl_xor_sync(0xffffffffu, c, 1);
+    const int k = (lane >> 4) * 4 + ((lane >> 3) & 1) * 2 + ((lane >> 2) & 1);     // which sum this lane has
+    if constexpr (NT > 32) {
+      if ((lane & 3) == 0 && k < N) buf[slot][k][warp] = c;
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xffffffffu, c, (i >> 2) * 16 + ((i >> 1) & 1) * 8 + (i & 1) * 4);
+    }
+  }
   if constexpr (NT > 32) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (lane == 0)
-#pragma unroll
-      for (int k = 0; k < N; ++k) buf[slot][k][warp] = v[k];
+    constexpr int W = NT / 32;
     __syncthreads();
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
+    if constexpr (N == 1) {
       float s = 0.f;
 #pragma unroll
-      for (int w = 0; w < NT / 32; ++w) s += buf[slot][k][w];
-      v[k] = s;
+      for (int w = 0; w < W; ++w) s += buf[slot][0][w];
+      v[0] = s;
+    } else {
+      // four lanes per sum add the warps' parts, then every lane takes all six
+      const int k = lane >> 2, part = lane & 3;
+      float s = 0.f;
+      if (k < N) {
+#pragma unroll
+        for (int w = 0; w < (W + 3) / 4; ++w)
+          if (W % 4 == 0 || part * ((W + 3) / 4) + w < W) s += buf[slot][k][part * ((W + 3) / 4) + w];
+      }
+      s += __shfl_xor_sync(0xffffffffu, s, 1);
+      s += __shfl_xor_sync(0xffffffffu, s, 2);
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xffffffffu, s, 4 * i);
     }
   }
 }
-
-// Threads per row and vectors per thread for rows of `vecs` vectors; the kernels are compiled for
-// exactly these.
-struct NormShape { int nt, vpt; };
 
 }  // namespace fgd
 #endif
