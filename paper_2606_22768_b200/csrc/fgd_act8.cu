@@ -15,9 +15,9 @@
 //
 // All four are bound by HBM: one pass, every byte read or written once.
 //
-// Vector kernels (rows and bases on 16-byte boundaries, width a multiple of 8): a thread takes 8
-// consecutive values, four neighbouring lanes make a group, so the group's largest magnitude is two
-// shuffles away.  Element kernels (any width and stride): a warp takes a group, a lane a value.
+// Vector kernels (rows and bases on 16-byte boundaries, width a multiple of 16 or 8): a thread takes 16 or 8
+// consecutive values, two or four neighbouring lanes make a group, so the group's largest magnitude is one or two
+// shuffles away.  Element kernels (any width and stride): a warp takes four groups, a lane one value of each.
 #include "fgd_dtype.cuh"
 #include "fgd_nvtx.h"
 
@@ -42,52 +42,113 @@ __device__ __forceinline__ int to_q8(float x, float inv) {
 }
 __device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
 
-__device__ __forceinline__ float sigmoid(float g) { return __fdividef(1.f, 1.f + __expf(-g)); }
+// 1 / (1 + 2^(-g log2 e)) from the hardware's exponential and reciprocal; a denominator beyond fp32 gives 0.
+__device__ __forceinline__ float2 sigmoid2(float2 g) {
+  float2 x = mul2(g, both(-1.4426950408889634f));
+  asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(x.x));
+  asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(x.y));
+  x = add2(x, both(1.f));
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(x.x));
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(x.y));
+  return x;
+}
 
-// Largest magnitude bits over the four lanes of a group.
-__device__ __forceinline__ uint32_t quad_max(uint32_t m) {
-  m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-  return max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+// Largest magnitude bits over the 32 / V neighbouring lanes of a group.
+template <int V>
+__device__ __forceinline__ uint32_t group_max(uint32_t m) {
+#pragma unroll
+  for (int k = 1; k < kGroup / V; k <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, k));
+  return m;
 }
 __device__ __forceinline__ uint32_t warp_max(uint32_t m) { return __reduce_max_sync(0xffffffffu, m); }
 
-// 8 consecutive values starting at p, as fp32.
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, float (&f)[8]) {
+// V consecutive values starting at p, as fp32.
+template <typename T, int V>
+__device__ __forceinline__ Vals<V> load_vals(const T* p) {
   constexpr int N = 16 / sizeof(T);
+  Vals<V> f;
 #pragma unroll
-  for (int j = 0; j < 8; j += N) {
+  for (int j = 0; j < V; j += N) {
     const Vals<N> r = unpack<T, N>(load_stream<T, N>(p + j));
 #pragma unroll
-    for (int i = 0; i < N; ++i) f[j + i] = r.v[i];
+    for (int i = 0; i < N; ++i) f.v[j + i] = r.v[i];
   }
+  return f;
 }
-template <typename T>
-__device__ __forceinline__ void store8(T* p, const float (&f)[8]) {
+template <typename T, int V>
+__device__ __forceinline__ void store_vals(T* p, const Vals<V>& f) {
   constexpr int N = 16 / sizeof(T);
 #pragma unroll
-  for (int j = 0; j < 8; j += N) {
+  for (int j = 0; j < V; j += N) {
     Vals<N> r;
 #pragma unroll
-    for (int i = 0; i < N; ++i) r.v[i] = f[j + i];
+    for (int i = 0; i < N; ++i) r.v[i] = f.v[j + i];
     store_stream<T, N>(p + j, round_to<T, N>(r));
   }
 }
-__device__ __forceinline__ uint2 quantise8(const float (&f)[8], float inv) {
-  uint32_t w[2] = {0u, 0u};
+template <int V>
+__device__ __forceinline__ Vals<V> no_vals() {
+  Vals<V> f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) w[i >> 2] |= (uint32_t)(to_q8(f[i], inv) & 255) << (8 * (i & 3));
-  return make_uint2(w[0], w[1]);
+  for (int i = 0; i < V; ++i) f.v[i] = 0.f;
+  return f;
 }
-__device__ __forceinline__ void dequantise8(uint2 q, float step, float (&f)[8]) {
+// Largest magnitude of the values as bits; a NaN among them gives NaN bits.
+template <int V>
+__device__ __forceinline__ uint32_t amax_of(const Vals<V>& f) {
+  float m = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) f[i] = (float)(int8_t)(((i < 4 ? q.x : q.y) >> (8 * (i & 3))) & 255u) * step;
+  for (int i = 0; i < V; i += 2) asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(fabsf(f.v[i])), "f"(fabsf(f.v[i + 1])));
+  return __float_as_uint(m);
 }
-__device__ __forceinline__ uint32_t amax8(const float (&f)[8]) {
-  uint32_t m = 0;
+// V stored bytes as they lie in memory: 4, 8 or 16.
+template <int V>
+using Bytes = std::conditional_t<V == 16, uint4, std::conditional_t<V == 8, uint2, uint32_t>>;
+// Quantisation in the mantissa: x / step + 1.5 2^23 rounds to nearest-even at the units place, and the low byte of the sum's bits is
+// q in two's complement.  No clamp is needed unless the largest magnitude reaches 127.5 steps, which the caller tells.
+template <int V>
+__device__ __forceinline__ Bytes<V> quantise(const Vals<V>& f, float inv, bool clamp) {
+  const float2 inv2 = both(inv), magic = both(12582912.f);
+  uint32_t w[V / 4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) m = max(m, abs_bits(f[i]));
-  return m;
+  for (int j = 0; j < V / 4; ++j) {
+    uint32_t b[4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float2 y = fma2(f.pair(2 * j + i), inv2, magic);
+      if (clamp) {
+        y.x = fminf(fmaxf(y.x, 12582912.f - 127.f), 12582912.f + 127.f);
+        y.y = fminf(fmaxf(y.y, 12582912.f - 127.f), 12582912.f + 127.f);
+      }
+      b[2 * i] = __float_as_uint(y.x);
+      b[2 * i + 1] = __float_as_uint(y.y);
+    }
+    w[j] = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+  }
+  if constexpr (V == 16) return make_uint4(w[0], w[1], w[2], w[3]);
+  else return make_uint2(w[0], w[1]);
+}
+// Does a group with this largest magnitude reach 127.5 steps?  (mantissa at or above 127.5 / 128)
+__device__ __forceinline__ bool tops_out(uint32_t amax_bits) { return (amax_bits & 0x7FFFFFu) >= 0x7F0000u; }
+// And back: q + 128 in the low byte of 2^23 is 2^23 + 128 + q; one exact fused operation takes the offset off and applies the step.
+template <int V>
+__device__ __forceinline__ Vals<V> dequantise(const Bytes<V>& q, float step) {
+  uint32_t w[V / 4];
+  if constexpr (V == 16) { w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w; }
+  else if constexpr (V == 8) { w[0] = q.x; w[1] = q.y; }
+  else w[0] = q;
+  const float2 step2 = both(step), off = both(-8388736.f * step);
+  Vals<V> f;
+#pragma unroll
+  for (int j = 0; j < V / 4; ++j) {
+    const uint32_t u = w[j] ^ 0x80808080u;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float2 y = make_float2(__uint_as_float(__byte_perm(u, 0x4B000000u, 0x7440 + 2 * i)), __uint_as_float(__byte_perm(u, 0x4B000000u, 0x7440 + 2 * i + 1)));
+      f.set(2 * j + i, fma2(y, step2, off));
+    }
+  }
+  return f;
 }
 
 struct Act8Args {
@@ -113,60 +174,85 @@ struct Walk {
   }
 };
 
-// ---- vector kernels: a unit is 8 values; every row is padded to whole groups, i.e. to a multiple of four
-// units, so that the four lanes of a group always work together
-template <typename T>
+// ---- vector kernels: a unit is V values; every row is padded to whole groups, so that the lanes of a group always work together.
+// V = 16 for 16-bit activations (16-byte stores of the checkpoint: save of 32768 x 4096 bf16 71.5 us against 78.6 with 8), 8 for fp32
+// (57 against 60) and for widths that are not a multiple of 16.
+template <typename T, int V>
 __global__ void __launch_bounds__(kBlock8) act8_save_kernel(const Act8Args a) {
-  const int units = (int)((a.width + kGroup - 1) / kGroup) * 4;
-  const int64_t total = a.rows * units, padded = (total + 31) / 32 * 32;   // whole warps stay in the loop for the shuffles
-  Walk w((int64_t)blockIdx.x * kBlock8 + threadIdx.x, (int64_t)gridDim.x * kBlock8, units);
-  for (int64_t i = (int64_t)blockIdx.x * kBlock8 + threadIdx.x; i < padded; i += (int64_t)gridDim.x * kBlock8, w.next()) {
-    const int c = w.unit * 8;
+  constexpr int L = kGroup / V;      // lanes of a group
+  const int units = (int)((a.width + kGroup - 1) / kGroup) * L;
+  const int64_t total = a.rows * units, padded = (total + 31) / 32 * 32, stride = (int64_t)gridDim.x * kBlock8;   // whole warps stay in the loop for the shuffles
+  int64_t i = (int64_t)blockIdx.x * kBlock8 + threadIdx.x;
+  Walk w(i, stride, units);
+  for (; i < padded; i += stride, w.next()) {
+    const int c = w.unit * V;
     const bool real = i < total && c < a.width;
-    float f[8] = {};
-    if (real) load8<T>(static_cast<const T*>(a.x) + w.row * a.ld_x + c, f);
-    const uint32_t e = step_exponent(quad_max(amax8(f)));
-    if (real) *reinterpret_cast<uint2*>(a.q + w.row * a.ld_q + c) = quantise8(f, inverse_step(e));
-    if (i < total && (w.unit & 3) == 0) a.e[w.row * a.ld_e + (w.unit >> 2)] = (uint8_t)e;
+    const Vals<V> f = real ? load_vals<T, V>(static_cast<const T*>(a.x) + w.row * a.ld_x + c) : no_vals<V>();
+    const uint32_t m = group_max<V>(amax_of<V>(f)), e = step_exponent(m);
+    const Bytes<V> q = __any_sync(0xffffffffu, tops_out(m)) ? quantise<V>(f, inverse_step(e), true) : quantise<V>(f, inverse_step(e), false);
+    if (real) __stcs(reinterpret_cast<Bytes<V>*>(a.q + w.row * a.ld_q + c), q);
+    if (i < total && w.unit % L == 0) a.e[w.row * a.ld_e + w.unit / L] = (uint8_t)e;
   }
 }
+// Reading back, a thread takes what makes one 16-byte store, so that a warp's stores are whole lines (two stores 32 bytes apart cost
+// 13 points of bandwidth), and has four such pieces on their way.
 template <typename T>
 __global__ void __launch_bounds__(kBlock8) act8_load_kernel(const Act8Args a) {
-  const int units = (int)(a.width / 8);
-  const int64_t total = a.rows * units;
-  Walk w((int64_t)blockIdx.x * kBlock8 + threadIdx.x, (int64_t)gridDim.x * kBlock8, units);
-  for (int64_t i = (int64_t)blockIdx.x * kBlock8 + threadIdx.x; i < total; i += (int64_t)gridDim.x * kBlock8, w.next()) {
-    const int c = w.unit * 8;
-    float f[8];
-    dequantise8(__ldcs(reinterpret_cast<const uint2*>(a.q + w.row * a.ld_q + c)), step_of(a.e[w.row * a.ld_e + (w.unit >> 2)]), f);
-    store8<T>(static_cast<T*>(a.out) + w.row * a.ld_out + c, f);
+  constexpr int V = 16 / sizeof(T), L = kGroup / V, U = 4;
+  const int units = (int)(a.width / V);
+  const int64_t total = a.rows * units, stride = (int64_t)gridDim.x * kBlock8;
+  int64_t i = (int64_t)blockIdx.x * kBlock8 + threadIdx.x;
+  Walk w(i, stride, units);
+  while (i < total) {
+    Bytes<V> q[U];
+    float step[U];
+    T* out[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k, i += stride, w.next()) {
+      out[k] = nullptr;
+      if (i >= total) continue;
+      const int c = w.unit * V;
+      q[k] = __ldcs(reinterpret_cast<const Bytes<V>*>(a.q + w.row * a.ld_q + c));
+      step[k] = step_of(a.e[w.row * a.ld_e + w.unit / L]);
+      out[k] = static_cast<T*>(a.out) + w.row * a.ld_out + c;
+    }
+#pragma unroll
+    for (int k = 0; k < U; ++k)
+      if (out[k]) store_vals<T, V>(out[k], dequantise<V>(q[k], step[k]));
   }
 }
-template <typename T>
+template <typename T, int V>
 __global__ void __launch_bounds__(kBlock8) swiglu8_forward_kernel(const Act8Args a) {
-  const int groups = (int)((a.width + kGroup - 1) / kGroup), units = groups * 4;
-  const int64_t total = a.rows * units, padded = (total + 31) / 32 * 32;
-  Walk w((int64_t)blockIdx.x * kBlock8 + threadIdx.x, (int64_t)gridDim.x * kBlock8, units);
-  for (int64_t i = (int64_t)blockIdx.x * kBlock8 + threadIdx.x; i < padded; i += (int64_t)gridDim.x * kBlock8, w.next()) {
-    const int c = w.unit * 8;
+  constexpr int L = kGroup / V;
+  const int groups = (int)((a.width + kGroup - 1) / kGroup), units = groups * L;
+  const int64_t total = a.rows * units, padded = (total + 31) / 32 * 32, stride = (int64_t)gridDim.x * kBlock8;
+  int64_t i = (int64_t)blockIdx.x * kBlock8 + threadIdx.x;
+  Walk w(i, stride, units);
+  for (; i < padded; i += stride, w.next()) {
+    const int c = w.unit * V;
     const bool real = i < total && c < a.width;
-    float g[8] = {}, u[8] = {};
-    if (real) {
-      const T* row = static_cast<const T*>(a.x) + w.row * a.ld_x + c;
-      load8<T>(row, g);
-      load8<T>(row + a.width, u);
+    const T* row = static_cast<const T*>(a.x) + w.row * a.ld_x + c;
+    const Vals<V> g = real ? load_vals<T, V>(row) : no_vals<V>(), u = real ? load_vals<T, V>(row + a.width) : no_vals<V>();
+    const uint32_t mg = group_max<V>(amax_of<V>(g)), mu = group_max<V>(amax_of<V>(u)), eg = step_exponent(mg), eu = step_exponent(mu);
+    Bytes<V> qg, qu;
+    if (__any_sync(0xffffffffu, tops_out(mg) || tops_out(mu))) {
+      qg = quantise<V>(g, inverse_step(eg), true);
+      qu = quantise<V>(u, inverse_step(eu), true);
+    } else {
+      qg = quantise<V>(g, inverse_step(eg), false);
+      qu = quantise<V>(u, inverse_step(eu), false);
     }
-    const uint32_t eg = step_exponent(quad_max(amax8(g))), eu = step_exponent(quad_max(amax8(u)));
     if (real) {
       int8_t* q = a.q + w.row * a.ld_q + c;
-      *reinterpret_cast<uint2*>(q) = quantise8(g, inverse_step(eg));
-      *reinterpret_cast<uint2*>(q + a.width) = quantise8(u, inverse_step(eu));
+      __stcs(reinterpret_cast<Bytes<V>*>(q), qg);
+      __stcs(reinterpret_cast<Bytes<V>*>(q + a.width), qu);
+      Vals<V> h;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) g[j] = g[j] * sigmoid(g[j]) * u[j];
-      store8<T>(static_cast<T*>(a.out) + w.row * a.ld_out + c, g);
+      for (int j = 0; j < V / 2; ++j) h.set(j, mul2(mul2(g.pair(j), sigmoid2(g.pair(j))), u.pair(j)));
+      store_vals<T, V>(static_cast<T*>(a.out) + w.row * a.ld_out + c, h);
     }
-    if (i < total && (w.unit & 3) == 0) {
-      uint8_t* e = a.e + w.row * a.ld_e + (w.unit >> 2);
+    if (i < total && w.unit % L == 0) {
+      uint8_t* e = a.e + w.row * a.ld_e + w.unit / L;
       e[0] = (uint8_t)eg;
       e[groups] = (uint8_t)eu;
     }
@@ -180,109 +266,165 @@ struct Swiglu8BackArgs {
   void* h; int64_t ld_h;             // NULL: not wanted
   int64_t rows, width;
 };
-__device__ __forceinline__ void swiglu_back(float dh, float g, float u, float& dg, float& du, float& h) {
-  const float s = sigmoid(g), gs = g * s;
-  h = gs * u;
-  du = dh * gs;
-  dg = dh * u * s * fmaf(g, 1.f - s, 1.f);
+// h = g s u, du = dh g s, dg = dh u s (1 + g - g s)
+__device__ __forceinline__ void swiglu_back(float2 dh, float2 g, float2 u, float2& dg, float2& du, float2& h) {
+  const float2 s = sigmoid2(g), gs = mul2(g, s);
+  h = mul2(gs, u);
+  du = mul2(dh, gs);
+  dg = mul2(mul2(mul2(dh, u), s), add2(fma2(gs, both(-1.f), g), both(1.f)));
 }
-template <typename T>
+template <typename T, int V>
 __global__ void __launch_bounds__(kBlock8) swiglu8_backward_kernel(const Swiglu8BackArgs a) {
-  const int groups = (int)((a.width + kGroup - 1) / kGroup), units = (int)(a.width / 8);
-  const int64_t total = a.rows * units;
-  Walk w((int64_t)blockIdx.x * kBlock8 + threadIdx.x, (int64_t)gridDim.x * kBlock8, units);
-  for (int64_t i = (int64_t)blockIdx.x * kBlock8 + threadIdx.x; i < total; i += (int64_t)gridDim.x * kBlock8, w.next()) {
-    const int c = w.unit * 8;
+  constexpr int L = kGroup / V;
+  const int groups = (int)((a.width + kGroup - 1) / kGroup), units = (int)(a.width / V);
+  const int64_t total = a.rows * units, stride = (int64_t)gridDim.x * kBlock8;
+  int64_t i = (int64_t)blockIdx.x * kBlock8 + threadIdx.x;
+  Walk w(i, stride, units);
+  for (; i < total; i += stride, w.next()) {
+    const int c = w.unit * V;
     const int8_t* q = a.q + w.row * a.ld_q + c;
-    const uint8_t* e = a.e + w.row * a.ld_e + (w.unit >> 2);
-    const uint2 qg = __ldcs(reinterpret_cast<const uint2*>(q)), qu = __ldcs(reinterpret_cast<const uint2*>(q + a.width));
-    float dh[8], g[8], u[8], h[8];
-    load8<T>(static_cast<const T*>(a.dh) + w.row * a.ld_dh + c, dh);
-    dequantise8(qg, step_of(e[0]), g);
-    dequantise8(qu, step_of(e[groups]), u);
+    const uint8_t* e = a.e + w.row * a.ld_e + w.unit / L;
+    const Bytes<V> qg = __ldcs(reinterpret_cast<const Bytes<V>*>(q)), qu = __ldcs(reinterpret_cast<const Bytes<V>*>(q + a.width));
+    const Vals<V> dh = load_vals<T, V>(static_cast<const T*>(a.dh) + w.row * a.ld_dh + c);
+    const Vals<V> g = dequantise<V>(qg, step_of(e[0])), u = dequantise<V>(qu, step_of(e[groups]));
+    Vals<V> dg, du, h;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) swiglu_back(dh[j], g[j], u[j], g[j], u[j], h[j]);
+    for (int j = 0; j < V / 2; ++j) {
+      float2 x, y, z;
+      swiglu_back(dh.pair(j), g.pair(j), u.pair(j), x, y, z);
+      dg.set(j, x); du.set(j, y); h.set(j, z);
+    }
     T* out = static_cast<T*>(a.dgu) + w.row * a.ld_dgu + c;
-    store8<T>(out, g);
-    store8<T>(out + a.width, u);
-    if (a.h) store8<T>(static_cast<T*>(a.h) + w.row * a.ld_h + c, h);
+    store_vals<T, V>(out, dg);
+    store_vals<T, V>(out + a.width, du);
+    if (a.h) store_vals<T, V>(static_cast<T*>(a.h) + w.row * a.ld_h + c, h);
   }
 }
 
-// ---- element kernels: a warp is a group, a lane a value
+// ---- element kernels: a warp takes four neighbouring groups of a row at a time, a lane one value of each
+constexpr int kSpan = 4;
+__device__ __forceinline__ int spans_of(int64_t width) { return (int)((width + kSpan * kGroup - 1) / (kSpan * kGroup)); }
+
 template <typename T>
 __global__ void __launch_bounds__(kBlock8) act8_save_elem_kernel(const Act8Args a) {
-  const int groups = (int)((a.width + kGroup - 1) / kGroup), lane = threadIdx.x & 31;
-  const int64_t stride = (int64_t)gridDim.x * (kBlock8 / 32), total = a.rows * groups;
+  const int groups = (int)((a.width + kGroup - 1) / kGroup), spans = spans_of(a.width), lane = threadIdx.x & 31;
+  const int64_t stride = (int64_t)gridDim.x * (kBlock8 / 32), total = a.rows * spans;
   int64_t i = (int64_t)blockIdx.x * (kBlock8 / 32) + (threadIdx.x >> 5);
-  Walk w(i, stride, groups);
+  Walk w(i, stride, spans);
   for (; i < total; i += stride, w.next()) {
-    const int64_t c = (int64_t)w.unit * kGroup + lane;
-    const bool real = c < a.width;
-    const float f = real ? to_f32<T>(static_cast<const T*>(a.x)[w.row * a.ld_x + c]) : 0.f;
-    const uint32_t e = step_exponent(warp_max(abs_bits(f)));
-    if (real) a.q[w.row * a.ld_q + c] = (int8_t)to_q8(f, inverse_step(e));
-    if (lane == 0) a.e[w.row * a.ld_e + w.unit] = (uint8_t)e;
+    const int g0 = w.unit * kSpan;
+    const T* x = static_cast<const T*>(a.x) + w.row * a.ld_x;
+    float f[kSpan];
+#pragma unroll
+    for (int k = 0; k < kSpan; ++k) {
+      const int64_t c = (int64_t)(g0 + k) * kGroup + lane;
+      f[k] = c < a.width ? to_f32<T>(x[c]) : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < kSpan; ++k) {
+      const int64_t c = (int64_t)(g0 + k) * kGroup + lane;
+      const uint32_t e = step_exponent(warp_max(abs_bits(f[k])));
+      if (c < a.width) a.q[w.row * a.ld_q + c] = (int8_t)to_q8(f[k], inverse_step(e));
+      if (lane == 0 && g0 + k < groups) a.e[w.row * a.ld_e + g0 + k] = (uint8_t)e;
+    }
   }
 }
 template <typename T>
 __global__ void __launch_bounds__(kBlock8) act8_load_elem_kernel(const Act8Args a) {
-  const int groups = (int)((a.width + kGroup - 1) / kGroup), lane = threadIdx.x & 31;
-  const int64_t stride = (int64_t)gridDim.x * (kBlock8 / 32), total = a.rows * groups;
+  const int spans = spans_of(a.width), lane = threadIdx.x & 31;
+  const int64_t stride = (int64_t)gridDim.x * (kBlock8 / 32), total = a.rows * spans;
   int64_t i = (int64_t)blockIdx.x * (kBlock8 / 32) + (threadIdx.x >> 5);
-  Walk w(i, stride, groups);
+  Walk w(i, stride, spans);
   for (; i < total; i += stride, w.next()) {
-    const int64_t c = (int64_t)w.unit * kGroup + lane;
-    if (c < a.width) static_cast<T*>(a.out)[w.row * a.ld_out + c] = from_f32<T>((float)a.q[w.row * a.ld_q + c] * step_of(a.e[w.row * a.ld_e + w.unit]));
+    float q[kSpan], s[kSpan];
+#pragma unroll
+    for (int k = 0; k < kSpan; ++k) {
+      const int64_t c = (int64_t)(w.unit * kSpan + k) * kGroup + lane;
+      const bool real = c < a.width;
+      q[k] = real ? (float)a.q[w.row * a.ld_q + c] : 0.f;
+      s[k] = real ? step_of(a.e[w.row * a.ld_e + w.unit * kSpan + k]) : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < kSpan; ++k) {
+      const int64_t c = (int64_t)(w.unit * kSpan + k) * kGroup + lane;
+      if (c < a.width) static_cast<T*>(a.out)[w.row * a.ld_out + c] = from_f32<T>(q[k] * s[k]);
+    }
   }
 }
 template <typename T>
 __global__ void __launch_bounds__(kBlock8) swiglu8_forward_elem_kernel(const Act8Args a) {
-  const int groups = (int)((a.width + kGroup - 1) / kGroup), lane = threadIdx.x & 31;
-  const int64_t stride = (int64_t)gridDim.x * (kBlock8 / 32), total = a.rows * groups;
+  const int groups = (int)((a.width + kGroup - 1) / kGroup), spans = spans_of(a.width), lane = threadIdx.x & 31;
+  const int64_t stride = (int64_t)gridDim.x * (kBlock8 / 32), total = a.rows * spans;
   int64_t i = (int64_t)blockIdx.x * (kBlock8 / 32) + (threadIdx.x >> 5);
-  Walk w(i, stride, groups);
+  Walk w(i, stride, spans);
   for (; i < total; i += stride, w.next()) {
-    const int64_t c = (int64_t)w.unit * kGroup + lane;
-    const bool real = c < a.width;
+    const int g0 = w.unit * kSpan;
     const T* row = static_cast<const T*>(a.x) + w.row * a.ld_x;
-    const float g = real ? to_f32<T>(row[c]) : 0.f, u = real ? to_f32<T>(row[a.width + c]) : 0.f;
-    const uint32_t eg = step_exponent(warp_max(abs_bits(g))), eu = step_exponent(warp_max(abs_bits(u)));
-    if (real) {
-      int8_t* q = a.q + w.row * a.ld_q + c;
-      q[0] = (int8_t)to_q8(g, inverse_step(eg));
-      q[a.width] = (int8_t)to_q8(u, inverse_step(eu));
-      static_cast<T*>(a.out)[w.row * a.ld_out + c] = from_f32<T>(g * sigmoid(g) * u);
+    float2 f[kSpan];
+#pragma unroll
+    for (int k = 0; k < kSpan; ++k) {
+      const int64_t c = (int64_t)(g0 + k) * kGroup + lane;
+      f[k] = c < a.width ? make_float2(to_f32<T>(row[c]), to_f32<T>(row[a.width + c])) : both(0.f);
     }
-    if (lane == 0) {
-      uint8_t* e = a.e + w.row * a.ld_e + w.unit;
-      e[0] = (uint8_t)eg;
-      e[groups] = (uint8_t)eu;
+#pragma unroll
+    for (int k = 0; k < kSpan; ++k) {
+      const int64_t c = (int64_t)(g0 + k) * kGroup + lane;
+      const uint32_t eg = step_exponent(warp_max(abs_bits(f[k].x))), eu = step_exponent(warp_max(abs_bits(f[k].y)));
+      if (c < a.width) {
+        int8_t* q = a.q + w.row * a.ld_q + c;
+        q[0] = (int8_t)to_q8(f[k].x, inverse_step(eg));
+        q[a.width] = (int8_t)to_q8(f[k].y, inverse_step(eu));
+        static_cast<T*>(a.out)[w.row * a.ld_out + c] = from_f32<T>(f[k].x * sigmoid2(both(f[k].x)).x * f[k].y);
+      }
+      if (lane == 0 && g0 + k < groups) {
+        uint8_t* e = a.e + w.row * a.ld_e + g0 + k;
+        e[0] = (uint8_t)eg;
+        e[groups] = (uint8_t)eu;
+      }
     }
   }
 }
 template <typename T>
 __global__ void __launch_bounds__(kBlock8) swiglu8_backward_elem_kernel(const Swiglu8BackArgs a) {
-  const int groups = (int)((a.width + kGroup - 1) / kGroup), lane = threadIdx.x & 31;
-  const int64_t stride = (int64_t)gridDim.x * (kBlock8 / 32), total = a.rows * groups;
+  const int groups = (int)((a.width + kGroup - 1) / kGroup), spans = spans_of(a.width), lane = threadIdx.x & 31;
+  const int64_t stride = (int64_t)gridDim.x * (kBlock8 / 32), total = a.rows * spans;
   int64_t i = (int64_t)blockIdx.x * (kBlock8 / 32) + (threadIdx.x >> 5);
-  Walk w(i, stride, groups);
+  Walk w(i, stride, spans);
   for (; i < total; i += stride, w.next()) {
-    const int64_t c = (int64_t)w.unit * kGroup + lane;
-    if (c >= a.width) continue;
-    const int8_t* q = a.q + w.row * a.ld_q + c;
-    const uint8_t* e = a.e + w.row * a.ld_e + w.unit;
-    float dg, du, h;
-    swiglu_back(to_f32<T>(static_cast<const T*>(a.dh)[w.row * a.ld_dh + c]), (float)q[0] * step_of(e[0]), (float)q[a.width] * step_of(e[groups]), dg, du, h);
-    T* out = static_cast<T*>(a.dgu) + w.row * a.ld_dgu + c;
-    out[0] = from_f32<T>(dg);
-    out[a.width] = from_f32<T>(du);
-    if (a.h) static_cast<T*>(a.h)[w.row * a.ld_h + c] = from_f32<T>(h);
+    float d[kSpan], g[kSpan], u[kSpan];
+#pragma unroll
+    for (int k = 0; k < kSpan; ++k) {
+      const int64_t c = (int64_t)(w.unit * kSpan + k) * kGroup + lane;
+      d[k] = g[k] = u[k] = 0.f;
+      if (c < a.width) {
+        const int8_t* q = a.q + w.row * a.ld_q + c;
+        const uint8_t* e = a.e + w.row * a.ld_e + w.unit * kSpan + k;
+        d[k] = to_f32<T>(static_cast<const T*>(a.dh)[w.row * a.ld_dh + c]);
+        g[k] = (float)q[0] * step_of(e[0]);
+        u[k] = (float)q[a.width] * step_of(e[groups]);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kSpan; ++k) {
+      const int64_t c = (int64_t)(w.unit * kSpan + k) * kGroup + lane;
+      if (c >= a.width) continue;
+      float2 dg, du, h;
+      swiglu_back(both(d[k]), both(g[k]), both(u[k]), dg, du, h);
+      T* out = static_cast<T*>(a.dgu) + w.row * a.ld_dgu + c;
+      out[0] = from_f32<T>(dg.x);
+      out[a.width] = from_f32<T>(du.x);
+      if (a.h) static_cast<T*>(a.h)[w.row * a.ld_h + c] = from_f32<T>(h.x);
+    }
   }
 }
 
 bool on16(const void* p, int64_t ld, int bytes) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (ld * bytes) % 16 == 0; }
-bool on8(const void* p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0 && ld % 8 == 0; }
+// Values per thread that width, base and stride of the stored bytes allow: 16 (16-bit activations), 8, or none (0).
+int unit_for(int dtype, const void* q, int64_t ld, int64_t width) {
+  for (int v : {16, 8})
+    if ((v == 8 || dtype != FGD_F32) && width % v == 0 && ld % v == 0 && (reinterpret_cast<uintptr_t>(q) & (uintptr_t)(v - 1)) == 0) return v;
+  return 0;
+}
 
 int check_dims(const char* who, int dtype, int64_t rows, int64_t width) {
   if (dtype_bytes(dtype) == 0) return op_fail(FGD_ERR_INVALID_ARG, "%s: unknown dtype %d", who, dtype);
@@ -301,12 +443,22 @@ int launched(const char* who) {
   return e == cudaSuccess ? FGD_OK : op_fail(FGD_ERR_CUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
 }
 
-#define FGD_BY_DTYPE(dtype, KERNEL, ...)                                             \
-  switch (dtype) {                                                                   \
-    case FGD_F32: KERNEL<float><<<__VA_ARGS__>>>(a); break;                          \
-    case FGD_BF16: KERNEL<__nv_bfloat16><<<__VA_ARGS__>>>(a); break;                 \
-    default: KERNEL<__half><<<__VA_ARGS__>>>(a); break;                              \
-  }
+// f(a value of the activation type)
+template <typename F>
+void by_dtype(int dtype, F f) {
+  if (dtype == FGD_F32) f(float{});
+  else if (dtype == FGD_BF16) f(__nv_bfloat16{});
+  else f(__half{});
+}
+// KERNEL<type, 16 or 8 values per thread>, or KERNEL_elem<type> where `unit` is 0.
+#define FGD_LAUNCH_DTYPE(KERNEL, THREADS16, THREADS8, THREADS_ELEM)                                       \
+  by_dtype(dtype, [&](auto zero) {                                                                         \
+    using T = decltype(zero);                                                                              \
+    if constexpr (sizeof(T) == 2)                                                                          \
+      if (unit == 16) { KERNEL##_kernel<T, 16><<<grid_for(THREADS16), kBlock8, 0, st>>>(a); return; }      \
+    if (unit == 8) KERNEL##_kernel<T, 8><<<grid_for(THREADS8), kBlock8, 0, st>>>(a);                       \
+    else KERNEL##_elem_kernel<T><<<grid_for(THREADS_ELEM), kBlock8, 0, st>>>(a);                           \
+  });
 
 }  // namespace
 
@@ -325,11 +477,8 @@ extern "C" int fgd_act_save8(int device, int dtype, int64_t rows, int64_t width,
   if (!dev.ok()) return op_fail(FGD_ERR_CUDA, "cannot select device %d", device);
   const Act8Args a{x, ld_x, nullptr, 0, q8, ld_q, e8, ld_e, rows, width};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (width % 8 == 0 && on16(x, ld_x, b) && on8(q8, ld_q)) {
-    FGD_BY_DTYPE(dtype, act8_save_kernel, grid_for(rows * groups * 4), kBlock8, 0, st)
-  } else {
-    FGD_BY_DTYPE(dtype, act8_save_elem_kernel, grid_for(rows * groups * 32), kBlock8, 0, st)
-  }
+  const int unit = on16(x, ld_x, b) ? unit_for(dtype, q8, ld_q, width) : 0;
+  FGD_LAUNCH_DTYPE(act8_save, rows * groups * 2, rows * groups * 4, rows * ((groups + 3) / 4) * 32)
   return launched("fgd_act_save8");
 }
 
@@ -348,11 +497,12 @@ extern "C" int fgd_act_load8(int device, int dtype, int64_t rows, int64_t width,
   if (!dev.ok()) return op_fail(FGD_ERR_CUDA, "cannot select device %d", device);
   const Act8Args a{nullptr, 0, out, ld_out, const_cast<int8_t*>(q8), ld_q, const_cast<uint8_t*>(e8), ld_e, rows, width};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (width % 8 == 0 && on16(out, ld_out, b) && on8(q8, ld_q)) {
-    FGD_BY_DTYPE(dtype, act8_load_kernel, grid_for(rows * (width / 8)), kBlock8, 0, st)
-  } else {
-    FGD_BY_DTYPE(dtype, act8_load_elem_kernel, grid_for(rows * groups * 32), kBlock8, 0, st)
-  }
+  const int unit = on16(out, ld_out, b) ? unit_for(dtype, q8, ld_q, width) : 0;
+  by_dtype(dtype, [&](auto zero) {
+    using T = decltype(zero);
+    if (unit) act8_load_kernel<T><<<grid_for(rows * (width * (int64_t)sizeof(T) / 16)), kBlock8, 0, st>>>(a);
+    else act8_load_elem_kernel<T><<<grid_for(rows * ((groups + 3) / 4) * 32), kBlock8, 0, st>>>(a);
+  });
   return launched("fgd_act_load8");
 }
 
@@ -374,11 +524,8 @@ extern "C" int fgd_swiglu8_forward(int device, int dtype, int64_t rows, int64_t 
   if (!dev.ok()) return op_fail(FGD_ERR_CUDA, "cannot select device %d", device);
   const Act8Args a{gu, ld_gu, h, ld_h, q8, ld_q, e8, ld_e, rows, width};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (width % 8 == 0 && on16(gu, ld_gu, b) && on16(h, ld_h, b) && on8(q8, ld_q)) {
-    FGD_BY_DTYPE(dtype, swiglu8_forward_kernel, grid_for(rows * groups * 4), kBlock8, 0, st)
-  } else {
-    FGD_BY_DTYPE(dtype, swiglu8_forward_elem_kernel, grid_for(rows * groups * 32), kBlock8, 0, st)
-  }
+  const int unit = on16(gu, ld_gu, b) && on16(h, ld_h, b) ? unit_for(dtype, q8, ld_q, width) : 0;
+  FGD_LAUNCH_DTYPE(swiglu8_forward, rows * groups * 2, rows * groups * 4, rows * ((groups + 3) / 4) * 32)
   return launched("fgd_swiglu8_forward");
 }
 
@@ -400,10 +547,7 @@ extern "C" int fgd_swiglu8_backward(int device, int dtype, int64_t rows, int64_t
   if (!dev.ok()) return op_fail(FGD_ERR_CUDA, "cannot select device %d", device);
   const Swiglu8BackArgs a{dh, ld_dh, q8, ld_q, e8, ld_e, dgu, ld_dgu, h, ld_h, rows, width};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (width % 8 == 0 && on16(dh, ld_dh, b) && on16(dgu, ld_dgu, b) && (!h || on16(h, ld_h, b)) && on8(q8, ld_q)) {
-    FGD_BY_DTYPE(dtype, swiglu8_backward_kernel, grid_for(rows * (width / 8)), kBlock8, 0, st)
-  } else {
-    FGD_BY_DTYPE(dtype, swiglu8_backward_elem_kernel, grid_for(rows * groups * 32), kBlock8, 0, st)
-  }
+  const int unit = on16(dh, ld_dh, b) && on16(dgu, ld_dgu, b) && (!h || on16(h, ld_h, b)) ? unit_for(dtype, q8, ld_q, width) : 0;
+  FGD_LAUNCH_DTYPE(swiglu8_backward, rows * (width / 16), rows * (width / 8), rows * ((groups + 3) / 4) * 32)
   return launched("fgd_swiglu8_backward");
 }
