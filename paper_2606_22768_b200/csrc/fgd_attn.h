@@ -13,7 +13,7 @@ namespace fgd {
 
 // A tile of rows of one sequence.  Tiles do not depend on heads or widths: a CTA's (tile, head) pair
 // comes from its index.
-struct AttnTile {
+struct alignas(16) AttnTile {
   int32_t start;   // first token of the sequence
   int32_t len;     // tokens of the sequence
   int32_t row;     // first row of the tile, counted from the sequence's start

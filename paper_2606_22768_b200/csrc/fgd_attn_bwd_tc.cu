@@ -3,15 +3,17 @@
 // key.  Each recomputes S and dP, seven products instead of five, and in return every sum stays in one CTA's tensor
 // memory: no atomics, no fp32 copy of dQ in memory, results that are bit-identical from run to run.
 //
-// Both kernels: ten warps, one CTA per SM, persistent.  Warps 0-7 do the element-wise part, two threads per row: thread
-// (half h, lane r) owns row r and columns [64 h, 64 h + 64) of a 128 x 128 tile; warp 8 loads by TMA, warp 9 issues MMAs.
-// A 16-bit factor goes back into tensor memory over the fp32 scores it came from, inside the columns that the same thread
-// has read: its two halves of 32 packed columns start 64 columns apart.
+// Both kernels: ten warps, one CTA per SM, persistent.  The CTA's own tile is 128 rows (a tensor-memory lane each); the other side
+// comes in blocks of 64 rows.  Two groups of four warps take the blocks by turns, one thread per row and 64 columns: each group has
+// its own S and dP columns, so one group's waits (a product and its way to the waiting warp take about 450 clocks beyond the product
+// itself) are the other's work, and the next block's products are issued before this block's sums.
+// Warp 8 loads by TMA, warp 9 issues the MMAs.  A 16-bit factor goes back into tensor memory over the fp32 values it came from.
 //
-// Query kernel, tensor memory S0 | S1 | dP | dQ:   S = Q K^T (two buffers, one block ahead), dP = dO V^T,
-//     dS = P o (dP - delta) over dP, dQ += dS K.
-// Key kernel, tensor memory S^T | dP^T | dV | dK:  S^T = K Q^T, P^T over S^T, dV += P^T dO, and while dS^T is formed the next S^T runs;
-//     dP^T = V dO^T, dS^T over dP^T, dK += dS^T Q, and while P^T of the next block is formed the next dP^T runs.
+// Query kernel, tensor memory S0 | S1 | dP0 | dP1 | dQ | Q | dO:  S = Q K^T, dP = dO V^T, dS = P o (dP - delta) over dP, dQ += dS K.
+//     Q and dO are operands from tensor memory, copied there once per item: with 64-row blocks a shared-memory A would be read
+//     twice as often and shared memory, not the MMAs, would set the pace.
+// Key kernel, tensor memory S0 | S1 | dP0 | dP1 | dV | dK:  S^T = K Q^T, P^T over S^T, dV += P^T dO, dP^T = V dO^T, dS^T over dP^T,
+//     dK += dS^T Q.  K and V have two buffers, so that the next item's are there when its first product is due.
 // `scale` multiplies dQ and dK once, at the end.
 #include "fgd_attn_tc.cuh"
 
@@ -20,42 +22,78 @@ using namespace fgd;
 namespace {
 
 constexpr int kBwdThreads = 320;
-constexpr int kQStagesK = 3, kQStagesV = 2;      // query kernel: K tiles stay for two products, V tiles for one
+constexpr int kBlock = 64;                            // rows of a block
 
-template <int DP> constexpr size_t dq_smem() { return 1024 + (size_t)(2 + kQStagesK + kQStagesV) * attn_tile_bytes<DP>(); }
-// key kernel: K, V, two stages of Q and dO, and the rows' lse and delta beside each stage
-template <int DP> constexpr size_t dkv_smem() { return 1024 + (size_t)6 * attn_tile_bytes<DP>() + 2 * 2 * 128 * sizeof(float); }
+template <int DP> constexpr uint32_t kTile = 128 * DP * 2;       // bytes of the CTA's own tile of one tensor
+template <int DP> constexpr uint32_t kBlk = kBlock * DP * 2;     // bytes of a block of one tensor
+// query kernel: stages of K (needed by two products) and of V
+constexpr int kStagesK = 6, kStagesV = 3;
+template <int DP> constexpr size_t dq_smem() { return 1024 + 2 * kTile<DP> + (kStagesK + kStagesV) * kBlk<DP>; }
+// key kernel: two buffers of K and V, stages of (Q, dO) blocks, and their rows' lse and delta
+template <int DP> constexpr int kStagesQ = DP == 128 ? 3 : 4;
+template <int DP> constexpr size_t dkv_smem() { return 1024 + 4 * kTile<DP> + 2 * kStagesQ<DP> * kBlk<DP> + kStagesQ<DP> * 2 * kBlock * sizeof(float); }
 
-// p and dS of one thread's 64 columns; packs 16-bit values two to a register
 template <bool BF16>
-__device__ __forceinline__ void pack64(const float (&x)[64], uint32_t (&w)[32]) {
+__device__ __forceinline__ void store_pairs(uint32_t addr, const float2 (&x)[32]) {
+  uint32_t w[32];
 #pragma unroll
-  for (int k = 0; k < 32; ++k) w[k] = pack2<BF16>(x[2 * k], x[2 * k + 1]);
+  for (int k = 0; k < 32; ++k) w[k] = pack2<BF16>(x[k].x, x[k].y);
+  tmem_st_32(addr, w);
+  tmem_st_wait();
+  tc_fence_before();
+}
+// 64 columns of this thread's row
+__device__ __forceinline__ void load_row64(uint32_t addr, uint32_t (&s)[64]) {
+  tmem_ld_32(addr, s);
+  tmem_ld_32(addr + 32, s + 32);
+  tmem_ld_done<64>(s);
 }
 
 // ------------------------------------------------------------------------------------------ dQ
+// Blocks of an item: keys [64 j, 64 j + 64), from the last block that the tile's rows see down to block 0.
+__device__ __forceinline__ int dq_blocks(const AttnTile& t) { return (min(t.row + kAttnRows, t.len) + kBlock - 1) / kBlock; }
+
+// Two consecutive words of 16-bit values of a tile in shared memory (128-byte swizzle) go to tensor memory: row r of the tile to lane r.
+template <int DP>
+__device__ __forceinline__ void tile_row_to_tmem(const unsigned char* tile, int r, uint32_t addr) {
+#pragma unroll
+  for (int b = 0; b < DP / 64; ++b) {
+    uint32_t w[32];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const uint4 v = *reinterpret_cast<const uint4*>(tile + b * kAttnBox + r * 128 + ((c ^ (r & 7)) << 4));
+      w[4 * c] = v.x; w[4 * c + 1] = v.y; w[4 * c + 2] = v.z; w[4 * c + 3] = v.w;
+    }
+    tmem_st_32(addr + 32 * b, w);
+  }
+  tmem_st_wait();
+  tc_fence_before();
+}
+
 template <int DP, bool BF16>
 __global__ void __launch_bounds__(kBwdThreads, 1)
-attn_dq_tc_kernel(const AttnArgs a, int64_t items, const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
+attn_dq_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                   const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo) {
-  constexpr uint32_t TILE = attn_tile_bytes<DP>();
-  constexpr int SK = kQStagesK, SV = kQStagesV;
+  constexpr uint32_t TILE = kTile<DP>, BLK = kBlk<DP>;
+  constexpr int SK = kStagesK, SV = kStagesV;
   extern __shared__ unsigned char smem_raw[];
-  // q_full, q_empty, raw, done, dp_full, ds_full, dq_done, dq_free | s_full[2] | k_full[SK], k_empty[SK], v_full[SV], v_empty[SV]
-  __shared__ __align__(8) unsigned long long bars[10 + 2 * (SK + SV)];
+  __shared__ __align__(8) unsigned long long bars[14 + 2 * (SK + SV)];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
   unsigned char* base = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  const uint32_t sq = smem_u32(base), sdo = sq + TILE, sk = sdo + TILE, sv = sk + SK * TILE;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint32_t b0 = smem_u32(bars);
-  const uint32_t q_full = b0, q_empty = b0 + 8, raw = b0 + 16, done = b0 + 24, dp_full = b0 + 32, ds_full = b0 + 40, dq_done = b0 + 48, dq_free = b0 + 56,
-                 s_full = b0 + 64, k_full = b0 + 80, k_empty = k_full + 8 * SK, v_full = k_empty + 8 * SK, v_empty = v_full + 8 * SV;
+  const uint32_t sq = smem_u32(base), sdo = sq + TILE, sk = sdo + TILE, sv = sk + SK * BLK;
+  const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
+  // qd_full: Q and dO are in shared memory; qd_read: and have been copied; qd_in: they are in tensor memory; qd_done: the item's
+  // products with them are done
+  const uint32_t b0 = smem_u32(bars), qd_full = b0, qd_read = b0 + 8, qd_in = b0 + 16, qd_done = b0 + 24, raw = b0 + 32, done = b0 + 40, dq_done = b0 + 48,
+                 dq_free = b0 + 56, s_full = b0 + 64, dp_full = b0 + 80, ds_full = b0 + 96, k_full = b0 + 112, k_empty = k_full + 8 * SK,
+                 v_full = k_empty + 8 * SK, v_empty = v_full + 8 * SV;
   if (tid == 0) {
     abort_flag = 0;
-    for (uint32_t b : {q_full, q_empty, raw, done, dp_full, dq_done, s_full, s_full + 8}) mbar_init(b, 1);
-    mbar_init(ds_full, 256);
-    mbar_init(dq_free, 256);
+    for (uint32_t b : {qd_full, qd_done, raw, done, dq_done, s_full, s_full + 8, dp_full, dp_full + 8}) mbar_init(b, 1);
+    for (uint32_t b : {qd_read, qd_in, dq_free}) mbar_init(b, 256);
+    mbar_init(ds_full, 128);
+    mbar_init(ds_full + 8, 128);
     for (int s = 0; s < 2 * (SK + SV); ++s) mbar_init(k_full + 8 * s, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -66,183 +104,171 @@ attn_dq_tc_kernel(const AttnArgs a, int64_t items, const __grid_constant__ CUten
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = tmem_slot, c_dp = 256, c_dq = 384;
+  const uint32_t tmem = (uint32_t)uniform((int)tmem_slot), c_dp = 128, c_dq = 256, c_q = 256 + DP, c_do = c_q + DP / 2;
   const AttnWait wait{&abort_flag, a.status};
   const int group = a.hq / a.hk;
-  auto item = [&](int64_t w, AttnTile& t, int& head, int& n) {
-    t = a.tiles[(int)(w / a.hq)];
-    head = (int)(w % a.hq);
-    n = t.row / kAttnRows + 1;
-  };
 
   if (warp == 8) {
     // ================================================================= loads: K and V of every block, from the diagonal down
     uint32_t u = 0, n_raw = 0;
-    int round = 0;
     bool ok = true;
-    for (; ok; ++round) {
-      const int64_t w = work_item(round);
-      if ((int64_t)round * gridDim.x >= items) break;
-      if (w >= items) continue;
-      AttnTile t;
-      int head, n;
-      item(w, t, head, n);
-      if (!(ok = wait(q_empty, (round & 1) ^ 1))) break;
+    ItemWalk walk(a.tiles, a.hq, items);
+    for (; ok && walk.valid; walk.next()) {
+      const AttnTile t = walk.t;
+      const int kvh = walk.h / group;
+      if (!(ok = wait(qd_read, (walk.round & 1) ^ 1))) break;
       if (elect_one()) {
-        mbar_expect_tx(q_full, 2 * TILE);
-        load_tile<DP>(sq, &mq, head, t.start + t.row, q_full);
-        load_tile<DP>(sdo, &mdo, head, t.start + t.row, q_full);
+        mbar_expect_tx(qd_full, 2 * TILE);
+        load_tile<DP>(sq, &mq, walk.h, t.start + t.row, qd_full);
+        load_tile<DP>(sdo, &mdo, walk.h, t.start + t.row, qd_full);
       }
-      for (int jb = n - 1; ok && jb >= 0; --jb, ++u) {
-        const int token = t.start + jb * 128, rows = t.len - jb * 128;
+      for (int j = dq_blocks(t) - 1; ok && j >= 0; --j, ++u) {
+        const int token = t.start + j * kBlock, rows = t.len - j * kBlock;
         const uint32_t ik = u % SK, iv = u % SV, kb = k_full + 8 * ik, vb = v_full + 8 * iv;
         if (!(ok = wait(k_empty + 8 * ik, ((u / SK) & 1) ^ 1))) break;
-        if (rows >= 128) {
+        if (rows >= kBlock) {
           if (elect_one()) {
-            mbar_expect_tx(kb, TILE);
-            load_tile<DP>(sk + ik * TILE, &mk, head / group, token, kb);
+            mbar_expect_tx(kb, BLK);
+            load_tile<DP, kBlock>(sk + ik * BLK, &mk, kvh, token, kb);
           }
         } else {     // dQ = dS K must not meet the next sequence's keys
           if (elect_one()) {
-            mbar_expect_tx(raw, TILE);
-            load_tile<DP>(sk + ik * TILE, &mk, head / group, token, raw);
+            mbar_expect_tx(raw, BLK);
+            load_tile<DP, kBlock>(sk + ik * BLK, &mk, kvh, token, raw);
           }
           ok = wait(raw, n_raw & 1);
           ++n_raw;
           if (!ok) { drain_wait(raw, (n_raw - 1) & 1); break; }
-          zero_rows<DP>(base + 2 * TILE + ik * TILE, rows, lane);
+          zero_rows<DP, kBlock>(base + 2 * TILE + ik * BLK, rows, lane);
           if (elect_one()) mbar_arrive(kb);
         }
         if (!(ok = wait(v_empty + 8 * iv, ((u / SV) & 1) ^ 1))) break;
         if (elect_one()) {
-          mbar_expect_tx(vb, TILE);
-          load_tile<DP>(sv + iv * TILE, &mv, head / group, token, vb);
+          mbar_expect_tx(vb, BLK);
+          load_tile<DP, kBlock>(sv + iv * BLK, &mv, kvh, token, vb);
         }
       }
     }
     if (wait.given_up()) {
-      const int r = round > 0 && !ok ? round : round - 1;
-      if (r >= 0) drain_wait(q_full, r & 1);
+      drain_wait(qd_full, walk.round & 1);
+      if (walk.round > 0) drain_wait(qd_full, (walk.round - 1) & 1);
       for (uint32_t k = u > (uint32_t)SK ? u - SK : 0; k <= u; ++k) drain_wait(k_full + 8 * (k % SK), (k / SK) & 1);
       for (uint32_t k = u > (uint32_t)SV ? u - SV : 0; k <= u; ++k) drain_wait(v_full + 8 * (k % SV), (k / SV) & 1);
     }
   } else if (warp == 9) {
     // ================================================================= MMAs
-    uint32_t u = 0;         // block index over all items
-    int n_ds = 0;
     bool ok = true;
-    auto score = [&](uint32_t k) {      // S of block k into buffer k & 1
-      if (!wait(k_full + 8 * (k % SK), (k / SK) & 1)) return false;
+    // products of the block that `ahead` points at (block index ua over all items)
+    ItemWalk ahead(a.tiles, a.hq, items);
+    int ia = 0, na = ahead.valid ? dq_blocks(ahead.t) : 0;
+    uint32_t ua = 0;
+    auto products = [&]() {
+      if (!ahead.valid) return true;
+      if (ia == 0 && !wait(qd_in, ahead.round & 1)) return false;
+      const uint32_t ik = ua % SK, iv = ua % SV, b = ua & 1;
+      if (!wait(k_full + 8 * ik, (ua / SK) & 1)) return false;
       tc_fence_after();
-      if (elect_one()) {
-        mma_columns<BF16, DP>(tmem + 128 * (k & 1), sq, sk + (k % SK) * TILE);
-        umma_commit(s_full + 8 * (k & 1));
+      mma_columns_t<BF16, DP, kBlock>(tmem + 64 * b, tmem + c_q, sk + ik * BLK);
+      mma_commit(s_full + 8 * b);
+      if (!wait(v_full + 8 * iv, (ua / SV) & 1)) return false;
+      tc_fence_after();
+      mma_columns_t<BF16, DP, kBlock>(tmem + c_dp + 64 * b, tmem + c_do, sv + iv * BLK);
+      mma_commit(dp_full + 8 * b);
+      mma_commit(v_empty + 8 * iv);
+      if (ia == na - 1) mma_commit(qd_done);
+      ++ua;
+      if (++ia == na) {
+        ahead.next();
+        ia = 0;
+        na = ahead.valid ? dq_blocks(ahead.t) : 0;
       }
       return true;
     };
-    auto dprob = [&](uint32_t k) {
-      if (!wait(v_full + 8 * (k % SV), (k / SV) & 1)) return false;
-      tc_fence_after();
-      if (elect_one()) {
-        mma_columns<BF16, DP>(tmem + c_dp, sdo, sv + (k % SV) * TILE);
-        umma_commit(dp_full);
-        umma_commit(v_empty + 8 * (k % SV));
-      }
-      return true;
-    };
-    int done_items = 0;
-    for (int round = 0; ok; ++round) {
-      const int64_t w = work_item(round);
-      if ((int64_t)round * gridDim.x >= items) break;
-      if (w >= items) continue;
-      AttnTile t;
-      int head, n;
-      item(w, t, head, n);
-      if (!(ok = wait(q_full, round & 1))) break;
-      if (!(ok = score(u) && dprob(u) && (n == 1 || score(u + 1)))) break;
-      if (n == 1 && elect_one()) umma_commit(q_empty);
+    ok = products() && products();
+    uint32_t u = 0;
+    for (ItemWalk walk(a.tiles, a.hq, items); ok && walk.valid; walk.next()) {
+      const int n = dq_blocks(walk.t);
       for (int i = 0; i < n; ++i, ++u) {
-        if (!(ok = wait(ds_full, n_ds & 1))) break;
-        ++n_ds;
-        if (i == 0 && !(ok = wait(dq_free, (done_items & 1) ^ 1))) break;
+        const uint32_t b = u & 1;
+        if (!(ok = wait(ds_full + 8 * b, (u >> 1) & 1))) break;
+        if (i == 0 && !(ok = wait(dq_free, (walk.round & 1) ^ 1))) break;
         tc_fence_after();
-        if (elect_one()) {
-          mma_rows<BF16, DP>(tmem + c_dq, tmem + c_dp, 64, sk + (u % SK) * TILE, i > 0);
-          if (i == n - 1) umma_commit(dq_done);
-          umma_commit(k_empty + 8 * (u % SK));
-        }
-        if (i + 1 < n && !(ok = dprob(u + 1))) break;
-        if (i + 2 < n && !(ok = score(u + 2))) break;
-        if (i + 2 == n && elect_one()) umma_commit(q_empty);      // the item's last product with Q and dO is on its way
+        mma_half_rows<BF16, DP, kBlock>(tmem + c_dq, tmem + c_dp + 64 * b, sk + (u % SK) * BLK, 0, i > 0);
+        mma_commit(k_empty + 8 * (u % SK));
+        if (i == n - 1) mma_commit(dq_done);
+        if (!(ok = products())) break;
       }
-      ++done_items;
     }
-    if (elect_one()) umma_commit(done);
+    mma_commit(done);
     drain_wait(done, 0);
   } else {
-    // ================================================================= P, dS, and dQ's way out
-    const int r = (warp & 3) * 32 + lane, h = warp >> 2;
+    // ================================================================= P, dS; Q and dO into tensor memory; dQ's way out
+    const int r = (warp & 3) * 32 + lane, g = warp >> 2;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const float c = a.scale * kLog2e;
-    uint32_t u = 0;
-    int n_items = 0;
+    const uint32_t ts = tmem + 64 * g + lanes, td = tmem + c_dp + 64 * g + lanes;
+    const float2 c2 = both(a.scale * kLog2e);
+    uint32_t u = 0;                // first block of the item
+    uint32_t mine = 0;             // blocks this group has done
     bool ok = true;
-    for (int round = 0; ok; ++round) {
-      const int64_t w = work_item(round);
-      if ((int64_t)round * gridDim.x >= items) break;
-      if (w >= items) continue;
-      AttnTile t;
-      int head, n;
-      item(w, t, head, n);
+    ItemWalk walk(a.tiles, a.hq, items);
+    // group 0 copies Q, group 1 dO, once the previous item's products are done
+    auto copy_in = [&](int round) {
+      if (round > 0 && !wait(qd_done, (round - 1) & 1)) return false;
+      if (!wait(qd_full, round & 1)) return false;
+      tc_fence_after();
+      tile_row_to_tmem<DP>(base + g * TILE, r, tmem + (g ? c_do : c_q) + lanes);
+      mbar_arrive(qd_read);
+      mbar_arrive(qd_in);
+      return true;
+    };
+    if (walk.valid) ok = copy_in(0);
+    while (ok && walk.valid) {
+      const AttnTile t = walk.t;
+      const int n = dq_blocks(t), head = walk.h, round = walk.round;
+      const int64_t row = t.start + t.row + r, at = (int64_t)head * a.tokens + row;
       const bool real = t.row + r < t.len;
-      const int64_t at = (int64_t)head * a.tokens + t.start + t.row + r;
-      const float lse = real ? a.lse[at] * kLog2e : 0.f, delta = real ? a.delta[at] : 0.f;
-      for (int i = 0; i < n; ++i, ++u) {
-        if (!(ok = wait(s_full + 8 * (u & 1), (u >> 1) & 1))) break;
+      const float2 lse2 = both(real ? -a.lse[at] * kLog2e : 0.f), delta2 = both(real ? -a.delta[at] : 0.f);
+      for (int i = (g ^ u) & 1; i < n; i += 2, ++mine) {
+        const int over = (n - 1 - i) * kBlock - t.row - r;      // column k is masked where k + over > 0
+        if (!(ok = wait(s_full + 8 * g, mine & 1))) break;
         tc_fence_after();
         uint32_t s[64];
-        const uint32_t ts = tmem + 128 * (u & 1) + 64 * h + lanes, td = tmem + c_dp + 64 * h + lanes;
-        tmem_ld_32(ts, s);
-        tmem_ld_32(ts + 32, s + 32);
-        tmem_ld_done<64>(s);
-        float p[64];
+        float2 p[32];
+        load_row64(ts, s);
 #pragma unroll
-        for (int k = 0; k < 64; ++k) p[k] = exp2_fast(fmaf(__uint_as_float(s[k]), c, -lse));
-        if (i == 0) {
-#pragma unroll
-          for (int k = 0; k < 64; ++k)
-            if (64 * h + k > r) p[k] = 0.f;
+        for (int k = 0; k < 32; ++k) {
+          p[k] = fma2(two(s + 2 * k), c2, lse2);
+          p[k].x = exp2_fast(p[k].x);
+          p[k].y = exp2_fast(p[k].y);
         }
-        if (!(ok = wait(dp_full, u & 1))) break;
+        if (!(ok = wait(dp_full + 8 * g, mine & 1))) break;
         tc_fence_after();
-        tmem_ld_32(td, s);
-        tmem_ld_32(td + 32, s + 32);
-        tmem_ld_done<64>(s);
-        const bool diagonal = i == 0;
+        load_row64(td, s);
 #pragma unroll
-        for (int k = 0; k < 64; ++k) p[k] *= __uint_as_float(s[k]) - delta;
-        if (diagonal) {      // (0 times a non-finite dP of a masked place)
+        for (int k = 0; k < 32; ++k) p[k] = mul2(p[k], add2(two(s + 2 * k), delta2));
+        if (i < 2) {      // the blocks that the diagonal can cross (0 times a non-finite value of a masked place is not 0)
 #pragma unroll
-          for (int k = 0; k < 64; ++k)
-            if (64 * h + k > r) p[k] = 0.f;
+          for (int k = 0; k < 32; ++k) {
+            if (2 * k + over > 0) p[k].x = 0.f;
+            if (2 * k + 1 + over > 0) p[k].y = 0.f;
+          }
         }
-        uint32_t ds[32];
-        pack64<BF16>(p, ds);
-        tmem_st_32(td, ds);
-        tmem_st_wait();
-        tc_fence_before();
-        mbar_arrive(ds_full);
+        store_pairs<BF16>(td, p);
+        mbar_arrive(ds_full + 8 * g);
       }
-      if (!ok || !(ok = wait(dq_done, n_items & 1))) break;
-      ++n_items;
+      if (!ok) break;
+      u += n;
+      walk.next();
+      if (walk.valid && !(ok = copy_in(round + 1))) break;      // before the wait below: the MMA warp may be waiting for it
+      if (!(ok = wait(dq_done, round & 1))) break;
       tc_fence_after();
-      char* out = a.dq.p + 2 * ((int64_t)(t.start + t.row + r) * a.dq.token + head * a.dq.head);
+      char* out = a.dq.p + 2 * (row * a.dq.token + head * a.dq.head);
 #pragma unroll
       for (int k = 0; k < DP / 2; k += 32) {
         uint32_t o[32];
-        tmem_ld_32(tmem + c_dq + h * (DP / 2) + k + lanes, o);
+        tmem_ld_32(tmem + c_dq + g * (DP / 2) + k + lanes, o);
         tmem_ld_done<32>(o);
-        if (real) store_columns<BF16, 32>(out, o, a.scale, h * (DP / 2) + k, a.d);
+        if (real) store_columns<BF16, 32>(out, o, a.scale, g * (DP / 2) + k, a.d);
       }
       tc_fence_before();
       mbar_arrive(dq_free);
@@ -257,30 +283,34 @@ attn_dq_tc_kernel(const AttnArgs a, int64_t items, const __grid_constant__ CUten
 }
 
 // ------------------------------------------------------------------------------------------ dK, dV
+// Blocks of an item: for every query head of the group, queries [64 i, 64 i + 64) from the key tile's first row to the sequence's end.
+__device__ __forceinline__ int dkv_blocks(const AttnTile& t) { return (t.len + kBlock - 1) / kBlock - t.row / kBlock; }
+
 template <int DP, bool BF16>
 __global__ void __launch_bounds__(kBwdThreads, 1)
-attn_dkv_tc_kernel(const AttnArgs a, int64_t items, const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
+attn_dkv_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                    const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo) {
-  constexpr uint32_t TILE = attn_tile_bytes<DP>();
+  constexpr uint32_t TILE = kTile<DP>, BLK = kBlk<DP>;
+  constexpr int SQ = kStagesQ<DP>;
   extern __shared__ unsigned char smem_raw[];
-  // kv_full, kv_empty, raw, done, s_full, p_full, dp_full, ds_full, out_done, out_free | q_full[2], q_empty[2], do_full[2], do_empty[2], row_full[2], row_empty[2]
-  __shared__ __align__(8) unsigned long long bars[22];
+  __shared__ __align__(8) unsigned long long bars[16 + 6 * SQ];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
   unsigned char* base = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  const uint32_t sk = smem_u32(base), sv = sk + TILE, sq = sv + TILE, sdo = sq + 2 * TILE;
-  float* row_stats = reinterpret_cast<float*>(base + 6 * TILE);      // [stage][lse | delta][128]
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint32_t b0 = smem_u32(bars);
-  const uint32_t kv_full = b0, kv_empty = b0 + 8, raw = b0 + 16, done = b0 + 24, s_full = b0 + 32, p_full = b0 + 40, dp_full = b0 + 48, ds_full = b0 + 56,
-                 out_done = b0 + 64, out_free = b0 + 72, q_full = b0 + 80, q_empty = b0 + 96, do_full = b0 + 112, do_empty = b0 + 128, row_full = b0 + 144,
-                 row_empty = b0 + 160;
+  // K0 | V0 | K1 | V1 | Q stages | dO stages | [stage][lse | delta][64]
+  const uint32_t skv = smem_u32(base), sq = skv + 4 * TILE, sdo = sq + SQ * BLK;
+  float* row_stats = reinterpret_cast<float*>(base + 4 * TILE + 2 * SQ * BLK);
+  const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
+  const uint32_t b0 = smem_u32(bars), raw = b0, done = b0 + 8, out_done = b0 + 16, out_free = b0 + 24, kv_full = b0 + 32, kv_empty = b0 + 48, s_full = b0 + 64,
+                 p_full = b0 + 80, dp_full = b0 + 96, ds_full = b0 + 112, q_full = b0 + 128, q_empty = q_full + 8 * SQ, do_full = q_empty + 8 * SQ,
+                 do_empty = do_full + 8 * SQ, row_full = do_empty + 8 * SQ, row_empty = row_full + 8 * SQ;
   if (tid == 0) {
     abort_flag = 0;
-    for (uint32_t b : {kv_full, kv_empty, raw, done, s_full, dp_full, out_done}) mbar_init(b, 1);
-    for (uint32_t b : {p_full, ds_full, out_free}) mbar_init(b, 256);
-    for (uint32_t b : {q_full, q_empty, do_full, do_empty}) { mbar_init(b, 1); mbar_init(b + 8, 1); }
-    for (int s = 0; s < 2; ++s) { mbar_init(row_full + 8 * s, 32); mbar_init(row_empty + 8 * s, 256); }
+    for (uint32_t b : {raw, done, out_done, kv_full, kv_full + 8, kv_empty, kv_empty + 8, s_full, s_full + 8, dp_full, dp_full + 8}) mbar_init(b, 1);
+    mbar_init(out_free, 256);
+    for (uint32_t b : {p_full, p_full + 8, ds_full, ds_full + 8}) mbar_init(b, 128);
+    for (int s = 0; s < 4 * SQ; ++s) mbar_init(q_full + 8 * s, 1);
+    for (int s = 0; s < SQ; ++s) { mbar_init(row_full + 8 * s, 32); mbar_init(row_empty + 8 * s, 128); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 9) {
@@ -290,223 +320,199 @@ attn_dkv_tc_kernel(const AttnArgs a, int64_t items, const __grid_constant__ CUte
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = tmem_slot, c_s = 0, c_dp = 128, c_dv = 256, c_dk = 384;
+  const uint32_t tmem = (uint32_t)uniform((int)tmem_slot), c_dp = 128, c_dv = 256, c_dk = 256 + DP;
   const AttnWait wait{&abort_flag, a.status};
   const int group = a.hq / a.hk;
-  // an item is a key tile and a key head; its blocks are the query tiles from the diagonal to the end, head by head
-  auto item = [&](int64_t w, AttnTile& t, int& kvh, int& first, int& per_head) {
-    t = a.tiles[(int)(w / a.hk)];
-    kvh = (int)(w % a.hk);
-    first = t.row / kAttnRows;
-    per_head = (t.len + kAttnRows - 1) / kAttnRows - first;
-  };
 
   if (warp == 8) {
     // ================================================================= loads
     uint32_t u = 0, n_raw = 0;
-    int round = 0;
     bool ok = true;
-    // one tile of queries or output gradients; rows beyond the sequence become zero (P^T dO and dS^T Q run over them)
-    auto rows_tile = [&](const CUtensorMap* map, uint32_t tile, uint32_t bar, int head, int token, int rows) {
-      if (rows >= 128) {
+    // one block of queries or output gradients; rows beyond the sequence become zero (P^T dO and dS^T Q run over them)
+    auto block = [&](const CUtensorMap* map, uint32_t offset, uint32_t bar, int head, int token, int rows) {
+      if (rows >= kBlock) {
         if (elect_one()) {
-          mbar_expect_tx(bar, TILE);
-          load_tile<DP>(sk + tile * TILE, map, head, token, bar);
+          mbar_expect_tx(bar, BLK);
+          load_tile<DP, kBlock>(skv + offset, map, head, token, bar);
         }
         return true;
       }
       if (elect_one()) {
-        mbar_expect_tx(raw, TILE);
-        load_tile<DP>(sk + tile * TILE, map, head, token, raw);
+        mbar_expect_tx(raw, BLK);
+        load_tile<DP, kBlock>(skv + offset, map, head, token, raw);
       }
       const bool here = wait(raw, n_raw & 1);
       ++n_raw;
       if (!here) { drain_wait(raw, (n_raw - 1) & 1); return false; }
-      zero_rows<DP>(base + tile * TILE, rows, lane);
+      zero_rows<DP, kBlock>(base + offset, rows, lane);
       if (elect_one()) mbar_arrive(bar);
       return true;
     };
-    for (; ok; ++round) {
-      const int64_t w = work_item(round);
-      if ((int64_t)round * gridDim.x >= items) break;
-      if (w >= items) continue;
-      AttnTile t;
-      int kvh, first, per_head;
-      item(w, t, kvh, first, per_head);
-      if (!(ok = wait(kv_empty, (round & 1) ^ 1))) break;
+    ItemWalk walk(a.tiles, a.hk, items);
+    for (; ok && walk.valid; walk.next()) {
+      const AttnTile t = walk.t;
+      const int kvh = walk.h, first = t.row / kBlock, per_head = dkv_blocks(t);
+      const uint32_t kb = walk.round & 1;
+      if (!(ok = wait(kv_empty + 8 * kb, ((walk.round >> 1) & 1) ^ 1))) break;
       if (elect_one()) {
-        mbar_expect_tx(kv_full, 2 * TILE);
-        load_tile<DP>(sk, &mk, kvh, t.start + t.row, kv_full);
-        load_tile<DP>(sv, &mv, kvh, t.start + t.row, kv_full);
+        mbar_expect_tx(kv_full + 8 * kb, 2 * TILE);
+        load_tile<DP>(skv + 2 * kb * TILE, &mk, kvh, t.start + t.row, kv_full + 8 * kb);
+        load_tile<DP>(skv + (2 * kb + 1) * TILE, &mv, kvh, t.start + t.row, kv_full + 8 * kb);
       }
       for (int h = 0; ok && h < group; ++h)
         for (int i = 0; ok && i < per_head; ++i, ++u) {
-          const int head = kvh * group + h, row = (first + i) * 128, rows = t.len - row;
-          const uint32_t s = u & 1, parity = ((u >> 1) & 1) ^ 1;
+          const int head = kvh * group + h, row = (first + i) * kBlock, rows = t.len - row;
+          const uint32_t s = u % SQ, parity = ((u / SQ) & 1) ^ 1;
           if (!(ok = wait(q_empty + 8 * s, parity))) break;
-          if (!(ok = rows_tile(&mq, 2 + s, q_full + 8 * s, head, t.start + row, rows))) break;
+          if (!(ok = block(&mq, 4 * TILE + s * BLK, q_full + 8 * s, head, t.start + row, rows))) break;
+          if (!(ok = wait(do_empty + 8 * s, parity))) break;
+          if (!(ok = block(&mdo, 4 * TILE + (SQ + s) * BLK, do_full + 8 * s, head, t.start + row, rows))) break;
           if (!(ok = wait(row_empty + 8 * s, parity))) break;
-          float* stats = row_stats + s * 256;
-          for (int k = lane; k < 128; k += 32) {      // rows beyond the end: P = 2^-inf = 0
+          float* stats = row_stats + s * 2 * kBlock;
+          for (int k = lane; k < kBlock; k += 32) {      // negated; rows beyond the end: P = 2^-inf = 0
             const int64_t at = (int64_t)head * a.tokens + t.start + row + k;
-            stats[k] = k < rows ? a.lse[at] * kLog2e : INFINITY;
-            stats[128 + k] = k < rows ? a.delta[at] : 0.f;
+            stats[k] = k < rows ? -a.lse[at] * kLog2e : -INFINITY;
+            stats[kBlock + k] = k < rows ? -a.delta[at] : 0.f;
           }
           mbar_arrive(row_full + 8 * s);
-          if (!(ok = wait(do_empty + 8 * s, parity))) break;
-          ok = rows_tile(&mdo, 4 + s, do_full + 8 * s, head, t.start + row, rows);
         }
     }
     if (wait.given_up()) {
-      const int r = round > 0 && !ok ? round : round - 1;
-      if (r >= 0) drain_wait(kv_full, r & 1);
-      for (uint32_t k = u > 2 ? u - 2 : 0; k <= u; ++k) {
-        drain_wait(q_full + 8 * (k & 1), (k >> 1) & 1);
-        drain_wait(do_full + 8 * (k & 1), (k >> 1) & 1);
+      for (int k = walk.round > 1 ? walk.round - 2 : 0; k <= walk.round; ++k) drain_wait(kv_full + 8 * (k & 1), (k >> 1) & 1);
+      for (uint32_t k = u > (uint32_t)SQ ? u - SQ : 0; k <= u; ++k) {
+        drain_wait(q_full + 8 * (k % SQ), (k / SQ) & 1);
+        drain_wait(do_full + 8 * (k % SQ), (k / SQ) & 1);
       }
     }
   } else if (warp == 9) {
     // ================================================================= MMAs
-    uint32_t u = 0;
-    int n_items = 0;
     bool ok = true;
-    auto score = [&](uint32_t k) {
-      if (!wait(q_full + 8 * (k & 1), (k >> 1) & 1)) return false;
+    ItemWalk ahead(a.tiles, a.hk, items);      // the item of block ua, whose S and dP are issued next
+    int ia = 0, na = ahead.valid ? group * dkv_blocks(ahead.t) : 0;
+    uint32_t ua = 0;
+    auto score = [&]() {
+      if (!ahead.valid) return true;
+      const uint32_t s = ua % SQ, b = ua & 1, kb = ahead.round & 1;
+      if (ia == 0 && !wait(kv_full + 8 * kb, (ahead.round >> 1) & 1)) return false;
+      if (!wait(q_full + 8 * s, (ua / SQ) & 1)) return false;
       tc_fence_after();
-      if (elect_one()) {
-        mma_columns<BF16, DP>(tmem + c_s, sk, sq + (k & 1) * TILE);
-        umma_commit(s_full);
+      mma_columns<BF16, DP, kBlock>(tmem + 64 * b, skv + 2 * kb * TILE, sq + s * BLK);
+      mma_commit(s_full + 8 * b);
+      return true;
+    };
+    auto dprob = [&]() {
+      if (!ahead.valid) return true;
+      const uint32_t s = ua % SQ, b = ua & 1, kb = ahead.round & 1;
+      if (!wait(do_full + 8 * s, (ua / SQ) & 1)) return false;
+      tc_fence_after();
+      mma_columns<BF16, DP, kBlock>(tmem + c_dp + 64 * b, skv + (2 * kb + 1) * TILE, sdo + s * BLK);
+      mma_commit(dp_full + 8 * b);
+      if (ia == na - 1) mma_commit(kv_empty + 8 * kb);
+      ++ua;
+      if (++ia == na) {
+        ahead.next();
+        ia = 0;
+        na = ahead.valid ? group * dkv_blocks(ahead.t) : 0;
       }
       return true;
     };
-    auto dprob = [&](uint32_t k) {
-      if (!wait(do_full + 8 * (k & 1), (k >> 1) & 1)) return false;
-      tc_fence_after();
-      if (elect_one()) {
-        mma_columns<BF16, DP>(tmem + c_dp, sv, sdo + (k & 1) * TILE);
-        umma_commit(dp_full);
-      }
-      return true;
-    };
-    for (int round = 0; ok; ++round) {
-      const int64_t w = work_item(round);
-      if ((int64_t)round * gridDim.x >= items) break;
-      if (w >= items) continue;
-      AttnTile t;
-      int kvh, first, per_head;
-      item(w, t, kvh, first, per_head);
-      const int n = group * per_head;
-      if (!(ok = wait(kv_full, round & 1))) break;
-      if (!(ok = score(u) && dprob(u))) break;
+    ok = score() && dprob() && score() && dprob();
+    uint32_t u = 0;
+    for (ItemWalk walk(a.tiles, a.hk, items); ok && walk.valid; walk.next()) {
+      const int n = group * dkv_blocks(walk.t);
       for (int i = 0; i < n; ++i, ++u) {
-        if (!(ok = wait(p_full, u & 1))) break;
-        if (i == 0 && !(ok = wait(out_free, (n_items & 1) ^ 1))) break;
+        const uint32_t s = u % SQ, b = u & 1, parity = (u >> 1) & 1;
+        if (!(ok = wait(p_full + 8 * b, parity))) break;
+        if (i == 0 && !(ok = wait(out_free, (walk.round & 1) ^ 1))) break;
         tc_fence_after();
-        if (elect_one()) {
-          mma_rows<BF16, DP>(tmem + c_dv, tmem + c_s, 64, sdo + (u & 1) * TILE, i > 0);
-          umma_commit(do_empty + 8 * (u & 1));
-        }
-        if (i + 1 < n && !(ok = score(u + 1))) break;
-        if (!(ok = wait(ds_full, u & 1))) break;
+        mma_half_rows<BF16, DP, kBlock>(tmem + c_dv, tmem + 64 * b, sdo + s * BLK, 0, i > 0);
+        mma_commit(do_empty + 8 * s);
+        if (!(ok = wait(ds_full + 8 * b, parity))) break;
         tc_fence_after();
-        if (elect_one()) {
-          mma_rows<BF16, DP>(tmem + c_dk, tmem + c_dp, 64, sq + (u & 1) * TILE, i > 0);
-          umma_commit(q_empty + 8 * (u & 1));
-          if (i == n - 1) { umma_commit(out_done); umma_commit(kv_empty); }
-        }
-        if (i + 1 < n && !(ok = dprob(u + 1))) break;
+        mma_half_rows<BF16, DP, kBlock>(tmem + c_dk, tmem + c_dp + 64 * b, sq + s * BLK, 0, i > 0);
+        mma_commit(q_empty + 8 * s);
+        if (i == n - 1) mma_commit(out_done);
+        if (!(ok = score() && dprob())) break;
       }
-      ++n_items;
     }
-    if (elect_one()) umma_commit(done);
+    mma_commit(done);
     drain_wait(done, 0);
   } else {
     // ================================================================= P^T, dS^T, and the gradients' way out
-    const int r = (warp & 3) * 32 + lane, h = warp >> 2;
+    const int r = (warp & 3) * 32 + lane, g = warp >> 2;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t ts = tmem + c_s + 64 * h + lanes, td = tmem + c_dp + 64 * h + lanes;
-    const float c = a.scale * kLog2e;
-    uint32_t u = 0;
-    int n_items = 0;
+    const uint32_t ts = tmem + 64 * g + lanes, td = tmem + c_dp + 64 * g + lanes;
+    const float2 c2 = both(a.scale * kLog2e);
+    uint32_t u = 0;                // first block of the item
+    uint32_t mine = 0;
     bool ok = true;
-    for (int round = 0; ok; ++round) {
-      const int64_t w = work_item(round);
-      if ((int64_t)round * gridDim.x >= items) break;
-      if (w >= items) continue;
-      AttnTile t;
-      int kvh, first, per_head;
-      item(w, t, kvh, first, per_head);
-      for (int i = 0, q = 0; i < group * per_head; ++i, ++u, q = q + 1 == per_head ? 0 : q + 1) {
-        const uint32_t st = u & 1;
-        const float4* lse4 = reinterpret_cast<const float4*>(row_stats + st * 256 + 64 * h);
-        const float4* delta4 = reinterpret_cast<const float4*>(row_stats + st * 256 + 128 + 64 * h);
-        if (!(ok = wait(row_full + 8 * st, (u >> 1) & 1))) break;
-        if (!(ok = wait(s_full, u & 1))) break;
+    ItemWalk walk(a.tiles, a.hk, items);
+    while (ok && walk.valid) {
+      const AttnTile t = walk.t;
+      const int kvh = walk.h, round = walk.round, per_head = dkv_blocks(t), n = group * per_head;
+      int i = (int)((g ^ u) & 1), q = i;      // q: the block's number within its head
+      for (; i < n; i += 2, q += 2, ++mine) {
+        while (q >= per_head) q -= per_head;
+        const uint32_t st = (u + i) % SQ, st_parity = ((u + i) / SQ) & 1;
+        const float4* lse4 = reinterpret_cast<const float4*>(row_stats + st * 2 * kBlock);
+        const float4* delta4 = lse4 + kBlock / 4;
+        const int under = q * kBlock - r;                       // column k is masked where k + under < 0
+        if (!(ok = wait(row_full + 8 * st, st_parity))) break;
+        if (!(ok = wait(s_full + 8 * g, mine & 1))) break;
         tc_fence_after();
-        uint32_t s[64], w16[32];
-        float p[64];
-        tmem_ld_32(ts, s);
-        tmem_ld_32(ts + 32, s + 32);
-        tmem_ld_done<64>(s);
+        uint32_t s[64];
+        float2 p[32];
+        load_row64(ts, s);
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
           const float4 l = lse4[k];
-          p[4 * k] = exp2_fast(fmaf(__uint_as_float(s[4 * k]), c, -l.x));
-          p[4 * k + 1] = exp2_fast(fmaf(__uint_as_float(s[4 * k + 1]), c, -l.y));
-          p[4 * k + 2] = exp2_fast(fmaf(__uint_as_float(s[4 * k + 2]), c, -l.z));
-          p[4 * k + 3] = exp2_fast(fmaf(__uint_as_float(s[4 * k + 3]), c, -l.w));
+          p[2 * k] = fma2(two(s + 4 * k), c2, make_float2(l.x, l.y));
+          p[2 * k + 1] = fma2(two(s + 4 * k + 2), c2, make_float2(l.z, l.w));
+          p[2 * k].x = exp2_fast(p[2 * k].x);
+          p[2 * k].y = exp2_fast(p[2 * k].y);
+          p[2 * k + 1].x = exp2_fast(p[2 * k + 1].x);
+          p[2 * k + 1].y = exp2_fast(p[2 * k + 1].y);
         }
-        if (q == 0) {      // on the diagonal: queries before the key do not see it
+        auto mask = [&]() {
 #pragma unroll
-          for (int k = 0; k < 64; ++k)
-            if (64 * h + k < r) p[k] = 0.f;
-        }
-        pack64<BF16>(p, w16);
-        tmem_st_32(ts, w16);
-        tmem_st_wait();
-        tc_fence_before();
-        mbar_arrive(p_full);
-        if (!(ok = wait(dp_full, u & 1))) break;
+          for (int k = 0; k < 32; ++k) {
+            if (2 * k + under < 0) p[k].x = 0.f;
+            if (2 * k + 1 + under < 0) p[k].y = 0.f;
+          }
+        };
+        if (q < 2) mask();      // queries before the key do not see it
+        store_pairs<BF16>(ts, p);
+        mbar_arrive(p_full + 8 * g);
+        if (!(ok = wait(dp_full + 8 * g, mine & 1))) break;
         tc_fence_after();
-        tmem_ld_32(td, s);
-        tmem_ld_32(td + 32, s + 32);
-        tmem_ld_done<64>(s);
+        load_row64(td, s);
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
           const float4 l = delta4[k];
-          p[4 * k] *= __uint_as_float(s[4 * k]) - l.x;
-          p[4 * k + 1] *= __uint_as_float(s[4 * k + 1]) - l.y;
-          p[4 * k + 2] *= __uint_as_float(s[4 * k + 2]) - l.z;
-          p[4 * k + 3] *= __uint_as_float(s[4 * k + 3]) - l.w;
+          p[2 * k] = mul2(p[2 * k], add2(two(s + 4 * k), make_float2(l.x, l.y)));
+          p[2 * k + 1] = mul2(p[2 * k + 1], add2(two(s + 4 * k + 2), make_float2(l.z, l.w)));
         }
-        if (q == 0) {
-#pragma unroll
-          for (int k = 0; k < 64; ++k)
-            if (64 * h + k < r) p[k] = 0.f;
-        }
+        if (q < 2) mask();      // (0 times a non-finite value of a masked place is not 0)
         mbar_arrive(row_empty + 8 * st);
-        pack64<BF16>(p, w16);
-        tmem_st_32(td, w16);
-        tmem_st_wait();
-        tc_fence_before();
-        mbar_arrive(ds_full);
+        store_pairs<BF16>(td, p);
+        mbar_arrive(ds_full + 8 * g);
       }
-      if (!ok || !(ok = wait(out_done, n_items & 1))) break;
-      ++n_items;
+      if (!ok) break;
+      u += n;
+      walk.next();
+      if (!(ok = wait(out_done, round & 1))) break;
       tc_fence_after();
       const bool real = t.row + r < t.len;
       const int64_t token = t.start + t.row + r;
-      char *ok_ = a.dk.p + 2 * (token * a.dk.token + kvh * a.dk.head), *ov = a.dv.p + 2 * (token * a.dv.token + kvh * a.dv.head);
+      // group 0 writes dK, group 1 dV
+      const AttnHeads& to = g ? a.dv : a.dk;
+      char* out = to.p + 2 * (token * to.token + kvh * to.head);
 #pragma unroll
-      for (int k = 0; k < DP / 2; k += 32) {
+      for (int k = 0; k < DP; k += 32) {
         uint32_t o[32];
-        const int c0 = h * (DP / 2) + k;
-        tmem_ld_32(tmem + c_dk + c0 + lanes, o);
+        tmem_ld_32(tmem + (g ? c_dv : c_dk) + k + lanes, o);
         tmem_ld_done<32>(o);
-        if (real) store_columns<BF16, 32>(ok_, o, a.scale, c0, a.d);
-        tmem_ld_32(tmem + c_dv + c0 + lanes, o);
-        tmem_ld_done<32>(o);
-        if (real) store_columns<BF16, 32>(ov, o, 1.f, c0, a.d);
+        if (real) store_columns<BF16, 32>(out, o, g ? 1.f : a.scale, k, a.d);
       }
       tc_fence_before();
       mbar_arrive(out_free);
@@ -524,23 +530,24 @@ template <int DP, bool BF16>
 int launch(const fgd_attn_plan* plan, AttnArgs a, cudaStream_t st) {
   const char* who = "fgd_attn_backward";
   CUtensorMap mq, mk, mv, mdo;
-  if (!attn_tensor_map(plan->encode_tiled, &mq, BF16, a.q, a.tokens, a.hq, a.d) || !attn_tensor_map(plan->encode_tiled, &mk, BF16, a.k, a.tokens, a.hk, a.d) ||
-      !attn_tensor_map(plan->encode_tiled, &mv, BF16, a.v, a.tokens, a.hk, a.d) || !attn_tensor_map(plan->encode_tiled, &mdo, BF16, a.dout, a.tokens, a.hq, a.d))
-    return op_fail(FGD_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed", who);
+  auto map = [&](CUtensorMap* m, const AttnHeads& t, int heads, int rows) { return attn_tensor_map(plan->encode_tiled, m, BF16, t, a.tokens, heads, a.d, rows); };
+  const int64_t items_kv = (int64_t)plan->n_kv * a.hk, items_q = (int64_t)plan->n_q * a.hq;
+  if (items_kv > 0x7fffffff - 1024 || items_q > 0x7fffffff - 1024) return op_fail(FGD_ERR_UNSUPPORTED, "%s: too many tiles", who);
   const int sms = sm_count();
   auto dq = attn_dq_tc_kernel<DP, BF16>;
   auto dkv = attn_dkv_tc_kernel<DP, BF16>;
   cudaError_t e = cudaFuncSetAttribute(dq, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dq_smem<DP>());
   if (e == cudaSuccess) e = cudaFuncSetAttribute(dkv, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dkv_smem<DP>());
-  if (e == cudaSuccess) {
-    int64_t items = (int64_t)plan->n_kv * a.hk;
-    a.tiles = plan->kv_tiles;
-    dkv<<<(unsigned)(items < sms ? items : sms), kBwdThreads, dkv_smem<DP>(), st>>>(a, items, mq, mk, mv, mdo);
-    items = (int64_t)plan->n_q * a.hq;
-    a.tiles = plan->q_tiles;
-    dq<<<(unsigned)(items < sms ? items : sms), kBwdThreads, dq_smem<DP>(), st>>>(a, items, mq, mk, mv, mdo);
-    e = cudaGetLastError();
-  }
+  if (e != cudaSuccess) return op_fail(FGD_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
+  if (!map(&mq, a.q, a.hq, kBlock) || !map(&mk, a.k, a.hk, kAttnRows) || !map(&mv, a.v, a.hk, kAttnRows) || !map(&mdo, a.dout, a.hq, kBlock))
+    return op_fail(FGD_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed", who);
+  a.tiles = plan->kv_tiles;
+  dkv<<<(unsigned)(items_kv < sms ? items_kv : sms), kBwdThreads, dkv_smem<DP>(), st>>>(a, (int)items_kv, mq, mk, mv, mdo);
+  if (!map(&mq, a.q, a.hq, kAttnRows) || !map(&mk, a.k, a.hk, kBlock) || !map(&mv, a.v, a.hk, kBlock) || !map(&mdo, a.dout, a.hq, kAttnRows))
+    return op_fail(FGD_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed", who);
+  a.tiles = plan->q_tiles;
+  dq<<<(unsigned)(items_q < sms ? items_q : sms), kBwdThreads, dq_smem<DP>(), st>>>(a, (int)items_q, mq, mk, mv, mdo);
+  e = cudaGetLastError();
   return e == cudaSuccess ? FGD_OK : op_fail(FGD_ERR_CUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
 }
 

@@ -32,9 +32,7 @@ struct FwdItem {
   int head[2], row[2], n[2];   // n: key blocks of the tile (0: no tile)
 };
 // pair_heads: heads 2 h and 2 h + 1 of one 128-row tile; otherwise rows [r, r + 256) of head h.
-__device__ __forceinline__ FwdItem fwd_item(const AttnArgs& a, int pair_heads, int per_tile, int64_t w) {
-  const int tile = (int)(w / per_tile), h = (int)(w - (int64_t)tile * per_tile);
-  const AttnTile t = a.tiles[tile];
+__device__ __forceinline__ FwdItem fwd_item(const AttnArgs& a, int pair_heads, const AttnTile& t, int h) {
   FwdItem it;
   it.start = t.start; it.len = t.len;
   it.head[0] = pair_heads ? 2 * h : h;
@@ -50,7 +48,7 @@ __device__ __forceinline__ FwdItem fwd_item(const AttnArgs& a, int pair_heads, i
 
 template <int DP, bool BF16>
 __global__ void __launch_bounds__(kFwdThreads, 1)
-attn_forward_tc_kernel(const AttnArgs a, int pair_heads, int per_tile, int64_t items, const __grid_constant__ CUtensorMap mq,
+attn_forward_tc_kernel(const AttnArgs a, int pair_heads, int per_tile, int items, const __grid_constant__ CUtensorMap mq,
                        const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv) {
   constexpr int ST = kFwdStages<DP>;
   constexpr uint32_t TILE = attn_tile_bytes<DP>();
@@ -61,7 +59,7 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, int per_tile, int64_t i
   __shared__ int abort_flag;
   unsigned char* base = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   const uint32_t sq = smem_u32(base), skv = sq + 2 * TILE;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
   const uint32_t b0 = smem_u32(bars);
   const uint32_t q_full = b0, q_empty = b0 + 8, raw = b0 + 16, done = b0 + 24, full = b0 + 32, empty = full + 8 * ST, s_full = empty + 8 * ST,
                  pv_done = s_full + 16, o_free = s_full + 32, p_full = s_full + 48;   // p_full + 16 t + 8 half: 64 columns of P each
@@ -82,7 +80,7 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, int per_tile, int64_t i
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = tmem_slot;
+  const uint32_t tmem = (uint32_t)uniform((int)tmem_slot);
   const AttnWait wait{&abort_flag, a.status};
   // tensor memory columns
   auto s_col = [](int t) { return (uint32_t)(128 * t); };
@@ -91,13 +89,11 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, int per_tile, int64_t i
   if (warp == 8) {
     // ================================================================= loads
     uint32_t u = 0, n_raw = 0;     // ring uses, repaired tiles
-    int round = 0;
     bool ok = true;
-    for (; ok; ++round) {
-      const int64_t w = work_item(round);
-      if ((int64_t)round * gridDim.x >= items) break;
-      if (w >= items) continue;
-      const FwdItem it = fwd_item(a, pair_heads, per_tile, w);
+    ItemWalk walk(a.tiles, per_tile, items);
+    for (; ok && walk.valid; walk.next()) {
+      const int round = walk.round;
+      const FwdItem it = fwd_item(a, pair_heads, walk.t, walk.h);
       static_assert(kAttnRows == 128, "TMA boxes are 128 rows");
       ok = wait(q_empty, (round & 1) ^ 1);
       if (!ok) break;
@@ -125,7 +121,7 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, int per_tile, int64_t i
             ok = wait(raw, n_raw & 1);
             ++n_raw;
             if (!ok) { drain_wait(raw, (n_raw - 1) & 1); break; }
-            zero_rows<DP>(base + 2 * TILE + s * TILE, rows, lane);
+            zero_rows<DP, 128>(base + 2 * TILE + s * TILE, rows, lane);
             if (elect_one()) mbar_arrive(bar);
           }
         }
@@ -133,8 +129,8 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, int per_tile, int64_t i
     }
     // a CTA that gave up still waits for its own copies
     if (wait.given_up()) {
-      const int r = round > 0 && !ok ? round : round - 1;
-      if (r >= 0) drain_wait(q_full, r & 1);
+      drain_wait(q_full, walk.round & 1);
+      if (walk.round > 0) drain_wait(q_full, (walk.round - 1) & 1);
       for (uint32_t k = u > (uint32_t)ST ? u - ST : 0; k < u; ++k) drain_wait(full + 8 * (k % ST), (k / ST) & 1);
     }
   } else if (warp == 9) {
@@ -143,26 +139,21 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, int per_tile, int64_t i
     uint32_t n_p[2] = {0, 0}, n_o[2] = {0, 0};
     bool ok = true;
     auto score = [&](int t, uint32_t stage) {
-      if (elect_one()) {
-        mma_columns<BF16, DP>(tmem + s_col(t), sq + t * TILE, skv + stage * TILE);
-        umma_commit(s_full + 8 * t);
-      }
+      mma_columns<BF16, DP>(tmem + s_col(t), sq + t * TILE, skv + stage * TILE);
+      mma_commit(s_full + 8 * t);
     };
-    auto release = [&](uint32_t use) { if (elect_one()) umma_commit(empty + 8 * (use % ST)); };
+    auto release = [&](uint32_t use) { mma_commit(empty + 8 * (use % ST)); };
     auto arrived = [&](uint32_t use) { return wait(full + 8 * (use % ST), (use / ST) & 1); };
-    for (int round = 0; ok; ++round) {
-      const int64_t w = work_item(round);
-      if ((int64_t)round * gridDim.x >= items) break;
-      if (w >= items) continue;
-      const FwdItem it = fwd_item(a, pair_heads, per_tile, w);
-      if (!(ok = wait(q_full, round & 1))) break;
+    for (ItemWalk walk(a.tiles, per_tile, items); ok && walk.valid; walk.next()) {
+      const FwdItem it = fwd_item(a, pair_heads, walk.t, walk.h);
+      if (!(ok = wait(q_full, walk.round & 1))) break;
       uint32_t uk = u++;
       if (!(ok = arrived(uk))) break;
       tc_fence_after();
       for (int t = 0; t < 2; ++t)
         if (it.nmax - 1 < it.n[t]) score(t, uk % ST);
       release(uk);
-      if (it.nmax == 1 && elect_one()) umma_commit(q_empty);
+      if (it.nmax == 1) mma_commit(q_empty);
       for (int jb = it.nmax - 1; ok && jb >= 0; --jb) {
         const uint32_t uv = u++;
         uk = u;
@@ -179,11 +170,11 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, int per_tile, int64_t i
               }
               if (!ok) break;
               tc_fence_after();
-              if (elect_one()) mma_half_rows<BF16, DP>(tmem + o_col(t), tmem + s_col(t) + 32 * half, skv + (uv % ST) * TILE, half, !first || half == 1);
+              mma_half_rows<BF16, DP>(tmem + o_col(t), tmem + s_col(t) + 32 * half, skv + (uv % ST) * TILE, half, !first || half == 1);
             }
             ++n_p[t];
             if (!ok) break;
-            if (elect_one()) umma_commit(pv_done + 8 * t);
+            mma_commit(pv_done + 8 * t);
           }
           if (t == 1) release(uv);
           if (jb > 0 && jb - 1 < it.n[t]) {
@@ -194,12 +185,12 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, int per_tile, int64_t i
           }
         }
         if (ok && jb > 0) { release(uk); ++u; }
-        if (ok && jb == 1 && elect_one()) umma_commit(q_empty);     // the last scores of this item are on their way
+        if (ok && jb == 1) mma_commit(q_empty);     // the last scores of this item are on their way
       }
       __syncwarp();
     }
     // tensor memory is not released under a running MMA
-    if (elect_one()) umma_commit(done);
+    mma_commit(done);
     drain_wait(done, 0);
   } else {
     // ================================================================= softmax
@@ -209,11 +200,8 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, int per_tile, int64_t i
     const float c = a.scale * kLog2e;
     uint32_t n_s = 0, n_pv = 0;
     bool ok = true;
-    for (int round = 0; ok; ++round) {
-      const int64_t w = work_item(round);
-      if ((int64_t)round * gridDim.x >= items) break;
-      if (w >= items) continue;
-      const FwdItem it = fwd_item(a, pair_heads, per_tile, w);
+    for (ItemWalk walk(a.tiles, per_tile, items); ok && walk.valid; walk.next()) {
+      const FwdItem it = fwd_item(a, pair_heads, walk.t, walk.h);
       const int n = it.n[t];
       if (n == 0) continue;
       float m = 0.f;
@@ -319,15 +307,16 @@ int launch(const fgd_attn_plan* plan, AttnArgs a, cudaStream_t st) {
   a.n_tiles = pair_heads ? plan->n_q : plan->n_q2;
   const int per_tile = pair_heads ? a.hq / 2 : a.hq;
   const int64_t items = (int64_t)a.n_tiles * per_tile;
+  if (items > 0x7fffffff - 1024) return op_fail(FGD_ERR_UNSUPPORTED, "%s: %lld tiles", who, (long long)items);
   CUtensorMap mq, mk, mv;
-  if (!attn_tensor_map(plan->encode_tiled, &mq, BF16, a.q, a.tokens, a.hq, a.d) || !attn_tensor_map(plan->encode_tiled, &mk, BF16, a.k, a.tokens, a.hk, a.d) ||
-      !attn_tensor_map(plan->encode_tiled, &mv, BF16, a.v, a.tokens, a.hk, a.d))
+  if (!attn_tensor_map(plan->encode_tiled, &mq, BF16, a.q, a.tokens, a.hq, a.d, 128) || !attn_tensor_map(plan->encode_tiled, &mk, BF16, a.k, a.tokens, a.hk, a.d, 128) ||
+      !attn_tensor_map(plan->encode_tiled, &mv, BF16, a.v, a.tokens, a.hk, a.d, 128))
     return op_fail(FGD_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed", who);
   auto kern = attn_forward_tc_kernel<DP, BF16>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)fwd_smem<DP>());
   if (e == cudaSuccess) {
     const int sms = sm_count();
-    kern<<<(unsigned)(items < sms ? items : sms), kFwdThreads, fwd_smem<DP>(), st>>>(a, pair_heads, per_tile, items, mq, mk, mv);
+    kern<<<(unsigned)(items < sms ? items : sms), kFwdThreads, fwd_smem<DP>(), st>>>(a, pair_heads, per_tile, (int)items, mq, mk, mv);
     e = cudaGetLastError();
   }
   return e == cudaSuccess ? FGD_OK : op_fail(FGD_ERR_CUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));

@@ -1,8 +1,8 @@
 // What the tensor-core attention kernels share: bounded waits, TMA loads of head tiles, tensor-memory
 // access, operand descriptors and MMA issue.
 //
-// A tile is 128 rows of one head, DP (64 or 128) columns wide, zero-filled beyond the head's width.  In shared memory it
-// is one or two boxes of 128 rows x 64 columns, 128 bytes per row, written by TMA with the 128-byte swizzle.  The same
+// A tile is 128 (or 64) rows of one head, DP (64 or 128) columns wide, zero-filled beyond the head's width.  In shared memory it
+// is one or two boxes of that many rows x 64 columns, 128 bytes per row, written by TMA with the 128-byte swizzle.  The same
 // box serves the MMAs in both directions: with the columns as the contraction (K-major: scores, dP) and with the
 // rows as the contraction (MN-major: P V, dS K, P^T dO, dS^T Q).
 #ifndef FGD_ATTN_TC_CUH_
@@ -58,18 +58,18 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
       ::"r"(dst), "l"(map), "r"(c), "r"(head), "r"(token), "r"(bar)
       : "memory");
 }
-// One tile: DP / 64 boxes, issued by one thread.
-template <int DP>
+// One tile of ROWS rows (the map's box height): DP / 64 boxes, issued by one thread.
+template <int DP, int ROWS = 128>
 __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, int head, int token, uint32_t bar) {
 #pragma unroll
-  for (int b = 0; b < DP / 64; ++b) tma_load_3d(dst + b * kAttnBox, map, b * 64, head, token, bar);
+  for (int b = 0; b < DP / 64; ++b) tma_load_3d(dst + b * ROWS * 128, map, b * 64, head, token, bar);
 }
-// Rows [first, 128) of a tile become zero (a row of a box is 128 contiguous bytes, the swizzle stays inside it), for the
+// Rows [first, ROWS) of a tile become zero (a row of a box is 128 contiguous bytes, the swizzle stays inside it), for the
 // asynchronous proxy to read.  One warp.
-template <int DP>
+template <int DP, int ROWS>
 __device__ __forceinline__ void zero_rows(unsigned char* tile, int first, int lane) {
   for (int b = 0; b < DP / 64; ++b)
-    for (int i = first * 8 + lane; i < 128 * 8; i += 32) reinterpret_cast<uint4*>(tile + b * kAttnBox)[i] = make_uint4(0u, 0u, 0u, 0u);
+    for (int i = first * 8 + lane; i < ROWS * 8; i += 32) reinterpret_cast<uint4*>(tile + b * ROWS * 128)[i] = make_uint4(0u, 0u, 0u, 0u);
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   __syncwarp();
 }
@@ -111,7 +111,12 @@ __device__ __forceinline__ void tmem_ld_done(uint32_t* r) {
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
-// ---- MMA issue (one thread).  M = 128 everywhere.
+// ---- MMA issue.  M = 128 everywhere.  Called by a whole converged warp; one elected lane (always the same) issues.
+// A value that all lanes of a warp share, told to the compiler: what it knows to be the same in every lane can sit in uniform
+// registers, where the MMA's operands have to be; without it every MMA pays for moving them there.
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); }
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
+
 template <bool BF16, int N, bool B_ROWS>   // B_ROWS: B's contraction runs over its rows (MN-major)
 __host__ __device__ constexpr uint32_t attn_idesc() {
   return (1u << 4) | ((BF16 ? 1u : 0u) << 7) | ((BF16 ? 1u : 0u) << 10) | ((B_ROWS ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | (8u << 24);
@@ -145,29 +150,40 @@ __device__ __forceinline__ void umma_f16_ts(uint32_t d, uint32_t a, uint32_t b, 
       ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "n"(kDescHigh)
       : "memory");
 }
-// D[128 x 128] = A B^T over the tiles' columns (both K-major): 16 columns per step, 32 bytes inside a swizzled row.
-template <bool BF16, int DP>
+// D[128 x N] = A B^T over the tiles' columns (both K-major): 16 columns per step, 32 bytes inside a swizzled row.  A has 128 rows,
+// B has N (its box height).
+template <bool BF16, int DP, int N = 128>
 __device__ __forceinline__ void mma_columns(uint32_t d, uint32_t a_tile, uint32_t b_tile) {
-  const uint32_t a = desc_low(a_tile, 16), b = desc_low(b_tile, 16);
+  const uint32_t a = uniform(desc_low(a_tile, 16)), b = uniform(desc_low(b_tile, 16)), c = uniform(d);
+  if (elect_one()) {
 #pragma unroll
-  for (int k = 0; k < DP / 16; ++k) {
-    const uint32_t off = ((k / 4) * kAttnBox + (k % 4) * 32) >> 4;
-    umma_f16_ss(d, a + off, b + off, attn_idesc<BF16, 128, false>(), k > 0 ? 1u : 0u);
+    for (int k = 0; k < DP / 16; ++k)
+      umma_f16_ss(c, a + (((k / 4) * 128 * 128 + (k % 4) * 32) >> 4), b + (((k / 4) * N * 128 + (k % 4) * 32) >> 4), attn_idesc<BF16, N, false>(), k > 0 ? 1u : 0u);
   }
 }
-// D[128 x DP] (+)= A B over 64 of B's 128 rows (half 0 or 1): A's 64 columns are 16-bit values in tensor memory, packed two
-// to a column, at [a, a + 32); 16 rows of B per step.
-template <bool BF16, int DP>
-__device__ __forceinline__ void mma_half_rows(uint32_t d, uint32_t a, uint32_t b_tile, int half, bool accumulate) {
-  const uint32_t b = desc_low(b_tile, kAttnBox) + half * (64 * 128 >> 4);
+// The same with A in tensor memory: row r in lane r, its columns packed two to a 32-bit column.
+template <bool BF16, int DP, int N>
+__device__ __forceinline__ void mma_columns_t(uint32_t d, uint32_t a_cols, uint32_t b_tile) {
+  const uint32_t a = uniform(a_cols), b = uniform(desc_low(b_tile, 16)), c = uniform(d);
+  if (elect_one()) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) umma_f16_ts(d, a + k * 8, b + k * (2048 >> 4), attn_idesc<BF16, DP, true>(), (accumulate || k > 0) ? 1u : 0u);
+    for (int k = 0; k < DP / 16; ++k) umma_f16_ts(c, a + k * 8, b + (((k / 4) * N * 128 + (k % 4) * 32) >> 4), attn_idesc<BF16, N, false>(), k > 0 ? 1u : 0u);
+  }
 }
-// All 128 rows: A's second half stands `a_half` columns after the first.
-template <bool BF16, int DP>
-__device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a, uint32_t a_half, uint32_t b_tile, bool accumulate) {
-  mma_half_rows<BF16, DP>(d, a, b_tile, 0, accumulate);
-  mma_half_rows<BF16, DP>(d, a + a_half, b_tile, 1, true);
+// D[128 x DP] (+)= A B over 64 rows of B (rows [64 half, 64 half + 64) of a tile of ROWS): A's 64 columns are 16-bit values in
+// tensor memory, packed two to a column, at [a, a + 32); 16 rows of B per step.
+template <bool BF16, int DP, int ROWS = 128>
+__device__ __forceinline__ void mma_half_rows(uint32_t d, uint32_t a_cols, uint32_t b_tile, int half, bool accumulate) {
+  const uint32_t a = uniform(a_cols), b = uniform(desc_low(b_tile, ROWS * 128) + half * (64 * 128 >> 4)), c = uniform(d), acc = uniform(accumulate ? 1u : 0u);
+  if (elect_one()) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) umma_f16_ts(c, a + k * 8, b + k * (2048 >> 4), attn_idesc<BF16, DP, true>(), k > 0 ? 1u : acc);
+  }
+}
+// Arrival on `bar` once everything issued so far is done.
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+  const uint32_t b = uniform(bar);
+  if (elect_one()) umma_commit(b);
 }
 
 // ---- arithmetic
@@ -204,23 +220,52 @@ __device__ __forceinline__ void store_columns(char* out, const uint32_t* r, floa
   }
 }
 
-// The order in which a persistent CTA takes the work items, which are sorted by descending work: forwards and backwards by
-// turns, so that a CTA that got a large item gets a small one next.
-__device__ __forceinline__ int64_t work_item(int round) {
-  return (int64_t)round * gridDim.x + ((round & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
-}
+// The work items of a persistent CTA: `items` = tiles x heads, sorted by descending work, taken forwards and backwards by turns so
+// that a CTA that got a large item gets a small one next.  The tile after the current one is read ahead: its latency (and the
+// division) would otherwise stand between two items in every role.
+struct ItemWalk {
+  const AttnTile* tiles;
+  int per_tile, items;
+  int round;             // of the current item, counted from 0
+  bool valid;
+  AttnTile t, t_next;
+  int h, h_next;
+  bool valid_next;
+  __device__ __forceinline__ void look(int r) {
+    const int w = r * (int)gridDim.x + ((r & 1) ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
+    valid_next = w < items;      // only the last, partial round can lack an item
+    if (valid_next) {
+      const int tile = w / per_tile;
+      h_next = w - tile * per_tile;
+      t_next = tiles[tile];
+    }
+  }
+  __device__ __forceinline__ ItemWalk(const AttnTile* tiles_, int per_tile_, int items_) : tiles(tiles_), per_tile(per_tile_), items(items_), round(-1) {
+    look(0);
+    next();
+  }
+  __device__ __forceinline__ void next() {
+    ++round;
+    valid = uniform(valid_next ? 1 : 0) != 0;
+    t.start = uniform(t_next.start);
+    t.len = uniform(t_next.len);
+    t.row = uniform(t_next.row);
+    h = uniform(h_next);
+    if (valid) look(round + 1);
+  }
+};
 
 // ---- host side
 typedef CUresult (*AttnEncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// Tensor map of a [tokens, heads, d] tensor: boxes of 64 columns x 1 head x 128 tokens; columns beyond d and tokens beyond the
+// Tensor map of a [tokens, heads, d] tensor: boxes of 64 columns x 1 head x `rows` tokens; columns beyond d and tokens beyond the
 // last read as zero.
-inline bool attn_tensor_map(void* encode, CUtensorMap* map, bool bf16, const AttnHeads& t, int64_t tokens, int heads, int d) {
+inline bool attn_tensor_map(void* encode, CUtensorMap* map, bool bf16, const AttnHeads& t, int64_t tokens, int heads, int d, int rows) {
   const cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)heads, (cuuint64_t)tokens};
   // the stride of an axis of one is never used, but has to be a valid one
   const cuuint64_t strides[2] = {heads > 1 ? (cuuint64_t)t.head * 2 : (cuuint64_t)d * 2, tokens > 1 ? (cuuint64_t)t.token * 2 : (cuuint64_t)d * 2};
-  const cuuint32_t box[3] = {64, 1, 128}, estr[3] = {1, 1, 1};
+  const cuuint32_t box[3] = {64, 1, (cuuint32_t)rows}, estr[3] = {1, 1, 1};
   return reinterpret_cast<AttnEncodeFn>(encode)(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, t.p, dims, strides, box, estr,
                                                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                                                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
