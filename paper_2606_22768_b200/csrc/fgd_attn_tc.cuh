@@ -161,15 +161,6 @@ __device__ __forceinline__ void mma_columns(uint32_t d, uint32_t a_tile, uint32_
       umma_f16_ss(c, a + (((k / 4) * 128 * 128 + (k % 4) * 32) >> 4), b + (((k / 4) * N * 128 + (k % 4) * 32) >> 4), attn_idesc<BF16, N, false>(), k > 0 ? 1u : 0u);
   }
 }
-// The same with A in tensor memory: row r in lane r, its columns packed two to a 32-bit column.
-template <bool BF16, int DP, int N>
-__device__ __forceinline__ void mma_columns_t(uint32_t d, uint32_t a_cols, uint32_t b_tile) {
-  const uint32_t a = uniform(a_cols), b = uniform(desc_low(b_tile, 16)), c = uniform(d);
-  if (elect_one()) {
-#pragma unroll
-    for (int k = 0; k < DP / 16; ++k) umma_f16_ts(c, a + k * 8, b + (((k / 4) * N * 128 + (k % 4) * 32) >> 4), attn_idesc<BF16, N, false>(), k > 0 ? 1u : 0u);
-  }
-}
 // D[128 x DP] (+)= A B over 64 rows of B (rows [64 half, 64 half + 64) of a tile of ROWS): A's 64 columns are 16-bit values in
 // tensor memory, packed two to a column, at [a, a + 32); 16 rows of B per step.
 template <bool BF16, int DP, int ROWS = 128>
@@ -178,6 +169,15 @@ __device__ __forceinline__ void mma_half_rows(uint32_t d, uint32_t a_cols, uint3
   if (elect_one()) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) umma_f16_ts(c, a + k * 8, b + k * (2048 >> 4), attn_idesc<BF16, DP, true>(), k > 0 ? 1u : acc);
+  }
+}
+// All 128 rows of a tile: A's second half stands `a_half` columns after the first.
+template <bool BF16, int DP>
+__device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a_cols, uint32_t a_half, uint32_t b_tile, bool accumulate) {
+  const uint32_t a = uniform(a_cols), b = uniform(desc_low(b_tile, 128 * 128)), c = uniform(d), acc = uniform(accumulate ? 1u : 0u);
+  if (elect_one()) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) umma_f16_ts(c, a + (k / 4) * a_half + (k % 4) * 8, b + k * (2048 >> 4), attn_idesc<BF16, DP, true>(), k > 0 ? 1u : acc);
   }
 }
 // Arrival on `bar` once everything issued so far is done.
