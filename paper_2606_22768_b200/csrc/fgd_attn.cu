@@ -193,6 +193,7 @@ extern "C" int fgd_attn_backward(fgd_attn_plan* plan, const fgd_attn_args* b, vo
   if (!dev.ok()) return op_fail(FGD_ERR_CUDA, "cannot select device %d", plan->device);
   const AttnArgs a = kernel_args(plan, b);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (int rc = attn_delta(b->dtype, a, st)) return rc;
-  return on_tensor_cores(plan, b, all, 8) ? attn_backward_tc(plan, b->dtype, a, st) : attn_backward_elem(plan, b->dtype, a, st);
+  const bool tc = on_tensor_cores(plan, b, all, 8);
+  if (int rc = attn_delta(b->dtype, tc, a, st)) return rc;
+  return tc ? attn_backward_tc(plan, b->dtype, a, st) : attn_backward_elem(plan, b->dtype, a, st);
 }

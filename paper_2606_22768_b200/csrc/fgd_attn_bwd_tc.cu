@@ -27,9 +27,12 @@ constexpr int kBwdThreads = 320;
 template <int DP> constexpr int kBufQ = DP == 128 ? 1 : 2;
 constexpr int kStagesK = 3, kStagesV = 2;
 template <int DP> constexpr size_t dq_smem() { return 1024 + (size_t)(2 * kBufQ<DP> + kStagesK + kStagesV) * attn_tile_bytes<DP>(); }
-// key kernel: K, V, stages of Q and dO, and the rows' lse and delta
-constexpr int kStagesQ = 2;
-template <int DP> constexpr size_t dkv_smem() { return 1024 + (size_t)(2 + 2 * kStagesQ) * attn_tile_bytes<DP>() + kStagesQ * 2 * 128 * sizeof(float); }
+// key kernel: K, V, stages of Q and dO, and of the rows' lse and delta, which a warp of their own fetches (behind the tiles, on the
+// loading warp's path, their latency held up every block: sixteen sequences of 1024, 16 heads of 64, 190 us)
+template <int DP> constexpr int kStagesQ = DP == 128 ? 2 : 4;
+constexpr int kStagesRow = 4;
+constexpr int kDkvThreads = 352;
+template <int DP> constexpr size_t dkv_smem() { return 1024 + (size_t)(2 + 2 * kStagesQ<DP>) * attn_tile_bytes<DP>() + kStagesRow * 2 * 128 * sizeof(float); }
 
 __device__ __forceinline__ void load_row64(uint32_t addr, uint32_t (&s)[64]) {
   tmem_ld_32(addr, s);
@@ -225,11 +228,7 @@ attn_dq_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensorM
         float2 p[32];
         load_row64(ts, s);
 #pragma unroll
-        for (int k = 0; k < 32; ++k) {
-          p[k] = fma2(two(s + 2 * k), c2, lse2);
-          p[k].x = exp2_fast(p[k].x);
-          p[k].y = exp2_fast(p[k].y);
-        }
+        for (int k = 0; k < 32; ++k) p[k] = exp2_pair(fma2(two(s + 2 * k), c2, lse2), k);
         if (!(ok = wait(dp_full, u & 1))) break;
         tc_fence_after();
         load_row64(td, s);
@@ -272,13 +271,13 @@ attn_dq_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensorM
 
 // ------------------------------------------------------------------------------------------ dK, dV
 template <int DP, bool BF16>
-__global__ void __launch_bounds__(kBwdThreads, 1)
+__global__ void __launch_bounds__(kDkvThreads, 1)
 attn_dkv_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                    const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo) {
   constexpr uint32_t TILE = attn_tile_bytes<DP>();
-  constexpr int SQ = kStagesQ;
+  constexpr int SQ = kStagesQ<DP>, SR = kStagesRow;
   extern __shared__ unsigned char smem_raw[];
-  __shared__ __align__(8) unsigned long long bars[12 + 6 * SQ];
+  __shared__ __align__(8) unsigned long long bars[12 + 4 * SQ + 2 * SR];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
   unsigned char* base = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -288,13 +287,13 @@ attn_dkv_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensor
   const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
   const uint32_t b0 = smem_u32(bars), raw = b0, done = b0 + 8, k_full = b0 + 16, k_empty = b0 + 24, v_full = b0 + 32, v_empty = b0 + 40, s_full = b0 + 48,
                  p_full = b0 + 56, dp_full = b0 + 64, ds_full = b0 + 72, out_done = b0 + 80, out_free = b0 + 88, q_full = b0 + 96, q_empty = q_full + 8 * SQ,
-                 do_full = q_empty + 8 * SQ, do_empty = do_full + 8 * SQ, row_full = do_empty + 8 * SQ, row_empty = row_full + 8 * SQ;
+                 do_full = q_empty + 8 * SQ, do_empty = do_full + 8 * SQ, row_full = do_empty + 8 * SQ, row_empty = row_full + 8 * SR;
   if (tid == 0) {
     abort_flag = 0;
     for (uint32_t b : {raw, done, k_full, k_empty, v_full, v_empty, s_full, dp_full, out_done}) mbar_init(b, 1);
     for (uint32_t b : {p_full, ds_full, out_free}) mbar_init(b, 256);
     for (int s = 0; s < 4 * SQ; ++s) mbar_init(q_full + 8 * s, 1);
-    for (int s = 0; s < SQ; ++s) { mbar_init(row_full + 8 * s, 32); mbar_init(row_empty + 8 * s, 256); }
+    for (int s = 0; s < SR; ++s) { mbar_init(row_full + 8 * s, 32); mbar_init(row_empty + 8 * s, 256); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 9) {
@@ -350,14 +349,6 @@ attn_dkv_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensor
           const uint32_t s = u % SQ, parity = ((u / SQ) & 1) ^ 1;
           if (!(ok = wait(q_empty + 8 * s, parity))) break;
           if (!(ok = tile(&mq, 2 + s, q_full + 8 * s, head, t.start + row, rows))) break;
-          if (!(ok = wait(row_empty + 8 * s, parity))) break;
-          float* stats = row_stats + s * 256;
-          for (int k = lane; k < 128; k += 32) {      // negated; rows beyond the end: P = 2^-inf = 0
-            const int64_t at = (int64_t)head * a.tokens + t.start + row + k;
-            stats[k] = k < rows ? -a.lse[at] * kLog2e : -INFINITY;
-            stats[128 + k] = k < rows ? -a.delta[at] : 0.f;
-          }
-          mbar_arrive(row_full + 8 * s);
           if (hh == 0 && i == 0) {      // V after the first Q: the item before frees V's buffer later than K's
             if (!(ok = wait(v_empty, (walk.round & 1) ^ 1))) break;
             if (elect_one()) {
@@ -378,6 +369,34 @@ attn_dkv_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensor
         drain_wait(q_full + 8 * (k % SQ), (k / SQ) & 1);
         drain_wait(do_full + 8 * (k % SQ), (k / SQ) & 1);
       }
+    }
+  } else if (warp == 10) {
+    // ================================================================= lse and delta of every block's rows
+    uint32_t u = 0;
+    bool ok = true;
+    for (ItemWalk walk(a.tiles, a.hk, items); ok && walk.valid; walk.next()) {
+      const AttnTile t = walk.t;
+      const int first = t.row / kAttnRows, per_head = per_head_of(t);
+      for (int hh = 0; ok && hh < group; ++hh)
+        for (int i = 0; i < per_head; ++i, ++u) {
+          const int row = (first + i) * 128, rows = t.len - row;
+          const int64_t at = (int64_t)(walk.h * group + hh) * a.tokens + t.start + row;
+          float lse[4], delta[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {      // negated; rows beyond the end: P = 2^-inf = 0
+            const int k = lane + 32 * j;
+            lse[j] = k < rows ? -a.lse[at + k] * kLog2e : -INFINITY;
+            delta[j] = k < rows ? -a.delta[at + k] : 0.f;
+          }
+          if (!(ok = wait(row_empty + 8 * (u % SR), ((u / SR) & 1) ^ 1))) break;
+          float* stats = row_stats + (u % SR) * 256;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            stats[lane + 32 * j] = lse[j];
+            stats[128 + lane + 32 * j] = delta[j];
+          }
+          mbar_arrive(row_full + 8 * (u % SR));
+        }
     }
   } else if (warp == 9) {
     // ================================================================= MMAs
@@ -438,10 +457,10 @@ attn_dkv_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensor
       const AttnTile t = walk.t;
       const int kvh = walk.h, round = walk.round, per_head = per_head_of(t), n = group * per_head;
       for (int i = 0, q = 0; i < n; ++i, ++u, q = q + 1 == per_head ? 0 : q + 1) {
-        const uint32_t st = u % SQ;
+        const uint32_t st = u % SR;
         const float4* lse4 = reinterpret_cast<const float4*>(row_stats + st * 256 + 64 * h);
         const float4* delta4 = lse4 + 32;
-        if (!(ok = wait(row_full + 8 * st, (u / SQ) & 1))) break;
+        if (!(ok = wait(row_full + 8 * st, (u / SR) & 1))) break;
         if (!(ok = wait(s_full, u & 1))) break;
         tc_fence_after();
         uint32_t s[64];
@@ -450,12 +469,8 @@ attn_dkv_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensor
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
           const float4 l = lse4[k];
-          p[2 * k] = fma2(two(s + 4 * k), c2, make_float2(l.x, l.y));
-          p[2 * k + 1] = fma2(two(s + 4 * k + 2), c2, make_float2(l.z, l.w));
-          p[2 * k].x = exp2_fast(p[2 * k].x);
-          p[2 * k].y = exp2_fast(p[2 * k].y);
-          p[2 * k + 1].x = exp2_fast(p[2 * k + 1].x);
-          p[2 * k + 1].y = exp2_fast(p[2 * k + 1].y);
+          p[2 * k] = exp2_pair(fma2(two(s + 4 * k), c2, make_float2(l.x, l.y)), 2 * k);
+          p[2 * k + 1] = exp2_pair(fma2(two(s + 4 * k + 2), c2, make_float2(l.z, l.w)), 2 * k + 1);
         }
         auto mask = [&]() {      // on the diagonal: queries before the key do not see it
 #pragma unroll
@@ -525,7 +540,7 @@ int launch(const fgd_attn_plan* plan, AttnArgs a, cudaStream_t st) {
   if (!map(&mq, a.q, a.hq) || !map(&mk, a.k, a.hk) || !map(&mv, a.v, a.hk) || !map(&mdo, a.dout, a.hq))
     return op_fail(FGD_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed", who);
   a.tiles = plan->kv_tiles;
-  dkv<<<(unsigned)(items_kv < sms ? items_kv : sms), kBwdThreads, dkv_smem<DP>(), st>>>(a, (int)items_kv, mq, mk, mv, mdo);
+  dkv<<<(unsigned)(items_kv < sms ? items_kv : sms), kDkvThreads, dkv_smem<DP>(), st>>>(a, (int)items_kv, mq, mk, mv, mdo);
   a.tiles = plan->q_tiles;
   dq<<<(unsigned)(items_q < sms ? items_q : sms), kBwdThreads, dq_smem<DP>(), st>>>(a, (int)items_q, mq, mk, mv, mdo);
   e = cudaGetLastError();

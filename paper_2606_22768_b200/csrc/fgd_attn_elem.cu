@@ -130,6 +130,45 @@ __global__ void __launch_bounds__(256) attn_delta_kernel(const AttnArgs a) {
   if (lane == 0) a.delta[(int64_t)head * a.tokens + token] = s;
 }
 
+// The same for 16-bit values in 16-byte vectors: L lanes take a row, a warp 32 tokens of one head (so that its 32 results are one
+// store), eight rows' loads per lane on their way at a time.
+template <typename T, int L>
+__global__ void __launch_bounds__(256) attn_delta_vec_kernel(const AttnArgs a) {
+  constexpr int RPS = 32 / L, AT_ONCE = 8;                 // rows per step of the warp, steps at a time
+  const int lane = threadIdx.x & 31, sub = lane / L, c = (lane % L) * 8;
+  const int64_t warp = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), head = warp % a.hq, token0 = warp / a.hq * 32;
+  if (token0 >= a.tokens) return;
+  float mine = 0.f;                                        // of token0 + lane
+#pragma unroll
+  for (int s0 = 0; s0 < L; s0 += AT_ONCE) {
+    ActPack<T, 8> o[AT_ONCE], g[AT_ONCE];
+#pragma unroll
+    for (int s = 0; s < AT_ONCE; ++s) {
+      const int64_t token = token0 + (s0 + s) * RPS + sub;
+      if (token < a.tokens && c < a.d) {
+        o[s] = load_stream<T, 8>(row_of<T>(a.o, token, (int)head) + c);
+        g[s] = load_stream<T, 8>(row_of<T>(a.dout, token, (int)head) + c);
+      } else {
+        zero(o[s]);
+        zero(g[s]);
+      }
+    }
+#pragma unroll
+    for (int s = 0; s < AT_ONCE; ++s) {
+      const Vals<8> x = unpack<T, 8>(o[s]), y = unpack<T, 8>(g[s]);
+      float2 v = both(0.f);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v = fma2(x.pair(k), y.pair(k), v);
+      float sum = v.x + v.y;
+#pragma unroll
+      for (int off = L / 2; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+      sum = __shfl_sync(0xffffffffu, sum, (lane % RPS) * L);
+      if (lane / RPS == s0 + s) mine = sum;
+    }
+  }
+  if (token0 + lane < a.tokens) a.delta[head * a.tokens + token0 + lane] = mine;
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kWarps * 32) attn_dq_elem_kernel(const AttnArgs a) {
   extern __shared__ float smem[];
@@ -259,14 +298,19 @@ int attn_forward_elem(const fgd_attn_plan* plan, int dtype, const AttnArgs& a, c
   }
 }
 
-int attn_delta(int dtype, const AttnArgs& a, cudaStream_t st) {
-  const int64_t blocks = (a.tokens * a.hq + 7) / 8;
+int attn_delta(int dtype, bool vectors, const AttnArgs& a, cudaStream_t st) {
+  const int64_t blocks = vectors ? ((a.tokens + 31) / 32 * a.hq + 7) / 8 : (a.tokens * a.hq + 7) / 8;
   if (blocks > 0x7fffffff) return op_fail(FGD_ERR_INVALID_ARG, "fgd_attn_backward: too many rows");
-  switch (dtype) {
-    case FGD_F32: attn_delta_kernel<float><<<(unsigned)blocks, 256, 0, st>>>(a); break;
-    case FGD_BF16: attn_delta_kernel<__nv_bfloat16><<<(unsigned)blocks, 256, 0, st>>>(a); break;
-    default: attn_delta_kernel<__half><<<(unsigned)blocks, 256, 0, st>>>(a); break;
-  }
+  auto vec = [&](auto zero) {
+    using T = decltype(zero);
+    if (a.d <= 64) attn_delta_vec_kernel<T, 8><<<(unsigned)blocks, 256, 0, st>>>(a);
+    else attn_delta_vec_kernel<T, 16><<<(unsigned)blocks, 256, 0, st>>>(a);
+  };
+  if (vectors && dtype == FGD_BF16) vec(__nv_bfloat16{});
+  else if (vectors) vec(__half{});
+  else if (dtype == FGD_F32) attn_delta_kernel<float><<<(unsigned)blocks, 256, 0, st>>>(a);
+  else if (dtype == FGD_BF16) attn_delta_kernel<__nv_bfloat16><<<(unsigned)blocks, 256, 0, st>>>(a);
+  else attn_delta_kernel<__half><<<(unsigned)blocks, 256, 0, st>>>(a);
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? FGD_OK : op_fail(FGD_ERR_CUDA, "fgd_attn_backward: launch failed: %s", cudaGetErrorString(e));
 }

@@ -258,9 +258,7 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, int per_tile, int items
           uint32_t p[16];
 #pragma unroll
           for (int k = 0; k < 16; ++k) {
-            float2 x = fma2(two(s + 32 * q + 2 * k), c2, m2);
-            x.x = exp2_fast(x.x);
-            x.y = exp2_fast(x.y);
+            const float2 x = exp2_pair(fma2(two(s + 32 * q + 2 * k), c2, m2), k);
             l = add2(l, x);
             p[k] = pack2<BF16>(x.x, x.y);
           }

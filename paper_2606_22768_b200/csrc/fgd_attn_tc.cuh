@@ -192,6 +192,27 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// 2^x on the FMA pipes: x = n + f with n the nearest integer, 2^f on [-1/2, 1/2] as a polynomial (minimax of degree 4 by Remez
+// exchange: relative error 2.7e-6, mean 4e-8, far below the 16-bit rounding of P and below 1e-6 in a row's sum), n added to the exponent.
+// The exponential units give 16 results a clock and SM, and a 128 x 128 block of scores has 16384 of them: 1024 clocks, as much as two of
+// its products take.  A share of the exponentials goes this way instead.  x below -126 gives 2^-126; an x that is not finite gives a
+// result that is not finite (or at least 2^127), or 2^-126 for -inf.
+__device__ __forceinline__ float2 exp2_poly(float2 x) {
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-126.f));
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-126.f));
+  const float2 t = add2(x, both(12582912.f)), f = fma2(add2(t, both(-12582912.f)), both(-1.f), x);
+  float2 p = fma2(both(0.009570102207362652f), f, both(0.05591785907745361f));
+  p = fma2(p, f, both(0.240247443318367f));
+  p = fma2(p, f, both(0.6931217908859253f));
+  p = fma2(p, f, both(0.9999992847442627f));
+  return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23)), __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
+}
+// 2^x for the k-th pair of a row: one pair in eight by polynomial (none, 1/8, 1/4: 16384 tokens forward 857, 828, 850 us; 1/2 in the
+// key kernel gains nothing either: the FMA pipes' instructions then cost what the exponential units save).
+__device__ __forceinline__ float2 exp2_pair(float2 x, int k) {
+  if (k % 8 == 7) return exp2_poly(x);
+  return make_float2(exp2_fast(x.x), exp2_fast(x.y));
+}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
