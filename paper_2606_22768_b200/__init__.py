@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass, field
 from typing import Optional
 
@@ -50,25 +51,10 @@ class _CMixDesc(ctypes.Structure):
                 ("w_self", ctypes.c_void_p), ("edge_mask", ctypes.c_void_p), ("W", ctypes.c_void_p)]
 
 
-class _CHeads(ctypes.Structure):
-    _fields_ = [("p", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
-
-
-class _CAttnArgs(ctypes.Structure):
-    _fields_ = [("dtype", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
-                ("q", _CHeads), ("k", _CHeads), ("v", _CHeads), ("o", _CHeads), ("lse", ctypes.c_void_p), ("scale", ctypes.c_double),
-                ("dout", _CHeads), ("delta", ctypes.c_void_p), ("dq", _CHeads), ("dk", _CHeads), ("dv", _CHeads)]
-
-
-class _CMat(ctypes.Structure):
-    _fields_ = [("p", ctypes.c_void_p), ("ld", ctypes.c_int64)]
-
-
-class _CBlockNormArgs(ctypes.Structure):
-    _fields_ = ([("dtype", ctypes.c_int32), ("workers", ctypes.c_int32), ("rows", ctypes.c_int64), ("width", ctypes.c_int64),
-                 ("gate_kind", ctypes.c_int32), ("eps", ctypes.c_double), ("res_scale", ctypes.c_double)]
-                + [(n, _CMat) for n in ("x", "y", "gate", "w_post", "w_pre", "x_new", "n", "dn", "dres", "dx", "dy", "dgate", "dw_post", "dw_pre")]
-                + [("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64)])
+# fgd_attn_args and fgd_block_norm_args as they lie in memory (native alignment).  Small calls are bound by what the host does per
+# call; one pack costs a fraction of filling nested ctypes structures.
+_ATTN_ARGS = struct.Struct("@4i 12q Qd 3qQ 9q")
+_NORM_ARGS = struct.Struct("@2i 2q i4x 2d 28q 2q")
 
 
 def _load():
@@ -98,11 +84,11 @@ def _load():
         "fgd_js_distance": (i32, [i32, i32, i64, i64, i32, vp, vp, vp, vp, vp, vp]),
         "fgd_attn_plan_create": (i32, [ctypes.POINTER(vp), i32, i32, vp]),
         "fgd_attn_plan_destroy": (i32, [vp]),
-        "fgd_attn_forward": (i32, [vp, ctypes.POINTER(_CAttnArgs), vp]),
-        "fgd_attn_backward": (i32, [vp, ctypes.POINTER(_CAttnArgs), vp]),
+        "fgd_attn_forward": (i32, [vp, vp, vp]),
+        "fgd_attn_backward": (i32, [vp, vp, vp]),
         "fgd_attn_status": (i32, [vp, vp]),
-        "fgd_block_norm_forward": (i32, [i32, ctypes.POINTER(_CBlockNormArgs), vp]),
-        "fgd_block_norm_backward": (i32, [i32, ctypes.POINTER(_CBlockNormArgs), vp]),
+        "fgd_block_norm_forward": (i32, [i32, vp, vp]),
+        "fgd_block_norm_backward": (i32, [i32, vp, vp]),
         "fgd_block_norm_workspace": (i64, [i32, i32, i32, i64, i64]),
         "fgd_act_save8": (i32, [i32, i32, i64, i64, vp, i64, vp, i64, vp, i64, vp]),
         "fgd_act_load8": (i32, [i32, i32, i64, i64, vp, i64, vp, i64, vp, i64, vp]),
@@ -443,14 +429,6 @@ def fgd_js_distance(worker_logits, avg_logits, top_idx, d_js, cd_worker, top_k: 
 FGD_F32, FGD_BF16, FGD_F16 = 0, 1, 2
 FGD_GATE_NONE, FGD_GATE_CHANNEL, FGD_GATE_ELEMENT = 0, 1, 2
 ACT8_GROUP = 32      # values that share one step in an 8-bit checkpoint
-_DTYPES = {"torch.float32": FGD_F32, "torch.bfloat16": FGD_BF16, "torch.float16": FGD_F16}
-
-
-def _dtype_of(t, name: str) -> int:
-    code = _DTYPES.get(str(t.dtype))
-    if code is None:
-        raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
-    return code
 
 
 def _op_check(rc: int) -> None:
@@ -458,8 +436,26 @@ def _op_check(rc: int) -> None:
         raise FgdError(rc, fgd_last_error(None))
 
 
-def _like(t, name: str, dtype, shape, device) -> None:
-    """Shape, type and device of a tensor argument."""
+def _types(torch):
+    """Codes of the activation types, by torch type."""
+    if not _types.codes:
+        _types.codes = {torch.float32: FGD_F32, torch.bfloat16: FGD_BF16, torch.float16: FGD_F16}
+    return _types.codes
+
+
+_types.codes = {}
+
+
+def _dtype_of(t, name: str) -> int:
+    import torch
+    code = _types(torch).get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+    return code
+
+
+def _refuse(t, name: str, dtype, shape, device) -> None:
+    """Why a tensor is not what it has to be."""
     if not getattr(t, "is_cuda", False):
         raise TypeError(f"{name} must be a CUDA tensor")
     if t.dtype != dtype:
@@ -468,13 +464,21 @@ def _like(t, name: str, dtype, shape, device) -> None:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, not on {device}")
+    raise ValueError(f"{name} must be contiguous along its last dimension")
 
 
 def _stream_on(stream, device):
     if stream is None:
         import torch
-        return torch.cuda.current_stream(device).cuda_stream
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # the handle without a Stream object around it (2 us of a small call)
+        return raw(device.index) if raw is not None else torch.cuda.current_stream(device).cuda_stream
     return getattr(stream, "cuda_stream", stream)
+
+
+def _device_of(t, name: str):
+    if not getattr(t, "is_cuda", False):
+        raise TypeError(f"{name} must be a CUDA tensor")
+    return t.device
 
 
 class AttnPlan:
@@ -507,95 +511,111 @@ def fgd_attn_status(plan: AttnPlan, stream=None) -> None:
     _op_check(_lib.fgd_attn_status(plan._h, _stream(stream)))
 
 
-def _heads(t, name: str, dtype, shape, device) -> _CHeads:
-    _like(t, name, dtype, shape, device)
-    if t.shape[2] > 1 and t.stride(2) != 1:
-        raise ValueError(f"{name} must be contiguous along the head width")
-    return _CHeads(t.data_ptr(), t.stride(0), t.stride(1))
+def _heads(t, name: str, dtype, shape, device):
+    """(pointer, token stride, head stride)"""
+    if t.dtype != dtype or t.shape != shape or t.device != device:
+        _refuse(t, name, dtype, shape, device)
+    token, head, last = t.stride()
+    if last != 1 and shape[2] > 1:
+        _refuse(t, name, dtype, shape, device)
+    return t.data_ptr(), token, head
 
 
-def _attn_args(plan, q, k, v, o, lse, scale):
+def _row_values(t, name: str, shape, device):
+    """Pointer of a contiguous fp32 [heads, tokens] tensor."""
+    import torch
+    if t.dtype != torch.float32 or t.shape != shape or t.device != device:
+        _refuse(t, name, torch.float32, shape, device)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+_NO_HEADS = (0, 0, 0)
+
+
+def _attn_shapes(plan, q, k):
     if q.dim() != 3 or k.dim() != 3:
         raise ValueError("q and k must be [tokens, heads, width]")
-    import torch
-    dev, (T, hq, d), hk = q.device, q.shape, k.shape[1]
-    if T != plan.tokens:
-        raise ValueError(f"q has {T} tokens, the plan {plan.tokens}")
-    if dev.type != "cuda" or dev.index != plan.device:
+    dev, qs, ks = _device_of(q, "q"), q.shape, k.shape
+    if qs[0] != plan.tokens:
+        raise ValueError(f"q has {qs[0]} tokens, the plan {plan.tokens}")
+    if dev.index != plan.device:
         raise ValueError(f"q is on {dev}, the plan on cuda:{plan.device}")
-    a = _CAttnArgs(_dtype_of(q, "q"), hq, hk, d, _heads(q, "q", q.dtype, (T, hq, d), dev), _heads(k, "k", q.dtype, (T, hk, d), dev),
-                   _heads(v, "v", q.dtype, (T, hk, d), dev), _heads(o, "o", q.dtype, (T, hq, d), dev))
-    _like(lse, "lse", torch.float32, (hq, T), dev)
-    if not lse.is_contiguous():
-        raise ValueError("lse must be contiguous")
-    a.lse, a.scale = lse.data_ptr(), float(d) ** -0.5 if scale is None else float(scale)
-    return a
+    return dev, qs, (qs[0], ks[1], qs[2]), (qs[1], qs[0])
 
 
 def fgd_attn_forward(plan: AttnPlan, q, k, v, o, lse, scale: Optional[float] = None, stream=None) -> None:
     """Causal attention over the plan's packed sequences: q [T, Hq, d], k and v [T, Hk, d] -> o [T, Hq, d], lse [Hq, T] (fp32).
     Any token and head strides (slices of a fused projection); ``scale`` defaults to d ** -0.5."""
-    a = _attn_args(plan, q, k, v, o, lse, scale)
-    _op_check(_lib.fgd_attn_forward(plan._h, ctypes.byref(a), _stream_on(stream, q.device)))
+    dev, qs, ks, rows = _attn_shapes(plan, q, k)
+    dt, d = q.dtype, qs[2]
+    args = _ATTN_ARGS.pack(_dtype_of(q, "q"), qs[1], ks[1], d, *_heads(q, "q", dt, qs, dev), *_heads(k, "k", dt, ks, dev), *_heads(v, "v", dt, ks, dev),
+                           *_heads(o, "o", dt, qs, dev), _row_values(lse, "lse", rows, dev), d ** -0.5 if scale is None else scale,
+                           *_NO_HEADS, 0, *_NO_HEADS, *_NO_HEADS, *_NO_HEADS)
+    _op_check(_lib.fgd_attn_forward(plan._h, args, _stream_on(stream, dev)))
 
 
 def fgd_attn_backward(plan: AttnPlan, q, k, v, o, dout, lse, delta, dq, dk, dv, scale: Optional[float] = None, stream=None) -> None:
     """Gradients of :func:`fgd_attn_forward` from its inputs, o and lse.  ``delta`` [Hq, T] (fp32) is scratch; dk and dv are summed
     over the query heads that share a key head."""
-    import torch
-    a = _attn_args(plan, q, k, v, o, lse, scale)
-    dev = q.device
-    _like(delta, "delta", torch.float32, lse.shape, dev)
-    if not delta.is_contiguous():
-        raise ValueError("delta must be contiguous")
-    a.delta = delta.data_ptr()
-    a.dout, a.dq = _heads(dout, "dout", q.dtype, q.shape, dev), _heads(dq, "dq", q.dtype, q.shape, dev)
-    a.dk, a.dv = _heads(dk, "dk", q.dtype, k.shape, dev), _heads(dv, "dv", q.dtype, k.shape, dev)
-    _op_check(_lib.fgd_attn_backward(plan._h, ctypes.byref(a), _stream_on(stream, dev)))
+    dev, qs, ks, rows = _attn_shapes(plan, q, k)
+    dt, d = q.dtype, qs[2]
+    args = _ATTN_ARGS.pack(_dtype_of(q, "q"), qs[1], ks[1], d, *_heads(q, "q", dt, qs, dev), *_heads(k, "k", dt, ks, dev), *_heads(v, "v", dt, ks, dev),
+                           *_heads(o, "o", dt, qs, dev), _row_values(lse, "lse", rows, dev), d ** -0.5 if scale is None else scale,
+                           *_heads(dout, "dout", dt, qs, dev), _row_values(delta, "delta", rows, dev),
+                           *_heads(dq, "dq", dt, qs, dev), *_heads(dk, "dk", dt, ks, dev), *_heads(dv, "dv", dt, ks, dev))
+    _op_check(_lib.fgd_attn_backward(plan._h, args, _stream_on(stream, dev)))
 
 
-def _mat(t, name: str, dtype, shape, device) -> _CMat:
+_NO_MAT = (0, 0)
+
+
+def _mat(t, name: str, dtype, rows: int, width: int, device):
+    """(pointer, row stride); (0, 0) for None"""
     if t is None:
-        return _CMat(None, 0)
-    _like(t, name, dtype, shape, device)
-    if shape[1] > 1 and t.stride(1) != 1:
-        raise ValueError(f"{name} must be contiguous along a row")
-    return _CMat(t.data_ptr(), t.stride(0) if shape[0] > 1 else max(t.stride(0), shape[1]))
+        return _NO_MAT
+    if t.dtype != dtype or t.shape != (rows, width) or t.device != device:
+        _refuse(t, name, dtype, (rows, width), device)
+    ld, last = t.stride()
+    if last != 1 and width > 1:
+        _refuse(t, name, dtype, (rows, width), device)
+    return t.data_ptr(), ld if rows > 1 else max(ld, width)
 
 
-def _block_norm_args(first, x_new, y, gate, w_post, w_pre, eps, res_scale):
-    """The part of the arguments that forward and backward share; ``first`` gives shape and type."""
+def _norm_shapes(first, gate, w_post, w_pre):
+    """device, rows, width, workers, gate kind and the type of the gate"""
+    import torch
     if first is None or first.dim() != 2:
         raise ValueError("activations must be [tokens, width]")
-    import torch
-    dev, (T, H) = first.device, first.shape
+    dev, (T, H) = _device_of(first, "activations"), first.shape
     channel = w_pre if w_pre is not None else w_post
     if channel is None and gate is not None and gate.dtype == torch.float32 and gate.shape != first.shape:
         channel = gate
     K = 1 if channel is None else channel.shape[0]
-    if T % K != 0:
+    if K < 1 or T % K != 0:
         raise ValueError(f"{T} rows do not split over {K} workers")
-    a = _CBlockNormArgs(_dtype_of(first, "activations"), K, T // K, H)
+    if gate is None:
+        return dev, T, H, K, FGD_GATE_NONE, torch.float32
     # [K, width] is a gate per channel, [T, width] one per element (one row per worker: the fp32 one counts as per channel)
-    by_channel = gate is not None and gate.shape[0] == K and (K != T or gate.dtype == torch.float32)
-    a.gate_kind = FGD_GATE_NONE if gate is None else FGD_GATE_CHANNEL if by_channel else FGD_GATE_ELEMENT
-    a.eps, a.res_scale = float(eps), float(res_scale)
-    f32 = torch.float32
-    a.x_new, a.y = _mat(x_new, "x_new", first.dtype, (T, H), dev), _mat(y, "y", first.dtype, (T, H), dev)
-    a.gate = _mat(gate, "gate", f32 if by_channel else first.dtype, (K if by_channel else T, H), dev)
-    a.w_post, a.w_pre = _mat(w_post, "w_post", f32, (K, H), dev), _mat(w_pre, "w_pre", f32, (K, H), dev)
-    return a, dev, T, H, K, by_channel
+    if gate.shape[0] == K and (K != T or gate.dtype == torch.float32):
+        return dev, T, H, K, FGD_GATE_CHANNEL, torch.float32
+    return dev, T, H, K, FGD_GATE_ELEMENT, first.dtype
 
 
 def fgd_block_norm_forward(x, y, gate, w_post, w_pre, x_new, n, eps: float = 1e-5, res_scale: float = 1.0, stream=None) -> None:
     """x_new = x + res_scale * gate * norm(y) * w_post and n = norm(x_new) * w_pre, in one pass.  Activations [T, H]; w_post, w_pre
     [K, H] fp32 for K workers with T / K rows each; gate None, [K, H] fp32 (per channel) or [T, H] (per element).  w_post, y, n (with
     w_pre), x_new and gate may be None, see ``include/fgd.h``; x_new may be x."""
-    a, dev, T, H, K, _ = _block_norm_args(x, x_new, y, gate, w_post, w_pre, eps, res_scale)
+    import torch
+    dev, T, H, K, kind, gate_type = _norm_shapes(x, gate, w_post, w_pre)
+    dt, f32, gate_rows = x.dtype, torch.float32, K if kind == FGD_GATE_CHANNEL else T
+    mats = (_mat(x, "x", dt, T, H, dev) + _mat(y, "y", dt, T, H, dev) + _mat(gate, "gate", gate_type, gate_rows, H, dev)
+            + _mat(w_post, "w_post", f32, K, H, dev) + _mat(w_pre, "w_pre", f32, K, H, dev) + _mat(x_new, "x_new", dt, T, H, dev) + _mat(n, "n", dt, T, H, dev))
     if T == 0:
         return
-    a.x, a.n = _mat(x, "x", x.dtype, (T, H), dev), _mat(n, "n", x.dtype, (T, H), dev)
-    _op_check(_lib.fgd_block_norm_forward(dev.index, ctypes.byref(a), _stream_on(stream, dev)))
+    args = _NORM_ARGS.pack(_dtype_of(x, "x"), K, T // K, H, kind, eps, res_scale, *mats, *_NO_MAT * 7, 0, 0)
+    _op_check(_lib.fgd_block_norm_forward(dev.index, args, _stream_on(stream, dev)))
 
 
 def fgd_block_norm_workspace(dtype: int, workers: int, rows: int, width: int, device: int = 0) -> int:
@@ -612,31 +632,25 @@ def fgd_block_norm_backward(dn, dres, x_new, y, gate, w_post, w_pre, dx, dy, dga
     (None: zero), dx may be dres.  ``workspace``: a uint8 CUDA tensor of :func:`fgd_block_norm_workspace` bytes (None: allocated here)."""
     import torch
     first = dn if dn is not None else dres
-    a, dev, T, H, K, by_channel = _block_norm_args(first, x_new, y, gate, w_post, w_pre, eps, res_scale)
-    f32 = torch.float32
-    a.dw_post, a.dw_pre = _mat(dw_post, "dw_post", f32, (K, H), dev), _mat(dw_pre, "dw_pre", f32, (K, H), dev)
-    a.dgate = _mat(dgate, "dgate", f32 if by_channel else first.dtype, (K if by_channel else T, H), dev)
+    dev, T, H, K, kind, gate_type = _norm_shapes(first, gate, w_post, w_pre)
+    dt, f32, gate_rows = first.dtype, torch.float32, K if kind == FGD_GATE_CHANNEL else T
+    mats = (_NO_MAT + _mat(y, "y", dt, T, H, dev) + _mat(gate, "gate", gate_type, gate_rows, H, dev) + _mat(w_post, "w_post", f32, K, H, dev)
+            + _mat(w_pre, "w_pre", f32, K, H, dev) + _mat(x_new, "x_new", dt, T, H, dev) + _NO_MAT + _mat(dn, "dn", dt, T, H, dev)
+            + _mat(dres, "dres", dt, T, H, dev) + _mat(dx, "dx", dt, T, H, dev) + _mat(dy, "dy", dt, T, H, dev) + _mat(dgate, "dgate", gate_type, gate_rows, H, dev)
+            + _mat(dw_post, "dw_post", f32, K, H, dev) + _mat(dw_pre, "dw_pre", f32, K, H, dev))
     if T == 0:
         with torch.cuda.stream(stream) if isinstance(stream, torch.cuda.Stream) else torch.cuda.device(dev):
             for g in (dw_post, dw_pre, dgate):
                 if g is not None:
                     g.zero_()
         return
-    for name, t in (("dn", dn), ("dres", dres), ("dx", dx), ("dy", dy)):
-        setattr(a, name, _mat(t, name, first.dtype, (T, H), dev))
-    need = fgd_block_norm_workspace(a.dtype, K, T // K, H, dev.index)
-    handle = _stream_on(stream, dev)
+    code, handle = _dtype_of(first, "activations"), _stream_on(stream, dev)
     if workspace is None:
-        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
-        if handle != torch.cuda.current_stream(dev).cuda_stream:   # the caching allocator must not hand it out again before the call has run
+        workspace = torch.empty(max(fgd_block_norm_workspace(code, K, T // K, H, dev.index), 1), dtype=torch.uint8, device=dev)
+        if stream is not None and handle != torch.cuda.current_stream(dev).cuda_stream:   # the caching allocator must not hand it out again before the call has run
             workspace.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(handle, device=dev))
-    a.workspace, a.workspace_bytes = _dev_ptr(workspace, "workspace", "torch.uint8"), workspace.numel()
-    _op_check(_lib.fgd_block_norm_backward(dev.index, ctypes.byref(a), handle))
-
-
-def _act8(t, name: str, dtype, rows: int, width: int, device):
-    m = _mat(t, name, dtype, (rows, width), device)
-    return m.p, m.ld
+    args = _NORM_ARGS.pack(code, K, T // K, H, kind, eps, res_scale, *mats, _dev_ptr(workspace, "workspace", "torch.uint8"), workspace.numel())
+    _op_check(_lib.fgd_block_norm_backward(dev.index, args, handle))
 
 
 def fgd_act_save8(x, q8, e8, stream=None) -> None:
@@ -644,9 +658,9 @@ def fgd_act_save8(x, q8, e8, stream=None) -> None:
     import torch
     if x.dim() != 2:
         raise ValueError("x must be [rows, width]")
-    (R, W), dev = x.shape, x.device
-    _op_check(_lib.fgd_act_save8(dev.index or 0, _dtype_of(x, "x"), R, W, *_act8(x, "x", x.dtype, R, W, dev), *_act8(q8, "q8", torch.int8, R, W, dev),
-                                 *_act8(e8, "e8", torch.uint8, R, -(-W // ACT8_GROUP), dev), _stream_on(stream, dev)))
+    (R, W), dev = x.shape, _device_of(x, "x")
+    _op_check(_lib.fgd_act_save8(dev.index, _dtype_of(x, "x"), R, W, *_mat(x, "x", x.dtype, R, W, dev), *_mat(q8, "q8", torch.int8, R, W, dev),
+                                 *_mat(e8, "e8", torch.uint8, R, -(-W // ACT8_GROUP), dev), _stream_on(stream, dev)))
 
 
 def fgd_act_load8(q8, e8, out, stream=None) -> None:
@@ -654,9 +668,9 @@ def fgd_act_load8(q8, e8, out, stream=None) -> None:
     import torch
     if out.dim() != 2:
         raise ValueError("out must be [rows, width]")
-    (R, W), dev = out.shape, out.device
-    _op_check(_lib.fgd_act_load8(dev.index or 0, _dtype_of(out, "out"), R, W, *_act8(q8, "q8", torch.int8, R, W, dev),
-                                 *_act8(e8, "e8", torch.uint8, R, -(-W // ACT8_GROUP), dev), *_act8(out, "out", out.dtype, R, W, dev), _stream_on(stream, dev)))
+    (R, W), dev = out.shape, _device_of(out, "out")
+    _op_check(_lib.fgd_act_load8(dev.index, _dtype_of(out, "out"), R, W, *_mat(q8, "q8", torch.int8, R, W, dev),
+                                 *_mat(e8, "e8", torch.uint8, R, -(-W // ACT8_GROUP), dev), *_mat(out, "out", out.dtype, R, W, dev), _stream_on(stream, dev)))
 
 
 def fgd_swiglu8_forward(gu, h, q8, e8, stream=None) -> None:
@@ -664,9 +678,9 @@ def fgd_swiglu8_forward(gu, h, q8, e8, stream=None) -> None:
     import torch
     if h.dim() != 2:
         raise ValueError("h must be [rows, width]")
-    (R, W), dev = h.shape, h.device
-    _op_check(_lib.fgd_swiglu8_forward(dev.index or 0, _dtype_of(h, "h"), R, W, *_act8(gu, "gu", h.dtype, R, 2 * W, dev), *_act8(h, "h", h.dtype, R, W, dev),
-                                       *_act8(q8, "q8", torch.int8, R, 2 * W, dev), *_act8(e8, "e8", torch.uint8, R, 2 * -(-W // ACT8_GROUP), dev),
+    (R, W), dev = h.shape, _device_of(h, "h")
+    _op_check(_lib.fgd_swiglu8_forward(dev.index, _dtype_of(h, "h"), R, W, *_mat(gu, "gu", h.dtype, R, 2 * W, dev), *_mat(h, "h", h.dtype, R, W, dev),
+                                       *_mat(q8, "q8", torch.int8, R, 2 * W, dev), *_mat(e8, "e8", torch.uint8, R, 2 * -(-W // ACT8_GROUP), dev),
                                        _stream_on(stream, dev)))
 
 
@@ -675,7 +689,7 @@ def fgd_swiglu8_backward(dh, q8, e8, dgu, h=None, stream=None) -> None:
     import torch
     if dh.dim() != 2:
         raise ValueError("dh must be [rows, width]")
-    (R, W), dev = dh.shape, dh.device
-    _op_check(_lib.fgd_swiglu8_backward(dev.index or 0, _dtype_of(dh, "dh"), R, W, *_act8(dh, "dh", dh.dtype, R, W, dev),
-                                        *_act8(q8, "q8", torch.int8, R, 2 * W, dev), *_act8(e8, "e8", torch.uint8, R, 2 * -(-W // ACT8_GROUP), dev),
-                                        *_act8(dgu, "dgu", dh.dtype, R, 2 * W, dev), *_act8(h, "h", dh.dtype, R, W, dev), _stream_on(stream, dev)))
+    (R, W), dev = dh.shape, _device_of(dh, "dh")
+    _op_check(_lib.fgd_swiglu8_backward(dev.index, _dtype_of(dh, "dh"), R, W, *_mat(dh, "dh", dh.dtype, R, W, dev),
+                                        *_mat(q8, "q8", torch.int8, R, 2 * W, dev), *_mat(e8, "e8", torch.uint8, R, 2 * -(-W // ACT8_GROUP), dev),
+                                        *_mat(dgu, "dgu", dh.dtype, R, 2 * W, dev), *_mat(h, "h", dh.dtype, R, W, dev), _stream_on(stream, dev)))

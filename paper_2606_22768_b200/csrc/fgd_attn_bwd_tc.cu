@@ -534,8 +534,8 @@ int launch(const fgd_attn_plan* plan, AttnArgs a, cudaStream_t st) {
   const int sms = sm_count();
   auto dq = attn_dq_tc_kernel<DP, BF16>;
   auto dkv = attn_dkv_tc_kernel<DP, BF16>;
-  cudaError_t e = cudaFuncSetAttribute(dq, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dq_smem<DP>());
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(dkv, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dkv_smem<DP>());
+  cudaError_t e = allow_smem<attn_dq_tc_kernel<DP, BF16>>(dq_smem<DP>());
+  if (e == cudaSuccess) e = allow_smem<attn_dkv_tc_kernel<DP, BF16>>(dkv_smem<DP>());
   if (e != cudaSuccess) return op_fail(FGD_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
   if (!map(&mq, a.q, a.hq) || !map(&mk, a.k, a.hk) || !map(&mv, a.v, a.hk) || !map(&mdo, a.dout, a.hq))
     return op_fail(FGD_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed", who);

@@ -311,7 +311,7 @@ int launch(const fgd_attn_plan* plan, AttnArgs a, cudaStream_t st) {
       !attn_tensor_map(plan->encode_tiled, &mv, BF16, a.v, a.tokens, a.hk, a.d, 128))
     return op_fail(FGD_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed", who);
   auto kern = attn_forward_tc_kernel<DP, BF16>;
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)fwd_smem<DP>());
+  cudaError_t e = allow_smem<attn_forward_tc_kernel<DP, BF16>>(fwd_smem<DP>());
   if (e == cudaSuccess) {
     const int sms = sm_count();
     kern<<<(unsigned)(items < sms ? items : sms), kFwdThreads, fwd_smem<DP>(), st>>>(a, pair_heads, per_tile, (int)items, mq, mk, mv);

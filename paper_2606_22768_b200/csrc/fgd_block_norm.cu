@@ -243,18 +243,23 @@ int ctas_per_worker(int64_t workers, int64_t rows, int nt, bool backward) {
   return (int)(c < 1 ? 1 : c);
 }
 
-template <typename T, int VEC, int NT, int VPT, int SF, int SB>
-cudaError_t launch_norm(const NormArgs& a, unsigned grid, bool backward, cudaStream_t st) {
-  const bool full = a.gate_kind == GATE_FULL;
-  auto kern = backward ? (full ? norm_backward_kernel<T, VEC, NT, VPT, SB, true> : norm_backward_kernel<T, VEC, NT, VPT, SB, false>)
-                       : (full ? norm_forward_kernel<T, VEC, NT, VPT, SF, true> : norm_forward_kernel<T, VEC, NT, VPT, SF, false>);
-  const size_t smem = (size_t)(backward ? SB * (full ? 5 : 4) : SF * (full ? 3 : 2)) * VPT * NT * 16;
-  cudaError_t e = smem > 32 * 1024 ? cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
+template <auto KERNEL>
+cudaError_t start(const NormArgs& a, unsigned grid, int threads, size_t smem, cudaStream_t st) {
+  cudaError_t e = smem > 32 * 1024 ? allow_smem<KERNEL>(smem) : cudaSuccess;
   if (e == cudaSuccess) {
-    kern<<<grid, NT, smem, st>>>(a);
+    KERNEL<<<grid, threads, smem, st>>>(a);
     e = cudaGetLastError();
   }
   return e;
+}
+template <typename T, int VEC, int NT, int VPT, int SF, int SB>
+cudaError_t launch_norm(const NormArgs& a, unsigned grid, bool backward, cudaStream_t st) {
+  constexpr size_t stage = (size_t)VPT * NT * 16;      // of one tensor
+  if (a.gate_kind == GATE_FULL)
+    return backward ? start<norm_backward_kernel<T, VEC, NT, VPT, SB, true>>(a, grid, NT, SB * 5 * stage, st)
+                    : start<norm_forward_kernel<T, VEC, NT, VPT, SF, true>>(a, grid, NT, SF * 3 * stage, st);
+  return backward ? start<norm_backward_kernel<T, VEC, NT, VPT, SB, false>>(a, grid, NT, SB * 4 * stage, st)
+                  : start<norm_forward_kernel<T, VEC, NT, VPT, SF, false>>(a, grid, NT, SF * 2 * stage, st);
 }
 template <typename T>
 cudaError_t launch_norm_shape(const NormArgs& a, Shape s, bool vec, unsigned grid, bool backward, cudaStream_t st) {

@@ -177,6 +177,18 @@ inline int sm_count() {
   return n;
 }
 
+// Opts a kernel in to `smem` bytes of dynamic shared memory, once per kernel (KERNEL names the instance) and device.
+template <auto KERNEL>
+cudaError_t allow_smem(size_t smem) {
+  static bool done[64] = {};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || (dev < 64 && done[dev])) return e;
+  e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e == cudaSuccess && dev < 64) done[dev] = true;
+  return e;
+}
+
 // The bytes that a matrix of `rows` rows of `width` elements, `ld` apart, touches.
 struct Span {
   uintptr_t lo = 0, hi = 0, ld = 0, width = 0;   // all in bytes; lo == hi: nothing
