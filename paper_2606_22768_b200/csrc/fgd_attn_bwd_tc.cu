@@ -267,6 +267,7 @@ attn_dq_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensorM
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
   }
+  wait_for_previous();      // started beside the key kernel: what follows in the stream has to find both done
 }
 
 // ------------------------------------------------------------------------------------------ dK, dV
@@ -300,6 +301,8 @@ attn_dkv_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensor
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  wait_for_previous();      // delta
+  let_next_start();         // the query kernel takes the SMs that this one leaves (or has no work for); it needs delta too, which is there now
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -540,10 +543,10 @@ int launch(const fgd_attn_plan* plan, AttnArgs a, cudaStream_t st) {
   if (!map(&mq, a.q, a.hq) || !map(&mk, a.k, a.hk) || !map(&mv, a.v, a.hk) || !map(&mdo, a.dout, a.hq))
     return op_fail(FGD_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed", who);
   a.tiles = plan->kv_tiles;
-  dkv<<<(unsigned)(items_kv < sms ? items_kv : sms), kDkvThreads, dkv_smem<DP>(), st>>>(a, (int)items_kv, mq, mk, mv, mdo);
+  e = launch_early(dkv, dim3((unsigned)(items_kv < sms ? items_kv : sms)), kDkvThreads, dkv_smem<DP>(), st, a, (int)items_kv, mq, mk, mv, mdo);
+  if (e != cudaSuccess) return op_fail(FGD_ERR_CUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
   a.tiles = plan->q_tiles;
-  dq<<<(unsigned)(items_q < sms ? items_q : sms), kBwdThreads, dq_smem<DP>(), st>>>(a, (int)items_q, mq, mk, mv, mdo);
-  e = cudaGetLastError();
+  e = launch_early(dq, dim3((unsigned)(items_q < sms ? items_q : sms)), kBwdThreads, dq_smem<DP>(), st, a, (int)items_q, mq, mk, mv, mdo);
   return e == cudaSuccess ? FGD_OK : op_fail(FGD_ERR_CUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
 }
 

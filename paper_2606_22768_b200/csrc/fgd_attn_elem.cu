@@ -135,6 +135,7 @@ __global__ void __launch_bounds__(256) attn_delta_kernel(const AttnArgs a) {
 template <typename T, int L>
 __global__ void __launch_bounds__(256) attn_delta_vec_kernel(const AttnArgs a) {
   constexpr int RPS = 32 / L, AT_ONCE = 8;                 // rows per step of the warp, steps at a time
+  let_next_start();
   const int lane = threadIdx.x & 31, sub = lane / L, c = (lane % L) * 8;
   const int64_t warp = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), head = warp % a.hq, token0 = warp / a.hq * 32;
   if (token0 >= a.tokens) return;

@@ -105,6 +105,7 @@ __global__ void __launch_bounds__(NT, NT <= 512 ? 512 / NT : 1) norm_backward_ke
   }
   RowFeed<T, VEC, NT, VPT, N, STAGES> feed;
   feed.start(in, a.width, ring, first, a.ctas, end);
+  let_next_start();      // the column sums' CTAs wait for this kernel's end on the SMs
   int slot = 0;
   for (int64_t row = first; row < end; row += a.ctas) {
     feed.next(in, row, a.ctas, end, row == first);
@@ -187,6 +188,7 @@ __global__ void __launch_bounds__(NT, NT <= 512 ? 512 / NT : 1) norm_backward_ke
 
 // Column sums over the CTAs of one worker, 32 columns per CTA, eight partial sums per column added in order.
 __global__ void __launch_bounds__(256) norm_columns_kernel(const NormArgs a) {
+  wait_for_previous();
   __shared__ float buf[2][8][32];
   const int lane = threadIdx.x & 31, part = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
   const int64_t worker = blockIdx.y;
@@ -265,14 +267,15 @@ template <typename T>
 cudaError_t launch_norm_shape(const NormArgs& a, Shape s, bool vec, unsigned grid, bool backward, cudaStream_t st) {
   constexpr int V = 16 / sizeof(T);
   if (vec) {
-    // rows in flight: forward 3 x 8 to 24 KB, backward 2 x 16 to 20 KB per 256 threads; two vectors per thread leave room for one
+    // rows in flight: forward 3 x 8 to 24 KB, backward 2 x 16 to 20 KB per 256 threads; two vectors per thread leave room for one.
+    // (Forward, 512 x 2: fp32 is faster without a ring, 94 against 85 % of the copy peak at 4096 columns, 16-bit with one, 66 against 57 % at 8192.)
     if (s.nt == 32) return launch_norm<T, V, 32, 1, 4, 3>(a, grid, backward, st);
     if (s.nt == 64) return launch_norm<T, V, 64, 1, 4, 3>(a, grid, backward, st);
     if (s.nt == 128) return launch_norm<T, V, 128, 1, 4, 3>(a, grid, backward, st);
     if (s.nt == 256 && s.vpt == 1) return launch_norm<T, V, 256, 1, 4, 3>(a, grid, backward, st);
     if (s.nt == 256) return launch_norm<T, V, 256, 2, 2, 2>(a, grid, backward, st);
     if (s.vpt == 1) return launch_norm<T, V, 512, 1, 4, 3>(a, grid, backward, st);
-    if (s.vpt == 2) return launch_norm<T, V, 512, 2, 2, 2>(a, grid, backward, st);
+    if (s.vpt == 2) return launch_norm<T, V, 512, 2, sizeof(T) == 4 ? 0 : 2, 2>(a, grid, backward, st);
     if (s.nt == 512) return launch_norm<T, V, 512, 4, 1, 1>(a, grid, backward, st);
     if constexpr (sizeof(T) == 4) return launch_norm<T, V, 1024, 4, 0, 0>(a, grid, backward, st);
     return cudaErrorInvalidValue;
@@ -374,8 +377,7 @@ int run_norm(const fgd_block_norm_args* b, bool backward, int device, void* stre
     default: e = launch_norm_shape<__half>(a, s, aligned, (unsigned)grid, backward, st); break;
   }
   if (e == cudaSuccess && columns) {
-    norm_columns_kernel<<<dim3((unsigned)((b->width + 31) / 32), (unsigned)b->workers), 256, 0, st>>>(a);
-    e = cudaGetLastError();
+    e = launch_early(norm_columns_kernel, dim3((unsigned)((b->width + 31) / 32), (unsigned)b->workers), 256, 0, st, a);
   }
   if (e != cudaSuccess) return op_fail(FGD_ERR_CUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
   return FGD_OK;

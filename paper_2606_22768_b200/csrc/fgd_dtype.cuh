@@ -11,6 +11,7 @@
 #include <cstdint>
 #include <cstdio>
 #include <type_traits>
+#include <utility>
 
 #include "fgd_internal.h"
 
@@ -175,6 +176,25 @@ inline int sm_count() {
   if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) n = 1;
   if (dev < 64) cached[dev] = n;
   return n;
+}
+
+// Programmatic dependent launch.  A kernel started with launch_early may begin while the kernel before it in the stream still runs,
+// once every CTA of that one has called let_next_start (or has ended); wait_for_previous then waits for its end and its writes.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+template <typename... P, typename... A>
+cudaError_t launch_early(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, A&&... args) {
+  cudaLaunchAttribute attr = {};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t c = {};
+  c.gridDim = grid;
+  c.blockDim = dim3(threads);
+  c.dynamicSmemBytes = smem;
+  c.stream = st;
+  c.attrs = &attr;
+  c.numAttrs = 1;
+  return cudaLaunchKernelEx(&c, kernel, P(std::forward<A>(args))...);
 }
 
 // Opts a kernel in to `smem` bytes of dynamic shared memory, once per kernel (KERNEL names the instance) and device.
