@@ -25,14 +25,15 @@ namespace {
 constexpr int kBwdThreads = 320;
 // query kernel: buffers of Q and dO, stages of K (needed by two products, two blocks apart) and of V
 template <int DP> constexpr int kBufQ = DP == 128 ? 1 : 2;
-constexpr int kStagesK = 3, kStagesV = 2;
-template <int DP> constexpr size_t dq_smem() { return 1024 + (size_t)(2 * kBufQ<DP> + kStagesK + kStagesV) * attn_tile_bytes<DP>(); }
+constexpr int kStagesK = 3;
+template <int DP> constexpr int kStagesV = DP == 128 ? 1 : 2;
+template <int DP> constexpr size_t dq_smem() { return 1024 + (size_t)(2 * kBufQ<DP> + kStagesK + kStagesV<DP>) * attn_tile_bytes<DP>() + 8 * kStoreStage; }
 // key kernel: K, V, stages of Q and dO, and of the rows' lse and delta, which a warp of their own fetches (behind the tiles, on the
 // loading warp's path, their latency held up every block: sixteen sequences of 1024, 16 heads of 64, 190 us)
 template <int DP> constexpr int kStagesQ = DP == 128 ? 2 : 4;
 constexpr int kStagesRow = 4;
 constexpr int kDkvThreads = 352;
-template <int DP> constexpr size_t dkv_smem() { return 1024 + (size_t)(2 + 2 * kStagesQ<DP>) * attn_tile_bytes<DP>() + kStagesRow * 2 * 128 * sizeof(float); }
+template <int DP> constexpr size_t dkv_smem() { return 1024 + (size_t)(2 + 2 * kStagesQ<DP>) * attn_tile_bytes<DP>() + kStagesRow * 2 * 128 * sizeof(float) + 8 * kStoreStage; }
 
 __device__ __forceinline__ void load_row64(uint32_t addr, uint32_t (&s)[64]) {
   tmem_ld_32(addr, s);
@@ -76,7 +77,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
 attn_dq_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                   const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo) {
   constexpr uint32_t TILE = attn_tile_bytes<DP>();
-  constexpr int SK = kStagesK, SV = kStagesV, NQ = kBufQ<DP>;
+  constexpr int SK = kStagesK, SV = kStagesV<DP>, NQ = kBufQ<DP>;
   extern __shared__ unsigned char smem_raw[];
   __shared__ __align__(8) unsigned long long bars[12 + 2 * (SK + SV)];
   __shared__ uint32_t tmem_slot;
@@ -218,7 +219,6 @@ attn_dq_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensorM
     while (ok && walk.valid) {
       const AttnTile t = walk.t;
       const int n = blocks(t), head = walk.h, round = walk.round;
-      const bool real = t.row + r < t.len;
       const float2 lse2 = both(-lse * kLog2e), delta2 = both(-delta);
       for (int i = 0; i < n; ++i, ++u) {
         const uint32_t ts = tmem + 128 * (u & 1) + 64 * h + lanes;
@@ -249,13 +249,14 @@ attn_dq_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensorM
       row_stats();
       if (!(ok = wait(dq_done, round & 1))) break;
       tc_fence_after();
-      char* out = a.dq.p + 2 * ((int64_t)(t.start + t.row + r) * a.dq.token + head * a.dq.head);
+      const int row0 = t.row + (warp & 3) * 32;
+      char* out = a.dq.p + 2 * ((int64_t)(t.start + row0) * a.dq.token + head * a.dq.head);
 #pragma unroll
       for (int k = 0; k < DP / 2; k += 32) {
         uint32_t o[32];
         tmem_ld_32(tmem + c_dq + h * (DP / 2) + k + lanes, o);
         tmem_ld_done<32>(o);
-        if (real) store_columns<BF16, 32>(out, o, a.scale, h * (DP / 2) + k, a.d);
+        store_rows<BF16>(base + (2 * NQ + SK + SV) * TILE + warp * kStoreStage, o, a.scale, out, 2 * a.dq.token, t.len - row0, h * (DP / 2) + k, a.d, lane);
       }
       tc_fence_before();
       mbar_arrive(dq_free);
@@ -503,17 +504,17 @@ attn_dkv_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensor
       walk.next();
       if (!(ok = wait(out_done, round & 1))) break;
       tc_fence_after();
-      const bool real = t.row + r < t.len;
-      const int64_t token = t.start + t.row + r;
+      const int row0 = t.row + (warp & 3) * 32;
       // half 0 writes dK, half 1 dV
       const AttnHeads& to = h ? a.dv : a.dk;
-      char* out = to.p + 2 * (token * to.token + kvh * to.head);
+      char* out = to.p + 2 * ((int64_t)(t.start + row0) * to.token + kvh * to.head);
+      unsigned char* stage = base + (2 + 2 * SQ) * TILE + SR * 2 * 128 * sizeof(float) + warp * kStoreStage;
 #pragma unroll
       for (int k = 0; k < DP; k += 32) {
         uint32_t o[32];
         tmem_ld_32(tmem + (h ? c_dv : c_dk) + k + lanes, o);
         tmem_ld_done<32>(o);
-        if (real) store_columns<BF16, 32>(out, o, h ? 1.f : a.scale, k, a.d);
+        store_rows<BF16>(stage, o, h ? 1.f : a.scale, out, 2 * to.token, t.len - row0, k, a.d, lane);
       }
       tc_fence_before();
       mbar_arrive(out_free);

@@ -25,7 +25,7 @@ template <int DP> constexpr int kFwdStages = DP == 128 ? 4 : 8;
 constexpr float kRescale = 8.f;   // log2
 
 template <int DP>
-constexpr size_t fwd_smem() { return 1024 + (size_t)(2 + kFwdStages<DP>) * attn_tile_bytes<DP>(); }
+constexpr size_t fwd_smem() { return 1024 + (size_t)(2 + kFwdStages<DP>) * attn_tile_bytes<DP>() + 8 * kStoreStage; }
 
 struct FwdItem {
   int start, len, kvh, nmax;
@@ -274,19 +274,18 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, int per_tile, int items
       if (!ok || !(ok = wait(pv_done + 8 * t, (n_pv - 1) & 1))) break;
       tc_fence_after();
       const float sum = l.x + l.y, f = 1.f / sum;
-      const int64_t row = it.row[t] + r;
-      const bool real = row < it.len;
-      char* out = a.o.p + 2 * ((it.start + row) * a.o.token + it.head[t] * a.o.head);
+      const int row0 = it.row[t] + (warp & 3) * 32;      // the warp's first row
+      char* out = a.o.p + 2 * ((int64_t)(it.start + row0) * a.o.token + it.head[t] * a.o.head);
 #pragma unroll
       for (int k = 0; k < DP; k += 32) {
         uint32_t o[32];
         tmem_ld_32(to + k, o);
         tmem_ld_done<32>(o);
-        if (real) store_columns<BF16, 32>(out, o, f, k, a.d);
+        store_rows<BF16>(base + (2 + ST) * TILE + warp * kStoreStage, o, f, out, 2 * a.o.token, it.len - row0, k, a.d, lane);
       }
       tc_fence_before();
       mbar_arrive(o_free + 8 * t);
-      if (real) a.lse[it.head[t] * a.tokens + it.start + row] = (m + log2f(sum)) * kLn2;
+      if (row0 + lane < it.len) a.lse[it.head[t] * a.tokens + it.start + row0 + lane] = (m + log2f(sum)) * kLn2;
     }
   }
   tc_fence_before();

@@ -226,19 +226,30 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
-// N columns [c0, c0 + N) of one row, times f, as 16-bit values to `out` (the row's first column); columns at or beyond d are not the row's.
-template <bool BF16, int N>
-__device__ __forceinline__ void store_columns(char* out, const uint32_t* r, float f, int c0, int d) {
+// 32 rows x 32 columns [c0, c0 + 32), a row in each lane's registers, times f, as 16-bit values to memory: through 2 KB of shared
+// memory of the warp's own, so that four lanes write 64 bytes of a row together.  (A lane writing its own row puts every store's 32
+// pieces on 32 lines: an item's outputs then hold up the load / store unit, and with it every wait of the CTA, for thousands of clocks.)
+// `out`: the warp's first row; rows at or beyond `rows` and columns at or beyond d are not written.
+constexpr size_t kStoreStage = 32 * 64;
+template <bool BF16>
+__device__ __forceinline__ void store_rows(unsigned char* stage, const uint32_t* r, float f, char* out, int64_t row_bytes, int rows, int c0, int d, int lane) {
 #pragma unroll
-  for (int c = 0; c < N; c += 8) {
-    if (c0 + c >= d) continue;
+  for (int j = 0; j < 4; ++j) {
     uint4 w;
-    w.x = pack2<BF16>(__uint_as_float(r[c]) * f, __uint_as_float(r[c + 1]) * f);
-    w.y = pack2<BF16>(__uint_as_float(r[c + 2]) * f, __uint_as_float(r[c + 3]) * f);
-    w.z = pack2<BF16>(__uint_as_float(r[c + 4]) * f, __uint_as_float(r[c + 5]) * f);
-    w.w = pack2<BF16>(__uint_as_float(r[c + 6]) * f, __uint_as_float(r[c + 7]) * f);
-    *reinterpret_cast<uint4*>(out + 2 * (c0 + c)) = w;
+    w.x = pack2<BF16>(__uint_as_float(r[8 * j]) * f, __uint_as_float(r[8 * j + 1]) * f);
+    w.y = pack2<BF16>(__uint_as_float(r[8 * j + 2]) * f, __uint_as_float(r[8 * j + 3]) * f);
+    w.z = pack2<BF16>(__uint_as_float(r[8 * j + 4]) * f, __uint_as_float(r[8 * j + 5]) * f);
+    w.w = pack2<BF16>(__uint_as_float(r[8 * j + 6]) * f, __uint_as_float(r[8 * j + 7]) * f);
+    *reinterpret_cast<uint4*>(stage + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4)) = w;      // (no bank is hit twice in a quarter warp)
   }
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = 8 * i + (lane >> 2), j = lane & 3;
+    const uint4 w = *reinterpret_cast<const uint4*>(stage + row * 64 + ((j ^ ((row >> 1) & 3)) << 4));
+    if (row < rows && c0 + 8 * j < d) *reinterpret_cast<uint4*>(out + row * row_bytes + 2 * (c0 + 8 * j)) = w;
+  }
+  __syncwarp();
 }
 
 // The work items of a persistent CTA: `items` = tiles x heads, sorted by descending work, taken forwards and backwards by turns so
