@@ -56,6 +56,7 @@ AttnArgs kernel_args(const fgd_attn_plan* plan, const fgd_attn_args* b) {
   a.dout = heads_of(b->dout); a.dq = heads_of(b->dq); a.dk = heads_of(b->dk); a.dv = heads_of(b->dv);
   a.lse = b->lse; a.delta = b->delta; a.tokens = plan->tokens;
   a.hq = b->n_q_heads; a.hk = b->n_kv_heads; a.d = b->head_dim; a.scale = (float)b->scale;
+  a.inv_group = (float)b->n_kv_heads / (float)b->n_q_heads;
   a.status = plan->status;
   return a;
 }

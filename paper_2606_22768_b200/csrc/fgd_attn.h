@@ -33,7 +33,7 @@ struct AttnArgs {
   float* delta;    // [n_q_heads, tokens]: sum over the width of o * dout
   int64_t tokens;
   int hq, hk, d;
-  float scale;
+  float scale, inv_group;   // inv_group: n_kv_heads / n_q_heads
   const AttnTile* tiles;
   int n_tiles;
   int* status;

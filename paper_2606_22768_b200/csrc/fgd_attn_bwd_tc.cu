@@ -58,7 +58,7 @@ struct BlockWalk {
   Count count;          // blocks of an item's tile
   int i, n;             // block and blocks of the item
   uint32_t u;           // block over all items
-  __device__ __forceinline__ BlockWalk(const AttnTile* tiles, int per_tile, int items, Count c) : walk(tiles, per_tile, items), count(c), i(0), u(0) { n = walk.valid ? count(walk.t) : 0; }
+  __device__ __forceinline__ BlockWalk(const AttnTile* tiles, FastDiv per_tile, int items, Count c) : walk(tiles, per_tile, items), count(c), i(0), u(0) { n = walk.valid ? count(walk.t) : 0; }
   __device__ __forceinline__ bool valid() const { return walk.valid; }
   __device__ __forceinline__ bool last() const { return i == n - 1; }
   __device__ __forceinline__ void next() {
@@ -74,7 +74,7 @@ struct BlockWalk {
 // ------------------------------------------------------------------------------------------ dQ
 template <int DP, bool BF16>
 __global__ void __launch_bounds__(kBwdThreads, 1)
-attn_dq_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
+attn_dq_tc_kernel(const AttnArgs a, FastDiv heads, int items, const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                   const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo) {
   constexpr uint32_t TILE = attn_tile_bytes<DP>();
   constexpr int SK = kStagesK, SV = kStagesV<DP>, NQ = kBufQ<DP>;
@@ -113,10 +113,10 @@ attn_dq_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensorM
     // ================================================================= loads
     uint32_t u = 0, n_raw = 0;
     bool ok = true;
-    ItemWalk walk(a.tiles, a.hq, items);
+    ItemWalk walk(a.tiles, heads, items);
     for (; ok && walk.valid; walk.next()) {
       const AttnTile t = walk.t;
-      const int kvh = walk.h / group;
+      const int kvh = (int)(((float)walk.h + 0.5f) * a.inv_group);      // (exact: heads are below 2^15)
       const uint32_t qb = walk.round % NQ;
       if (!(ok = wait(q_empty + 8 * qb, ((walk.round / NQ) & 1) ^ 1))) break;
       if (elect_one()) {
@@ -159,7 +159,7 @@ attn_dq_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensorM
   } else if (warp == 9) {
     // ================================================================= MMAs
     bool ok = true;
-    BlockWalk as(a.tiles, a.hq, items, blocks), ad(a.tiles, a.hq, items, blocks), now(a.tiles, a.hq, items, blocks);
+    BlockWalk as(a.tiles, heads, items, blocks), ad(a.tiles, heads, items, blocks), now(a.tiles, heads, items, blocks);
     auto score = [&]() {
       if (!as.valid()) return true;
       const uint32_t k = as.u, qb = as.walk.round % NQ;
@@ -206,7 +206,7 @@ attn_dq_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensorM
     const float2 c2 = both(a.scale * kLog2e);
     uint32_t u = 0;
     bool ok = true;
-    ItemWalk walk(a.tiles, a.hq, items);
+    ItemWalk walk(a.tiles, heads, items);
     float lse = 0.f, delta = 0.f;      // of this thread's row of the coming item
     auto row_stats = [&]() {
       if (walk.valid && walk.t.row + r < walk.t.len) {
@@ -251,7 +251,7 @@ attn_dq_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensorM
       tc_fence_after();
       const int row0 = t.row + (warp & 3) * 32;
       char* out = a.dq.p + 2 * ((int64_t)(t.start + row0) * a.dq.token + head * a.dq.head);
-#pragma unroll
+#pragma unroll 1      // (once per item: code that stays short stays in the instruction cache)
       for (int k = 0; k < DP / 2; k += 32) {
         uint32_t o[32];
         tmem_ld_32(tmem + c_dq + h * (DP / 2) + k + lanes, o);
@@ -274,7 +274,7 @@ attn_dq_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensorM
 // ------------------------------------------------------------------------------------------ dK, dV
 template <int DP, bool BF16>
 __global__ void __launch_bounds__(kDkvThreads, 1)
-attn_dkv_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
+attn_dkv_tc_kernel(const AttnArgs a, FastDiv heads, int items, const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                    const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo) {
   constexpr uint32_t TILE = attn_tile_bytes<DP>();
   constexpr int SQ = kStagesQ<DP>, SR = kStagesRow;
@@ -338,7 +338,7 @@ attn_dkv_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensor
       if (elect_one()) mbar_arrive(bar);
       return true;
     };
-    ItemWalk walk(a.tiles, a.hk, items);
+    ItemWalk walk(a.tiles, heads, items);
     for (; ok && walk.valid; walk.next()) {
       const AttnTile t = walk.t;
       const int kvh = walk.h, first = t.row / kAttnRows, per_head = per_head_of(t);
@@ -378,7 +378,7 @@ attn_dkv_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensor
     // ================================================================= lse and delta of every block's rows
     uint32_t u = 0;
     bool ok = true;
-    for (ItemWalk walk(a.tiles, a.hk, items); ok && walk.valid; walk.next()) {
+    for (ItemWalk walk(a.tiles, heads, items); ok && walk.valid; walk.next()) {
       const AttnTile t = walk.t;
       const int first = t.row / kAttnRows, per_head = per_head_of(t);
       for (int hh = 0; ok && hh < group; ++hh)
@@ -405,7 +405,7 @@ attn_dkv_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensor
   } else if (warp == 9) {
     // ================================================================= MMAs
     bool ok = true;
-    BlockWalk as(a.tiles, a.hk, items, blocks), ad(a.tiles, a.hk, items, blocks), now(a.tiles, a.hk, items, blocks);
+    BlockWalk as(a.tiles, heads, items, blocks), ad(a.tiles, heads, items, blocks), now(a.tiles, heads, items, blocks);
     auto score = [&]() {
       if (!as.valid()) return true;
       const uint32_t k = as.u;
@@ -456,7 +456,7 @@ attn_dkv_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensor
     const float2 c2 = both(a.scale * kLog2e);
     uint32_t u = 0;
     bool ok = true;
-    ItemWalk walk(a.tiles, a.hk, items);
+    ItemWalk walk(a.tiles, heads, items);
     while (ok && walk.valid) {
       const AttnTile t = walk.t;
       const int kvh = walk.h, round = walk.round, per_head = per_head_of(t), n = group * per_head;
@@ -509,7 +509,7 @@ attn_dkv_tc_kernel(const AttnArgs a, int items, const __grid_constant__ CUtensor
       const AttnHeads& to = h ? a.dv : a.dk;
       char* out = to.p + 2 * ((int64_t)(t.start + row0) * to.token + kvh * to.head);
       unsigned char* stage = base + (2 + 2 * SQ) * TILE + SR * 2 * 128 * sizeof(float) + warp * kStoreStage;
-#pragma unroll
+#pragma unroll 1
       for (int k = 0; k < DP; k += 32) {
         uint32_t o[32];
         tmem_ld_32(tmem + (h ? c_dv : c_dk) + k + lanes, o);
@@ -544,10 +544,10 @@ int launch(const fgd_attn_plan* plan, AttnArgs a, cudaStream_t st) {
   if (!map(&mq, a.q, a.hq) || !map(&mk, a.k, a.hk) || !map(&mv, a.v, a.hk) || !map(&mdo, a.dout, a.hq))
     return op_fail(FGD_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed", who);
   a.tiles = plan->kv_tiles;
-  e = launch_early(dkv, dim3((unsigned)(items_kv < sms ? items_kv : sms)), kDkvThreads, dkv_smem<DP>(), st, a, (int)items_kv, mq, mk, mv, mdo);
+  e = launch_early(dkv, dim3((unsigned)(items_kv < sms ? items_kv : sms)), kDkvThreads, dkv_smem<DP>(), st, a, FastDiv(a.hk), (int)items_kv, mq, mk, mv, mdo);
   if (e != cudaSuccess) return op_fail(FGD_ERR_CUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
   a.tiles = plan->q_tiles;
-  e = launch_early(dq, dim3((unsigned)(items_q < sms ? items_q : sms)), kBwdThreads, dq_smem<DP>(), st, a, (int)items_q, mq, mk, mv, mdo);
+  e = launch_early(dq, dim3((unsigned)(items_q < sms ? items_q : sms)), kBwdThreads, dq_smem<DP>(), st, a, FastDiv(a.hq), (int)items_q, mq, mk, mv, mdo);
   return e == cudaSuccess ? FGD_OK : op_fail(FGD_ERR_CUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
 }
 

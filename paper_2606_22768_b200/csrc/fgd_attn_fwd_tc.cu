@@ -42,13 +42,13 @@ __device__ __forceinline__ FwdItem fwd_item(const AttnArgs& a, int pair_heads, c
   it.n[0] = t.row / kAttnRows + 1;
   it.n[1] = it.row[1] < t.len ? it.row[1] / kAttnRows + 1 : 0;
   it.nmax = max(it.n[0], it.n[1]);
-  it.kvh = it.head[0] / (a.hq / a.hk);
+  it.kvh = (int)(((float)it.head[0] + 0.5f) * a.inv_group);      // (exact: heads are below 2^15)
   return it;
 }
 
 template <int DP, bool BF16>
 __global__ void __launch_bounds__(kFwdThreads, 1)
-attn_forward_tc_kernel(const AttnArgs a, int pair_heads, int per_tile, int items, const __grid_constant__ CUtensorMap mq,
+attn_forward_tc_kernel(const AttnArgs a, int pair_heads, FastDiv per_tile, int items, const __grid_constant__ CUtensorMap mq,
                        const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv) {
   constexpr int ST = kFwdStages<DP>;
   constexpr uint32_t TILE = attn_tile_bytes<DP>();
@@ -313,7 +313,7 @@ int launch(const fgd_attn_plan* plan, AttnArgs a, cudaStream_t st) {
   cudaError_t e = allow_smem<attn_forward_tc_kernel<DP, BF16>>(fwd_smem<DP>());
   if (e == cudaSuccess) {
     const int sms = sm_count();
-    kern<<<(unsigned)(items < sms ? items : sms), kFwdThreads, fwd_smem<DP>(), st>>>(a, pair_heads, per_tile, (int)items, mq, mk, mv);
+    kern<<<(unsigned)(items < sms ? items : sms), kFwdThreads, fwd_smem<DP>(), st>>>(a, pair_heads, FastDiv(per_tile), (int)items, mq, mk, mv);
     e = cudaGetLastError();
   }
   return e == cudaSuccess ? FGD_OK : op_fail(FGD_ERR_CUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));

@@ -252,12 +252,31 @@ __device__ __forceinline__ void store_rows(unsigned char* stage, const uint32_t*
   __syncwarp();
 }
 
+// Division of numbers below 2^31 by a divisor fixed at launch: a high product and a shift.
+struct FastDiv {
+  uint32_t d, mul, shift;
+  FastDiv() = default;
+  explicit FastDiv(int divisor) : d((uint32_t)divisor) {      // mul = ceil(2^(32 + shift) / d), 2^shift >= d: exact for 31-bit numbers
+    shift = 0;
+    while ((1u << shift) < d) ++shift;
+    const uint64_t m = (((uint64_t)1 << (32 + shift)) + d - 1) / d;
+    mul = (uint32_t)(m - ((uint64_t)1 << 32) * (d > 1 && shift > 0 ? 1 : 0));
+    if (d == 1) mul = 0;
+  }
+  __device__ __forceinline__ int div(int n) const {
+    if (d == 1) return n;
+    const uint32_t t = __umulhi((uint32_t)n, mul);      // m = 2^32 + mul: n m / 2^32 = n + t
+    return (int)(((uint32_t)n + t) >> shift);
+  }
+};
+
 // The work items of a persistent CTA: `items` = tiles x heads, sorted by descending work, taken forwards and backwards by turns so
 // that a CTA that got a large item gets a small one next.  The tile after the current one is read ahead: its latency (and the
 // division) would otherwise stand between two items in every role.
 struct ItemWalk {
   const AttnTile* tiles;
-  int per_tile, items;
+  FastDiv per_tile;
+  int items;
   int round;             // of the current item, counted from 0
   bool valid;
   AttnTile t, t_next;
@@ -267,12 +286,12 @@ struct ItemWalk {
     const int w = r * (int)gridDim.x + ((r & 1) ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
     valid_next = w < items;      // only the last, partial round can lack an item
     if (valid_next) {
-      const int tile = w / per_tile;
-      h_next = w - tile * per_tile;
+      const int tile = per_tile.div(w);
+      h_next = w - tile * (int)per_tile.d;
       t_next = tiles[tile];
     }
   }
-  __device__ __forceinline__ ItemWalk(const AttnTile* tiles_, int per_tile_, int items_) : tiles(tiles_), per_tile(per_tile_), items(items_), round(-1) {
+  __device__ __forceinline__ ItemWalk(const AttnTile* tiles_, FastDiv per_tile_, int items_) : tiles(tiles_), per_tile(per_tile_), items(items_), round(-1) {
     look(0);
     next();
   }
