@@ -322,6 +322,9 @@ int fgd_attn_backward(fgd_attn_plan* plan, const fgd_attn_args* args, void* stre
 /* As fgd_device_status, for the kernels that used this plan: synchronises `stream`, reports
  * FGD_ERR_TIMEOUT if a bounded device-side wait gave up since the last check, and clears the flag. */
 int fgd_attn_status(fgd_attn_plan* plan, void* stream);
+/* As fgd_debug_set, for the kernels that use this plan: FGD_DEBUG_SPIN_LIMIT, and FGD_DEBUG_SKIP_TILE (every CTA of a
+ * tensor-core kernel announces but never issues the load of its value-th streamed tile, counted from 0).  Not for production use. */
+int fgd_attn_debug_set(fgd_attn_plan* plan, int key, int64_t value);
 
 /* A [rows, width] matrix, `ld` elements between rows; p == NULL: absent. */
 typedef struct {

@@ -87,6 +87,7 @@ def _load():
         "fgd_attn_forward": (i32, [vp, vp, vp]),
         "fgd_attn_backward": (i32, [vp, vp, vp]),
         "fgd_attn_status": (i32, [vp, vp]),
+        "fgd_attn_debug_set": (i32, [vp, i32, i64]),
         "fgd_block_norm_forward": (i32, [i32, vp, vp]),
         "fgd_block_norm_backward": (i32, [i32, vp, vp]),
         "fgd_block_norm_workspace": (i64, [i32, i32, i32, i64, i64]),
@@ -509,6 +510,11 @@ class AttnPlan:
 def fgd_attn_status(plan: AttnPlan, stream=None) -> None:
     """Synchronises the stream; raises FgdError(FGD_ERR_TIMEOUT) if a device-side wait of a kernel of this plan gave up."""
     _op_check(_lib.fgd_attn_status(plan._h, _stream(stream)))
+
+
+def fgd_attn_debug_set(plan: AttnPlan, key: int, value: int) -> None:
+    """Test hooks for the bounded device-side waits of the attention kernels (see ``include/fgd.h``)."""
+    _op_check(_lib.fgd_attn_debug_set(plan._h, int(key), int(value)))
 
 
 def _heads(t, name: str, dtype, shape, device):

@@ -58,6 +58,8 @@ AttnArgs kernel_args(const fgd_attn_plan* plan, const fgd_attn_args* b) {
   a.hq = b->n_q_heads; a.hk = b->n_kv_heads; a.d = b->head_dim; a.scale = (float)b->scale;
   a.inv_group = (float)b->n_kv_heads / (float)b->n_q_heads;
   a.status = plan->status;
+  a.spin_limit = plan->dbg_spin_limit ? plan->dbg_spin_limit : kAttnSpin;
+  a.skip = plan->dbg_skip;
   return a;
 }
 
@@ -133,6 +135,22 @@ extern "C" int fgd_attn_plan_destroy(fgd_attn_plan* plan) {
   if (plan->q_tiles) cudaFree(plan->q_tiles);
   delete plan;
   return FGD_OK;
+}
+
+extern "C" int fgd_attn_debug_set(fgd_attn_plan* plan, int key, int64_t value) {
+  if (!plan) return op_fail(FGD_ERR_INVALID_ARG, "fgd_attn_debug_set: NULL plan");
+  switch (key) {
+    case FGD_DEBUG_SPIN_LIMIT:
+      if (value < 0 || value > (int64_t)0xffffffffu) return op_fail(FGD_ERR_INVALID_ARG, "fgd_attn_debug_set: spin limit %lld out of range", (long long)value);
+      plan->dbg_spin_limit = (uint32_t)value;
+      return FGD_OK;
+    case FGD_DEBUG_SKIP_TILE:
+      if (value < -1 || value > 0x7fffffff) return op_fail(FGD_ERR_INVALID_ARG, "fgd_attn_debug_set: tile index %lld out of range", (long long)value);
+      plan->dbg_skip = (int)value;
+      return FGD_OK;
+    default:
+      return op_fail(FGD_ERR_INVALID_ARG, "fgd_attn_debug_set: unknown key %d", key);
+  }
 }
 
 extern "C" int fgd_attn_status(fgd_attn_plan* plan, void* stream) {

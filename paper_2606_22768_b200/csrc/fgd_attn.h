@@ -21,6 +21,7 @@ struct alignas(16) AttnTile {
 };
 
 constexpr int kAttnRows = 128;   // rows of a tile
+constexpr uint32_t kAttnSpin = 1u << 22;   // polls before a wait gives up
 
 struct AttnHeads {
   char* p;
@@ -37,6 +38,8 @@ struct AttnArgs {
   const AttnTile* tiles;
   int n_tiles;
   int* status;
+  uint32_t spin_limit;   // polls before a wait gives up
+  int skip;              // test hook: the streamed tile of every CTA whose load is announced but not issued (-1: none)
 };
 
 }  // namespace fgd
@@ -52,6 +55,8 @@ struct fgd_attn_plan {
   fgd::AttnTile* kv_tiles = nullptr;   // 128 rows each, by descending number of rows that follow
   int* status = nullptr;               // set by a device-side wait that gave up
   void* encode_tiled = nullptr;        // cuTensorMapEncodeTiled
+  uint32_t dbg_spin_limit = 0;         // fgd_attn_debug_set: 0 = the default
+  int dbg_skip = -1;
 };
 
 namespace fgd {

@@ -104,7 +104,7 @@ attn_dq_tc_kernel(const AttnArgs a, FastDiv heads, int items, const __grid_const
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = uniform(tmem_slot), c_dp = 256, c_dq = 384;
-  const AttnWait wait{&abort_flag, a.status};
+  const AttnWait wait{&abort_flag, a.status, a.spin_limit};
   const int group = a.hq / a.hk;
   // the key blocks that a query tile sees, from the diagonal down to block 0
   auto blocks = [](const AttnTile& t) { return t.row / kAttnRows + 1; };
@@ -131,16 +131,16 @@ attn_dq_tc_kernel(const AttnArgs a, FastDiv heads, int items, const __grid_const
         if (rows >= 128) {
           if (elect_one()) {
             mbar_expect_tx(kb, TILE);
-            load_tile<DP>(sk + ik * TILE, &mk, kvh, token, kb);
+            if ((int)u != a.skip) load_tile<DP>(sk + ik * TILE, &mk, kvh, token, kb);
           }
         } else {     // dQ = dS K must not meet the next sequence's keys
           if (elect_one()) {
             mbar_expect_tx(raw, TILE);
-            load_tile<DP>(sk + ik * TILE, &mk, kvh, token, raw);
+            if ((int)u != a.skip) load_tile<DP>(sk + ik * TILE, &mk, kvh, token, raw);
           }
           ok = wait(raw, n_raw & 1);
           ++n_raw;
-          if (!ok) { drain_wait(raw, (n_raw - 1) & 1); break; }
+          if (!ok) { wait.drain(raw, (n_raw - 1) & 1); break; }
           zero_rows<DP, 128>(base + (2 * NQ + ik) * TILE, rows, lane);
           if (elect_one()) mbar_arrive(kb);
         }
@@ -152,9 +152,9 @@ attn_dq_tc_kernel(const AttnArgs a, FastDiv heads, int items, const __grid_const
       }
     }
     if (wait.given_up()) {
-      for (int k = walk.round > 0 ? walk.round - 1 : 0; k <= walk.round; ++k) drain_wait(q_full + 8 * (k % NQ), (k / NQ) & 1);
-      for (uint32_t k = u > (uint32_t)SK ? u - SK : 0; k <= u; ++k) drain_wait(k_full + 8 * (k % SK), (k / SK) & 1);
-      for (uint32_t k = u > (uint32_t)SV ? u - SV : 0; k <= u; ++k) drain_wait(v_full + 8 * (k % SV), (k / SV) & 1);
+      for (int k = walk.round > 0 ? walk.round - 1 : 0; k <= walk.round; ++k) wait.drain(q_full + 8 * (k % NQ), (k / NQ) & 1);
+      for (uint32_t k = u > (uint32_t)SK ? u - SK : 0; k <= u; ++k) wait.drain(k_full + 8 * (k % SK), (k / SK) & 1);
+      for (uint32_t k = u > (uint32_t)SV ? u - SV : 0; k <= u; ++k) wait.drain(v_full + 8 * (k % SV), (k / SV) & 1);
     }
   } else if (warp == 9) {
     // ================================================================= MMAs
@@ -197,7 +197,7 @@ attn_dq_tc_kernel(const AttnArgs a, FastDiv heads, int items, const __grid_const
       ok = dprob() && score();
     }
     mma_commit(done);
-    drain_wait(done, 0);
+    wait.drain(done, 0);
   } else {
     // ================================================================= P, dS, and dQ's way out
     const int r = (warp & 3) * 32 + lane, h = warp >> 2;
@@ -308,7 +308,7 @@ attn_dkv_tc_kernel(const AttnArgs a, FastDiv heads, int items, const __grid_cons
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = uniform(tmem_slot), c_s = 0, c_dp = 128, c_dv = 256, c_dk = 384;
-  const AttnWait wait{&abort_flag, a.status};
+  const AttnWait wait{&abort_flag, a.status, a.spin_limit};
   const int group = a.hq / a.hk;
   // an item's blocks: for every query head of the group, the query tiles from the key tile's own to the sequence's end
   auto per_head_of = [](const AttnTile& t) { return (t.len + kAttnRows - 1) / kAttnRows - t.row / kAttnRows; };
@@ -323,17 +323,17 @@ attn_dkv_tc_kernel(const AttnArgs a, FastDiv heads, int items, const __grid_cons
       if (rows >= 128) {
         if (elect_one()) {
           mbar_expect_tx(bar, TILE);
-          load_tile<DP>(sk + number * TILE, map, head, token, bar);
+          if ((int)u != a.skip) load_tile<DP>(sk + number * TILE, map, head, token, bar);
         }
         return true;
       }
       if (elect_one()) {
         mbar_expect_tx(raw, TILE);
-        load_tile<DP>(sk + number * TILE, map, head, token, raw);
+        if ((int)u != a.skip) load_tile<DP>(sk + number * TILE, map, head, token, raw);
       }
       const bool here = wait(raw, n_raw & 1);
       ++n_raw;
-      if (!here) { drain_wait(raw, (n_raw - 1) & 1); return false; }
+      if (!here) { wait.drain(raw, (n_raw - 1) & 1); return false; }
       zero_rows<DP, 128>(base + number * TILE, rows, lane);
       if (elect_one()) mbar_arrive(bar);
       return true;
@@ -366,12 +366,12 @@ attn_dkv_tc_kernel(const AttnArgs a, FastDiv heads, int items, const __grid_cons
     }
     if (wait.given_up()) {
       for (int k = walk.round > 0 ? walk.round - 1 : 0; k <= walk.round; ++k) {
-        drain_wait(k_full, k & 1);
-        drain_wait(v_full, k & 1);
+        wait.drain(k_full, k & 1);
+        wait.drain(v_full, k & 1);
       }
       for (uint32_t k = u > (uint32_t)SQ ? u - SQ : 0; k <= u; ++k) {
-        drain_wait(q_full + 8 * (k % SQ), (k / SQ) & 1);
-        drain_wait(do_full + 8 * (k % SQ), (k / SQ) & 1);
+        wait.drain(q_full + 8 * (k % SQ), (k / SQ) & 1);
+        wait.drain(do_full + 8 * (k % SQ), (k / SQ) & 1);
       }
     }
   } else if (warp == 10) {
@@ -447,7 +447,7 @@ attn_dkv_tc_kernel(const AttnArgs a, FastDiv heads, int items, const __grid_cons
       ok = dprob();
     }
     mma_commit(done);
-    drain_wait(done, 0);
+    wait.drain(done, 0);
   } else {
     // ================================================================= P^T, dS^T, and the gradients' way out
     const int r = (warp & 3) * 32 + lane, h = warp >> 2;

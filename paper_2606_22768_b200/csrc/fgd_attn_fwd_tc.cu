@@ -81,7 +81,7 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, FastDiv per_tile, int i
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = (uint32_t)uniform((int)tmem_slot);
-  const AttnWait wait{&abort_flag, a.status};
+  const AttnWait wait{&abort_flag, a.status, a.spin_limit};
   // tensor memory columns
   auto s_col = [](int t) { return (uint32_t)(128 * t); };
   auto o_col = [](int t) { return (uint32_t)(256 + 128 * t); };
@@ -111,16 +111,16 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, FastDiv per_tile, int i
           if (v == 0 || rows >= 128) {
             if (elect_one()) {
               mbar_expect_tx(bar, TILE);
-              load_tile<DP>(dst, v ? &mv : &mk, it.kvh, token, bar);
+              if ((int)u != a.skip) load_tile<DP>(dst, v ? &mv : &mk, it.kvh, token, bar);
             }
           } else {     // the sequence ends inside this tile
             if (elect_one()) {
               mbar_expect_tx(raw, TILE);
-              load_tile<DP>(dst, &mv, it.kvh, token, raw);
+              if ((int)u != a.skip) load_tile<DP>(dst, &mv, it.kvh, token, raw);
             }
             ok = wait(raw, n_raw & 1);
             ++n_raw;
-            if (!ok) { drain_wait(raw, (n_raw - 1) & 1); break; }
+            if (!ok) { wait.drain(raw, (n_raw - 1) & 1); break; }
             zero_rows<DP, 128>(base + 2 * TILE + s * TILE, rows, lane);
             if (elect_one()) mbar_arrive(bar);
           }
@@ -129,9 +129,9 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, FastDiv per_tile, int i
     }
     // a CTA that gave up still waits for its own copies
     if (wait.given_up()) {
-      drain_wait(q_full, walk.round & 1);
-      if (walk.round > 0) drain_wait(q_full, (walk.round - 1) & 1);
-      for (uint32_t k = u > (uint32_t)ST ? u - ST : 0; k < u; ++k) drain_wait(full + 8 * (k % ST), (k / ST) & 1);
+      wait.drain(q_full, walk.round & 1);
+      if (walk.round > 0) wait.drain(q_full, (walk.round - 1) & 1);
+      for (uint32_t k = u > (uint32_t)ST ? u - ST : 0; k < u; ++k) wait.drain(full + 8 * (k % ST), (k / ST) & 1);
     }
   } else if (warp == 9) {
     // ================================================================= MMAs
@@ -191,7 +191,7 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, FastDiv per_tile, int i
     }
     // tensor memory is not released under a running MMA
     mma_commit(done);
-    drain_wait(done, 0);
+    wait.drain(done, 0);
   } else {
     // ================================================================= softmax
     const int t = warp >> 2, r = (warp & 3) * 32 + lane;

@@ -17,20 +17,20 @@
 namespace fgd {
 
 constexpr uint32_t kAttnBox = 128 * 128;           // bytes of a 128 x 64 box of 16-bit values
-constexpr uint32_t kAttnSpin = 1u << 22;           // polls before a wait gives up
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 template <int DP>
 __host__ __device__ constexpr uint32_t attn_tile_bytes() { return kAttnBox * (DP / 64); }
 
-// A wait that ends: after kAttnSpin polls, or once another thread of the CTA has given up.  Called by whole warps; all
+// A wait that ends: after `limit` polls, or once another thread of the CTA has given up.  Called by whole warps; all
 // lanes get the same answer, so that a warp that gives up leaves together (tensor-memory access is warp-wide).
 struct AttnWait {
   int* abort_flag;   // shared memory
   int* status;       // the plan's status word
+  uint32_t limit;
   __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const {
     bool here = false;
-    for (uint32_t it = 0; it < kAttnSpin && !here; ++it) {
+    for (uint32_t it = 0; it < limit && !here; ++it) {
       uint32_t ok;
       asm volatile(
           "{\n\t.reg .pred p;\n\t"
@@ -48,9 +48,9 @@ struct AttnWait {
     return false;
   }
   __device__ __forceinline__ bool given_up() const { return *(volatile int*)abort_flag != 0; }
+  // Only for a CTA's end: whatever the flag says, still bounded.
+  __device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) const { mbar_wait(bar, parity, limit); }
 };
-// Only for the end of a CTA that gave up: wait whatever the flag says, still bounded.
-__device__ __forceinline__ void drain_wait(uint32_t bar, uint32_t parity) { mbar_wait(bar, parity, kAttnSpin); }
 
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int c, int head, int token, uint32_t bar) {
   asm volatile(

@@ -287,6 +287,55 @@ def test_attention_stream_and_graph():
     assert all(torch.equal(a, b) for a, b in zip(want, (o, lse, dq, dk, dv)))
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_wait_runs_out_and_plan_recovers(d):
+    """A load that never comes: the kernels record a timeout, give everything back and return; the plan then works as a new one does."""
+    import paper_2606_22768_b200 as fgd
+    torch = _torch()
+    cu, T, hq, hk = [0, 700, 900], 900, 4, 2
+    q, k, v, do = (_randn((T, h, d), "bf16", i) for i, h in enumerate((hq, hk, hk, hq)))
+
+    def run(plan):
+        o, lse = torch.zeros_like(q), torch.zeros((hq, T), device="cuda")
+        delta, dq, dk, dv = torch.zeros_like(lse), torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v)
+        fgd.fgd_attn_forward(plan, q, k, v, o, lse)
+        torch.cuda.synchronize()
+        return o, lse, (delta, dq, dk, dv)
+
+    def back(plan, o, lse, outs):
+        fgd.fgd_attn_backward(plan, q, k, v, o, do, lse, *outs)
+        torch.cuda.synchronize()
+
+    def timed_out(plan):
+        with pytest.raises(fgd.FgdError) as e:
+            fgd.fgd_attn_status(plan)
+        assert e.value.status == fgd.FGD_ERR_TIMEOUT
+        fgd.fgd_attn_status(plan)                                         # reported once
+
+    fresh = fgd.AttnPlan(cu)
+    want = run(fresh)
+    back(fresh, want[0], want[1], want[2])
+    fgd.fgd_attn_status(fresh)
+    for skip in (1, 2):                                                   # a middle tile; in the forward pass a K and a V tile
+        plan = fgd.AttnPlan(cu)
+        fgd.fgd_attn_debug_set(plan, fgd.FGD_DEBUG_SPIN_LIMIT, 4096)
+        fgd.fgd_attn_debug_set(plan, fgd.FGD_DEBUG_SKIP_TILE, skip)
+        run(plan)
+        timed_out(plan)
+        back(plan, want[0], want[1], tuple(torch.zeros_like(t) for t in want[2]))
+        timed_out(plan)
+        fgd.fgd_attn_debug_set(plan, fgd.FGD_DEBUG_SPIN_LIMIT, 0)
+        fgd.fgd_attn_debug_set(plan, fgd.FGD_DEBUG_SKIP_TILE, -1)
+        got = run(plan)
+        back(plan, got[0], got[1], got[2])
+        fgd.fgd_attn_status(plan)
+        for a, b in zip(want[:2] + want[2], got[:2] + got[2]):
+            assert torch.equal(a, b)
+    for key, value in ((fgd.FGD_DEBUG_SKIP_TILE, -2), (fgd.FGD_DEBUG_SPIN_LIMIT, -1), (99, 0)):
+        with pytest.raises(fgd.FgdError):
+            fgd.fgd_attn_debug_set(fresh, key, value)
+
+
 def test_attention_refusals():
     import paper_2606_22768_b200 as fgd
     torch = _torch()
