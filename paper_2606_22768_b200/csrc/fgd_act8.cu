@@ -17,9 +17,10 @@
 //
 // Vector kernels (rows and bases on 16-byte boundaries, width a multiple of 16 or 8): a thread takes 16 or 8
 // consecutive values, two or four neighbouring lanes make a group, so the group's largest magnitude is one or two
-// shuffles away.  Element kernels (any width and stride): a warp takes four groups, a lane one value of each.
+// shuffles away.  Any other width, base or stride: 16 values to a lane as well, moved with shifts (fgd_shift.cuh).
 #include "fgd_dtype.cuh"
 #include "fgd_nvtx.h"
+#include "fgd_shift.cuh"
 
 using namespace fgd;
 
@@ -37,10 +38,6 @@ __device__ __forceinline__ uint32_t step_exponent(uint32_t amax_bits) {
 }
 __device__ __forceinline__ float step_of(uint32_t e) { return e >= 255u ? __uint_as_float(0x7FC00000u) : __uint_as_float(e << 23); }
 __device__ __forceinline__ float inverse_step(uint32_t e) { return e >= 255u ? 0.f : __uint_as_float((254u - e) << 23); }
-__device__ __forceinline__ int to_q8(float x, float inv) {
-  return __float2int_rn(fminf(fmaxf(x * inv, -127.f), 127.f));
-}
-__device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
 
 // 1 / (1 + 2^(-g log2 e)) from the hardware's exponential and reciprocal; a denominator beyond fp32 gives 0.
 __device__ __forceinline__ float2 sigmoid2(float2 g) {
@@ -60,7 +57,6 @@ __device__ __forceinline__ uint32_t group_max(uint32_t m) {
   for (int k = 1; k < kGroup / V; k <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, k));
   return m;
 }
-__device__ __forceinline__ uint32_t warp_max(uint32_t m) { return __reduce_max_sync(0xffffffffu, m); }
 
 // V consecutive values starting at p, as fp32.
 template <typename T, int V>
@@ -301,123 +297,158 @@ __global__ void __launch_bounds__(kBlock8) swiglu8_backward_kernel(const Swiglu8
   }
 }
 
-// ---- element kernels: a warp takes four neighbouring groups of a row at a time, a lane one value of each
-constexpr int kSpan = 4;
-__device__ __forceinline__ int spans_of(int64_t width) { return (int)((width + kSpan * kGroup - 1) / (kSpan * kGroup)); }
+// ---- kernels for every other width, base and stride: a unit is 16 values, moved by fgd_shift.cuh
+constexpr int kAny = 16;
+template <typename T>
+constexpr int kAnyWords = kAny * (int)sizeof(T) / 4;
+
+// Unit (row, unit) of a lane in the padded walk, and who its neighbours in the warp are.
+struct AnyUnit {
+  int c, left, valid;            // first column; columns from there to the row's end, clipped to [-16, 16]
+  bool mine, has_prev, has_next;
+  __device__ __forceinline__ AnyUnit(const Walk& w, bool in_range, int64_t width) {
+    const int lane = threadIdx.x & 31;
+    c = w.unit * kAny;
+    const int64_t l = width - c;
+    left = (int)(l > kAny ? kAny : l < -kAny ? -kAny : l);
+    mine = in_range && left > 0;
+    valid = mine ? left : -64;   // (of a lane without a unit nothing is stored)
+    has_prev = lane > 0 && w.unit > 0;
+    has_next = mine && lane < 31 && l > kAny;
+  }
+};
+template <typename T>
+__device__ __forceinline__ Vals<kAny> any_vals(const uint32_t (&w)[kAnyWords<T>], int left) {
+  Vals<kAny> f;
+#pragma unroll
+  for (int i = 0; i < kAnyWords<T>; ++i) {
+    if constexpr (sizeof(T) == 4) f.v[i] = __uint_as_float(w[i]);
+    else f.set(i, halves<T>(w[i]));
+  }
+  if (left < kAny) {             // beyond the row: the next row's values, or none
+#pragma unroll
+    for (int i = 0; i < kAny; ++i) f.v[i] = i < left ? f.v[i] : 0.f;
+  }
+  return f;
+}
+template <typename T>
+__device__ __forceinline__ Vals<kAny> any_load(const T* p, const AnyUnit& u, const T* lo, const T* hi) {
+  uint32_t w[kAnyWords<T>];
+  load_unit<sizeof(T), kAnyWords<T>>(reinterpret_cast<const char*>(p), u.mine, u.has_next, reinterpret_cast<const char*>(lo), reinterpret_cast<const char*>(hi), w);
+  return any_vals<T>(w, u.left);
+}
+__device__ __forceinline__ uint4 any_load8(const int8_t* p, const AnyUnit& u, const int8_t* lo, const int8_t* hi) {
+  uint32_t w[4];
+  load_unit<1, 4>(reinterpret_cast<const char*>(p), u.mine, u.has_next, reinterpret_cast<const char*>(lo), reinterpret_cast<const char*>(hi), w);
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <typename T>
+__device__ __forceinline__ void any_store(T* p, const AnyUnit& u, const Vals<kAny>& f) {
+  uint32_t w[kAnyWords<T>];
+#pragma unroll
+  for (int i = 0; i < kAnyWords<T>; ++i) {
+    if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(f.v[i]);
+    else w[i] = from_pair<T>(f.v[2 * i], f.v[2 * i + 1]);
+  }
+  store_unit<sizeof(T), kAnyWords<T>>(reinterpret_cast<char*>(p), u.valid * (int)sizeof(T), u.has_prev, u.has_next, w);
+}
+__device__ __forceinline__ void any_store8(int8_t* p, const AnyUnit& u, uint4 q) {
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+  store_unit<1, 4>(reinterpret_cast<char*>(p), u.valid, u.has_prev, u.has_next, w);
+}
 
 template <typename T>
-__global__ void __launch_bounds__(kBlock8) act8_save_elem_kernel(const Act8Args a) {
-  const int groups = (int)((a.width + kGroup - 1) / kGroup), spans = spans_of(a.width), lane = threadIdx.x & 31;
-  const int64_t stride = (int64_t)gridDim.x * (kBlock8 / 32), total = a.rows * spans;
-  int64_t i = (int64_t)blockIdx.x * (kBlock8 / 32) + (threadIdx.x >> 5);
-  Walk w(i, stride, spans);
-  for (; i < total; i += stride, w.next()) {
-    const int g0 = w.unit * kSpan;
-    const T* x = static_cast<const T*>(a.x) + w.row * a.ld_x;
-    float f[kSpan];
+__global__ void __launch_bounds__(kBlock8) act8_save_any_kernel(const Act8Args a) {
+  const int units = (int)((a.width + kGroup - 1) / kGroup) * 2;
+  const int64_t total = a.rows * units, padded = (total + 31) / 32 * 32, stride = (int64_t)gridDim.x * kBlock8;
+  int64_t i = (int64_t)blockIdx.x * kBlock8 + threadIdx.x;
+  Walk w(i, stride, units);
+  const T* x = static_cast<const T*>(a.x);
+  const T* end = x + (a.rows - 1) * a.ld_x + a.width;
+  for (; i < padded; i += stride, w.next()) {
+    const AnyUnit u(w, i < total, a.width);
+    const Vals<kAny> f = any_load<T>(x + w.row * a.ld_x + u.c, u, x, end);
+    const uint32_t m = group_max<kAny>(u.mine ? amax_of<kAny>(f) : 0u), e = step_exponent(m);
+    const uint4 q = __any_sync(0xffffffffu, tops_out(m)) ? quantise<kAny>(f, inverse_step(e), true) : quantise<kAny>(f, inverse_step(e), false);
+    any_store8(a.q + w.row * a.ld_q + u.c, u, q);
+    if (i < total && w.unit % 2 == 0) a.e[w.row * a.ld_e + w.unit / 2] = (uint8_t)e;
+  }
+}
+template <typename T>
+__global__ void __launch_bounds__(kBlock8) act8_load_any_kernel(const Act8Args a) {
+  const int units = (int)((a.width + kAny - 1) / kAny);
+  const int64_t total = a.rows * units, padded = (total + 31) / 32 * 32, stride = (int64_t)gridDim.x * kBlock8;
+  int64_t i = (int64_t)blockIdx.x * kBlock8 + threadIdx.x;
+  Walk w(i, stride, units);
+  const int8_t* end = a.q + (a.rows - 1) * a.ld_q + a.width;
+  for (; i < padded; i += stride, w.next()) {
+    const AnyUnit u(w, i < total, a.width);
+    const float step = u.mine ? step_of(a.e[w.row * a.ld_e + w.unit / 2]) : 0.f;
+    const uint4 q = any_load8(a.q + w.row * a.ld_q + u.c, u, a.q, end);
+    any_store<T>(static_cast<T*>(a.out) + w.row * a.ld_out + u.c, u, dequantise<kAny>(q, step));
+  }
+}
+template <typename T>
+__global__ void __launch_bounds__(kBlock8) swiglu8_forward_any_kernel(const Act8Args a) {
+  const int groups = (int)((a.width + kGroup - 1) / kGroup), units = groups * 2;
+  const int64_t total = a.rows * units, padded = (total + 31) / 32 * 32, stride = (int64_t)gridDim.x * kBlock8;
+  int64_t i = (int64_t)blockIdx.x * kBlock8 + threadIdx.x;
+  Walk w(i, stride, units);
+  const T* x = static_cast<const T*>(a.x);
+  const T* end = x + (a.rows - 1) * a.ld_x + 2 * a.width;
+  for (; i < padded; i += stride, w.next()) {
+    const AnyUnit n(w, i < total, a.width);
+    const T* row = x + w.row * a.ld_x + n.c;
+    const Vals<kAny> g = any_load<T>(row, n, x, end), u = any_load<T>(row + a.width, n, x, end);
+    const uint32_t mg = group_max<kAny>(n.mine ? amax_of<kAny>(g) : 0u), mu = group_max<kAny>(n.mine ? amax_of<kAny>(u) : 0u), eg = step_exponent(mg),
+                   eu = step_exponent(mu);
+    const bool clamp = __any_sync(0xffffffffu, tops_out(mg) || tops_out(mu));
+    int8_t* q = a.q + w.row * a.ld_q + n.c;
+    any_store8(q, n, clamp ? quantise<kAny>(g, inverse_step(eg), true) : quantise<kAny>(g, inverse_step(eg), false));
+    any_store8(q + a.width, n, clamp ? quantise<kAny>(u, inverse_step(eu), true) : quantise<kAny>(u, inverse_step(eu), false));
+    Vals<kAny> h;
 #pragma unroll
-    for (int k = 0; k < kSpan; ++k) {
-      const int64_t c = (int64_t)(g0 + k) * kGroup + lane;
-      f[k] = c < a.width ? to_f32<T>(x[c]) : 0.f;
-    }
-#pragma unroll
-    for (int k = 0; k < kSpan; ++k) {
-      const int64_t c = (int64_t)(g0 + k) * kGroup + lane;
-      const uint32_t e = step_exponent(warp_max(abs_bits(f[k])));
-      if (c < a.width) a.q[w.row * a.ld_q + c] = (int8_t)to_q8(f[k], inverse_step(e));
-      if (lane == 0 && g0 + k < groups) a.e[w.row * a.ld_e + g0 + k] = (uint8_t)e;
+    for (int j = 0; j < kAny / 2; ++j) h.set(j, mul2(mul2(g.pair(j), sigmoid2(g.pair(j))), u.pair(j)));
+    any_store<T>(static_cast<T*>(a.out) + w.row * a.ld_out + n.c, n, h);
+    if (i < total && w.unit % 2 == 0) {
+      uint8_t* e = a.e + w.row * a.ld_e + w.unit / 2;
+      e[0] = (uint8_t)eg;
+      e[groups] = (uint8_t)eu;
     }
   }
 }
 template <typename T>
-__global__ void __launch_bounds__(kBlock8) act8_load_elem_kernel(const Act8Args a) {
-  const int spans = spans_of(a.width), lane = threadIdx.x & 31;
-  const int64_t stride = (int64_t)gridDim.x * (kBlock8 / 32), total = a.rows * spans;
-  int64_t i = (int64_t)blockIdx.x * (kBlock8 / 32) + (threadIdx.x >> 5);
-  Walk w(i, stride, spans);
-  for (; i < total; i += stride, w.next()) {
-    float q[kSpan], s[kSpan];
+__global__ void __launch_bounds__(kBlock8) swiglu8_backward_any_kernel(const Swiglu8BackArgs a) {
+  const int groups = (int)((a.width + kGroup - 1) / kGroup), units = (int)((a.width + kAny - 1) / kAny);
+  const int64_t total = a.rows * units, padded = (total + 31) / 32 * 32, stride = (int64_t)gridDim.x * kBlock8;
+  int64_t i = (int64_t)blockIdx.x * kBlock8 + threadIdx.x;
+  Walk w(i, stride, units);
+  const T* dh = static_cast<const T*>(a.dh);
+  const T* end = dh + (a.rows - 1) * a.ld_dh + a.width;
+  const int8_t* end8 = a.q + (a.rows - 1) * a.ld_q + 2 * a.width;
+  for (; i < padded; i += stride, w.next()) {
+    const AnyUnit n(w, i < total, a.width);
+    const int8_t* q = a.q + w.row * a.ld_q + n.c;
+    const uint8_t* e = a.e + w.row * a.ld_e + w.unit / 2;
+    const float sg = n.mine ? step_of(e[0]) : 0.f, su = n.mine ? step_of(e[groups]) : 0.f;
+    const uint4 qg = any_load8(q, n, a.q, end8), qu = any_load8(q + a.width, n, a.q, end8);
+    const Vals<kAny> d = any_load<T>(dh + w.row * a.ld_dh + n.c, n, dh, end), g = dequantise<kAny>(qg, sg), u = dequantise<kAny>(qu, su);
+    Vals<kAny> dg, du, h;
 #pragma unroll
-    for (int k = 0; k < kSpan; ++k) {
-      const int64_t c = (int64_t)(w.unit * kSpan + k) * kGroup + lane;
-      const bool real = c < a.width;
-      q[k] = real ? (float)a.q[w.row * a.ld_q + c] : 0.f;
-      s[k] = real ? step_of(a.e[w.row * a.ld_e + w.unit * kSpan + k]) : 0.f;
+    for (int j = 0; j < kAny / 2; ++j) {
+      float2 x, y, z;
+      swiglu_back(d.pair(j), g.pair(j), u.pair(j), x, y, z);
+      dg.set(j, x); du.set(j, y); h.set(j, z);
     }
-#pragma unroll
-    for (int k = 0; k < kSpan; ++k) {
-      const int64_t c = (int64_t)(w.unit * kSpan + k) * kGroup + lane;
-      if (c < a.width) static_cast<T*>(a.out)[w.row * a.ld_out + c] = from_f32<T>(q[k] * s[k]);
-    }
-  }
-}
-template <typename T>
-__global__ void __launch_bounds__(kBlock8) swiglu8_forward_elem_kernel(const Act8Args a) {
-  const int groups = (int)((a.width + kGroup - 1) / kGroup), spans = spans_of(a.width), lane = threadIdx.x & 31;
-  const int64_t stride = (int64_t)gridDim.x * (kBlock8 / 32), total = a.rows * spans;
-  int64_t i = (int64_t)blockIdx.x * (kBlock8 / 32) + (threadIdx.x >> 5);
-  Walk w(i, stride, spans);
-  for (; i < total; i += stride, w.next()) {
-    const int g0 = w.unit * kSpan;
-    const T* row = static_cast<const T*>(a.x) + w.row * a.ld_x;
-    float2 f[kSpan];
-#pragma unroll
-    for (int k = 0; k < kSpan; ++k) {
-      const int64_t c = (int64_t)(g0 + k) * kGroup + lane;
-      f[k] = c < a.width ? make_float2(to_f32<T>(row[c]), to_f32<T>(row[a.width + c])) : both(0.f);
-    }
-#pragma unroll
-    for (int k = 0; k < kSpan; ++k) {
-      const int64_t c = (int64_t)(g0 + k) * kGroup + lane;
-      const uint32_t eg = step_exponent(warp_max(abs_bits(f[k].x))), eu = step_exponent(warp_max(abs_bits(f[k].y)));
-      if (c < a.width) {
-        int8_t* q = a.q + w.row * a.ld_q + c;
-        q[0] = (int8_t)to_q8(f[k].x, inverse_step(eg));
-        q[a.width] = (int8_t)to_q8(f[k].y, inverse_step(eu));
-        static_cast<T*>(a.out)[w.row * a.ld_out + c] = from_f32<T>(f[k].x * sigmoid2(both(f[k].x)).x * f[k].y);
-      }
-      if (lane == 0 && g0 + k < groups) {
-        uint8_t* e = a.e + w.row * a.ld_e + g0 + k;
-        e[0] = (uint8_t)eg;
-        e[groups] = (uint8_t)eu;
-      }
-    }
-  }
-}
-template <typename T>
-__global__ void __launch_bounds__(kBlock8) swiglu8_backward_elem_kernel(const Swiglu8BackArgs a) {
-  const int groups = (int)((a.width + kGroup - 1) / kGroup), spans = spans_of(a.width), lane = threadIdx.x & 31;
-  const int64_t stride = (int64_t)gridDim.x * (kBlock8 / 32), total = a.rows * spans;
-  int64_t i = (int64_t)blockIdx.x * (kBlock8 / 32) + (threadIdx.x >> 5);
-  Walk w(i, stride, spans);
-  for (; i < total; i += stride, w.next()) {
-    float d[kSpan], g[kSpan], u[kSpan];
-#pragma unroll
-    for (int k = 0; k < kSpan; ++k) {
-      const int64_t c = (int64_t)(w.unit * kSpan + k) * kGroup + lane;
-      d[k] = g[k] = u[k] = 0.f;
-      if (c < a.width) {
-        const int8_t* q = a.q + w.row * a.ld_q + c;
-        const uint8_t* e = a.e + w.row * a.ld_e + w.unit * kSpan + k;
-        d[k] = to_f32<T>(static_cast<const T*>(a.dh)[w.row * a.ld_dh + c]);
-        g[k] = (float)q[0] * step_of(e[0]);
-        u[k] = (float)q[a.width] * step_of(e[groups]);
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < kSpan; ++k) {
-      const int64_t c = (int64_t)(w.unit * kSpan + k) * kGroup + lane;
-      if (c >= a.width) continue;
-      float2 dg, du, h;
-      swiglu_back(both(d[k]), both(g[k]), both(u[k]), dg, du, h);
-      T* out = static_cast<T*>(a.dgu) + w.row * a.ld_dgu + c;
-      out[0] = from_f32<T>(dg.x);
-      out[a.width] = from_f32<T>(du.x);
-      if (a.h) static_cast<T*>(a.h)[w.row * a.ld_h + c] = from_f32<T>(h.x);
-    }
+    T* out = static_cast<T*>(a.dgu) + w.row * a.ld_dgu + n.c;
+    any_store<T>(out, n, dg);
+    any_store<T>(out + a.width, n, du);
+    if (a.h) any_store<T>(static_cast<T*>(a.h) + w.row * a.ld_h + n.c, n, h);
   }
 }
 
+// Is the pointer on a boundary of its elements?  (Rows then are too.)
+bool on_elements(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)bytes == 0; }
 bool on16(const void* p, int64_t ld, int bytes) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (ld * bytes) % 16 == 0; }
 // Values per thread that width, base and stride of the stored bytes allow: 16 (16-bit activations), 8, or none (0).
 int unit_for(int dtype, const void* q, int64_t ld, int64_t width) {
@@ -450,14 +481,14 @@ void by_dtype(int dtype, F f) {
   else if (dtype == FGD_BF16) f(__nv_bfloat16{});
   else f(__half{});
 }
-// KERNEL<type, 16 or 8 values per thread>, or KERNEL_elem<type> where `unit` is 0.
-#define FGD_LAUNCH_DTYPE(KERNEL, THREADS16, THREADS8, THREADS_ELEM)                                       \
+// KERNEL<type, 16 or 8 values per thread>, or KERNEL_any<type> where `unit` is 0.
+#define FGD_LAUNCH_DTYPE(KERNEL, THREADS16, THREADS8)                                                     \
   by_dtype(dtype, [&](auto zero) {                                                                         \
     using T = decltype(zero);                                                                              \
     if constexpr (sizeof(T) == 2)                                                                          \
       if (unit == 16) { KERNEL##_kernel<T, 16><<<grid_for(THREADS16), kBlock8, 0, st>>>(a); return; }      \
     if (unit == 8) KERNEL##_kernel<T, 8><<<grid_for(THREADS8), kBlock8, 0, st>>>(a);                       \
-    else KERNEL##_elem_kernel<T><<<grid_for(THREADS_ELEM), kBlock8, 0, st>>>(a);                           \
+    else KERNEL##_any_kernel<T><<<grid_for(rows * groups * 2), kBlock8, 0, st>>>(a);                       \
   });
 
 }  // namespace
@@ -471,6 +502,7 @@ extern "C" int fgd_act_save8(int device, int dtype, int64_t rows, int64_t width,
   if (!x || !q8 || !e8) return op_fail(FGD_ERR_INVALID_ARG, "fgd_act_save8: NULL pointer");
   if (ld_x < width || ld_q < width || ld_e < groups) return op_fail(FGD_ERR_INVALID_ARG, "fgd_act_save8: a row stride is below the row's width");
   const int b = dtype_bytes(dtype);
+  if (!on_elements(x, b)) return op_fail(FGD_ERR_INVALID_ARG, "fgd_act_save8: a pointer is not on a boundary of its elements");
   const Span sx = span_of(x, rows, width, ld_x, b), sq = span_of(q8, rows, width, ld_q, 1), se = span_of(e8, rows, groups, ld_e, 1);
   if (sx.overlaps(sq) || sx.overlaps(se) || sq.overlaps(se)) return op_fail(FGD_ERR_ALIAS, "fgd_act_save8: tensors overlap");
   DeviceScope dev(device);
@@ -478,7 +510,7 @@ extern "C" int fgd_act_save8(int device, int dtype, int64_t rows, int64_t width,
   const Act8Args a{x, ld_x, nullptr, 0, q8, ld_q, e8, ld_e, rows, width};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int unit = on16(x, ld_x, b) ? unit_for(dtype, q8, ld_q, width) : 0;
-  FGD_LAUNCH_DTYPE(act8_save, rows * groups * 2, rows * groups * 4, rows * ((groups + 3) / 4) * 32)
+  FGD_LAUNCH_DTYPE(act8_save, rows * groups * 2, rows * groups * 4)
   return launched("fgd_act_save8");
 }
 
@@ -491,6 +523,7 @@ extern "C" int fgd_act_load8(int device, int dtype, int64_t rows, int64_t width,
   if (!out || !q8 || !e8) return op_fail(FGD_ERR_INVALID_ARG, "fgd_act_load8: NULL pointer");
   if (ld_out < width || ld_q < width || ld_e < groups) return op_fail(FGD_ERR_INVALID_ARG, "fgd_act_load8: a row stride is below the row's width");
   const int b = dtype_bytes(dtype);
+  if (!on_elements(out, b)) return op_fail(FGD_ERR_INVALID_ARG, "fgd_act_load8: a pointer is not on a boundary of its elements");
   const Span so = span_of(out, rows, width, ld_out, b);
   if (so.overlaps(span_of(q8, rows, width, ld_q, 1)) || so.overlaps(span_of(e8, rows, groups, ld_e, 1))) return op_fail(FGD_ERR_ALIAS, "fgd_act_load8: tensors overlap");
   DeviceScope dev(device);
@@ -501,7 +534,7 @@ extern "C" int fgd_act_load8(int device, int dtype, int64_t rows, int64_t width,
   by_dtype(dtype, [&](auto zero) {
     using T = decltype(zero);
     if (unit) act8_load_kernel<T><<<grid_for(rows * (width * (int64_t)sizeof(T) / 16)), kBlock8, 0, st>>>(a);
-    else act8_load_elem_kernel<T><<<grid_for(rows * ((groups + 3) / 4) * 32), kBlock8, 0, st>>>(a);
+    else act8_load_any_kernel<T><<<grid_for(rows * groups * 2), kBlock8, 0, st>>>(a);
   });
   return launched("fgd_act_load8");
 }
@@ -516,6 +549,7 @@ extern "C" int fgd_swiglu8_forward(int device, int dtype, int64_t rows, int64_t 
   if (ld_gu < 2 * width || ld_h < width || ld_q < 2 * width || ld_e < 2 * groups)
     return op_fail(FGD_ERR_INVALID_ARG, "fgd_swiglu8_forward: a row stride is below the row's width");
   const int b = dtype_bytes(dtype);
+  if (!on_elements(gu, b) || !on_elements(h, b)) return op_fail(FGD_ERR_INVALID_ARG, "fgd_swiglu8_forward: a pointer is not on a boundary of its elements");
   const Span sx = span_of(gu, rows, 2 * width, ld_gu, b), sh = span_of(h, rows, width, ld_h, b), sq = span_of(q8, rows, 2 * width, ld_q, 1),
              se = span_of(e8, rows, 2 * groups, ld_e, 1);
   if (sx.overlaps(sh) || sx.overlaps(sq) || sx.overlaps(se) || sh.overlaps(sq) || sh.overlaps(se) || sq.overlaps(se))
@@ -525,7 +559,7 @@ extern "C" int fgd_swiglu8_forward(int device, int dtype, int64_t rows, int64_t 
   const Act8Args a{gu, ld_gu, h, ld_h, q8, ld_q, e8, ld_e, rows, width};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int unit = on16(gu, ld_gu, b) && on16(h, ld_h, b) ? unit_for(dtype, q8, ld_q, width) : 0;
-  FGD_LAUNCH_DTYPE(swiglu8_forward, rows * groups * 2, rows * groups * 4, rows * ((groups + 3) / 4) * 32)
+  FGD_LAUNCH_DTYPE(swiglu8_forward, rows * groups * 2, rows * groups * 4)
   return launched("fgd_swiglu8_forward");
 }
 
@@ -539,6 +573,7 @@ extern "C" int fgd_swiglu8_backward(int device, int dtype, int64_t rows, int64_t
   if (ld_dh < width || ld_dgu < 2 * width || (h && ld_h < width) || ld_q < 2 * width || ld_e < 2 * groups)
     return op_fail(FGD_ERR_INVALID_ARG, "fgd_swiglu8_backward: a row stride is below the row's width");
   const int b = dtype_bytes(dtype);
+  if (!on_elements(dh, b) || !on_elements(dgu, b) || !on_elements(h, b)) return op_fail(FGD_ERR_INVALID_ARG, "fgd_swiglu8_backward: a pointer is not on a boundary of its elements");
   const Span sd = span_of(dh, rows, width, ld_dh, b), so = span_of(dgu, rows, 2 * width, ld_dgu, b), sh = span_of(h, rows, width, ld_h, b),
              sq = span_of(q8, rows, 2 * width, ld_q, 1), se = span_of(e8, rows, 2 * groups, ld_e, 1);
   if (so.overlaps(sd) || so.overlaps(sh) || so.overlaps(sq) || so.overlaps(se) || sh.overlaps(sd) || sh.overlaps(sq) || sh.overlaps(se))
@@ -548,6 +583,6 @@ extern "C" int fgd_swiglu8_backward(int device, int dtype, int64_t rows, int64_t
   const Swiglu8BackArgs a{dh, ld_dh, q8, ld_q, e8, ld_e, dgu, ld_dgu, h, ld_h, rows, width};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int unit = on16(dh, ld_dh, b) && on16(dgu, ld_dgu, b) && (!h || on16(h, ld_h, b)) ? unit_for(dtype, q8, ld_q, width) : 0;
-  FGD_LAUNCH_DTYPE(swiglu8_backward, rows * (width / 16), rows * (width / 8), rows * ((groups + 3) / 4) * 32)
+  FGD_LAUNCH_DTYPE(swiglu8_backward, rows * (width / 16), rows * (width / 8))
   return launched("fgd_swiglu8_backward");
 }
