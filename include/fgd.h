@@ -346,7 +346,8 @@ typedef enum { FGD_GATE_NONE = 0, FGD_GATE_CHANNEL = 1, FGD_GATE_ELEMENT = 2 } f
  *   dx (of x, and of x_new's other readers' sum), dy, dgate, dw_post, dw_pre; dx may be dres itself.
  * Per-channel tensors (w_post, w_pre, a CHANNEL gate and their gradients) are fp32 [workers, width]; activations
  * and an ELEMENT gate are of `dtype`.  Outputs may not overlap anything else.  width <= 16384,
- * workers <= FGD_MAX_K.  Full speed: 16-byte aligned rows and width a multiple of 16 bytes; otherwise an element-wise kernel. */
+ * workers <= FGD_MAX_K, every pointer on a boundary of its elements.  Full speed: 16-byte aligned rows and width a multiple of 16
+ * bytes; other rows go at about half of it. */
 typedef struct {
   int32_t dtype, workers;
   int64_t rows; /* per worker */

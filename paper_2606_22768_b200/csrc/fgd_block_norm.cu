@@ -6,10 +6,10 @@ using namespace fgd;
 
 namespace {
 
-// A thread with at most 8 elements of a row keeps the per-channel factors in registers for all its rows; with more it reads them again
-// (from L1) in every row.  Arithmetic runs on pairs of fp32 values: with 16-bit activations a scalar version is bound by its
+// A thread with at most 8 elements of a row keeps the per-channel factors in registers for all its rows.  With more it keeps them in
+// shared memory (KEEP, behind the ring), or, where that is full, reads them again in every row.  Arithmetic runs on pairs of fp32 values: with 16-bit activations a scalar version is bound by its
 // instructions, not by HBM.
-template <typename T, int VEC, int NT, int VPT, int STAGES, bool FULL>
+template <typename T, int VEC, int NT, int VPT, int STAGES, bool FULL, bool ANY, bool KEEP>
 __global__ void __launch_bounds__(NT, NT * VPT <= 1024 ? 1024 / NT > 16 ? 16 : 1024 / NT : 1) norm_forward_kernel(const NormArgs a) {
   constexpr bool HOLD = VEC * VPT <= 8;
   constexpr int P = pairs_of<VEC>;
@@ -24,12 +24,15 @@ __global__ void __launch_bounds__(NT, NT * VPT <= 1024 ? 1024 / NT > 16 ? 16 : 1
 #pragma unroll
   for (int j = 0; j < VPT; ++j) c[j] = (threadIdx.x + j * NT) * VEC;
   Vals<VEC> wt[VPT], wn[VPT];
-  if constexpr (HOLD) {
-    post_factors<VEC, VPT>(a, worker, c, wt);
-    load_channel<VEC, VPT>(a.w_pre, worker, c, a.width, wn);
+  if constexpr (HOLD || KEEP) {
+    post_factors<VEC, VPT, ANY>(a, worker, c, wt);
+    load_channel<VEC, VPT, ANY>(a.w_pre, worker, c, a.width, wn);
   }
-  RowFeed<T, VEC, NT, VPT, N, STAGES> feed;
-  feed.start(in, a.width, ring, first, a.ctas, end);
+  Factors<VEC, VPT, NT, KEEP> ft, fn;
+  ft.start(ring + STAGES * N * RowFeed<T, VEC, NT, VPT, N, STAGES, ANY>::kStageBytes, 0, wt);
+  fn.start(ring + STAGES * N * RowFeed<T, VEC, NT, VPT, N, STAGES, ANY>::kStageBytes, 1, wn);
+  RowFeed<T, VEC, NT, VPT, N, STAGES, ANY> feed;
+  feed.start(in, a.width, ring, first, a.ctas, end, a.last_row);
   int slot = 0;
   for (int64_t row = first; row < end; row += a.ctas) {
     feed.next(in, row, a.ctas, end, row == first);
@@ -47,40 +50,41 @@ __global__ void __launch_bounds__(NT, NT * VPT <= 1024 ? 1024 / NT > 16 ? 16 : 1
       cta_sum<1, NT>(ss, buf, slot); slot ^= 1;
       ry = rsqrtf(fmaf(ss[0], a.inv_width, a.eps));
     }
-    if constexpr (!HOLD) post_factors<VEC, VPT>(a, worker, c, wt);
+    if constexpr (!HOLD && !KEEP) post_factors<VEC, VPT, ANY>(a, worker, c, wt);
     sum = both(0.f);
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
       v[j] = feed.get(X, j);
-      const Vals<VEC> y = feed.get(Y, j);
+      const Vals<VEC> y = feed.get(Y, j), ftj = ft.get(wt, j);
       Vals<VEC> g;
       if constexpr (FULL) g = feed.get(G, j);
 #pragma unroll
       for (int i = 0; i < P; ++i) {
         float2 u = mul2(get2(y, i), both(ry));
         if constexpr (FULL) u = mul2(u, get2(g, i));
-        const float2 x = fma2(u, get2(wt[j], i), get2(v[j], i));
+        const float2 x = fma2(u, get2(ftj, i), get2(v[j], i));
         put2(v[j], i, x);
         sum = fma2(x, x, sum);
       }
-      if (a.x_new.p && c[j] < a.width) store_vec<T, VEC>(a.x_new, row, c[j], v[j]);
+      if (a.x_new.p) store_vec<T, VEC, ANY>(a.x_new, row, c[j], a.width, v[j]);
     }
     if (a.n.p) {
       ss[0] = sum.x + sum.y;
       cta_sum<1, NT>(ss, buf, slot); slot ^= 1;
       const float2 rx = both(rsqrtf(fmaf(ss[0], a.inv_width, a.eps)));
-      if constexpr (!HOLD) load_channel<VEC, VPT>(a.w_pre, worker, c, a.width, wn);
+      if constexpr (!HOLD && !KEEP) load_channel<VEC, VPT, ANY>(a.w_pre, worker, c, a.width, wn);
 #pragma unroll
       for (int j = 0; j < VPT; ++j) {
+        const Vals<VEC> fnj = fn.get(wn, j);
 #pragma unroll
-        for (int i = 0; i < P; ++i) put2(v[j], i, mul2(mul2(get2(v[j], i), rx), get2(wn[j], i)));
-        if (c[j] < a.width) store_vec<T, VEC>(a.n, row, c[j], v[j]);
+        for (int i = 0; i < P; ++i) put2(v[j], i, mul2(mul2(get2(v[j], i), rx), get2(fnj, i)));
+        store_vec<T, VEC, ANY>(a.n, row, c[j], a.width, v[j]);
       }
     }
   }
 }
 
-template <typename T, int VEC, int NT, int VPT, int STAGES, bool FULL>
+template <typename T, int VEC, int NT, int VPT, int STAGES, bool FULL, bool ANY, bool KEEP>
 __global__ void __launch_bounds__(NT, NT <= 512 ? 512 / NT : 1) norm_backward_kernel(const NormArgs a) {
   constexpr bool HOLD = VEC * VPT <= 8;
   constexpr int P = pairs_of<VEC>;
@@ -99,19 +103,22 @@ __global__ void __launch_bounds__(NT, NT <= 512 ? 512 / NT : 1) norm_backward_ke
   for (int j = 0; j < VPT; ++j)
 #pragma unroll
     for (int i = 0; i < VEC; ++i) acc_pre[j].v[i] = acc_post[j].v[i] = 0.f;
-  if constexpr (HOLD) {
-    post_factors<VEC, VPT>(a, worker, c, wt);
-    load_channel<VEC, VPT>(a.w_pre, worker, c, a.width, wn);
+  if constexpr (HOLD || KEEP) {
+    post_factors<VEC, VPT, ANY>(a, worker, c, wt);
+    load_channel<VEC, VPT, ANY>(a.w_pre, worker, c, a.width, wn);
   }
-  RowFeed<T, VEC, NT, VPT, N, STAGES> feed;
-  feed.start(in, a.width, ring, first, a.ctas, end);
+  Factors<VEC, VPT, NT, KEEP> ft, fn;
+  ft.start(ring + STAGES * N * RowFeed<T, VEC, NT, VPT, N, STAGES, ANY>::kStageBytes, 0, wt);
+  fn.start(ring + STAGES * N * RowFeed<T, VEC, NT, VPT, N, STAGES, ANY>::kStageBytes, 1, wn);
+  RowFeed<T, VEC, NT, VPT, N, STAGES, ANY> feed;
+  feed.start(in, a.width, ring, first, a.ctas, end, a.last_row);
   let_next_start();      // the column sums' CTAs wait for this kernel's end on the SMs
   int slot = 0;
   for (int64_t row = first; row < end; row += a.ctas) {
     feed.next(in, row, a.ctas, end, row == first);
-    if constexpr (!HOLD) {
-      post_factors<VEC, VPT>(a, worker, c, wt);
-      load_channel<VEC, VPT>(a.w_pre, worker, c, a.width, wn);
+    if constexpr (!HOLD && !KEEP) {
+      post_factors<VEC, VPT, ANY>(a, worker, c, wt);
+      load_channel<VEC, VPT, ANY>(a.w_pre, worker, c, a.width, wn);
     }
     // the six sums; t0 = s g w_post y
     float2 s2[6];
@@ -119,13 +126,13 @@ __global__ void __launch_bounds__(NT, NT <= 512 ? 512 / NT : 1) norm_backward_ke
     for (int k = 0; k < 6; ++k) s2[k] = both(0.f);
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
-      const Vals<VEC> x = feed.get(X, j), y = feed.get(Y, j), n = feed.get(DN, j), d = feed.get(DR, j);
+      const Vals<VEC> x = feed.get(X, j), y = feed.get(Y, j), n = feed.get(DN, j), d = feed.get(DR, j), ftj = ft.get(wt, j), fnj = fn.get(wn, j);
       Vals<VEC> g;
       if constexpr (FULL) g = feed.get(G, j);
 #pragma unroll
       for (int i = 0; i < P; ++i) {
-        const float2 xv = get2(x, i), yv = get2(y, i), av = mul2(get2(n, i), get2(wn[j], i));
-        float2 t0 = mul2(get2(wt[j], i), yv);
+        const float2 xv = get2(x, i), yv = get2(y, i), av = mul2(get2(n, i), get2(fnj, i));
+        float2 t0 = mul2(get2(ftj, i), yv);
         if constexpr (FULL) t0 = mul2(t0, get2(g, i));
         s2[0] = fma2(xv, xv, s2[0]);
         s2[1] = fma2(yv, yv, s2[1]);
@@ -144,43 +151,37 @@ __global__ void __launch_bounds__(NT, NT <= 512 ? 512 / NT : 1) norm_backward_ke
     const float k = rx * rx * (rx * s[2] * a.inv_width);                       // dX = dres + rx a - k x'
     const float m = post ? ry * ry * a.inv_width * (s[3] + rx * s[4] - k * s[5]) : 0.f;   // dy = ry (b - m y)
     const float2 rx2 = both(rx), mk2 = both(-k), ry2 = both(ry), mr2 = both(-m * ry), sry2 = both(a.scale * ry);
-    if constexpr (!HOLD) {
-      post_factors<VEC, VPT>(a, worker, c, wt);
-      load_channel<VEC, VPT>(a.w_pre, worker, c, a.width, wn);
+    if constexpr (!HOLD && !KEEP) {
+      post_factors<VEC, VPT, ANY>(a, worker, c, wt);
+      load_channel<VEC, VPT, ANY>(a.w_pre, worker, c, a.width, wn);
     }
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
-      const Vals<VEC> x = feed.get(X, j), y = feed.get(Y, j), n = feed.get(DN, j), d = feed.get(DR, j);
-      Vals<VEC> wp[1], g, ox, oy, og;
-      if constexpr (FULL) {
-        const int cj[1] = {c[j]};
-        load_channel<VEC, 1>(a.w_post, worker, cj, a.width, wp);
-        g = feed.get(G, j);
-      }
+      const Vals<VEC> x = feed.get(X, j), y = feed.get(Y, j), n = feed.get(DN, j), d = feed.get(DR, j), ftj = ft.get(wt, j), fnj = fn.get(wn, j);
+      Vals<VEC> g, ox, oy, og;
+      if constexpr (FULL) g = feed.get(G, j);
 #pragma unroll
       for (int i = 0; i < P; ++i) {
         const float2 xv = get2(x, i), yv = get2(y, i), nv = get2(n, i), xr = mul2(xv, rx2);
         put2(acc_pre[j], i, fma2(nv, xr, get2(acc_pre[j], i)));
-        const float2 dX = fma2(mk2, xv, fma2(rx2, mul2(nv, get2(wn[j], i)), get2(d, i)));
+        const float2 dX = fma2(mk2, xv, fma2(rx2, mul2(nv, get2(fnj, i)), get2(d, i)));
         const float2 syh = mul2(yv, sry2), dg = FULL ? mul2(dX, get2(g, i)) : dX;          // syh = s yh
         put2(ox, i, dX);
-        put2(oy, i, fma2(mr2, yv, mul2(mul2(dg, get2(wt[j], i)), ry2)));
+        put2(oy, i, fma2(mr2, yv, mul2(mul2(dg, get2(ftj, i)), ry2)));
         put2(acc_post[j], i, fma2(dg, syh, get2(acc_post[j], i)));
-        if constexpr (FULL) put2(og, i, mul2(mul2(dX, syh), get2(wp[0], i)));
+        if constexpr (FULL) put2(og, i, mul2(mul2(dX, mul2(yv, ry2)), get2(ftj, i)));      // (ft is s w_post here)
       }
-      if (c[j] < a.width) {
-        store_vec<T, VEC>(a.dx, row, c[j], ox);
-        if (has_y) store_vec<T, VEC>(a.dy, row, c[j], oy);
-        if constexpr (FULL) store_vec<T, VEC>(a.dgate, row, c[j], og);
-      }
+      store_vec<T, VEC, ANY>(a.dx, row, c[j], a.width, ox);
+      if (has_y) store_vec<T, VEC, ANY>(a.dy, row, c[j], a.width, oy);
+      if constexpr (FULL) store_vec<T, VEC, ANY>(a.dgate, row, c[j], a.width, og);
     }
   }
   float* out = a.partial + (size_t)blockIdx.x * 2 * a.width;
 #pragma unroll
   for (int j = 0; j < VPT; ++j)
-    if (c[j] < a.width)
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) {
+    for (int i = 0; i < VEC; ++i)
+      if (c[j] + i < a.width) {
         out[c[j] + i] = acc_pre[j].v[i];
         out[a.width + c[j] + i] = acc_post[j].v[i];
       }
@@ -213,79 +214,77 @@ __global__ void __launch_bounds__(256) norm_columns_kernel(const NormArgs a) {
 
 // ---- host
 constexpr int kMaxWidth = 16384;
+constexpr size_t kMaxSmem = 226 * 1024;      // of a CTA, beside what the kernels hold statically
 struct Shape { int nt, vpt; };
 // Threads per row x vectors per thread: one vector while a row fits 512 threads of them.
 Shape shape_for(int width, int vec, bool backward) {
   const int vecs = (width + vec - 1) / vec;
-  if (vec > 1) {
-    if (vecs <= 32) return {32, 1};
-    if (vecs <= 64) return {64, 1};
-    if (vecs <= 128) return {128, 1};
-    if (vecs <= 256) return {256, 1};
-    if (vecs <= 512) return backward ? Shape{256, 2} : Shape{512, 1};
-    if (vecs <= 1024) return {512, 2};
-    if (vecs <= 2048) return {512, 4};
-    return {1024, 4};      // fp32 above 8192 columns
-  }
+  if (vecs <= 32) return {32, 1};
+  if (vecs <= 64) return {64, 1};
   if (vecs <= 128) return {128, 1};
-  if (vecs <= 1024) return {256, 4};
+  if (vecs <= 256) return {256, 1};
+  if (vecs <= 512) return backward ? Shape{256, 2} : Shape{512, 1};
+  if (vecs <= 1024) return {512, 2};
   if (vecs <= 2048) return {512, 4};
-  if (vecs <= 4096) return {1024, 4};
-  if (vecs <= 8192) return {1024, 8};
-  return {1024, 16};
+  return {1024, 4};      // fp32 above 8192 columns
 }
-// CTAs that share an SM (the kernels' launch bounds leave registers for them).
-int ctas_per_sm(int nt, bool backward) {
-  const int c = (backward ? 512 : 1024) / nt;
+// CTAs that share an SM: the kernels' launch bounds leave registers for them; `smem` is the dynamic part of what each of them takes.
+int ctas_per_sm(int nt, bool backward, size_t smem) {
+  const int regs = (backward ? 512 : 1024) / nt, room = (int)(228 * 1024 / (smem + 2 * 1024)), c = regs < room ? regs : room;
   return c < 1 ? 1 : c > 16 ? 16 : c;
 }
-int ctas_per_worker(int64_t workers, int64_t rows, int nt, bool backward) {
-  int64_t c = ((int64_t)sm_count() * ctas_per_sm(nt, backward) + workers - 1) / workers;
+int ctas_per_worker(int64_t workers, int64_t rows, int nt, bool backward, size_t smem) {
+  int64_t c = (int64_t)sm_count() * ctas_per_sm(nt, backward, smem) / workers;      // (rounded down: a CTA too many takes as long as all of them, 267 against 151 us for 8 x 1024 x 8192 bf16 backward)
   if (c > rows) c = rows;
   return (int)(c < 1 ? 1 : c);
 }
 
+// Launches with as many CTAs as fit the SMs beside each other (their number: a.ctas per worker).
 template <auto KERNEL>
-cudaError_t start(const NormArgs& a, unsigned grid, int threads, size_t smem, cudaStream_t st) {
+cudaError_t start(NormArgs& a, int64_t workers, bool backward, int threads, size_t smem, cudaStream_t st) {
+  a.ctas = ctas_per_worker(workers, a.rows, threads, backward, smem);
   cudaError_t e = smem > 32 * 1024 ? allow_smem<KERNEL>(smem) : cudaSuccess;
   if (e == cudaSuccess) {
-    KERNEL<<<grid, threads, smem, st>>>(a);
+    KERNEL<<<(unsigned)(workers * a.ctas), threads, smem, st>>>(a);
     e = cudaGetLastError();
   }
   return e;
 }
-template <typename T, int VEC, int NT, int VPT, int SF, int SB>
-cudaError_t launch_norm(const NormArgs& a, unsigned grid, bool backward, cudaStream_t st) {
-  constexpr size_t stage = (size_t)VPT * NT * 16;      // of one tensor
+template <typename T, int NT, int VPT, int SF, int SB, bool ANY>
+cudaError_t launch_norm(NormArgs& a, int64_t workers, bool backward, cudaStream_t st) {
+  constexpr int VEC = 16 / sizeof(T);
+  constexpr size_t stage = (size_t)VPT * (NT / 32) * (ANY ? 33 : 32) * 16;      // of one tensor
+  constexpr size_t factors = VEC * VPT > 8 ? (size_t)VPT * NT * VEC * 8 : 0;
+  // The backward pass reads the factors twice a row: in shared memory wherever they fit (2048 rows x 8 of 4096 bf16: 209 us from L1 and
+  // L2, 140 so).  Forward, once a row, they take a second CTA's place on the SM (8192 columns, 74 % of the copy peak without): only
+  // where weights off their 16-byte boundaries would be read one by one (8 x 1676 x 5003 bf16: 444 us without, 246 so).
+  constexpr bool kb4 = factors && SB * 4 * stage + factors <= kMaxSmem, kb5 = factors && SB * 5 * stage + factors <= kMaxSmem,
+                 kf2 = ANY && factors && SF * 2 * stage + factors <= kMaxSmem, kf3 = ANY && factors && SF * 3 * stage + factors <= kMaxSmem;
   if (a.gate_kind == GATE_FULL)
-    return backward ? start<norm_backward_kernel<T, VEC, NT, VPT, SB, true>>(a, grid, NT, SB * 5 * stage, st)
-                    : start<norm_forward_kernel<T, VEC, NT, VPT, SF, true>>(a, grid, NT, SF * 3 * stage, st);
-  return backward ? start<norm_backward_kernel<T, VEC, NT, VPT, SB, false>>(a, grid, NT, SB * 4 * stage, st)
-                  : start<norm_forward_kernel<T, VEC, NT, VPT, SF, false>>(a, grid, NT, SF * 2 * stage, st);
+    return backward ? start<norm_backward_kernel<T, VEC, NT, VPT, SB, true, ANY, kb5>>(a, workers, backward, NT, SB * 5 * stage + kb5 * factors, st)
+                    : start<norm_forward_kernel<T, VEC, NT, VPT, SF, true, ANY, kf3>>(a, workers, backward, NT, SF * 3 * stage + kf3 * factors, st);
+  return backward ? start<norm_backward_kernel<T, VEC, NT, VPT, SB, false, ANY, kb4>>(a, workers, backward, NT, SB * 4 * stage + kb4 * factors, st)
+                  : start<norm_forward_kernel<T, VEC, NT, VPT, SF, false, ANY, kf2>>(a, workers, backward, NT, SF * 2 * stage + kf2 * factors, st);
 }
-template <typename T>
-cudaError_t launch_norm_shape(const NormArgs& a, Shape s, bool vec, unsigned grid, bool backward, cudaStream_t st) {
-  constexpr int V = 16 / sizeof(T);
-  if (vec) {
-    // rows in flight: forward 3 x 8 to 24 KB, backward 2 x 16 to 20 KB per 256 threads; two vectors per thread leave room for one.
-    // (Forward, 512 x 2: fp32 is faster without a ring, 94 against 85 % of the copy peak at 4096 columns, 16-bit with one, 66 against 57 % at 8192.)
-    if (s.nt == 32) return launch_norm<T, V, 32, 1, 4, 3>(a, grid, backward, st);
-    if (s.nt == 64) return launch_norm<T, V, 64, 1, 4, 3>(a, grid, backward, st);
-    if (s.nt == 128) return launch_norm<T, V, 128, 1, 4, 3>(a, grid, backward, st);
-    if (s.nt == 256 && s.vpt == 1) return launch_norm<T, V, 256, 1, 4, 3>(a, grid, backward, st);
-    if (s.nt == 256) return launch_norm<T, V, 256, 2, 2, 2>(a, grid, backward, st);
-    if (s.vpt == 1) return launch_norm<T, V, 512, 1, 4, 3>(a, grid, backward, st);
-    if (s.vpt == 2) return launch_norm<T, V, 512, 2, sizeof(T) == 4 ? 0 : 2, 2>(a, grid, backward, st);
-    if (s.nt == 512) return launch_norm<T, V, 512, 4, 1, 1>(a, grid, backward, st);
-    if constexpr (sizeof(T) == 4) return launch_norm<T, V, 1024, 4, 0, 0>(a, grid, backward, st);
-    return cudaErrorInvalidValue;
-  }
-  if (s.nt == 128) return launch_norm<T, 1, 128, 1, 0, 0>(a, grid, backward, st);
-  if (s.nt == 256) return launch_norm<T, 1, 256, 4, 0, 0>(a, grid, backward, st);
-  if (s.nt == 512) return launch_norm<T, 1, 512, 4, 0, 0>(a, grid, backward, st);
-  if (s.vpt == 4) return launch_norm<T, 1, 1024, 4, 0, 0>(a, grid, backward, st);
-  if (s.vpt == 8) return launch_norm<T, 1, 1024, 8, 0, 0>(a, grid, backward, st);
-  return launch_norm<T, 1, 1024, 16, 0, 0>(a, grid, backward, st);
+template <typename T, bool ANY>
+cudaError_t launch_norm_shape(NormArgs& a, Shape s, int64_t workers, bool backward, cudaStream_t st) {
+  // rows in flight: forward 3 x 8 to 24 KB, backward 2 x 16 to 20 KB per 256 threads; two vectors per thread leave room for one.
+  // (Forward, 512 x 2: fp32 is faster without a ring, 94 against 85 % of the copy peak at 4096 columns, 16-bit with one, 66 against 57 % at 8192.)
+  if (s.nt == 32) return launch_norm<T, 32, 1, 4, 3, ANY>(a, workers, backward, st);
+  if (s.nt == 64) return launch_norm<T, 64, 1, 4, 3, ANY>(a, workers, backward, st);
+  if (s.nt == 128) return launch_norm<T, 128, 1, 4, 3, ANY>(a, workers, backward, st);
+  if (s.nt == 256 && s.vpt == 1) return launch_norm<T, 256, 1, 4, 3, ANY>(a, workers, backward, st);
+  if (s.nt == 256) return launch_norm<T, 256, 2, 2, 2, ANY>(a, workers, backward, st);
+  if (s.vpt == 1) return launch_norm<T, 512, 1, 4, 3, ANY>(a, workers, backward, st);
+  if (s.vpt == 2) return launch_norm<T, 512, 2, sizeof(T) == 4 ? (ANY ? 2 : 0) : (ANY ? 1 : 2), 2, ANY>(a, workers, backward, st);
+  if (s.nt == 512) return launch_norm<T, 512, 4, 1, 1, ANY>(a, workers, backward, st);
+  if constexpr (sizeof(T) == 4) return launch_norm<T, 1024, 4, 0, 0, ANY>(a, workers, backward, st);
+  return cudaErrorInvalidValue;
+}
+
+// The column sums of the most CTAs that a backward pass of this shape can start.
+int64_t workspace_bytes(int64_t workers, int64_t rows, int nt, int64_t width) {
+  return workers * ctas_per_worker(workers, rows, nt, true, 0) * 2 * width * (int64_t)sizeof(float);
 }
 
 struct Named { const char* name; const fgd_mat* m; bool wanted, present_needed, channel; };
@@ -330,6 +329,7 @@ int run_norm(const fgd_block_norm_args* b, bool backward, int device, void* stre
     }
     if (e.m->ld < b->width) return op_fail(FGD_ERR_INVALID_ARG, "%s: row stride of %s is below the width", who, e.name);
     const int64_t size = e.channel ? 4 : bytes;
+    if (reinterpret_cast<uintptr_t>(e.m->p) % size != 0) return op_fail(FGD_ERR_INVALID_ARG, "%s: %s is not on a boundary of its elements", who, e.name);
     if (reinterpret_cast<uintptr_t>(e.m->p) % 16 != 0 || (e.m->ld * size) % 16 != 0) aligned = false;
   }
   if (!backward && !pre && !y) return op_fail(FGD_ERR_INVALID_ARG, "%s: nothing to do (neither y nor n)", who);
@@ -352,30 +352,31 @@ int run_norm(const fgd_block_norm_args* b, bool backward, int device, void* stre
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool columns = backward && (pre || post || b->gate_kind == GATE_ROW);
   if (T == 0 && !columns) return FGD_OK;
-  const Shape s = shape_for((int)b->width, aligned ? vec : 1, backward);
+  const Shape s = shape_for((int)b->width, vec, backward);
   NormArgs a = {};
   auto mat = [](const fgd_mat& m, bool use) { return NormMat{use ? static_cast<char*>(m.p) : nullptr, m.ld}; };
   a.x = mat(b->x, !backward); a.y = mat(b->y, y); a.gate = mat(b->gate, gate); a.w_post = mat(b->w_post, post); a.w_pre = mat(b->w_pre, pre);
   a.x_new = mat(b->x_new, backward ? pre : (y || b->x_new.p != b->x.p)); a.n = mat(b->n, !backward && pre);
   a.dn = mat(b->dn, backward && pre); a.dres = mat(b->dres, backward); a.dx = mat(b->dx, backward); a.dy = mat(b->dy, backward && y);
   a.dgate = mat(b->dgate, backward && gate); a.dw_post = mat(b->dw_post, backward && post); a.dw_pre = mat(b->dw_pre, backward && pre);
-  a.rows = b->rows; a.width = (int)b->width; a.gate_kind = b->gate_kind;
-  a.ctas = ctas_per_worker(b->workers, b->rows, s.nt, backward);
+  a.rows = b->rows; a.last_row = T - 1; a.width = (int)b->width; a.gate_kind = b->gate_kind;
   a.eps = (float)b->eps; a.scale = (float)b->res_scale; a.inv_width = 1.f / (float)b->width;
-  const int64_t grid = (int64_t)b->workers * a.ctas;
-  if (grid > 0x7fffffff) return op_fail(FGD_ERR_INVALID_ARG, "%s: too many workers", who);
   if (backward) {
-    const int64_t need = grid * 2 * b->width * (int64_t)sizeof(float);
+    const int64_t need = workspace_bytes(b->workers, b->rows, s.nt, b->width);
     if (!b->workspace || b->workspace_bytes < need || reinterpret_cast<uintptr_t>(b->workspace) % 4 != 0)
       return op_fail(FGD_ERR_INVALID_ARG, "%s: needs a workspace of %lld bytes (fgd_block_norm_workspace)", who, (long long)need);
     a.partial = static_cast<float*>(b->workspace);
   }
   cudaError_t e;
-  switch (b->dtype) {
-    case FGD_F32: e = launch_norm_shape<float>(a, s, aligned, (unsigned)grid, backward, st); break;
-    case FGD_BF16: e = launch_norm_shape<__nv_bfloat16>(a, s, aligned, (unsigned)grid, backward, st); break;
-    default: e = launch_norm_shape<__half>(a, s, aligned, (unsigned)grid, backward, st); break;
-  }
+  auto launch = [&](auto any) {
+    constexpr bool ANY = decltype(any)::value;
+    switch (b->dtype) {
+      case FGD_F32: return launch_norm_shape<float, ANY>(a, s, b->workers, backward, st);
+      case FGD_BF16: return launch_norm_shape<__nv_bfloat16, ANY>(a, s, b->workers, backward, st);
+      default: return launch_norm_shape<__half, ANY>(a, s, b->workers, backward, st);
+    }
+  };
+  e = aligned ? launch(std::false_type{}) : launch(std::true_type{});
   if (e == cudaSuccess && columns) {
     e = launch_early(norm_columns_kernel, dim3((unsigned)((b->width + 31) / 32), (unsigned)b->workers), 256, 0, st, a);
   }
@@ -389,8 +390,7 @@ extern "C" int64_t fgd_block_norm_workspace(int device, int dtype, int workers, 
   const int bytes = dtype_bytes(dtype);
   if (bytes == 0 || workers < 1 || workers > FGD_MAX_K || rows < 0 || rows > 0x7fffffff || width < 1 || width > kMaxWidth) return FGD_ERR_INVALID_ARG;
   DeviceScope dev(device);
-  // the element-wise shapes have no fewer threads per row than the vector shapes, so no more CTAs
-  return (int64_t)workers * ctas_per_worker(workers, rows, shape_for((int)width, 16 / bytes, true).nt, true) * 2 * width * (int64_t)sizeof(float);
+  return workspace_bytes(workers, rows, shape_for((int)width, 16 / bytes, true).nt, width);
 }
 extern "C" int fgd_block_norm_forward(int device, const fgd_block_norm_args* args, void* stream) {
   FGD_NVTX_RANGE("fgd_block_norm_forward");

@@ -2,29 +2,37 @@
 //
 // Lane i of a warp owns a unit: 4 NW consecutive bytes, those after lane i - 1's where both lie in one row.  A unit starts s bytes
 // behind a 16-byte boundary.  Reading, a lane fetches the chunks from that boundary on, gets the one after its last from the next
-// lane, and takes its unit out of the two with selects and funnel shifts; writing, it takes the end of the unit before its own from the
+// lane, and takes its unit out of the two with funnel shifts; writing, it takes the end of the unit before its own from the
 // previous lane.  Only where a row, or the warp's part of it, begins or ends inside a chunk are fewer than 16 bytes written.
-// Against one element per lane and access (bf16, odd widths): 16 to 28 % of the copy peak became what the kernels' comments say.
+// What it gave against one element per lane and access, in % of the copy peak at odd widths, bf16: 8-bit save + load 16 to 40, SwiGLU
+// 28 to 42, block norm forward 14 to 42 (1001 columns) and 33 (5003), backward 9 to 34 and 23.  What is left is the shifting itself
+// and the cut chunks, not memory: 16-byte aligned rows reach 67 to 90.
 // Bytes around a row are read with it, but none outside [lo, hi), the tensor; only the unit's own are ever written.
 #ifndef FGD_SHIFT_CUH_
 #define FGD_SHIFT_CUH_
 
 #include <cstdint>
+#include <type_traits>
 
 namespace fgd {
 
-// r = the 4 N bytes of x from byte k on, 0 <= k <= 16.
+// r = the 4 N bytes of x from byte k on, 0 <= k <= 16.  The lanes of a row agree on k, so the word offset is a branch that all of them
+// take: N funnel shifts instead of 3 N selects before them.
 template <int N>
 __device__ __forceinline__ void shift_words(const uint32_t (&x)[N + 4], uint32_t k, uint32_t (&r)[N]) {
-  uint32_t y[N + 4];
+  const uint32_t bits = 8 * (k & 3);
+  auto from = [&](auto offset) {
+    constexpr int W = decltype(offset)::value;
 #pragma unroll
-  for (int i = 0; i < N + 4; ++i) y[i] = i < N && (k & 16) ? x[i + 4] : x[i];
-#pragma unroll
-  for (int i = 0; i < N + 2; ++i) y[i] = k & 8 ? y[i + 2] : y[i];
-#pragma unroll
-  for (int i = 0; i < N + 1; ++i) y[i] = k & 4 ? y[i + 1] : y[i];
-#pragma unroll
-  for (int i = 0; i < N; ++i) r[i] = __funnelshift_r(y[i], y[i + 1], 8 * (k & 3));
+    for (int i = 0; i < N; ++i) r[i] = __funnelshift_r(x[i + W], x[i + W + 1 < N + 4 ? i + W + 1 : N + 3], bits);
+  };
+  switch (k >> 2) {
+    case 0: from(std::integral_constant<int, 0>{}); break;
+    case 1: from(std::integral_constant<int, 1>{}); break;
+    case 2: from(std::integral_constant<int, 2>{}); break;
+    case 3: from(std::integral_constant<int, 3>{}); break;
+    default: from(std::integral_constant<int, 4>{}); break;      // k == 16
+  }
 }
 
 template <int ES>

@@ -646,6 +646,63 @@ def test_swiglu8_large_gates():
     assert bool(torch.isfinite(dgu).all())
 
 
+class _Anywhere:
+    """Copies of tensors at odd offsets and strides inside guarded buffers."""
+
+    def __init__(self, seed):
+        self.rng, self.kept = np.random.default_rng(seed), []
+
+    def __call__(self, t):
+        torch = _torch()
+        if t is None:
+            return None
+        R, W = t.shape
+        at, ld = int(self.rng.integers(1, 9)), W + int(self.rng.integers(0, 6))
+        buf = torch.full((at + R * ld + 9,), 77, dtype=t.dtype, device="cuda")
+        view = buf[at:at + R * ld].view(R, ld)[:, :W]
+        view.copy_(t)
+        free = torch.ones_like(buf, dtype=torch.bool)
+        free[at:at + R * ld].view(R, ld)[:, :W] = False
+        self.kept.append((buf, free))
+        return view
+
+    def check(self):
+        for buf, free in self.kept:
+            assert bool((buf[free] == 77).all()), "written outside a tensor"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("R,W", [(1, 8), (2, 16), (7, 24), (40, 8), (3, 264), (5, 520), (2, 1032), (3, 2056), (2, 4104), (9, 8192)])
+def test_rows_that_start_anywhere(R, W, dtype):
+    """The same bits as with aligned rows, and nothing beside the rows touched."""
+    import paper_2606_22768_b200 as fgd
+    torch = _torch()
+    K, G = 2, -(-W // 32)
+    for seed in range(3):
+        place = _Anywhere(100 * W + R + seed)
+        x, y, dn, dr, gate = (_randn((K * R, W), dtype, i, 2.0) for i in range(5))
+        wa, wb = 1.0 + 0.3 * _randn((K, W), "f32", 6), 1.0 + 0.3 * _randn((K, W), "f32", 7)
+        outs = []
+        for f in (lambda t: t, place):
+            a = [f(t) for t in (x, y, gate, wa, wb)]
+            e = [f(torch.zeros_like(x)) for _ in range(5)]
+            d = [f(torch.zeros_like(wa)) for _ in range(2)]
+            fgd.fgd_block_norm_forward(*a, e[0], e[1], 1e-5, 0.5)
+            fgd.fgd_block_norm_backward(f(dn), f(dr), e[0], *a[1:], e[2], e[3], e[4], *d, 1e-5, 0.5)
+            q, s = f(torch.zeros((K * R, W), dtype=torch.int8, device="cuda")), torch.zeros((K * R, G), dtype=torch.uint8, device="cuda")
+            back = f(torch.zeros_like(x))
+            fgd.fgd_act_save8(a[0], q, s)
+            fgd.fgd_act_load8(q, s, back)
+            gu, h, q2, s2 = f(torch.cat((x, y), 1)), f(torch.zeros_like(x)), f(torch.zeros((K * R, 2 * W), dtype=torch.int8, device="cuda")), torch.zeros((K * R, 2 * G), dtype=torch.uint8, device="cuda")
+            dgu, h2 = f(torch.zeros_like(gu)), f(torch.zeros_like(x))
+            fgd.fgd_swiglu8_forward(gu, h, q2, s2)
+            fgd.fgd_swiglu8_backward(f(dn), q2, s2, dgu, h2)
+            outs.append(e + d + [q, s, back, h, q2, s2, dgu, h2])
+        for i, (a, b) in enumerate(zip(*outs)):
+            assert torch.equal(a, b), f"output {i} differs"
+        place.check()
+
+
 def test_act8_refusals():
     import paper_2606_22768_b200 as fgd
     torch = _torch()
