@@ -270,7 +270,7 @@ __device__ __forceinline__ void swiglu_back(float2 dh, float2 g, float2 u, float
   dg = mul2(mul2(mul2(dh, u), s), add2(fma2(gs, both(-1.f), g), both(1.f)));
 }
 template <typename T, int V>
-__global__ void __launch_bounds__(kBlock8) swiglu8_backward_kernel(const Swiglu8BackArgs a) {
+__global__ void __launch_bounds__(kBlock8, 4) swiglu8_backward_kernel(const Swiglu8BackArgs a) {
   constexpr int L = kGroup / V;
   const int groups = (int)((a.width + kGroup - 1) / kGroup), units = (int)(a.width / V);
   const int64_t total = a.rows * units, stride = (int64_t)gridDim.x * kBlock8;
@@ -299,6 +299,7 @@ __global__ void __launch_bounds__(kBlock8) swiglu8_backward_kernel(const Swiglu8
 
 // ---- kernels for every other width, base and stride: a unit is 16 values, moved by fgd_shift.cuh
 constexpr int kAny = 16;
+constexpr int kAnyWaves = 4;      // (1 to 8 are within 3 %, 16 is 6 % slower)
 template <typename T>
 constexpr int kAnyWords = kAny * (int)sizeof(T) / 4;
 
@@ -463,10 +464,23 @@ int check_dims(const char* who, int dtype, int64_t rows, int64_t width) {
   return FGD_OK;
 }
 
-// Threads enough to cover the work, at most eight CTAs per SM of a grid that strides over the rest.
-unsigned grid_for(int64_t threads) {
-  const int64_t want = (threads + kBlock8 - 1) / kBlock8, most = (int64_t)sm_count() * 8;
-  return (unsigned)(want < most ? want : most);
+// Launches KERNEL with threads enough to cover the work, at most `waves` times as many CTAs as run at once: they stride over the rest.
+// What is best was measured, per kernel, over 1 to 64 waves: the kernels that write least or most against what they read want many short
+// CTAs, which the hardware hands out as others end (bf16, 32768 x 4096 save: 71 us with 1 wave, 65 with 8 and 16, 67 with 32; 16384 x 5632
+// SwiGLU backward 190, 154 with 8, 149 with 16, 153 with 32); the other two want one wave (load 69, 73 with 8, 82 with 32; SwiGLU
+// forward 131 and 135; but with fp32 16 waves, forward + backward of 5957 x 5632 182 with one, 170 so).
+template <auto KERNEL, typename A>
+void go(int waves, int64_t threads, cudaStream_t st, const A& a) {
+  static int cached[64] = {};
+  int dev = 0, fit = 0;
+  const bool known = cudaGetDevice(&dev) == cudaSuccess && dev < 64;
+  if (known) fit = cached[dev];
+  if (fit == 0) {
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&fit, KERNEL, kBlock8, 0) != cudaSuccess || fit < 1) fit = 1;
+    if (known) cached[dev] = fit;
+  }
+  const int64_t want = (threads + kBlock8 - 1) / kBlock8, most = (int64_t)sm_count() * fit * waves;
+  KERNEL<<<(unsigned)(want < most ? want : most), kBlock8, 0, st>>>(a);
 }
 
 int launched(const char* who) {
@@ -482,13 +496,13 @@ void by_dtype(int dtype, F f) {
   else f(__half{});
 }
 // KERNEL<type, 16 or 8 values per thread>, or KERNEL_any<type> where `unit` is 0.
-#define FGD_LAUNCH_DTYPE(KERNEL, THREADS16, THREADS8)                                                     \
+#define FGD_LAUNCH_DTYPE(KERNEL, WAVES, THREADS16, THREADS8)                                              \
   by_dtype(dtype, [&](auto zero) {                                                                         \
     using T = decltype(zero);                                                                              \
     if constexpr (sizeof(T) == 2)                                                                          \
-      if (unit == 16) { KERNEL##_kernel<T, 16><<<grid_for(THREADS16), kBlock8, 0, st>>>(a); return; }      \
-    if (unit == 8) KERNEL##_kernel<T, 8><<<grid_for(THREADS8), kBlock8, 0, st>>>(a);                       \
-    else KERNEL##_any_kernel<T><<<grid_for(rows * groups * 2), kBlock8, 0, st>>>(a);                       \
+      if (unit == 16) { go<KERNEL##_kernel<T, 16>>(WAVES, THREADS16, st, a); return; }                     \
+    if (unit == 8) go<KERNEL##_kernel<T, 8>>(WAVES, THREADS8, st, a);                                      \
+    else go<KERNEL##_any_kernel<T>>(kAnyWaves, rows * groups * 2, st, a);                                  \
   });
 
 }  // namespace
@@ -510,7 +524,7 @@ extern "C" int fgd_act_save8(int device, int dtype, int64_t rows, int64_t width,
   const Act8Args a{x, ld_x, nullptr, 0, q8, ld_q, e8, ld_e, rows, width};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int unit = on16(x, ld_x, b) ? unit_for(dtype, q8, ld_q, width) : 0;
-  FGD_LAUNCH_DTYPE(act8_save, rows * groups * 2, rows * groups * 4)
+  FGD_LAUNCH_DTYPE(act8_save, 8, rows * groups * 2, rows * groups * 4)
   return launched("fgd_act_save8");
 }
 
@@ -533,8 +547,8 @@ extern "C" int fgd_act_load8(int device, int dtype, int64_t rows, int64_t width,
   const int unit = on16(out, ld_out, b) ? unit_for(dtype, q8, ld_q, width) : 0;
   by_dtype(dtype, [&](auto zero) {
     using T = decltype(zero);
-    if (unit) act8_load_kernel<T><<<grid_for(rows * (width * (int64_t)sizeof(T) / 16)), kBlock8, 0, st>>>(a);
-    else act8_load_any_kernel<T><<<grid_for(rows * groups * 2), kBlock8, 0, st>>>(a);
+    if (unit) go<act8_load_kernel<T>>(1, rows * (width * (int64_t)sizeof(T) / 16), st, a);
+    else go<act8_load_any_kernel<T>>(kAnyWaves, rows * groups * 2, st, a);
   });
   return launched("fgd_act_load8");
 }
@@ -559,7 +573,7 @@ extern "C" int fgd_swiglu8_forward(int device, int dtype, int64_t rows, int64_t 
   const Act8Args a{gu, ld_gu, h, ld_h, q8, ld_q, e8, ld_e, rows, width};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int unit = on16(gu, ld_gu, b) && on16(h, ld_h, b) ? unit_for(dtype, q8, ld_q, width) : 0;
-  FGD_LAUNCH_DTYPE(swiglu8_forward, rows * groups * 2, rows * groups * 4)
+  FGD_LAUNCH_DTYPE(swiglu8_forward, sizeof(T) == 4 ? 16 : 1, rows * groups * 2, rows * groups * 4)
   return launched("fgd_swiglu8_forward");
 }
 
@@ -583,6 +597,6 @@ extern "C" int fgd_swiglu8_backward(int device, int dtype, int64_t rows, int64_t
   const Swiglu8BackArgs a{dh, ld_dh, q8, ld_q, e8, ld_e, dgu, ld_dgu, h, ld_h, rows, width};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int unit = on16(dh, ld_dh, b) && on16(dgu, ld_dgu, b) && (!h || on16(h, ld_h, b)) ? unit_for(dtype, q8, ld_q, width) : 0;
-  FGD_LAUNCH_DTYPE(swiglu8_backward, rows * (width / 16), rows * (width / 8))
+  FGD_LAUNCH_DTYPE(swiglu8_backward, 16, rows * (width / 16), rows * (width / 8))
   return launched("fgd_swiglu8_backward");
 }
