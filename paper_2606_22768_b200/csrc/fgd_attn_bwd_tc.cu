@@ -14,8 +14,14 @@
 //     runs; dP^T = V dO^T, dS^T over dP^T, dK += dS^T Q, and while P^T of the next block is formed the next dP^T runs.
 // `scale` multiplies dQ and dK once, at the end.
 //
-// Blocks of 64 rows taken by the two groups of four warps in turns hide more latency and were slower (8192 tokens, 16 heads of
-// 128: 355 + 570 us against 290 + 480): the issuing warp's own path, about 100 clocks a commit and 150 a wait, does not shrink with the block.
+// Rounding: P and dS are rounded to the 16-bit type as factors of the next product (5 products in fp32 would need tf32 operands at
+// half the rate and twice the shared memory): gradients are .0025 of their norm off in bf16, .0017 with the output's rounding alone.
+//
+// What bounds them: the chain product -> element-wise part -> product of a block, 61 and 64 % of the tensor pipe's cycles busy (key and
+// query kernel; the products alone are 2050 and 1540 of some 3500 and 2500 clocks a block).  8192 tokens, 16 heads of 128 over 4: dQ 318
+// us, dK + dV 435 us; 16 x 1024 tokens, 16 heads of 64: 91 and 122, where a block's exponentials (1024 clocks) take as long as the
+// products.  Blocks of 64 rows taken by the two groups of four warps in turns hide more latency and were slower, 355 + 570 us: the
+// issuing warp's own path, about 100 clocks a commit and 150 a wait, does not shrink with the block.
 #include "fgd_attn_tc.cuh"
 
 using namespace fgd;
@@ -29,7 +35,7 @@ constexpr int kStagesK = 3;
 template <int DP> constexpr int kStagesV = DP == 128 ? 1 : 2;
 template <int DP> constexpr size_t dq_smem() { return 1024 + (size_t)(2 * kBufQ<DP> + kStagesK + kStagesV<DP>) * attn_tile_bytes<DP>() + 8 * kStoreStage; }
 // key kernel: K, V, stages of Q and dO, and of the rows' lse and delta, which a warp of their own fetches (behind the tiles, on the
-// loading warp's path, their latency held up every block: sixteen sequences of 1024, 16 heads of 64, 190 us)
+// loading warp's path, their latency held up every block: sixteen sequences of 1024, 16 heads of 64, 190 us, 136 so)
 template <int DP> constexpr int kStagesQ = DP == 128 ? 2 : 4;
 constexpr int kStagesRow = 4;
 constexpr int kDkvThreads = 352;

@@ -9,7 +9,9 @@
 // rows through shared memory, one row per lane for the scores, one column per lane and 32-column step for the
 // products.  The softmax runs over the key tiles with a running maximum and sum; the gradient recomputes P from lse.
 // Only unmasked pairs enter a product, so what stands in masked places never reaches a result.
-// Bound by fp32 FMAs and shared-memory loads.
+// Bound by fp32 FMAs and the shared-memory loads that feed them, one load for two FMAs: 16384 tokens, 16 heads of 128 over 4, forward
+// 155 ms, where the tensor cores take 0.97.  delta has kernels of its own for 16-byte rows (8 elements a lane, several rows to a warp;
+// 14.6 us for 8192 tokens of 16 x 128, 4.6 TB/s).
 #include "fgd_attn.h"
 #include "fgd_dtype.cuh"
 

@@ -21,7 +21,7 @@
 // once, and a second kernel adds the CTAs up in a fixed order (no atomics: bit-identical from run to run).
 // Rows off their 16-byte boundaries go the same way in shifted chunks (fgd_shift.cuh).
 // Measured, % of the copy peak at work's own bytes (8 workers, gate per channel, bf16): forward 79 at 2048 columns, 88 at 4096, 74 at
-// 8192; backward 82, 88, 81; fp32 82 to 90 and 93, 94, 82.
+// 8192; backward 86, 88, 82; fp32 82 to 90 and 94, 94, 82.
 // The workers' rows never share a CTA's sums: each of the K workers has CTAs of its own.
 #ifndef FGD_BLOCK_NORM_CUH_
 #define FGD_BLOCK_NORM_CUH_
@@ -120,7 +120,9 @@ struct RowFeed {
   int width, stage;
   int64_t last;               // the tensors' last row
   uint32_t shift[ANY ? N : 1];
-  static constexpr bool HELD = STAGES == 0 || (ANY && VPT <= 2);      // the current row is in registers (ANY: shifted once, read twice)
+  // The current row in registers: shifted once, read twice (ANY), or read once from the ring (backward: 8 x 4096 x 2048 bf16 150 us
+  // from the ring twice, 143 so; with a gate per element, N = 5, 178 against 183, and forward 103 against 105: from the ring).
+  static constexpr bool HELD = STAGES == 0 || (ANY && VPT <= 2) || (N == 4 && VPT == 1);
   ActPack<T, VEC> cur[HELD ? N : 1][HELD ? VPT : 1];
 
   __device__ __forceinline__ int column(int j) const { return (int)(threadIdx.x + j * NT) * VEC; }
