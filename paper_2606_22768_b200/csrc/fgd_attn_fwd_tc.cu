@@ -25,7 +25,8 @@
 // measured matrix peak.  A tile's end (last P V, output, next item's first P) costs about 3800 clocks, which is what short sequences
 // pay: 9 sequences of 1 to 2011 tokens 67 us, 41 %.
 // Slower: two threads per row (maxima traded through shared memory; 1025 us at 16384 tokens), the next item's first S before the other
-// tile's last P V, outputs held back until after the next item's first P.
+// tile's last P V, outputs held back until after the
+// next item's first P; for widths to 64, four query tiles and blocks of 64 keys (16 x 1024, 16 heads of 64: 96 against 80 us).
 #include "fgd_attn_tc.cuh"
 
 using namespace fgd;
@@ -216,6 +217,7 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, FastDiv per_tile, int i
       const FwdItem it = fwd_item(a, pair_heads, walk.t, walk.h);
       const int n = it.n[t];
       if (n == 0) continue;
+      const bool real = it.row[t] + r < it.len;
       float m = 0.f;
       float2 l = make_float2(0.f, 0.f);
       for (int jb = n - 1; jb >= 0; --jb) {
@@ -245,7 +247,7 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, FastDiv per_tile, int i
         const float top = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * c;
         if (diagonal) {
           m = top == -INFINITY ? 0.f : top;
-        } else if (__any_sync(0xffffffffu, top > m + kRescale)) {
+        } else if (__any_sync(0xffffffffu, real && top > m + kRescale)) {      // (rows of another sequence have no say in it)
           const float mn = fmaxf(m, top), f = exp2_fast(m - mn);
           if (!(ok = wait(pv_done + 8 * t, (n_pv - 1) & 1))) break;
           tc_fence_after();

@@ -181,6 +181,25 @@ def test_attention_other_sequences_do_not_leak(d, dtype, bad):
         assert torch.equal(a[good.cuda()], b[good.cuda()]), f"{name} of a clean sequence changed"
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_neighbours_do_not_change_rounding(d):
+    """Large values in the next sequence, which shares a tile of rows, leave this one's results as they were, bit for bit."""
+    import paper_2606_22768_b200 as fgd
+    torch = _torch()
+    hq, hk = 4, 2
+    plan = fgd.AttnPlan([0, 650, 760])
+    q, k, v = (_randn((760, h, d), "bf16", i) for i, h in enumerate((hq, hk, hk)))
+    res = []
+    for factor in (1.0, 64.0):
+        q2 = q.clone()
+        q2[650:] *= factor
+        o, lse = torch.empty_like(q), torch.empty((hq, 760), device="cuda")
+        fgd.fgd_attn_forward(plan, q2, k, v, o, lse)
+        res.append((o[:650], lse[:, :650]))
+    for a, b in zip(*res):
+        assert torch.equal(a, b)
+
+
 def test_attention_later_keys_do_not_leak():
     """A NaN key or query of a later token never reaches an earlier token's output."""
     import paper_2606_22768_b200 as fgd
