@@ -370,8 +370,9 @@ int64_t fgd_block_norm_workspace(int device, int dtype, int workers, int64_t row
  * share a power-of-two step.  e8 = max(biased exponent of the group's largest magnitude - 6, 1),
  * q8 = round-to-even(x 2^(127 - e8)) held to [-127, 127], value = q8 2^(e8 - 127); e8 = 255 marks a
  * group with an infinity or a NaN, which reads back as NaN.  Error: half a step, at most 1/128 of the
- * group's largest magnitude (one step for an fp32 or fp16 value in the topmost 1/256 below a power of two).  bf16 values read back
- * are exact.
+ * group's largest magnitude (one step for an fp32 or fp16 value in the topmost 1/256 below a power of two).  Read back as
+ * bf16 the stored value q8 2^(e8 - 127) is not rounded again.  Any width and row stride; 16-byte aligned rows and widths that are
+ * multiples of 16 run at full speed, others at about half of it.  Every pointer stands on a boundary of its elements.
  *   x, out: device [rows, width] of `dtype`;  q8: int8 [rows, width];  e8: uint8 [rows, ceil(width / 32)]. */
 int fgd_act_save8(int device, int dtype, int64_t rows, int64_t width, const void* x, int64_t ld_x, int8_t* q8, int64_t ld_q,
                   uint8_t* e8, int64_t ld_e, void* stream);
