@@ -127,14 +127,15 @@ __device__ __forceinline__ Bytes<V> quantise(const Vals<V>& f, float inv, bool c
 }
 // Does a group with this largest magnitude reach 127.5 steps?  (mantissa at or above 127.5 / 128)
 __device__ __forceinline__ bool tops_out(uint32_t amax_bits) { return (amax_bits & 0x7FFFFFu) >= 0x7F0000u; }
-// And back: q + 128 in the low byte of 2^23 is 2^23 + 128 + q; one exact fused operation takes the offset off and applies the step.
+// And back: q + 128 in the low byte of 2^23 is 2^23 + 128 + q; the offset comes off before the step is applied, both exactly.  (One fused
+// operation with offset x step would do, but that product is beyond fp32 for steps from 2^105 on: groups above 2^111.)
 template <int V>
 __device__ __forceinline__ Vals<V> dequantise(const Bytes<V>& q, float step) {
   uint32_t w[V / 4];
   if constexpr (V == 16) { w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w; }
   else if constexpr (V == 8) { w[0] = q.x; w[1] = q.y; }
   else w[0] = q;
-  const float2 step2 = both(step), off = both(-8388736.f * step);
+  const float2 step2 = both(step), off = both(-8388736.f);
   Vals<V> f;
 #pragma unroll
   for (int j = 0; j < V / 4; ++j) {
@@ -142,7 +143,7 @@ __device__ __forceinline__ Vals<V> dequantise(const Bytes<V>& q, float step) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const float2 y = make_float2(__uint_as_float(__byte_perm(u, 0x4B000000u, 0x7440 + 2 * i)), __uint_as_float(__byte_perm(u, 0x4B000000u, 0x7440 + 2 * i + 1)));
-      f.set(2 * j + i, fma2(y, step2, off));
+      f.set(2 * j + i, mul2(add2(y, off), step2));
     }
   }
   return f;

@@ -1,0 +1,66 @@
+"""The inner step's operators at the ends of their types' ranges, with non-finite values, on other streams and through autograd: cases in
+which a result can be wrong although ordinary values are right.
+
+Tolerances as in the operators' own tests: u is the unit roundoff of the activations' type, fp32 arithmetic adds multiples of 2^-24.
+"""
+import numpy as np
+import pytest
+
+from oracle import inner as O
+
+from .test_gpu_inner_ops import F32, TINY, U, _dt, _matrix, _near, _np, _randn, _torch
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------- 8-bit checkpoints
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("W", [64, 72, 65])
+def test_act8_reads_back_every_magnitude(W, dtype):
+    """Groups whose largest magnitude is 2^-126 to 2^128: what is read back is q8 2^(e8 - 127), bit for bit, zeros and small members too."""
+    import paper_2606_22768_b200 as fgd
+    torch = _torch()
+    gen = torch.Generator().manual_seed(W)
+    powers = torch.arange(-126, 128, dtype=torch.float64)[:, None]
+    x = 2 * torch.rand((254, W), generator=gen, dtype=torch.float64) - 1
+    x[:, 5::7] *= 1e-3
+    x[:, 3::11] = 0
+    x[:, 1], x[:, 33], x[:, -1] = 1.0, -1.984375, 1.0            # (127 steps exactly, and beyond: held there)
+    x = (x * 2.0 ** powers).to(_dt(dtype)).cuda()
+    q, e = torch.empty((254, W), dtype=torch.int8, device="cuda"), torch.empty((254, -(-W // 32)), dtype=torch.uint8, device="cuda")
+    back = torch.empty_like(x)
+    fgd.fgd_act_save8(x, q, e)
+    fgd.fgd_act_load8(q, e, back)
+    rq, re = O.save8(_np(x))
+    assert re.min() == 1 and re.max() == 248
+    assert np.array_equal(q.cpu().numpy(), rq) and np.array_equal(e.cpu().numpy(), re)
+    assert np.array_equal(_np(back), O.load8(rq, re))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("F", [64, 72, 65])
+def test_swiglu8_backward_of_large_values(F, dtype):
+    """u from 2^-90 to 2^120 beside a moderate g."""
+    import paper_2606_22768_b200 as fgd
+    torch = _torch()
+    u = U[dtype]
+    powers = torch.arange(-90, 121, 3)[:, None]
+    R = len(powers)
+    gu = torch.cat((_randn((R, F), "f32", 1).cpu(), (_randn((R, F), "f32", 2).cpu().clamp(-4, 4) * 2.0 ** powers.double()).float()), 1).to(_dt(dtype)).cuda()
+    h, h2 = torch.empty((R, F), dtype=gu.dtype, device="cuda"), torch.empty((R, F), dtype=gu.dtype, device="cuda")
+    q, e = torch.empty((R, 2 * F), dtype=torch.int8, device="cuda"), torch.empty((R, 2 * -(-F // 32)), dtype=torch.uint8, device="cuda")
+    dh, dgu = _randn((R, F), dtype, 3), torch.empty_like(gu)
+    fgd.fgd_swiglu8_forward(gu, h, q, e)
+    fgd.fgd_swiglu8_backward(dh, q, e, dgu, h2)
+    x = _np(gu)
+    (qg, eg), (qu, eu) = O.save8(x[:, :F]), O.save8(x[:, F:])
+    assert np.array_equal(q.cpu().numpy(), np.hstack([qg, qu])) and np.array_equal(e.cpu().numpy(), np.hstack([eg, eu])) and eu.max() >= 240
+    g8, u8 = O.load8(qg, eg), O.load8(qu, eu)
+    fp8 = 2.0 ** -20 * (1 + np.abs(g8))
+    rg, ru = O.swiglu_grad(_np(dh), g8, u8)
+    _near(dgu[:, :F], rg, u * np.abs(rg) + fp8 * np.abs(_np(dh) * u8) / (1 + np.exp(-g8)) * (1 + np.abs(g8)), "dg")
+    _near(dgu[:, F:], ru, (u + fp8) * np.abs(ru), "du")
+    ref = O.swiglu(g8, u8)
+    _near(h2, ref, (u + fp8) * np.abs(ref), "h again")
+
+
