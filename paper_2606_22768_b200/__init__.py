@@ -476,6 +476,14 @@ def _stream_on(stream, device):
     return getattr(stream, "cuda_stream", stream)
 
 
+def _as_current(stream, handle, device):
+    """Context in which torch allocates and works on the stream of a call: the argument as it was given (None: the current one), its handle."""
+    import torch
+    if stream is not None and not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)
+    return torch.cuda.stream(stream)
+
+
 def _device_of(t, name: str):
     if not getattr(t, "is_cuda", False):
         raise TypeError(f"{name} must be a CUDA tensor")
@@ -644,17 +652,22 @@ def fgd_block_norm_backward(dn, dres, x_new, y, gate, w_post, w_pre, dx, dy, dga
             + _mat(w_pre, "w_pre", f32, K, H, dev) + _mat(x_new, "x_new", dt, T, H, dev) + _NO_MAT + _mat(dn, "dn", dt, T, H, dev)
             + _mat(dres, "dres", dt, T, H, dev) + _mat(dx, "dx", dt, T, H, dev) + _mat(dy, "dy", dt, T, H, dev) + _mat(dgate, "dgate", gate_type, gate_rows, H, dev)
             + _mat(dw_post, "dw_post", f32, K, H, dev) + _mat(dw_pre, "dw_pre", f32, K, H, dev))
+    code, handle = _dtype_of(first, "activations"), _stream_on(stream, dev)
     if T == 0:
-        with torch.cuda.stream(stream) if isinstance(stream, torch.cuda.Stream) else torch.cuda.device(dev):
+        with _as_current(stream, handle, dev):
             for g in (dw_post, dw_pre, dgate):
                 if g is not None:
                     g.zero_()
         return
-    code, handle = _dtype_of(first, "activations"), _stream_on(stream, dev)
     if workspace is None:
-        workspace = torch.empty(max(fgd_block_norm_workspace(code, K, T // K, H, dev.index), 1), dtype=torch.uint8, device=dev)
-        if stream is not None and handle != torch.cuda.current_stream(dev).cuda_stream:   # the caching allocator must not hand it out again before the call has run
-            workspace.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(handle, device=dev))
+        size = max(fgd_block_norm_workspace(code, K, T // K, H, dev.index), 1)
+        if stream is None:
+            workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+        else:
+            # From the memory of the stream that uses it: a block of another stream's may have uses on that stream still to come before
+            # this call, and would need to be kept from others until after it.
+            with _as_current(stream, handle, dev):
+                workspace = torch.empty(size, dtype=torch.uint8, device=dev)
     args = _NORM_ARGS.pack(code, K, T // K, H, kind, eps, res_scale, *mats, _dev_ptr(workspace, "workspace", "torch.uint8"), workspace.numel())
     _op_check(_lib.fgd_block_norm_backward(dev.index, args, handle))
 

@@ -64,3 +64,33 @@ def test_swiglu8_backward_of_large_values(F, dtype):
     _near(h2, ref, (u + fp8) * np.abs(ref), "h again")
 
 
+# ------------------------------------------------------------------------------- streams
+@pytest.mark.parametrize("given_as", ["stream", "handle"])
+def test_block_norm_workspace_belongs_to_the_calls_stream(given_as):
+    """Without a workspace the call takes one from its own stream's memory: a block that was freed on the current stream, and is still to be
+    written there, is not handed to a call on another stream."""
+    import paper_2606_22768_b200 as fgd
+    torch = _torch()
+    T, H = 512, 1024
+    dn, dr, x, y = (_randn((T, H), "bf16", i) for i in range(4))
+    w = torch.ones((1, H), device="cuda")
+    want = [torch.empty_like(x), torch.empty_like(x), torch.empty_like(w), torch.empty_like(w)]
+    got = [torch.empty_like(t) for t in want]
+    need = fgd.fgd_block_norm_workspace(fgd.FGD_BF16, 1, T, H)
+    fgd.fgd_block_norm_backward(dn, dr, x, y, None, w, w, want[0], want[1], None, want[2], want[3])
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    for _ in range(5):
+        blocks = [torch.empty(need, dtype=torch.uint8, device="cuda") for _ in range(4)]
+        torch.cuda._sleep(20_000_000)                                     # the current stream is behind, and then writes the blocks
+        for b in blocks:
+            for _ in range(20):
+                b.fill_(0x7F)
+        del blocks, b
+        fgd.fgd_block_norm_backward(dn, dr, x, y, None, w, w, got[0], got[1], None, got[2], got[3],
+                                    stream=side if given_as == "stream" else side.cuda_stream)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
