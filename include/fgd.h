@@ -308,9 +308,10 @@ typedef struct {
 /* A packing: sequence i holds the tokens [cu_seqlens[i], cu_seqlens[i+1]) (HOST memory, n_seqs + 1 values,
  * cu_seqlens[0] = 0, not decreasing; empty sequences are fine).  The plan keeps the work list of the
  * kernels on the device (a few bytes per 128 tokens), so create it once per batch and use it for every
- * layer, forward and backward, on any head count and width.  Creating it allocates and copies (not inside
- * a stream capture); the calls that use it do neither and can be captured.  A plan is used by one
- * host thread at a time; kernels of one plan may run on several streams at once. */
+ * layer, forward and backward, on any head count and width.  Creating it allocates, copies and
+ * waits for the copy (not inside a stream capture), so that any stream can use it next; the calls that use it do none of that and can
+ * be captured.  Destroying it waits for the device; a graph that captured calls needs its plan for as long as it is replayed.  A plan is
+ * used by one host thread at a time; kernels of one plan may run on several streams at once. */
 typedef struct fgd_attn_plan fgd_attn_plan;
 int fgd_attn_plan_create(fgd_attn_plan** out, int device, int n_seqs, const int64_t* cu_seqlens);
 int fgd_attn_plan_destroy(fgd_attn_plan* plan);

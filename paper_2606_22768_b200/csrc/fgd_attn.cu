@@ -110,6 +110,9 @@ extern "C" int fgd_attn_plan_create(fgd_attn_plan** out, int device, int n_seqs,
       p->kv_tiles = p->q2_tiles + q2.size();
       p->status = reinterpret_cast<int*>(p->kv_tiles + kv.size());
       e = cudaMemcpy(p->q_tiles, all.data(), bytes, cudaMemcpyHostToDevice);
+      // From pageable memory that call may return before the bytes are on the device, and streams that do not wait for the default one may
+      // use the plan next.
+      if (e == cudaSuccess) e = cudaStreamSynchronize(cudaStreamLegacy);
     }
     if (e == cudaSuccess) {
       cudaDriverEntryPointQueryResult qr;

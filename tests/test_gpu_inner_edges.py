@@ -94,3 +94,25 @@ def test_block_norm_workspace_belongs_to_the_calls_stream(given_as):
         assert all(torch.equal(a, b) for a, b in zip(want, got))
 
 
+def test_attention_plan_is_ready_on_every_stream():
+    """A plan can be used on a stream that does not wait for the default one as soon as it exists."""
+    import paper_2606_22768_b200 as fgd
+    torch = _torch()
+    rng = np.random.default_rng(0)
+    side = torch.cuda.Stream()
+    hq, hk, d, T = 4, 2, 64, 3000
+    q, k, v = (_randn((T, h, d), "bf16", i) for i, h in enumerate((hq, hk, hk)))
+    torch.cuda.synchronize()
+    for _ in range(8):
+        cu = np.concatenate([[0], np.sort(rng.integers(0, T, 600)), [T]])
+        o, lse = torch.empty_like(q), torch.empty((hq, T), device="cuda")
+        torch.cuda.synchronize()
+        plan = fgd.AttnPlan(cu)
+        fgd.fgd_attn_forward(plan, q, k, v, o, lse, stream=side)
+        side.synchronize()
+        o2, lse2 = torch.empty_like(q), torch.empty_like(lse)
+        fgd.fgd_attn_forward(plan, q, k, v, o2, lse2)
+        fgd.fgd_attn_status(plan)
+        assert torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
