@@ -116,3 +116,24 @@ def test_attention_plan_is_ready_on_every_stream():
         assert torch.equal(o, o2) and torch.equal(lse, lse2)
 
 
+# ------------------------------------------------------------------------------- autograd
+def test_second_derivatives_are_refused():
+    """The backward passes are not differentiable: a second derivative through them is an error, not a result without their terms."""
+    from paper_2606_22768_b200 import AttnPlan, inner
+    torch = _torch()
+    plan = AttnPlan([0, 20, 32])
+
+    def leaf(shape, seed, dtype="bf16"):
+        return _randn(shape, dtype, seed).requires_grad_(True)
+
+    q, k, v = leaf((32, 4, 64), 0), leaf((32, 2, 64), 1), leaf((32, 2, 64), 2)
+    x, y, w_post, w_pre = leaf((32, 64), 3), leaf((32, 64), 4), leaf((2, 64), 5, "f32"), leaf((2, 64), 6, "f32")
+    gu, w = leaf((32, 128), 7), leaf((2, 48, 64), 8)
+    for name, out, t in (("attention", inner.attention(q, k, v, plan), q), ("block_norm", inner.block_norm(x, y, None, w_post, w_pre)[1], x),
+                         ("swiglu8", inner.swiglu8(gu), gu), ("linear8", inner.linear8(x, w), w)):
+        g, = torch.autograd.grad(out.float().square().sum(), t, create_graph=True)
+        with pytest.raises(RuntimeError, match="once_differentiable"):
+            torch.autograd.grad((g * t).float().sum(), t)
+            pytest.fail(f"{name}: a second derivative came back")
+
+
