@@ -6,22 +6,33 @@ for the backward pass -- as autograd functions; matrix products are plain librar
 workers take their step in one pass: activations are [K * rows, width] with worker m's rows at [m * rows, (m + 1) * rows).
 
 What a block keeps for its backward pass: the residual stream and the block outputs (the norms need them), q, k, v, o and lse, and in
-8 bits the inputs of its projections and of SwiGLU.  The backward passes are not differentiable themselves: asking for a second derivative
-through them is an error.
+8 bits the inputs of its projections and of SwiGLU.  The backward passes are not differentiable themselves: create_graph=True is an error
+in them.
 """
 from __future__ import annotations
 
+import functools
 from dataclasses import dataclass
 from typing import Dict, Optional, Tuple
 
 import torch
-from torch.autograd.function import once_differentiable
 
 from . import (ACT8_GROUP, AttnPlan, fgd_act_load8, fgd_act_save8, fgd_attn_backward, fgd_attn_forward, fgd_block_norm_backward, fgd_block_norm_forward,
                fgd_swiglu8_backward, fgd_swiglu8_forward)
 
 
 # ------------------------------------------------------------------------------- operators
+def _first_order(backward):
+    """A backward pass whose results carry no graph.  Where one is asked for they would count as constants, and a second derivative would
+    silently lack their terms: refused here, since a refusal that waits for the second pass is not reached by every way to start it."""
+    @functools.wraps(backward)
+    def checked(ctx, *grads):
+        if torch.is_grad_enabled():      # in a backward pass: create_graph=True
+            raise RuntimeError("the inner step's operators are not differentiable twice: their backward passes do not run with create_graph=True")
+        return backward(ctx, *grads)
+    return checked
+
+
 class _Attention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, plan, scale):
@@ -33,7 +44,7 @@ class _Attention(torch.autograd.Function):
         return o
 
     @staticmethod
-    @once_differentiable
+    @_first_order
     def backward(ctx, do):
         q, k, v, o, lse = ctx.saved_tensors
         dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
@@ -57,7 +68,7 @@ class _BlockNorm(torch.autograd.Function):
         return (x.view_as(x) if y is None else x_new), n
 
     @staticmethod
-    @once_differentiable
+    @_first_order
     def backward(ctx, dres, dn):
         x_new, y, gate, w_post, w_pre = ctx.saved_tensors
         like = lambda t: None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device)  # noqa: E731
@@ -84,7 +95,7 @@ class _Swiglu8(torch.autograd.Function):
         return h
 
     @staticmethod
-    @once_differentiable
+    @_first_order
     def backward(ctx, dh):
         q8, e8 = ctx.saved_tensors
         dgu = torch.empty(q8.shape, dtype=dh.dtype, device=dh.device)
@@ -108,7 +119,7 @@ class _Linear8(torch.autograd.Function):
         return torch.bmm(x.view(K, -1, x.shape[1]), w.transpose(1, 2)).view(x.shape[0], w.shape[1])
 
     @staticmethod
-    @once_differentiable
+    @_first_order
     def backward(ctx, dy):
         q8, e8, w = ctx.saved_tensors
         K = w.shape[0]

@@ -131,9 +131,11 @@ def test_second_derivatives_are_refused():
     gu, w = leaf((32, 128), 7), leaf((2, 48, 64), 8)
     for name, out, t in (("attention", inner.attention(q, k, v, plan), q), ("block_norm", inner.block_norm(x, y, None, w_post, w_pre)[1], x),
                          ("swiglu8", inner.swiglu8(gu), gu), ("linear8", inner.linear8(x, w), w)):
-        g, = torch.autograd.grad(out.float().square().sum(), t, create_graph=True)
-        with pytest.raises(RuntimeError, match="once_differentiable"):
-            torch.autograd.grad((g * t).float().sum(), t)
-            pytest.fail(f"{name}: a second derivative came back")
+        for loss in (out.float().square().sum(), out.float().sum()):      # (the gradient that comes in depends on the inputs, or is constant)
+            with pytest.raises(RuntimeError, match="differentiable twice"):
+                g, = torch.autograd.grad(loss, t, create_graph=True, retain_graph=True)
+                torch.autograd.grad((g * t).float().sum(), t)
+                pytest.fail(f"{name}: a second derivative came back")
+            torch.autograd.grad(loss, t, retain_graph=True)               # the first derivative is there as before
 
 
