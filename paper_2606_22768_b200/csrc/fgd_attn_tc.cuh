@@ -193,19 +193,21 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return y;
 }
 // 2^x on the FMA pipes: x = n + f with n the nearest integer, 2^f on [-1/2, 1/2] as a polynomial (minimax of degree 4 by Remez
-// exchange: relative error 2.7e-6, mean 4e-8, far below the 16-bit rounding of P and below 1e-6 in a row's sum), n added to the exponent.
+// exchange: relative error 2.7e-6, mean 4e-8, far below the 16-bit rounding of P and below 1e-6 in a row's sum), times 2^n.
 // The exponential units give 16 results a clock and SM, and a 128 x 128 block of scores has 16384 of them: 1024 clocks, as much as two of
-// its products take.  A share of the exponentials goes this way instead.  x below -126 gives 2^-126; an x that is not finite gives a
-// result that is not finite (or at least 2^127), or 2^-126 for -inf.
+// its products take.  A share of the exponentials goes this way instead.  Which of a row's columns do is fixed, so at the ends it has to give
+// what the hardware's exponential gives: x below -126.5, -inf among them, gives 0 (n = -127 has the bits of 0: a masked place has no
+// weight, not 2^-126), and a NaN stays one, as +inf becomes one.  x up to 128; scores exceed neither their row's maximum by more than 8 nor its lse.
 __device__ __forceinline__ float2 exp2_poly(float2 x) {
-  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-126.f));
-  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-126.f));
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-127.f));
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-127.f));
   const float2 t = add2(x, both(12582912.f)), f = fma2(add2(t, both(-12582912.f)), both(-1.f), x);
   float2 p = fma2(both(0.009570102207362652f), f, both(0.05591785907745361f));
   p = fma2(p, f, both(0.240247443318367f));
   p = fma2(p, f, both(0.6931217908859253f));
   p = fma2(p, f, both(0.9999992847442627f));
-  return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23)), __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
+  const float2 scale = make_float2(__uint_as_float((__float_as_uint(t.x) << 23) + 0x3F800000u), __uint_as_float((__float_as_uint(t.y) << 23) + 0x3F800000u));
+  return mul2(p, scale);
 }
 // 2^x for the k-th pair of a row: one pair in eight by polynomial (none, 1/8, 1/4: 16384 tokens forward 857, 828, 850 us; 1/2 in the
 // key kernel gains nothing either: the FMA pipes' instructions then cost what the exponential units save).

@@ -139,3 +139,41 @@ def test_second_derivatives_are_refused():
             torch.autograd.grad(loss, t, retain_graph=True)               # the first derivative is there as before
 
 
+# ------------------------------------------------------------------------------- attention: masked and non-finite values
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_large_values_of_later_tokens_do_not_leak(d):
+    """Finite values of later tokens, up to the type's largest, leave an earlier token's output as it was, bit for bit."""
+    import paper_2606_22768_b200 as fgd
+    torch = _torch()
+    q, k, v = (_randn((300, h, d), "bf16", i) for i, h in enumerate((4, 2, 2)))
+    plan = fgd.AttnPlan([0, 300])
+    res = []
+    for value in (None, 3e38, -3e38):
+        v2 = v.clone()
+        if value is not None:
+            v2[150:] = value
+        o, lse = torch.empty_like(q), torch.empty((4, 300), device="cuda")
+        fgd.fgd_attn_forward(plan, q, k, v2, o, lse)
+        res.append(o[:150])
+    assert torch.equal(res[0], res[1]) and torch.equal(res[0], res[2])
+
+
+@pytest.mark.parametrize("d,dtype", [(64, "bf16"), (128, "f16"), (64, "f32")])
+def test_attention_nan_key_in_any_column(d, dtype):
+    """A NaN key makes every row that sees it NaN, output and lse, wherever in a block of keys it stands; the rows before it stay."""
+    import paper_2606_22768_b200 as fgd
+    torch = _torch()
+    T, hq, hk = 300, 4, 2
+    q, k, v = (_randn((T, h, d), dtype, i) for i, h in enumerate((hq, hk, hk)))
+    plan = fgd.AttnPlan([0, T])
+    o0, lse0 = torch.empty_like(q), torch.empty((hq, T), device="cuda")
+    fgd.fgd_attn_forward(plan, q, k, v, o0, lse0)
+    for at in list(range(16)) + [62, 63, 126, 127, 142, 143, 255, 270, 299]:
+        bad = k.clone()
+        bad[at] = float("nan")
+        o, lse = torch.empty_like(q), torch.empty_like(lse0)
+        fgd.fgd_attn_forward(plan, q, bad, v, o, lse)
+        assert torch.equal(o[:at], o0[:at]) and torch.equal(lse[:, :at], lse0[:, :at]), f"key {at}"
+        assert bool(o[at:].isnan().all()) and bool(lse[:, at:].isnan().all()), f"key {at}"
+
+
