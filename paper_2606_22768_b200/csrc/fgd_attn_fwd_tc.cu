@@ -246,7 +246,8 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, FastDiv per_tile, int i
         half_max(64);
         const float top = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * c;
         if (diagonal) {
-          m = top == -INFINITY ? 0.f : top;
+          // No finite score here (an infinite key): a maximum that every later finite one exceeds, and from which -inf is still -inf away.
+          m = top == -INFINITY ? -1.7e38f : top;
         } else if (__any_sync(0xffffffffu, real && top > m + kRescale)) {      // (rows of another sequence have no say in it)
           const float mn = fmaxf(m, top), f = exp2_fast(m - mn);
           if (!(ok = wait(pv_done + 8 * t, (n_pv - 1) & 1))) break;

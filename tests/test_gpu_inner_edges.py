@@ -177,3 +177,41 @@ def test_attention_nan_key_in_any_column(d, dtype):
         assert bool(o[at:].isnan().all()) and bool(lse[:, at:].isnan().all()), f"key {at}"
 
 
+@pytest.mark.parametrize("d,dtype", [(64, "bf16"), (128, "f16"), (64, "f32")])
+def test_attention_minus_infinity_scores(d, dtype):
+    """A key whose scores are all -inf has no weight, also where it is the only key that a row sees of its own block of 128: the row is the
+    softmax of the others, however low their scores."""
+    import paper_2606_22768_b200 as fgd
+    torch = _torch()
+    T, hq, hk, scale = 300, 4, 2, 0.125
+    q, k, v = (_randn((T, h, d), dtype, i) for i, h in enumerate((hq, hk, hk)))
+    q[..., 0], k[..., 0] = 1.0, 0.0
+    q[..., 1], k[..., 1] = 16.0, -200.0                                   # every score is about -400
+    k[256, :, 0] = float("-inf")
+    plan = fgd.AttnPlan([0, T])
+    o, lse = torch.empty_like(q), torch.empty((hq, T), device="cuda")
+    fgd.fgd_attn_forward(plan, q, k, v, o, lse, scale)
+    fgd.fgd_attn_status(plan)
+    ref, ref_lse, mag = O.attention(_np(q), _np(k), _np(v), [0, T], scale)
+    u, fp = U[dtype], F32 * (16 + d / 4 + 8 * 450)
+    _near(o, ref, u * np.abs(ref) + (1.01 * u + fp) * mag + TINY[dtype], "o")
+    _near(lse, ref_lse, fp + 4 * F32 * np.abs(ref_lse), "lse")
+
+
+@pytest.mark.parametrize("d,dtype", [(64, "bf16"), (128, "f16"), (64, "f32")])
+def test_attention_row_without_a_finite_score(d, dtype):
+    """A row that sees scores of -inf alone has no softmax: NaN, and an lse that is not finite; the rows beside it are as without it."""
+    import paper_2606_22768_b200 as fgd
+    torch = _torch()
+    q, k, v = (_randn((41, h, d), dtype, i).abs() for i, h in enumerate((4, 2, 2)))
+    plan = fgd.AttnPlan([0, 1, 41])
+    res = []
+    for value in (1.0, float("-inf")):
+        k[0] = value
+        o, lse = torch.empty_like(q), torch.empty((4, 41), device="cuda")
+        fgd.fgd_attn_forward(plan, q, k, v, o, lse)
+        res.append((o, lse))
+    assert bool(res[1][0][0].isnan().all()) and not bool(torch.isfinite(res[1][1][:, 0]).any())
+    assert torch.equal(res[0][0][1:], res[1][0][1:]) and torch.equal(res[0][1][:, 1:], res[1][1][:, 1:])
+
+
