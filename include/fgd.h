@@ -301,7 +301,7 @@ typedef struct {
   double scale;
   /* backward only: */
   fgd_heads dout;       /* gradient of o */
-  float* delta;         /* [n_q_heads, tokens] scratch: sum over the width of o * dout */
+  float* delta;         /* [n_q_heads, tokens] scratch (sums over the width of o * dout, o as it was stored); not an output */
   fgd_heads dq, dk, dv; /* outputs; dk, dv summed over the query heads that share them */
 } fgd_attn_args;
 

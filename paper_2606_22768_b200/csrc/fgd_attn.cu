@@ -216,6 +216,6 @@ extern "C" int fgd_attn_backward(fgd_attn_plan* plan, const fgd_attn_args* b, vo
   const AttnArgs a = kernel_args(plan, b);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool tc = on_tensor_cores(plan, b, all, 8);
-  if (int rc = attn_delta(b->dtype, tc, a, st)) return rc;
+  if (int rc = attn_delta(plan, b->dtype, tc, a, st)) return rc;
   return tc ? attn_backward_tc(plan, b->dtype, a, st) : attn_backward_elem(plan, b->dtype, a, st);
 }

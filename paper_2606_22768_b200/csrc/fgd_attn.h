@@ -67,7 +67,8 @@ int attn_backward_elem(const fgd_attn_plan* plan, int dtype, const AttnArgs& a, 
 // Tensor-core kernels: bf16 and fp16, width a multiple of 8 up to 128, 16-byte rows, scale > 0.
 int attn_forward_tc(const fgd_attn_plan* plan, int dtype, const AttnArgs& a, cudaStream_t st);
 int attn_backward_tc(const fgd_attn_plan* plan, int dtype, const AttnArgs& a, cudaStream_t st);
-// delta of every (token, head); `vectors`: o and dout are 16-bit, in 16-byte vectors, at most 128 wide
-int attn_delta(int dtype, bool vectors, const AttnArgs& a, cudaStream_t st);
+// delta of every (token, head); `vectors`: o and dout are 16-bit, in 16-byte vectors, at most 128 wide (then, in fp16, also what
+// the tensor-core kernels choose their factors' scale from, in delta and dq)
+int attn_delta(const fgd_attn_plan* plan, int dtype, bool vectors, AttnArgs a, cudaStream_t st);
 }  // namespace fgd
 #endif

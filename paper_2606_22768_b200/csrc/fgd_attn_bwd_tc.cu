@@ -14,6 +14,11 @@
 //     runs; dP^T = V dO^T, dS^T over dP^T, dK += dS^T Q, and while P^T of the next block is formed the next dP^T runs.
 // `scale` multiplies dQ and dK once, at the end.
 //
+// fp16 alone: dS is held times a power of two, and P times 2^10, so that small gradients and long rows stay above the type's smallest
+// values and large ones below its largest (attn_lift; fgd_attn_elem.cu has the bounds it goes by): per 32 rows in the query kernel, per item in the
+// key kernel, where a sum runs over rows.  The output's factor takes it back, exactly; in the loops it costs no instruction.  Forward + backward
+// against dS as it is: 288 tokens 34.9 us (32.8), 16 x 1024 of 16 heads of 64 316 us (302: v is read once more), 8192 of 16 x 128 1 % more.
+//
 // Rounding: P and dS are rounded to the 16-bit type as factors of the next product (5 products in fp32 would need tf32 operands at
 // half the rate and twice the shared memory): gradients are .0025 of their norm off in bf16, .0017 with the output's rounding alone.
 //
@@ -46,6 +51,21 @@ __device__ __forceinline__ void load_row64(uint32_t addr, uint32_t (&s)[64]) {
   tmem_ld_32(addr + 32, s + 32);
   tmem_ld_done<64>(s);
 }
+// The power of two that takes b = max |dout| max |v| (0: none) to [2^6, 2^7): dP and delta, at most width x b <= 128 b in magnitude, then stay
+// below 2^14, dS below 2^15.  b is 0 or in [2^-48, 2^32).
+__device__ __forceinline__ float attn_lift(float b) {
+  const uint32_t e = __float_as_uint(b) >> 23;
+  return e == 0 ? 1.f : __uint_as_float((2 * 127 + 6 - e) << 23);
+}
+__device__ __forceinline__ float power_inverse(float p) { return __uint_as_float((254u << 23) - __float_as_uint(p)); }      // 1 / 2^k, |k| < 126
+constexpr float kLiftP = 1024.f;
+// What the fp16 delta kernel left for the 32 rows of `head` from `token` on: the largest |v| (low half; the first head of a group has it) and
+// |dout| (high), and the first row's delta.  Positive fp16 values order as integers do.
+__device__ __forceinline__ uint32_t rows_tops(const AttnArgs& a, int64_t token, int head) { return __ldcg(reinterpret_cast<const uint32_t*>(a.delta + head * a.tokens + token)); }
+__device__ __forceinline__ float first_delta(const AttnArgs& a, int64_t token, int head) {
+  return __ldcg(reinterpret_cast<const float*>(a.dq.p + 2 * (token * a.dq.token + head * a.dq.head)));
+}
+__device__ __forceinline__ float tops_bound(uint32_t v, uint32_t dout) { return halves<__half>(v & 0xFFFFu).x * halves<__half>(dout >> 16).x; }
 // 64 values of this thread's row as 16-bit factors of the next product
 template <bool BF16>
 __device__ __forceinline__ void store_pairs(uint32_t addr, const float2 (&x)[32]) {
@@ -214,18 +234,32 @@ attn_dq_tc_kernel(const AttnArgs a, FastDiv heads, int items, const __grid_const
     bool ok = true;
     ItemWalk walk(a.tiles, heads, items);
     float lse = 0.f, delta = 0.f;      // of this thread's row of the coming item
+    uint32_t top_v = 0, top_g = 0;     // fp16: of 32 of the keys that the warp's rows see, and of its rows
     auto row_stats = [&]() {
-      if (walk.valid && walk.t.row + r < walk.t.len) {
+      const int first = walk.t.row + r - lane;      // the warp's first row
+      if (walk.valid && first + lane < walk.t.len) {
         const int64_t at = (int64_t)walk.h * a.tokens + walk.t.start + walk.t.row + r;
         lse = a.lse[at];
         delta = a.delta[at];
+        if (!BF16 && lane == 0) delta = first_delta(a, walk.t.start + first, walk.h);
+      }
+      if constexpr (!BF16) {
+        top_v = top_g = 0;
+        if (walk.valid && first < walk.t.len) {
+          const int kv = walk.h / group * group;      // the head that has v's
+          top_g = rows_tops(a, walk.t.start + first, walk.h);
+          if (32 * lane <= first) top_v = rows_tops(a, walk.t.start + 32 * lane, kv) & 0xFFFFu;
+          for (int row = 32 * (lane + 32); row <= first; row += 32 * 32) top_v = max(top_v, rows_tops(a, walk.t.start + row, kv) & 0xFFFFu);
+        }
       }
     };
     row_stats();
     while (ok && walk.valid) {
       const AttnTile t = walk.t;
       const int n = blocks(t), head = walk.h, round = walk.round;
-      const float2 lse2 = both(-lse * kLog2e), delta2 = both(-delta);
+      const float lift = BF16 ? 1.f : attn_lift(tops_bound(__reduce_max_sync(0xffffffffu, top_v), top_g));
+      const float2 lse2 = both(-lse * kLog2e), lift2 = both(lift), delta2 = both(-delta * lift);
+      const float factor = BF16 ? a.scale : a.scale * power_inverse(lift);
       for (int i = 0; i < n; ++i, ++u) {
         const uint32_t ts = tmem + 128 * (u & 1) + 64 * h + lanes;
         if (!(ok = wait(s_full + 8 * (u & 1), (u >> 1) & 1))) break;
@@ -239,7 +273,7 @@ attn_dq_tc_kernel(const AttnArgs a, FastDiv heads, int items, const __grid_const
         tc_fence_after();
         load_row64(td, s);
 #pragma unroll
-        for (int k = 0; k < 32; ++k) p[k] = mul2(p[k], add2(two(s + 2 * k), delta2));
+        for (int k = 0; k < 32; ++k) p[k] = mul2(p[k], BF16 ? add2(two(s + 2 * k), delta2) : fma2(two(s + 2 * k), lift2, delta2));
         if (i == 0) {      // the block on the diagonal (0 times a non-finite value of a masked place is not 0)
 #pragma unroll
           for (int k = 0; k < 32; ++k) {
@@ -255,6 +289,7 @@ attn_dq_tc_kernel(const AttnArgs a, FastDiv heads, int items, const __grid_const
       row_stats();
       if (!(ok = wait(dq_done, round & 1))) break;
       tc_fence_after();
+      if (!BF16 && round == 0) wait_for_previous();      // the key kernel reads what stands where the results go
       const int row0 = t.row + (warp & 3) * 32;
       char* out = a.dq.p + 2 * ((int64_t)(t.start + row0) * a.dq.token + head * a.dq.head);
 #pragma unroll 1      // (once per item: code that stays short stays in the instruction cache)
@@ -262,7 +297,7 @@ attn_dq_tc_kernel(const AttnArgs a, FastDiv heads, int items, const __grid_const
         uint32_t o[32];
         tmem_ld_32(tmem + c_dq + h * (DP / 2) + k + lanes, o);
         tmem_ld_done<32>(o);
-        store_rows<BF16>(base + (2 * NQ + SK + SV) * TILE + warp * kStoreStage, o, a.scale, out, 2 * a.dq.token, t.len - row0, h * (DP / 2) + k, a.d, lane);
+        store_rows<BF16>(base + (2 * NQ + SK + SV) * TILE + warp * kStoreStage, o, factor, out, 2 * a.dq.token, t.len - row0, h * (DP / 2) + k, a.d, lane);
       }
       tc_fence_before();
       mbar_arrive(dq_free);
@@ -286,6 +321,7 @@ attn_dkv_tc_kernel(const AttnArgs a, FastDiv heads, int items, const __grid_cons
   constexpr int SQ = kStagesQ<DP>, SR = kStagesRow;
   extern __shared__ unsigned char smem_raw[];
   __shared__ __align__(8) unsigned long long bars[12 + 4 * SQ + 2 * SR];
+  __shared__ float lift_of[SR];      // of the item that a stage of rows belongs to, over P's own
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
   unsigned char* base = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -387,16 +423,32 @@ attn_dkv_tc_kernel(const AttnArgs a, FastDiv heads, int items, const __grid_cons
     for (ItemWalk walk(a.tiles, heads, items); ok && walk.valid; walk.next()) {
       const AttnTile t = walk.t;
       const int first = t.row / kAttnRows, per_head = per_head_of(t);
+      float lift = 1.f;
+      if constexpr (!BF16) {
+        uint32_t v = 0, g = 0;      // (v of the whole sequence: the item's queries see all of it)
+        for (int row = 32 * lane; row < t.len; row += 32 * 32) v = max(v, rows_tops(a, t.start + row, walk.h * group) & 0xFFFFu);
+        for (int hh = 0; hh < group; ++hh)
+          for (int row = t.row + 32 * lane; row < t.len; row += 32 * 32) g = max(g, rows_tops(a, t.start + row, walk.h * group + hh));
+        lift = attn_lift(tops_bound(__reduce_max_sync(0xffffffffu, v), __reduce_max_sync(0xffffffffu, g))) * (1.f / kLiftP);
+      }
       for (int hh = 0; ok && hh < group; ++hh)
         for (int i = 0; i < per_head; ++i, ++u) {
           const int row = (first + i) * 128, rows = t.len - row;
           const int64_t at = (int64_t)(walk.h * group + hh) * a.tokens + t.start + row;
-          float lse[4], delta[4];
+          float lse[4], delta[4], first = 0.f;      // first: lane j's is the delta of row 32 j
+          if (!BF16 && lane < 4 && 32 * lane < rows) first = first_delta(a, t.start + row + 32 * lane, walk.h * group + hh);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {      // negated; rows beyond the end: P = 2^-inf = 0
             const int k = lane + 32 * j;
-            lse[j] = k < rows ? -a.lse[at + k] * kLog2e : -INFINITY;
-            delta[j] = k < rows ? -a.delta[at + k] : 0.f;
+            lse[j] = k < rows ? -a.lse[at + k] * kLog2e + (BF16 ? 0.f : 10.f) : -INFINITY;      // (kLiftP)
+            delta[j] = k < rows ? -a.delta[at + k] * lift : 0.f;
+          }
+          if constexpr (!BF16) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float f = -__shfl_sync(0xffffffffu, first, j) * lift;
+              if (lane == 0) delta[j] = f;
+            }
           }
           if (!(ok = wait(row_empty + 8 * (u % SR), ((u / SR) & 1) ^ 1))) break;
           float* stats = row_stats + (u % SR) * 256;
@@ -405,6 +457,7 @@ attn_dkv_tc_kernel(const AttnArgs a, FastDiv heads, int items, const __grid_cons
             stats[lane + 32 * j] = lse[j];
             stats[128 + lane + 32 * j] = delta[j];
           }
+          if (!BF16 && lane == 0) lift_of[u % SR] = lift;
           mbar_arrive(row_full + 8 * (u % SR));
         }
     }
@@ -466,11 +519,13 @@ attn_dkv_tc_kernel(const AttnArgs a, FastDiv heads, int items, const __grid_cons
     while (ok && walk.valid) {
       const AttnTile t = walk.t;
       const int kvh = walk.h, round = walk.round, per_head = per_head_of(t), n = group * per_head;
+      float lift = 1.f;
       for (int i = 0, q = 0; i < n; ++i, ++u, q = q + 1 == per_head ? 0 : q + 1) {
         const uint32_t st = u % SR;
         const float4* lse4 = reinterpret_cast<const float4*>(row_stats + st * 256 + 64 * h);
         const float4* delta4 = lse4 + 32;
         if (!(ok = wait(row_full + 8 * st, (u / SR) & 1))) break;
+        if constexpr (!BF16) lift = lift_of[st];
         if (!(ok = wait(s_full, u & 1))) break;
         tc_fence_after();
         uint32_t s[64];
@@ -498,8 +553,9 @@ attn_dkv_tc_kernel(const AttnArgs a, FastDiv heads, int items, const __grid_cons
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
           const float4 l = delta4[k];
-          p[2 * k] = mul2(p[2 * k], add2(two(s + 4 * k), make_float2(l.x, l.y)));
-          p[2 * k + 1] = mul2(p[2 * k + 1], add2(two(s + 4 * k + 2), make_float2(l.z, l.w)));
+          const float2 x = two(s + 4 * k), y = two(s + 4 * k + 2);
+          p[2 * k] = mul2(p[2 * k], BF16 ? add2(x, make_float2(l.x, l.y)) : fma2(x, both(lift), make_float2(l.x, l.y)));
+          p[2 * k + 1] = mul2(p[2 * k + 1], BF16 ? add2(y, make_float2(l.z, l.w)) : fma2(y, both(lift), make_float2(l.z, l.w)));
         }
         if (q == 0) mask();      // (0 times a non-finite value of a masked place is not 0)
         mbar_arrive(row_empty + 8 * st);
@@ -513,6 +569,7 @@ attn_dkv_tc_kernel(const AttnArgs a, FastDiv heads, int items, const __grid_cons
       const int row0 = t.row + (warp & 3) * 32;
       // half 0 writes dK, half 1 dV
       const AttnHeads& to = h ? a.dv : a.dk;
+      const float back = BF16 ? 1.f : 1.f / kLiftP, factor = h ? back : BF16 ? a.scale : a.scale * back * power_inverse(lift);
       char* out = to.p + 2 * ((int64_t)(t.start + row0) * to.token + kvh * to.head);
       unsigned char* stage = base + (2 + 2 * SQ) * TILE + SR * 2 * 128 * sizeof(float) + warp * kStoreStage;
 #pragma unroll 1
@@ -520,7 +577,7 @@ attn_dkv_tc_kernel(const AttnArgs a, FastDiv heads, int items, const __grid_cons
         uint32_t o[32];
         tmem_ld_32(tmem + (h ? c_dv : c_dk) + k + lanes, o);
         tmem_ld_done<32>(o);
-        store_rows<BF16>(stage, o, h ? 1.f : a.scale, out, 2 * to.token, t.len - row0, k, a.d, lane);
+        store_rows<BF16>(stage, o, factor, out, 2 * to.token, t.len - row0, k, a.d, lane);
       }
       tc_fence_before();
       mbar_arrive(out_free);

@@ -133,24 +133,28 @@ __global__ void __launch_bounds__(256) attn_delta_kernel(const AttnArgs a) {
 }
 
 // The same for 16-bit values in 16-byte vectors: L lanes take a row, a warp 32 tokens of one head (so that its 32 results are one
-// store), eight rows' loads per lane on their way at a time.
-template <typename T, int L>
-__global__ void __launch_bounds__(256) attn_delta_vec_kernel(const AttnArgs a) {
+// store), eight rows' loads per lane on their way at a time.  -> delta of token0 + lane, and, where TOP asks for it, the largest
+// magnitude of dout that this lane has met, as fp16 bits; tokens at or beyond `end` count as zero.
+__device__ __forceinline__ uint32_t top_of(uint32_t top, uint4 w) {      // of pairs of fp16 magnitudes, which order as integers do
+  top = __vmaxu2(__vmaxu2(top, w.x & 0x7FFF7FFFu), w.y & 0x7FFF7FFFu);
+  return __vmaxu2(__vmaxu2(top, w.z & 0x7FFF7FFFu), w.w & 0x7FFF7FFFu);
+}
+// of a warp; infinities and NaN count as the largest finite value
+__device__ __forceinline__ uint16_t warp_top(uint32_t top) { return (uint16_t)min(__reduce_max_sync(0xffffffffu, max(top >> 16, top & 0xFFFFu)), 0x7BFFu); }
+template <typename T, int L, bool TOP>
+__device__ __forceinline__ float delta_of_32(const AttnArgs& a, int head, int64_t token0, int64_t end, uint32_t& top) {
   constexpr int RPS = 32 / L, AT_ONCE = 8;                 // rows per step of the warp, steps at a time
-  let_next_start();
   const int lane = threadIdx.x & 31, sub = lane / L, c = (lane % L) * 8;
-  const int64_t warp = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), head = warp % a.hq, token0 = warp / a.hq * 32;
-  if (token0 >= a.tokens) return;
-  float mine = 0.f;                                        // of token0 + lane
+  float mine = 0.f;
 #pragma unroll
   for (int s0 = 0; s0 < L; s0 += AT_ONCE) {
     ActPack<T, 8> o[AT_ONCE], g[AT_ONCE];
 #pragma unroll
     for (int s = 0; s < AT_ONCE; ++s) {
       const int64_t token = token0 + (s0 + s) * RPS + sub;
-      if (token < a.tokens && c < a.d) {
-        o[s] = load_stream<T, 8>(row_of<T>(a.o, token, (int)head) + c);
-        g[s] = load_stream<T, 8>(row_of<T>(a.dout, token, (int)head) + c);
+      if (token < end && c < a.d) {
+        o[s] = load_stream<T, 8>(row_of<T>(a.o, token, head) + c);
+        g[s] = load_stream<T, 8>(row_of<T>(a.dout, token, head) + c);
       } else {
         zero(o[s]);
         zero(g[s]);
@@ -167,9 +171,69 @@ __global__ void __launch_bounds__(256) attn_delta_vec_kernel(const AttnArgs a) {
       for (int off = L / 2; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
       sum = __shfl_sync(0xffffffffu, sum, (lane % RPS) * L);
       if (lane / RPS == s0 + s) mine = sum;
+      if constexpr (TOP) top = top_of(top, g[s].w);
     }
   }
-  if (token0 + lane < a.tokens) a.delta[head * a.tokens + token0 + lane] = mine;
+  return mine;
+}
+template <int L>
+__global__ void __launch_bounds__(256) attn_delta_bf16_kernel(const AttnArgs a) {
+  let_next_start();
+  const int lane = threadIdx.x & 31;
+  const int64_t warp = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), head = warp % a.hq, token0 = warp / a.hq * 32;
+  if (token0 >= a.tokens) return;
+  uint32_t unused = 0;
+  const float delta = delta_of_32<__nv_bfloat16, L, false>(a, (int)head, token0, a.tokens, unused);
+  if (token0 + lane < a.tokens) a.delta[head * a.tokens + token0 + lane] = delta;
+}
+
+// fp16: dS = P (dP - delta) goes back to the tensor cores in a type whose smallest normal value is 2^-14 and whose largest is 65504, while
+// the gradients it comes from may have any size.  So it is held times a power of two, which the output's factor takes back.  The terms of a
+// row are bounded by |dP|, |delta| <= width x (the largest |dout| of the row) x (the largest |v| of the keys that it sees): this kernel leaves
+// both of every 32 rows, and the gradient kernels choose from them (attn_lift), out of one sequence alone, so that no other
+// sequence's values change a rounding.  Where: the two are fp16 values and fit one word, which takes the place of the first row's delta; that
+// delta stands in the first word of the same row of dq, where its reader alone writes, later (a scratch of the call's own would have to be
+// asked for; a kernel of its own for the largest |v| took 4 us longer on 288 tokens).  A warp: 32 rows of one tile and one head, of dout or of v.
+template <int L>
+__global__ void __launch_bounds__(256) attn_delta_f16_kernel(const AttnArgs a) {
+  let_next_start();
+  const int64_t warp = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int heads = a.hq + a.hk;
+  const int64_t quarter = warp / heads;
+  if (quarter >= 4 * (int64_t)a.n_tiles) return;
+  const AttnTile t = a.tiles[quarter >> 2];
+  const int lane = threadIdx.x & 31, head = (int)(warp - quarter * heads), row = t.row + 32 * (int)(quarter & 3);
+  if (row >= t.len) return;
+  const int64_t token0 = (int64_t)t.start + row, end = (int64_t)t.start + t.len;
+  uint32_t top = 0;
+  if (head < a.hq) {
+    const float delta = delta_of_32<__half, L, true>(a, head, token0, end, top);
+    float* at = a.delta + head * a.tokens + token0;
+    const uint16_t most = warp_top(top);
+    if (lane == 0) {
+      reinterpret_cast<uint16_t*>(at)[1] = most;
+      *reinterpret_cast<float*>(row_out<__half>(a.dq, token0, head)) = delta;
+    } else if (token0 + lane < end) {
+      at[lane] = delta;
+    }
+  } else {
+    constexpr int RPS = 32 / L, AT_ONCE = 8;
+    const int kvh = head - a.hq, c = (lane % L) * 8;
+#pragma unroll
+    for (int s0 = 0; s0 < L; s0 += AT_ONCE) {
+      ActPack<__half, 8> v[AT_ONCE];
+#pragma unroll
+      for (int s = 0; s < AT_ONCE; ++s) {
+        const int64_t token = token0 + (s0 + s) * RPS + lane / L;
+        if (token < end && c < a.d) v[s] = load_stream<__half, 8>(row_of<__half>(a.v, token, kvh) + c);
+        else zero(v[s]);
+      }
+#pragma unroll
+      for (int s = 0; s < AT_ONCE; ++s) top = top_of(top, v[s].w);
+    }
+    const uint16_t most = warp_top(top);
+    if (lane == 0) reinterpret_cast<uint16_t*>(a.delta + (int64_t)kvh * (a.hq / a.hk) * a.tokens + token0)[0] = most;
+  }
 }
 
 template <typename T>
@@ -301,16 +365,16 @@ int attn_forward_elem(const fgd_attn_plan* plan, int dtype, const AttnArgs& a, c
   }
 }
 
-int attn_delta(int dtype, bool vectors, const AttnArgs& a, cudaStream_t st) {
-  const int64_t blocks = vectors ? ((a.tokens + 31) / 32 * a.hq + 7) / 8 : (a.tokens * a.hq + 7) / 8;
+int attn_delta(const fgd_attn_plan* plan, int dtype, bool vectors, AttnArgs a, cudaStream_t st) {
+  const bool quarters = vectors && dtype == FGD_F16;
+  a.tiles = plan->q_tiles;
+  a.n_tiles = plan->n_q;
+  const int64_t warps = quarters ? 4 * (int64_t)a.n_tiles * (a.hq + a.hk) : (vectors ? (a.tokens + 31) / 32 : a.tokens) * a.hq, blocks = (warps + 7) / 8;
   if (blocks > 0x7fffffff) return op_fail(FGD_ERR_INVALID_ARG, "fgd_attn_backward: too many rows");
-  auto vec = [&](auto zero) {
-    using T = decltype(zero);
-    if (a.d <= 64) attn_delta_vec_kernel<T, 8><<<(unsigned)blocks, 256, 0, st>>>(a);
-    else attn_delta_vec_kernel<T, 16><<<(unsigned)blocks, 256, 0, st>>>(a);
-  };
-  if (vectors && dtype == FGD_BF16) vec(__nv_bfloat16{});
-  else if (vectors) vec(__half{});
+  if (quarters && a.d <= 64) attn_delta_f16_kernel<8><<<(unsigned)blocks, 256, 0, st>>>(a);
+  else if (quarters) attn_delta_f16_kernel<16><<<(unsigned)blocks, 256, 0, st>>>(a);
+  else if (vectors && a.d <= 64) attn_delta_bf16_kernel<8><<<(unsigned)blocks, 256, 0, st>>>(a);
+  else if (vectors) attn_delta_bf16_kernel<16><<<(unsigned)blocks, 256, 0, st>>>(a);
   else if (dtype == FGD_F32) attn_delta_kernel<float><<<(unsigned)blocks, 256, 0, st>>>(a);
   else if (dtype == FGD_BF16) attn_delta_kernel<__nv_bfloat16><<<(unsigned)blocks, 256, 0, st>>>(a);
   else attn_delta_kernel<__half><<<(unsigned)blocks, 256, 0, st>>>(a);

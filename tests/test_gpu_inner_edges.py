@@ -215,3 +215,59 @@ def test_attention_row_without_a_finite_score(d, dtype):
     assert torch.equal(res[0][0][1:], res[1][0][1:]) and torch.equal(res[0][1][:, 1:], res[1][1][:, 1:])
 
 
+# ------------------------------------------------------------------------------- attention: gradients of any size in fp16
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("power", [-13, 12])
+def test_attention_gradient_scales_with_dout_f16(d, power):
+    """dout times a power of two gives the gradients times that power, but for the rounding of the results: nothing between loses bits to the
+    type's smallest values or runs over its largest.  (dout in steps of 1/8, so that it stays exact; long rows, so that P is small.)"""
+    import paper_2606_22768_b200 as fgd
+    torch = _torch()
+    lens, hq, hk, u = (1900, 200), 4, 2, U["f16"]
+    cu = np.concatenate([[0], np.cumsum(lens)])
+    T = int(cu[-1])
+    q, k = _randn((T, hq, d), "f16", 0), _randn((T, hk, d), "f16", 1)
+    v = _randn((T, hk, d), "f16", 2, 4.0)
+    do = (torch.round(_randn((T, hq, d), "f32", 3) * 8) / 8).clamp(-3.875, 3.875).half()
+    plan = fgd.AttnPlan(cu)
+    o, lse = torch.empty_like(q), torch.empty((hq, T), device="cuda")
+    fgd.fgd_attn_forward(plan, q, k, v, o, lse)
+    f, res = 2.0 ** power, []
+    for g in (do, do * f):
+        delta, dq, dk, dv = torch.empty_like(lse), torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+        fgd.fgd_attn_backward(plan, q, k, v, o, g, lse, delta, dq, dk, dv)
+        res.append((dq, dk, dv))
+    fgd.fgd_attn_status(plan)
+    for n, a, b in zip(("dq", "dk", "dv"), *res):
+        want, b = _np(a) * f, _np(b)
+        inside = np.abs(want) < 65504 * (1 - 4 * u)                       # (a few results are beyond the type)
+        assert inside.mean() > 0.999 and (np.abs(b[~inside]) > 65504 * (1 - 8 * u)).all()
+        _near(b[inside], want[inside], 2.02 * u * np.abs(want[inside]) + (1 + f) * 2.0 ** -25, n)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_gradient_of_small_dout_f16(d):
+    """Gradients of a dout around 2^-13 against 64 bits.  dS is held times a power of two that takes max |dout| max |v| to 2^6 or more, so a term
+    loses at most 2^-25 max |dout| max |v| / 64, below 2^-27 max |dout| here (max |v| < 16); P, held times 2^10, 2^-35."""
+    import paper_2606_22768_b200 as fgd
+    torch = _torch()
+    lens, hq, hk, u = (1200, 70), 4, 2, U["f16"]
+    cu = np.concatenate([[0], np.cumsum(lens)])
+    T = int(cu[-1])
+    q, k, v = (_randn((T, h, d), "f16", i) for i, h in enumerate((hq, hk, hk)))
+    do = _randn((T, hq, d), "f16", 3, 2.0 ** -13)
+    plan = fgd.AttnPlan(cu)
+    o, lse = torch.empty_like(q), torch.empty((hq, T), device="cuda")
+    fgd.fgd_attn_forward(plan, q, k, v, o, lse)
+    delta, dq, dk, dv = torch.empty_like(lse), torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    fgd.fgd_attn_backward(plan, q, k, v, o, do, lse, delta, dq, dk, dv)
+    g, m = O.attention_grad(_np(q), _np(k), _np(v), _np(do), cu, d ** -0.5)
+    n, amax = max(lens), float(do.abs().max())
+    assert float(v.abs().max()) < 16
+    floor = {"dq": n * 2.0 ** -27 * amax * d ** -0.5 * float(k.abs().max()), "dk": 2 * n * 2.0 ** -27 * amax * d ** -0.5 * float(q.abs().max()),
+             "dv": 2 * n * 2.0 ** -35 * amax}
+    fp = F32 * (16 + d / 4 + 8 * d ** -0.5 * float(_np(q).__pow__(2).sum(2).max() * _np(k).__pow__(2).sum(2).max()) ** 0.5)
+    for name, t in (("dq", dq), ("dk", dk), ("dv", dv)):
+        _near(t, g[name], u * np.abs(g[name]) + (2.02 * u + 4 * fp) * m[name] + TINY["f16"] + floor[name], name)
+
+
