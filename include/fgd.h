@@ -343,7 +343,8 @@ typedef enum { FGD_GATE_NONE = 0, FGD_GATE_CHANNEL = 1, FGD_GATE_ELEMENT = 2 } f
  *   n = x_new r_x w_pre, r_x = 1/sqrt(mean(x_new^2) + eps)   (n absent: no norm; n is formed from the
  *                                                      fp32 x_new, before it is rounded to its type)
  * x_new may be x itself.  Gradients (x_new and y as they were stored; dres = gradient of x_new from
- * elsewhere, absent = 0; dn absent: n was not formed):
+ * elsewhere, absent = 0; dn absent: n was not formed or not used, dw_pre, where given, is then zero; gradients of what is absent
+ * are not written):
  *   dx (of x, and of x_new's other readers' sum), dy, dgate, dw_post, dw_pre; dx may be dres itself.
  * Per-channel tensors (w_post, w_pre, a CHANNEL gate and their gradients) are fp32 [workers, width]; activations
  * and an ELEMENT gate are of `dtype`.  Outputs may not overlap anything else.  width <= 16384,

@@ -643,7 +643,7 @@ def fgd_block_norm_workspace(dtype: int, workers: int, rows: int, width: int, de
 def fgd_block_norm_backward(dn, dres, x_new, y, gate, w_post, w_pre, dx, dy, dgate, dw_post, dw_pre, eps: float = 1e-5, res_scale: float = 1.0,
                             workspace=None, stream=None) -> None:
     """Gradients of :func:`fgd_block_norm_forward` from x_new and y as stored; dn is the gradient of n, dres that of x_new from elsewhere
-    (None: zero), dx may be dres.  ``workspace``: a uint8 CUDA tensor of :func:`fgd_block_norm_workspace` bytes (None: allocated here)."""
+    (None: zero; without dn, dw_pre becomes zero), dx may be dres.  ``workspace``: a uint8 CUDA tensor of :func:`fgd_block_norm_workspace` bytes (None: allocated here)."""
     import torch
     first = dn if dn is not None else dres
     dev, T, H, K, kind, gate_type = _norm_shapes(first, gate, w_post, w_pre)

@@ -300,6 +300,7 @@ int run_norm(const fgd_block_norm_args* b, bool backward, int device, void* stre
   if (b->gate_kind < GATE_NONE || b->gate_kind > GATE_FULL) return op_fail(FGD_ERR_INVALID_ARG, "%s: gate_kind %d", who, b->gate_kind);
   const bool y = b->y.p != nullptr, post = b->w_post.p != nullptr, gate = b->gate_kind != GATE_NONE, full = b->gate_kind == GATE_FULL;
   const bool pre = backward ? b->dn.p != nullptr : b->n.p != nullptr;
+  const bool dpre = backward && (pre || b->dw_pre.p != nullptr);      // without dn it is zero
   if (!y && (post || gate)) return op_fail(FGD_ERR_INVALID_ARG, "%s: w_post and gate need a block output y", who);
   // name, matrix, used by this call, required, per channel
   const Named all[] = {
@@ -316,7 +317,7 @@ int run_norm(const fgd_block_norm_args* b, bool backward, int device, void* stre
       {"dy", &b->dy, backward && y, true, false},
       {"dgate", &b->dgate, backward && gate, true, !full},
       {"dw_post", &b->dw_post, backward && post, true, true},
-      {"dw_pre", &b->dw_pre, backward && pre, true, true},
+      {"dw_pre", &b->dw_pre, dpre, true, true},
   };
   const int vec = 16 / bytes;
   bool aligned = b->width % vec == 0;
@@ -350,7 +351,7 @@ int run_norm(const fgd_block_norm_args* b, bool backward, int device, void* stre
   DeviceScope dev(device);
   if (!dev.ok()) return op_fail(FGD_ERR_CUDA, "cannot select device %d", device);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const bool columns = backward && (pre || post || b->gate_kind == GATE_ROW);
+  const bool columns = dpre || (backward && (post || b->gate_kind == GATE_ROW));
   if (T == 0 && !columns) return FGD_OK;
   const Shape s = shape_for((int)b->width, vec, backward);
   NormArgs a = {};
@@ -358,7 +359,7 @@ int run_norm(const fgd_block_norm_args* b, bool backward, int device, void* stre
   a.x = mat(b->x, !backward); a.y = mat(b->y, y); a.gate = mat(b->gate, gate); a.w_post = mat(b->w_post, post); a.w_pre = mat(b->w_pre, pre);
   a.x_new = mat(b->x_new, backward ? pre : (y || b->x_new.p != b->x.p)); a.n = mat(b->n, !backward && pre);
   a.dn = mat(b->dn, backward && pre); a.dres = mat(b->dres, backward); a.dx = mat(b->dx, backward); a.dy = mat(b->dy, backward && y);
-  a.dgate = mat(b->dgate, backward && gate); a.dw_post = mat(b->dw_post, backward && post); a.dw_pre = mat(b->dw_pre, backward && pre);
+  a.dgate = mat(b->dgate, backward && gate); a.dw_post = mat(b->dw_post, backward && post); a.dw_pre = mat(b->dw_pre, dpre);
   a.rows = b->rows; a.last_row = T - 1; a.width = (int)b->width; a.gate_kind = b->gate_kind;
   a.eps = (float)b->eps; a.scale = (float)b->res_scale; a.inv_width = 1.f / (float)b->width;
   if (backward) {

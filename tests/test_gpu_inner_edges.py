@@ -271,3 +271,19 @@ def test_attention_gradient_of_small_dout_f16(d):
         _near(t, g[name], u * np.abs(g[name]) + (2.02 * u + 4 * fp) * m[name] + TINY["f16"] + floor[name], name)
 
 
+# ------------------------------------------------------------------------------- block norm
+@pytest.mark.parametrize("H", [64, 77])
+def test_block_norm_weight_gradient_without_dn(H):
+    """The norm before the next block unused (no dn): its weight's gradient is zero, not what the memory held."""
+    import paper_2606_22768_b200 as fgd
+    torch = _torch()
+    dr, x, y = (_randn((6, H), "bf16", i) for i in range(3))
+    w = torch.ones((2, H), device="cuda")
+    for rows in (6, 0):
+        out = [torch.full((rows, H), 7.0, dtype=x.dtype, device="cuda") for _ in range(2)]
+        dpost, dpre = torch.full((2, H), 7.0, device="cuda"), torch.full((2, H), 7.0, device="cuda")
+        fgd.fgd_block_norm_backward(None, dr[:rows], x[:rows], y[:rows], None, w, w, out[0], out[1], None, dpost, dpre)
+        assert bool((dpre == 0).all())
+        assert torch.equal(out[0], dr[:rows])
+
+
