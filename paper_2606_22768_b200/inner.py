@@ -17,7 +17,7 @@ from typing import Dict, Optional, Tuple
 
 import torch
 
-from . import (ACT8_GROUP, AttnPlan, fgd_act_load8, fgd_act_save8, fgd_attn_backward, fgd_attn_forward, fgd_block_norm_backward, fgd_block_norm_forward,
+from . import (ACT8_GROUP, AttnPlan, fgd_act_load8, fgd_act_save8, fgd_attn_backward, fgd_attn_forward, fgd_attn_status, fgd_block_norm_backward, fgd_block_norm_forward,
                fgd_swiglu8_backward, fgd_swiglu8_forward)
 
 
@@ -255,10 +255,12 @@ class InnerSteps:
         self.m, self.v, self.t = torch.zeros_like(theta), torch.zeros_like(theta), 0
 
     def step(self, tokens, targets, plan: AttnPlan, positions) -> torch.Tensor:
-        """One step on a batch; returns the workers' losses before it."""
+        """One step on a batch; returns the workers' losses before it.  Raises FgdError, with parameters and moments as they were, if a
+        device-side wait of the attention kernels gave up (it waits for the gradients to know)."""
         leaf = self.theta.detach().requires_grad_(True)
         losses = worker_losses(decoder_logits(leaf, tokens, plan, positions, self.cfg), targets)
         losses.sum().backward()      # (the workers share no parameter: every row gets its own worker's gradient)
+        fgd_attn_status(plan)
         with torch.no_grad():
             self.t += 1
             b1, b2 = self.betas

@@ -287,3 +287,34 @@ def test_block_norm_weight_gradient_without_dn(H):
         assert torch.equal(out[0], dr[:rows])
 
 
+# ------------------------------------------------------------------------------- the inner steps
+def test_inner_step_refuses_invalid_gradients():
+    """A device-side wait that gave up leaves invalid gradients: the step raises, and parameters and moments stay as they were."""
+    import paper_2606_22768_b200 as fgd
+    from paper_2606_22768_b200 import inner
+    torch = _torch()
+    K, lens, cfg = 2, [200, 60], inner.DecoderConfig()
+    rows = sum(lens)
+    layout, P = inner.param_layout(cfg)
+    theta = torch.zeros((K, P), device="cuda")
+    inner.init_params(theta, cfg, 1)
+    gen = torch.Generator().manual_seed(2)
+    tokens, targets = (torch.randint(cfg.vocab, (K, rows), generator=gen).cuda() for _ in range(2))
+    positions = torch.cat([torch.arange(n) for n in lens * K]).cuda()
+    plan = fgd.AttnPlan(np.concatenate([[0], np.cumsum(lens * K)]))
+    want = inner.InnerSteps(theta.clone(), cfg)
+    want.step(tokens, targets, plan, positions)
+    steps = inner.InnerSteps(theta.clone(), cfg)
+    fgd.fgd_attn_debug_set(plan, fgd.FGD_DEBUG_SPIN_LIMIT, 4096)
+    fgd.fgd_attn_debug_set(plan, fgd.FGD_DEBUG_SKIP_TILE, 1)
+    with pytest.raises(fgd.FgdError) as e:
+        steps.step(tokens, targets, plan, positions)
+    assert e.value.status == fgd.FGD_ERR_TIMEOUT
+    assert torch.equal(steps.theta, theta) and not bool(steps.m.any()) and not bool(steps.v.any()) and steps.t == 0
+    fgd.fgd_attn_debug_set(plan, fgd.FGD_DEBUG_SPIN_LIMIT, 0)
+    fgd.fgd_attn_debug_set(plan, fgd.FGD_DEBUG_SKIP_TILE, -1)
+    steps.step(tokens, targets, plan, positions)
+    behind = layout["0.attn.pre"][0]      # (the embedding's own gradient is a sum by atomics, torch's, whose bits do not repeat)
+    assert torch.equal(steps.theta[:, behind:], want.theta[:, behind:])
+
+
