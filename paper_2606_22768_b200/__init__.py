@@ -516,8 +516,10 @@ class AttnPlan:
 
 
 def fgd_attn_status(plan: AttnPlan, stream=None) -> None:
-    """Synchronises the stream; raises FgdError(FGD_ERR_TIMEOUT) if a device-side wait of a kernel of this plan gave up."""
-    _op_check(_lib.fgd_attn_status(plan._h, _stream(stream)))
+    """Synchronises the stream (None: the current one of the plan's device); raises FgdError(FGD_ERR_TIMEOUT) if a device-side wait of a
+    kernel of this plan gave up."""
+    import torch
+    _op_check(_lib.fgd_attn_status(plan._h, _stream_on(stream, torch.device("cuda", plan.device))))
 
 
 def fgd_attn_debug_set(plan: AttnPlan, key: int, value: int) -> None:

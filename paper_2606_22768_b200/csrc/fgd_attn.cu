@@ -159,6 +159,7 @@ extern "C" int fgd_attn_debug_set(fgd_attn_plan* plan, int key, int64_t value) {
 extern "C" int fgd_attn_status(fgd_attn_plan* plan, void* stream) {
   if (!plan) return op_fail(FGD_ERR_INVALID_ARG, "fgd_attn_status: NULL plan");
   DeviceScope dev(plan->device);
+  if (!dev.ok()) return op_fail(FGD_ERR_CUDA, "cannot select device %d", plan->device);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   int word = 0;
   cudaError_t e = cudaMemcpyAsync(&word, plan->status, sizeof(int), cudaMemcpyDeviceToHost, st);
