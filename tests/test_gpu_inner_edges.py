@@ -318,3 +318,44 @@ def test_inner_step_refuses_invalid_gradients():
     assert torch.equal(steps.theta[:, behind:], want.theta[:, behind:])
 
 
+@pytest.mark.parametrize("F", [64, 65])
+def test_swiglu8_sigmoid_in_fp32(F):
+    """fp32 activations get an fp32 sigmoid.  Exponential within 2 units, denominator, quotient and two products half a unit each: 2^-21 of the
+    result, whatever the gate's size."""
+    import paper_2606_22768_b200 as fgd
+    torch = _torch()
+    gate = torch.linspace(-86, 86, 40 * F).view(40, F)
+    gu = torch.cat((gate, _randn((40, F), "f32", 1).cpu()), 1).cuda()
+    h, h2 = torch.empty((40, F), device="cuda"), torch.empty((40, F), device="cuda")
+    q, e = torch.empty((40, 2 * F), dtype=torch.int8, device="cuda"), torch.empty((40, 2 * -(-F // 32)), dtype=torch.uint8, device="cuda")
+    fgd.fgd_swiglu8_forward(gu, h, q, e)
+    x = _np(gu)
+    ref = O.swiglu(x[:, :F], x[:, F:])
+    _near(h, ref, 2.0 ** -21 * np.abs(ref), "h")
+    dh, dgu = _randn((40, F), "f32", 2), torch.empty_like(gu)
+    fgd.fgd_swiglu8_backward(dh, q, e, dgu, h2)
+    g8, u8 = O.load8(*O.save8(x[:, :F])), O.load8(*O.save8(x[:, F:]))
+    _, ru = O.swiglu_grad(_np(dh), g8, u8)
+    _near(dgu[:, F:], ru, 2.0 ** -21 * np.abs(ru), "du")
+    ref = O.swiglu(g8, u8)
+    _near(h2, ref, 2.0 ** -21 * np.abs(ref), "h again")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("F", [32, 33])
+def test_swiglu8_forward_of_extreme_gates(F, dtype):
+    """g sigmoid(g) u at the ends: the gate itself above, zero below, an infinite one infinite above and NaN below (inf x 0), NaN stays."""
+    import paper_2606_22768_b200 as fgd
+    torch = _torch()
+    top = torch.finfo(_dt(dtype)).max
+    gate = torch.tensor([float("inf"), float("-inf"), float("nan"), top, -top, top / 8, -top / 8, 0.0, 1e4, -1e4, 130.0, -130.0])
+    gu = torch.ones((len(gate), 2 * F), dtype=_dt(dtype), device="cuda")
+    gu[:, :F] = gate[:, None].to(_dt(dtype)).cuda()
+    h = torch.empty((len(gate), F), dtype=gu.dtype, device="cuda")
+    q, e = torch.empty((len(gate), 2 * F), dtype=torch.int8, device="cuda"), torch.empty((len(gate), 2 * -(-F // 32)), dtype=torch.uint8, device="cuda")
+    fgd.fgd_swiglu8_forward(gu, h, q, e)
+    want = torch.where(gate > 0, gu[:, 0].cpu().float(), torch.where(gate < 0, torch.zeros(()), gate))
+    want[1] = float("nan")
+    assert torch.equal(torch.nan_to_num(h.float().cpu(), nan=-7.0), torch.nan_to_num(want, nan=-7.0)[:, None].expand(-1, F).contiguous())
+
+
