@@ -359,3 +359,33 @@ def test_swiglu8_forward_of_extreme_gates(F, dtype):
     assert torch.equal(torch.nan_to_num(h.float().cpu(), nan=-7.0), torch.nan_to_num(want, nan=-7.0)[:, None].expand(-1, F).contiguous())
 
 
+@pytest.mark.parametrize("dtype,off", [("f32", 1e-4), ("f16", 0.005)])
+def test_decoder_in_other_types(dtype, off):
+    """Loss, logits and gradients of the decoder in fp32 and fp16 against fp64: the logits see the type's roundings alone (a few dozen of 2^-11
+    in fp16; library products and sums in fp32), the gradients also the 8-bit checkpoints, about 1.5 % of the values' norm each."""
+    import paper_2606_22768_b200 as fgd
+    from paper_2606_22768_b200 import inner
+    from .test_gpu_inner_path import _plain_logits
+    torch = _torch()
+    cfg = inner.DecoderConfig(vocab=96, width=128, layers=2, n_q_heads=4, n_kv_heads=2, head_dim=32, ffn=160)
+    lens, K = [70, 1, 130, 33], 2
+    rows = sum(lens)
+    layout, P = inner.param_layout(cfg)
+    theta = torch.zeros((K, P), device="cuda")
+    inner.init_params(theta, cfg, 1)
+    gen = torch.Generator().manual_seed(2)
+    theta += (0.05 * torch.randn(theta.shape, generator=gen)).cuda()
+    tokens, targets = (torch.randint(cfg.vocab, (K, rows), generator=gen).cuda() for _ in range(2))
+    plan = fgd.AttnPlan(np.concatenate([[0], np.cumsum(lens * K)]))
+    positions = torch.cat([torch.arange(n) for n in lens * K]).cuda()
+    leaf, ref = theta.clone().requires_grad_(True), theta.double().requires_grad_(True)
+    logits, want = inner.decoder_logits(leaf, tokens, plan, positions, cfg, _dt(dtype)), _plain_logits(ref, tokens, lens, cfg)
+    inner.worker_losses(logits, targets).sum().backward()
+    loss = -torch.gather(torch.log_softmax(want, -1), 2, targets[:, :, None]).mean((1, 2))
+    loss.sum().backward()
+    fgd.fgd_attn_status(plan)
+    assert float((logits.detach().double() - want.detach()).norm() / want.detach().norm()) < off
+    for name, (at, shape) in layout.items():
+        n = int(np.prod(shape))
+        g, w = leaf.grad[:, at:at + n].double(), ref.grad[:, at:at + n]
+        assert float((g - w).norm() / w.norm()) < 0.08, name
