@@ -100,7 +100,7 @@ extern "C" int fgd_attn_plan_create(fgd_attn_plan** out, int device, int n_seqs,
     all.insert(all.end(), kv.begin(), kv.end());
     all.push_back({0, 0, 0, 0});   // the status word
     fgd_attn_plan* p = new fgd_attn_plan;   // the last allocation that can throw
-    p->device = device; p->tokens = tokens; p->n_seqs = n_seqs;
+    p->device = device; p->tokens = tokens;
     p->n_q = (int)q.size(); p->n_q2 = (int)q2.size(); p->n_kv = (int)kv.size();
     DeviceScope dev(device);
     const size_t bytes = sizeof(AttnTile) * all.size();

@@ -48,7 +48,6 @@ struct AttnArgs {
 struct fgd_attn_plan {
   int device = 0;
   int64_t tokens = 0;
-  int n_seqs = 0;
   int n_q = 0, n_q2 = 0, n_kv = 0;
   fgd::AttnTile* q_tiles = nullptr;    // 128 rows each, by descending row (a row meets the keys before it)
   fgd::AttnTile* q2_tiles = nullptr;   // 256 rows each

@@ -167,7 +167,7 @@ attn_dq_tc_kernel(const AttnArgs a, FastDiv heads, int items, const __grid_const
           ok = wait(raw, n_raw & 1);
           ++n_raw;
           if (!ok) { wait.drain(raw, (n_raw - 1) & 1); break; }
-          zero_rows<DP, 128>(base + (2 * NQ + ik) * TILE, rows, lane);
+          zero_rows<DP>(base + (2 * NQ + ik) * TILE, rows, lane);
           if (elect_one()) mbar_arrive(kb);
         }
         if (!(ok = wait(v_empty + 8 * iv, ((u / SV) & 1) ^ 1))) break;
@@ -376,7 +376,7 @@ attn_dkv_tc_kernel(const AttnArgs a, FastDiv heads, int items, const __grid_cons
       const bool here = wait(raw, n_raw & 1);
       ++n_raw;
       if (!here) { wait.drain(raw, (n_raw - 1) & 1); return false; }
-      zero_rows<DP, 128>(base + number * TILE, rows, lane);
+      zero_rows<DP>(base + number * TILE, rows, lane);
       if (elect_one()) mbar_arrive(bar);
       return true;
     };
@@ -595,7 +595,7 @@ template <int DP, bool BF16>
 int launch(const fgd_attn_plan* plan, AttnArgs a, cudaStream_t st) {
   const char* who = "fgd_attn_backward";
   CUtensorMap mq, mk, mv, mdo;
-  auto map = [&](CUtensorMap* m, const AttnHeads& t, int heads) { return attn_tensor_map(plan->encode_tiled, m, BF16, t, a.tokens, heads, a.d, kAttnRows); };
+  auto map = [&](CUtensorMap* m, const AttnHeads& t, int heads) { return attn_tensor_map(plan->encode_tiled, m, BF16, t, a.tokens, heads, a.d); };
   const int64_t items_kv = (int64_t)plan->n_kv * a.hk, items_q = (int64_t)plan->n_q * a.hq;
   if (items_kv > 0x7fffffff - 1024 || items_q > 0x7fffffff - 1024) return op_fail(FGD_ERR_UNSUPPORTED, "%s: too many tiles", who);
   const int sms = sm_count();

@@ -107,7 +107,6 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, FastDiv per_tile, int i
     for (; ok && walk.valid; walk.next()) {
       const int round = walk.round;
       const FwdItem it = fwd_item(a, pair_heads, walk.t, walk.h);
-      static_assert(kAttnRows == 128, "TMA boxes are 128 rows");
       ok = wait(q_empty, (round & 1) ^ 1);
       if (!ok) break;
       if (elect_one()) {
@@ -134,7 +133,7 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, FastDiv per_tile, int i
             ok = wait(raw, n_raw & 1);
             ++n_raw;
             if (!ok) { wait.drain(raw, (n_raw - 1) & 1); break; }
-            zero_rows<DP, 128>(base + 2 * TILE + s * TILE, rows, lane);
+            zero_rows<DP>(base + 2 * TILE + s * TILE, rows, lane);
             if (elect_one()) mbar_arrive(bar);
           }
         }
@@ -321,8 +320,8 @@ int launch(const fgd_attn_plan* plan, AttnArgs a, cudaStream_t st) {
   const int64_t items = (int64_t)a.n_tiles * per_tile;
   if (items > 0x7fffffff - 1024) return op_fail(FGD_ERR_UNSUPPORTED, "%s: %lld tiles", who, (long long)items);
   CUtensorMap mq, mk, mv;
-  if (!attn_tensor_map(plan->encode_tiled, &mq, BF16, a.q, a.tokens, a.hq, a.d, 128) || !attn_tensor_map(plan->encode_tiled, &mk, BF16, a.k, a.tokens, a.hk, a.d, 128) ||
-      !attn_tensor_map(plan->encode_tiled, &mv, BF16, a.v, a.tokens, a.hk, a.d, 128))
+  if (!attn_tensor_map(plan->encode_tiled, &mq, BF16, a.q, a.tokens, a.hq, a.d) || !attn_tensor_map(plan->encode_tiled, &mk, BF16, a.k, a.tokens, a.hk, a.d) ||
+      !attn_tensor_map(plan->encode_tiled, &mv, BF16, a.v, a.tokens, a.hk, a.d))
     return op_fail(FGD_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed", who);
   auto kern = attn_forward_tc_kernel<DP, BF16>;
   cudaError_t e = allow_smem<attn_forward_tc_kernel<DP, BF16>>(fwd_smem<DP>());

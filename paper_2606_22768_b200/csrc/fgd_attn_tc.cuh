@@ -1,8 +1,8 @@
 // What the tensor-core attention kernels share: bounded waits, TMA loads of head tiles, tensor-memory
 // access, operand descriptors and MMA issue.
 //
-// A tile is 128 (or 64) rows of one head, DP (64 or 128) columns wide, zero-filled beyond the head's width.  In shared memory it
-// is one or two boxes of that many rows x 64 columns, 128 bytes per row, written by TMA with the 128-byte swizzle.  The same
+// A tile is 128 rows of one head, DP (64 or 128) columns wide, zero-filled beyond the head's width.  In shared memory it
+// is one or two boxes of 128 rows x 64 columns, 128 bytes per row, written by TMA with the 128-byte swizzle.  The same
 // box serves the MMAs in both directions: with the columns as the contraction (K-major: scores, dP) and with the
 // rows as the contraction (MN-major: P V, dS K, P^T dO, dS^T Q).
 #ifndef FGD_ATTN_TC_CUH_
@@ -17,6 +17,7 @@
 namespace fgd {
 
 constexpr uint32_t kAttnBox = 128 * 128;           // bytes of a 128 x 64 box of 16-bit values
+static_assert(kAttnRows == 128, "a tile's boxes and MMAs are 128 rows");
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 template <int DP>
@@ -58,18 +59,18 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
       ::"r"(dst), "l"(map), "r"(c), "r"(head), "r"(token), "r"(bar)
       : "memory");
 }
-// One tile of ROWS rows (the map's box height): DP / 64 boxes, issued by one thread.
-template <int DP, int ROWS = 128>
+// One tile: DP / 64 boxes, issued by one thread.
+template <int DP>
 __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, int head, int token, uint32_t bar) {
 #pragma unroll
-  for (int b = 0; b < DP / 64; ++b) tma_load_3d(dst + b * ROWS * 128, map, b * 64, head, token, bar);
+  for (int b = 0; b < DP / 64; ++b) tma_load_3d(dst + b * kAttnBox, map, b * 64, head, token, bar);
 }
-// Rows [first, ROWS) of a tile become zero (a row of a box is 128 contiguous bytes, the swizzle stays inside it), for the
+// Rows [first, 128) of a tile become zero (a row of a box is 128 contiguous bytes, the swizzle stays inside it), for the
 // asynchronous proxy to read.  One warp.
-template <int DP, int ROWS>
+template <int DP>
 __device__ __forceinline__ void zero_rows(unsigned char* tile, int first, int lane) {
   for (int b = 0; b < DP / 64; ++b)
-    for (int i = first * 8 + lane; i < ROWS * 8; i += 32) reinterpret_cast<uint4*>(tile + b * ROWS * 128)[i] = make_uint4(0u, 0u, 0u, 0u);
+    for (int i = first * 8 + lane; i < kAttnRows * 8; i += 32) reinterpret_cast<uint4*>(tile + b * kAttnBox)[i] = make_uint4(0u, 0u, 0u, 0u);
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   __syncwarp();
 }
@@ -150,22 +151,21 @@ __device__ __forceinline__ void umma_f16_ts(uint32_t d, uint32_t a, uint32_t b, 
       ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "n"(kDescHigh)
       : "memory");
 }
-// D[128 x N] = A B^T over the tiles' columns (both K-major): 16 columns per step, 32 bytes inside a swizzled row.  A has 128 rows,
-// B has N (its box height).
-template <bool BF16, int DP, int N = 128>
+// D[128 x 128] = A B^T over the tiles' columns (both K-major): 16 columns per step, 32 bytes inside a swizzled row.
+template <bool BF16, int DP>
 __device__ __forceinline__ void mma_columns(uint32_t d, uint32_t a_tile, uint32_t b_tile) {
   const uint32_t a = uniform(desc_low(a_tile, 16)), b = uniform(desc_low(b_tile, 16)), c = uniform(d);
   if (elect_one()) {
 #pragma unroll
     for (int k = 0; k < DP / 16; ++k)
-      umma_f16_ss(c, a + (((k / 4) * 128 * 128 + (k % 4) * 32) >> 4), b + (((k / 4) * N * 128 + (k % 4) * 32) >> 4), attn_idesc<BF16, N, false>(), k > 0 ? 1u : 0u);
+      umma_f16_ss(c, a + (((k / 4) * 128 * 128 + (k % 4) * 32) >> 4), b + (((k / 4) * 128 * 128 + (k % 4) * 32) >> 4), attn_idesc<BF16, 128, false>(), k > 0 ? 1u : 0u);
   }
 }
-// D[128 x DP] (+)= A B over 64 rows of B (rows [64 half, 64 half + 64) of a tile of ROWS): A's 64 columns are 16-bit values in
+// D[128 x DP] (+)= A B over 64 rows of B (rows [64 half, 64 half + 64) of a tile): A's 64 columns are 16-bit values in
 // tensor memory, packed two to a column, at [a, a + 32); 16 rows of B per step.
-template <bool BF16, int DP, int ROWS = 128>
+template <bool BF16, int DP>
 __device__ __forceinline__ void mma_half_rows(uint32_t d, uint32_t a_cols, uint32_t b_tile, int half, bool accumulate) {
-  const uint32_t a = uniform(a_cols), b = uniform(desc_low(b_tile, ROWS * 128) + half * (64 * 128 >> 4)), c = uniform(d), acc = uniform(accumulate ? 1u : 0u);
+  const uint32_t a = uniform(a_cols), b = uniform(desc_low(b_tile, 128 * 128) + half * (64 * 128 >> 4)), c = uniform(d), acc = uniform(accumulate ? 1u : 0u);
   if (elect_one()) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) umma_f16_ts(c, a + k * 8, b + k * (2048 >> 4), attn_idesc<BF16, DP, true>(), k > 0 ? 1u : acc);
@@ -312,13 +312,13 @@ struct ItemWalk {
 typedef CUresult (*AttnEncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// Tensor map of a [tokens, heads, d] tensor: boxes of 64 columns x 1 head x `rows` tokens; columns beyond d and tokens beyond the
+// Tensor map of a [tokens, heads, d] tensor: boxes of 64 columns x 1 head x 128 tokens; columns beyond d and tokens beyond the
 // last read as zero.
-inline bool attn_tensor_map(void* encode, CUtensorMap* map, bool bf16, const AttnHeads& t, int64_t tokens, int heads, int d, int rows) {
+inline bool attn_tensor_map(void* encode, CUtensorMap* map, bool bf16, const AttnHeads& t, int64_t tokens, int heads, int d) {
   const cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)heads, (cuuint64_t)tokens};
   // the stride of an axis of one is never used, but has to be a valid one
   const cuuint64_t strides[2] = {heads > 1 ? (cuuint64_t)t.head * 2 : (cuuint64_t)d * 2, tokens > 1 ? (cuuint64_t)t.token * 2 : (cuuint64_t)d * 2};
-  const cuuint32_t box[3] = {64, 1, (cuuint32_t)rows}, estr[3] = {1, 1, 1};
+  const cuuint32_t box[3] = {64, 1, (cuuint32_t)kAttnRows}, estr[3] = {1, 1, 1};
   return reinterpret_cast<AttnEncodeFn>(encode)(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, t.p, dims, strides, box, estr,
                                                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                                                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;

@@ -12,7 +12,7 @@ namespace {
 template <typename T, int VEC, int NT, int VPT, int STAGES, bool FULL, bool ANY, bool KEEP>
 __global__ void __launch_bounds__(NT, NT * VPT <= 1024 ? 1024 / NT > 16 ? 16 : 1024 / NT : 1) norm_forward_kernel(const NormArgs a) {
   constexpr bool HOLD = VEC * VPT <= 8;
-  constexpr int P = pairs_of<VEC>;
+  constexpr int P = VEC / 2;
   enum { X, Y, G, N = FULL ? 3 : 2 };
   extern __shared__ __align__(16) unsigned char ring[];
   __shared__ __align__(16) float buf[2][1][NT / 32];
@@ -44,7 +44,7 @@ __global__ void __launch_bounds__(NT, NT * VPT <= 1024 ? 1024 / NT > 16 ? 16 : 1
       for (int j = 0; j < VPT; ++j) {
         const Vals<VEC> y = feed.get(Y, j);
 #pragma unroll
-        for (int i = 0; i < P; ++i) sum = fma2(get2(y, i), get2(y, i), sum);
+        for (int i = 0; i < P; ++i) sum = fma2(y.pair(i), y.pair(i), sum);
       }
       ss[0] = sum.x + sum.y;
       cta_sum<1, NT>(ss, buf, slot); slot ^= 1;
@@ -60,10 +60,10 @@ __global__ void __launch_bounds__(NT, NT * VPT <= 1024 ? 1024 / NT > 16 ? 16 : 1
       if constexpr (FULL) g = feed.get(G, j);
 #pragma unroll
       for (int i = 0; i < P; ++i) {
-        float2 u = mul2(get2(y, i), both(ry));
-        if constexpr (FULL) u = mul2(u, get2(g, i));
-        const float2 x = fma2(u, get2(ftj, i), get2(v[j], i));
-        put2(v[j], i, x);
+        float2 u = mul2(y.pair(i), both(ry));
+        if constexpr (FULL) u = mul2(u, g.pair(i));
+        const float2 x = fma2(u, ftj.pair(i), v[j].pair(i));
+        v[j].set(i, x);
         sum = fma2(x, x, sum);
       }
       if (a.x_new.p) store_vec<T, VEC, ANY>(a.x_new, row, c[j], a.width, v[j]);
@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(NT, NT * VPT <= 1024 ? 1024 / NT > 16 ? 16 : 1
       for (int j = 0; j < VPT; ++j) {
         const Vals<VEC> fnj = fn.get(wn, j);
 #pragma unroll
-        for (int i = 0; i < P; ++i) put2(v[j], i, mul2(mul2(get2(v[j], i), rx), get2(fnj, i)));
+        for (int i = 0; i < P; ++i) v[j].set(i, mul2(mul2(v[j].pair(i), rx), fnj.pair(i)));
         store_vec<T, VEC, ANY>(a.n, row, c[j], a.width, v[j]);
       }
     }
@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(NT, NT * VPT <= 1024 ? 1024 / NT > 16 ? 16 : 1
 template <typename T, int VEC, int NT, int VPT, int STAGES, bool FULL, bool ANY, bool KEEP>
 __global__ void __launch_bounds__(NT, NT <= 512 ? 512 / NT : 1) norm_backward_kernel(const NormArgs a) {
   constexpr bool HOLD = VEC * VPT <= 8;
-  constexpr int P = pairs_of<VEC>;
+  constexpr int P = VEC / 2;
   enum { X, Y, DN, DR, G, N = FULL ? 5 : 4 };
   extern __shared__ __align__(16) unsigned char ring[];
   __shared__ __align__(16) float buf[2][6][NT / 32];
@@ -131,13 +131,13 @@ __global__ void __launch_bounds__(NT, NT <= 512 ? 512 / NT : 1) norm_backward_ke
       if constexpr (FULL) g = feed.get(G, j);
 #pragma unroll
       for (int i = 0; i < P; ++i) {
-        const float2 xv = get2(x, i), yv = get2(y, i), av = mul2(get2(n, i), get2(fnj, i));
-        float2 t0 = mul2(get2(ftj, i), yv);
-        if constexpr (FULL) t0 = mul2(t0, get2(g, i));
+        const float2 xv = x.pair(i), yv = y.pair(i), av = mul2(n.pair(i), fnj.pair(i));
+        float2 t0 = mul2(ftj.pair(i), yv);
+        if constexpr (FULL) t0 = mul2(t0, g.pair(i));
         s2[0] = fma2(xv, xv, s2[0]);
         s2[1] = fma2(yv, yv, s2[1]);
         s2[2] = fma2(av, xv, s2[2]);
-        s2[3] = fma2(t0, get2(d, i), s2[3]);
+        s2[3] = fma2(t0, d.pair(i), s2[3]);
         s2[4] = fma2(t0, av, s2[4]);
         s2[5] = fma2(t0, xv, s2[5]);
       }
@@ -162,14 +162,14 @@ __global__ void __launch_bounds__(NT, NT <= 512 ? 512 / NT : 1) norm_backward_ke
       if constexpr (FULL) g = feed.get(G, j);
 #pragma unroll
       for (int i = 0; i < P; ++i) {
-        const float2 xv = get2(x, i), yv = get2(y, i), nv = get2(n, i), xr = mul2(xv, rx2);
-        put2(acc_pre[j], i, fma2(nv, xr, get2(acc_pre[j], i)));
-        const float2 dX = fma2(mk2, xv, fma2(rx2, mul2(nv, get2(fnj, i)), get2(d, i)));
-        const float2 syh = mul2(yv, sry2), dg = FULL ? mul2(dX, get2(g, i)) : dX;          // syh = s yh
-        put2(ox, i, dX);
-        put2(oy, i, fma2(mr2, yv, mul2(mul2(dg, get2(ftj, i)), ry2)));
-        put2(acc_post[j], i, fma2(dg, syh, get2(acc_post[j], i)));
-        if constexpr (FULL) put2(og, i, mul2(mul2(dX, mul2(yv, ry2)), get2(ftj, i)));      // (ft is s w_post here)
+        const float2 xv = x.pair(i), yv = y.pair(i), nv = n.pair(i), xr = mul2(xv, rx2);
+        acc_pre[j].set(i, fma2(nv, xr, acc_pre[j].pair(i)));
+        const float2 dX = fma2(mk2, xv, fma2(rx2, mul2(nv, fnj.pair(i)), d.pair(i)));
+        const float2 syh = mul2(yv, sry2), dg = FULL ? mul2(dX, g.pair(i)) : dX;          // syh = s yh
+        ox.set(i, dX);
+        oy.set(i, fma2(mr2, yv, mul2(mul2(dg, ftj.pair(i)), ry2)));
+        acc_post[j].set(i, fma2(dg, syh, acc_post[j].pair(i)));
+        if constexpr (FULL) og.set(i, mul2(mul2(dX, mul2(yv, ry2)), ftj.pair(i)));      // (ft is s w_post here)
       }
       store_vec<T, VEC, ANY>(a.dx, row, c[j], a.width, ox);
       if (has_y) store_vec<T, VEC, ANY>(a.dy, row, c[j], a.width, oy);
@@ -342,7 +342,7 @@ int run_norm(const fgd_block_norm_args* b, bool backward, int device, void* stre
     for (const Named& e : all) {
       if (!e.wanted || !e.m->p || e.m == o.m) continue;
       const bool in_place = e.m->p == o.m->p && e.m->ld == o.m->ld && ((o.m == &b->x_new && e.m == &b->x) || (o.m == &b->dx && e.m == &b->dres));
-      if (in_place || (o.m == &b->x && e.m == &b->x_new)) continue;
+      if (in_place) continue;
       const Span so = span_of(o.m->p, o.channel ? b->workers : T, b->width, o.m->ld, o.channel ? 4 : bytes);
       const Span se = span_of(e.m->p, e.channel ? b->workers : T, b->width, e.m->ld, e.channel ? 4 : bytes);
       if (so.overlaps(se)) return op_fail(FGD_ERR_ALIAS, "%s: %s overlaps %s", who, o.name, e.name);

@@ -26,33 +26,25 @@ template <> __device__ __forceinline__ float from_f32<float>(float v) { return v
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
 
-// N consecutive activations as they lie in memory: 16 bytes, or one element on the element-wise paths.  Kept as whole words
-// (as an array of 16-bit values the compiler gives each a register of its own and spends more instructions on taking the
-// words apart and together than on the arithmetic).
+// N consecutive activations as they lie in memory: 16 bytes.  Kept as whole words (as an array of 16-bit values the compiler gives
+// each a register of its own and spends more instructions on taking the words apart and together than on the arithmetic).
 template <typename T, int N>
 struct ActPack {
-  static_assert(sizeof(T) * N == 16 || N == 1, "a 16-byte vector or one element");
-  static constexpr bool kVector = sizeof(T) * N == 16;
-  using Word = std::conditional_t<kVector, uint4, T>;
-  Word w;
+  static_assert(sizeof(T) * N == 16, "a 16-byte vector");
+  uint4 w;
 };
 // Streaming access: activations are read once and written once per call, so they leave L1 alone.
 template <typename T, int N>
 __device__ __forceinline__ ActPack<T, N> load_stream(const T* p) {
-  ActPack<T, N> r;
-  if constexpr (ActPack<T, N>::kVector) r.w = __ldcs(reinterpret_cast<const uint4*>(p));
-  else r.w = *p;
-  return r;
+  return ActPack<T, N>{__ldcs(reinterpret_cast<const uint4*>(p))};
 }
 template <typename T, int N>
 __device__ __forceinline__ void store_stream(T* p, const ActPack<T, N>& r) {
-  if constexpr (ActPack<T, N>::kVector) __stcs(reinterpret_cast<uint4*>(p), r.w);
-  else *p = r.w;
+  __stcs(reinterpret_cast<uint4*>(p), r.w);
 }
 template <typename T, int N>
 __device__ __forceinline__ void zero(ActPack<T, N>& r) {
-  if constexpr (ActPack<T, N>::kVector) r.w = make_uint4(0u, 0u, 0u, 0u);
-  else r.w = from_f32<T>(0.f);
+  r.w = make_uint4(0u, 0u, 0u, 0u);
 }
 
 // Two fp32 operations per instruction.
@@ -79,25 +71,14 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
 }
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 
-// N consecutive values as fp32, handled in pairs where N is even.
+// N consecutive values as fp32, handled in pairs.
 template <int N>
 struct Vals {
+  static_assert(N % 2 == 0, "pairs");
   float v[N];
   __device__ __forceinline__ float2 pair(int i) const { return make_float2(v[2 * i], v[2 * i + 1]); }
   __device__ __forceinline__ void set(int i, float2 p) { v[2 * i] = p.x; v[2 * i + 1] = p.y; }
 };
-// f(pair index, pair) for every pair; an odd single value is handled as a pair with a zero that goes nowhere.
-template <int N> constexpr int pairs_of = (N + 1) / 2;
-template <int N>
-__device__ __forceinline__ float2 get2(const Vals<N>& a, int i) {
-  if constexpr (N % 2 == 0) return a.pair(i);
-  else return make_float2(a.v[i], 0.f);
-}
-template <int N>
-__device__ __forceinline__ void put2(Vals<N>& a, int i, float2 p) {
-  if constexpr (N % 2 == 0) a.set(i, p);
-  else a.v[i] = p.x;
-}
 // Two 16-bit values of a word.
 template <typename T>
 __device__ __forceinline__ float2 halves(uint32_t w) {
@@ -117,9 +98,7 @@ __device__ __forceinline__ uint32_t from_pair(float lo, float hi) {
 template <typename T, int N>
 __device__ __forceinline__ Vals<N> unpack(const ActPack<T, N>& p) {
   Vals<N> r;
-  if constexpr (!ActPack<T, N>::kVector) {
-    r.v[0] = to_f32<T>(p.w);
-  } else if constexpr (sizeof(T) == 4) {
+  if constexpr (sizeof(T) == 4) {
     r.v[0] = __uint_as_float(p.w.x); r.v[1] = __uint_as_float(p.w.y); r.v[2] = __uint_as_float(p.w.z); r.v[3] = __uint_as_float(p.w.w);
   } else {
     r.set(0, halves<T>(p.w.x)); r.set(1, halves<T>(p.w.y)); r.set(2, halves<T>(p.w.z)); r.set(3, halves<T>(p.w.w));
@@ -129,9 +108,7 @@ __device__ __forceinline__ Vals<N> unpack(const ActPack<T, N>& p) {
 template <typename T, int N>
 __device__ __forceinline__ ActPack<T, N> round_to(const Vals<N>& a) {
   ActPack<T, N> r;
-  if constexpr (!ActPack<T, N>::kVector) {
-    r.w = from_f32<T>(a.v[0]);
-  } else if constexpr (sizeof(T) == 4) {
+  if constexpr (sizeof(T) == 4) {
     r.w = make_uint4(__float_as_uint(a.v[0]), __float_as_uint(a.v[1]), __float_as_uint(a.v[2]), __float_as_uint(a.v[3]));
   } else {
     r.w = make_uint4(from_pair<T>(a.v[0], a.v[1]), from_pair<T>(a.v[2], a.v[3]), from_pair<T>(a.v[4], a.v[5]), from_pair<T>(a.v[6], a.v[7]));
