@@ -317,7 +317,7 @@ int fgd_attn_plan_create(fgd_attn_plan** out, int device, int n_seqs, const int6
 int fgd_attn_plan_destroy(fgd_attn_plan* plan);
 /* head_dim <= 256.  bf16 and fp16 with head_dim a multiple of 8 up to 128, 16-byte aligned bases and strides that
  * are multiples of 8 elements run on the tensor cores; everything else on the CUDA cores (slower, not an error).
- * Outputs may not overlap any other tensor. */
+ * Every pointer stands on a boundary of its elements.  Outputs may not overlap any other tensor. */
 int fgd_attn_forward(fgd_attn_plan* plan, const fgd_attn_args* args, void* stream);
 int fgd_attn_backward(fgd_attn_plan* plan, const fgd_attn_args* args, void* stream);
 /* As fgd_device_status, for the kernels that used this plan: synchronises `stream`, reports

@@ -23,8 +23,9 @@ Span heads_span(const fgd_heads& t, int64_t tokens, int heads, int d, int bytes)
   return span_of(t.p, heads, (tokens - 1) * t.token_stride + d, t.head_stride, bytes);
 }
 
-int check_heads(const char* who, const HeadsArg& h, int64_t tokens, int d) {
+int check_heads(const char* who, const HeadsArg& h, int64_t tokens, int d, int bytes) {
   if (!h.t->p) return op_fail(FGD_ERR_INVALID_ARG, "%s: %s is NULL", who, h.name);
+  if (reinterpret_cast<uintptr_t>(h.t->p) % bytes != 0) return op_fail(FGD_ERR_INVALID_ARG, "%s: %s is not on a boundary of its elements", who, h.name);
   const int64_t ts = h.t->token_stride, hs = h.t->head_stride;
   if (ts < 0 || hs < 0) return op_fail(FGD_ERR_INVALID_ARG, "%s: %s has a negative stride", who, h.name);
   if (!h.output) return FGD_OK;
@@ -45,6 +46,7 @@ int check_common(const char* who, const fgd_attn_plan* plan, const fgd_attn_args
   if (b->head_dim > kAttnElemMaxDim) return op_fail(FGD_ERR_UNSUPPORTED, "%s: head_dim %d above %d", who, b->head_dim, kAttnElemMaxDim);
   if (!std::isfinite(b->scale)) return op_fail(FGD_ERR_INVALID_ARG, "%s: scale is not finite", who);
   if (!b->lse && plan->tokens > 0) return op_fail(FGD_ERR_INVALID_ARG, "%s: lse is NULL", who);
+  if (reinterpret_cast<uintptr_t>(b->lse) % sizeof(float) != 0) return op_fail(FGD_ERR_INVALID_ARG, "%s: lse is not on a boundary of its elements", who);
   return FGD_OK;
 }
 
@@ -178,7 +180,7 @@ extern "C" int fgd_attn_forward(fgd_attn_plan* plan, const fgd_attn_args* b, voi
   const HeadsArg all[] = {{"q", &b->q, b->n_q_heads, false}, {"k", &b->k, b->n_kv_heads, false}, {"v", &b->v, b->n_kv_heads, false}, {"o", &b->o, b->n_q_heads, true}};
   const int bytes = dtype_bytes(b->dtype);
   for (const HeadsArg& h : all)
-    if (int rc = check_heads(who, h, plan->tokens, b->head_dim)) return rc;
+    if (int rc = check_heads(who, h, plan->tokens, b->head_dim, bytes)) return rc;
   const Span so = heads_span(b->o, plan->tokens, b->n_q_heads, b->head_dim, bytes), sl = span_of(b->lse, b->n_q_heads, plan->tokens, plan->tokens, 4);
   for (int i = 0; i < 3; ++i) {
     const Span s = heads_span(*all[i].t, plan->tokens, all[i].heads, b->head_dim, bytes);
@@ -198,13 +200,14 @@ extern "C" int fgd_attn_backward(fgd_attn_plan* plan, const fgd_attn_args* b, vo
   if (int rc = check_common(who, plan, b)) return rc;
   if (plan->tokens == 0) return FGD_OK;
   if (!b->delta) return op_fail(FGD_ERR_INVALID_ARG, "%s: delta is NULL", who);
+  if (reinterpret_cast<uintptr_t>(b->delta) % sizeof(float) != 0) return op_fail(FGD_ERR_INVALID_ARG, "%s: delta is not on a boundary of its elements", who);
   const HeadsArg all[] = {{"q", &b->q, b->n_q_heads, false}, {"k", &b->k, b->n_kv_heads, false}, {"v", &b->v, b->n_kv_heads, false},
                           {"o", &b->o, b->n_q_heads, false}, {"dout", &b->dout, b->n_q_heads, false},
                           {"dq", &b->dq, b->n_q_heads, true}, {"dk", &b->dk, b->n_kv_heads, true}, {"dv", &b->dv, b->n_kv_heads, true}};
   const int bytes = dtype_bytes(b->dtype);
   Span spans[10];
   for (int i = 0; i < 8; ++i) {
-    if (int rc = check_heads(who, all[i], plan->tokens, b->head_dim)) return rc;
+    if (int rc = check_heads(who, all[i], plan->tokens, b->head_dim, bytes)) return rc;
     spans[i] = heads_span(*all[i].t, plan->tokens, all[i].heads, b->head_dim, bytes);
   }
   spans[8] = span_of(b->lse, b->n_q_heads, plan->tokens, plan->tokens, 4);

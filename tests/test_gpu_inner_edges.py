@@ -389,3 +389,32 @@ def test_decoder_in_other_types(dtype, off):
         n = int(np.prod(shape))
         g, w = leaf.grad[:, at:at + n].double(), ref.grad[:, at:at + n]
         assert float((g - w).norm() / w.norm()) < 0.08, name
+
+
+# ------------------------------------------------------------------------------- refusals of the C entry points
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_attention_refuses_pointers_between_elements(dtype):
+    """Refused before anything is launched (torch makes no such tensors, so the arguments are packed here)."""
+    import paper_2606_22768_b200 as fgd
+    torch = _torch()
+    T, hq, hk, d = 40, 2, 1, 64
+    plan = fgd.AttnPlan([0, T])
+    q, o, do, dq = (_randn((T, hq, d), dtype, i) for i in range(4))
+    k, v, dk, dv = (_randn((T, hk, d), dtype, 4 + i) for i in range(4))
+    lse, delta = torch.zeros((hq, T), device="cuda"), torch.zeros((hq, T), device="cuda")
+    heads = [(t.data_ptr(), t.stride(0), t.stride(1)) for t in (q, k, v, o, do, dq, dk, dv)]
+    code = {"bf16": fgd.FGD_BF16, "f16": fgd.FGD_F16, "f32": fgd.FGD_F32}[dtype]
+
+    def pack(off):
+        at = [(p + (1 if i == off else 0), s, h) for i, (p, s, h) in enumerate(heads)]
+        return fgd._ATTN_ARGS.pack(code, hq, hk, d, *at[0], *at[1], *at[2], *at[3], lse.data_ptr() + 2 * (off == 8), 0.125, *at[4],
+                                   delta.data_ptr() + 2 * (off == 9), *at[5], *at[6], *at[7])
+
+    for off in range(10):
+        if off in (0, 1, 2, 3, 8):
+            assert fgd._lib.fgd_attn_forward(plan._h, pack(off), None) == fgd.FGD_ERR_INVALID_ARG
+            assert "boundary" in fgd.fgd_last_error(None)
+        assert fgd._lib.fgd_attn_backward(plan._h, pack(off), None) == fgd.FGD_ERR_INVALID_ARG
+        assert "boundary" in fgd.fgd_last_error(None)
+    assert fgd._lib.fgd_attn_forward(plan._h, pack(-1), None) == fgd.FGD_OK
+    fgd.fgd_attn_status(plan)
