@@ -6,7 +6,7 @@ for the backward pass -- as autograd functions; matrix products are plain librar
 workers take their step in one pass: activations are [K * rows, width] with worker m's rows at [m * rows, (m + 1) * rows).
 
 What a block keeps for its backward pass: the residual stream and the block outputs (the norms need them), q, k, v, o and lse, and in
-8 bits the inputs of its projections and of SwiGLU.  The backward passes are not differentiable themselves: create_graph=True is an error
+8 bits the inputs of its projections and of SwiGLU (whose output, the last projection's input, comes from there again).  The backward passes are not differentiable themselves: create_graph=True is an error
 in them.
 """
 from __future__ import annotations
@@ -134,6 +134,34 @@ def linear8(x, w):
     return _Linear8.apply(x, w)
 
 
+class _Swiglu8Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, gu, w):
+        K, rows, width = w.shape[0], gu.shape[0], gu.shape[1] // 2
+        h = torch.empty((rows, width), dtype=gu.dtype, device=gu.device)
+        q8 = torch.empty((rows, 2 * width), dtype=torch.int8, device=gu.device)
+        e8 = torch.empty((rows, 2 * -(-width // ACT8_GROUP)), dtype=torch.uint8, device=gu.device)
+        fgd_swiglu8_forward(gu, h, q8, e8)
+        ctx.save_for_backward(q8, e8, w)
+        return torch.bmm(h.view(K, -1, width), w.transpose(1, 2)).view(rows, w.shape[1])
+
+    @staticmethod
+    @_first_order
+    def backward(ctx, dy):
+        q8, e8, w = ctx.saved_tensors
+        K, rows, width = w.shape[0], q8.shape[0], w.shape[2]
+        dy = dy.contiguous().view(K, -1, w.shape[1])
+        dgu, h = torch.empty(q8.shape, dtype=dy.dtype, device=dy.device), torch.empty((rows, width), dtype=dy.dtype, device=dy.device)
+        fgd_swiglu8_backward(torch.bmm(dy, w).view(rows, width), q8, e8, dgu, h)
+        return dgu, torch.bmm(dy.transpose(1, 2), h.view(K, -1, width))
+
+
+def swiglu8_linear(gu, w):
+    """Per worker (silu(g) * u) w^T of gu = [g | u]: gu [K * rows, 2 in], w [K, out, in]; keeps g and u in 8 bits and nothing else: the gradient
+    of w takes the product that the backward pass forms again from them."""
+    return _Swiglu8Linear.apply(gu, w)
+
+
 # ------------------------------------------------------------------------------- decoder
 @dataclass(frozen=True)
 class DecoderConfig:
@@ -233,7 +261,7 @@ def decoder_logits(theta: torch.Tensor, tokens: torch.Tensor, plan: AttnPlan, po
         o = attention(q, k, qkv[:, hq + hk:], plan)
         y = linear8(o.view(T, hq * d), mat(f"{i}.out"))
         x, n = block_norm(x, y, vec(f"{i}.attn.gate"), vec(f"{i}.attn.post"), vec(f"{i}.mlp.pre"), cfg.eps, cfg.res_scale)
-        y = linear8(swiglu8(linear8(n, mat(f"{i}.up"))), mat(f"{i}.down"))
+        y = swiglu8_linear(linear8(n, mat(f"{i}.up")), mat(f"{i}.down"))
         after = vec(f"{i + 1}.attn.pre") if i + 1 < cfg.layers else vec("final")
         x, n = block_norm(x, y, vec(f"{i}.mlp.gate"), vec(f"{i}.mlp.post"), after, cfg.eps, cfg.res_scale)
     return linear8(n, mat("head")).view(K, rows, cfg.vocab)

@@ -418,3 +418,31 @@ def test_attention_refuses_pointers_between_elements(dtype):
         assert "boundary" in fgd.fgd_last_error(None)
     assert fgd._lib.fgd_attn_forward(plan._h, pack(-1), None) == fgd.FGD_OK
     fgd.fgd_attn_status(plan)
+
+
+# ------------------------------------------------------------------------------- what a block keeps
+def test_swiglu8_linear():
+    """Output and gradients of the fused pair, and that beside the weights only the checkpoint of g and u is kept: 2 bytes and a little per element
+    of the hidden width.  The gradients are those at the checkpointed values, with one rounding of each factor: u of every term."""
+    from paper_2606_22768_b200 import inner
+    torch = _torch()
+    K, R, F, N, u = 2, 40, 96, 48, U["bf16"]
+    gu, w, dy = _randn((K * R, 2 * F), "bf16", 0), _randn((K, N, F), "bf16", 1, F ** -0.5), _randn((K * R, N), "bf16", 2)
+    gu.requires_grad_(True), w.requires_grad_(True)
+    kept = []
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: kept.append(t) or t, lambda t: t):
+        y = inner.swiglu8_linear(gu, w)
+    assert sum(t.numel() * t.element_size() for t in kept if t is not w and t.data_ptr() != w.data_ptr()) == K * R * 2 * (F + F // 32)
+    y.backward(dy)
+    x, wd, dyd = _np(gu), _np(w), _np(dy).reshape(K, R, N)
+    h = O.swiglu(x[:, :F], x[:, F:]).reshape(K, R, F)
+    ref, mag = h @ wd.transpose(0, 2, 1), np.abs(h) @ np.abs(wd).transpose(0, 2, 1)
+    _near(y, ref.reshape(-1, N), u * np.abs(ref.reshape(-1, N)) + 1.1 * u * mag.reshape(-1, N), "y")
+    g8, u8 = O.load8(*O.save8(x[:, :F])), O.load8(*O.save8(x[:, F:]))
+    h8 = O.swiglu(g8, u8).reshape(K, R, F)
+    ref, mag = dyd.transpose(0, 2, 1) @ h8, np.abs(dyd).transpose(0, 2, 1) @ np.abs(h8)
+    _near(w.grad, ref, u * np.abs(ref) + 1.1 * u * mag, "dw")
+    dh, dh_mag = (dyd @ wd).reshape(-1, F), (np.abs(dyd) @ np.abs(wd)).reshape(-1, F)
+    rg, ru = O.swiglu_grad(dh, g8, u8)
+    mg, mu = O.swiglu_grad(dh_mag, g8, u8)
+    _near(gu.grad, np.hstack([rg, ru]), u * np.abs(np.hstack([rg, ru])) + 1.1 * u * np.abs(np.hstack([mg, mu])), "dgu")
