@@ -9,8 +9,9 @@
 // rows through shared memory, one row per lane for the scores, one column per lane and 32-column step for the
 // products.  The softmax runs over the key tiles with a running maximum and sum; the gradient recomputes P from lse.
 // Only unmasked pairs enter a product, so what stands in masked places never reaches a result.
-// Bound by fp32 FMAs and the shared-memory loads that feed them, one load for two FMAs: 16384 tokens, 16 heads of 128 over 4, forward
-// 155 ms, where the tensor cores take 0.97.  delta has kernels of its own for 16-byte rows (8 elements a lane, several rows to a warp;
+// Bound by the shared-memory loads that feed the fp32 FMAs: a score's dot product takes two for one, the products with P and dS one for one,
+// so the FMA units run at about a tenth of their rate: 16384 tokens, 16 heads of 128 over 4, forward 155 ms, where the tensor cores take
+// 0.97; 4 x 1024 tokens of the same in fp32 forward 2.9 ms, forward + backward 12.9.  delta has kernels of its own for 16-byte rows (8 elements a lane, several rows to a warp;
 // 14.6 us for 8192 tokens of 16 x 128, 4.6 TB/s).
 #include "fgd_attn.h"
 #include "fgd_dtype.cuh"
@@ -133,16 +134,19 @@ __global__ void __launch_bounds__(256) attn_delta_kernel(const AttnArgs a) {
 }
 
 // The same for 16-bit values in 16-byte vectors: L lanes take a row, a warp 32 tokens of one head (so that its 32 results are one
-// store), eight rows' loads per lane on their way at a time.  -> delta of token0 + lane, and, where TOP asks for it, the largest
-// magnitude of dout that this lane has met, as fp16 bits; tokens at or beyond `end` count as zero.
-__device__ __forceinline__ uint32_t top_of(uint32_t top, uint4 w) {      // of pairs of fp16 magnitudes, which order as integers do
-  top = __vmaxu2(__vmaxu2(top, w.x & 0x7FFF7FFFu), w.y & 0x7FFF7FFFu);
-  return __vmaxu2(__vmaxu2(top, w.z & 0x7FFF7FFFu), w.w & 0x7FFF7FFFu);
+// store), eight rows' loads per lane on their way at a time.  -> delta of token0 + lane, and, where TOP asks for it, the largest finite
+// magnitudes of dout that this lane has met, of a word's low and high halves; tokens at or beyond `end` count as zero.
+__device__ __forceinline__ __half2 top_of(__half2 top, uint32_t w) {
+  const __half2 x = __habs2(*reinterpret_cast<const __half2*>(&w));
+  return __hmax2(top, __hfma2(x, __float2half2_rn(0.f), x));      // x 0 + x: NaN where x is not finite, and the maximum passes a NaN over
 }
-// of a warp; infinities and NaN count as the largest finite value
-__device__ __forceinline__ uint16_t warp_top(uint32_t top) { return (uint16_t)min(__reduce_max_sync(0xffffffffu, max(top >> 16, top & 0xFFFFu)), 0x7BFFu); }
+__device__ __forceinline__ __half2 top_of(__half2 top, uint4 w) { return top_of(top_of(top_of(top_of(top, w.x), w.y), w.z), w.w); }
+// of a warp, as bits
+__device__ __forceinline__ uint16_t warp_top(__half2 top) {
+  return (uint16_t)__reduce_max_sync(0xffffffffu, (uint32_t)__half_as_ushort(__hmax(__low2half(top), __high2half(top))));
+}
 template <typename T, int L, bool TOP>
-__device__ __forceinline__ float delta_of_32(const AttnArgs& a, int head, int64_t token0, int64_t end, uint32_t& top) {
+__device__ __forceinline__ float delta_of_32(const AttnArgs& a, int head, int64_t token0, int64_t end, __half2& top) {
   constexpr int RPS = 32 / L, AT_ONCE = 8;                 // rows per step of the warp, steps at a time
   const int lane = threadIdx.x & 31, sub = lane / L, c = (lane % L) * 8;
   float mine = 0.f;
@@ -182,7 +186,7 @@ __global__ void __launch_bounds__(256) attn_delta_bf16_kernel(const AttnArgs a) 
   const int lane = threadIdx.x & 31;
   const int64_t warp = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), head = warp % a.hq, token0 = warp / a.hq * 32;
   if (token0 >= a.tokens) return;
-  uint32_t unused = 0;
+  __half2 unused{};
   const float delta = delta_of_32<__nv_bfloat16, L, false>(a, (int)head, token0, a.tokens, unused);
   if (token0 + lane < a.tokens) a.delta[head * a.tokens + token0 + lane] = delta;
 }
@@ -190,7 +194,7 @@ __global__ void __launch_bounds__(256) attn_delta_bf16_kernel(const AttnArgs a) 
 // fp16: dS = P (dP - delta) goes back to the tensor cores in a type whose smallest normal value is 2^-14 and whose largest is 65504, while
 // the gradients it comes from may have any size.  So it is held times a power of two, which the output's factor takes back.  The terms of a
 // row are bounded by |dP|, |delta| <= width x (the largest |dout| of the row) x (the largest |v| of the keys that it sees): this kernel leaves
-// both of every 32 rows, and the gradient kernels choose from them (attn_lift), out of one sequence alone, so that no other
+// both of every 32 rows (the largest finite ones: what is not finite makes its own terms so, and has no say in the others), and the gradient kernels choose from them (attn_lift), out of one sequence alone, so that no other
 // sequence's values change a rounding.  Where: the two are fp16 values and fit one word, which takes the place of the first row's delta; that
 // delta stands in the first word of the same row of dq, where its reader alone writes, later (a scratch of the call's own would have to be
 // asked for; a kernel of its own for the largest |v| took 4 us longer on 288 tokens).  A warp: 32 rows of one tile and one head, of dout or of v.
@@ -205,7 +209,7 @@ __global__ void __launch_bounds__(256) attn_delta_f16_kernel(const AttnArgs a) {
   const int lane = threadIdx.x & 31, head = (int)(warp - quarter * heads), row = t.row + 32 * (int)(quarter & 3);
   if (row >= t.len) return;
   const int64_t token0 = (int64_t)t.start + row, end = (int64_t)t.start + t.len;
-  uint32_t top = 0;
+  __half2 top = __float2half2_rn(0.f);
   if (head < a.hq) {
     const float delta = delta_of_32<__half, L, true>(a, head, token0, end, top);
     float* at = a.delta + head * a.tokens + token0;

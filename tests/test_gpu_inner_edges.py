@@ -446,3 +446,28 @@ def test_swiglu8_linear():
     rg, ru = O.swiglu_grad(dh, g8, u8)
     mg, mu = O.swiglu_grad(dh_mag, g8, u8)
     _near(gu.grad, np.hstack([rg, ru]), u * np.abs(np.hstack([rg, ru])) + 1.1 * u * np.abs(np.hstack([mg, mu])), "dgu")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bad", ["inf", "nan"])
+def test_attention_gradient_beside_a_non_finite_dout_f16(d, bad):
+    """A row whose dout is not finite has no say in how the factors of others are held: rows beside it, and keys that it does not see, get the
+    bits that they get with zeros there."""
+    import paper_2606_22768_b200 as fgd
+    torch = _torch()
+    T, hq, hk, at = 300, 4, 2, 290
+    q, k, v = (_randn((T, h, d), "f16", i) for i, h in enumerate((hq, hk, hk)))
+    do = _randn((T, hq, d), "f16", 3, 2.0 ** -13)
+    plan = fgd.AttnPlan([0, T])
+    o, lse = torch.empty_like(q), torch.empty((hq, T), device="cuda")
+    fgd.fgd_attn_forward(plan, q, k, v, o, lse)
+    res = []
+    for value in (0.0, float(bad)):
+        do[at] = value
+        delta, dq, dk, dv = torch.empty_like(lse), torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+        fgd.fgd_attn_backward(plan, q, k, v, o, do, lse, delta, dq, dk, dv)
+        res.append((dq, dk))
+    (dq0, dk0), (dq1, dk1) = res
+    assert torch.equal(dq0[:at], dq1[:at]) and torch.equal(dq0[at + 1:], dq1[at + 1:])
+    assert torch.equal(dk0[at + 1:], dk1[at + 1:])
+    assert not bool(torch.isfinite(dq1[at]).any())
