@@ -289,9 +289,14 @@ typedef struct {
  *   S_ij = scale q_i . k_j for the keys j <= i of the same sequence,  P = softmax_j(S),
  *   o_i = sum_j P_ij v_j,   lse_i = log sum_j exp(S_ij)
  * n_q_heads is a multiple of n_kv_heads; query head h reads key head h / (n_q_heads / n_kv_heads).
- * What stands in another sequence's rows (infinities, NaN) never reaches a result; inside a sequence a
- * query sees no score of a later key, but a non-finite v of a later row of the same 128-row
- * block can reach it (0 x inf), on the tensor-core path. */
+ * What stands in another sequence's rows (infinities, NaN) never reaches a result.  Inside a sequence a
+ * query sees no score of a later key and no finite v of one; on the tensor-core path a non-finite v of a later row of the
+ * same 128-row block can reach it (0 x inf), and in the gradients a non-finite k of a later row dq, a non-finite q or
+ * dout of an earlier one dk and dv.  A NaN score makes its row NaN, o and lse; a score of -inf has no weight, and a row
+ * without any other is NaN.
+ * On the tensor cores P and dS are rounded to the activations' type as factors of their products, in fp16 times a power of two of their
+ * own (so dout may be of any size); delta is formed from o as it was stored.  o is then off by about 1.25, the gradients
+ * by 1.5 times what rounding them alone costs. */
 typedef struct {
   int32_t dtype; /* fgd_dtype of every fgd_heads tensor */
   int32_t n_q_heads, n_kv_heads, head_dim;

@@ -13,8 +13,8 @@
 // checkpoint (g^, u^), never g and u:
 //     sg = 1 / (1 + exp(-g^)),  du = dh g^ sg,  dg = dh u^ sg (1 + g^ (1 - sg)),  h = g^ sg u^ (again).
 //
-// All four are bound by HBM: one pass, every byte read or written once.  Measured, of the copy peak, bf16: save 94 %, load 89 % (32768 x
-// 4096: 65 and 69 us), SwiGLU forward 86 %, backward 94 % (16384 x 5632: 131 and 150 us); fp32 save 95, load 86.
+// All four are bound by HBM: one pass, every byte read or written once.  Measured, of the copy peak, bf16: save 96 %, load 90 % (32768 x
+// 4096: 65 and 69 us), SwiGLU forward 88 %, backward 98 % (16384 x 5632: 130 and 144 us); fp32 save 95, load 85, SwiGLU 99 and 92 to 95.
 //
 // Vector kernels (rows and bases on 16-byte boundaries, width a multiple of 16 or 8): a thread takes 16 or 8
 // consecutive values, two or four neighbouring lanes make a group, so the group's largest magnitude is one or two

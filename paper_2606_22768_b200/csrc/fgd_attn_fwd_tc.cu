@@ -21,9 +21,11 @@
 // What bounds it: a tile's own chain, S (512 clocks at width 128) -> softmax (about 1850: 128 columns from tensor memory, maximum,
 // exponentials, P back) -> P V (512) with a hop of 300 to 450 clocks between units, since P lies over S and the next S has to wait
 // for P V.  Two tiles side by side hide half of it: 58 % of the tensor pipe's and 56 % of the exponential units' cycles are busy
-// (8192 tokens, 16 heads of 128 over 4: 243 us, 1.13 PFLOP/s).  16384 tokens: 830 us from a cool device, 965 under load, 70 % of the
-// measured matrix peak.  A tile's end (last P V, output, next item's first P) costs about 3800 clocks, which is what short sequences
-// pay: 9 sequences of 1 to 2011 tokens 67 us, 41 %.
+// (8192 tokens, 16 heads of 128 over 4: 243 us, 1.13 PFLOP/s).  16384 tokens: 971 us, 70 % of the measured matrix peak (83 % of what it
+// sustains).  Sequences of different lengths, 9 of 1 to 2011 tokens, 67 us, 41 %: beside the chain, the fixed back-and-forth walk over the
+// items gives the fullest CTA 17 % more than the mean (longest first to whoever is free: 5 %), and a tile's end (last P V, output, next
+// item's first P) costs about 3800 clocks, 7 us for 3.7 items.
+// 168 registers a thread at 320 threads; 78 bytes spilt, in every instance.
 // Slower: two threads per row (maxima traded through shared memory; 1025 us at 16384 tokens), the next item's first S before the other
 // tile's last P V, outputs held back until after the
 // next item's first P; for widths to 64, four query tiles and blocks of 64 keys (16 x 1024, 16 heads of 64: 96 against 80 us).

@@ -20,8 +20,10 @@
 // per-channel gate are column sums: every CTA keeps its own in registers over its rows and writes them
 // once, and a second kernel adds the CTAs up in a fixed order (no atomics: bit-identical from run to run).
 // Rows off their 16-byte boundaries go the same way in shifted chunks (fgd_shift.cuh).
-// Measured, % of the copy peak at work's own bytes (8 workers, gate per channel, bf16): forward 79 at 2048 columns, 88 at 4096, 74 at
-// 8192; backward 86, 88, 82; fp32 82 to 90 and 94, 94, 82.
+// Measured, % of the copy peak at the activations' and weights' own bytes (8 workers, gate per channel, 2^26 elements a tensor in bf16, 2^25
+// in fp32): forward bf16 80 at 2048 columns, 90 at 4096, 69 at 8192, 59 at 16384, backward 86, 86, 79, 40; fp32 82, 90, 72, 63 and 93, 93, 82, 37.
+// Some instances spill, bytes a thread: fp32 above 8192 columns 36 to 832, 16-bit backward above 8192 204 to 432, and off the boundaries above
+// 2048 columns 176 to 492.
 // The workers' rows never share a CTA's sums: each of the K workers has CTAs of its own.
 #ifndef FGD_BLOCK_NORM_CUH_
 #define FGD_BLOCK_NORM_CUH_
@@ -120,8 +122,8 @@ struct RowFeed {
   int width, stage;
   int64_t last;               // the tensors' last row
   uint32_t shift[ANY ? N : 1];
-  // The current row in registers: shifted once, read twice (ANY), or read once from the ring (backward: 8 x 4096 x 2048 bf16 150 us
-  // from the ring twice, 143 so; with a gate per element, N = 5, 178 against 183, and forward 103 against 105: from the ring).
+  // The current row in registers: shifted once, read twice (ANY), or read once from the ring (backward, two sets of inputs in turn: 8 x 4096 x
+  // 2048 bf16 150 us from the ring twice, 144 so; with a gate per element, N = 5, 178 against 183, and forward 103 against 105: from the ring).
   static constexpr bool HELD = STAGES == 0 || (ANY && VPT <= 2) || (N == 4 && VPT == 1);
   ActPack<T, VEC> cur[HELD ? N : 1][HELD ? VPT : 1];
 

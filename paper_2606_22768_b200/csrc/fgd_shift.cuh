@@ -4,8 +4,8 @@
 // behind a 16-byte boundary.  Reading, a lane fetches the chunks from that boundary on, gets the one after its last from the next
 // lane, and takes its unit out of the two with funnel shifts; writing, it takes the end of the unit before its own from the
 // previous lane.  Only where a row, or the warp's part of it, begins or ends inside a chunk are fewer than 16 bytes written.
-// What it gave against one element per lane and access, in % of the copy peak at odd widths, bf16: 8-bit save + load 16 to 40, SwiGLU
-// 28 to 42, block norm forward 14 to 42 (1001 columns) and 33 (5003), backward 9 to 34 and 23.  What is left is the shifting itself
+// What it gave against one element per lane and access, in % of the copy peak at odd widths, bf16: 8-bit save + load 16 to 50 (777 columns),
+// SwiGLU 28 to 46, block norm forward 14 to 42 (1001 columns) and 33 (5003), backward 9 to 34 and 23.  What is left is the shifting itself
 // and the cut chunks, not memory: 16-byte aligned rows reach 67 to 90.
 // Bytes around a row are read with it, but none outside [lo, hi), the tensor; only the unit's own are ever written.
 #ifndef FGD_SHIFT_CUH_
