@@ -606,8 +606,8 @@ def _norm_shapes(first, gate, w_post, w_pre):
         raise ValueError("activations must be [tokens, width]")
     dev, (T, H) = _device_of(first, "activations"), first.shape
     channel = w_pre if w_pre is not None else w_post
-    if channel is None and gate is not None and gate.dtype == torch.float32 and gate.shape != first.shape:
-        channel = gate
+    if channel is None and gate is not None and gate.dtype == torch.float32 and (gate.shape != first.shape or first.dtype != torch.float32):
+        channel = gate      # (of 16-bit activations an fp32 gate is always one per channel)
     K = 1 if channel is None else channel.shape[0]
     if K < 1 or T % K != 0:
         raise ValueError(f"{T} rows do not split over {K} workers")

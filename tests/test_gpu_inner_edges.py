@@ -8,7 +8,7 @@ import pytest
 
 from oracle import inner as O
 
-from .test_gpu_inner_ops import F32, TINY, U, _dt, _matrix, _near, _np, _randn, _torch
+from .test_gpu_inner_ops import F32, TINY, U, _dt, _near, _norm_case, _np, _randn, _torch
 
 pytestmark = pytest.mark.gpu
 
@@ -471,3 +471,11 @@ def test_attention_gradient_beside_a_non_finite_dout_f16(d, bad):
     assert torch.equal(dq0[:at], dq1[:at]) and torch.equal(dq0[at + 1:], dq1[at + 1:])
     assert torch.equal(dk0[at + 1:], dk1[at + 1:])
     assert not bool(torch.isfinite(dq1[at]).any())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("K", [1, 2, 8])
+def test_block_norm_channel_gate_alone_with_one_row_per_worker(K, dtype):
+    """A gate per channel says how many workers there are, also where each has a single row and no norm has weights."""
+    _norm_case(K, 1, 33, dtype, "channel", post=False, pre=False)
+    _norm_case(K, 3, 33, dtype, "channel", post=False, pre=False)
