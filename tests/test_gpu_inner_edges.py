@@ -479,3 +479,56 @@ def test_block_norm_channel_gate_alone_with_one_row_per_worker(K, dtype):
     """A gate per channel says how many workers there are, also where each has a single row and no norm has weights."""
     _norm_case(K, 1, 33, dtype, "channel", post=False, pre=False)
     _norm_case(K, 3, 33, dtype, "channel", post=False, pre=False)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_f16_gradient_on_streams_in_graphs_and_after_a_timeout(d):
+    """The fp16 gradient hands values on in rows of dq that are not written yet: the same bits on another stream, from a replayed graph, with two
+    plans' calls in flight at once, and by a plan whose wait ran out before."""
+    import paper_2606_22768_b200 as fgd
+    torch = _torch()
+    cu, T, hq, hk = [0, 700, 900], 900, 4, 2
+    q, k, v, do = (_randn((T, h, d), "f16", i) for i, h in enumerate((hq, hk, hk, hq)))
+    plan, other = fgd.AttnPlan(cu), fgd.AttnPlan(cu)
+    o, lse = torch.empty_like(q), torch.empty((hq, T), device="cuda")
+    fgd.fgd_attn_forward(plan, q, k, v, o, lse)
+
+    def outputs():
+        return [torch.full_like(t, 7.0) for t in (lse, q, k, v)]
+
+    def back(p, out, stream=None):
+        fgd.fgd_attn_backward(p, q, k, v, o, do, lse, *out, stream=stream)
+
+    want = outputs()
+    back(plan, want)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = [outputs() for _ in range(6)]
+    torch.cuda.synchronize()
+    for i, out in enumerate(got):
+        back((plan, other)[i % 2], out, side if i % 3 == 0 else None)
+    torch.cuda.synchronize()
+    g, out = torch.cuda.CUDAGraph(), outputs()
+    with torch.cuda.graph(g):
+        back(plan, out)
+        back(plan, out)
+    for t in out:
+        t.fill_(-1)
+    g.replay()
+    g.replay()
+    torch.cuda.synchronize()
+    fgd.fgd_attn_debug_set(other, fgd.FGD_DEBUG_SPIN_LIMIT, 4096)
+    fgd.fgd_attn_debug_set(other, fgd.FGD_DEBUG_SKIP_TILE, 1)
+    back(other, outputs())
+    with pytest.raises(fgd.FgdError) as e:
+        fgd.fgd_attn_status(other)
+    assert e.value.status == fgd.FGD_ERR_TIMEOUT
+    fgd.fgd_attn_debug_set(other, fgd.FGD_DEBUG_SPIN_LIMIT, 0)
+    fgd.fgd_attn_debug_set(other, fgd.FGD_DEBUG_SKIP_TILE, -1)
+    after = outputs()
+    back(other, after)
+    fgd.fgd_attn_status(other)
+    fgd.fgd_attn_status(plan)
+    for res in got + [out, after]:
+        for a, b in zip(want[1:], res[1:]):
+            assert torch.equal(a, b)
