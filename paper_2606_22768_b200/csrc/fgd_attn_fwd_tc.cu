@@ -11,7 +11,8 @@
 // O += P V and its next S run on the tensor cores.
 //
 // The running maximum only moves O when it has grown by more than 2^8 since O was last scaled: P and the row sum use the
-// same stale maximum, so the quotient is exact, and the 16-bit P keeps its relative precision below 2^8 too.
+// same stale maximum, so the quotient is exact, and the 16-bit P keeps its relative precision below 2^8 too.  In fp16 P is held times 2^7, at most
+// 2^15, so that weights keep it down to 2^-21 of the largest; the sum has the factor too, and lse takes it back.
 // Only the block on the diagonal is masked; rows of V beyond the sequence's end are zeroed in shared memory, so nothing of the
 // next sequence (0 x inf) reaches a result.
 //
@@ -38,6 +39,7 @@ namespace {
 constexpr int kFwdThreads = 320;
 template <int DP> constexpr int kFwdStages = DP == 128 ? 4 : 8;
 constexpr float kRescale = 8.f;   // log2
+template <bool BF16> constexpr float kLift = BF16 ? 0.f : 7.f;   // log2 of P's factor
 
 template <int DP>
 constexpr size_t fwd_smem() { return 1024 + (size_t)(2 + kFwdStages<DP>) * attn_tile_bytes<DP>() + 8 * kStoreStage; }
@@ -268,7 +270,7 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, FastDiv per_tile, int i
           m = mn;
         }
         // p = 2^(c s - m), 32 columns at a time
-        const float2 c2 = make_float2(c, c), m2 = make_float2(-m, -m);
+        const float2 c2 = both(c), m2 = both(kLift<BF16> - m);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           uint32_t p[16];
@@ -301,7 +303,7 @@ attn_forward_tc_kernel(const AttnArgs a, int pair_heads, FastDiv per_tile, int i
       }
       tc_fence_before();
       mbar_arrive(o_free + 8 * t);
-      if (row0 + lane < it.len) a.lse[it.head[t] * a.tokens + it.start + row0 + lane] = (m + log2f(sum)) * kLn2;
+      if (row0 + lane < it.len) a.lse[it.head[t] * a.tokens + it.start + row0 + lane] = (m + (log2f(sum) - kLift<BF16>)) * kLn2;
     }
   }
   tc_fence_before();

@@ -532,3 +532,25 @@ def test_attention_f16_gradient_on_streams_in_graphs_and_after_a_timeout(d):
     for res in got + [out, after]:
         for a, b in zip(want[1:], res[1:]):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_small_weights_f16(d):
+    """Weights down to 2^-21 of the largest keep the type's relative precision: pairs of tokens whose second one gives the first, with a large v, a
+    weight from 1/2 to e^-14."""
+    import paper_2606_22768_b200 as fgd
+    torch = _torch()
+    n, u = 300, U["f16"]
+    q, k, v = torch.zeros((2 * n, 2, d)), torch.zeros((2 * n, 1, d)), _randn((2 * n, 1, d), "f32", 0).cpu() * 1000
+    q[..., 0] = 1.0
+    k[0::2, 0, 0] = -torch.linspace(0, 14, n)
+    v[1::2] = 0
+    q, k, v = (t.half().cuda() for t in (q, k, v))
+    cu = list(range(0, 2 * n + 1, 2))
+    plan = fgd.AttnPlan(cu)
+    o, lse = torch.empty_like(q), torch.empty((2, 2 * n), device="cuda")
+    fgd.fgd_attn_forward(plan, q, k, v, o, lse, 1.0)
+    ref, ref_lse, mag = O.attention(_np(q), _np(k), _np(v), cu, 1.0)
+    fp = F32 * (16 + d / 4 + 8 * 14)
+    _near(o, ref, u * np.abs(ref) + (1.01 * u + fp) * mag + TINY["f16"], "o")
+    _near(lse, ref_lse, fp + 4 * F32 * np.abs(ref_lse), "lse")
