@@ -11,8 +11,8 @@
 // Only unmasked pairs enter a product, so what stands in masked places never reaches a result.
 // Bound by the shared-memory loads that feed the fp32 FMAs: a score's dot product takes two for one, the products with P and dS one for one,
 // so the FMA units run at about a tenth of their rate: 16384 tokens, 16 heads of 128 over 4, forward 155 ms, where the tensor cores take
-// 0.97; 4 x 1024 tokens of the same in fp32 forward 2.9 ms, forward + backward 12.9.  delta has kernels of its own for 16-byte rows (8 elements a lane, several rows to a warp;
-// 14.6 us for 8192 tokens of 16 x 128, 4.6 TB/s).
+// 0.97; 4 x 1024 tokens of the same in fp32 forward 2.9 ms, forward + backward 12.9.  delta has kernels of its own for 16-byte rows
+// (8 elements a lane, several rows to a warp; 14.6 us for 8192 tokens of 16 x 128, 4.6 TB/s).
 #include "fgd_attn.h"
 #include "fgd_dtype.cuh"
 

@@ -209,7 +209,7 @@ __device__ __forceinline__ float2 exp2_poly(float2 x) {
   const float2 scale = make_float2(__uint_as_float((__float_as_uint(t.x) << 23) + 0x3F800000u), __uint_as_float((__float_as_uint(t.y) << 23) + 0x3F800000u));
   return mul2(p, scale);
 }
-// 2^x for the k-th pair of a row: one pair in eight by polynomial.  Measured at width 128 alone, on one device in one call: none, 1/8, 1/4:
+// 2^x for the k-th pair of a row: one pair in eight by polynomial.  Measured at width 128 alone, on one device: none, 1/8, 1/4:
 // 16384 tokens forward 857, 828, 850 us; 1/2 in the key kernel gains nothing either, since the FMA pipes' instructions then cost what the
 // exponential units save.  Up to width 64, where the exponentials outlast the products, the best share was not looked for.
 __device__ __forceinline__ float2 exp2_pair(float2 x, int k) {
