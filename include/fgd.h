@@ -397,6 +397,62 @@ int fgd_swiglu8_backward(int device, int dtype, int64_t rows, int64_t width, con
                          int64_t ld_q, const uint8_t* e8, int64_t ld_e, void* dgu, int64_t ld_dgu, void* h, int64_t ld_h,
                          void* stream);
 
+/* Queries and keys on their way to attention: norm of every head and rotation by the token's position, for `workers` workers at
+ * once (worker m owns the tokens [m rows, (m+1) rows) and row m of the weights).  For a head x of head_dim channels
+ *   z = x r w, r = 1/sqrt(mean(x^2) + eps)          (weights absent: z = x)
+ *   a' = a cos - b sin, b' = b cos + a sin          for the pairs (a, b) of the first rotary_dim channels of z: (i, i + rotary_dim / 2),
+ *                                                   or with `interleaved` (2i, 2i + 1); the other channels are z's
+ * with cos and sin from row positions[token] of the tables (row `token` where position_bytes is 0).  A position outside the tables
+ * makes its token's results (and the worker's weight gradients) NaN.  Backward: dq, dk from dq_out, dk_out and q, k as they went in; dw_q, dw_k
+ * summed over tokens and heads in a fixed order.  Without weights q and k are not read, and every product and sum is rounded by itself in fp32.
+ * q_out may be q itself, k_out k, dq dq_out, dk dk_out; otherwise outputs may not overlap anything. */
+typedef struct {
+  int32_t dtype, workers;
+  int64_t rows; /* per worker */
+  int32_t n_q_heads, n_k_heads /* 0: no keys */, head_dim, rotary_dim;
+  int32_t interleaved, position_bytes; /* 8: int64, 4: int32, 0: no positions */
+  int64_t table_rows;
+  double eps;
+  fgd_mat cos, sin;       /* fp32 [table_rows, rotary_dim / 2] */
+  const void* positions;  /* [workers * rows] */
+  fgd_mat w_q, w_k;       /* fp32 [workers, head_dim], each may be absent */
+  fgd_heads q, k;         /* inputs (backward: read only where there are weights) */
+  fgd_heads q_out, k_out; /* forward: outputs */
+  fgd_heads dq_out, dk_out;     /* backward: inputs */
+  fgd_heads dq, dk;             /* backward: outputs */
+  fgd_mat dw_q, dw_k;           /* backward: fp32 [workers, head_dim], required where there are weights */
+  void* workspace;              /* backward with weights: device scratch */
+  int64_t workspace_bytes;
+} fgd_qk_rope_args;
+/* head_dim <= 256, workers <= FGD_MAX_K, rotary_dim even.  Full speed: 16-byte aligned heads, rotary_dim / 2 and the rest's half multiples of
+ * 16 bytes, tables on 16-byte boundaries; everything else goes channel by channel (16-bit heads of which a half is 8 bytes' multiple, in between). */
+int fgd_qk_rope_forward(int device, const fgd_qk_rope_args* args, void* stream);
+int fgd_qk_rope_backward(int device, const fgd_qk_rope_args* args, void* stream);
+/* Bytes of scratch fgd_qk_rope_backward needs where there are weights (>= 0), or a negative status. */
+int64_t fgd_qk_rope_workspace(int device, int workers, int head_dim);
+
+/* Embeddings of K workers' tokens.  tokens: device int64 or int32 (token_bytes 8 or 4) [workers, rows], ld_tokens apart; table: fp32, row v of worker m at
+ * table + m worker_stride + v row_stride, e.g. a column range of the flat [K, ld] parameter matrix; out, dout: [workers * rows, width] of `dtype`.
+ *   forward:  out = scale table[token], rounded once.  A token below 0 is padding, its row zero; one at vocab or above makes its row NaN.
+ *   backward: dtable[v] = scale times the sum of dout over the tokens that are v (in fp32, in an order that depends on the tokens alone);
+ *             every row of dtable is written, those of absent tokens with zero; tokens outside [0, vocab) have no part.
+ * width <= 65536, vocab <= 2^30, workers <= FGD_MAX_K. */
+int fgd_embed_forward(int device, int dtype, int workers, int64_t rows, int64_t vocab, int64_t width, const void* tokens, int token_bytes, int64_t ld_tokens,
+                      const float* table, int64_t worker_stride, int64_t row_stride, double scale, void* out, int64_t ld_out, void* stream);
+int fgd_embed_backward(int device, int dtype, int workers, int64_t rows, int64_t vocab, int64_t width, const void* tokens, int token_bytes, int64_t ld_tokens,
+                       const void* dout, int64_t ld_dout, double scale, float* dtable, int64_t worker_stride, int64_t row_stride, void* workspace,
+                       int64_t workspace_bytes, void* stream);
+/* Bytes of scratch fgd_embed_backward needs (>= 0), or a negative status. */
+int64_t fgd_embed_workspace(int workers, int64_t rows, int64_t vocab, int64_t width);
+
+/* Dropout with a mask that is a function of (seed, offset, row, column) and is never stored; on the gradient it is its own backward pass.
+ *   out[r][c] = x[r][c] / (1 - p) where word(r, c) >= round(p 2^32), else 0 (whatever x holds there)
+ *   word(r, c): word c % 4 of Philox4x32 with seven rounds, counter (c / 4, r, low, high word of the offset), key (low, high word of the seed)
+ * `counter`: device memory, added to the offset when the kernel runs (NULL: nothing), so that a captured call has another mask at every replay.
+ * 0 <= p < 1; rows < 2^32, width < 2^31.  out may be x itself, and otherwise may not overlap it.  Any base and stride on element boundaries. */
+int fgd_dropout(int device, int dtype, int64_t rows, int64_t width, const void* x, int64_t ld_x, void* out, int64_t ld_out, double p, uint64_t seed,
+                uint64_t offset, const int64_t* counter, void* stream);
+
 /* (No counterpart in the paper: a packaging variant of fgd_consensus_distance.)
  * Same result as fgd_consensus_distance, for callers that cannot allocate GPU memory and so
  * cannot create a context: it needs no fgd_ctx and calls no cudaMalloc / cudaFree or any other

@@ -164,3 +164,91 @@ def swiglu_grad(dh, g, u):
     dh, g, u = _f8(dh), _f8(g), _f8(u)
     s = 1.0 / (1.0 + np.exp(-g))
     return dh * u * s * (1.0 + g * (1.0 - s)), dh * g * s
+
+
+# ------------------------------------------------------------------------------- head norms and rotation
+def _pairs(d, rot, interleaved):
+    """Channels of the first and second members of the rotated pairs."""
+    i = np.arange(rot // 2)
+    return (2 * i, 2 * i + 1) if interleaved else (i, i + rot // 2)
+
+
+def _turn(z, cos, sin, interleaved, sign=1.0):
+    """[T, H, d] turned by [T, r / 2] angles, and the magnitudes of the terms."""
+    a, b = _pairs(z.shape[2], 2 * cos.shape[1], interleaved)
+    c, s = cos[:, None], sign * sin[:, None]
+    y, m = z.copy(), np.abs(z)
+    y[..., a], y[..., b] = z[..., a] * c - z[..., b] * s, z[..., b] * c + z[..., a] * s
+    m[..., a], m[..., b] = np.abs(z[..., a] * c) + np.abs(z[..., b] * s), np.abs(z[..., b] * c) + np.abs(z[..., a] * s)
+    return y, m
+
+
+def head_rope(x, w, cos, sin, workers, interleaved, eps):
+    """x [T, H, d], w [K, d] or None, cos and sin [T, r / 2] of the tokens -> y and the magnitudes of its terms."""
+    x, cos, sin = _f8(x), _f8(cos), _f8(sin)
+    z = x
+    if w is not None:
+        z = x / np.sqrt((x * x).mean(2, keepdims=True) + eps) * _per_row(w, workers, x.shape[0] // workers)[:, None]
+    return _turn(z, cos, sin, interleaved)
+
+
+def head_rope_grad(dy, x, w, cos, sin, workers, interleaved, eps):
+    """-> dx, dw (None without w) and the magnitudes of their terms."""
+    dy, x, cos, sin = _f8(dy), _f8(x), _f8(cos), _f8(sin)
+    dz, mz = _turn(dy, cos, sin, interleaved, -1.0)
+    if w is None:
+        return dz, None, mz, None
+    T, _, d = x.shape
+    r = 1.0 / np.sqrt((x * x).mean(2, keepdims=True) + eps)
+    wr = _per_row(w, workers, T // workers)[:, None]
+    xh, g, mg = x * r, dz * wr, mz * np.abs(wr)
+    dx = r * (g - xh * (g * xh).mean(2, keepdims=True))
+    mx = r * (mg + np.abs(xh) * (mg * np.abs(xh)).mean(2, keepdims=True))
+    per = lambda t: t.reshape(workers, -1, d).sum(1)  # noqa: E731
+    return dx, per(dz * xh), mx, per(mz * np.abs(xh))
+
+
+# ------------------------------------------------------------------------------- embeddings
+def embed(tokens, table, scale):
+    """tokens [K, rows], table [K, V, W] -> [K * rows, W]; below 0: zero, from V on: NaN."""
+    table = _f8(table)
+    K, V, W = table.shape
+    out = np.zeros((K, tokens.shape[1], W))
+    for m in range(K):
+        inside = (tokens[m] >= 0) & (tokens[m] < V)
+        out[m, inside] = scale * table[m, tokens[m, inside]]
+        out[m, tokens[m] >= V] = np.nan
+    return out.reshape(-1, W)
+
+
+def embed_grad(tokens, dout, V, scale):
+    """-> gradient of the table [K, V, W], the magnitudes of its terms, and how many terms each row has [K, V]."""
+    K, rows = tokens.shape
+    d = _f8(dout).reshape(K, rows, -1)
+    g, m, n = np.zeros((K, V, d.shape[2])), np.zeros((K, V, d.shape[2])), np.zeros((K, V), dtype=np.int64)
+    for k in range(K):
+        ok = (tokens[k] >= 0) & (tokens[k] < V)
+        np.add.at(g[k], tokens[k, ok], scale * d[k, ok])
+        np.add.at(m[k], tokens[k, ok], np.abs(scale * d[k, ok]))
+        np.add.at(n[k], tokens[k, ok], 1)
+    return g, m, n
+
+
+# ------------------------------------------------------------------------------- dropout
+def philox4x32(counter, key, rounds):
+    """Philox4x32 (Salmon, Moraes, Dror, Shaw, SC 2011): four counter words (arrays) and two key words -> four words."""
+    c, k = [np.asarray(w, dtype=np.uint64) for w in counter], [int(w) for w in key]
+    low, half = np.uint64(0xFFFFFFFF), np.uint64(32)
+    for _ in range(rounds):
+        p, q = c[0] * np.uint64(0xD2511F53), c[2] * np.uint64(0xCD9E8D57)
+        c = [(q >> half) ^ c[1] ^ np.uint64(k[0]), q & low, (p >> half) ^ c[3] ^ np.uint64(k[1]), p & low]
+        k = [(k[0] + 0x9E3779B9) % 2 ** 32, (k[1] + 0xBB67AE85) % 2 ** 32]
+    return c
+
+
+def dropout_keeps(rows, width, p, seed, offset):
+    """Which values a dropout of [rows, width] keeps."""
+    row, column = np.arange(rows, dtype=np.uint64)[:, None], np.arange(width, dtype=np.uint64)[None, :]
+    words = philox4x32((column // np.uint64(4), row, np.uint64(offset % 2 ** 32), np.uint64(offset // 2 ** 32 % 2 ** 32)), (seed % 2 ** 32, seed // 2 ** 32 % 2 ** 32), 7)
+    word = np.choose((column % np.uint64(4)).astype(np.int64), [np.broadcast_to(w, (rows, width)) for w in words])
+    return word >= np.uint64(min(round(p * 2 ** 32), 2 ** 32 - 1))

@@ -51,10 +51,11 @@ class _CMixDesc(ctypes.Structure):
                 ("w_self", ctypes.c_void_p), ("edge_mask", ctypes.c_void_p), ("W", ctypes.c_void_p)]
 
 
-# fgd_attn_args and fgd_block_norm_args as they lie in memory (native alignment).  Small calls are bound by what the host does per
+# fgd_attn_args, fgd_block_norm_args and fgd_qk_rope_args as they lie in memory (native alignment).  Small calls are bound by what the host does per
 # call; one pack costs a fraction of filling nested ctypes structures.
 _ATTN_ARGS = struct.Struct("@4i 12q Qd 3qQ 9q")
 _NORM_ARGS = struct.Struct("@2i 2q i4x 2d 28q 2q")
+_ROPE_ARGS = struct.Struct("@2i q 6i q d 37q 2q")
 
 
 def _load():
@@ -95,6 +96,13 @@ def _load():
         "fgd_act_load8": (i32, [i32, i32, i64, i64, vp, i64, vp, i64, vp, i64, vp]),
         "fgd_swiglu8_forward": (i32, [i32, i32, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp]),
         "fgd_swiglu8_backward": (i32, [i32, i32, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp]),
+        "fgd_qk_rope_forward": (i32, [i32, vp, vp]),
+        "fgd_qk_rope_backward": (i32, [i32, vp, vp]),
+        "fgd_qk_rope_workspace": (i64, [i32, i32, i32]),
+        "fgd_embed_forward": (i32, [i32, i32, i32, i64, i64, i64, vp, i32, i64, vp, i64, i64, dbl, vp, i64, vp]),
+        "fgd_embed_backward": (i32, [i32, i32, i32, i64, i64, i64, vp, i32, i64, vp, i64, dbl, vp, i64, i64, vp, i64, vp]),
+        "fgd_embed_workspace": (i64, [i32, i64, i64, i64]),
+        "fgd_dropout": (i32, [i32, i32, i64, i64, vp, i64, vp, i64, dbl, u64, u64, vp, vp]),
         "fgd_topo_ring": (i32, [i32, vp, vp, vp]),
         "fgd_topo_onepeer_xor": (i32, [i32, i64, vp, vp, vp]),
         "fgd_topo_hypercube": (i32, [i32, vp, vp, vp]),
@@ -484,6 +492,16 @@ def _as_current(stream, handle, device):
     return torch.cuda.stream(stream)
 
 
+def _scratch(size: int, stream, handle, device):
+    """Workspace of a call: from the memory of the stream that uses it.  A block of another stream's may have uses on that stream still to come before
+    this call, and would need to be kept from others until after it."""
+    import torch
+    if stream is None:
+        return torch.empty(max(size, 1), dtype=torch.uint8, device=device)
+    with _as_current(stream, handle, device):
+        return torch.empty(max(size, 1), dtype=torch.uint8, device=device)
+
+
 def _device_of(t, name: str):
     if not getattr(t, "is_cuda", False):
         raise TypeError(f"{name} must be a CUDA tensor")
@@ -662,14 +680,7 @@ def fgd_block_norm_backward(dn, dres, x_new, y, gate, w_post, w_pre, dx, dy, dga
                     g.zero_()
         return
     if workspace is None:
-        size = max(fgd_block_norm_workspace(code, K, T // K, H, dev.index), 1)
-        if stream is None:
-            workspace = torch.empty(size, dtype=torch.uint8, device=dev)
-        else:
-            # From the memory of the stream that uses it: a block of another stream's may have uses on that stream still to come before
-            # this call, and would need to be kept from others until after it.
-            with _as_current(stream, handle, dev):
-                workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+        workspace = _scratch(fgd_block_norm_workspace(code, K, T // K, H, dev.index), stream, handle, dev)
     args = _NORM_ARGS.pack(code, K, T // K, H, kind, eps, res_scale, *mats, _dev_ptr(workspace, "workspace", "torch.uint8"), workspace.numel())
     _op_check(_lib.fgd_block_norm_backward(dev.index, args, handle))
 
@@ -714,3 +725,147 @@ def fgd_swiglu8_backward(dh, q8, e8, dgu, h=None, stream=None) -> None:
     _op_check(_lib.fgd_swiglu8_backward(dev.index, _dtype_of(dh, "dh"), R, W, *_mat(dh, "dh", dh.dtype, R, W, dev),
                                         *_mat(q8, "q8", torch.int8, R, 2 * W, dev), *_mat(e8, "e8", torch.uint8, R, 2 * -(-W // ACT8_GROUP), dev),
                                         *_mat(dgu, "dgu", dh.dtype, R, 2 * W, dev), *_mat(h, "h", dh.dtype, R, W, dev), _stream_on(stream, dev)))
+
+
+def _whole_numbers(t, name: str, shape, device):
+    """Pointer and bytes of a contiguous-rowed int64 or int32 tensor."""
+    import torch
+    if t.dtype != torch.int64 and t.dtype != torch.int32:
+        raise TypeError(f"{name} must be int64 or int32, got {t.dtype}")
+    if t.shape != shape or t.device != device or (t.stride(-1) != 1 and shape[-1] > 1):
+        _refuse(t, name, t.dtype, shape, device)
+    return t.data_ptr(), t.element_size()
+
+
+def _rope_shapes(q, k, w_q, w_k, cos):
+    """device, query and key shapes, workers, (rows of the tables, half of the rotated width)"""
+    if q.dim() != 3 or (k is not None and k.dim() != 3):
+        raise ValueError("q and k must be [tokens, heads, width]")
+    if cos.dim() != 2:
+        raise ValueError("cos and sin must be [rows, rotated width / 2]")
+    dev, qs = _device_of(q, "q"), q.shape
+    ks = (qs[0], 0 if k is None else k.shape[1], qs[2])
+    w = w_q if w_q is not None else w_k
+    K = 1 if w is None else w.shape[0]
+    if K < 1 or qs[0] % K != 0:
+        raise ValueError(f"{qs[0]} tokens do not split over {K} workers")
+    return dev, qs, ks, K, cos.shape
+
+
+def _rope_pack(q, cos, sin, positions, w_q, w_k, eps, interleaved, shapes, heads, dw, workspace):
+    import torch
+    dev, qs, ks, K, (N, half) = shapes
+    f32, d = torch.float32, qs[2]
+    pos, pos_bytes = (0, 0) if positions is None else _whole_numbers(positions, "positions", (qs[0],), dev)
+    return _ROPE_ARGS.pack(_dtype_of(q, "q"), K, qs[0] // K, qs[1], ks[1], d, 2 * half, int(interleaved), pos_bytes, N, eps, *_mat(cos, "cos", f32, N, half, dev),
+                           *_mat(sin, "sin", f32, N, half, dev), pos, *_mat(w_q, "w_q", f32, K, d, dev), *_mat(w_k, "w_k", f32, K, d, dev), *heads,
+                           *_mat(dw[0], "dw_q", f32, K, d, dev), *_mat(dw[1], "dw_k", f32, K, d, dev), *workspace)
+
+
+def _key_heads(t, name: str, dtype, shape, device):
+    if shape[1] == 0 and t is None:
+        return _NO_HEADS
+    return _heads(t, name, dtype, shape, device)
+
+
+def fgd_qk_rope_forward(q, k, w_q, w_k, cos, sin, positions, q_out, k_out, eps: float = 1e-5, interleaved: bool = False, stream=None) -> None:
+    """Queries [T, Hq, d] and keys [T, Hk, d] (None: no keys) normalised per head with w_q, w_k ([K, d] fp32 for K workers with T / K tokens each; None: not
+    normalised) and rotated by rows ``positions`` ([T] int64 or int32; None: row t) of the tables cos and sin ([N, r / 2] fp32; the first r channels turn).
+    Any token and head strides; q_out may be q, k_out k.  See ``include/fgd.h``."""
+    shapes = dev, qs, ks, _, _ = _rope_shapes(q, k, w_q, w_k, cos)
+    dt = q.dtype
+    heads = (*_heads(q, "q", dt, qs, dev), *_key_heads(k, "k", dt, ks, dev), *_heads(q_out, "q_out", dt, qs, dev), *_key_heads(k_out, "k_out", dt, ks, dev),
+             *_NO_HEADS, *_NO_HEADS, *_NO_HEADS, *_NO_HEADS)
+    args = _rope_pack(q, cos, sin, positions, w_q, w_k, eps, interleaved, shapes, heads, (None, None), _NO_MAT)
+    _op_check(_lib.fgd_qk_rope_forward(dev.index, args, _stream_on(stream, dev)))
+
+
+def fgd_qk_rope_workspace(workers: int, head_dim: int, device: int = 0) -> int:
+    """Bytes of scratch that :func:`fgd_qk_rope_backward` needs where there are weights."""
+    n = int(_lib.fgd_qk_rope_workspace(int(device), int(workers), int(head_dim)))
+    if n < 0:
+        raise FgdError(n, "fgd_qk_rope_workspace: argument out of range")
+    return n
+
+
+def fgd_qk_rope_backward(dq_out, dk_out, q, k, w_q, w_k, cos, sin, positions, dq, dk, dw_q, dw_k, eps: float = 1e-5, interleaved: bool = False,
+                         workspace=None, stream=None) -> None:
+    """Gradients of :func:`fgd_qk_rope_forward` from its inputs (q and k may be None where neither is normalised); dq may be dq_out, dk dk_out.
+    ``workspace``: a uint8 CUDA tensor of :func:`fgd_qk_rope_workspace` bytes (None: allocated here)."""
+    shapes = dev, qs, ks, K, _ = _rope_shapes(dq_out, dk_out, w_q, w_k, cos)
+    dt = dq_out.dtype
+    heads = (*(_NO_HEADS if w_q is None else _heads(q, "q", dt, qs, dev)), *(_NO_HEADS if w_k is None else _key_heads(k, "k", dt, ks, dev)), *_NO_HEADS, *_NO_HEADS,
+             *_heads(dq_out, "dq_out", dt, qs, dev), *_key_heads(dk_out, "dk_out", dt, ks, dev), *_heads(dq, "dq", dt, qs, dev), *_key_heads(dk, "dk", dt, ks, dev))
+    handle = _stream_on(stream, dev)
+    if workspace is None and (w_q is not None or w_k is not None):
+        workspace = _scratch(fgd_qk_rope_workspace(K, qs[2], dev.index), stream, handle, dev)
+    room = _NO_MAT if workspace is None else (_dev_ptr(workspace, "workspace", "torch.uint8"), workspace.numel())
+    args = _rope_pack(dq_out, cos, sin, positions, w_q, w_k, eps, interleaved, shapes, heads, (dw_q, dw_k), room)
+    _op_check(_lib.fgd_qk_rope_backward(dev.index, args, handle))
+
+
+def _table(t, name: str, device):
+    """(pointer, worker stride, row stride) of an fp32 [workers, vocabulary, width] tensor"""
+    import torch
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [workers, vocabulary, width]")
+    if t.dtype != torch.float32 or t.device != device or (t.stride(2) != 1 and t.shape[2] > 1):
+        _refuse(t, name, torch.float32, t.shape, device)
+    K, V, W = t.shape
+    row = t.stride(1) if V > 1 else W
+    return t.data_ptr(), t.stride(0) if K > 1 else V * row, row
+
+
+def _embed_tokens(tokens, K, device):
+    if tokens.dim() != 2 or tokens.shape[0] != K:
+        raise ValueError(f"tokens must be [{K}, rows], got {tuple(tokens.shape)}")
+    ptr, size = _whole_numbers(tokens, "tokens", tokens.shape, device)
+    return ptr, size, tokens.stride(0) if K > 1 else max(tokens.shape[1], 1)
+
+
+def fgd_embed_forward(tokens, table, out, scale: float = 1.0, stream=None) -> None:
+    """out[m * rows + i] = scale * table[m, tokens[m, i]]: tokens [K, rows] int64 or int32, table [K, V, W] fp32 (e.g. a column range of the parameter
+    matrix), out [K * rows, W].  A token below 0 is padding: its row is zero."""
+    dev = _device_of(out, "out")
+    if out.dim() != 2:
+        raise ValueError("out must be [tokens, width]")
+    tab, (K, V, W) = _table(table, "table", dev), table.shape
+    tok = _embed_tokens(tokens, K, dev)
+    _op_check(_lib.fgd_embed_forward(dev.index, _dtype_of(out, "out"), K, tokens.shape[1], V, W, *tok, *tab, scale,
+                                     *_mat(out, "out", out.dtype, K * tokens.shape[1], W, dev), _stream_on(stream, dev)))
+
+
+def fgd_embed_workspace(workers: int, rows: int, vocab: int, width: int) -> int:
+    """Bytes of scratch that :func:`fgd_embed_backward` needs for ``rows`` tokens per worker."""
+    n = int(_lib.fgd_embed_workspace(int(workers), int(rows), int(vocab), int(width)))
+    if n < 0:
+        raise FgdError(n, "fgd_embed_workspace: argument out of range")
+    return n
+
+
+def fgd_embed_backward(tokens, dout, dtable, scale: float = 1.0, workspace=None, stream=None) -> None:
+    """Gradient of :func:`fgd_embed_forward`: dtable [K, V, W] (fp32), all of it, from dout [K * rows, W].  ``workspace``: a uint8 CUDA tensor of
+    :func:`fgd_embed_workspace` bytes (None: allocated here)."""
+    dev = _device_of(dout, "dout")
+    if dout.dim() != 2:
+        raise ValueError("dout must be [tokens, width]")
+    tab, (K, V, W) = _table(dtable, "dtable", dev), dtable.shape
+    tok, rows = _embed_tokens(tokens, K, dev), tokens.shape[1]
+    grad, handle = _mat(dout, "dout", dout.dtype, K * rows, W, dev), _stream_on(stream, dev)
+    if workspace is None:
+        workspace = _scratch(fgd_embed_workspace(K, rows, V, W), stream, handle, dev)
+    _op_check(_lib.fgd_embed_backward(dev.index, _dtype_of(dout, "dout"), K, rows, V, W, *tok, *grad, scale, *tab, _dev_ptr(workspace, "workspace", "torch.uint8"),
+                                      workspace.numel(), handle))
+
+
+def fgd_dropout(x, out, p: float, seed: int, offset: int = 0, counter=None, stream=None) -> None:
+    """out = x / (1 - p) where the generator of (seed, offset, row, column) keeps the value, else 0; the mask is never stored, and the backward pass is the
+    same call on the gradient.  ``counter``: a CUDA int64 tensor of one value that is added to the offset when the kernel runs.  out may be x."""
+    import torch
+    if x.dim() != 2:
+        raise ValueError("x must be [rows, width]")
+    (R, W), dev = x.shape, _device_of(x, "x")
+    if counter is not None and (counter.dtype != torch.int64 or counter.numel() != 1 or counter.device != dev):
+        raise ValueError("counter must be one int64 value on the device of x")
+    _op_check(_lib.fgd_dropout(dev.index, _dtype_of(x, "x"), R, W, *_mat(x, "x", x.dtype, R, W, dev), *_mat(out, "out", x.dtype, R, W, dev), p, seed, offset,
+                               0 if counter is None else counter.data_ptr(), _stream_on(stream, dev)))

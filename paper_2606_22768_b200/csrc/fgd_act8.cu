@@ -18,10 +18,10 @@
 //
 // Vector kernels (rows and bases on 16-byte boundaries, width a multiple of 16 or 8): a thread takes 16 or 8
 // consecutive values, two or four neighbouring lanes make a group, so the group's largest magnitude is one or two
-// shuffles away.  Any other width, base or stride: 16 values to a lane as well, moved with shifts (fgd_shift.cuh).
+// shuffles away.  Any other width, base or stride: 16 values to a lane as well, moved with shifts (fgd_units.cuh).
 #include "fgd_dtype.cuh"
 #include "fgd_nvtx.h"
-#include "fgd_shift.cuh"
+#include "fgd_units.cuh"
 
 using namespace fgd;
 
@@ -182,21 +182,6 @@ struct Act8Args {
   int64_t rows, width;
 };
 
-// A walk over (row, unit) with `units` units per row, gridDim x blockDim units at a time, without a
-// division in the loop.
-struct Walk {
-  int64_t row, step_row;
-  int unit, step_unit, units;
-  __device__ __forceinline__ Walk(int64_t first, int64_t stride, int units_) : units(units_) {
-    row = first / units; unit = (int)(first - row * units);
-    step_row = stride / units; step_unit = (int)(stride - step_row * units);
-  }
-  __device__ __forceinline__ void next() {
-    row += step_row; unit += step_unit;
-    if (unit >= units) { unit -= units; ++row; }
-  }
-};
-
 // ---- vector kernels: a unit is V values; every row is padded to whole groups, so that the lanes of a group always work together.
 // V = 16 for 16-bit activations (16-byte stores of the checkpoint: save of 32768 x 4096 bf16 71.5 us against 78.6 with 8), 8 for fp32
 // (57 against 60) and for widths that are not a multiple of 16.
@@ -325,61 +310,14 @@ __global__ void __launch_bounds__(kBlock8, 4) swiglu8_backward_kernel(const Swig
   }
 }
 
-// ---- kernels for every other width, base and stride: a unit is 16 values, moved by fgd_shift.cuh
+// ---- kernels for every other width, base and stride: a unit is 16 values, moved by fgd_units.cuh
 constexpr int kAny = 16;
 constexpr int kAnyWaves = 4;      // (1 to 8 are within 3 %, 16 is 6 % slower)
-template <typename T>
-constexpr int kAnyWords = kAny * (int)sizeof(T) / 4;
-
-// Unit (row, unit) of a lane in the padded walk, and who its neighbours in the warp are.
-struct AnyUnit {
-  int c, left, valid;            // first column; columns from there to the row's end, clipped to [-16, 16]
-  bool mine, has_prev, has_next;
-  __device__ __forceinline__ AnyUnit(const Walk& w, bool in_range, int64_t width) {
-    const int lane = threadIdx.x & 31;
-    c = w.unit * kAny;
-    const int64_t l = width - c;
-    left = (int)(l > kAny ? kAny : l < -kAny ? -kAny : l);
-    mine = in_range && left > 0;
-    valid = mine ? left : -64;   // (of a lane without a unit nothing is stored)
-    has_prev = lane > 0 && w.unit > 0;
-    has_next = mine && lane < 31 && l > kAny;
-  }
-};
-template <typename T>
-__device__ __forceinline__ Vals<kAny> any_vals(const uint32_t (&w)[kAnyWords<T>], int left) {
-  Vals<kAny> f;
-#pragma unroll
-  for (int i = 0; i < kAnyWords<T>; ++i) {
-    if constexpr (sizeof(T) == 4) f.v[i] = __uint_as_float(w[i]);
-    else f.set(i, halves<T>(w[i]));
-  }
-  if (left < kAny) {             // beyond the row: the next row's values, or none
-#pragma unroll
-    for (int i = 0; i < kAny; ++i) f.v[i] = i < left ? f.v[i] : 0.f;
-  }
-  return f;
-}
-template <typename T>
-__device__ __forceinline__ Vals<kAny> any_load(const T* p, const AnyUnit& u, const T* lo, const T* hi) {
-  uint32_t w[kAnyWords<T>];
-  load_unit<sizeof(T), kAnyWords<T>>(reinterpret_cast<const char*>(p), u.mine, u.has_next, reinterpret_cast<const char*>(lo), reinterpret_cast<const char*>(hi), w);
-  return any_vals<T>(w, u.left);
-}
+using AnyUnit = ShiftedUnit<kAny>;
 __device__ __forceinline__ uint4 any_load8(const int8_t* p, const AnyUnit& u, const int8_t* lo, const int8_t* hi) {
   uint32_t w[4];
   load_unit<1, 4>(reinterpret_cast<const char*>(p), u.mine, u.has_next, reinterpret_cast<const char*>(lo), reinterpret_cast<const char*>(hi), w);
   return make_uint4(w[0], w[1], w[2], w[3]);
-}
-template <typename T>
-__device__ __forceinline__ void any_store(T* p, const AnyUnit& u, const Vals<kAny>& f) {
-  uint32_t w[kAnyWords<T>];
-#pragma unroll
-  for (int i = 0; i < kAnyWords<T>; ++i) {
-    if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(f.v[i]);
-    else w[i] = from_pair<T>(f.v[2 * i], f.v[2 * i + 1]);
-  }
-  store_unit<sizeof(T), kAnyWords<T>>(reinterpret_cast<char*>(p), u.valid * (int)sizeof(T), u.has_prev, u.has_next, w);
 }
 __device__ __forceinline__ void any_store8(int8_t* p, const AnyUnit& u, uint4 q) {
   const uint32_t w[4] = {q.x, q.y, q.z, q.w};
@@ -396,7 +334,7 @@ __global__ void __launch_bounds__(kBlock8) act8_save_any_kernel(const Act8Args a
   const T* end = x + (a.rows - 1) * a.ld_x + a.width;
   for (; i < padded; i += stride, w.next()) {
     const AnyUnit u(w, i < total, a.width);
-    const Vals<kAny> f = any_load<T>(x + w.row * a.ld_x + u.c, u, x, end);
+    const Vals<kAny> f = load_shifted<T, kAny>(x + w.row * a.ld_x + u.c, u, x, end);
     const uint32_t m = group_max<kAny>(u.mine ? amax_of<kAny>(f) : 0u), e = step_exponent(m);
     const uint4 q = __any_sync(0xffffffffu, tops_out(m)) ? quantise<kAny>(f, inverse_step(e), true) : quantise<kAny>(f, inverse_step(e), false);
     any_store8(a.q + w.row * a.ld_q + u.c, u, q);
@@ -414,7 +352,7 @@ __global__ void __launch_bounds__(kBlock8) act8_load_any_kernel(const Act8Args a
     const AnyUnit u(w, i < total, a.width);
     const float step = u.mine ? step_of(a.e[w.row * a.ld_e + w.unit / 2]) : 0.f;
     const uint4 q = any_load8(a.q + w.row * a.ld_q + u.c, u, a.q, end);
-    any_store<T>(static_cast<T*>(a.out) + w.row * a.ld_out + u.c, u, dequantise<kAny>(q, step));
+    store_shifted<T, kAny>(static_cast<T*>(a.out) + w.row * a.ld_out + u.c, u, dequantise<kAny>(q, step));
   }
 }
 template <typename T>
@@ -428,7 +366,7 @@ __global__ void __launch_bounds__(kBlock8) swiglu8_forward_any_kernel(const Act8
   for (; i < padded; i += stride, w.next()) {
     const AnyUnit n(w, i < total, a.width);
     const T* row = x + w.row * a.ld_x + n.c;
-    const Vals<kAny> g = any_load<T>(row, n, x, end), u = any_load<T>(row + a.width, n, x, end);
+    const Vals<kAny> g = load_shifted<T, kAny>(row, n, x, end), u = load_shifted<T, kAny>(row + a.width, n, x, end);
     const uint32_t mg = group_max<kAny>(n.mine ? amax_of<kAny>(g) : 0u), mu = group_max<kAny>(n.mine ? amax_of<kAny>(u) : 0u), eg = step_exponent(mg),
                    eu = step_exponent(mu);
     const bool clamp = __any_sync(0xffffffffu, tops_out(mg) || tops_out(mu));
@@ -438,7 +376,7 @@ __global__ void __launch_bounds__(kBlock8) swiglu8_forward_any_kernel(const Act8
     Vals<kAny> h;
 #pragma unroll
     for (int j = 0; j < kAny / 2; ++j) h.set(j, mul2(mul2(g.pair(j), sigmoid2<T>(g.pair(j))), u.pair(j)));
-    any_store<T>(static_cast<T*>(a.out) + w.row * a.ld_out + n.c, n, h);
+    store_shifted<T, kAny>(static_cast<T*>(a.out) + w.row * a.ld_out + n.c, n, h);
     if (i < total && w.unit % 2 == 0) {
       uint8_t* e = a.e + w.row * a.ld_e + w.unit / 2;
       e[0] = (uint8_t)eg;
@@ -461,7 +399,7 @@ __global__ void __launch_bounds__(kBlock8) swiglu8_backward_any_kernel(const Swi
     const uint8_t* e = a.e + w.row * a.ld_e + w.unit / 2;
     const float sg = n.mine ? step_of(e[0]) : 0.f, su = n.mine ? step_of(e[groups]) : 0.f;
     const uint4 qg = any_load8(q, n, a.q, end8), qu = any_load8(q + a.width, n, a.q, end8);
-    const Vals<kAny> d = any_load<T>(dh + w.row * a.ld_dh + n.c, n, dh, end), g = dequantise<kAny>(qg, sg), u = dequantise<kAny>(qu, su);
+    const Vals<kAny> d = load_shifted<T, kAny>(dh + w.row * a.ld_dh + n.c, n, dh, end), g = dequantise<kAny>(qg, sg), u = dequantise<kAny>(qu, su);
     Vals<kAny> dg, du, h;
 #pragma unroll
     for (int j = 0; j < kAny / 2; ++j) {
@@ -470,9 +408,9 @@ __global__ void __launch_bounds__(kBlock8) swiglu8_backward_any_kernel(const Swi
       dg.set(j, x); du.set(j, y); h.set(j, z);
     }
     T* out = static_cast<T*>(a.dgu) + w.row * a.ld_dgu + n.c;
-    any_store<T>(out, n, dg);
-    any_store<T>(out + a.width, n, du);
-    if (a.h) any_store<T>(static_cast<T*>(a.h) + w.row * a.ld_h + n.c, n, h);
+    store_shifted<T, kAny>(out, n, dg);
+    store_shifted<T, kAny>(out + a.width, n, du);
+    if (a.h) store_shifted<T, kAny>(static_cast<T*>(a.h) + w.row * a.ld_h + n.c, n, h);
   }
 }
 

@@ -91,3 +91,54 @@ def test_save8_error_bound():
     top = np.repeat(np.abs(x).reshape(50, 2, 32).max(2), 32, axis=1)
     assert (np.abs(back - x) <= top / 64 * (1 + 1e-12)).all()                 # a step is at most 1/64 of the largest magnitude
     assert np.mean(np.abs(back - x) <= top / 128 * (1 + 1e-12)) > 0.99        # and only a value above 127 steps is more than half a step off
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("d,rot,normed", [(6, 6, True), (7, 4, True), (8, 4, False)])
+def test_head_rope_gradient_against_differences(d, rot, normed, interleaved):
+    rng = np.random.default_rng(2)
+    T, K = 4, 2
+    x, dy, w = rng.normal(size=(T, 3, d)), rng.normal(size=(T, 3, d)), 1 + 0.3 * rng.normal(size=(K, d))
+    angle = rng.normal(size=(T, rot // 2))
+    f = lambda: O.head_rope(x, w if normed else None, np.cos(angle), np.sin(angle), K, interleaved, 1e-3)[0]  # noqa: E731
+    dx, dw, _, _ = O.head_rope_grad(dy, x, w if normed else None, np.cos(angle), np.sin(angle), K, interleaved, 1e-3)
+    np.testing.assert_allclose(dx, _difference(f, x, dy), rtol=1e-6, atol=1e-8)
+    if normed:
+        np.testing.assert_allclose(dw, _difference(f, w, dy), rtol=1e-6, atol=1e-8)
+
+
+def test_head_rope_closed_forms():
+    """A quarter turn; lengths are kept; the norm's heads have root mean square 1."""
+    x = np.arange(1.0, 7.0).reshape(1, 1, 6)
+    quarter = (np.zeros((1, 2)), np.ones((1, 2)))
+    np.testing.assert_array_equal(O.head_rope(x, None, *quarter, 1, False, 0.0)[0].ravel(), [-3, -4, 1, 2, 5, 6])
+    np.testing.assert_array_equal(O.head_rope(x, None, *quarter, 1, True, 0.0)[0].ravel(), [-2, 1, -4, 3, 5, 6])
+    angle = np.array([[0.3, 1.1, 2.0]])
+    y, _ = O.head_rope(x, np.ones((1, 6)), np.cos(angle), np.sin(angle), 1, False, 0.0)
+    assert abs((y ** 2).mean() - 1.0) < 1e-12
+
+
+def test_embed_gradient_is_the_transpose():
+    rng = np.random.default_rng(3)
+    tokens, table, dout = rng.integers(-2, 9, (2, 20)), rng.normal(size=(2, 7, 3)), rng.normal(size=(40, 3))
+    out = O.embed(tokens, table, 0.5)
+    assert np.isnan(out[(tokens >= 7).ravel()]).all() and (out[(tokens < 0).ravel()] == 0).all()
+    inside = (tokens < 7).ravel()
+    g, _, n = O.embed_grad(tokens, dout, 7, 0.5)
+    np.testing.assert_allclose((out[inside] * dout[inside]).sum(), (g * table).sum())
+    assert n.sum() == ((tokens >= 0) & (tokens < 7)).sum()
+
+
+def test_philox_known_answers():
+    """The published test vectors of Philox4x32 with seven and ten rounds: all zeros, all ones, digits of pi."""
+    zeros, ones, pi = [0] * 6, [0xFFFFFFFF] * 6, [0x243F6A88, 0x85A308D3, 0x13198A2E, 0x03707344, 0xA4093822, 0x299F31D0]
+    for rounds, words, want in ((7, zeros, "5f6fb709 0d893f64 4f121f81 4f730a48"), (10, zeros, "6627e8d5 e169c58d bc57ac4c 9b00dbd8"),
+                                (10, ones, "408f276d 41c83b0e a20bc7c6 6d5451fd"), (10, pi, "d16cfe09 94fdcceb 5001e420 24126ea1")):
+        assert [int(w) for w in O.philox4x32(words[:4], words[4:], rounds)] == [int(w, 16) for w in want.split()]
+
+
+def test_dropout_mask_rate_and_words():
+    keeps = O.dropout_keeps(300, 203, 0.25, 7, 1 << 40)
+    assert abs(keeps.mean() - 0.75) < 5 * (0.25 * 0.75 / keeps.size) ** 0.5
+    word = O.philox4x32((50, 9, 0, 1 << 8), (7, 0), 7)[2]
+    assert keeps[9, 202] == (word >= 2 ** 30)
