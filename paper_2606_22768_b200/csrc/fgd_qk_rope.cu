@@ -8,9 +8,11 @@
 // Without weights the backward pass is the transposed rotation alone: the forward kernel with -sin.
 //
 // A lane holds 2 V channels of a head: a chunk of V consecutive ones and the chunk of their partners, so the rotation needs no other lane and the
-// norm log2(lanes) shuffles.  LG lanes make a head, 32 / LG heads a warp.  Of those, gt (the largest power of two that divides the head count)
-// belong to one token, so a lane's cos and sin serve all its heads; CTAs belong to one worker and to q or k, so its weights, and in the
-// backward pass the sums of their gradients, stay in registers.
+// norm log2(lanes) shuffles.  LG lanes make a head, 32 / LG heads a warp.  Of those, gt (the largest power of two that divides both head counts)
+// belong to one token: a warp goes through its tokens' heads gt at a time, and a lane's cos and sin serve all that it has of a token.  It takes all
+// its q first and then its k: so the weights and, in the backward pass, the sums of their gradients (CTAs belong to one worker) stay in
+// registers, of one side at a time.  What the next steps need is on its way meanwhile: activations through a ring in shared memory that each lane
+// fills for itself (cp.async), the next token's cos and sin in registers.
 #include <cmath>
 
 #include "fgd_dtype.cuh"
@@ -24,11 +26,11 @@ namespace {
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxDim = 256;
 
-struct RopeHeads { char* p; int64_t ts, hs; };
+struct RopeHeads { char* p; int64_t ts, hs, step; };      // strides and gt heads, in bytes
 struct RopeSide {
   RopeHeads x, y, g;           // forward: input, output; backward: input, gradient out, gradient in
   const float* w; int64_t w_ld;
-  int heads, gt, ctas;         // gt: lane groups that share a token; CTAs of one worker
+  int batches;                 // of gt heads of a token
 };
 struct RopeArgs {
   RopeSide side[2];
@@ -36,8 +38,9 @@ struct RopeArgs {
   const void* positions; int position_bytes;
   int64_t rows, table_rows;
   int d, rot, lg, pairs;       // lanes of a head; chunk pairs of a head
+  int gt;                      // lane groups that share a token
   float eps, inv_d, turn;      // turn: 1, or -1 for the transposed rotation
-  float* partial;              // backward: [side][worker][cta][d]
+  float* partial;              // backward: [worker][cta][q or k][d]
 };
 
 // V consecutive values as they lie in memory.
@@ -50,6 +53,10 @@ struct Chunk {
     else if constexpr (kBytes == 8) { const uint2 v = __ldcs(reinterpret_cast<const uint2*>(p)); w[0] = v.x; w[1] = v.y; }
     else if constexpr (kBytes == 4) w[0] = __ldcs(reinterpret_cast<const uint32_t*>(p));
     else w[0] = __ldcs(reinterpret_cast<const unsigned short*>(p));
+  }
+  __device__ __forceinline__ void from_shared(uint32_t p) {
+    if constexpr (kBytes == 16) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(p) : "memory");
+    else if constexpr (kBytes == 8) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(p) : "memory");
   }
   __device__ __forceinline__ void store(T* p) const {
     if constexpr (kBytes == 16) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
@@ -123,45 +130,125 @@ __device__ __forceinline__ void load_table(const float* p, float* f) {
   }
 }
 // cos and sin of a token for a lane's channels.  A position outside the tables turns the whole head into NaN: `good` is false.
-template <int V, int NC, bool INTER>
-__device__ __forceinline__ bool load_angles(const RopeArgs& a, const Geometry<V, NC, INTER>& geo, int64_t token, bool real, float (&cs)[NC][V], float (&sn)[NC][V]) {
-  const int64_t pos = real ? position_of(a, token) : 0;
-  const bool good = pos >= 0 && pos < a.table_rows;
+template <int V, int NC>
+struct Angles {
+  float cs[NC][V], sn[NC][V];
+  bool good;
+  template <bool INTER>
+  __device__ __forceinline__ void load(const RopeArgs& a, const Geometry<V, NC, INTER>& geo, int64_t pos) {
+    good = pos >= 0 && pos < a.table_rows;
 #pragma unroll
-  for (int j = 0; j < NC; ++j) {
+    for (int j = 0; j < NC; ++j) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) { cs[j][i] = 1.f; sn[j][i] = 0.f; }
-    if (real && good && geo.turns[j] && geo.has0[j]) {
-      load_table<V>(a.cos + pos * a.cos_ld + geo.at[j], cs[j]);
-      load_table<V>(a.sin + pos * a.sin_ld + geo.at[j], sn[j]);
+      for (int i = 0; i < V; ++i) { cs[j][i] = 1.f; sn[j][i] = 0.f; }
+      if (good && geo.turns[j] && geo.has0[j]) {
+        load_table<V>(a.cos + pos * a.cos_ld + geo.at[j], cs[j]);
+        load_table<V>(a.sin + pos * a.sin_ld + geo.at[j], sn[j]);
+      }
     }
   }
-  return good;
+};
+
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
 }
-// The pairs of a chunk and its partner, turned by +-angle.  Products and sums are rounded one by one: so every form of the rotation that
-// computes in fp32 without contraction agrees with this one to the bit.
+// N tensors' chunk pairs of a step, kDepth - 1 steps ahead.  A lane reads back what it copied itself: no barrier.  A lane without a chunk reads the
+// zeros that it put there first; of a token beyond the last it reads anything, and nothing is made of it.  Values of fewer than 8 bytes (V == 1) are
+// loaded when they are needed.
+template <typename T, int V, int NC, int N>
+struct Feed {
+  static constexpr int kBytes = V * sizeof(T), kDepth = 4;
+  static constexpr bool kRing = kBytes >= 8;
+  static constexpr int kPart = 32 * kBytes, kSlot = N * 2 * kPart, kWarpBytes = kRing ? kDepth * kSlot : 0;
+  uint32_t base, at;      // of the lane's part of a warp's ring; the slot of the current step
+  __device__ __forceinline__ void start(unsigned char* ring, bool has) {
+    if constexpr (kRing) {
+      base = (uint32_t)__cvta_generic_to_shared(ring) + (threadIdx.x / 32) * kWarpBytes + (threadIdx.x & 31) * kBytes;
+      at = 0;
+      if (!has) {
+#pragma unroll
+        for (int i = 0; i < kDepth * N * 2; ++i) asm volatile("st.shared.v2.b32 [%0], {%1, %1};" ::"r"(base + i * kPart), "r"(0) : "memory");
+        if constexpr (kBytes == 16) {
+#pragma unroll
+          for (int i = 0; i < kDepth * N * 2; ++i) asm volatile("st.shared.v2.b32 [%0], {%1, %1};" ::"r"(base + i * kPart + 8), "r"(0) : "memory");
+        }
+      }
+    }
+  }
+  // The step `ahead` behind the current one; kDepth - 1: into the slot of the one before it.
+  template <bool INTER>
+  __device__ __forceinline__ void fetch(const char* const (&p)[N], bool real, bool all, int ahead, const Geometry<V, NC, INTER>& geo) {
+    [[maybe_unused]] const int partner = (geo.c1[0] - geo.c0[0]) * (int)sizeof(T);
+    if constexpr (kRing) {
+      const uint32_t to = base + (at + ahead * kSlot) % kWarpBytes;
+      if (real && geo.has0[0]) {
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+          if (n == 0 || all) {
+            copy_async<kBytes>(to + 2 * n * kPart, p[n]);
+            copy_async<kBytes>(to + (2 * n + 1) * kPart, p[n] + partner);
+          }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+  }
+  __device__ __forceinline__ void wait() {
+    if constexpr (kRing) asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 2) : "memory");
+  }
+  template <bool INTER>
+  __device__ __forceinline__ void get(float (&z)[NC][2 * V], int n, const char* p, bool real, const Geometry<V, NC, INTER>& geo) {
+#pragma unroll
+    for (int j = 0; j < NC; ++j)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        Chunk<T, V> c;
+        if constexpr (kRing) {
+          c.from_shared(base + at + (2 * n + half) * kPart);
+        } else {
+          c.clear();
+          if (real && (half ? geo.has1[j] : geo.has0[j])) c.load(reinterpret_cast<const T*>(p) + (half ? geo.c1[j] : geo.c0[j]) - geo.c0[0]);
+        }
+        c.get(z[j] + half * V);
+      }
+  }
+  __device__ __forceinline__ void next() {
+    if constexpr (kRing) at = (at + kSlot) % kWarpBytes;
+  }
+};
+
+__device__ __forceinline__ float2 two(const float* f) { return make_float2(f[0], f[1]); }
+__device__ __forceinline__ void put(float* f, float2 v) { f[0] = v.x; f[1] = v.y; }
+// The pairs of a chunk and its partner, turned: turn is 1, or -1 for the transposed rotation.  Products and sums are rounded one by one, and every form
+// of the rotation that computes in fp32 without contraction agrees with this one to the bit.  (A sum is written as a product with +-1, which is
+// exact, because the compiler contracts a packed product and a packed sum into one operation; the factor is one that it does not know.)
 template <int V, bool INTER>
 __device__ __forceinline__ void rotate(float (&z)[2 * V], const float (&cs)[V], const float (&sn)[V], float turn) {
+  if constexpr (INTER || V == 1) {
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    float& a = z[INTER ? 2 * i : i];
-    float& b = z[INTER ? 2 * i + 1 : V + i];
-    const float s = turn * sn[i], p = __fsub_rn(__fmul_rn(a, cs[i]), __fmul_rn(b, s)), q = __fadd_rn(__fmul_rn(b, cs[i]), __fmul_rn(a, s));
-    a = p; b = q;
+    for (int i = 0; i < V; ++i) {
+      const float a = z[INTER ? 2 * i : i], b = z[INTER ? 2 * i + 1 : V + i];
+      z[INTER ? 2 * i : i] = fmaf(__fmul_rn(b, sn[i]), -turn, __fmul_rn(a, cs[i]));
+      z[INTER ? 2 * i + 1 : V + i] = fmaf(__fmul_rn(a, sn[i]), turn, __fmul_rn(b, cs[i]));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; i += 2) {
+      const float2 a = two(z + i), b = two(z + V + i), c = two(cs + i), s = two(sn + i);
+      put(z + i, fma2(mul2(b, s), both(-turn), mul2(a, c)));
+      put(z + V + i, fma2(mul2(a, s), both(turn), mul2(b, c)));
+    }
   }
 }
-// Sum over the lanes of a head; all lanes of the warp take part.
-__device__ __forceinline__ float head_sum(float v, int lg) {
-  for (int o = 1; o < lg; o *= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-template <typename T, int V, int NC, bool INTER>
-__device__ __forceinline__ void load_head(Chunk<T, V> (&r)[NC][2], const T* p, bool real, const Geometry<V, NC, INTER>& geo) {
+// Sums over the lanes of a head, a power of two; all lanes of the warp take part.
+template <int N>
+__device__ __forceinline__ void head_sums(float (&v)[N], int lg) {
 #pragma unroll
-  for (int j = 0; j < NC; ++j) {
-    r[j][0].clear(); r[j][1].clear();
-    if (real && geo.has0[j]) r[j][0].load(p + geo.c0[j]);
-    if (real && geo.has1[j]) r[j][1].load(p + geo.c1[j]);
+  for (int o = 1; o < 32; o *= 2) {
+    if (o >= lg) break;
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n] += __shfl_xor_sync(0xffffffffu, v[n], o);
   }
 }
 template <typename T, int V, int NC, bool INTER>
@@ -170,202 +257,232 @@ __device__ __forceinline__ void store_head(const float (&z)[NC][2 * V], T* p, bo
   for (int j = 0; j < NC; ++j) {
     Chunk<T, V> c;
     c.set(z[j]);
-    if (real && geo.has0[j]) c.store(p + geo.c0[j]);
+    if (real && geo.has0[j]) c.store(p + geo.c0[j] - geo.c0[0]);
     c.set(z[j] + V);
-    if (real && geo.has1[j]) c.store(p + geo.c1[j]);
+    if (real && geo.has1[j]) c.store(p + geo.c1[j] - geo.c0[0]);
   }
 }
 template <int V, int NC, bool INTER>
-__device__ __forceinline__ void load_weights(const RopeSide& s, int worker, const Geometry<V, NC, INTER>& geo, float (&w)[NC][2 * V]) {
+__device__ __forceinline__ void load_weights(const float* w, const Geometry<V, NC, INTER>& geo, float (&f)[NC][2 * V]) {
 #pragma unroll
   for (int j = 0; j < NC; ++j)
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      w[j][i] = geo.has0[j] ? __ldg(s.w + worker * s.w_ld + geo.c0[j] + i) : 0.f;
-      w[j][V + i] = geo.has1[j] ? __ldg(s.w + worker * s.w_ld + geo.c1[j] + i) : 0.f;
+      f[j][i] = geo.has0[j] ? __ldg(w + geo.c0[j] + i) : 0.f;
+      f[j][V + i] = geo.has1[j] ? __ldg(w + geo.c1[j] + i) : 0.f;
     }
 }
-
-// UH: heads of a lane in flight at once.
-template <typename T, int V, int NC, int UH, bool INTER>
-__global__ void __launch_bounds__(kThreads) rope_forward_kernel(const RopeArgs a) {
-  const bool is_k = (int)blockIdx.x >= a.side[0].ctas;
-  const RopeSide& s = a.side[is_k];
-  const int cta = blockIdx.x - (is_k ? a.side[0].ctas : 0), worker = blockIdx.y, lane = threadIdx.x & 31, group = lane / a.lg;
-  const int tokens = 32 / a.lg / s.gt;      // of a warp at once
-  const Geometry<V, NC, INTER> geo(lane % a.lg, a);
-  const bool norm = s.w != nullptr;
-  float w[NC][2 * V];
-  if (norm) load_weights(s, worker, geo, w);
-  const T* x = reinterpret_cast<const T*>(s.x.p);
-  T* y = reinterpret_cast<T*>(s.y.p);
-  for (int64_t t0 = (int64_t)(cta * kWarps + threadIdx.x / 32) * tokens; t0 < a.rows; t0 += (int64_t)s.ctas * kWarps * tokens) {
-    const int64_t local = t0 + group / s.gt, token = worker * a.rows + local;
-    const bool real = local < a.rows;
-    float cs[NC][V], sn[NC][V];
-    const bool good = load_angles(a, geo, token, real, cs, sn);
-    for (int h0 = group % s.gt; h0 < s.heads; h0 += s.gt * UH) {      // gt divides the heads: the groups leave the loop together
-      Chunk<T, V> raw[UH][NC][2];
-#pragma unroll
-      for (int u = 0; u < UH; ++u) load_head<T, V, NC, INTER>(raw[u], x + token * s.x.ts + (h0 + u * s.gt) * s.x.hs, real && h0 + u * s.gt < s.heads, geo);
-#pragma unroll
-      for (int u = 0; u < UH; ++u) {
-        if (h0 + u * s.gt >= s.heads) break;
-        float z[NC][2 * V];
-        float ss = 0.f;
-#pragma unroll
-        for (int j = 0; j < NC; ++j) {
-          raw[u][j][0].get(z[j]);
-          raw[u][j][1].get(z[j] + V);
-        }
-        if (norm) {
-#pragma unroll
-          for (int j = 0; j < NC; ++j)
-#pragma unroll
-            for (int i = 0; i < 2 * V; ++i) ss = fmaf(z[j][i], z[j][i], ss);
-          const float r = rsqrtf(fmaf(head_sum(ss, a.lg), a.inv_d, a.eps));
-#pragma unroll
-          for (int j = 0; j < NC; ++j)
-#pragma unroll
-            for (int i = 0; i < 2 * V; ++i) z[j][i] *= r * w[j][i];
-        }
-#pragma unroll
-        for (int j = 0; j < NC; ++j) {
-          if (geo.turns[j]) rotate<V, INTER>(z[j], cs[j], sn[j], a.turn);
-          if (!good) {
-#pragma unroll
-            for (int i = 0; i < 2 * V; ++i) z[j][i] = __int_as_float(0x7fffffff);
-          }
-        }
-        store_head<T, V, NC, INTER>(z, y + token * s.y.ts + (h0 + u * s.gt) * s.y.hs, real, geo);
-      }
-    }
-  }
-}
-
-// With weights; UH as above.
-template <typename T, int V, int NC, int UH, bool INTER>
-__global__ void __launch_bounds__(kThreads) rope_backward_kernel(const RopeArgs a) {
-  __shared__ float sums[kWarps][kMaxDim];
-  const bool is_k = (int)blockIdx.x >= a.side[0].ctas;
-  const RopeSide& s = a.side[is_k];
-  const int cta = blockIdx.x - (is_k ? a.side[0].ctas : 0), worker = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x / 32, group = lane / a.lg;
-  const int tokens = 32 / a.lg / s.gt;
-  const Geometry<V, NC, INTER> geo(lane % a.lg, a);
-  float w[NC][2 * V], dw[NC][2 * V];
-  const bool norm = s.w != nullptr;      // (of one side only: the other is the rotation alone)
+template <int V, int NC>
+__device__ __forceinline__ void poison(float (&z)[NC][2 * V]) {
 #pragma unroll
   for (int j = 0; j < NC; ++j)
 #pragma unroll
-    for (int i = 0; i < 2 * V; ++i) w[j][i] = dw[j][i] = 0.f;
-  if (norm) load_weights(s, worker, geo, w);
-  let_next_start();
-  const T* x = reinterpret_cast<const T*>(s.x.p);
-  const T* g = reinterpret_cast<const T*>(s.g.p);
-  T* y = reinterpret_cast<T*>(s.y.p);
-  for (int64_t t0 = (int64_t)(cta * kWarps + warp) * tokens; t0 < a.rows; t0 += (int64_t)s.ctas * kWarps * tokens) {
-    const int64_t local = t0 + group / s.gt, token = worker * a.rows + local;
-    const bool real = local < a.rows;
-    float cs[NC][V], sn[NC][V];
-    const bool good = load_angles(a, geo, token, real, cs, sn);
-    for (int h0 = group % s.gt; h0 < s.heads; h0 += s.gt * UH) {
-      Chunk<T, V> rx[UH][NC][2], rg[UH][NC][2];
+    for (int i = 0; i < 2 * V; ++i) z[j][i] = __int_as_float(0x7fffffff);
+}
+
+// GRAD: the backward pass with weights.  Otherwise the forward pass, or the transposed rotation alone.
+template <typename T, int V, int NC, bool INTER, bool GRAD>
+__global__ void __launch_bounds__(kThreads, 2) rope_kernel(const __grid_constant__ RopeArgs a) {
+  constexpr int N = GRAD ? 2 : 1;      // tensors that are read: the gradient, x; or x alone
+  using Ring = Feed<T, V, NC, N>;
+  extern __shared__ __align__(16) unsigned char ring[];
+  __shared__ float sums[GRAD ? 2 : 1][GRAD ? kWarps : 1][kMaxDim];
+  const int worker = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x / 32, group = lane / a.lg, sub = group % a.gt;
+  const uint32_t tokens = 32 / a.lg / a.gt, mine = group / a.gt;      // tokens of a warp at once, this lane's among them
+  const uint32_t rows = (uint32_t)a.rows, stride = gridDim.x * kWarps * tokens, first = (blockIdx.x * kWarps + warp) * tokens;
+  const int64_t base = worker * a.rows + mine;
+  const Geometry<V, NC, INTER> geo(lane % a.lg, a);
+  if constexpr (GRAD) let_next_start();      // the sums' CTAs wait for this kernel's end on the SMs
+  // The step that is fetched next, kDepth - 1 ahead: side, first token of the warp's group, batch, addresses.  (An address moves on by a constant
+  // within a token; worked out anew in every step they were a third of the kernel's instructions.)
+  int ahead_side = first < rows ? 0 : 2, ahead_b = 0;
+  uint32_t ahead_t0 = first;
+  const char* in[N];
+  auto at = [&](const RopeHeads& h, uint32_t t0) { return h.p + (base + t0) * h.ts + sub * h.hs + geo.c0[0] * (int)sizeof(T); };      // of a lane's first channel
+  auto seek = [&](const RopeSide& s) {
+    in[0] = at(GRAD ? s.g : s.x, ahead_t0);
+    if constexpr (GRAD) in[N - 1] = at(s.x, ahead_t0);
+  };
+  auto advance = [&] {
+    if (ahead_side == 2) return;
+    const RopeSide& s = a.side[ahead_side];
+    if (++ahead_b < s.batches) {
+      in[0] += GRAD ? s.g.step : s.x.step;
+      if constexpr (GRAD) in[N - 1] += s.x.step;
+      return;
+    }
+    ahead_b = 0;
+    ahead_t0 += stride;
+    if (ahead_t0 >= rows) {
+      ahead_t0 = first;
+      if (++ahead_side == 1 && a.side[1].batches == 0) ahead_side = 2;
+    }
+    if (ahead_side < 2) seek(a.side[ahead_side]);
+  };
+  Ring feed;
+  auto fetch = [&](int steps) {
+    const bool real = ahead_side < 2 && ahead_t0 + mine < rows;
+    feed.fetch(in, real, real && a.side[ahead_side & 1].w != nullptr, steps, geo);      // (without weights x may be absent)
+  };
+  seek(a.side[0]);
+  feed.start(ring, geo.has0[0]);
+  if constexpr (Ring::kRing) {
 #pragma unroll
-      for (int u = 0; u < UH; ++u) {
-        const int h = h0 + u * s.gt;
-        load_head<T, V, NC, INTER>(rg[u], g + token * s.g.ts + h * s.g.hs, real && h < s.heads, geo);
-        load_head<T, V, NC, INTER>(rx[u], x + token * s.x.ts + h * s.x.hs, real && norm && h < s.heads, geo);
+    for (int i = 0; i < Ring::kDepth - 1; ++i) {
+      fetch(i);
+      advance();
+    }
+  }
+#pragma unroll 1
+  for (int side = 0; side < 2; ++side) {
+    const RopeSide& s = a.side[side];
+    if (s.batches == 0) break;
+    const bool norm = s.w != nullptr;      // (of the gradient's kernel: one of the sides may be the rotation alone)
+    float w[NC][2 * V], dw[NC][2 * V];
+    if (norm) load_weights(s.w + worker * s.w_ld, geo, w);
+#pragma unroll
+    for (int j = 0; j < NC; ++j)
+#pragma unroll
+      for (int i = 0; i < 2 * V; ++i) dw[j][i] = 0.f;
+    // Forward: positions two tokens ahead, cos and sin one.  (The backward pass has no registers for that: with them 126 us, without 108, for
+    // 8 x 4096 tokens of 20 heads of 128.)
+    auto position = [&](uint32_t t0) { return t0 + mine < rows ? position_of(a, base + t0) : (int64_t)-1; };
+    Angles<V, NC> turn, next;
+    int64_t pos = -1;
+    if constexpr (!GRAD) {
+      next.load(a, geo, position(first));
+      pos = position(first + stride);
+    }
+    for (uint32_t t0 = first; t0 < rows; t0 += stride) {
+      const bool real = t0 + mine < rows;
+      if constexpr (GRAD) {
+        turn.load(a, geo, position(t0));
+      } else {
+        turn = next;
+        next.load(a, geo, pos);
+        pos = position(t0 + 2 * stride);
       }
-#pragma unroll
-      for (int u = 0; u < UH; ++u) {
-        const int h = h0 + u * s.gt;
-        if (h >= s.heads) break;
+      char* out = at(s.y, t0);
+#pragma unroll 2
+      for (int b = 0; b < s.batches; ++b, out += s.y.step) {
+        feed.wait();
         float z[NC][2 * V], v[NC][2 * V];
-        float ss = 0.f, sg = 0.f;
+        feed.get(z, 0, in[0], real, geo);
+        if constexpr (GRAD) feed.get(v, 1, in[N - 1], real && norm, geo);
+        if constexpr (Ring::kRing) fetch(Ring::kDepth - 1);
+        advance();
+        feed.next();
+        if constexpr (!GRAD) {
+          if (norm) {
+            float2 ss = both(0.f);
 #pragma unroll
-        for (int j = 0; j < NC; ++j) {
-          rg[u][j][0].get(z[j]); rg[u][j][1].get(z[j] + V);
-          rx[u][j][0].get(v[j]); rx[u][j][1].get(v[j] + V);
-          if (geo.turns[j]) rotate<V, INTER>(z[j], cs[j], sn[j], a.turn);
-          if (!good) {
+            for (int j = 0; j < NC; ++j)
 #pragma unroll
-            for (int i = 0; i < 2 * V; ++i) z[j][i] = __int_as_float(0x7fffffff);
+              for (int i = 0; i < 2 * V; i += 2) ss = fma2(two(z[j] + i), two(z[j] + i), ss);
+            float sum[1] = {ss.x + ss.y};
+            head_sums(sum, a.lg);
+            const float2 r = both(rsqrtf(fmaf(sum[0], a.inv_d, a.eps)));
+#pragma unroll
+            for (int j = 0; j < NC; ++j)
+#pragma unroll
+              for (int i = 0; i < 2 * V; i += 2) put(z[j] + i, mul2(two(z[j] + i), mul2(r, two(w[j] + i))));
           }
+        }
+#pragma unroll
+        for (int j = 0; j < NC; ++j)
+          if (geo.turns[j]) rotate<V, INTER>(z[j], turn.cs[j], turn.sn[j], a.turn);
+        if (!turn.good) poison<V, NC>(z);
+        if constexpr (GRAD) {
+          if (norm) {
+            // u = dz x: dw += u r, dx = r dz w - k x, k = r^3 mean(u w)
+            float2 ss = both(0.f), sg = both(0.f);
+#pragma unroll
+            for (int j = 0; j < NC; ++j)
+#pragma unroll
+              for (int i = 0; i < 2 * V; i += 2) {
+                const float2 x = two(v[j] + i);
+                ss = fma2(x, x, ss);
+                sg = fma2(mul2(two(z[j] + i), x), two(w[j] + i), sg);
+              }
+            float sum[2] = {ss.x + ss.y, sg.x + sg.y};
+            head_sums(sum, a.lg);
+            const float r = rsqrtf(fmaf(sum[0], a.inv_d, a.eps)), k = r * r * (r * sum[1] * a.inv_d);
+            if (real) {
+#pragma unroll
+              for (int j = 0; j < NC; ++j)
+#pragma unroll
+                for (int i = 0; i < 2 * V; i += 2) {
+                  const float2 x = two(v[j] + i), dz = two(z[j] + i);
+                  put(dw[j] + i, fma2(mul2(dz, x), both(r), two(dw[j] + i)));
+                  put(z[j] + i, fma2(both(r), mul2(dz, two(w[j] + i)), mul2(both(-k), x)));
+                }
+            }
+          }
+        }
+        store_head<T, V, NC, INTER>(z, reinterpret_cast<T*>(out), real, geo);
+      }
+    }
+    if constexpr (GRAD) {
+      if (norm) {
+#pragma unroll
+        for (int j = 0; j < NC; ++j)
 #pragma unroll
           for (int i = 0; i < 2 * V; ++i) {
-            ss = fmaf(v[j][i], v[j][i], ss);
-            sg = fmaf(z[j][i] * w[j][i], v[j][i], sg);
+            float t = dw[j][i];
+            for (int o = a.lg; o < 32; o *= 2) t += __shfl_xor_sync(0xffffffffu, t, o);
+            const bool has = i < V ? geo.has0[j] : geo.has1[j];
+            if (group == 0 && has) sums[side][warp][i < V ? geo.c0[j] + i : geo.c1[j] + i - V] = t;
           }
-        }
-        if (norm) {
-          ss = head_sum(ss, a.lg);
-          sg = head_sum(sg, a.lg);
-          const float r = rsqrtf(fmaf(ss, a.inv_d, a.eps)), k = r * r * (r * sg * a.inv_d);
-#pragma unroll
-          for (int j = 0; j < NC; ++j)
-#pragma unroll
-            for (int i = 0; i < 2 * V; ++i) {
-              const float t = z[j][i] * r;
-              dw[j][i] = fmaf(t, v[j][i], dw[j][i]);
-              z[j][i] = fmaf(t, w[j][i], -k * v[j][i]);
-            }
-        }
-        store_head<T, V, NC, INTER>(z, y + token * s.y.ts + h * s.y.hs, real, geo);
       }
     }
   }
-  if (!norm) return;      // (the whole CTA)
+  if constexpr (GRAD) {
+    __syncthreads();
 #pragma unroll
-  for (int j = 0; j < NC; ++j)
+    for (int side = 0; side < 2; ++side) {
+      if (!a.side[side].w) continue;
+      float* out = a.partial + (((int64_t)worker * gridDim.x + blockIdx.x) * 2 + side) * a.d;
+      for (int c = threadIdx.x; c < a.d; c += kThreads) {
+        float t = sums[side][0][c];
 #pragma unroll
-    for (int i = 0; i < 2 * V; ++i) {
-      float t = dw[j][i];
-      for (int o = a.lg; o < 32; o *= 2) t += __shfl_xor_sync(0xffffffffu, t, o);
-      const bool has = i < V ? geo.has0[j] : geo.has1[j];
-      if (group == 0 && has) sums[warp][i < V ? geo.c0[j] + i : geo.c1[j] + i - V] = t;
+        for (int i = 1; i < kWarps; ++i) t += sums[side][i][c];
+        out[c] = t;
+      }
     }
-  __syncthreads();
-  float* out = a.partial + ((is_k ? (int64_t)gridDim.y * a.side[0].ctas : 0) + (int64_t)worker * s.ctas + cta) * a.d;
-  for (int c = threadIdx.x; c < a.d; c += kThreads) {
-    float t = sums[0][c];
-#pragma unroll
-    for (int i = 1; i < kWarps; ++i) t += sums[i][c];
-    out[c] = t;
   }
 }
 
 // dw of a worker and side: its CTAs' sums, eight at a time added in order, 32 channels a CTA.
-struct RopeSums { const float* partial; float* dw[2]; int64_t ld[2]; int ctas[2], d; };
+struct RopeSums { const float* partial; float* dw[2]; int64_t ld[2]; int ctas, d; };
 __global__ void __launch_bounds__(256) rope_sums_kernel(const RopeSums a) {
   wait_for_previous();
   __shared__ float buf[8][32];
   const int lane = threadIdx.x & 31, part = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, worker = blockIdx.y, side = blockIdx.z;
-  if (!a.dw[side]) return;
-  const float* p = a.partial + ((side ? (int64_t)gridDim.y * a.ctas[0] : 0) + (int64_t)worker * a.ctas[side]) * a.d;
+  float* dw = side ? a.dw[1] : a.dw[0];
+  if (!dw) return;
   float t = 0.f;
   if (c < a.d)
-    for (int i = part; i < a.ctas[side]; i += 8) t += p[(int64_t)i * a.d + c];
+    for (int i = part; i < a.ctas; i += 8) t += a.partial[(((int64_t)worker * a.ctas + i) * 2 + side) * a.d + c];
   buf[part][lane] = t;
   __syncthreads();
   if (part != 0 || c >= a.d) return;
 #pragma unroll
   for (int i = 1; i < 8; ++i) t += buf[i][lane];
-  a.dw[side][worker * a.ld[side] + c] = t;
+  dw[worker * (side ? a.ld[1] : a.ld[0]) + c] = t;
 }
 
 // ---- host
 constexpr int kCtasPerSm = 2;      // of the persistent grid
 
-int64_t tokens_per_warp(int lg, int gt) { return 32 / lg / gt; }
-int group_of(int heads, int groups) {      // the largest power of two that divides the heads, at most `groups`
+// The largest power of two that divides both head counts, at most `groups`.
+int group_of(int q_heads, int k_heads, int groups) {
   int g = 1;
-  while (g < groups && heads % (2 * g) == 0) g *= 2;
+  while (g < groups && q_heads % (2 * g) == 0 && k_heads % (2 * g) == 0) g *= 2;
   return g;
 }
-// CTAs of one worker for a side with `heads` of all `total` heads: its share of the SMs' places, and no more than there is work for.
-int ctas_for(int64_t workers, int64_t rows, int heads, int total, int64_t warp_tokens) {
-  if (heads == 0) return 0;
-  int64_t c = (int64_t)sm_count() * kCtasPerSm * heads / ((int64_t)total * workers);
+// CTAs of one worker: its share of the SMs' places, and no more than there is work for.
+int ctas_for(int64_t workers, int64_t rows, int64_t warp_tokens) {
+  int64_t c = (int64_t)sm_count() * kCtasPerSm / workers;
   const int64_t most = (rows + kWarps * warp_tokens - 1) / (kWarps * warp_tokens);
   if (c > most) c = most;
   return (int)(c < 1 ? 1 : c);
@@ -377,20 +494,22 @@ bool vector_of(const void* p, int64_t s0, int64_t s1, int bytes, int vec) {
 
 struct Launch { int vec, lg, pairs; };
 
-int64_t workspace_bytes(int workers, int d) { return ((int64_t)sm_count() * kCtasPerSm + 2 * (int64_t)workers) * d * (int64_t)sizeof(float); }
+int64_t workspace_bytes(int workers, int d) { return ((int64_t)sm_count() * kCtasPerSm + workers) * 2 * d * (int64_t)sizeof(float); }
 
-template <typename T, int V, int NC>
-cudaError_t launch(const RopeArgs& a, int workers, bool sums, bool inter, cudaStream_t st) {
-  const dim3 grid(a.side[0].ctas + a.side[1].ctas, workers);
-  constexpr int UF = NC > 1 ? 1 : 4, UB = NC > 1 ? 1 : 2;
-  if (sums) {
-    if (inter) rope_backward_kernel<T, V, NC, UB, true><<<grid, kThreads, 0, st>>>(a);
-    else rope_backward_kernel<T, V, NC, UB, false><<<grid, kThreads, 0, st>>>(a);
-  } else {
-    if (inter) rope_forward_kernel<T, V, NC, UF, true><<<grid, kThreads, 0, st>>>(a);
-    else rope_forward_kernel<T, V, NC, UF, false><<<grid, kThreads, 0, st>>>(a);
+template <typename T, int V, int NC, bool INTER, bool GRAD>
+cudaError_t start(const RopeArgs& a, int workers, int ctas, cudaStream_t st) {
+  constexpr size_t smem = kWarps * Feed<T, V, NC, GRAD ? 2 : 1>::kWarpBytes;
+  cudaError_t e = smem > 32 * 1024 ? allow_smem<rope_kernel<T, V, NC, INTER, GRAD>>(smem) : cudaSuccess;
+  if (e == cudaSuccess) {
+    rope_kernel<T, V, NC, INTER, GRAD><<<dim3(ctas, workers), kThreads, smem, st>>>(a);
+    e = cudaGetLastError();
   }
-  return cudaGetLastError();
+  return e;
+}
+template <typename T, int V, int NC>
+cudaError_t launch(const RopeArgs& a, int workers, int ctas, bool grad, bool inter, cudaStream_t st) {
+  if (grad) return inter ? start<T, V, NC, true, true>(a, workers, ctas, st) : start<T, V, NC, false, true>(a, workers, ctas, st);
+  return inter ? start<T, V, NC, true, false>(a, workers, ctas, st) : start<T, V, NC, false, false>(a, workers, ctas, st);
 }
 
 struct Mat { const char* name; const void* p; int64_t rows, width, ld; bool output; };
@@ -519,18 +638,12 @@ int run_rope(const fgd_qk_rope_args* b, bool backward, int device, void* stream)
   c.partial = a.partial; c.d = d;
   for (int i = 0; i < 2; ++i) {
     RopeSide& s = a.side[i];
-    auto at = [](const fgd_heads& t) { return RopeHeads{static_cast<char*>(t.p), t.token_stride, t.head_stride}; };
+    auto at = [&](const fgd_heads& t) { return RopeHeads{static_cast<char*>(t.p), t.token_stride * bytes, t.head_stride * bytes, 0}; };
     s.x = at(sums ? *x[i] : *in[i]); s.y = at(*out[i]); s.g = at(*in[i]);
     s.w = norm[i] ? static_cast<const float*>(w[i]->p) : nullptr;
     s.w_ld = w[i]->ld;
-    s.heads = heads[i];
-    if (T > 0) {
-      s.gt = heads[i] ? group_of(heads[i], 32 / l.lg) : 1;
-      s.ctas = ctas_for(b->workers, b->rows, heads[i], heads[0] + heads[1], tokens_per_warp(l.lg, s.gt));
-    }
     c.dw[i] = norm[i] ? static_cast<float*>(dw[i]->p) : nullptr;
     c.ld[i] = dw[i]->ld;
-    c.ctas[i] = s.ctas;
   }
   cudaError_t e = cudaSuccess;
   if (T > 0) {
@@ -538,14 +651,21 @@ int run_rope(const fgd_qk_rope_args* b, bool backward, int device, void* stream)
     a.positions = has_positions ? b->positions : nullptr; a.position_bytes = b->position_bytes;
     a.rows = b->rows; a.table_rows = b->table_rows;
     a.d = d; a.rot = rot; a.lg = l.lg; a.pairs = l.pairs;
+    a.gt = group_of(heads[0], heads[1], 32 / l.lg);
+    for (int i = 0; i < 2; ++i) {
+      RopeSide& side = a.side[i];
+      side.batches = heads[i] / a.gt;
+      for (RopeHeads* h : {&side.x, &side.y, &side.g}) h->step = h->hs * a.gt;
+    }
+    c.ctas = ctas_for(b->workers, b->rows, 32 / l.lg / a.gt);
     a.eps = (float)b->eps; a.inv_d = 1.f / (float)d; a.turn = backward ? -1.f : 1.f;
     const bool inter = b->interleaved != 0;
     auto by_vec = [&](auto zero) {
       using E = decltype(zero);
       if constexpr (sizeof(E) == 2)
-        if (l.vec == 8) return launch<E, 8, 1>(a, b->workers, sums, inter, st);
-      if (l.vec == 4) return launch<E, 4, 1>(a, b->workers, sums, inter, st);
-      return launch<E, 1, 4>(a, b->workers, sums, inter, st);
+        if (l.vec == 8) return launch<E, 8, 1>(a, b->workers, c.ctas, sums, inter, st);
+      if (l.vec == 4) return launch<E, 4, 1>(a, b->workers, c.ctas, sums, inter, st);
+      return launch<E, 1, 4>(a, b->workers, c.ctas, sums, inter, st);
     };
     switch (b->dtype) {
       case FGD_F32: e = by_vec(float{}); break;
