@@ -5,7 +5,6 @@
 // The backward pass is the same call on the gradient.  A function of the row and column, not of the address: any width, stride, launch shape
 // and device gives the same mask.
 //
-// A thread takes 16 bytes: two groups of four words for 16-bit activations, one for fp32.
 #include <cmath>
 
 #include "fgd_dtype.cuh"
@@ -29,65 +28,103 @@ struct DropoutArgs {
   float scale;
 };
 
-__device__ __forceinline__ uint4 philox(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0, uint32_t k1) {
-#pragma unroll
-  for (int i = 0; i < 7; ++i) {
-    const uint64_t p = (uint64_t)c0 * 0xD2511F53u, q = (uint64_t)c2 * 0xCD9E8D57u;
-    c0 = (uint32_t)(q >> 32) ^ c1 ^ k0;
-    c1 = (uint32_t)q;
-    c2 = (uint32_t)(p >> 32) ^ c3 ^ k1;
-    c3 = (uint32_t)p;
-    k0 += 0x9E3779B9u;
-    k1 += 0xBB67AE85u;
+// The generator for one row.  Of the first two rounds' four products one depends on the offset alone and one on the row alone: they are made once.
+struct RowWords {
+  uint32_t low1, high2, low2, c3, k0, k1;
+  __device__ __forceinline__ RowWords(uint32_t row, uint64_t offset, const DropoutArgs& a) : c3((uint32_t)(offset >> 32)), k0(a.k0), k1(a.k1) {
+    const uint64_t q = (uint64_t)(uint32_t)offset * kM1;
+    low1 = (uint32_t)q;
+    const uint64_t p = (uint64_t)((uint32_t)(q >> 32) ^ row ^ k0) * kM0;
+    high2 = (uint32_t)(p >> 32);
+    low2 = (uint32_t)p;
   }
-  return make_uint4(c0, c1, c2, c3);
-}
+  // the four words of columns 4 c0 .. 4 c0 + 3
+  __device__ __forceinline__ uint4 words(uint32_t group) const {
+    const uint64_t p = (uint64_t)group * kM0;
+    const uint64_t q = (uint64_t)((uint32_t)(p >> 32) ^ c3 ^ k1) * kM1;
+    uint32_t a = (uint32_t)(q >> 32) ^ low1 ^ (k0 + kW0), b = (uint32_t)q, c = high2 ^ (uint32_t)p ^ (k1 + kW1), d = low2;
+#pragma unroll
+    for (uint32_t i = 2; i < 7; ++i) {
+      const uint64_t s = (uint64_t)a * kM0, t = (uint64_t)c * kM1;
+      a = (uint32_t)(t >> 32) ^ b ^ (k0 + i * kW0);
+      b = (uint32_t)t;
+      c = (uint32_t)(s >> 32) ^ d ^ (k1 + i * kW1);
+      d = (uint32_t)s;
+    }
+    return make_uint4(a, b, c, d);
+  }
 
-// The values of a unit of V columns from column c of row r on.
+ private:
+  static constexpr uint32_t kM0 = 0xD2511F53u, kM1 = 0xCD9E8D57u, kW0 = 0x9E3779B9u, kW1 = 0xBB67AE85u;
+};
+
+// The values of V columns from column c on.
 template <int V>
-__device__ __forceinline__ Vals<V> drop(const Vals<V>& x, uint32_t c, uint32_t r, uint64_t offset, const DropoutArgs& a) {
+__device__ __forceinline__ Vals<V> drop(const Vals<V>& x, uint32_t c, const RowWords& row, const DropoutArgs& a) {
   Vals<V> y;
 #pragma unroll
   for (int g = 0; g < V / 4; ++g) {
-    const uint4 w = philox(c / 4 + g, r, (uint32_t)offset, (uint32_t)(offset >> 32), a.k0, a.k1);
-    y.v[4 * g] = w.x >= a.threshold ? x.v[4 * g] * a.scale : 0.f;
-    y.v[4 * g + 1] = w.y >= a.threshold ? x.v[4 * g + 1] * a.scale : 0.f;
-    y.v[4 * g + 2] = w.z >= a.threshold ? x.v[4 * g + 2] * a.scale : 0.f;
-    y.v[4 * g + 3] = w.w >= a.threshold ? x.v[4 * g + 3] * a.scale : 0.f;
+    const uint4 w = row.words(c / 4 + g);
+    const float2 lo = mul2(x.pair(2 * g), both(a.scale)), hi = mul2(x.pair(2 * g + 1), both(a.scale));
+    y.v[4 * g] = w.x >= a.threshold ? lo.x : 0.f;
+    y.v[4 * g + 1] = w.y >= a.threshold ? lo.y : 0.f;
+    y.v[4 * g + 2] = w.z >= a.threshold ? hi.x : 0.f;
+    y.v[4 * g + 3] = w.w >= a.threshold ? hi.y : 0.f;
   }
   return y;
 }
 
-// SHIFTED: rows that start off the 16-byte boundaries, or do not end on one.
-template <typename T, bool SHIFTED>
+__device__ __forceinline__ uint64_t offset_of(const DropoutArgs& a) { return a.offset + (a.counter ? (uint64_t)__ldg(a.counter) : 0u); }
+
+// Rows on 16-byte boundaries: a warp takes strips of kStrip x 32 units of 16 bytes of a row.  32768 x 4096 bf16: 86 us, 95 % of the copy peak (with one
+// unit a thread and nothing shared between them 106 us: bound by the generator's instructions).
+constexpr int kStrip = 4;
+template <typename T>
 __global__ void __launch_bounds__(kThreads) dropout_kernel(const DropoutArgs a) {
   constexpr int V = 16 / sizeof(T);
+  const uint64_t offset = offset_of(a);
+  const int lane = threadIdx.x & 31, strips = (int)((a.width + 32 * kStrip * V - 1) / (32 * kStrip * V));
+  const int64_t total = a.rows * strips, stride = (int64_t)gridDim.x * (kThreads / 32);
+  int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / 32;
+  Walk w(i, stride, strips);
+  for (; i < total; i += stride, w.next()) {
+    const int64_t c0 = ((int64_t)w.unit * (32 * kStrip) + lane) * V;
+    const T* x = reinterpret_cast<const T*>(a.x) + w.row * a.ld_x + c0;
+    T* out = reinterpret_cast<T*>(a.out) + w.row * a.ld_out + c0;
+    ActPack<T, V> raw[kStrip];
+#pragma unroll
+    for (int k = 0; k < kStrip; ++k)
+      if (c0 + k * 32 * V < a.width) raw[k] = load_stream<T, V>(x + k * 32 * V);
+    const RowWords row((uint32_t)w.row, offset, a);
+#pragma unroll
+    for (int k = 0; k < kStrip; ++k)
+      if (c0 + k * 32 * V < a.width) store_stream<T, V>(out + k * 32 * V, round_to<T, V>(drop<V>(unpack<T, V>(raw[k]), (uint32_t)(c0 + k * 32 * V), row, a)));
+  }
+}
+
+// Rows that start or end anywhere, and narrow ones: units of 16 values, moved with shifts (fgd_units.cuh).  5003 x 4097 fp32: 35 us, 71 % of the copy
+// peak; bf16 54 %: what the shifts and the generator cost in instructions.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) dropout_shifted_kernel(const DropoutArgs a) {
+  constexpr int V = 16;
+  const uint64_t offset = offset_of(a);
   const int units = (int)((a.width + V - 1) / V);
-  const int64_t total = a.rows * units, stride = (int64_t)gridDim.x * kThreads;
-  const uint64_t offset = a.offset + (a.counter ? (uint64_t)*a.counter : 0u);
+  const int64_t total = a.rows * units, padded = (total + 31) / 32 * 32, stride = (int64_t)gridDim.x * kThreads;      // whole warps stay for the shuffles
   const T* x = reinterpret_cast<const T*>(a.x);
+  const T* end = x + (a.rows - 1) * a.ld_x + a.width;
   T* out = reinterpret_cast<T*>(a.out);
   int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
   Walk w(i, stride, units);
-  if constexpr (SHIFTED) {
-    const T* end = x + (a.rows - 1) * a.ld_x + a.width;
-    const int64_t padded = (total + 31) / 32 * 32;      // whole warps stay for the shuffles
-    for (; i < padded; i += stride, w.next()) {
-      const ShiftedUnit<V> u(w, i < total, a.width);
-      const Vals<V> v = load_shifted<T, V>(x + w.row * a.ld_x + u.c, u, x, end);
-      store_shifted<T, V>(out + w.row * a.ld_out + u.c, u, drop<V>(v, (uint32_t)u.c, (uint32_t)w.row, offset, a));
-    }
-  } else {
-    for (; i < total; i += stride, w.next()) {
-      const int64_t c = (int64_t)w.unit * V;
-      const Vals<V> v = unpack<T, V>(load_stream<T, V>(x + w.row * a.ld_x + c));
-      store_stream<T, V>(out + w.row * a.ld_out + c, round_to<T, V>(drop<V>(v, (uint32_t)c, (uint32_t)w.row, offset, a)));
-    }
+  for (; i < padded; i += stride, w.next()) {
+    const ShiftedUnit<V> u(w, i < total, a.width);
+    const Vals<V> v = load_shifted<T, V>(x + w.row * a.ld_x + u.c, u, x, end);
+    const RowWords row((uint32_t)w.row, offset, a);
+    store_shifted<T, V>(out + w.row * a.ld_out + u.c, u, drop<V>(v, (uint32_t)u.c, row, a));
   }
 }
 
 template <auto KERNEL>
-cudaError_t go(const DropoutArgs& a, int64_t units, int waves, cudaStream_t st) {
+cudaError_t go(const DropoutArgs& a, int64_t threads, int waves, cudaStream_t st) {
   static int cached[64] = {};
   int dev = 0, fit = 0;
   const bool known = cudaGetDevice(&dev) == cudaSuccess && dev < 64;
@@ -96,7 +133,7 @@ cudaError_t go(const DropoutArgs& a, int64_t units, int waves, cudaStream_t st) 
     if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&fit, KERNEL, kThreads, 0) != cudaSuccess || fit < 1) fit = 1;
     if (known) cached[dev] = fit;
   }
-  const int64_t want = (units + kThreads - 1) / kThreads, most = (int64_t)sm_count() * fit * waves;
+  const int64_t want = (threads + kThreads - 1) / kThreads, most = (int64_t)sm_count() * fit * waves;
   KERNEL<<<(unsigned)(want < most ? want : most), kThreads, 0, st>>>(a);
   return cudaGetLastError();
 }
@@ -132,13 +169,15 @@ extern "C" int fgd_dropout(int device, int dtype, int64_t rows, int64_t width, c
   a.threshold = t > 4294967295.0 ? 4294967295u : (uint32_t)t;      // (2^32: p within 2^-33 of 1)
   a.scale = (float)(1.0 / (1.0 - p));
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const int64_t units = rows * ((width * b + 15) / 16);
-  const bool aligned = (width * b) % 16 == 0 && on16(x, ld_x, b) && on16(out, ld_out, b);
-  cudaError_t e;
-  switch (dtype) {
-    case FGD_F32: e = aligned ? go<dropout_kernel<float, false>>(a, units, 4, st) : go<dropout_kernel<float, true>>(a, units, 4, st); break;
-    case FGD_BF16: e = aligned ? go<dropout_kernel<__nv_bfloat16, false>>(a, units, 4, st) : go<dropout_kernel<__nv_bfloat16, true>>(a, units, 4, st); break;
-    default: e = aligned ? go<dropout_kernel<__half, false>>(a, units, 4, st) : go<dropout_kernel<__half, true>>(a, units, 4, st); break;
-  }
+  // Strips where rows are on 16-byte boundaries and give a warp a full pass: 100 MB of bf16, 256 columns 46 us against 57 by shifts, 128 columns 84
+  // against 57.  (Of 2, 4 and 8 passes to a strip 92, 86 and 93 us for 32768 x 4096 bf16; of 1, 4, 16, 64 CTAs for each place on the SMs 92, 86, 90,
+  // 94; by shifts 1 is the best: 5003 x 4097 fp32 34.9 us, 4: 36.2, 16: 38.5.)
+  const bool strips = (width * b) % 16 == 0 && width * b >= 32 * 16 && on16(x, ld_x, b) && on16(out, ld_out, b);
+  auto launch = [&](auto zero) {
+    using T = decltype(zero);
+    constexpr int64_t strip = 32 * kStrip * 16 / sizeof(T);
+    return strips ? go<dropout_kernel<T>>(a, rows * ((width + strip - 1) / strip) * 32, 4, st) : go<dropout_shifted_kernel<T>>(a, rows * ((width + 15) / 16), 1, st);
+  };
+  const cudaError_t e = dtype == FGD_F32 ? launch(float{}) : dtype == FGD_BF16 ? launch(__nv_bfloat16{}) : launch(__half{});
   return e == cudaSuccess ? FGD_OK : op_fail(FGD_ERR_CUDA, "fgd_dropout: launch failed: %s", cudaGetErrorString(e));
 }
