@@ -5,10 +5,11 @@
 // commonest may be 7 % of a batch) and most of a vocabulary not at all, so the work is cut by tokens, not by rows, without atomics on floats:
 //   sort   each worker's (token, position) pairs by token, stable, in one launch: a cluster of CTAs per worker, radix passes of up to ten bits;
 //          histograms cross the cluster through distributed shared memory.  Marks the tokens that occur in a bitmap.
-//   rows   the sorted list in chunks of 64: a warp adds up the runs of equal tokens within its chunk, for 32 lanes x 16 bytes of columns.  A run that
-//          lies inside the chunk is a finished row; the pieces of one that crosses chunks go to scratch.  Other warps write the rows of
+//   rows   the sorted list in chunks: a warp adds up the runs of equal tokens within its chunk, for 32 lanes x 16 bytes of columns.  A run that
+//          lies inside the chunk is a finished row; the pieces of one that crosses chunks go to scratch.  Other CTAs write the rows of
 //          absent tokens with zeros.
-//   joins  the pieces of a run, added in order by the chunk that it starts in.
+//   joins  the pieces of the runs that cross chunks, which are few, eight warps to a run.
+// A few tokens need no sort: a warp looks through all of them for the one that its row of the table stands for, in one launch.
 // The order of every sum depends on the tokens alone.
 #include <cooperative_groups.h>
 
@@ -24,11 +25,12 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
-constexpr int kCluster = 8;           // CTAs that sort one worker's tokens
+constexpr int kCluster = 16;          // CTAs that sort one worker's tokens
 constexpr int kSortFew = 4096;        // up to so many a single one does
-constexpr int kMaxItems = 4;          // keys of a thread in one tile
+constexpr int kItems = 8;             // keys of a thread in one tile
 constexpr int kMaxBits = 10;          // of a radix pass
-constexpr int kChunk = 64;            // sorted tokens that a warp adds up
+constexpr int kChunk = 64, kShortChunk = 16;      // sorted tokens that a warp adds up
+constexpr int kNoSort = 512;          // rows up to which the tokens are not sorted
 constexpr int64_t kMaxWidth = 65536, kMaxVocab = 1 << 30;
 
 struct Tokens {
@@ -51,7 +53,7 @@ struct EmbedArgs {
   const float* table; int64_t worker_stride, row_stride;
   char* out; int64_t ld_out;
   int64_t rows, tokens_total, vocab;
-  int width, parts;            // slabs of a row that a warp takes together are kSlabs
+  int width, parts, slabs;     // of a row: parts that a warp takes, of so many slabs each (kSlabs at most)
   float scale;
 };
 constexpr int kSlabs = 4;
@@ -63,7 +65,7 @@ __global__ void __launch_bounds__(kThreads) embed_forward_kernel(const EmbedArgs
   const int64_t items = a.tokens_total * a.parts;
   for (int64_t item = (int64_t)blockIdx.x * kWarps + threadIdx.x / 32; item < items; item += (int64_t)gridDim.x * kWarps) {
     const int64_t t = item / a.parts, worker = t / a.rows;
-    const int c0 = (int)(item - t * a.parts) * (kSlabs * S::kColumns);
+    const int c0 = (int)(item - t * a.parts) * (a.slabs * S::kColumns), end = min(a.width, c0 + a.slabs * S::kColumns);
     const int64_t tok = a.tokens.at(worker, t - worker * a.rows);
     const bool real = tok >= 0 && tok < a.vocab;
     const float other = tok < 0 ? 0.f : __int_as_float(0x7fffffff);
@@ -75,12 +77,12 @@ __global__ void __launch_bounds__(kThreads) embed_forward_kernel(const EmbedArgs
       const int c = c0 + s * S::kColumns;
       if constexpr (ANY) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[s].v[j] = real && c + S::col(j) < a.width ? __ldg(row + c + S::col(j)) : other;
+        for (int j = 0; j < V; ++j) v[s].v[j] = real && c + S::col(j) < end ? __ldg(row + c + S::col(j)) : other;
       } else {
 #pragma unroll
         for (int j = 0; j < V; j += 4) {
           float4 f = make_float4(other, other, other, other);
-          if (real && c + S::col(0) < a.width) f = __ldg(reinterpret_cast<const float4*>(row + c + S::col(j)));
+          if (real && c + S::col(0) < end) f = __ldg(reinterpret_cast<const float4*>(row + c + S::col(j)));
           v[s].v[j] = f.x; v[s].v[j + 1] = f.y; v[s].v[j + 2] = f.z; v[s].v[j + 3] = f.w;
         }
       }
@@ -93,9 +95,9 @@ __global__ void __launch_bounds__(kThreads) embed_forward_kernel(const EmbedArgs
       if constexpr (ANY) {
 #pragma unroll
         for (int j = 0; j < V; ++j)
-          if (c + S::col(j) < a.width) out[c + S::col(j)] = from_f32<T>(v[s].v[j]);
+          if (c + S::col(j) < end) out[c + S::col(j)] = from_f32<T>(v[s].v[j]);
       } else {
-        if (c + S::col(0) < a.width) store_stream<T, V>(out + c + S::col(0), round_to<T, V>(v[s]));
+        if (c + S::col(0) < end) store_stream<T, V>(out + c + S::col(0), round_to<T, V>(v[s]));
       }
     }
   }
@@ -105,10 +107,22 @@ __global__ void __launch_bounds__(kThreads) embed_forward_kernel(const EmbedArgs
 struct SortArgs {
   Tokens tokens;
   int64_t vocab;
-  int rows, cluster, bits, passes;
+  int workers, rows, cluster, bits, passes;
   uint2 *pairs, *other;        // [worker][rows]: the result, and what the passes alternate with
   uint32_t* present; int words;      // [worker][words] bitmap of the vocabulary
+  int* joins;                  // length of the list of runs that cross chunks: cleared here
 };
+
+// Lanes whose digit is this lane's: a ballot for every bit.  (`real` lanes among themselves.)
+__device__ __forceinline__ uint32_t same_digit(uint32_t digit, bool real, int bits) {
+  uint32_t same = __ballot_sync(0xffffffffu, real);
+  for (int b = 0; b < bits; ++b) {
+    const bool one = digit >> b & 1u;
+    const uint32_t ones = __ballot_sync(0xffffffffu, one);
+    same &= one ? ones : ~ones;
+  }
+  return same;
+}
 
 // Pairs (token, position); a token outside the vocabulary counts as `vocab` and comes last.
 __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortArgs a) {
@@ -122,34 +136,95 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortArgs
   __shared__ uint32_t warp_total[kSortWarps];
   uint32_t* present = a.present + worker * a.words;
   for (int i = rank * kSortThreads + tid; i < a.words; i += a.cluster * kSortThreads) present[i] = 0u;
+  if (blockIdx.x == 0 && tid == 0) *a.joins = 0;
   const int part = (a.rows + a.cluster - 1) / a.cluster, first = min(rank * part, a.rows), n = min(part, a.rows - first);
-  const int items = part >= kMaxItems * kSortThreads ? kMaxItems : (part + kSortThreads - 1) / kSortThreads;
+  const int items = part >= kItems * kSortThreads ? kItems : (part + kSortThreads - 1) / kSortThreads, tile = items * kSortThreads;
   uint2 *dst = a.passes & 1 ? a.pairs : a.other, *src = a.passes & 1 ? a.other : a.pairs;      // the last pass writes the result
   dst += worker * a.rows; src += worker * a.rows;
+  unsigned short* mine = count + warp * bins;
   for (int pass = 0; pass < a.passes; ++pass) {
     const int shift = pass * a.bits;
-    auto load = [&](int i) -> uint2 {
-      if (pass > 0) return __ldcg(src + first + i);
-      const int64_t tok = a.tokens.at(worker, first + i);
-      return make_uint2(tok >= 0 && tok < a.vocab ? (uint32_t)tok : (uint32_t)a.vocab, (uint32_t)(first + i));
+    uint2 key[kItems];
+    uint32_t before_me[kItems];      // keys of the same digit earlier in the warp's part of the tile
+    // a warp's keys are consecutive, so ranks follow the order of the keys
+    auto load = [&](int t0) {
+#pragma unroll
+      for (int j = 0; j < kItems; ++j) {
+        const int i = t0 + (warp * items + j) * 32 + lane;
+        if (j >= items || i >= n) continue;
+        if (pass > 0) {
+          key[j] = __ldcg(src + first + i);
+        } else {
+          const int64_t tok = a.tokens.at(worker, first + i);
+          key[j] = make_uint2(tok >= 0 && tok < a.vocab ? (uint32_t)tok : (uint32_t)a.vocab, (uint32_t)(first + i));
+        }
+      }
     };
-    for (int b = tid; b < bins; b += kSortThreads) hist[b] = 0u;
-    __syncthreads();
-    for (int i0 = warp * 32; i0 < n; i0 += kSortThreads) {
-      const int i = i0 + lane;
-      const uint32_t digit = i < n ? load(i).x >> shift & (bins - 1) : 0xffffffffu;
-      const uint32_t same = __match_any_sync(0xffffffffu, digit);
-      if (i < n && (same & ((1u << lane) - 1)) == 0) atomicAdd(&hist[digit], (uint32_t)__popc(same));
+    auto rank_tile = [&](int t0) {      // -> before_me and the warps' counts
+      for (int b = tid; b < kSortWarps * bins / 2; b += kSortThreads) reinterpret_cast<uint32_t*>(count)[b] = 0u;
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < kItems; ++j) {
+        if (j >= items) break;
+        const bool real = t0 + (warp * items + j) * 32 + lane < n;
+        const uint32_t digit = real ? key[j].x >> shift & (bins - 1) : 0u;
+        const uint32_t same = same_digit(digit, real, a.bits), lower = same & ((1u << lane) - 1);
+        const uint32_t old = real ? mine[digit] : 0u;
+        __syncwarp();
+        if (real && lower == 0) mine[digit] = (unsigned short)(old + __popc(same));
+        __syncwarp();
+        before_me[j] = old + __popc(lower);
+      }
+      __syncthreads();
+    };
+    auto sum_warps = [&]() -> uint32_t {      // counts become those of the warps before; -> the tile's of bin `tid`
+      uint32_t sum = 0;
+      if (tid < bins) {
+        uint32_t c[kSortWarps];
+#pragma unroll
+        for (int w = 0; w < kSortWarps; ++w) c[w] = count[w * bins + tid];
+#pragma unroll
+        for (int w = 0; w < kSortWarps; ++w) {
+          count[w * bins + tid] = (unsigned short)sum;
+          sum += c[w];
+        }
+      }
+      return sum;
+    };
+    // this CTA's histogram: of its only tile as it is ranked, of several beforehand
+    const bool single = n <= tile;
+    uint32_t tile_sum = 0;
+    if (single) {
+      load(0);
+      rank_tile(0);
+      tile_sum = sum_warps();
+      if (tid < bins) hist[tid] = tile_sum;
+    } else {
+      if (tid < bins) hist[tid] = 0u;
+      for (int t0 = 0; t0 < n; t0 += tile) {
+        load(t0);
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kItems; ++j) {
+          const bool real = j < items && t0 + (warp * items + j) * 32 + lane < n;
+          const uint32_t digit = real ? key[j].x >> shift & (bins - 1) : 0u;
+          const uint32_t same = same_digit(digit, real, a.bits);
+          if (real && (same & ((1u << lane) - 1)) == 0) atomicAdd(&hist[digit], (uint32_t)__popc(same));
+        }
+      }
     }
     cluster.sync();
     // where each digit starts: keys of smaller digits anywhere, and of this digit in the CTAs before; bins <= kSortThreads
     uint32_t before = 0, total = 0;
-    if (tid < bins)
-      for (int r = 0; r < a.cluster; ++r) {
-        const uint32_t h = cluster.map_shared_rank(hist, r)[tid];
-        total += h;
-        if (r < rank) before += h;
-      }
+    if (tid < bins) {
+#pragma unroll
+      for (int r = 0; r < kCluster; ++r)
+        if (r < a.cluster) {
+          const uint32_t h = cluster.map_shared_rank(hist, r)[tid];
+          total += h;
+          if (r < rank) before += h;
+        }
+    }
     uint32_t scan = total;
 #pragma unroll
     for (int o = 1; o < 32; o *= 2) {
@@ -169,52 +244,37 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortArgs
     }
     __syncthreads();
     if (tid < bins) base[tid] = scan - total + (warp ? warp_total[warp - 1] : 0u) + before;
-    // tiles: a warp's keys are consecutive, so ranks follow the order of the keys
-    for (int t0 = 0; t0 < n; t0 += items * kSortThreads) {
-      for (int b = tid; b < kSortWarps * bins / 2; b += kSortThreads) reinterpret_cast<uint32_t*>(count)[b] = 0u;
-      __syncthreads();
-      uint2 key[kMaxItems];
-      uint32_t before_me[kMaxItems];
-      unsigned short* mine = count + warp * bins;
-#pragma unroll
-      for (int j = 0; j < kMaxItems; ++j) {
-        const int i = t0 + (warp * items + j) * 32 + lane;
-        const bool real = j < items && i < n;
-        key[j] = real ? load(i) : make_uint2(0u, 0u);
-        const uint32_t digit = real ? key[j].x >> shift & (bins - 1) : 0xffffffffu;
-        const uint32_t same = __match_any_sync(0xffffffffu, digit), lower = same & ((1u << lane) - 1);
-        const uint32_t old = real ? mine[digit] : 0u;
-        __syncwarp();
-        if (real && lower == 0) mine[digit] = (unsigned short)(old + __popc(same));
-        __syncwarp();
-        before_me[j] = old + __popc(lower);
+    for (int t0 = 0; t0 < n; t0 += tile) {
+      if (!single) {
+        load(t0);
+        rank_tile(t0);
+        tile_sum = sum_warps();
       }
       __syncthreads();
-      uint32_t sum = 0;
-      if (tid < bins)
-        for (int w = 0; w < kSortWarps; ++w) {
-          const uint32_t c = count[w * bins + tid];
-          count[w * bins + tid] = (unsigned short)sum;
-          sum += c;
-        }
-      __syncthreads();
 #pragma unroll
-      for (int j = 0; j < kMaxItems; ++j) {
-        const int i = t0 + (warp * items + j) * 32 + lane;
-        if (j < items && i < n) {
+      for (int j = 0; j < kItems; ++j) {
+        if (j < items && t0 + (warp * items + j) * 32 + lane < n) {
           const uint32_t digit = key[j].x >> shift & (bins - 1);
           dst[base[digit] + mine[digit] + before_me[j]] = key[j];
         }
       }
       __syncthreads();
-      if (tid < bins) base[tid] += sum;
+      if (tid < bins) base[tid] += tile_sum;
     }
     cluster.sync();      // the pass has been written, and every histogram read
     uint2* t = src; src = dst; dst = t;
   }
-  for (int i = tid; i < n; i += kSortThreads) {
-    const uint32_t key = __ldcg(src + first + i).x;
-    if (key < a.vocab && (first + i == 0 || __ldcg(src + first + i - 1).x != key)) atomicOr(present + key / 32, 1u << (key % 32));
+  for (int i0 = 0; i0 < n; i0 += kItems * kSortThreads) {
+    uint32_t key[kItems], prev[kItems];
+#pragma unroll
+    for (int j = 0; j < kItems; ++j) {
+      const int i = i0 + j * kSortThreads + tid;
+      key[j] = i < n ? __ldcg(src + first + i).x : (uint32_t)a.vocab;
+      prev[j] = i < n && first + i > 0 ? __ldcg(src + first + i - 1).x : 0xffffffffu;
+    }
+#pragma unroll
+    for (int j = 0; j < kItems; ++j)
+      if (key[j] < a.vocab && prev[j] != key[j]) atomicOr(present + key[j] / 32, 1u << (key[j] % 32));
   }
 }
 
@@ -225,7 +285,8 @@ struct RowsArgs {
   float* table; int64_t worker_stride, row_stride;
   float* pieces;               // [worker][chunk][2][width]: of a run that began before the chunk, and of one that goes on behind it
   int64_t vocab;
-  int workers, rows, chunks, slabs, width, sum_ctas;
+  int* joins; uint2* list;     // how many runs cross chunks; the chunks (of all workers) that they start in, their tokens
+  int workers, rows, chunk, chunks, slabs, width, sum_ctas;
   float scale;
 };
 
@@ -269,7 +330,7 @@ __global__ void __launch_bounds__(kThreads) embed_rows_kernel(const RowsArgs a) 
   const int64_t item = (int64_t)blockIdx.x * kWarps + warp;
   if (item >= (int64_t)a.workers * a.chunks * a.slabs) return;
   const int64_t wc = item / a.slabs, worker = wc / a.chunks;
-  const int c = (int)(item - wc * a.slabs) * S::kColumns, first = (int)(wc - worker * a.chunks) * kChunk, n = min(kChunk, a.rows - first);
+  const int c = (int)(item - wc * a.slabs) * S::kColumns, first = (int)(wc - worker * a.chunks) * a.chunk, n = min(a.chunk, a.rows - first);
   const uint2* e = a.pairs + worker * a.rows + first;
   const T* dout = reinterpret_cast<const T*>(a.dout) + worker * a.rows * a.ld;
   // this chunk's pairs, two a lane, and the tokens beside it (all ones: none)
@@ -322,37 +383,181 @@ __global__ void __launch_bounds__(kThreads) embed_rows_kernel(const RowsArgs a) 
       }
     }
   }
-  if (real > 0 && !(ends >> (real - 1) & 1u)) write_floats<T, ANY>(cut ? pieces : pieces + a.width, acc, 1.f, c, a.width);      // goes on in the next chunk
+  if (real > 0 && !(ends >> (real - 1) & 1u)) {      // goes on in the next chunk
+    write_floats<T, ANY>(cut ? pieces : pieces + a.width, acc, 1.f, c, a.width);
+    const uint32_t key = __shfl_sync(0xffffffffu, real > 32 ? p1.x : p0.x, (real - 1) & 31);
+    if (!cut && c == 0 && lane == 0) a.list[atomicAdd(a.joins, 1)] = make_uint2((uint32_t)wc, key);
+  }
 }
 
-// A run that crosses chunks belongs to the chunk that it starts in.
-template <typename T, bool ANY>
+// Runs that cross chunks, listed in no particular order by the chunk that they start in.  128 columns to a CTA, a run to each of its warps; where the run
+// has more than kPieces further pieces, all warps share it: of 8 kPieces consecutive ones each adds kPieces, and their sums are added in
+// the warps' order.
+constexpr int kPieces = 8;
 __global__ void __launch_bounds__(kThreads) embed_joins_kernel(const RowsArgs a) {
-  using S = Slab<T, ANY>;
-  constexpr int V = S::V;
+  __shared__ __align__(16) float sums[kWarps][128];
+  __shared__ uint2 shared_run[kWarps];
   wait_for_previous();
-  const int64_t item = (int64_t)blockIdx.x * kWarps + threadIdx.x / 32;
-  if (item >= (int64_t)a.workers * a.chunks * a.slabs) return;
-  const int64_t wc = item / a.slabs, worker = wc / a.chunks;
-  const int c = (int)(item - wc * a.slabs) * S::kColumns, chunk = (int)(wc - worker * a.chunks), first = chunk * kChunk, end = first + kChunk;
-  const uint2* e = a.pairs + worker * a.rows;
-  if (end >= a.rows) return;
-  const uint32_t key = e[end - 1].x;
-  if (key >= (uint32_t)a.vocab || e[end].x != key || (first > 0 && e[first - 1].x == key)) return;
-  const float* piece = a.pieces + wc * 2 * a.width;
-  auto read = [&](const float* p, float (&f)[V]) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, c0 = blockIdx.y * 128 + lane;
+  const int runs = *a.joins;
+  // adds the pieces of the run with this token in the chunks from k on, kPieces at most; -> how many there were.  FIRST: the one in chunk k is
+  // known to exist, and is fetched with the tokens that tell of the others.
+  auto add = [&](auto first, float (&acc)[4], const uint2* e, const float* pieces, uint32_t key, int64_t k) -> int {
+    constexpr bool FIRST = decltype(first)::value;
+    const bool has = lane < kPieces && k + lane < a.chunks && e[(k + lane) * a.chunk].x == key;
+    float p[kPieces][4];
+    if constexpr (FIRST) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) f[j] += c + S::col(j) < a.width ? p[c + S::col(j)] : 0.f;
+      for (int j = 0; j < 4; ++j) p[0][j] = c0 + 32 * j < a.width ? pieces[k * 2 * a.width + c0 + 32 * j] : 0.f;
+    }
+    const int n = __popc(__ballot_sync(0xffffffffu, has));      // (the first n)
+#pragma unroll
+    for (int i = FIRST; i < kPieces; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) p[i][j] = i < n && c0 + 32 * j < a.width ? pieces[(k + i) * 2 * a.width + c0 + 32 * j] : 0.f;
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j] += p[i][j];
+    return n;
+  };
+  for (int run0 = blockIdx.x * kWarps; run0 < runs; run0 += gridDim.x * kWarps) {
+    uint2 run = make_uint2(0u, 0u);
+    bool longer = false;
+    if (run0 + warp < runs) {
+      run = a.list[run0 + warp];
+      const int64_t worker = run.x / (uint32_t)a.chunks, chunk = run.x % (uint32_t)a.chunks;
+      const uint2* e = a.pairs + worker * a.rows;
+      const float* pieces = a.pieces + worker * a.chunks * 2 * a.width;
+      const int64_t next = chunk + 1 + kPieces;
+      longer = next < a.chunks && e[next * a.chunk].x == run.y;
+      float acc[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j] = c0 + 32 * j < a.width ? pieces[(chunk * 2 + 1) * a.width + c0 + 32 * j] : 0.f;
+      if (!longer) {
+        add(std::true_type{}, acc, e, pieces, run.y, chunk + 1);
+        float* row = a.table + worker * a.worker_stride + (int64_t)run.y * a.row_stride;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (c0 + 32 * j < a.width) row[c0 + 32 * j] = acc[j] * a.scale;
+      }
+    }
+    if (!__syncthreads_or(longer)) continue;
+    if (lane == 0) shared_run[warp] = longer ? run : make_uint2(0xffffffffu, 0u);
+    __syncthreads();
+    for (int i = 0; i < kWarps; ++i) {
+      const uint2 r = shared_run[i];
+      if (r.x == 0xffffffffu) continue;
+      const int64_t worker = r.x / (uint32_t)a.chunks, chunk = r.x % (uint32_t)a.chunks;
+      const uint2* e = a.pairs + worker * a.rows;
+      const float* pieces = a.pieces + worker * a.chunks * 2 * a.width;
+      float acc[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int64_t k = chunk + 1 + warp * kPieces; add(std::false_type{}, acc, e, pieces, r.y, k) == kPieces; k += kWarps * kPieces) {}
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sums[warp][lane + 32 * j] = acc[j];
+      __syncthreads();
+      const int c = blockIdx.y * 128 + threadIdx.x;
+      if (threadIdx.x < 128 && c < a.width) {
+        float t = pieces[(chunk * 2 + 1) * a.width + c];
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) t += sums[w][threadIdx.x];
+        a.table[worker * a.worker_stride + (int64_t)r.y * a.row_stride + c] = t * a.scale;
+      }
+      __syncthreads();
+    }
+    __syncthreads();
+  }
+}
+
+// ---- few tokens
+struct FewArgs {
+  Tokens tokens;
+  const char* dout; int64_t ld;
+  float* table; int64_t worker_stride, row_stride, vocab;
+  int rows, width, slabs;
+  float scale;
+};
+constexpr int kTogether = 32;      // tokens of one row above which all warps add them up together
+
+// A warp has a row of the table: it lists the tokens that are that row's and adds up what belongs to them, eight at a time on their way.
+template <typename T, bool ANY>
+__global__ void __launch_bounds__(kThreads) embed_few_kernel(const FewArgs a) {
+  using S = Slab<T, ANY>;
+  constexpr int V = S::V, kAhead = 8;
+  __shared__ int tokens[kNoSort];
+  __shared__ unsigned short list[kWarps][kNoSort];
+  __shared__ int lengths[kWarps];
+  __shared__ __align__(16) float sums[kWarps][S::kColumns];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  const int64_t worker = blockIdx.y, v0 = (int64_t)blockIdx.x * kWarps, v = v0 + warp;
+  for (int i = threadIdx.x; i < a.rows; i += kThreads) {
+    const int64_t tok = a.tokens.at(worker, i);
+    tokens[i] = tok >= 0 && tok < a.vocab ? (int)tok : -1;
+  }
+  __syncthreads();
+  int n = 0;
+  for (int i0 = 0; i0 < a.rows; i0 += 32) {
+    const bool hit = i0 + lane < a.rows && tokens[i0 + lane] == v;
+    const uint32_t hits = __ballot_sync(0xffffffffu, hit);
+    if (hit) list[warp][n + __popc(hits & ((1u << lane) - 1))] = (unsigned short)(i0 + lane);
+    n += __popc(hits);
+  }
+  if (lane == 0) lengths[warp] = n;
+  __syncthreads();
+  const T* dout = reinterpret_cast<const T*>(a.dout) + worker * a.rows * a.ld;
+  float* table = a.table + worker * a.worker_stride;
+  // positions [from, to) of a list
+  auto add = [&](const unsigned short* which, int from, int to, int c, float (&acc)[V]) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) acc[j] = 0.f;
+    for (int i0 = from; i0 < to; i0 += kAhead) {
+      Vals<V> x[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const bool real = i0 + k < to;
+        const T* row = dout + (real ? which[i0 + k] : 0) * a.ld;
+        if constexpr (ANY) {
+#pragma unroll
+          for (int j = 0; j < V; ++j) x[k].v[j] = real && c + S::col(j) < a.width ? to_f32(row[c + S::col(j)]) : 0.f;
+        } else {
+          ActPack<T, V> r;
+          zero(r);
+          if (real && c + S::col(0) < a.width) r = load_stream<T, V>(row + c + S::col(0));
+          x[k] = unpack<T, V>(r);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (i0 + k < to) {
+#pragma unroll
+          for (int j = 0; j < V; ++j) acc[j] += x[k].v[j];
+        }
+    }
   };
   float acc[V];
+  for (int slab = blockIdx.z; slab < a.slabs; slab += gridDim.z) {
+    const int c = slab * S::kColumns;
+    if (v < a.vocab && n <= kTogether) {
+      add(list[warp], 0, n, c, acc);
+      write_floats<T, ANY>(table + v * a.row_stride, acc, a.scale, c, a.width);
+    }
+    for (int w = 0; w < kWarps; ++w) {
+      const int all = lengths[w];
+      if (all <= kTogether) continue;      // (the whole CTA)
+      const int each = (all + kWarps - 1) / kWarps, from = min(warp * each, all);
+      add(list[w], from, min(from + each, all), c, acc);
 #pragma unroll
-  for (int j = 0; j < V; ++j) acc[j] = 0.f;
-  read(piece + a.width, acc);
-  for (int k = chunk + 1; k < a.chunks && e[k * kChunk].x == key; ++k) {
-    piece += 2 * a.width;
-    read(piece, acc);
+      for (int j = 0; j < V; ++j) sums[warp][S::col(j)] = acc[j];
+      __syncthreads();
+      for (int i = threadIdx.x; i < S::kColumns; i += kThreads) {
+        float t = sums[0][i];
+#pragma unroll
+        for (int k = 1; k < kWarps; ++k) t += sums[k][i];
+        if (c + i < a.width) table[(v0 + w) * a.row_stride + c + i] = t * a.scale;
+      }
+      __syncthreads();
+    }
   }
-  write_floats<T, ANY>(a.table + worker * a.worker_stride + (int64_t)key * a.row_stride, acc, a.scale, c, a.width);
 }
 
 // ---- host
@@ -383,23 +588,30 @@ bool aligned(const float* table, int64_t worker_stride, int64_t row_stride, int 
 }
 
 int64_t round16(int64_t n) { return (n + 15) / 16 * 16; }
-struct Layout { int64_t pairs, other, present, pieces, total; int chunks, words; };
+struct Layout { int64_t pairs, other, present, joins, list, pieces, total; int chunk, chunks, words; };
 Layout layout_of(int64_t workers, int64_t rows, int64_t vocab, int64_t width) {
-  Layout l;
-  l.chunks = (int)((rows + kChunk - 1) / kChunk);
+  Layout l = {};
+  if (rows <= kNoSort) return l;
+  // Short chunks where long ones would be too few for the SMs' warps.
+  l.chunk = workers * (rows / kChunk) * ((width + 255) / 256) < 16 * 148 ? kShortChunk : kChunk;
+  l.chunks = (int)((rows + l.chunk - 1) / l.chunk);
   l.words = (int)((vocab + 31) / 32);
-  l.pairs = 0;
   l.other = l.pairs + round16(workers * rows * (int64_t)sizeof(uint2));
   l.present = l.other + round16(workers * rows * (int64_t)sizeof(uint2));
-  l.pieces = l.present + round16(workers * l.words * 4);
-  l.total = l.pieces + (l.chunks > 1 ? workers * l.chunks * 2 * round16(width * 4) : 0);
+  l.joins = l.present + round16(workers * l.words * 4);
+  l.list = l.joins + 16;
+  l.pieces = l.list + round16(workers * l.chunks * (int64_t)sizeof(uint2));
+  l.total = l.pieces + workers * l.chunks * 2 * round16(width * 4);
   return l;
 }
 
 template <typename T, bool ANY>
 cudaError_t forward(const EmbedArgs& e, cudaStream_t st) {
   EmbedArgs a = e;
-  a.parts = (a.width + kSlabs * Slab<T, ANY>::kColumns - 1) / (kSlabs * Slab<T, ANY>::kColumns);
+  const int slabs = (a.width + Slab<T, ANY>::kColumns - 1) / Slab<T, ANY>::kColumns;
+  a.parts = (slabs + kSlabs - 1) / kSlabs;
+  a.slabs = (slabs + a.parts - 1) / a.parts;
+  a.parts = (slabs + a.slabs - 1) / a.slabs;
   const int64_t ctas = (a.tokens_total * a.parts + kWarps - 1) / kWarps, most = (int64_t)sm_count() * 64;
   embed_forward_kernel<T, ANY><<<(unsigned)(ctas < most ? ctas : most), kThreads, 0, st>>>(a);
   return cudaGetLastError();
@@ -408,22 +620,34 @@ template <typename T, bool ANY>
 cudaError_t backward(const RowsArgs& r, cudaStream_t st) {
   RowsArgs a = r;
   a.slabs = (a.width + Slab<T, ANY>::kColumns - 1) / Slab<T, ANY>::kColumns;
-  const int64_t sums = ((int64_t)a.workers * a.chunks * a.slabs + kWarps - 1) / kWarps;
-  a.sum_ctas = (int)sums;
-  cudaError_t e = launch_early(embed_rows_kernel<T, ANY>, dim3((unsigned)(sums + (int64_t)a.workers * a.words)), kThreads, 0, st, a);
-  if (e == cudaSuccess && a.chunks > 1) e = launch_early(embed_joins_kernel<T, ANY>, dim3((unsigned)sums), kThreads, 0, st, a);
+  a.sum_ctas = (int)(((int64_t)a.workers * a.chunks * a.slabs + kWarps - 1) / kWarps);
+  cudaError_t e = launch_early(embed_rows_kernel<T, ANY>, dim3((unsigned)(a.sum_ctas + (int64_t)a.workers * a.words)), kThreads, 0, st, a);
+  if (e == cudaSuccess) {
+    const int64_t columns = (a.width + 127) / 128, most = ((int64_t)a.workers * a.chunks + kWarps - 1) / kWarps, want = (int64_t)sm_count() * 4 / columns + 1;
+    e = launch_early(embed_joins_kernel, dim3((unsigned)(want < most ? want : most), (unsigned)columns), kThreads, 0, st, a);
+  }
   return e;
 }
-cudaError_t sort(const SortArgs& a, int workers, cudaStream_t st) {
+template <typename T, bool ANY>
+cudaError_t few(const FewArgs& f, int workers, cudaStream_t st) {
+  FewArgs a = f;
+  a.slabs = (a.width + Slab<T, ANY>::kColumns - 1) / Slab<T, ANY>::kColumns;
+  // every CTA looks through the tokens, so columns are cut only as far as the SMs would stay empty
+  const int64_t ctas = (a.vocab + kWarps - 1) / kWarps, want = (int64_t)sm_count() * 4 / (ctas * workers) + 1;
+  embed_few_kernel<T, ANY><<<dim3((unsigned)ctas, workers, (unsigned)(want < a.slabs ? want : a.slabs)), kThreads, 0, st>>>(a);
+  return cudaGetLastError();
+}
+cudaError_t sort(const SortArgs& a, cudaStream_t st) {
   const size_t smem = ((size_t)8 << a.bits) + ((size_t)kSortWarps * 2 << a.bits);
   cudaError_t e = allow_smem<embed_sort_kernel>(((size_t)8 << kMaxBits) + ((size_t)kSortWarps * 2 << kMaxBits));
   if (e != cudaSuccess) return e;
+  if (a.cluster > 8 && (e = cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)) != cudaSuccess) return e;
   cudaLaunchAttribute attr = {};
   attr.id = cudaLaunchAttributeClusterDimension;
   attr.val.clusterDim.x = a.cluster;
   attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
   cudaLaunchConfig_t c = {};
-  c.gridDim = dim3((unsigned)(workers * a.cluster));
+  c.gridDim = dim3((unsigned)(a.workers * a.cluster));
   c.blockDim = dim3(kSortThreads);
   c.dynamicSmemBytes = smem;
   c.stream = st;
@@ -480,15 +704,26 @@ extern "C" int fgd_embed_backward(int device, int dtype, int workers, int64_t ro
   if (int rc = check_common(who, dtype, workers, rows, vocab, width, tokens, token_bytes, ld_tokens, dtable, worker_stride, row_stride, scale, dout, ld_dout)) return rc;
   const int b = dtype_bytes(dtype);
   const Layout l = layout_of(workers, rows, vocab, width);
-  if (!workspace || workspace_bytes < l.total || reinterpret_cast<uintptr_t>(workspace) % 16 != 0)
+  if (l.total > 0 && (!workspace || workspace_bytes < l.total || reinterpret_cast<uintptr_t>(workspace) % 16 != 0))
     return op_fail(FGD_ERR_INVALID_ARG, "%s: needs a workspace of %lld bytes on a 16-byte boundary (fgd_embed_workspace)", who, (long long)l.total);
-  const Span st_ = table_span(dtable, workers, vocab, width, worker_stride, row_stride), sw = span_of(workspace, 1, l.total, l.total, 1);
+  const Span st_ = table_span(dtable, workers, vocab, width, worker_stride, row_stride), sw = l.total > 0 ? span_of(workspace, 1, l.total, l.total, 1) : Span{};
   const Span sx = span_of(dout, workers * rows, width, ld_dout, b), sk = span_of(tokens, workers, rows, ld_tokens, token_bytes);
   if (st_.overlaps(sx) || st_.overlaps(sk) || st_.overlaps(sw) || sw.overlaps(sx) || sw.overlaps(sk)) return op_fail(FGD_ERR_ALIAS, "%s: dtable or the workspace overlaps another tensor", who);
-  const int64_t ctas = (int64_t)workers * l.words + (int64_t)workers * l.chunks * ((width + 127) / 128);
+  const int64_t ctas = rows <= kNoSort ? (vocab + kWarps - 1) / kWarps : (int64_t)workers * l.words + (int64_t)workers * l.chunks * ((width + 127) / 128);
   if (ctas > 0x7fffffff) return op_fail(FGD_ERR_UNSUPPORTED, "%s: more work than one launch holds", who);
   DeviceScope dev(device);
   if (!dev.ok()) return op_fail(FGD_ERR_CUDA, "cannot select device %d", device);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const bool any = !aligned(dtable, worker_stride, row_stride, workers, dout, ld_dout, b, width);
+  if (rows <= kNoSort) {
+    FewArgs f = {};
+    f.tokens = Tokens{tokens, token_bytes, ld_tokens};
+    f.dout = static_cast<const char*>(dout); f.ld = ld_dout;
+    f.table = dtable; f.worker_stride = worker_stride; f.row_stride = row_stride; f.vocab = vocab;
+    f.rows = (int)rows; f.width = (int)width; f.scale = (float)scale;
+    const cudaError_t e = by_type(dtype, any, [&](auto zero, auto any_) { return few<decltype(zero), decltype(any_)::value>(f, workers, st); });
+    return e == cudaSuccess ? FGD_OK : op_fail(FGD_ERR_CUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
+  }
   char* ws = static_cast<char*>(workspace);
   SortArgs s = {};
   s.tokens = Tokens{tokens, token_bytes, ld_tokens};
@@ -500,17 +735,18 @@ extern "C" int fgd_embed_backward(int device, int dtype, int workers, int64_t ro
   s.bits = (bits + s.passes - 1) / s.passes;
   s.pairs = reinterpret_cast<uint2*>(ws + l.pairs); s.other = reinterpret_cast<uint2*>(ws + l.other);
   s.present = reinterpret_cast<uint32_t*>(ws + l.present); s.words = l.words;
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  cudaError_t e = sort(s, workers, st);
+  s.joins = reinterpret_cast<int*>(ws + l.joins);
+  s.workers = workers;
+  cudaError_t e = sort(s, st);
   if (e == cudaSuccess) {
     RowsArgs r = {};
     r.pairs = s.pairs; r.present = s.present; r.words = l.words;
     r.dout = static_cast<const char*>(dout); r.ld = ld_dout;
     r.table = dtable; r.worker_stride = worker_stride; r.row_stride = row_stride;
     r.pieces = reinterpret_cast<float*>(ws + l.pieces);
-    r.vocab = vocab; r.workers = workers; r.rows = (int)rows; r.chunks = l.chunks; r.width = (int)width; r.scale = (float)scale;
-    e = by_type(dtype, !aligned(dtable, worker_stride, row_stride, workers, dout, ld_dout, b, width),
-                [&](auto zero, auto any) { return backward<decltype(zero), decltype(any)::value>(r, st); });
+    r.vocab = vocab; r.workers = workers; r.rows = (int)rows; r.chunk = l.chunk; r.chunks = l.chunks;
+    r.joins = s.joins; r.list = reinterpret_cast<uint2*>(ws + l.list); r.width = (int)width; r.scale = (float)scale;
+    e = by_type(dtype, any, [&](auto zero, auto any_) { return backward<decltype(zero), decltype(any_)::value>(r, st); });
   }
   return e == cudaSuccess ? FGD_OK : op_fail(FGD_ERR_CUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
 }

@@ -96,17 +96,18 @@ def test_embed_refuses(backward, status, change):
 
 @pytest.mark.parametrize("backward,status,change", [
     (False, ALIAS, dict(x=_at(0))), (True, ALIAS, dict(table=_at(0))), (True, ALIAS, dict(table=_at(3) + 16)), (True, ALIAS, dict(x=_at(3))), (True, INVALID, dict(workspace=0)),
-    (True, INVALID, dict(workspace=_at(3) + 8)), (True, INVALID, dict(workspace_bytes=100)),
+    (True, INVALID, dict(workspace=_at(3) + 8)), (True, INVALID, dict(workspace_bytes=100)), (True, ALIAS, dict(workspace=_at(0))),
 ])
 def test_embed_refuses_more(backward, status, change):
-    assert _embed(backward, **change) == status
+    """(With tokens enough that the gradient needs its workspace.)"""
+    assert _embed(backward, **{"rows": 1000, "ld_tokens": 1000, **change}) == status
 
 
 def test_embed_workspace():
     for args in ((0, 1, 1, 1), (1, -1, 1, 1), (1, 1, 0, 1), (1, 1, 1, 65537)):
         with pytest.raises(fgd.FgdError):
             fgd.fgd_embed_workspace(*args)
-    assert fgd.fgd_embed_workspace(2, 0, 50, 64) > 0
+    assert fgd.fgd_embed_workspace(2, 0, 50, 64) >= 0 and fgd.fgd_embed_workspace(2, 1000, 50, 64) > 0
 
 
 # ------------------------------------------------------------------------------- dropout
