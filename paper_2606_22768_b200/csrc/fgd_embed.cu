@@ -30,7 +30,7 @@ constexpr int kSortFew = 4096;        // up to so many a single one does
 constexpr int kItems = 8;             // keys of a thread in one tile
 constexpr int kMaxBits = 10;          // of a radix pass
 constexpr int kChunk = 64, kShortChunk = 16;      // sorted tokens that a warp adds up
-constexpr int kNoSort = 512;          // rows up to which the tokens are not sorted
+constexpr int kNoSort = 512;          // tokens of a worker up to which they may go unsorted
 constexpr int64_t kMaxWidth = 65536, kMaxVocab = 1 << 30;
 
 struct Tokens {
@@ -58,38 +58,49 @@ struct EmbedArgs {
 };
 constexpr int kSlabs = 4;
 
-template <typename T, bool ANY>
-__global__ void __launch_bounds__(kThreads) embed_forward_kernel(const EmbedArgs a) {
+// A warp has kSlabs slabs on their way at once: of one row, or where a row is no more than one (SHORT) of as many rows.  (Rows and slabs
+// mixed freely, 4 x 8192 tokens of 2048 take 61 us instead of 39: every slab then has its own token, and its place to be worked out.)  39 us are 94 % of the
+// copy peak; five CTAs to an SM, with four 41, with six 49.
+template <typename T, bool ANY, bool SHORT>
+__global__ void __launch_bounds__(kThreads, SHORT ? 4 : 5) embed_forward_kernel(const EmbedArgs a) {
   using S = Slab<T, ANY>;
-  constexpr int V = S::V;
-  const int64_t items = a.tokens_total * a.parts;
+  constexpr int V = S::V, ROWS = SHORT ? kSlabs : 1;
+  const int64_t items = SHORT ? (a.tokens_total + ROWS - 1) / ROWS : a.tokens_total * a.parts;
   for (int64_t item = (int64_t)blockIdx.x * kWarps + threadIdx.x / 32; item < items; item += (int64_t)gridDim.x * kWarps) {
-    const int64_t t = item / a.parts, worker = t / a.rows;
-    const int c0 = (int)(item - t * a.parts) * (a.slabs * S::kColumns), end = min(a.width, c0 + a.slabs * S::kColumns);
-    const int64_t tok = a.tokens.at(worker, t - worker * a.rows);
-    const bool real = tok >= 0 && tok < a.vocab;
-    const float other = tok < 0 ? 0.f : __int_as_float(0x7fffffff);
-    const float* row = a.table + worker * a.worker_stride + (real ? tok : 0) * a.row_stride;
-    T* out = reinterpret_cast<T*>(a.out) + t * a.ld_out;
+    const int64_t t0 = SHORT ? item * ROWS : item / a.parts;
+    const int c0 = SHORT ? 0 : (int)(item - t0 * a.parts) * (a.slabs * S::kColumns), end = SHORT ? a.width : min(a.width, c0 + a.slabs * S::kColumns);
+    const float* row[ROWS];
+    float other[ROWS];         // of a token outside the vocabulary
+    bool real[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      const int64_t t = t0 + r < a.tokens_total ? t0 + r : t0, worker = t / a.rows, tok = a.tokens.at(worker, t - worker * a.rows);
+      real[r] = tok >= 0 && tok < a.vocab;
+      other[r] = tok < 0 ? 0.f : __int_as_float(0x7fffffff);
+      row[r] = a.table + worker * a.worker_stride + (real[r] ? tok : 0) * a.row_stride;
+    }
     Vals<V> v[kSlabs];
 #pragma unroll
     for (int s = 0; s < kSlabs; ++s) {
-      const int c = c0 + s * S::kColumns;
+      const int r = SHORT ? s : 0, c = SHORT ? 0 : c0 + s * S::kColumns;
       if constexpr (ANY) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[s].v[j] = real && c + S::col(j) < end ? __ldg(row + c + S::col(j)) : other;
+        for (int j = 0; j < V; ++j) v[s].v[j] = real[r] && c + S::col(j) < end ? __ldg(row[r] + c + S::col(j)) : other[r];
       } else {
 #pragma unroll
         for (int j = 0; j < V; j += 4) {
-          float4 f = make_float4(other, other, other, other);
-          if (real && c + S::col(0) < end) f = __ldg(reinterpret_cast<const float4*>(row + c + S::col(j)));
+          float4 f = make_float4(other[r], other[r], other[r], other[r]);
+          if (real[r] && c + S::col(0) < end) f = __ldg(reinterpret_cast<const float4*>(row[r] + c + S::col(j)));
           v[s].v[j] = f.x; v[s].v[j + 1] = f.y; v[s].v[j + 2] = f.z; v[s].v[j + 3] = f.w;
         }
       }
     }
 #pragma unroll
     for (int s = 0; s < kSlabs; ++s) {
-      const int c = c0 + s * S::kColumns;
+      const int64_t t = t0 + (SHORT ? s : 0);
+      if (t >= a.tokens_total) break;
+      T* out = reinterpret_cast<T*>(a.out) + t * a.ld_out;
+      const int c = SHORT ? 0 : c0 + s * S::kColumns;
 #pragma unroll
       for (int j = 0; j < V; ++j) v[s].v[j] *= a.scale;
       if constexpr (ANY) {
@@ -286,10 +297,17 @@ struct RowsArgs {
   float* pieces;               // [worker][chunk][2][width]: of a run that began before the chunk, and of one that goes on behind it
   int64_t vocab;
   int* joins; uint2* list;     // how many runs cross chunks; the chunks (of all workers) that they start in, their tokens
-  int workers, rows, chunk, chunks, slabs, width, sum_ctas;
+  int workers, rows, chunk, chunks, slabs, width, sum_ctas, cta_words, zero_lanes;
   float scale;
 };
 
+// *p as fp32, or 0.  Always loads (from `safe` where there is nothing): as a branch around load and conversion it would wait for one value after the
+// other, 181 against 30 us where many go together.
+template <typename T>
+__device__ __forceinline__ float load_or_zero(bool real, const T* p, const T* safe) {
+  const float f = to_f32(*(real ? p : safe));
+  return real ? f : 0.f;
+}
 template <typename T, bool ANY>
 __device__ __forceinline__ void write_floats(float* row, const float (&f)[Slab<T, ANY>::V], float scale, int c, int width) {
   using S = Slab<T, ANY>;
@@ -312,17 +330,20 @@ __global__ void __launch_bounds__(kThreads) embed_rows_kernel(const RowsArgs a) 
   constexpr int V = S::V, kAhead = 8;
   wait_for_previous();
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
-  if ((int)blockIdx.x >= a.sum_ctas) {      // rows of absent tokens: 32 of them, a word of the bitmap, per CTA
-    const int64_t word = blockIdx.x - a.sum_ctas, worker = word / a.words;
-    const int v0 = (int)(word - worker * a.words) * 32;
-    const uint32_t present = a.present[word];
-    for (int i = warp; i < 32 && v0 + i < a.vocab; i += kWarps) {
-      if (present >> i & 1u) continue;
-      float* row = a.table + worker * a.worker_stride + (int64_t)(v0 + i) * a.row_stride;
+  if ((int)blockIdx.x >= a.sum_ctas) {      // rows of absent tokens: some words of the bitmap, 32 rows each
+    const int per_worker = (a.words + a.cta_words - 1) / a.cta_words, cta = blockIdx.x - a.sum_ctas;
+    const int64_t worker = cta / per_worker;
+    const int first = (int)(cta - worker * per_worker) * a.cta_words, last = min(first + a.cta_words, a.words);
+    float* table = a.table + worker * a.worker_stride;
+    // zero_lanes of a warp to a row
+    const int group = lane / a.zero_lanes, groups = 32 / a.zero_lanes, l = lane % a.zero_lanes;
+    for (int64_t v = (int64_t)first * 32 + warp * groups + group; v < (int64_t)last * 32 && v < a.vocab; v += kWarps * groups) {
+      if (a.present[worker * a.words + v / 32] >> (v % 32) & 1u) continue;
+      float* row = table + v * a.row_stride;
       if constexpr (ANY) {
-        for (int c = lane; c < a.width; c += 32) row[c] = 0.f;
+        for (int c = l; c < a.width; c += a.zero_lanes) row[c] = 0.f;
       } else {
-        for (int c = lane * 4; c < a.width; c += 128) __stcs(reinterpret_cast<float4*>(row + c), make_float4(0.f, 0.f, 0.f, 0.f));
+        for (int c = l * 4; c < a.width; c += a.zero_lanes * 4) __stcs(reinterpret_cast<float4*>(row + c), make_float4(0.f, 0.f, 0.f, 0.f));
       }
     }
     return;
@@ -518,7 +539,7 @@ __global__ void __launch_bounds__(kThreads) embed_few_kernel(const FewArgs a) {
         const T* row = dout + (real ? which[i0 + k] : 0) * a.ld;
         if constexpr (ANY) {
 #pragma unroll
-          for (int j = 0; j < V; ++j) x[k].v[j] = real && c + S::col(j) < a.width ? to_f32(row[c + S::col(j)]) : 0.f;
+          for (int j = 0; j < V; ++j) x[k].v[j] = load_or_zero(real && c + S::col(j) < a.width, row + c + S::col(j), dout);
         } else {
           ActPack<T, V> r;
           zero(r);
@@ -588,10 +609,13 @@ bool aligned(const float* table, int64_t worker_stride, int64_t row_stride, int 
 }
 
 int64_t round16(int64_t n) { return (n + 15) / 16 * 16; }
+// Few tokens and little of a table: every warp looks through all tokens for its row.  4 x 384 tokens of 256, 256 wide, bf16: 6.2 us, sorted 20; but
+// 4 x 203 of 1195, 2242 wide, 129 us (one warp adds up all columns of a common token) and 512 of 32000, 2048 wide, 106 us (the looking), sorted 55.
+bool no_sort(int64_t workers, int64_t rows, int64_t vocab, int64_t width) { return rows <= kNoSort && workers * vocab * ((width + 255) / 256) <= 16384; }
 struct Layout { int64_t pairs, other, present, joins, list, pieces, total; int chunk, chunks, words; };
 Layout layout_of(int64_t workers, int64_t rows, int64_t vocab, int64_t width) {
   Layout l = {};
-  if (rows <= kNoSort) return l;
+  if (no_sort(workers, rows, vocab, width)) return l;
   // Short chunks where long ones would be too few for the SMs' warps.
   l.chunk = workers * (rows / kChunk) * ((width + 255) / 256) < 16 * 148 ? kShortChunk : kChunk;
   l.chunks = (int)((rows + l.chunk - 1) / l.chunk);
@@ -610,10 +634,11 @@ cudaError_t forward(const EmbedArgs& e, cudaStream_t st) {
   EmbedArgs a = e;
   const int slabs = (a.width + Slab<T, ANY>::kColumns - 1) / Slab<T, ANY>::kColumns;
   a.parts = (slabs + kSlabs - 1) / kSlabs;
-  a.slabs = (slabs + a.parts - 1) / a.parts;
-  a.parts = (slabs + a.slabs - 1) / a.slabs;
-  const int64_t ctas = (a.tokens_total * a.parts + kWarps - 1) / kWarps, most = (int64_t)sm_count() * 64;
-  embed_forward_kernel<T, ANY><<<(unsigned)(ctas < most ? ctas : most), kThreads, 0, st>>>(a);
+  a.slabs = kSlabs;
+  const int64_t items = slabs == 1 ? (a.tokens_total + kSlabs - 1) / kSlabs : a.tokens_total * a.parts, ctas = (items + kWarps - 1) / kWarps, most = (int64_t)sm_count() * 64;
+  const unsigned grid = (unsigned)(ctas < most ? ctas : most);
+  if (slabs == 1) embed_forward_kernel<T, ANY, true><<<grid, kThreads, 0, st>>>(a);
+  else embed_forward_kernel<T, ANY, false><<<grid, kThreads, 0, st>>>(a);
   return cudaGetLastError();
 }
 template <typename T, bool ANY>
@@ -621,7 +646,14 @@ cudaError_t backward(const RowsArgs& r, cudaStream_t st) {
   RowsArgs a = r;
   a.slabs = (a.width + Slab<T, ANY>::kColumns - 1) / Slab<T, ANY>::kColumns;
   a.sum_ctas = (int)(((int64_t)a.workers * a.chunks * a.slabs + kWarps - 1) / kWarps);
-  cudaError_t e = launch_early(embed_rows_kernel<T, ANY>, dim3((unsigned)(a.sum_ctas + (int64_t)a.workers * a.words)), kThreads, 0, st, a);
+  // zeros: 256 KB to a CTA, or 32 rows; a float4 (or float) to a lane, as many lanes to a row as have one
+  a.cta_words = (int)((256 * 1024) / ((int64_t)a.width * 4 * 32));
+  const int64_t share = (int64_t)a.workers * a.words / ((int64_t)sm_count() * 8);      // (no fewer CTAs than the SMs hold)
+  if (a.cta_words > share) a.cta_words = (int)share;
+  if (a.cta_words < 1) a.cta_words = 1;
+  for (a.zero_lanes = 1; a.zero_lanes < 32 && a.zero_lanes * (ANY ? 1 : 4) < a.width;) a.zero_lanes *= 2;
+  const int64_t zeros = (int64_t)a.workers * ((a.words + a.cta_words - 1) / a.cta_words);
+  cudaError_t e = launch_early(embed_rows_kernel<T, ANY>, dim3((unsigned)(a.sum_ctas + zeros)), kThreads, 0, st, a);
   if (e == cudaSuccess) {
     const int64_t columns = (a.width + 127) / 128, most = ((int64_t)a.workers * a.chunks + kWarps - 1) / kWarps, want = (int64_t)sm_count() * 4 / columns + 1;
     e = launch_early(embed_joins_kernel, dim3((unsigned)(want < most ? want : most), (unsigned)columns), kThreads, 0, st, a);
@@ -709,13 +741,13 @@ extern "C" int fgd_embed_backward(int device, int dtype, int workers, int64_t ro
   const Span st_ = table_span(dtable, workers, vocab, width, worker_stride, row_stride), sw = l.total > 0 ? span_of(workspace, 1, l.total, l.total, 1) : Span{};
   const Span sx = span_of(dout, workers * rows, width, ld_dout, b), sk = span_of(tokens, workers, rows, ld_tokens, token_bytes);
   if (st_.overlaps(sx) || st_.overlaps(sk) || st_.overlaps(sw) || sw.overlaps(sx) || sw.overlaps(sk)) return op_fail(FGD_ERR_ALIAS, "%s: dtable or the workspace overlaps another tensor", who);
-  const int64_t ctas = rows <= kNoSort ? (vocab + kWarps - 1) / kWarps : (int64_t)workers * l.words + (int64_t)workers * l.chunks * ((width + 127) / 128);
+  const int64_t ctas = no_sort(workers, rows, vocab, width) ? (vocab + kWarps - 1) / kWarps : (int64_t)workers * l.words + (int64_t)workers * l.chunks * ((width + 127) / 128);
   if (ctas > 0x7fffffff) return op_fail(FGD_ERR_UNSUPPORTED, "%s: more work than one launch holds", who);
   DeviceScope dev(device);
   if (!dev.ok()) return op_fail(FGD_ERR_CUDA, "cannot select device %d", device);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool any = !aligned(dtable, worker_stride, row_stride, workers, dout, ld_dout, b, width);
-  if (rows <= kNoSort) {
+  if (no_sort(workers, rows, vocab, width)) {
     FewArgs f = {};
     f.tokens = Tokens{tokens, token_bytes, ld_tokens};
     f.dout = static_cast<const char*>(dout); f.ld = ld_dout;

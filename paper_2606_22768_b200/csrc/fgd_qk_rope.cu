@@ -13,6 +13,7 @@
 // its q first and then its k: so the weights and, in the backward pass, the sums of their gradients (CTAs belong to one worker) stay in
 // registers, of one side at a time.  What the next steps need is on its way meanwhile: activations through a ring in shared memory that each lane
 // fills for itself (cp.async), the next token's cos and sin in registers.
+#include <algorithm>
 #include <cmath>
 
 #include "fgd_dtype.cuh"
@@ -26,7 +27,7 @@ namespace {
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxDim = 256;
 
-struct RopeHeads { char* p; int64_t ts, hs, step; };      // strides and gt heads, in bytes
+struct RopeHeads { char* p; int64_t ts, hs, step; };      // strides, and from one of a warp's batches to the next, in bytes
 struct RopeSide {
   RopeHeads x, y, g;           // forward: input, output; backward: input, gradient out, gradient in
   const float* w; int64_t w_ld;
@@ -38,7 +39,7 @@ struct RopeArgs {
   const void* positions; int position_bytes;
   int64_t rows, table_rows;
   int d, rot, lg, pairs;       // lanes of a head; chunk pairs of a head
-  int gt;                      // lane groups that share a token
+  int gt, split;               // lane groups that share a token; warps that share its batches
   float eps, inv_d, turn;      // turn: 1, or -1 for the transposed rotation
   float* partial;              // backward: [worker][cta][q or k][d]
 };
@@ -289,16 +290,17 @@ __global__ void __launch_bounds__(kThreads, 2) rope_kernel(const __grid_constant
   __shared__ float sums[GRAD ? 2 : 1][GRAD ? kWarps : 1][kMaxDim];
   const int worker = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x / 32, group = lane / a.lg, sub = group % a.gt;
   const uint32_t tokens = 32 / a.lg / a.gt, mine = group / a.gt;      // tokens of a warp at once, this lane's among them
-  const uint32_t rows = (uint32_t)a.rows, stride = gridDim.x * kWarps * tokens, first = (blockIdx.x * kWarps + warp) * tokens;
+  const uint32_t rows = (uint32_t)a.rows, place = blockIdx.x * kWarps + warp, stride = gridDim.x * kWarps / a.split * tokens, first = place / a.split * tokens;
+  const int part = place % a.split;
   const int64_t base = worker * a.rows + mine;
   const Geometry<V, NC, INTER> geo(lane % a.lg, a);
   if constexpr (GRAD) let_next_start();      // the sums' CTAs wait for this kernel's end on the SMs
   // The step that is fetched next, kDepth - 1 ahead: side, first token of the warp's group, batch, addresses.  (An address moves on by a constant
   // within a token; worked out anew in every step they were a third of the kernel's instructions.)
-  int ahead_side = first < rows ? 0 : 2, ahead_b = 0;
+  int ahead_side = first < rows ? 0 : 2, ahead_b = part;
   uint32_t ahead_t0 = first;
   const char* in[N];
-  auto at = [&](const RopeHeads& h, uint32_t t0) { return h.p + (base + t0) * h.ts + sub * h.hs + geo.c0[0] * (int)sizeof(T); };      // of a lane's first channel
+  auto at = [&](const RopeHeads& h, uint32_t t0) { return h.p + (base + t0) * h.ts + (sub + part * a.gt) * h.hs + geo.c0[0] * (int)sizeof(T); };      // of a lane's first channel
   auto seek = [&](const RopeSide& s) {
     in[0] = at(GRAD ? s.g : s.x, ahead_t0);
     if constexpr (GRAD) in[N - 1] = at(s.x, ahead_t0);
@@ -306,12 +308,12 @@ __global__ void __launch_bounds__(kThreads, 2) rope_kernel(const __grid_constant
   auto advance = [&] {
     if (ahead_side == 2) return;
     const RopeSide& s = a.side[ahead_side];
-    if (++ahead_b < s.batches) {
+    if ((ahead_b += a.split) < s.batches) {
       in[0] += GRAD ? s.g.step : s.x.step;
       if constexpr (GRAD) in[N - 1] += s.x.step;
       return;
     }
-    ahead_b = 0;
+    ahead_b = part;
     ahead_t0 += stride;
     if (ahead_t0 >= rows) {
       ahead_t0 = first;
@@ -364,7 +366,7 @@ __global__ void __launch_bounds__(kThreads, 2) rope_kernel(const __grid_constant
       }
       char* out = at(s.y, t0);
 #pragma unroll 2
-      for (int b = 0; b < s.batches; ++b, out += s.y.step) {
+      for (int b = part; b < s.batches; b += a.split, out += s.y.step) {
         feed.wait();
         float z[NC][2 * V], v[NC][2 * V];
         feed.get(z, 0, in[0], real, geo);
@@ -652,12 +654,17 @@ int run_rope(const fgd_qk_rope_args* b, bool backward, int device, void* stream)
     a.rows = b->rows; a.table_rows = b->table_rows;
     a.d = d; a.rot = rot; a.lg = l.lg; a.pairs = l.pairs;
     a.gt = group_of(heads[0], heads[1], 32 / l.lg);
+    // Where tokens are too few for the SMs' warps, several share a token's heads.
+    const int64_t tokens = 32 / l.lg / a.gt, warps = b->workers * ((b->rows + tokens - 1) / tokens), places = (int64_t)sm_count() * kCtasPerSm * kWarps;
+    const int fewest = (use[1] ? std::min(heads[0], heads[1]) : heads[0]) / a.gt;
+    a.split = 1;
+    while (a.split * 2 <= fewest && a.split * 2 * warps <= places && a.split < kWarps) a.split *= 2;
     for (int i = 0; i < 2; ++i) {
       RopeSide& side = a.side[i];
       side.batches = heads[i] / a.gt;
-      for (RopeHeads* h : {&side.x, &side.y, &side.g}) h->step = h->hs * a.gt;
+      for (RopeHeads* h : {&side.x, &side.y, &side.g}) h->step = h->hs * a.gt * a.split;
     }
-    c.ctas = ctas_for(b->workers, b->rows, 32 / l.lg / a.gt);
+    c.ctas = ctas_for(b->workers, b->rows * a.split, tokens);
     a.eps = (float)b->eps; a.inv_d = 1.f / (float)d; a.turn = backward ? -1.f : 1.f;
     const bool inter = b->interleaved != 0;
     auto by_vec = [&](auto zero) {
