@@ -1,6 +1,6 @@
 """K workers train a small decoder on one GPU: H inner steps on the library's operators, then one outer round, over and over.
 
-    python examples/inner_and_outer.py [--workers 4] [--rounds 5] [--inner 20]
+    python examples/inner_and_outer.py [--workers 4] [--rounds 5] [--inner 20] [--qk-norm] [--dropout 0.1]
 
 Every worker sees its own packed sequences of different lengths from one synthetic language (a fixed random successor table with
 noise).  After every round: the workers' losses, the L2 consensus distance, and the JS distance between each worker's predictions and those of
@@ -42,13 +42,15 @@ def main(argv=None):
     ap.add_argument("--inner", type=int, default=20)
     ap.add_argument("--lr", type=float, default=2e-3)
     ap.add_argument("--seed", type=int, default=0)
+    ap.add_argument("--qk-norm", action="store_true", help="norms of queries and keys")
+    ap.add_argument("--dropout", type=float, default=0.0)
     a = ap.parse_args(argv)
-    K, cfg = a.workers, inner.DecoderConfig()
+    K, cfg = a.workers, inner.DecoderConfig(qk_norm=a.qk_norm, dropout=a.dropout)
     _, P = inner.param_layout(cfg)
     theta = torch.zeros((K, P), device="cuda")
     inner.init_params(theta, cfg, a.seed)
     local, momentum = theta.clone(), torch.zeros_like(theta)
-    steps, drv = inner.InnerSteps(local, cfg, lr=a.lr), OuterRound(K, P)
+    steps, drv = inner.InnerSteps(local, cfg, lr=a.lr, seed=a.seed), OuterRound(K, P)
     rng = np.random.default_rng(a.seed)
     successor = rng.permutation(cfg.vocab)
     lens = [180, 65, 1, 138]

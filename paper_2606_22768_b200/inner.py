@@ -1,24 +1,24 @@
 """Inner steps of the K workers on one GPU: a small Llama-style decoder whose parameters are rows of the flat [K, ld] matrix that
 the outer round works on.
 
-The decoder block runs on the library's operators -- packed causal attention, the fused block norm, and activations kept in 8 bits
-for the backward pass -- as autograd functions; matrix products are plain library products, batched over the workers.  All K
+The decoder runs on the library's operators -- embeddings, norms and rotation of queries and keys, packed causal attention, the fused block
+norm, dropout, and activations kept in 8 bits for the backward pass -- as autograd functions; matrix products are plain library products, batched over the workers.  All K
 workers take their step in one pass: activations are [K * rows, width] with worker m's rows at [m * rows, (m + 1) * rows).
 
-What a block keeps for its backward pass: the residual stream and the block outputs (the norms need them), q, k, v, o and lse, and in
-8 bits the inputs of its projections and of SwiGLU (whose output, the last projection's input, comes from there again).  The backward passes are not differentiable themselves: create_graph=True is an error
+What a block keeps for its backward pass: the residual stream and the block outputs (the norms need them), q, k, v, o and lse, with norms of q and k the
+projection's output, no mask of dropout (it is made again), and in 8 bits the inputs of its projections and of SwiGLU (whose output, the last projection's input, comes from there again).  The backward passes are not differentiable themselves: create_graph=True is an error
 in them.
 """
 from __future__ import annotations
 
 import functools
 from dataclasses import dataclass
-from typing import Dict, Optional, Tuple
+from typing import Dict, Optional, Tuple, Union
 
 import torch
 
 from . import (ACT8_GROUP, AttnPlan, fgd_act_load8, fgd_act_save8, fgd_attn_backward, fgd_attn_forward, fgd_attn_status, fgd_block_norm_backward, fgd_block_norm_forward,
-               fgd_swiglu8_backward, fgd_swiglu8_forward)
+               fgd_dropout, fgd_embed_backward, fgd_embed_forward, fgd_qk_rope_backward, fgd_qk_rope_forward, fgd_swiglu8_backward, fgd_swiglu8_forward)
 
 
 # ------------------------------------------------------------------------------- operators
@@ -55,6 +55,84 @@ class _Attention(torch.autograd.Function):
 def attention(q, k, v, plan: AttnPlan, scale: Optional[float] = None):
     """Causal attention over the plan's packed sequences: q [T, Hq, d], k and v [T, Hk, d] -> [T, Hq, d]."""
     return _Attention.apply(q, k, v, plan, scale)
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, tokens, table, scale, dtype):
+        out = torch.empty((tokens.numel(), table.shape[2]), dtype=dtype, device=table.device)
+        fgd_embed_forward(tokens, table, out, scale)
+        ctx.save_for_backward(tokens)
+        ctx.shape, ctx.scale = table.shape, scale
+        return out
+
+    @staticmethod
+    @_first_order
+    def backward(ctx, dout):
+        tokens, = ctx.saved_tensors
+        dtable = torch.empty(ctx.shape, dtype=torch.float32, device=dout.device)
+        fgd_embed_backward(tokens, dout.contiguous(), dtable, ctx.scale)
+        return None, dtable, None, None
+
+
+def embedding(tokens, table, scale: float = 1.0, dtype: torch.dtype = torch.bfloat16):
+    """scale * table[m, tokens[m]] of every worker m: tokens [K, rows] (below 0: padding, a row of zeros), table [K, V, W] fp32, which may be a column range
+    of the parameter matrix -> [K * rows, W]."""
+    return _Embedding.apply(tokens, table, scale, dtype)
+
+
+class _QkvRope(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, qkv, w_q, w_k, cos, sin, positions, n_q, n_k, eps, interleaved):
+        q, k = qkv[:, :n_q], qkv[:, n_q:n_q + n_k]
+        q_out, k_out = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
+        fgd_qk_rope_forward(q, k, w_q, w_k, cos, sin, positions, q_out, k_out, eps, interleaved)
+        ctx.save_for_backward(None if w_q is None and w_k is None else qkv, w_q, w_k, cos, sin, positions)
+        ctx.heads, ctx.eps, ctx.interleaved = (n_q, n_k, qkv.shape[1]), eps, interleaved
+        return q_out, k_out, qkv[:, n_q + n_k:]
+
+    @staticmethod
+    @_first_order
+    def backward(ctx, dq_out, dk_out, dv):
+        qkv, w_q, w_k, cos, sin, positions = ctx.saved_tensors
+        n_q, n_k, heads = ctx.heads
+        dqkv = torch.empty((dq_out.shape[0], heads, dq_out.shape[2]), dtype=dq_out.dtype, device=dq_out.device)
+        like = lambda t: None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device)  # noqa: E731
+        dw_q, dw_k = like(w_q), like(w_k)
+        q, k = (None, None) if qkv is None else (qkv[:, :n_q], qkv[:, n_q:n_q + n_k])
+        fgd_qk_rope_backward(dq_out.contiguous(), dk_out.contiguous(), q, k, w_q, w_k, cos, sin, positions, dqkv[:, :n_q], dqkv[:, n_q:n_q + n_k], dw_q, dw_k,
+                             ctx.eps, ctx.interleaved)
+        dqkv[:, n_q + n_k:].copy_(dv)
+        return dqkv, dw_q, dw_k, None, None, None, None, None, None, None
+
+
+def qkv_rope(qkv, n_q: int, n_k: int, cos, sin, positions=None, w_q=None, w_k=None, eps: float = 1e-5, interleaved: bool = False):
+    """(q, k, v) of a fused projection's output [T, n_q + n_k + values' heads, d]: q and k normalised per head (w_q, w_k [K, d]; None: not) and rotated by rows
+    ``positions`` (None: row t) of the tables cos and sin [N, r / 2]; v is a view of qkv."""
+    return _QkvRope.apply(qkv, w_q, w_k, cos, sin, positions, n_q, n_k, eps, interleaved)
+
+
+class _Dropout(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, p, seed, offset, counter):
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        fgd_dropout(x, out, p, seed, offset, counter)
+        ctx.save_for_backward(counter)      # (changed in place before the backward pass it would give another mask: an error there)
+        ctx.how = p, seed, offset
+        return out
+
+    @staticmethod
+    @_first_order
+    def backward(ctx, dout):
+        counter, = ctx.saved_tensors
+        dx = torch.empty(dout.shape, dtype=dout.dtype, device=dout.device)
+        fgd_dropout(dout.contiguous(), dx, *ctx.how, counter)
+        return dx, None, None, None, None
+
+
+def dropout(x, p: float, seed: int, offset: int = 0, counter=None):
+    """x / (1 - p) or 0, x [rows, width]; the mask is a function of (seed, offset + counter, row, column) and is made again in the backward pass."""
+    return _Dropout.apply(x, p, seed, offset, counter)
 
 
 class _BlockNorm(torch.autograd.Function):
@@ -174,6 +252,9 @@ class DecoderConfig:
     ffn: int = 512
     eps: float = 1e-5
     rope_base: float = 10000.0
+    embed_scale: float = 1.0
+    qk_norm: bool = False      # norms of queries and keys, per head, with weights per channel
+    dropout: float = 0.0       # of the embeddings and of every block's output, in training
 
     @property
     def res_scale(self) -> float:
@@ -199,6 +280,9 @@ def param_layout(cfg: DecoderConfig) -> Tuple[Dict[str, Tuple[int, Tuple[int, ..
         for block in ("attn", "mlp"):
             for name in ("pre", "post", "gate"):
                 add(f"{i}.{block}.{name}", cfg.width)
+        if cfg.qk_norm:
+            for name in ("q_norm", "k_norm"):
+                add(f"{i}.{name}", cfg.head_dim)
         add(f"{i}.qkv", qkv, cfg.width)
         add(f"{i}.out", cfg.width, cfg.n_q_heads * cfg.head_dim)
         add(f"{i}.up", 2 * cfg.ffn, cfg.width)
@@ -227,18 +311,14 @@ def init_params(theta: torch.Tensor, cfg: DecoderConfig, seed: int = 0) -> None:
 def _rope(cfg: DecoderConfig, positions):
     freq = cfg.rope_base ** (-torch.arange(0, cfg.head_dim, 2, device=positions.device, dtype=torch.float32) / cfg.head_dim)
     angle = positions[:, None].float() * freq
-    return angle.cos()[:, None], angle.sin()[:, None]
-
-
-def _rotate(x, cos, sin):
-    a, b = x.float().chunk(2, -1)
-    return torch.cat((a * cos - b * sin, b * cos + a * sin), -1).to(x.dtype)
+    return angle.cos(), angle.sin()
 
 
 def decoder_logits(theta: torch.Tensor, tokens: torch.Tensor, plan: AttnPlan, positions: torch.Tensor, cfg: DecoderConfig,
-                   dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+                   dtype: torch.dtype = torch.bfloat16, draw: Optional[Tuple[int, Union[int, torch.Tensor]]] = None) -> torch.Tensor:
     """Logits [K, rows, vocab] of the K workers.  theta [K, ld] fp32 (may require gradients), tokens [K, rows], positions [K * rows] of
-    every token in its sequence; the plan covers all K * rows tokens, worker after worker."""
+    every token in its sequence; the plan covers all K * rows tokens, worker after worker.  ``draw`` = (seed, step) in training: which of the
+    generator's masks cfg.dropout takes; the step is a number below 2^32 or, for captured passes, a CUDA int64 tensor of one.  None: no dropout."""
     layout, _ = param_layout(cfg)
     K, rows = tokens.shape
     T, hq, hk, d = K * rows, cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
@@ -251,17 +331,27 @@ def decoder_logits(theta: torch.Tensor, tokens: torch.Tensor, plan: AttnPlan, po
         at, (o, i) = layout[name]
         return theta[:, at:at + o * i].to(dtype).view(K, o, i)
 
+    sites = iter(range(1 + 2 * cfg.layers))
+
+    def dropped(x):      # every place has an offset of its own
+        if draw is None or cfg.dropout == 0.0:
+            return x
+        seed, step = draw
+        site = next(sites) << 32
+        return dropout(x, cfg.dropout, seed, site, step) if isinstance(step, torch.Tensor) else dropout(x, cfg.dropout, seed, site + step)
+
     cos, sin = _rope(cfg, positions)
-    embed = mat("embed")
-    x = torch.gather(embed, 1, tokens[:, :, None].expand(-1, -1, cfg.width)).reshape(T, cfg.width)
+    at, (V, W) = layout["embed"]
+    x = dropped(embedding(tokens, theta[:, at:at + V * W].unflatten(1, (V, W)), cfg.embed_scale, dtype))
     x, n = block_norm(x, None, None, None, vec("0.attn.pre"), cfg.eps)
     for i in range(cfg.layers):
         qkv = linear8(n, mat(f"{i}.qkv")).view(T, hq + 2 * hk, d)
-        q, k = _rotate(qkv[:, :hq], cos, sin), _rotate(qkv[:, hq:hq + hk], cos, sin)
-        o = attention(q, k, qkv[:, hq + hk:], plan)
-        y = linear8(o.view(T, hq * d), mat(f"{i}.out"))
+        w_q, w_k = (vec(f"{i}.q_norm"), vec(f"{i}.k_norm")) if cfg.qk_norm else (None, None)
+        q, k, v = qkv_rope(qkv, hq, hk, cos, sin, None, w_q, w_k, cfg.eps)
+        o = attention(q, k, v, plan)
+        y = dropped(linear8(o.view(T, hq * d), mat(f"{i}.out")))
         x, n = block_norm(x, y, vec(f"{i}.attn.gate"), vec(f"{i}.attn.post"), vec(f"{i}.mlp.pre"), cfg.eps, cfg.res_scale)
-        y = swiglu8_linear(linear8(n, mat(f"{i}.up")), mat(f"{i}.down"))
+        y = dropped(swiglu8_linear(linear8(n, mat(f"{i}.up")), mat(f"{i}.down")))
         after = vec(f"{i + 1}.attn.pre") if i + 1 < cfg.layers else vec("final")
         x, n = block_norm(x, y, vec(f"{i}.mlp.gate"), vec(f"{i}.mlp.post"), after, cfg.eps, cfg.res_scale)
     return linear8(n, mat("head")).view(K, rows, cfg.vocab)
@@ -278,15 +368,16 @@ def worker_losses(logits: torch.Tensor, targets: torch.Tensor) -> torch.Tensor:
 class InnerSteps:
     """H local AdamW steps of all K workers on theta [K, ld] (each worker's own gradient, its own moments)."""
 
-    def __init__(self, theta: torch.Tensor, cfg: DecoderConfig, lr: float = 1e-3, betas=(0.9, 0.95), eps: float = 1e-8, weight_decay: float = 0.0):
-        self.theta, self.cfg, self.lr, self.betas, self.eps, self.weight_decay = theta, cfg, lr, betas, eps, weight_decay
+    def __init__(self, theta: torch.Tensor, cfg: DecoderConfig, lr: float = 1e-3, betas=(0.9, 0.95), eps: float = 1e-8, weight_decay: float = 0.0,
+                 seed: int = 0):
+        self.theta, self.cfg, self.lr, self.betas, self.eps, self.weight_decay, self.seed = theta, cfg, lr, betas, eps, weight_decay, seed
         self.m, self.v, self.t = torch.zeros_like(theta), torch.zeros_like(theta), 0
 
     def step(self, tokens, targets, plan: AttnPlan, positions) -> torch.Tensor:
         """One step on a batch; returns the workers' losses before it.  Raises FgdError, with parameters and moments as they were, if a
         device-side wait of the attention kernels gave up (it waits for the gradients to know)."""
         leaf = self.theta.detach().requires_grad_(True)
-        losses = worker_losses(decoder_logits(leaf, tokens, plan, positions, self.cfg), targets)
+        losses = worker_losses(decoder_logits(leaf, tokens, plan, positions, self.cfg, draw=(self.seed, self.t)), targets)
         losses.sum().backward()      # (the workers share no parameter: every row gets its own worker's gradient)
         fgd_attn_status(plan)
         with torch.no_grad():
