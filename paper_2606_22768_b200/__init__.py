@@ -852,10 +852,14 @@ def fgd_embed_backward(tokens, dout, dtable, scale: float = 1.0, workspace=None,
     tab, (K, V, W) = _table(dtable, "dtable", dev), dtable.shape
     tok, rows = _embed_tokens(tokens, K, dev), tokens.shape[1]
     grad, handle = _mat(dout, "dout", dout.dtype, K * rows, W, dev), _stream_on(stream, dev)
+    room = 0, 0
     if workspace is None:
-        workspace = _scratch(fgd_embed_workspace(K, rows, V, W), stream, handle, dev)
-    _op_check(_lib.fgd_embed_backward(dev.index, _dtype_of(dout, "dout"), K, rows, V, W, *tok, *grad, scale, *tab, _dev_ptr(workspace, "workspace", "torch.uint8"),
-                                      workspace.numel(), handle))
+        size = fgd_embed_workspace(K, rows, V, W)
+        if size:
+            workspace = _scratch(size, stream, handle, dev)
+    if workspace is not None:
+        room = _dev_ptr(workspace, "workspace", "torch.uint8"), workspace.numel()
+    _op_check(_lib.fgd_embed_backward(dev.index, _dtype_of(dout, "dout"), K, rows, V, W, *tok, *grad, scale, *tab, *room, handle))
 
 
 def fgd_dropout(x, out, p: float, seed: int, offset: int = 0, counter=None, stream=None) -> None:

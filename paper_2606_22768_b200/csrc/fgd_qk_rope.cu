@@ -13,7 +13,6 @@
 // its q first and then its k: so the weights and, in the backward pass, the sums of their gradients (CTAs belong to one worker) stay in
 // registers, of one side at a time.  What the next steps need is on its way meanwhile: activations through a ring in shared memory that each lane
 // fills for itself (cp.async), the next token's cos and sin in registers.
-#include <algorithm>
 #include <cmath>
 
 #include "fgd_dtype.cuh"
@@ -24,7 +23,10 @@ using namespace fgd;
 
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kThreads = 128, kWarps = kThreads / 32;
+// CTAs on an SM: what the kernels' registers allow.  (The backward pass with four, that is 128 registers a thread and some of them spilled: 109 us for
+// 8 x 4096 tokens of 20 heads of 128, against 96.)
+constexpr int kForwardCtas = 4, kBackwardCtas = 3;
 constexpr int kMaxDim = 256;
 
 struct RopeHeads { char* p; int64_t ts, hs, step; };      // strides, and from one of a warp's batches to the next, in bytes
@@ -283,7 +285,7 @@ __device__ __forceinline__ void poison(float (&z)[NC][2 * V]) {
 
 // GRAD: the backward pass with weights.  Otherwise the forward pass, or the transposed rotation alone.
 template <typename T, int V, int NC, bool INTER, bool GRAD>
-__global__ void __launch_bounds__(kThreads, 2) rope_kernel(const __grid_constant__ RopeArgs a) {
+__global__ void __launch_bounds__(kThreads, GRAD ? kBackwardCtas : kForwardCtas) rope_kernel(const __grid_constant__ RopeArgs a) {
   constexpr int N = GRAD ? 2 : 1;      // tensors that are read: the gradient, x; or x alone
   using Ring = Feed<T, V, NC, N>;
   extern __shared__ __align__(16) unsigned char ring[];
@@ -297,7 +299,7 @@ __global__ void __launch_bounds__(kThreads, 2) rope_kernel(const __grid_constant
   if constexpr (GRAD) let_next_start();      // the sums' CTAs wait for this kernel's end on the SMs
   // The step that is fetched next, kDepth - 1 ahead: side, first token of the warp's group, batch, addresses.  (An address moves on by a constant
   // within a token; worked out anew in every step they were a third of the kernel's instructions.)
-  int ahead_side = first < rows ? 0 : 2, ahead_b = part;
+  int ahead_side = first >= rows ? 2 : part < a.side[0].batches ? 0 : 1, ahead_b = part;
   uint32_t ahead_t0 = first;
   const char* in[N];
   auto at = [&](const RopeHeads& h, uint32_t t0) { return h.p + (base + t0) * h.ts + (sub + part * a.gt) * h.hs + geo.c0[0] * (int)sizeof(T); };      // of a lane's first channel
@@ -317,7 +319,7 @@ __global__ void __launch_bounds__(kThreads, 2) rope_kernel(const __grid_constant
     ahead_t0 += stride;
     if (ahead_t0 >= rows) {
       ahead_t0 = first;
-      if (++ahead_side == 1 && a.side[1].batches == 0) ahead_side = 2;
+      if (++ahead_side == 1 && part >= a.side[1].batches) ahead_side = 2;
     }
     if (ahead_side < 2) seek(a.side[ahead_side]);
   };
@@ -326,7 +328,8 @@ __global__ void __launch_bounds__(kThreads, 2) rope_kernel(const __grid_constant
     const bool real = ahead_side < 2 && ahead_t0 + mine < rows;
     feed.fetch(in, real, real && a.side[ahead_side & 1].w != nullptr, steps, geo);      // (without weights x may be absent)
   };
-  seek(a.side[0]);
+  if (ahead_side == 1 && part >= a.side[1].batches) ahead_side = 2;
+  seek(a.side[ahead_side & 1]);
   feed.start(ring, geo.has0[0]);
   if constexpr (Ring::kRing) {
 #pragma unroll
@@ -338,7 +341,6 @@ __global__ void __launch_bounds__(kThreads, 2) rope_kernel(const __grid_constant
 #pragma unroll 1
   for (int side = 0; side < 2; ++side) {
     const RopeSide& s = a.side[side];
-    if (s.batches == 0) break;
     const bool norm = s.w != nullptr;      // (of the gradient's kernel: one of the sides may be the rotation alone)
     float w[NC][2 * V], dw[NC][2 * V];
     if (norm) load_weights(s.w + worker * s.w_ld, geo, w);
@@ -346,26 +348,24 @@ __global__ void __launch_bounds__(kThreads, 2) rope_kernel(const __grid_constant
     for (int j = 0; j < NC; ++j)
 #pragma unroll
       for (int i = 0; i < 2 * V; ++i) dw[j][i] = 0.f;
-    // Forward: positions two tokens ahead, cos and sin one.  (The backward pass has no registers for that: with them 126 us, without 108, for
-    // 8 x 4096 tokens of 20 heads of 128.)
+    // Forward: positions two tokens ahead, cos and sin one.  The backward pass has no registers for that: 126 us with them for 8 x 4096 tokens of 20
+    // heads of 128, 109 without.
     auto position = [&](uint32_t t0) { return t0 + mine < rows ? position_of(a, base + t0) : (int64_t)-1; };
     Angles<V, NC> turn, next;
-    int64_t pos = -1;
-    if constexpr (!GRAD) {
-      next.load(a, geo, position(first));
-      pos = position(first + stride);
-    }
-    for (uint32_t t0 = first; t0 < rows; t0 += stride) {
+    if constexpr (!GRAD) next.load(a, geo, position(first));
+    int64_t pos = position(GRAD ? first : first + stride);
+    for (uint32_t t0 = part < s.batches ? first : rows; t0 < rows; t0 += stride) {
       const bool real = t0 + mine < rows;
       if constexpr (GRAD) {
-        turn.load(a, geo, position(t0));
+        turn.load(a, geo, pos);
+        pos = position(t0 + stride);
       } else {
         turn = next;
         next.load(a, geo, pos);
         pos = position(t0 + 2 * stride);
       }
       char* out = at(s.y, t0);
-#pragma unroll 2
+#pragma unroll (GRAD ? 1 : 2)
       for (int b = part; b < s.batches; b += a.split, out += s.y.step) {
         feed.wait();
         float z[NC][2 * V], v[NC][2 * V];
@@ -454,28 +454,29 @@ __global__ void __launch_bounds__(kThreads, 2) rope_kernel(const __grid_constant
   }
 }
 
-// dw of a worker and side: its CTAs' sums, eight at a time added in order, 32 channels a CTA.
+// dw of a worker and side: its CTAs' sums, 32 at a time added in order, 32 channels a CTA.
+constexpr int kParts = 32;
 struct RopeSums { const float* partial; float* dw[2]; int64_t ld[2]; int ctas, d; };
-__global__ void __launch_bounds__(256) rope_sums_kernel(const RopeSums a) {
+__global__ void __launch_bounds__(32 * kParts) rope_sums_kernel(const __grid_constant__ RopeSums a) {
   wait_for_previous();
-  __shared__ float buf[8][32];
+  __shared__ float buf[kParts][32];
   const int lane = threadIdx.x & 31, part = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, worker = blockIdx.y, side = blockIdx.z;
-  float* dw = side ? a.dw[1] : a.dw[0];
-  if (!dw) return;
+  if (!a.dw[side]) return;
+  const float* p = a.partial + ((int64_t)worker * a.ctas * 2 + side) * a.d + c;
   float t = 0.f;
-  if (c < a.d)
-    for (int i = part; i < a.ctas; i += 8) t += a.partial[(((int64_t)worker * a.ctas + i) * 2 + side) * a.d + c];
+  if (c < a.d) {
+#pragma unroll 8
+    for (int i = part; i < a.ctas; i += kParts) t += p[(int64_t)i * 2 * a.d];
+  }
   buf[part][lane] = t;
   __syncthreads();
   if (part != 0 || c >= a.d) return;
 #pragma unroll
-  for (int i = 1; i < 8; ++i) t += buf[i][lane];
-  dw[worker * (side ? a.ld[1] : a.ld[0]) + c] = t;
+  for (int i = 1; i < kParts; ++i) t += buf[i][lane];
+  a.dw[side][worker * a.ld[side] + c] = t;
 }
 
 // ---- host
-constexpr int kCtasPerSm = 2;      // of the persistent grid
-
 // The largest power of two that divides both head counts, at most `groups`.
 int group_of(int q_heads, int k_heads, int groups) {
   int g = 1;
@@ -483,8 +484,8 @@ int group_of(int q_heads, int k_heads, int groups) {
   return g;
 }
 // CTAs of one worker: its share of the SMs' places, and no more than there is work for.
-int ctas_for(int64_t workers, int64_t rows, int64_t warp_tokens) {
-  int64_t c = (int64_t)sm_count() * kCtasPerSm / workers;
+int ctas_for(int per_sm, int64_t workers, int64_t rows, int64_t warp_tokens) {
+  int64_t c = (int64_t)sm_count() * per_sm / workers;
   const int64_t most = (rows + kWarps * warp_tokens - 1) / (kWarps * warp_tokens);
   if (c > most) c = most;
   return (int)(c < 1 ? 1 : c);
@@ -496,7 +497,7 @@ bool vector_of(const void* p, int64_t s0, int64_t s1, int bytes, int vec) {
 
 struct Launch { int vec, lg, pairs; };
 
-int64_t workspace_bytes(int workers, int d) { return ((int64_t)sm_count() * kCtasPerSm + workers) * 2 * d * (int64_t)sizeof(float); }
+int64_t workspace_bytes(int workers, int d) { return ((int64_t)sm_count() * kBackwardCtas + workers) * 2 * d * (int64_t)sizeof(float); }
 
 template <typename T, int V, int NC, bool INTER, bool GRAD>
 cudaError_t start(const RopeArgs& a, int workers, int ctas, cudaStream_t st) {
@@ -654,17 +655,21 @@ int run_rope(const fgd_qk_rope_args* b, bool backward, int device, void* stream)
     a.rows = b->rows; a.table_rows = b->table_rows;
     a.d = d; a.rot = rot; a.lg = l.lg; a.pairs = l.pairs;
     a.gt = group_of(heads[0], heads[1], 32 / l.lg);
-    // Where tokens are too few for the SMs' warps, several share a token's heads.
-    const int64_t tokens = 32 / l.lg / a.gt, warps = b->workers * ((b->rows + tokens - 1) / tokens), places = (int64_t)sm_count() * kCtasPerSm * kWarps;
-    const int fewest = (use[1] ? std::min(heads[0], heads[1]) : heads[0]) / a.gt;
-    a.split = 1;
-    while (a.split * 2 <= fewest && a.split * 2 * warps <= places && a.split < kWarps) a.split *= 2;
+    // Warps share a token's heads where that evens out the rounds of the SMs' warps over the tokens (a step for a batch, and two more for each token).
+    const int64_t tokens = 32 / l.lg / a.gt, warps = b->workers * ((b->rows + tokens - 1) / tokens);
+    const int per_sm = sums ? kBackwardCtas : kForwardCtas;
+    int64_t least = 0;
+    for (int split = 1; split <= kWarps; split *= 2) {
+      const int64_t places = (int64_t)sm_count() * per_sm * kWarps, rounds = (warps * split + places - 1) / places;
+      const int64_t cost = rounds * ((heads[0] / a.gt + split - 1) / split + (heads[1] / a.gt + split - 1) / split + 2);
+      if (split == 1 || cost < least) { least = cost; a.split = split; }
+    }
     for (int i = 0; i < 2; ++i) {
       RopeSide& side = a.side[i];
       side.batches = heads[i] / a.gt;
       for (RopeHeads* h : {&side.x, &side.y, &side.g}) h->step = h->hs * a.gt * a.split;
     }
-    c.ctas = ctas_for(b->workers, b->rows * a.split, tokens);
+    c.ctas = ctas_for(per_sm, b->workers, b->rows * a.split, tokens);
     a.eps = (float)b->eps; a.inv_d = 1.f / (float)d; a.turn = backward ? -1.f : 1.f;
     const bool inter = b->interleaved != 0;
     auto by_vec = [&](auto zero) {
@@ -680,7 +685,7 @@ int run_rope(const fgd_qk_rope_args* b, bool backward, int device, void* stream)
       default: e = by_vec(__half{}); break;
     }
   }
-  if (e == cudaSuccess && sums) e = launch_early(rope_sums_kernel, dim3((unsigned)((d + 31) / 32), (unsigned)b->workers, 2), 256, 0, st, c);
+  if (e == cudaSuccess && sums) e = launch_early(rope_sums_kernel, dim3((unsigned)((d + 31) / 32), (unsigned)b->workers, 2), 32 * kParts, 0, st, c);
   return e == cudaSuccess ? FGD_OK : op_fail(FGD_ERR_CUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
 }
 
