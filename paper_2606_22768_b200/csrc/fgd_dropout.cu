@@ -58,13 +58,13 @@ struct RowWords {
   static constexpr uint32_t kM0 = 0xD2511F53u, kM1 = 0xCD9E8D57u, kW0 = 0x9E3779B9u, kW1 = 0xBB67AE85u;
 };
 
-// The values of V columns from column c on.
+// V values from column 4 group on.
 template <int V>
-__device__ __forceinline__ Vals<V> drop(const Vals<V>& x, uint32_t c, const RowWords& row, const DropoutArgs& a) {
+__device__ __forceinline__ Vals<V> drop(const Vals<V>& x, uint32_t group, const RowWords& row, const DropoutArgs& a) {
   Vals<V> y;
 #pragma unroll
   for (int g = 0; g < V / 4; ++g) {
-    const uint4 w = row.words(c / 4 + g);
+    const uint4 w = row.words(group + g);
     const float2 lo = mul2(x.pair(2 * g), both(a.scale)), hi = mul2(x.pair(2 * g + 1), both(a.scale));
     y.v[4 * g] = w.x >= a.threshold ? lo.x : 0.f;
     y.v[4 * g + 1] = w.y >= a.threshold ? lo.y : 0.f;
@@ -73,37 +73,100 @@ __device__ __forceinline__ Vals<V> drop(const Vals<V>& x, uint32_t c, const RowW
   }
   return y;
 }
+// The generator's verdicts on V columns from column 4 group on, a bit each.
+template <int V>
+__device__ __forceinline__ uint32_t verdicts(uint32_t group, const RowWords& row, const DropoutArgs& a) {
+  uint32_t keep = 0;
+#pragma unroll
+  for (int g = 0; g < V / 4; ++g) {
+    const uint4 w = row.words(group + g);
+    keep |= (w.x >= a.threshold ? 1u << 4 * g : 0u) | (w.y >= a.threshold ? 2u << 4 * g : 0u) | (w.z >= a.threshold ? 4u << 4 * g : 0u) | (w.w >= a.threshold ? 8u << 4 * g : 0u);
+  }
+  return keep;
+}
 
 __device__ __forceinline__ uint64_t offset_of(const DropoutArgs& a) { return a.offset + (a.counter ? (uint64_t)__ldg(a.counter) : 0u); }
 
-// Rows on 16-byte boundaries: a warp takes strips of kStrip x 32 units of 16 bytes of a row.  32768 x 4096 bf16: 86 us, 95 % of the copy peak (with one
-// unit a thread and nothing shared between them 106 us: bound by the generator's instructions).
+// A warp takes strips of kStrip x 32 chunks of 16 bytes of a row.  32768 x 4096 bf16: 86 us, 95 % of the copy peak (with one chunk a thread and nothing
+// shared between them 106 us: bound by the generator's instructions).
+// INSIDE: rows that start inside a chunk, x and out at the same place of one.  A row's chunks are then those of memory; its first and last are
+// taken value by value.  Where columns of a chunk begin m behind a group of the generator, a lane makes V verdicts from that group on and gets
+// the m that it lacks from the next lane.
 constexpr int kStrip = 4;
-template <typename T>
+// The values of a chunk at p that are columns of the row: c is the first one's.
+template <typename T, int V>
+__device__ __forceinline__ ActPack<T, V> load_some(const T* p, int c, int width) {
+  Vals<V> v;
+#pragma unroll
+  for (int j = 0; j < V; ++j) v.v[j] = 0.f;
+#pragma unroll
+  for (int j = 0; j < V; ++j)
+    if (c + j >= 0 && c + j < width) v.v[j] = to_f32(p[j]);
+  return round_to<T, V>(v);
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_some(T* p, const ActPack<T, V>& y, int c, int width) {
+  const Vals<V> v = unpack<T, V>(y);
+#pragma unroll
+  for (int j = 0; j < V; ++j)
+    if (c + j >= 0 && c + j < width) p[j] = from_f32<T>(v.v[j]);
+}
+template <typename T, bool INSIDE>
 __global__ void __launch_bounds__(kThreads) dropout_kernel(const DropoutArgs a) {
-  constexpr int V = 16 / sizeof(T);
+  constexpr int V = 16 / sizeof(T), kColumns = 32 * kStrip * V;
   const uint64_t offset = offset_of(a);
-  const int lane = threadIdx.x & 31, strips = (int)((a.width + 32 * kStrip * V - 1) / (32 * kStrip * V));
+  const int lane = threadIdx.x & 31, strips = (int)((a.width + (INSIDE ? V - 1 : 0) + kColumns - 1) / kColumns);
   const int64_t total = a.rows * strips, stride = (int64_t)gridDim.x * (kThreads / 32);
   int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / 32;
   Walk w(i, stride, strips);
   for (; i < total; i += stride, w.next()) {
-    const int64_t c0 = ((int64_t)w.unit * (32 * kStrip) + lane) * V;
-    const T* x = reinterpret_cast<const T*>(a.x) + w.row * a.ld_x + c0;
-    T* out = reinterpret_cast<T*>(a.out) + w.row * a.ld_out + c0;
+    const T* x = reinterpret_cast<const T*>(a.x) + w.row * a.ld_x;
+    T* out = reinterpret_cast<T*>(a.out) + w.row * a.ld_out;
+    const int before = INSIDE ? (int)((reinterpret_cast<uintptr_t>(x) & 15u) / sizeof(T)) : 0;      // columns that the row's first chunk has before it
+    const int c0 = (w.unit * (32 * kStrip) + lane) * V - before, width = (int)a.width;      // (they end below 2^31: see the launch)
+    const RowWords row((uint32_t)w.row, offset, a);
     ActPack<T, V> raw[kStrip];
 #pragma unroll
-    for (int k = 0; k < kStrip; ++k)
-      if (c0 + k * 32 * V < a.width) raw[k] = load_stream<T, V>(x + k * 32 * V);
-    const RowWords row((uint32_t)w.row, offset, a);
+    for (int k = 0; k < kStrip; ++k) {
+      const int c = c0 + k * 32 * V;
+      if (!INSIDE ? c < width : c >= 0 && c + V <= width) raw[k] = load_stream<T, V>(x + c);
+      else if (INSIDE && c > -V && c < width) raw[k] = load_some<T, V>(x + c, c, width);
+    }
+    if constexpr (INSIDE) {
+      const int m = -before & 3;      // c0 - m is a multiple of 4 (-4 in a row's first chunk, where what is made of that group is not used)
+      const int group = (c0 - m) >> 2, chunks = (width - c0 + lane * V + V - 1) / V;      // (of the row from this strip's first on: the same in all lanes)
+      uint32_t keep[kStrip + 1];
 #pragma unroll
-    for (int k = 0; k < kStrip; ++k)
-      if (c0 + k * 32 * V < a.width) store_stream<T, V>(out + k * 32 * V, round_to<T, V>(drop<V>(unpack<T, V>(raw[k]), (uint32_t)(c0 + k * 32 * V), row, a)));
+      for (int k = 0; k <= kStrip; ++k)
+        if (k * 32 < chunks || k == 0) keep[k] = k < kStrip ? verdicts<V>((uint32_t)(group + k * 8 * V), row, a) : verdicts<4>((uint32_t)(group + k * 8 * V), row, a);
+#pragma unroll
+      for (int k = 0; k < kStrip; ++k) {
+        if (k * 32 >= chunks) break;
+        const uint32_t above = __shfl_down_sync(0xffffffffu, keep[k], 1), first = (k + 1) * 32 < chunks ? __shfl_sync(0xffffffffu, keep[k + 1], 0) : 0u;
+        const uint32_t bits = (keep[k] | (lane == 31 ? first : above) << V) >> m;
+        const int c = c0 + k * 32 * V;
+        Vals<V> y = unpack<T, V>(raw[k]);
+#pragma unroll
+        for (int j = 0; j < V; j += 2) {
+          const float2 t = mul2(y.pair(j / 2), both(a.scale));
+          y.v[j] = bits >> j & 1u ? t.x : 0.f;
+          y.v[j + 1] = bits >> j & 2u ? t.y : 0.f;
+        }
+        if (c >= 0 && c + V <= width) store_stream<T, V>(out + c, round_to<T, V>(y));
+        else if (c < width) store_some<T, V>(out + c, round_to<T, V>(y), c, width);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < kStrip; ++k) {
+        const int c = c0 + k * 32 * V;
+        if (c < width) store_stream<T, V>(out + c, round_to<T, V>(drop<V>(unpack<T, V>(raw[k]), (uint32_t)c / 4, row, a)));
+      }
+    }
   }
 }
 
-// Rows that start or end anywhere, and narrow ones: units of 16 values, moved with shifts (fgd_units.cuh).  5003 x 4097 fp32: 35 us, 71 % of the copy
-// peak; bf16 54 %: what the shifts and the generator cost in instructions.
+// Every other row: units of 16 values, moved with shifts (fgd_units.cuh).  fp32 70 % of the copy peak, bf16 33 to 54 %: what the shifts and the generator cost
+// in instructions.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) dropout_shifted_kernel(const DropoutArgs a) {
   constexpr int V = 16;
@@ -119,7 +182,7 @@ __global__ void __launch_bounds__(kThreads) dropout_shifted_kernel(const Dropout
     const ShiftedUnit<V> u(w, i < total, a.width);
     const Vals<V> v = load_shifted<T, V>(x + w.row * a.ld_x + u.c, u, x, end);
     const RowWords row((uint32_t)w.row, offset, a);
-    store_shifted<T, V>(out + w.row * a.ld_out + u.c, u, drop<V>(v, (uint32_t)u.c, row, a));
+    store_shifted<T, V>(out + w.row * a.ld_out + u.c, u, drop<V>(v, (uint32_t)u.c / 4, row, a));
   }
 }
 
@@ -147,7 +210,7 @@ extern "C" int fgd_dropout(int device, int dtype, int64_t rows, int64_t width, c
   FGD_NVTX_RANGE("fgd_dropout");
   const int b = dtype_bytes(dtype);
   if (b == 0) return op_fail(FGD_ERR_INVALID_ARG, "fgd_dropout: unknown dtype %d", dtype);
-  if (rows < 0 || rows > 0xffffffffll || width < 0 || width > 0x7fffffffll - 64)
+  if (rows < 0 || rows > 0xffffffffll || width < 0 || width > 0x7fffffffll - 4096)
     return op_fail(FGD_ERR_INVALID_ARG, "fgd_dropout: rows=%lld, width=%lld out of range", (long long)rows, (long long)width);
   if (!(p >= 0.0 && p < 1.0)) return op_fail(FGD_ERR_INVALID_ARG, "fgd_dropout: p=%g is not in [0, 1)", p);
   if (rows == 0 || width == 0) return FGD_OK;
@@ -169,14 +232,18 @@ extern "C" int fgd_dropout(int device, int dtype, int64_t rows, int64_t width, c
   a.threshold = t > 4294967295.0 ? 4294967295u : (uint32_t)t;      // (2^32: p within 2^-33 of 1)
   a.scale = (float)(1.0 / (1.0 - p));
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  // Strips where rows are on 16-byte boundaries and give a warp a full pass: 100 MB of bf16, 256 columns 46 us against 57 by shifts, 128 columns 84
-  // against 57.  (Of 2, 4 and 8 passes to a strip 92, 86 and 93 us for 32768 x 4096 bf16; of 1, 4, 16, 64 CTAs for each place on the SMs 92, 86, 90,
-  // 94; by shifts 1 is the best: 5003 x 4097 fp32 34.9 us, 4: 36.2, 16: 38.5.)
+  // 100 MB of bf16: strips where rows are on 16-byte boundaries and give a warp a full pass (256 columns 46 us against 57 by shifts, 128 columns 84
+  // against 57); inside chunks where both sides lie alike and rows are long (3033 columns 58 against 68, 1025 92 against 72; fp32 37 against 42 and
+  // 43 against 44); else by shifts.  CTAs for each place on the SMs: of 1, 4, 16, 64 for strips 92, 86, 90, 94 us (32768 x 4096), by shifts 35, 36, 39, 38
+  // (5003 x 4097 fp32); chunks to a lane of a strip: of 2, 4, 8 92, 86, 93.
   const bool strips = (width * b) % 16 == 0 && width * b >= 32 * 16 && on16(x, ld_x, b) && on16(out, ld_out, b);
+  const bool together = width * b >= 4096 && ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(out)) & 15u) == 0 && ((ld_x - ld_out) * b) % 16 == 0;
   auto launch = [&](auto zero) {
     using T = decltype(zero);
-    constexpr int64_t strip = 32 * kStrip * 16 / sizeof(T);
-    return strips ? go<dropout_kernel<T>>(a, rows * ((width + strip - 1) / strip) * 32, 4, st) : go<dropout_shifted_kernel<T>>(a, rows * ((width + 15) / 16), 1, st);
+    constexpr int64_t V = 16 / sizeof(T), strip = 32 * kStrip * V;
+    if (strips) return go<dropout_kernel<T, false>>(a, rows * ((width + strip - 1) / strip) * 32, 4, st);
+    if (together) return go<dropout_kernel<T, true>>(a, rows * ((width + V - 1 + strip - 1) / strip) * 32, 4, st);
+    return go<dropout_shifted_kernel<T>>(a, rows * ((width + 15) / 16), 1, st);
   };
   const cudaError_t e = dtype == FGD_F32 ? launch(float{}) : dtype == FGD_BF16 ? launch(__nv_bfloat16{}) : launch(__half{});
   return e == cudaSuccess ? FGD_OK : op_fail(FGD_ERR_CUDA, "fgd_dropout: launch failed: %s", cudaGetErrorString(e));

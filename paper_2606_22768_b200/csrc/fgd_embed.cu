@@ -52,63 +52,63 @@ struct EmbedArgs {
   Tokens tokens;
   const float* table; int64_t worker_stride, row_stride;
   char* out; int64_t ld_out;
-  int64_t rows, tokens_total, vocab;
-  int width, parts, slabs;     // of a row: parts that a warp takes, of so many slabs each (kSlabs at most)
+  int64_t rows, vocab;
+  int width;
   float scale;
 };
 constexpr int kSlabs = 4;
 
-// A warp has kSlabs slabs on their way at once: of one row, or where a row is no more than one (SHORT) of as many rows.  (Rows and slabs
-// mixed freely, 4 x 8192 tokens of 2048 take 61 us instead of 39: every slab then has its own token, and its place to be worked out.)  39 us are 94 % of the
-// copy peak; five CTAs to an SM, with four 41, with six 49.
+// A warp has kSlabs slabs on their way at once: of one row, or where a row is no more than one (SHORT) of as many rows.  4 x 8192 tokens of 2048 bf16
+// 39 us, 94 % of the copy peak (with rows and slabs mixed freely 61: every slab then has its own token, and its place to be worked out); 41160 tokens of
+// 1002 columns 22 us, 57 %.  CTAs to an SM: as many as the registers of the loads in flight allow (six of five: 45 us).
 template <typename T, bool ANY, bool SHORT>
-__global__ void __launch_bounds__(kThreads, SHORT ? 4 : 5) embed_forward_kernel(const EmbedArgs a) {
+__global__ void __launch_bounds__(kThreads, SHORT ? 3 : ANY ? 4 : 5) embed_forward_kernel(const EmbedArgs a) {
   using S = Slab<T, ANY>;
   constexpr int V = S::V, ROWS = SHORT ? kSlabs : 1;
-  const int64_t items = SHORT ? (a.tokens_total + ROWS - 1) / ROWS : a.tokens_total * a.parts;
-  for (int64_t item = (int64_t)blockIdx.x * kWarps + threadIdx.x / 32; item < items; item += (int64_t)gridDim.x * kWarps) {
-    const int64_t t0 = SHORT ? item * ROWS : item / a.parts;
-    const int c0 = SHORT ? 0 : (int)(item - t0 * a.parts) * (a.slabs * S::kColumns), end = SHORT ? a.width : min(a.width, c0 + a.slabs * S::kColumns);
-    const float* row[ROWS];
-    float other[ROWS];         // of a token outside the vocabulary
-    bool real[ROWS];
+  // the worker is the grid's second axis: 64-bit divisions would be a good part of the instructions
+  const int64_t worker = blockIdx.y, t0 = ((int64_t)blockIdx.x * kWarps + threadIdx.x / 32) * ROWS;
+  if (t0 >= a.rows) return;
+  const float* row[ROWS];
+  float other[ROWS];           // of a token outside the vocabulary
+  bool real[ROWS];
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-      const int64_t t = t0 + r < a.tokens_total ? t0 + r : t0, worker = t / a.rows, tok = a.tokens.at(worker, t - worker * a.rows);
-      real[r] = tok >= 0 && tok < a.vocab;
-      other[r] = tok < 0 ? 0.f : __int_as_float(0x7fffffff);
-      row[r] = a.table + worker * a.worker_stride + (real[r] ? tok : 0) * a.row_stride;
-    }
+  for (int r = 0; r < ROWS; ++r) {
+    const int64_t tok = a.tokens.at(worker, t0 + r < a.rows ? t0 + r : t0);
+    real[r] = tok >= 0 && tok < a.vocab;
+    other[r] = tok < 0 ? 0.f : __int_as_float(0x7fffffff);
+    row[r] = a.table + worker * a.worker_stride + (real[r] ? tok : 0) * a.row_stride;
+  }
+  T* const out0 = reinterpret_cast<T*>(a.out) + (worker * a.rows + t0) * a.ld_out;
+  for (int c0 = blockIdx.z * (kSlabs * S::kColumns); c0 < a.width; c0 += gridDim.z * (kSlabs * S::kColumns)) {
     Vals<V> v[kSlabs];
 #pragma unroll
     for (int s = 0; s < kSlabs; ++s) {
       const int r = SHORT ? s : 0, c = SHORT ? 0 : c0 + s * S::kColumns;
       if constexpr (ANY) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[s].v[j] = real[r] && c + S::col(j) < end ? __ldg(row[r] + c + S::col(j)) : other[r];
+        for (int j = 0; j < V; ++j) v[s].v[j] = real[r] && c + S::col(j) < a.width ? __ldg(row[r] + c + S::col(j)) : other[r];
       } else {
 #pragma unroll
         for (int j = 0; j < V; j += 4) {
           float4 f = make_float4(other[r], other[r], other[r], other[r]);
-          if (real[r] && c + S::col(0) < end) f = __ldg(reinterpret_cast<const float4*>(row[r] + c + S::col(j)));
+          if (real[r] && c + S::col(0) < a.width) f = __ldg(reinterpret_cast<const float4*>(row[r] + c + S::col(j)));
           v[s].v[j] = f.x; v[s].v[j + 1] = f.y; v[s].v[j + 2] = f.z; v[s].v[j + 3] = f.w;
         }
       }
     }
 #pragma unroll
     for (int s = 0; s < kSlabs; ++s) {
-      const int64_t t = t0 + (SHORT ? s : 0);
-      if (t >= a.tokens_total) break;
-      T* out = reinterpret_cast<T*>(a.out) + t * a.ld_out;
+      if (SHORT && t0 + s >= a.rows) break;
+      T* out = out0 + (SHORT ? s : 0) * a.ld_out;
       const int c = SHORT ? 0 : c0 + s * S::kColumns;
 #pragma unroll
       for (int j = 0; j < V; ++j) v[s].v[j] *= a.scale;
       if constexpr (ANY) {
 #pragma unroll
         for (int j = 0; j < V; ++j)
-          if (c + S::col(j) < end) out[c + S::col(j)] = from_f32<T>(v[s].v[j]);
+          if (c + S::col(j) < a.width) out[c + S::col(j)] = from_f32<T>(v[s].v[j]);
       } else {
-        if (c + S::col(0) < end) store_stream<T, V>(out + c + S::col(0), round_to<T, V>(v[s]));
+        if (c + S::col(0) < a.width) store_stream<T, V>(out + c + S::col(0), round_to<T, V>(v[s]));
       }
     }
   }
@@ -630,13 +630,12 @@ Layout layout_of(int64_t workers, int64_t rows, int64_t vocab, int64_t width) {
 }
 
 template <typename T, bool ANY>
-cudaError_t forward(const EmbedArgs& e, cudaStream_t st) {
-  EmbedArgs a = e;
+cudaError_t forward(const EmbedArgs& a, int workers, cudaStream_t st) {
   const int slabs = (a.width + Slab<T, ANY>::kColumns - 1) / Slab<T, ANY>::kColumns;
-  a.parts = (slabs + kSlabs - 1) / kSlabs;
-  a.slabs = kSlabs;
-  const int64_t items = slabs == 1 ? (a.tokens_total + kSlabs - 1) / kSlabs : a.tokens_total * a.parts, ctas = (items + kWarps - 1) / kWarps, most = (int64_t)sm_count() * 64;
-  const unsigned grid = (unsigned)(ctas < most ? ctas : most);
+  const int64_t rows = slabs == 1 ? (a.rows + kSlabs - 1) / kSlabs : a.rows, ctas = (rows + kWarps - 1) / kWarps;
+  // a warp goes through its whole row, unless there are few rows: then its parts go to several
+  const int64_t parts = (slabs + kSlabs - 1) / kSlabs, cuts = (int64_t)sm_count() * 4 / (ctas * workers) + 1;
+  const dim3 grid((unsigned)ctas, (unsigned)workers, (unsigned)(cuts < parts ? cuts : parts));
   if (slabs == 1) embed_forward_kernel<T, ANY, true><<<grid, kThreads, 0, st>>>(a);
   else embed_forward_kernel<T, ANY, false><<<grid, kThreads, 0, st>>>(a);
   return cudaGetLastError();
@@ -722,9 +721,9 @@ extern "C" int fgd_embed_forward(int device, int dtype, int workers, int64_t row
   a.tokens = Tokens{tokens, token_bytes, ld_tokens};
   a.table = table; a.worker_stride = worker_stride; a.row_stride = row_stride;
   a.out = static_cast<char*>(out); a.ld_out = ld_out;
-  a.rows = rows; a.tokens_total = workers * rows; a.vocab = vocab; a.width = (int)width; a.scale = (float)scale;
+  a.rows = rows; a.vocab = vocab; a.width = (int)width; a.scale = (float)scale;
   const cudaError_t e = by_type(dtype, !aligned(table, worker_stride, row_stride, workers, out, ld_out, b, width),
-                                [&](auto zero, auto any) { return forward<decltype(zero), decltype(any)::value>(a, static_cast<cudaStream_t>(stream)); });
+                                [&](auto zero, auto any) { return forward<decltype(zero), decltype(any)::value>(a, workers, static_cast<cudaStream_t>(stream)); });
   return e == cudaSuccess ? FGD_OK : op_fail(FGD_ERR_CUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
 }
 

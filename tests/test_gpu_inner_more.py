@@ -378,7 +378,7 @@ def test_embed_gradient_is_the_transpose_of_the_lookup():
 # ------------------------------------------------------------------------------- dropout
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("R,W,ld,lead", [(1, 1, 1, 0), (3, 7, 7, 0), (40, 777, 777, 0), (5, 64, 64, 0), (33, 1024, 1040, 16), (9, 130, 131, 1), (17, 4097, 4097, 3), (2, 16, 1000, 5),
-                                         (300, 4, 4, 0), (1000, 33, 36, 2)])
+                                         (300, 4, 4, 0), (1000, 33, 36, 2), (6, 2500, 2501, 1), (4, 5001, 5005, 2), (9, 2049, 2049, 0), (5, 8195, 8203, 7)])
 def test_dropout(R, W, ld, lead, dtype):
     import paper_2606_22768_b200 as fgd
     torch = _torch()
