@@ -60,6 +60,7 @@ struct Chunk {
   __device__ __forceinline__ void from_shared(uint32_t p) {
     if constexpr (kBytes == 16) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(p) : "memory");
     else if constexpr (kBytes == 8) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(p) : "memory");
+    else asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[0]) : "r"(p) : "memory");
   }
   __device__ __forceinline__ void store(T* p) const {
     if constexpr (kBytes == 16) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
@@ -98,6 +99,9 @@ struct Chunk {
 // Where a lane's chunk pairs lie in a head: chunk j's first channels c0 and c1, its first table column, and what of it exists.
 template <int V, int NC, bool INTER>
 struct Geometry {
+  // Neighbouring pairs lie inside the chunks, half of them in each (a lane's two chunks are apart all the same: side by side, memory would be read in
+  // half sectors, 43 us instead of 31 for 16384 tokens of 20 heads of 128); of single values the pair is the two chunks.
+  static constexpr bool kInside = INTER && V > 1, kBeside = INTER && V == 1;
   int c0[NC], c1[NC], at[NC];
   bool has0[NC], has1[NC], turns[NC];
   __device__ __forceinline__ Geometry(int sub, const RopeArgs& a) {
@@ -106,8 +110,8 @@ struct Geometry {
     for (int j = 0; j < NC; ++j) {
       const int p = sub + j * a.lg;
       turns[j] = p < turning;
-      at[j] = p * V;
-      if (turns[j]) { c0[j] = INTER ? 2 * p * V : p * V; c1[j] = INTER ? c0[j] + V : c0[j] + a.rot / 2; }
+      at[j] = kInside ? p * V / 2 : p * V;
+      if (turns[j]) { c0[j] = kBeside ? 2 * p : p * V; c1[j] = kBeside ? c0[j] + 1 : c0[j] + a.rot / 2; }
       else { c0[j] = a.rot + (p - turning) * V; c1[j] = c0[j] + rest * V; }
       has0[j] = p < a.pairs && c0[j] < a.d;
       has1[j] = p < a.pairs && c1[j] < a.d;
@@ -145,8 +149,16 @@ struct Angles {
 #pragma unroll
       for (int i = 0; i < V; ++i) { cs[j][i] = 1.f; sn[j][i] = 0.f; }
       if (good && geo.turns[j] && geo.has0[j]) {
-        load_table<V>(a.cos + pos * a.cos_ld + geo.at[j], cs[j]);
-        load_table<V>(a.sin + pos * a.sin_ld + geo.at[j], sn[j]);
+        const float *c = a.cos + pos * a.cos_ld + geo.at[j], *s = a.sin + pos * a.sin_ld + geo.at[j];
+        if constexpr (Geometry<V, NC, INTER>::kInside) {
+          load_table<V / 2>(c, cs[j]);
+          load_table<V / 2>(s, sn[j]);
+          load_table<V / 2>(c + a.rot / 4, cs[j] + V / 2);
+          load_table<V / 2>(s + a.rot / 4, sn[j] + V / 2);
+        } else {
+          load_table<V>(c, cs[j]);
+          load_table<V>(s, sn[j]);
+        }
       }
     }
   }
@@ -155,36 +167,59 @@ struct Angles {
 template <int BYTES>
 __device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
   if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-  else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
 }
-// N tensors' chunk pairs of a step, kDepth - 1 steps ahead.  A lane reads back what it copied itself: no barrier.  A lane without a chunk reads the
-// zeros that it put there first; of a token beyond the last it reads anything, and nothing is made of it.  Values of fewer than 8 bytes (V == 1) are
-// loaded when they are needed.
+__device__ __forceinline__ float2 two(const float* f) { return make_float2(f[0], f[1]); }
+__device__ __forceinline__ void put(float* f, float2 v) { f[0] = v.x; f[1] = v.y; }
+// A lane's 2 V channels in registers: the pairs' first members, then their second ones, whichever way they lie in memory (neighbours where INTER).
+template <int V, bool INTER>
+__device__ __forceinline__ void to_pairs(float (&z)[2 * V]) {
+  if constexpr (INTER) {
+    float m[2 * V];
+#pragma unroll
+    for (int i = 0; i < 2 * V; ++i) m[i] = z[i];
+#pragma unroll
+    for (int i = 0; i < V; ++i) { z[i] = m[2 * i]; z[V + i] = m[2 * i + 1]; }
+  }
+}
+template <int V, bool INTER>
+__device__ __forceinline__ void from_pairs(float (&z)[2 * V]) {
+  if constexpr (INTER) {
+    float m[2 * V];
+#pragma unroll
+    for (int i = 0; i < 2 * V; ++i) m[i] = z[i];
+#pragma unroll
+    for (int i = 0; i < V; ++i) { z[2 * i] = m[i]; z[2 * i + 1] = m[V + i]; }
+  }
+}
+
+// N tensors' chunk pairs of a step, kDepth - 1 steps ahead: in shared memory where a lane has one pair of at least 4 bytes each.  A lane reads back what
+// it copied itself: no barrier.  A lane without a chunk reads the zeros that it put there first; of a token beyond the last it reads anything,
+// and nothing is made of it.  Else one step ahead, in registers.
 template <typename T, int V, int NC, int N>
 struct Feed {
-  static constexpr int kBytes = V * sizeof(T), kDepth = 4;
-  static constexpr bool kRing = kBytes >= 8;
-  static constexpr int kPart = 32 * kBytes, kSlot = N * 2 * kPart, kWarpBytes = kRing ? kDepth * kSlot : 0;
+  static constexpr int kBytes = V * sizeof(T);
+  static constexpr bool kRing = kBytes >= 4 && NC == 1;
+  static constexpr int kDepth = kRing ? 4 : 2, kPart = 32 * kBytes, kSlot = N * 2 * kPart, kWarpBytes = kRing ? kDepth * kSlot : 0;
   uint32_t base, at;      // of the lane's part of a warp's ring; the slot of the current step
+  Chunk<T, V> held[kRing ? 1 : N][kRing ? 1 : NC][2];
   __device__ __forceinline__ void start(unsigned char* ring, bool has) {
     if constexpr (kRing) {
       base = (uint32_t)__cvta_generic_to_shared(ring) + (threadIdx.x / 32) * kWarpBytes + (threadIdx.x & 31) * kBytes;
       at = 0;
       if (!has) {
 #pragma unroll
-        for (int i = 0; i < kDepth * N * 2; ++i) asm volatile("st.shared.v2.b32 [%0], {%1, %1};" ::"r"(base + i * kPart), "r"(0) : "memory");
-        if constexpr (kBytes == 16) {
+        for (int i = 0; i < kDepth * N * 2; ++i)
 #pragma unroll
-          for (int i = 0; i < kDepth * N * 2; ++i) asm volatile("st.shared.v2.b32 [%0], {%1, %1};" ::"r"(base + i * kPart + 8), "r"(0) : "memory");
-        }
+          for (int b = 0; b < kBytes; b += 4) asm volatile("st.shared.b32 [%0], %1;" ::"r"(base + i * kPart + b), "r"(0) : "memory");
       }
     }
   }
   // The step `ahead` behind the current one; kDepth - 1: into the slot of the one before it.
   template <bool INTER>
   __device__ __forceinline__ void fetch(const char* const (&p)[N], bool real, bool all, int ahead, const Geometry<V, NC, INTER>& geo) {
-    [[maybe_unused]] const int partner = (geo.c1[0] - geo.c0[0]) * (int)sizeof(T);
     if constexpr (kRing) {
+      const int partner = (geo.c1[0] - geo.c0[0]) * (int)sizeof(T);
       const uint32_t to = base + (at + ahead * kSlot) % kWarpBytes;
       if (real && geo.has0[0]) {
 #pragma unroll
@@ -195,46 +230,52 @@ struct Feed {
           }
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
+    } else {
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int j = 0; j < NC; ++j)
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            held[n][j][half].clear();
+            if (real && (n == 0 || all) && (half ? geo.has1[j] : geo.has0[j])) held[n][j][half].load(reinterpret_cast<const T*>(p[n]) + (half ? geo.c1[j] : geo.c0[j]) - geo.c0[0]);
+          }
     }
   }
   __device__ __forceinline__ void wait() {
     if constexpr (kRing) asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 2) : "memory");
   }
   template <bool INTER>
-  __device__ __forceinline__ void get(float (&z)[NC][2 * V], int n, const char* p, bool real, const Geometry<V, NC, INTER>& geo) {
+  __device__ __forceinline__ void get(float (&z)[NC][2 * V], int n, std::bool_constant<INTER>) {
 #pragma unroll
-    for (int j = 0; j < NC; ++j)
+    for (int j = 0; j < NC; ++j) {
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        Chunk<T, V> c;
         if constexpr (kRing) {
+          Chunk<T, V> c;
           c.from_shared(base + at + (2 * n + half) * kPart);
+          c.get(z[j] + half * V);
         } else {
-          c.clear();
-          if (real && (half ? geo.has1[j] : geo.has0[j])) c.load(reinterpret_cast<const T*>(p) + (half ? geo.c1[j] : geo.c0[j]) - geo.c0[0]);
+          held[n][j][half].get(z[j] + half * V);
         }
-        c.get(z[j] + half * V);
       }
+      to_pairs<V, INTER>(z[j]);
+    }
   }
   __device__ __forceinline__ void next() {
     if constexpr (kRing) at = (at + kSlot) % kWarpBytes;
   }
 };
 
-__device__ __forceinline__ float2 two(const float* f) { return make_float2(f[0], f[1]); }
-__device__ __forceinline__ void put(float* f, float2 v) { f[0] = v.x; f[1] = v.y; }
 // The pairs of a chunk and its partner, turned: turn is 1, or -1 for the transposed rotation.  Products and sums are rounded one by one, and every form
 // of the rotation that computes in fp32 without contraction agrees with this one to the bit.  (A sum is written as a product with +-1, which is
 // exact, because the compiler contracts a packed product and a packed sum into one operation; the factor is one that it does not know.)
-template <int V, bool INTER>
+template <int V>
 __device__ __forceinline__ void rotate(float (&z)[2 * V], const float (&cs)[V], const float (&sn)[V], float turn) {
-  if constexpr (INTER || V == 1) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float a = z[INTER ? 2 * i : i], b = z[INTER ? 2 * i + 1 : V + i];
-      z[INTER ? 2 * i : i] = fmaf(__fmul_rn(b, sn[i]), -turn, __fmul_rn(a, cs[i]));
-      z[INTER ? 2 * i + 1 : V + i] = fmaf(__fmul_rn(a, sn[i]), turn, __fmul_rn(b, cs[i]));
-    }
+  if constexpr (V == 1) {
+    const float a = z[0], b = z[1];
+    z[0] = fmaf(__fmul_rn(b, sn[0]), -turn, __fmul_rn(a, cs[0]));
+    z[1] = fmaf(__fmul_rn(a, sn[0]), turn, __fmul_rn(b, cs[0]));
   } else {
 #pragma unroll
     for (int i = 0; i < V; i += 2) {
@@ -255,9 +296,10 @@ __device__ __forceinline__ void head_sums(float (&v)[N], int lg) {
   }
 }
 template <typename T, int V, int NC, bool INTER>
-__device__ __forceinline__ void store_head(const float (&z)[NC][2 * V], T* p, bool real, const Geometry<V, NC, INTER>& geo) {
+__device__ __forceinline__ void store_head(float (&z)[NC][2 * V], T* p, bool real, const Geometry<V, NC, INTER>& geo) {
 #pragma unroll
   for (int j = 0; j < NC; ++j) {
+    from_pairs<V, INTER>(z[j]);
     Chunk<T, V> c;
     c.set(z[j]);
     if (real && geo.has0[j]) c.store(p + geo.c0[j] - geo.c0[0]);
@@ -268,12 +310,14 @@ __device__ __forceinline__ void store_head(const float (&z)[NC][2 * V], T* p, bo
 template <int V, int NC, bool INTER>
 __device__ __forceinline__ void load_weights(const float* w, const Geometry<V, NC, INTER>& geo, float (&f)[NC][2 * V]) {
 #pragma unroll
-  for (int j = 0; j < NC; ++j)
+  for (int j = 0; j < NC; ++j) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       f[j][i] = geo.has0[j] ? __ldg(w + geo.c0[j] + i) : 0.f;
       f[j][V + i] = geo.has1[j] ? __ldg(w + geo.c1[j] + i) : 0.f;
     }
+    to_pairs<V, INTER>(f[j]);
+  }
 }
 template <int V, int NC>
 __device__ __forceinline__ void poison(float (&z)[NC][2 * V]) {
@@ -331,12 +375,10 @@ __global__ void __launch_bounds__(kThreads, GRAD ? kBackwardCtas : kForwardCtas)
   if (ahead_side == 1 && part >= a.side[1].batches) ahead_side = 2;
   seek(a.side[ahead_side & 1]);
   feed.start(ring, geo.has0[0]);
-  if constexpr (Ring::kRing) {
 #pragma unroll
-    for (int i = 0; i < Ring::kDepth - 1; ++i) {
-      fetch(i);
-      advance();
-    }
+  for (int i = 0; i < Ring::kDepth - 1; ++i) {
+    fetch(i);
+    advance();
   }
 #pragma unroll 1
   for (int side = 0; side < 2; ++side) {
@@ -369,9 +411,9 @@ __global__ void __launch_bounds__(kThreads, GRAD ? kBackwardCtas : kForwardCtas)
       for (int b = part; b < s.batches; b += a.split, out += s.y.step) {
         feed.wait();
         float z[NC][2 * V], v[NC][2 * V];
-        feed.get(z, 0, in[0], real, geo);
-        if constexpr (GRAD) feed.get(v, 1, in[N - 1], real && norm, geo);
-        if constexpr (Ring::kRing) fetch(Ring::kDepth - 1);
+        feed.get(z, 0, std::bool_constant<INTER>{});
+        if constexpr (GRAD) feed.get(v, 1, std::bool_constant<INTER>{});
+        fetch(Ring::kDepth - 1);
         advance();
         feed.next();
         if constexpr (!GRAD) {
@@ -392,7 +434,7 @@ __global__ void __launch_bounds__(kThreads, GRAD ? kBackwardCtas : kForwardCtas)
         }
 #pragma unroll
         for (int j = 0; j < NC; ++j)
-          if (geo.turns[j]) rotate<V, INTER>(z[j], turn.cs[j], turn.sn[j], a.turn);
+          if (geo.turns[j]) rotate<V>(z[j], turn.cs[j], turn.sn[j], a.turn);
         if (!turn.good) poison<V, NC>(z);
         if constexpr (GRAD) {
           if (norm) {
@@ -426,6 +468,8 @@ __global__ void __launch_bounds__(kThreads, GRAD ? kBackwardCtas : kForwardCtas)
     }
     if constexpr (GRAD) {
       if (norm) {
+#pragma unroll
+        for (int j = 0; j < NC; ++j) from_pairs<V, INTER>(dw[j]);
 #pragma unroll
         for (int j = 0; j < NC; ++j)
 #pragma unroll
@@ -599,9 +643,10 @@ int run_rope(const fgd_qk_rope_args* b, bool backward, int device, void* stream)
       for (int j = 0; j < n_mats; ++j)
         if (tensors[i].span.overlaps(span_of(mats[j].p, mats[j].rows, mats[j].width, mats[j].ld, 4))) return op_fail(FGD_ERR_ALIAS, "%s: %s overlaps %s", who, tensors[i].name, mats[j].name);
     }
-    // Chunks of 16 bytes; of 8 where a half of the rotated channels is no multiple of that (16-bit heads of 72); else one by one.
-    for (; vec > 1; vec = vec == 8 ? 4 : 1) {
-      bool fits = chunked(vec) && vector_of(b->cos.p, b->cos.ld, 0, 4, 4) && vector_of(b->sin.p, b->sin.ld, 0, 4, 4);
+    // Chunks of 16 bytes; of 8 or 4 where a half of the rotated channels, or of the others, is no multiple of that (16-bit heads of 72, of 100); else
+    // one by one.
+    for (; vec > 1; vec = bytes == 2 ? vec / 2 : 1) {
+      bool fits = chunked(vec) && (vec == 2 ? d <= 128 : vector_of(b->cos.p, b->cos.ld, 0, 4, 4) && vector_of(b->sin.p, b->sin.ld, 0, 4, 4));
       for (int i = 0; i < n_tensors && fits; ++i) fits = vector_of(tensors[i].t->p, tensors[i].t->token_stride, tensors[i].t->head_stride, bytes, vec);
       if (fits) break;
     }
@@ -674,10 +719,12 @@ int run_rope(const fgd_qk_rope_args* b, bool backward, int device, void* stream)
     const bool inter = b->interleaved != 0;
     auto by_vec = [&](auto zero) {
       using E = decltype(zero);
-      if constexpr (sizeof(E) == 2)
+      if constexpr (sizeof(E) == 2) {
         if (l.vec == 8) return launch<E, 8, 1>(a, b->workers, c.ctas, sums, inter, st);
+        if (l.vec == 2) return launch<E, 2, 1>(a, b->workers, c.ctas, sums, inter, st);
+      }
       if (l.vec == 4) return launch<E, 4, 1>(a, b->workers, c.ctas, sums, inter, st);
-      return launch<E, 1, 4>(a, b->workers, c.ctas, sums, inter, st);
+      return l.pairs <= 64 ? launch<E, 1, 2>(a, b->workers, c.ctas, sums, inter, st) : launch<E, 1, 4>(a, b->workers, c.ctas, sums, inter, st);
     };
     switch (b->dtype) {
       case FGD_F32: e = by_vec(float{}); break;
