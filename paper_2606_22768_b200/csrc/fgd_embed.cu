@@ -575,7 +575,7 @@ __global__ void __launch_bounds__(kThreads) embed_few_kernel(const FewArgs a) {
 
 // ---- host
 int check_common(const char* who, int dtype, int workers, int64_t rows, int64_t vocab, int64_t width, const void* tokens, int token_bytes, int64_t ld_tokens,
-                 const float* table, int64_t worker_stride, int64_t row_stride, double scale, const void* x, int64_t ld_x) {
+                 const float* table, int64_t worker_stride, int64_t row_stride, bool output, double scale, const void* x, int64_t ld_x) {
   const int b = dtype_bytes(dtype);
   if (b == 0) return op_fail(FGD_ERR_INVALID_ARG, "%s: unknown dtype %d", who, dtype);
   if (workers < 1 || workers > FGD_MAX_K || rows < 0 || rows > 0x7fffffff - 65536 || vocab < 1 || vocab > kMaxVocab || width < 1)
@@ -585,8 +585,8 @@ int check_common(const char* who, int dtype, int workers, int64_t rows, int64_t 
   if (!std::isfinite(scale)) return op_fail(FGD_ERR_INVALID_ARG, "%s: scale is not finite", who);
   if (!table || (rows > 0 && (!tokens || !x))) return op_fail(FGD_ERR_INVALID_ARG, "%s: NULL pointer", who);
   if (rows > 0 && (ld_tokens < rows || ld_x < width)) return op_fail(FGD_ERR_INVALID_ARG, "%s: a row stride is below the row's width", who);
-  if (row_stride < width || (workers > 1 && worker_stride < (vocab - 1) * row_stride + width))
-    return op_fail(FGD_ERR_INVALID_ARG, "%s: rows of the table overlap one another", who);
+  if (row_stride < width || worker_stride < 0) return op_fail(FGD_ERR_INVALID_ARG, "%s: a stride of the table is below its row's width, or negative", who);
+  if (output && workers > 1 && worker_stride < (vocab - 1) * row_stride + width) return op_fail(FGD_ERR_INVALID_ARG, "%s: the workers' tables overlap one another", who);
   if (reinterpret_cast<uintptr_t>(tokens) % token_bytes != 0 || reinterpret_cast<uintptr_t>(table) % 4 != 0 || reinterpret_cast<uintptr_t>(x) % b != 0)
     return op_fail(FGD_ERR_INVALID_ARG, "%s: a pointer is not on a boundary of its elements", who);
   return FGD_OK;
@@ -645,7 +645,7 @@ cudaError_t backward(const RowsArgs& r, cudaStream_t st) {
   for (a.zero_lanes = 1; a.zero_lanes < 32 && a.zero_lanes * (ANY ? 1 : 4) < a.width;) a.zero_lanes *= 2;
   const int64_t zeros = (int64_t)a.workers * ((a.words + a.cta_words - 1) / a.cta_words);
   cudaError_t e = launch_early(embed_rows_kernel<T, ANY>, dim3((unsigned)(a.sum_ctas + zeros)), kThreads, 0, st, a);
-  if (e == cudaSuccess) {
+  if (e == cudaSuccess && a.chunks > 0) {
     const int64_t columns = (a.width + 127) / 128, most = ((int64_t)a.workers * a.chunks + kWarps - 1) / kWarps, want = (int64_t)sm_count() * 4 / columns + 1;
     e = launch_early(embed_joins_kernel, dim3((unsigned)(want < most ? want : most), (unsigned)columns), kThreads, 0, st, a);
   }
@@ -660,11 +660,38 @@ cudaError_t few(const FewArgs& f, int workers, cudaStream_t st) {
   embed_few_kernel<T, ANY><<<dim3((unsigned)ctas, workers, (unsigned)(want < a.slabs ? want : a.slabs)), kThreads, 0, st>>>(a);
   return cudaGetLastError();
 }
-cudaError_t sort(const SortArgs& a, cudaStream_t st) {
-  const size_t smem = ((size_t)8 << a.bits) + ((size_t)kSortWarps * 2 << a.bits);
-  cudaError_t e = allow_smem<embed_sort_kernel>(((size_t)8 << kMaxBits) + ((size_t)kSortWarps * 2 << kMaxBits));
+// CTAs of a cluster that sorts many tokens: sixteen where the device can place so many (65536 tokens 25 us, eight 35), which CUDA does not promise.
+cudaError_t cluster_size(int* size, size_t smem) {
+  static int cached[64] = {};
+  int dev = 0, active = 0;
+  cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  if (a.cluster > 8 && (e = cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)) != cudaSuccess) return e;
+  if (dev < 64 && cached[dev]) { *size = cached[dev]; return cudaSuccess; }
+  *size = kCluster / 2;
+  if (cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess) {
+    cudaLaunchAttribute attr = {};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = kCluster;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t c = {};
+    c.gridDim = dim3(kCluster);
+    c.blockDim = dim3(kSortThreads);
+    c.dynamicSmemBytes = smem;
+    c.attrs = &attr;
+    c.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&active, embed_sort_kernel, &c) == cudaSuccess && active > 0) *size = kCluster;
+  }
+  (void)cudaGetLastError();      // (a refusal is an answer)
+  if (dev < 64) cached[dev] = *size;
+  return cudaSuccess;
+}
+cudaError_t sort(SortArgs& a, cudaStream_t st) {
+  const size_t smem = ((size_t)8 << a.bits) + ((size_t)kSortWarps * 2 << a.bits);
+  const size_t most = ((size_t)8 << kMaxBits) + ((size_t)kSortWarps * 2 << kMaxBits);
+  cudaError_t e = allow_smem<embed_sort_kernel>(most);
+  a.cluster = 1;
+  if (e == cudaSuccess && a.rows > kSortFew) e = cluster_size(&a.cluster, most);
+  if (e != cudaSuccess) return e;
   cudaLaunchAttribute attr = {};
   attr.id = cudaLaunchAttributeClusterDimension;
   attr.val.clusterDim.x = a.cluster;
@@ -701,7 +728,7 @@ extern "C" int fgd_embed_forward(int device, int dtype, int workers, int64_t row
                                  void* stream) {
   FGD_NVTX_RANGE("fgd_embed_forward");
   const char* who = "fgd_embed_forward";
-  if (int rc = check_common(who, dtype, workers, rows, vocab, width, tokens, token_bytes, ld_tokens, table, worker_stride, row_stride, scale, out, ld_out)) return rc;
+  if (int rc = check_common(who, dtype, workers, rows, vocab, width, tokens, token_bytes, ld_tokens, table, worker_stride, row_stride, false, scale, out, ld_out)) return rc;
   if (rows == 0) return FGD_OK;
   const int b = dtype_bytes(dtype);
   const Span so = span_of(out, workers * rows, width, ld_out, b);
@@ -724,7 +751,7 @@ extern "C" int fgd_embed_backward(int device, int dtype, int workers, int64_t ro
                                   void* workspace, int64_t workspace_bytes, void* stream) {
   FGD_NVTX_RANGE("fgd_embed_backward");
   const char* who = "fgd_embed_backward";
-  if (int rc = check_common(who, dtype, workers, rows, vocab, width, tokens, token_bytes, ld_tokens, dtable, worker_stride, row_stride, scale, dout, ld_dout)) return rc;
+  if (int rc = check_common(who, dtype, workers, rows, vocab, width, tokens, token_bytes, ld_tokens, dtable, worker_stride, row_stride, true, scale, dout, ld_dout)) return rc;
   const int b = dtype_bytes(dtype);
   const Layout l = layout_of(workers, rows, vocab, width);
   if (l.total > 0 && (!workspace || workspace_bytes < l.total || reinterpret_cast<uintptr_t>(workspace) % 16 != 0))
@@ -751,7 +778,6 @@ extern "C" int fgd_embed_backward(int device, int dtype, int workers, int64_t ro
   SortArgs s = {};
   s.tokens = Tokens{tokens, token_bytes, ld_tokens};
   s.vocab = vocab; s.rows = (int)rows;
-  s.cluster = rows <= kSortFew ? 1 : kCluster;
   int bits = 1;
   while ((int64_t)1 << bits <= vocab) ++bits;      // keys 0 .. vocab
   s.passes = (bits + kMaxBits - 1) / kMaxBits;

@@ -576,6 +576,7 @@ int run_rope(const fgd_qk_rope_args* b, bool backward, int device, void* stream)
   const int64_t T = b->workers * b->rows;
   const bool use[2] = {true, b->n_k_heads > 0};
   const bool norm[2] = {b->w_q.p != nullptr, use[1] && b->w_k.p != nullptr}, any_norm = norm[0] || norm[1];
+  if (!use[1] && b->w_k.p) return op_fail(FGD_ERR_INVALID_ARG, "%s: w_k without keys", who);
   if (b->table_rows < 0) return op_fail(FGD_ERR_INVALID_ARG, "%s: table_rows %lld", who, (long long)b->table_rows);
   const bool has_positions = b->position_bytes != 0;
   if (has_positions && !b->positions && T > 0) return op_fail(FGD_ERR_INVALID_ARG, "%s: positions is NULL", who);

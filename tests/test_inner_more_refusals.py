@@ -36,7 +36,7 @@ def _rope(backward, **change):
     (INVALID, dict(hk=-1)), (INVALID, dict(d=0)), (UNSUPPORTED, dict(d=257)), (INVALID, dict(rot=0)), (INVALID, dict(rot=63)), (INVALID, dict(rot=66)),
     (INVALID, dict(position_bytes=2)), (INVALID, dict(positions=0)), (INVALID, dict(positions=_at(2) + 4)), (INVALID, dict(position_bytes=0, table_rows=19)),
     (INVALID, dict(table_rows=-1)), (INVALID, dict(eps=-1e-9)), (INVALID, dict(eps=float("nan"))), (INVALID, dict(eps=float("inf"))), (INVALID, dict(cos=(0, 32))),
-    (INVALID, dict(sin=(_at(1), 31))), (INVALID, dict(cos=(_at(0) + 2, 32))), (INVALID, dict(w_q=(_at(3), 63))), (INVALID, dict(w_k=(_at(4) + 1, 64))),
+    (INVALID, dict(sin=(_at(1), 31))), (INVALID, dict(cos=(_at(0) + 2, 32))), (INVALID, dict(w_q=(_at(3), 63))), (INVALID, dict(w_k=(_at(4) + 1, 64))), (INVALID, dict(hk=0)),
 ])
 def test_rope_refuses(backward, status, change):
     assert _rope(backward, **change) == status
@@ -87,7 +87,7 @@ def _embed(backward, **change):
     (INVALID, dict(dtype=-1)), (INVALID, dict(workers=0)), (INVALID, dict(workers=65)), (INVALID, dict(rows=-1)), (INVALID, dict(rows=1 << 31)), (INVALID, dict(vocab=0)),
     (INVALID, dict(vocab=(1 << 30) + 1)), (INVALID, dict(width=0)), (UNSUPPORTED, dict(width=65537)), (INVALID, dict(token_bytes=2)), (INVALID, dict(scale=float("inf"))),
     (INVALID, dict(table=0)), (INVALID, dict(tokens=0)), (INVALID, dict(x=0)), (INVALID, dict(ld_tokens=9)), (INVALID, dict(ld_x=63)), (INVALID, dict(row_stride=63)),
-    (INVALID, dict(worker_stride=3199)), (INVALID, dict(tokens=_at(0) + 4)), (INVALID, dict(table=_at(1) + 2)), (INVALID, dict(x=_at(2) + 1)),
+    (INVALID, dict(worker_stride=-64)), (INVALID, dict(tokens=_at(0) + 4)), (INVALID, dict(table=_at(1) + 2)), (INVALID, dict(x=_at(2) + 1)),
     (ALIAS, dict(x=_at(1) + 256)), (ALIAS, dict(x=_at(1) - 256)),
 ])
 def test_embed_refuses(backward, status, change):
@@ -95,7 +95,7 @@ def test_embed_refuses(backward, status, change):
 
 
 @pytest.mark.parametrize("backward,status,change", [
-    (False, ALIAS, dict(x=_at(0))), (True, ALIAS, dict(table=_at(0))), (True, ALIAS, dict(table=_at(3) + 16)), (True, ALIAS, dict(x=_at(3))), (True, INVALID, dict(workspace=0)),
+    (False, ALIAS, dict(x=_at(0))), (True, INVALID, dict(worker_stride=3199)), (True, INVALID, dict(worker_stride=0)), (True, ALIAS, dict(table=_at(0))), (True, ALIAS, dict(table=_at(3) + 16)), (True, ALIAS, dict(x=_at(3))), (True, INVALID, dict(workspace=0)),
     (True, INVALID, dict(workspace=_at(3) + 8)), (True, INVALID, dict(workspace_bytes=100)), (True, ALIAS, dict(workspace=_at(0))),
 ])
 def test_embed_refuses_more(backward, status, change):
