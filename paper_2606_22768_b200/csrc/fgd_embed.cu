@@ -11,6 +11,8 @@
 //   joins  the pieces of the runs that cross chunks, which are few, eight warps to a run.
 // A few tokens need no sort: a warp looks through all of them for the one that its row of the table stands for, in one launch.
 // The order of every sum depends on the tokens alone.
+// 4 x 8192 tokens of 32000 rows, 2048 wide, bf16: 189 us, 94 % of the copy peak (sort 14, rows and zeros 168, joins 6); 65536 tokens of 50257, 1536 wide, f16:
+// 127 us (25, 84, 14).
 #include <cooperative_groups.h>
 
 #include <cmath>
@@ -602,7 +604,8 @@ bool aligned(const float* table, int64_t worker_stride, int64_t row_stride, int 
 
 int64_t round16(int64_t n) { return (n + 15) / 16 * 16; }
 // Few tokens and little of a table: every warp looks through all tokens for its row.  4 x 384 tokens of 256, 256 wide, bf16: 6.2 us, sorted 20; but
-// 4 x 203 of 1195, 2242 wide, 129 us (one warp adds up all columns of a common token) and 512 of 32000, 2048 wide, 106 us (the looking), sorted 55.
+// 4 x 203 of 1195, 2240 wide, 42 us (one warp adds up all columns of a common token), sorted 26, and 2 x 419 of 94350, 264 wide, fp32, 154 us (the looking),
+// sorted 47.
 bool no_sort(int64_t workers, int64_t rows, int64_t vocab, int64_t width) { return rows <= kNoSort && workers * vocab * ((width + 255) / 256) <= 16384; }
 struct Layout { int64_t pairs, other, present, joins, list, pieces, total; int chunk, chunks, words; };
 Layout layout_of(int64_t workers, int64_t rows, int64_t vocab, int64_t width) {
