@@ -27,8 +27,7 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
-constexpr int kCluster = 16;          // CTAs that sort one worker's tokens
-constexpr int kSortFew = 4096;        // up to so many a single one does
+constexpr int kCluster = 16;          // CTAs that sort one worker's tokens, at most
 constexpr int kItems = 8;             // keys of a thread in one tile
 constexpr int kMaxBits = 10;          // of a radix pass
 constexpr int kChunk = 64, kShortChunk = 16;      // sorted tokens that a warp adds up
@@ -663,7 +662,7 @@ cudaError_t few(const FewArgs& f, int workers, cudaStream_t st) {
   embed_few_kernel<T, ANY><<<dim3((unsigned)ctas, workers, (unsigned)(want < a.slabs ? want : a.slabs)), kThreads, 0, st>>>(a);
   return cudaGetLastError();
 }
-// CTAs of a cluster that sorts many tokens: sixteen where the device can place so many (65536 tokens 25 us, eight 35), which CUDA does not promise.
+// CTAs of a cluster that sorts many tokens: sixteen where the device can place so many (of 65536 tokens 25 us, eight 35), which CUDA does not promise.
 cudaError_t cluster_size(int* size, size_t smem) {
   static int cached[64] = {};
   int dev = 0, active = 0;
@@ -692,8 +691,9 @@ cudaError_t sort(SortArgs& a, cudaStream_t st) {
   const size_t smem = ((size_t)8 << a.bits) + ((size_t)kSortWarps * 2 << a.bits);
   const size_t most = ((size_t)8 << kMaxBits) + ((size_t)kSortWarps * 2 << kMaxBits);
   cudaError_t e = allow_smem<embed_sort_kernel>(most);
-  a.cluster = 1;
-  if (e == cudaSuccess && a.rows > kSortFew) e = cluster_size(&a.cluster, most);
+  // 3000 tokens of 20000: one CTA 18.2 us, four 10.8, eight 11.6, sixteen 14.1; 8000: four 14.4, eight 12.6, sixteen 14.3; 30000: 31, 21, 18.
+  a.cluster = a.rows <= 4096 ? 4 : 8;
+  if (e == cudaSuccess && a.rows > 16384) e = cluster_size(&a.cluster, most);
   if (e != cudaSuccess) return e;
   cudaLaunchAttribute attr = {};
   attr.id = cudaLaunchAttributeClusterDimension;

@@ -283,7 +283,7 @@ def _text(K, rows, V, seed=0):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("K,rows,V,W", [(1, 1, 1, 1), (1, 1, 5, 8), (2, 63, 7, 64), (1, 64, 64, 40), (3, 65, 33, 136), (1, 129, 1000, 257), (8, 17, 300, 256), (1, 33, 257, 1001),
-                                        (2, 500, 1023, 24), (2, 512, 40, 520), (2, 513, 1023, 24), (2, 600, 1024, 24), (3, 1024, 11, 300), (1, 1500, 3000, 2048), (1, 4096, 100, 16), (1, 4097, 2000, 48), (2, 9000, 5000, 32), (1, 70000, 300, 8), (1, 140000, 70000, 8)])
+                                        (2, 500, 1023, 24), (2, 512, 40, 520), (2, 513, 1023, 24), (2, 600, 1024, 24), (3, 1024, 11, 300), (1, 1500, 3000, 2048), (1, 4096, 100, 16), (1, 4097, 2000, 48), (2, 9000, 5000, 32), (1, 16384, 900, 8), (1, 16385, 900, 8), (1, 70000, 300, 8), (1, 140000, 70000, 8)])
 def test_embed(K, rows, V, W, dtype):
     _embed_case(_text(K, rows, V), V, W, dtype)
 
@@ -492,7 +492,7 @@ def test_dropout_counter_in_a_graph():
 
 
 # ------------------------------------------------------------------------------- streams and graphs
-@pytest.mark.parametrize("rows", [900, 5000])
+@pytest.mark.parametrize("rows", [900, 5000, 17000])
 @pytest.mark.parametrize("given", [False, True])
 def test_on_streams_and_in_graphs(given, rows):
     """All three, forward and backward, on another stream and captured twice, with workspaces of the caller and without."""
