@@ -424,8 +424,9 @@ typedef struct {
   void* workspace;              /* backward with weights: device scratch */
   int64_t workspace_bytes;
 } fgd_qk_rope_args;
-/* head_dim <= 256, workers <= FGD_MAX_K, rotary_dim even.  Full speed: 16-byte aligned heads, rotary_dim / 2 and the rest's half multiples of
- * 16 bytes, tables on 16-byte boundaries; everything else goes channel by channel (16-bit heads of which a half is 8 bytes' multiple, in between). */
+/* head_dim <= 256, workers <= FGD_MAX_K, rotary_dim even.  Full speed: heads on 16-byte boundaries, rotary_dim / 2 and half of the other channels
+ * multiples of 16 bytes, tables on 16-byte boundaries.  16-bit heads of which these are multiples of 8 or (to 128 channels) 4 bytes take 1.5 to 4 times
+ * as long per byte, everything else, channel by channel, 6 to 8 times.  A workspace, here and below, belongs to one call at a time. */
 int fgd_qk_rope_forward(int device, const fgd_qk_rope_args* args, void* stream);
 int fgd_qk_rope_backward(int device, const fgd_qk_rope_args* args, void* stream);
 /* Bytes of scratch fgd_qk_rope_backward needs where there are weights (>= 0), or a negative status. */

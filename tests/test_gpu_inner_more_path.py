@@ -241,3 +241,14 @@ def test_inner_steps_with_everything():
         assert all(bool(x.isfinite().all()) for x in losses)
         runs.append(steps.theta)
     assert torch.equal(runs[0], runs[1]) and not torch.equal(runs[0], runs[2])
+
+
+def test_example_runs_with_norms_and_dropout():
+    import importlib.util
+    import os
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    spec = importlib.util.spec_from_file_location("inner_and_outer", os.path.join(root, "examples", "inner_and_outer.py"))
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    history = ex.main(["--rounds", "2", "--inner", "2", "--workers", "2", "--qk-norm", "--dropout", "0.1"])
+    assert len(history) == 2 and all(np.isfinite(v) for row in history for v in row)
