@@ -762,6 +762,51 @@ def _rope_pack(q, cos, sin, positions, w_q, w_k, eps, interleaved, shapes, heads
                            *_mat(dw[0], "dw_q", f32, K, d, dev), *_mat(dw[1], "dw_k", f32, K, d, dev), *workspace)
 
 
+_NO_ROPE_GRADS, _NO_ROPE_OUTPUTS = (0,) * 18, (0,) * 6
+
+
+def _rope_usual(q, k, q_to, k_to, w_q, w_k, cos, sin, positions, eps, interleaved, x_q=None, x_k=None, dw_q=None, dw_k=None):
+    """The arguments of a call as they usually are, checked; None where anything is not as usual: then the checks one by one say what is wrong, if it is.
+    (Small calls are bound by what the host does: written out, this takes about 6 us of it where the checks one by one take 9.)  q, k go in and q_to, k_to come out,
+    gradients in a backward pass; x_q, x_k and dw_q, dw_k are then its q, k and the gradients of the weights."""
+    import torch
+    if k is None or positions is None or (w_q is None) is not (w_k is None):
+        return None
+    f32, dt, dev, qs, ks, table, pt, code = torch.float32, q.dtype, q.device, q.shape, k.shape, cos.shape, positions.dtype, _types.codes.get(q.dtype)
+    if len(qs) != 3 or len(ks) != 3 or len(table) != 2 or code is None or dev.type != "cuda":
+        return None
+    (T, hq, d), hk, (rows, half) = qs, ks[1], table
+    if (ks[0] != T or ks[2] != d or k.dtype is not dt or q_to.dtype is not dt or k_to.dtype is not dt or q_to.shape != qs or k_to.shape != ks or k.device != dev
+            or q_to.device != dev or k_to.device != dev or cos.dtype is not f32 or sin.dtype is not f32 or sin.shape != table or cos.device != dev or sin.device != dev
+            or positions.shape != (T,) or positions.device != dev or (pt is not torch.int64 and pt is not torch.int32)):
+        return None
+    (q0, q1, q2), (k0, k1, k2), (y0, y1, y2), (z0, z1, z2) = q.stride(), k.stride(), q_to.stride(), k_to.stride()
+    (c0, c1), (s0, s1), (p0,) = cos.stride(), sin.stride(), positions.stride()
+    if not (q2 == k2 == y2 == z2 == c1 == s1 == p0 == 1 and c0 >= half and s0 >= half):
+        return None
+    K, weights, inputs, grads = 1, (0, 0, 0, 0), (0, 0, 0, 0, 0, 0), (0, 0, 0, 0)
+    if w_q is not None:
+        ws = w_q.shape
+        K = ws[0]
+        if K < 1 or T % K or ws != (K, d) or w_k.shape != ws or w_q.dtype is not f32 or w_k.dtype is not f32 or w_q.device != dev or w_k.device != dev:
+            return None
+        (g0, g1), (h0, h1) = w_q.stride(), w_k.stride()
+        if not (g1 == h1 == 1 and g0 >= d and h0 >= d):
+            return None
+        weights = w_q.data_ptr(), g0, w_k.data_ptr(), h0
+        if dw_q is not None:
+            if (x_q.dtype is not dt or x_k.dtype is not dt or x_q.shape != qs or x_k.shape != ks or x_q.device != dev or x_k.device != dev or dw_q.dtype is not f32
+                    or dw_k.dtype is not f32 or dw_q.shape != ws or dw_k.shape != ws or dw_q.device != dev or dw_k.device != dev):
+                return None
+            (a0, a1, a2), (b0, b1, b2), (g0, g1), (h0, h1) = x_q.stride(), x_k.stride(), dw_q.stride(), dw_k.stride()
+            if not (a2 == b2 == g1 == h1 == 1 and g0 >= d and h0 >= d):
+                return None
+            inputs, grads = (x_q.data_ptr(), a0, a1, x_k.data_ptr(), b0, b1), (dw_q.data_ptr(), g0, dw_k.data_ptr(), h0)
+    head = (code, K, T // K, hq, hk, d, 2 * half, int(interleaved), 8 if pt is torch.int64 else 4, rows, eps, cos.data_ptr(), c0, sin.data_ptr(), s0,
+            positions.data_ptr(), *weights)
+    return dev, K, d, head, inputs, (q.data_ptr(), q0, q1, k.data_ptr(), k0, k1), (q_to.data_ptr(), y0, y1, k_to.data_ptr(), z0, z1), grads
+
+
 def _key_heads(t, name: str, dtype, shape, device):
     if shape[1] == 0 and t is None:
         return _NO_HEADS
@@ -772,6 +817,11 @@ def fgd_qk_rope_forward(q, k, w_q, w_k, cos, sin, positions, q_out, k_out, eps: 
     """Queries [T, Hq, d] and keys [T, Hk, d] (None: no keys) normalised per head with w_q, w_k ([K, d] fp32 for K workers with T / K tokens each; None: not
     normalised) and rotated by rows ``positions`` ([T] int64 or int32; None: row t) of the tables cos and sin ([N, r / 2] fp32; the first r channels turn).
     Any token and head strides; q_out may be q, k_out k.  See ``include/fgd.h``."""
+    usual = _rope_usual(q, k, q_out, k_out, w_q, w_k, cos, sin, positions, eps, interleaved)
+    if usual is not None:
+        dev, _, _, head, _, source, target, _ = usual
+        _op_check(_lib.fgd_qk_rope_forward(dev.index, _ROPE_ARGS.pack(*head, *source, *target, *_NO_ROPE_GRADS), _stream_on(stream, dev)))
+        return
     shapes = dev, qs, ks, _, _ = _rope_shapes(q, k, w_q, w_k, cos)
     dt = q.dtype
     heads = (*_heads(q, "q", dt, qs, dev), *_key_heads(k, "k", dt, ks, dev), *_heads(q_out, "q_out", dt, qs, dev), *_key_heads(k_out, "k_out", dt, ks, dev),
@@ -792,6 +842,17 @@ def fgd_qk_rope_backward(dq_out, dk_out, q, k, w_q, w_k, cos, sin, positions, dq
                          workspace=None, stream=None) -> None:
     """Gradients of :func:`fgd_qk_rope_forward` from its inputs (q and k may be None where neither is normalised); dq may be dq_out, dk dk_out.
     ``workspace``: a uint8 CUDA tensor of :func:`fgd_qk_rope_workspace` bytes (None: allocated here)."""
+    usual = None
+    if w_q is not None and q is not None and k is not None and dw_q is not None and dw_k is not None:
+        usual = _rope_usual(dq_out, dk_out, dq, dk, w_q, w_k, cos, sin, positions, eps, interleaved, q, k, dw_q, dw_k)
+    if usual is not None:
+        dev, K, d, head, inputs, source, target, grads = usual
+        handle = _stream_on(stream, dev)
+        if workspace is None:
+            workspace = _scratch(fgd_qk_rope_workspace(K, d, dev.index), stream, handle, dev)
+        args = _ROPE_ARGS.pack(*head, *inputs, *_NO_ROPE_OUTPUTS, *source, *target, *grads, _dev_ptr(workspace, "workspace", "torch.uint8"), workspace.numel())
+        _op_check(_lib.fgd_qk_rope_backward(dev.index, args, handle))
+        return
     shapes = dev, qs, ks, K, _ = _rope_shapes(dq_out, dk_out, w_q, w_k, cos)
     dt = dq_out.dtype
     heads = (*(_NO_HEADS if w_q is None else _heads(q, "q", dt, qs, dev)), *(_NO_HEADS if w_k is None else _key_heads(k, "k", dt, ks, dev)), *_NO_HEADS, *_NO_HEADS,
@@ -823,9 +884,28 @@ def _embed_tokens(tokens, K, device):
     return ptr, size, tokens.stride(0) if K > 1 else max(tokens.shape[1], 1)
 
 
+def _embed_usual(tokens, table, x):
+    """As :func:`_rope_usual`: tokens [K, R], table [K, V, W], x [K * R, W] and their pointers and strides."""
+    import torch
+    ks, ts, dev, tt, code = table.shape, tokens.shape, x.device, tokens.dtype, _types.codes.get(x.dtype)
+    if (len(ks) != 3 or len(ts) != 2 or code is None or dev.type != "cuda" or ts[0] != ks[0] or x.shape != (ts[0] * ts[1], ks[2]) or table.dtype is not torch.float32
+            or table.device != dev or tokens.device != dev or (tt is not torch.int64 and tt is not torch.int32)):
+        return None
+    (s0, s1, s2), (t0, t1), (x0, x1) = table.stride(), tokens.stride(), x.stride()
+    if not (s2 == t1 == x1 == 1 and s1 >= ks[2] and t0 >= ts[1] and x0 >= ks[2]):
+        return None
+    return (dev, code, ks, ts[1], (tokens.data_ptr(), 8 if tt is torch.int64 else 4, t0), (table.data_ptr(), s0 if ks[0] > 1 else ks[1] * s1, s1),
+            (x.data_ptr(), x0))
+
+
 def fgd_embed_forward(tokens, table, out, scale: float = 1.0, stream=None) -> None:
     """out[m * rows + i] = scale * table[m, tokens[m, i]]: tokens [K, rows] int64 or int32, table [K, V, W] fp32 (e.g. a column range of the parameter
     matrix), out [K * rows, W].  A token below 0 is padding: its row is zero."""
+    usual = _embed_usual(tokens, table, out)
+    if usual is not None:
+        dev, code, (K, V, W), R, tok, tab, mat = usual
+        _op_check(_lib.fgd_embed_forward(dev.index, code, K, R, V, W, *tok, *tab, scale, *mat, _stream_on(stream, dev)))
+        return
     dev = _device_of(out, "out")
     if out.dim() != 2:
         raise ValueError("out must be [tokens, width]")
@@ -846,12 +926,17 @@ def fgd_embed_workspace(workers: int, rows: int, vocab: int, width: int) -> int:
 def fgd_embed_backward(tokens, dout, dtable, scale: float = 1.0, workspace=None, stream=None) -> None:
     """Gradient of :func:`fgd_embed_forward`: dtable [K, V, W] (fp32), all of it, from dout [K * rows, W].  ``workspace``: a uint8 CUDA tensor of
     :func:`fgd_embed_workspace` bytes (None: allocated here)."""
-    dev = _device_of(dout, "dout")
-    if dout.dim() != 2:
-        raise ValueError("dout must be [tokens, width]")
-    tab, (K, V, W) = _table(dtable, "dtable", dev), dtable.shape
-    tok, rows = _embed_tokens(tokens, K, dev), tokens.shape[1]
-    grad, handle = _mat(dout, "dout", dout.dtype, K * rows, W, dev), _stream_on(stream, dev)
+    usual = _embed_usual(tokens, dtable, dout)
+    if usual is not None:
+        dev, code, (K, V, W), rows, tok, tab, grad = usual
+    else:
+        dev = _device_of(dout, "dout")
+        if dout.dim() != 2:
+            raise ValueError("dout must be [tokens, width]")
+        tab, (K, V, W) = _table(dtable, "dtable", dev), dtable.shape
+        tok, rows = _embed_tokens(tokens, K, dev), tokens.shape[1]
+        code, grad = _dtype_of(dout, "dout"), _mat(dout, "dout", dout.dtype, K * rows, W, dev)
+    handle = _stream_on(stream, dev)
     room = 0, 0
     if workspace is None:
         size = fgd_embed_workspace(K, rows, V, W)
@@ -859,13 +944,19 @@ def fgd_embed_backward(tokens, dout, dtable, scale: float = 1.0, workspace=None,
             workspace = _scratch(size, stream, handle, dev)
     if workspace is not None:
         room = _dev_ptr(workspace, "workspace", "torch.uint8"), workspace.numel()
-    _op_check(_lib.fgd_embed_backward(dev.index, _dtype_of(dout, "dout"), K, rows, V, W, *tok, *grad, scale, *tab, *room, handle))
+    _op_check(_lib.fgd_embed_backward(dev.index, code, K, rows, V, W, *tok, *grad, scale, *tab, *room, handle))
 
 
 def fgd_dropout(x, out, p: float, seed: int, offset: int = 0, counter=None, stream=None) -> None:
     """out = x / (1 - p) where the generator of (seed, offset, row, column) keeps the value, else 0; the mask is never stored, and the backward pass is the
     same call on the gradient.  ``counter``: a CUDA int64 tensor of one value that is added to the offset when the kernel runs.  out may be x."""
     import torch
+    xs, dt, dev, code = x.shape, x.dtype, x.device, _types.codes.get(x.dtype)
+    if counter is None and len(xs) == 2 and code is not None and dev.type == "cuda" and out.dtype is dt and out.shape == xs and out.device == dev:
+        (x0, x1), (o0, o1), (R, W) = x.stride(), out.stride(), xs
+        if x1 == o1 == 1 and x0 >= W and o0 >= W:      # as it usually is; else the checks one by one
+            _op_check(_lib.fgd_dropout(dev.index, code, R, W, x.data_ptr(), x0, out.data_ptr(), o0, p, seed, offset, 0, _stream_on(stream, dev)))
+            return
     if x.dim() != 2:
         raise ValueError("x must be [rows, width]")
     (R, W), dev = x.shape, _device_of(x, "x")
