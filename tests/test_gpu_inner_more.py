@@ -491,6 +491,76 @@ def test_dropout_counter_in_a_graph():
     assert np.array_equal(_np(out) != 0, O.dropout_keeps(50, 96, 0.4, 21, 2 ** 64 - 50))
 
 
+# ------------------------------------------------------------------------------- what the bindings do before the kernels
+def test_bindings_give_the_kernels_the_same_either_way(monkeypatch):
+    """The checks of the usual call, written out, and the checks one by one pass the same arguments: the same bits, strides and all."""
+    import paper_2606_22768_b200 as fgd
+    torch = _torch()
+    K, rows, V, W, hq, hk, d = 2, 21, 30, 48, 3, 1, 40
+    T = K * rows
+    theta = 1.0 + _randn((K, V * W + 2 * d + 3), "f32", 0, 0.2)
+    table, w_q, w_k = theta[:, :V * W].view(K, V, W), theta[:, V * W:V * W + d], theta[:, V * W + d:V * W + 2 * d]
+    tokens = torch.from_numpy(_text(K, rows + 4, V)).cuda()[:, :rows]
+    cos, sin = _tables(40, 24, pad=3)
+    pos = torch.arange(T, device="cuda", dtype=torch.int32) % 40
+    (q, _), (k, _), (gq, _), (gk, _) = (_layout(T, h, d, "bf16", "fused", fill=_randn((T, h, d), "bf16", 3 + i)) for i, h in enumerate((hq, hk, hq, hk)))
+
+    def run(counter=None):
+        grads = torch.zeros_like(theta)
+        e, dtable = torch.zeros((T, W + 8), device="cuda", dtype=torch.bfloat16)[:, :W], grads[:, :V * W].view(K, V, W)
+        yq, yk, dq, dk, dr = (torch.zeros_like(t) for t in (q, k, q, k, e))
+        fgd.fgd_embed_forward(tokens, table, e, 0.5)
+        fgd.fgd_embed_backward(tokens, e, dtable, 0.5)
+        fgd.fgd_dropout(e, dr, 0.3, 5, 6, counter)
+        fgd.fgd_qk_rope_forward(q, k, w_q, w_k, cos, sin, pos, yq, yk, 1e-4, True)
+        fgd.fgd_qk_rope_backward(gq, gk, q, k, w_q, w_k, cos, sin, pos, dq, dk, grads[:, V * W:V * W + d], grads[:, V * W + d:V * W + 2 * d], 1e-4, True)
+        return e.clone(), grads, yq, yk, dq, dk, dr
+
+    first = run()
+    monkeypatch.setattr(fgd, "_rope_usual", lambda *a: None)
+    monkeypatch.setattr(fgd, "_embed_usual", lambda *a: None)
+    assert all(torch.equal(a, b) and bool(a.any()) for a, b in zip(first, run(torch.zeros((), dtype=torch.int64, device="cuda"))))
+
+
+def test_bindings_refuse_on_the_gpu():
+    """What no kernel may get, one argument of a good call changed at a time: an error, and the outputs as they were."""
+    import paper_2606_22768_b200 as fgd
+    torch = _torch()
+    K, rows, V, W, h, d = 2, 4, 9, 16, 2, 32
+    T, f32 = K * rows, torch.float32
+    cos, sin = _tables(20, d)
+    full = lambda *shape, dtype=torch.bfloat16: torch.full(shape, 3.0, device="cuda", dtype=dtype)      # noqa: E731
+    pos, w = torch.zeros(T, dtype=torch.int64, device="cuda"), full(K, d, dtype=f32)
+    tokens, table = torch.zeros((K, rows), dtype=torch.int64, device="cuda"), full(K, V, W, dtype=f32)
+    forward = dict(q=full(T, h, d), k=full(T, h, d), w_q=w, w_k=w, cos=cos, sin=sin, positions=pos, q_out=full(T, h, d), k_out=full(T, h, d))
+    backward = dict(dq_out=full(T, h, d), dk_out=full(T, h, d), q=full(T, h, d), k=full(T, h, d), w_q=w, w_k=w, cos=cos, sin=sin, positions=pos,
+                    dq=full(T, h, d), dk=full(T, h, d), dw_q=full(K, d, dtype=f32), dw_k=full(K, d, dtype=f32))
+    x = full(T, W)
+    wrong = lambda t: (t.cpu(), t[:-1], t.to(torch.float64), t.unsqueeze(0))      # noqa: E731
+
+    def refused(call, good, extra):
+        kept = {n: t.clone() for n, t in good.items()}
+        for name, t in [(n, t) for n in good for t in wrong(good[n])] + extra:
+            with pytest.raises((TypeError, ValueError, fgd.FgdError)):
+                call(**{**good, name: t})
+                raise AssertionError(f"{name} {tuple(t.shape)} {t.dtype} {t.device} was taken")
+        assert all(torch.equal(good[n], t) for n, t in kept.items())
+
+    narrow = torch.empty((T, h, 2 * d), device="cuda", dtype=torch.bfloat16)[:, :, ::2]
+    refused(fgd.fgd_qk_rope_forward, forward, [
+        ("q", narrow), ("k", full(T, h, d - 1)), ("k_out", full(T, h + 1, d)), ("q_out", full(1, h, d).expand(T, h, d)), ("q_out", forward["k"]), ("k_out", forward["q_out"]),
+        ("q_out", forward["q"][:, :1].expand(T, h, d)), ("w_q", full(K + 1, d, dtype=f32)), ("w_k", full(K, d + 1, dtype=f32)), ("positions", pos.to(torch.int16)),
+        ("positions", torch.zeros(2 * T, dtype=torch.int64, device="cuda")[::2]), ("cos", cos[:, :-1]), ("sin", sin.t().contiguous().t())])
+    refused(fgd.fgd_qk_rope_backward, backward, [
+        ("q", narrow), ("dk_out", full(T, h, d - 1)), ("dq", full(1, h, d).expand(T, h, d)), ("dq", backward["q"]), ("dw_q", w), ("dw_k", backward["dw_q"]),
+        ("dw_q", full(1, d, dtype=f32).expand(K, d)), ("dw_q", full(K, 2 * d, dtype=f32)[:, ::2]), ("dw_k", full(K + 1, d, dtype=f32)), ("positions", pos[:-1])])
+    for call, good in ((fgd.fgd_embed_forward, dict(tokens=tokens, table=table, out=x)), (fgd.fgd_embed_backward, dict(tokens=tokens, dout=x, dtable=table))):
+        refused(call, good, [("tokens", tokens.to(torch.int16)), (list(good)[1 + ("out" not in good)], full(K, V, 2 * W, dtype=f32)[:, :, ::2])])
+    refused(fgd.fgd_embed_forward, dict(tokens=tokens, table=table, out=x), [("out", full(1, W).expand(T, W)), ("out", full(T, 2 * W)[:, ::2])])
+    refused(fgd.fgd_embed_backward, dict(tokens=tokens, dout=x, dtable=table), [("dtable", full(1, V, W, dtype=f32).expand(K, V, W)), ("dout", full(T, 2 * W)[:, ::2])])
+    refused(lambda x, out: fgd.fgd_dropout(x, out, 0.5, 0), dict(x=x, out=full(T, W)), [("out", full(1, W).expand(T, W)), ("x", full(T, 2 * W)[:, ::2]), ("out", x.t()), ("out", full(T, W + 1))])
+
+
 # ------------------------------------------------------------------------------- streams and graphs
 @pytest.mark.parametrize("rows", [900, 5000, 17000])
 @pytest.mark.parametrize("given", [False, True])
