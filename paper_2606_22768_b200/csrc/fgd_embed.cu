@@ -11,8 +11,8 @@
 //   joins  the pieces of the runs that cross chunks, which are few, eight warps to a run.
 // A few tokens need no sort: a warp looks through all of them for the one that its row of the table stands for, in one launch.
 // The order of every sum depends on the tokens alone.
-// 4 x 8192 tokens of 32000 rows, 2048 wide, bf16: 189 us, 94 % of the copy peak (sort 14, rows and zeros 168, joins 6); 65536 tokens of 50257, 1536 wide, f16:
-// 127 us (25, 84, 14).
+// 4 x 8192 tokens of 32000 rows, 2048 wide, bf16: 188 us, 94 % of the copy peak (sort 14, rows and zeros 168, joins 6); 65536 tokens of 50257, 1536 wide, f16:
+// 121 us (25, 84, 8).
 #include <cooperative_groups.h>
 
 #include <cmath>
@@ -139,11 +139,12 @@ __device__ __forceinline__ uint32_t same_digit(uint32_t digit, bool real, int bi
 // Pairs (token, position); a token outside the vocabulary counts as `vocab` and comes last.
 __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortArgs a) {
   const cg::cluster_group cluster = cg::this_cluster();
+  asm volatile("barrier.cluster.arrive;" ::: "memory");      // its wait: before the first store to another CTA, which has to be there by then
   extern __shared__ __align__(16) unsigned char smem[];
   const int bins = 1 << a.bits, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = blockIdx.x % a.cluster;
   const int64_t worker = blockIdx.x / a.cluster;
-  uint32_t* hist = reinterpret_cast<uint32_t*>(smem);                       // [bins] of this CTA's part
-  uint32_t* base = hist + bins;                                              // [bins] where the next key of a digit goes
+  uint32_t* hist = reinterpret_cast<uint32_t*>(smem);                       // [cluster][bins] of all CTAs' parts
+  uint32_t* base = hist + a.cluster * bins;                                  // [bins] where the next key of a digit goes
   unsigned short* count = reinterpret_cast<unsigned short*>(base + bins);    // [warp][bins] of a tile
   __shared__ uint32_t warp_total[kSortWarps];
   uint32_t* present = a.present + worker * a.words;
@@ -210,9 +211,8 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortArgs
       load(0);
       rank_tile(0);
       tile_sum = sum_warps();
-      if (tid < bins) hist[tid] = tile_sum;
     } else {
-      if (tid < bins) hist[tid] = 0u;
+      if (tid < bins) base[tid] = 0u;
       for (int t0 = 0; t0 < n; t0 += tile) {
         load(t0);
         __syncthreads();
@@ -221,9 +221,16 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortArgs
           const bool real = j < items && t0 + (warp * items + j) * 32 + lane < n;
           const uint32_t digit = real ? key[j].x >> shift & (bins - 1) : 0u;
           const uint32_t same = same_digit(digit, real, a.bits);
-          if (real && (same & ((1u << lane) - 1)) == 0) atomicAdd(&hist[digit], (uint32_t)__popc(same));
+          if (real && (same & ((1u << lane) - 1)) == 0) atomicAdd(&base[digit], (uint32_t)__popc(same));
         }
       }
+      __syncthreads();
+    }
+    // to every CTA of the cluster: stores, which nothing waits for as it would for loads (4 x 8192 tokens 1 us less)
+    if (pass == 0) asm volatile("barrier.cluster.wait;" ::: "memory");
+    if (tid < bins) {
+      const uint32_t h = single ? tile_sum : base[tid];
+      for (int r = 0; r < a.cluster; ++r) cluster.map_shared_rank(hist, r)[rank * bins + tid] = h;
     }
     cluster.sync();
     // where each digit starts: keys of smaller digits anywhere, and of this digit in the CTAs before; bins <= kSortThreads
@@ -232,7 +239,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortArgs
 #pragma unroll
       for (int r = 0; r < kCluster; ++r)
         if (r < a.cluster) {
-          const uint32_t h = cluster.map_shared_rank(hist, r)[tid];
+          const uint32_t h = hist[r * bins + tid];
           total += h;
           if (r < rank) before += h;
         }
@@ -413,7 +420,8 @@ __global__ void __launch_bounds__(kThreads) embed_rows_kernel(const RowsArgs a) 
   }
 }
 
-// Runs that cross chunks, listed in no particular order by the chunk that they start in.  128 columns to a CTA, a run to each of its warps; where the run
+// Runs that cross chunks, listed in no particular order by the chunk that they start in.  128 columns to a CTA, a run to each of its warps, from all over
+// the list: long runs stand together in it where common tokens have neighbouring numbers (65536 tokens 4 us less than with eight in a row).  Where the run
 // has more than kPieces further pieces, all warps share it: of 8 kPieces consecutive ones each adds kPieces, and their sums are added in
 // the warps' order.
 constexpr int kPieces = 8;
@@ -444,11 +452,12 @@ __global__ void __launch_bounds__(kThreads) embed_joins_kernel(const RowsArgs a)
       for (int j = 0; j < 4; ++j) acc[j] += p[i][j];
     return n;
   };
-  for (int run0 = blockIdx.x * kWarps; run0 < runs; run0 += gridDim.x * kWarps) {
+  for (int run0 = blockIdx.x; run0 < runs; run0 += gridDim.x * kWarps) {
+    const int mine = run0 + warp * gridDim.x;
     uint2 run = make_uint2(0u, 0u);
     bool longer = false;
-    if (run0 + warp < runs) {
-      run = a.list[run0 + warp];
+    if (mine < runs) {
+      run = a.list[mine];
       const int64_t worker = run.x / (uint32_t)a.chunks, chunk = run.x % (uint32_t)a.chunks;
       const uint2* e = a.pairs + worker * a.rows;
       const float* pieces = a.pieces + worker * a.chunks * 2 * a.width;
@@ -648,8 +657,9 @@ cudaError_t backward(const RowsArgs& r, cudaStream_t st) {
   const int64_t zeros = (int64_t)a.workers * ((a.words + a.cta_words - 1) / a.cta_words);
   cudaError_t e = launch_early(embed_rows_kernel<T, ANY>, dim3((unsigned)(a.sum_ctas + zeros)), kThreads, 0, st, a);
   if (e == cudaSuccess && a.chunks > 0) {
-    const int64_t columns = (a.width + 127) / 128, most = ((int64_t)a.workers * a.chunks + kWarps - 1) / kWarps, want = (int64_t)sm_count() * 4 / columns + 1;
-    e = launch_early(embed_joins_kernel, dim3((unsigned)(want < most ? want : most), (unsigned)columns), kThreads, 0, st, a);
+    // the CTAs that the SMs hold at once, three of 70 registers each: a few more are a second round (of 65536 tokens 3 us)
+    const int64_t columns = (a.width + 127) / 128, most = ((int64_t)a.workers * a.chunks + kWarps - 1) / kWarps, want = (int64_t)sm_count() * 3 / columns;
+    e = launch_early(embed_joins_kernel, dim3((unsigned)(want < 1 ? 1 : want < most ? want : most), (unsigned)columns), kThreads, 0, st, a);
   }
   return e;
 }
@@ -688,8 +698,8 @@ cudaError_t cluster_size(int* size, size_t smem) {
   return cudaSuccess;
 }
 cudaError_t sort(SortArgs& a, cudaStream_t st) {
-  const size_t smem = ((size_t)8 << a.bits) + ((size_t)kSortWarps * 2 << a.bits);
-  const size_t most = ((size_t)8 << kMaxBits) + ((size_t)kSortWarps * 2 << kMaxBits);
+  const auto smem = [&](int cluster, int bits) { return ((size_t)(4 * cluster + 4 + 2 * kSortWarps) << bits); };
+  const size_t most = smem(kCluster, kMaxBits);
   cudaError_t e = allow_smem<embed_sort_kernel>(most);
   // 3000 tokens of 20000: one CTA 18.2 us, four 10.8, eight 11.6, sixteen 14.1; 8000: four 14.4, eight 12.6, sixteen 14.3; 30000: 31, 21, 18.
   a.cluster = a.rows <= 4096 ? 4 : 8;
@@ -702,7 +712,7 @@ cudaError_t sort(SortArgs& a, cudaStream_t st) {
   cudaLaunchConfig_t c = {};
   c.gridDim = dim3((unsigned)(a.workers * a.cluster));
   c.blockDim = dim3(kSortThreads);
-  c.dynamicSmemBytes = smem;
+  c.dynamicSmemBytes = smem(a.cluster, a.bits);
   c.stream = st;
   c.attrs = &attr;
   c.numAttrs = 1;
