@@ -27,9 +27,12 @@ using namespace fgd;
 namespace {
 
 constexpr int kThreads = 128, kWarps = kThreads / 32;
-// CTAs on an SM: what the kernels' registers allow.  (The backward pass with four, that is 128 registers a thread and some of them spilled: 109 us for
-// 8 x 4096 tokens of 20 heads of 128, against 96.)
-constexpr int kForwardCtas = 4, kBackwardCtas = 3;
+// CTAs on an SM: what the kernels' registers allow, by the channels of a lane.  (Eight pairs: four and three; the backward pass with four, 128 registers a
+// thread and some of them spilled, takes 109 us for 8 x 4096 tokens of 20 heads of 128 instead of 96.  Fewer pairs: one CTA more: 16384 tokens of 20
+// heads, bf16, 72 wide 40 and 69 us with four and three, 38 and 61 with five and four; 100 wide 65 and 120, 61 and 97; 66 wide 96 and 223, 89 and 170; 80 wide fp32
+// 44 and 73, 41 and 62.  The one that loses: backward of 128 wide fp32, 85 and 92.)
+constexpr int ctas_of(int v, int nc, bool grad) { return (grad ? 4 : 5) - (v == 8 || nc == 4); }
+constexpr int kMostBackwardCtas = 4;
 constexpr int kMaxDim = 256;
 
 struct RopeHeads { char* p; int64_t ts, hs, step; };      // strides, and from one of a warp's batches to the next, in bytes
@@ -332,7 +335,7 @@ __device__ __forceinline__ void poison(float (&z)[NC][2 * V]) {
 
 // GRAD: the backward pass with weights.  Otherwise the forward pass, or the transposed rotation alone.
 template <typename T, int V, int NC, bool INTER, bool GRAD>
-__global__ void __launch_bounds__(kThreads, GRAD ? kBackwardCtas : kForwardCtas) rope_kernel(const __grid_constant__ RopeArgs a) {
+__global__ void __launch_bounds__(kThreads, ctas_of(V, NC, GRAD)) rope_kernel(const __grid_constant__ RopeArgs a) {
   constexpr int N = GRAD ? 2 : 1;      // tensors that are read: the gradient, x; or x alone
   using Ring = Feed<T, V, NC, N>;
   extern __shared__ __align__(16) unsigned char ring[];
@@ -544,7 +547,7 @@ bool vector_of(const void* p, int64_t s0, int64_t s1, int bytes, int vec) {
 
 struct Launch { int vec, lg, pairs; };
 
-int64_t workspace_bytes(int workers, int d) { return ((int64_t)sm_count() * kBackwardCtas + workers) * 2 * d * (int64_t)sizeof(float); }
+int64_t workspace_bytes(int workers, int d) { return ((int64_t)sm_count() * kMostBackwardCtas + workers) * 2 * d * (int64_t)sizeof(float); }
 
 template <typename T, int V, int NC, bool INTER, bool GRAD>
 cudaError_t start(const RopeArgs& a, int workers, int ctas, cudaStream_t st) {
@@ -706,7 +709,7 @@ int run_rope(const fgd_qk_rope_args* b, bool backward, int device, void* stream)
     a.gt = group_of(heads[0], heads[1], 32 / l.lg);
     // Warps share a token's heads where that evens out the rounds of the SMs' warps over the tokens (a step for a batch, and two more for each token).
     const int64_t tokens = 32 / l.lg / a.gt, warps = b->workers * ((b->rows + tokens - 1) / tokens);
-    const int per_sm = sums ? kBackwardCtas : kForwardCtas;
+    const int per_sm = ctas_of(l.vec, l.vec > 1 ? 1 : l.pairs <= 64 ? 2 : 4, sums);
     int64_t least = 0;
     for (int split = 1; split <= kWarps; split *= 2) {
       const int64_t places = (int64_t)sm_count() * per_sm * kWarps, rounds = (warps * split + places - 1) / places;
