@@ -11,7 +11,7 @@
 // rotation 60), backward 95 us (81 %; 83 to 85); rotation alone of 16384 tokens 31 us (83 %).
 //
 // A lane holds 2 V channels of a head: a chunk of V consecutive ones and the chunk of their partners, so the rotation needs no other lane and the
-// norm log2(lanes) shuffles.  LG lanes make a head, 32 / LG heads a warp.  Of those, gt (the largest power of two that divides both head counts)
+// norm log2(lanes) shuffles.  LG lanes make a head, 32 / LG heads a warp.  Of those, gt (the most that divide their number and both head counts)
 // belong to one token: a warp goes through its tokens' heads gt at a time, and a lane's cos and sin serve all that it has of a token.  It takes all
 // its q first and then its k: so the weights and, in the backward pass, the sums of their gradients (CTAs belong to one worker) stay in
 // registers, of one side at a time.  What the next steps need is on its way meanwhile: activations through a ring in shared memory that each lane
@@ -29,7 +29,7 @@ namespace {
 constexpr int kThreads = 128, kWarps = kThreads / 32;
 // CTAs on an SM: what the kernels' registers allow, by the channels of a lane.  (Eight pairs: four and three; the backward pass with four, 128 registers a
 // thread and some of them spilled, takes 109 us for 8 x 4096 tokens of 20 heads of 128 instead of 96.  Fewer pairs: one CTA more: 16384 tokens of 20
-// heads, bf16, 72 wide 40 and 69 us with four and three, 38 and 61 with five and four; 100 wide 65 and 120, 61 and 97; 66 wide 96 and 223, 89 and 170; 80 wide fp32
+// heads, bf16, 72 wide (with 16 lanes) 40 and 69 us with four and three, 38 and 61 with five and four; 100 wide 65 and 120, 61 and 97; 66 wide 96 and 223, 89 and 170; 80 wide fp32
 // 44 and 73, 41 and 62.  The one that loses: backward of 128 wide fp32, 85 and 92.)
 constexpr int ctas_of(int v, int nc, bool grad) { return (grad ? 4 : 5) - (v == 8 || nc == 4); }
 constexpr int kMostBackwardCtas = 4;
@@ -291,14 +291,29 @@ __device__ __forceinline__ void rotate(float (&z)[2 * V], const float (&cs)[V], 
     }
   }
 }
-// Sums over the lanes of a head, a power of two; all lanes of the warp take part.
-template <int N>
-__device__ __forceinline__ void head_sums(float (&v)[N], int lg) {
+// Sums over the lanes of a head, for each of them; `place` is a lane's in its head.  All lanes of the warp take part.  EXACT: any number of lanes, else
+// a power of two.
+template <bool EXACT, int N>
+__device__ __forceinline__ void head_sums(float (&v)[N], int lg, int place) {
+  if constexpr (EXACT) {      // folded in halves onto the first lane
 #pragma unroll
-  for (int o = 1; o < 32; o *= 2) {
-    if (o >= lg) break;
+    for (int o = 8; o > 0; o /= 2) {
+      if (o >= lg) continue;
 #pragma unroll
-    for (int n = 0; n < N; ++n) v[n] += __shfl_xor_sync(0xffffffffu, v[n], o);
+      for (int n = 0; n < N; ++n) {
+        const float t = __shfl_down_sync(0xffffffffu, v[n], o);
+        if (place + o < lg) v[n] += t;
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n] = __shfl_sync(0xffffffffu, v[n], (threadIdx.x & 31) - place);
+  } else {
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+      if (o >= lg) break;
+#pragma unroll
+      for (int n = 0; n < N; ++n) v[n] += __shfl_xor_sync(0xffffffffu, v[n], o);
+    }
   }
 }
 template <typename T, int V, int NC, bool INTER>
@@ -333,19 +348,22 @@ __device__ __forceinline__ void poison(float (&z)[NC][2 * V]) {
     for (int i = 0; i < 2 * V; ++i) z[j][i] = __int_as_float(0x7fffffff);
 }
 
-// GRAD: the backward pass with weights.  Otherwise the forward pass, or the transposed rotation alone.
-template <typename T, int V, int NC, bool INTER, bool GRAD>
+// GRAD: the backward pass with weights.  Otherwise the forward pass, or the transposed rotation alone.  EXACT: a.lg is any number of lanes up to 16.
+template <typename T, int V, int NC, bool INTER, bool GRAD, bool EXACT>
 __global__ void __launch_bounds__(kThreads, ctas_of(V, NC, GRAD)) rope_kernel(const __grid_constant__ RopeArgs a) {
   constexpr int N = GRAD ? 2 : 1;      // tensors that are read: the gradient, x; or x alone
   using Ring = Feed<T, V, NC, N>;
   extern __shared__ __align__(16) unsigned char ring[];
   __shared__ float sums[GRAD ? 2 : 1][GRAD ? kWarps : 1][kMaxDim];
-  const int worker = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x / 32, group = lane / a.lg, sub = group % a.gt;
+  const int worker = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  // (lanes behind the last head that fits have no channels)
+  const bool extra = EXACT && lane >= 32 / a.lg * a.lg;
+  const int group = extra ? 0 : lane / a.lg, in_head = extra ? a.pairs : lane % a.lg, sub = group % a.gt;
   const uint32_t tokens = 32 / a.lg / a.gt, mine = group / a.gt;      // tokens of a warp at once, this lane's among them
   const uint32_t rows = (uint32_t)a.rows, place = blockIdx.x * kWarps + warp, stride = gridDim.x * kWarps / a.split * tokens, first = place / a.split * tokens;
   const int part = place % a.split;
   const int64_t base = worker * a.rows + mine;
-  const Geometry<V, NC, INTER> geo(lane % a.lg, a);
+  const Geometry<V, NC, INTER> geo(in_head, a);
   if constexpr (GRAD) let_next_start();      // the sums' CTAs wait for this kernel's end on the SMs
   // The step that is fetched next, kDepth - 1 ahead: side, first token of the warp's group, batch, addresses.  (An address moves on by a constant
   // within a token; worked out anew in every step they were a third of the kernel's instructions.)
@@ -430,7 +448,7 @@ __global__ void __launch_bounds__(kThreads, ctas_of(V, NC, GRAD)) rope_kernel(co
 #pragma unroll
               for (int i = 0; i < 2 * V; i += 2) ss = fma2(two(z[j] + i), two(z[j] + i), ss);
             float sum[1] = {ss.x + ss.y};
-            head_sums(sum, a.lg);
+            head_sums<EXACT>(sum, a.lg, in_head);
             const float2 r = both(rsqrtf(fmaf(sum[0], a.inv_d, a.eps)));
 #pragma unroll
             for (int j = 0; j < NC; ++j)
@@ -455,7 +473,7 @@ __global__ void __launch_bounds__(kThreads, ctas_of(V, NC, GRAD)) rope_kernel(co
                 sg = fma2(mul2(two(z[j] + i), x), two(w[j] + i), sg);
               }
             float sum[2] = {ss.x + ss.y, sg.x + sg.y};
-            head_sums(sum, a.lg);
+            head_sums<EXACT>(sum, a.lg, in_head);
             const float r = rsqrtf(fmaf(sum[0], a.inv_d, a.eps)), k = r * r * (r * sum[1] * a.inv_d);
             if (real) {
 #pragma unroll
@@ -481,7 +499,11 @@ __global__ void __launch_bounds__(kThreads, ctas_of(V, NC, GRAD)) rope_kernel(co
 #pragma unroll
           for (int i = 0; i < 2 * V; ++i) {
             float t = dw[j][i];
-            for (int o = a.lg; o < 32; o *= 2) t += __shfl_xor_sync(0xffffffffu, t, o);
+            if constexpr (EXACT) {
+              for (int o = a.lg; o + a.lg <= 32; o += a.lg) t += __shfl_sync(0xffffffffu, dw[j][i], (lane + o) & 31);
+            } else {
+              for (int o = a.lg; o < 32; o *= 2) t += __shfl_xor_sync(0xffffffffu, t, o);
+            }
             const bool has = i < V ? geo.has0[j] : geo.has1[j];
             if (group == 0 && has) sums[side][warp][i < V ? geo.c0[j] + i : geo.c1[j] + i - V] = t;
           }
@@ -527,10 +549,10 @@ __global__ void __launch_bounds__(32 * kParts) rope_sums_kernel(const __grid_con
 }
 
 // ---- host
-// The largest power of two that divides both head counts, at most `groups`.
+// The most of a warp's lane groups that can share a token's heads evenly: it divides their number and both head counts.
 int group_of(int q_heads, int k_heads, int groups) {
-  int g = 1;
-  while (g < groups && q_heads % (2 * g) == 0 && k_heads % (2 * g) == 0) g *= 2;
+  int g = groups;
+  while (groups % g != 0 || q_heads % g != 0 || k_heads % g != 0) --g;
   return g;
 }
 // CTAs of one worker: its share of the SMs' places, and no more than there is work for.
@@ -549,20 +571,26 @@ struct Launch { int vec, lg, pairs; };
 
 int64_t workspace_bytes(int workers, int d) { return ((int64_t)sm_count() * kMostBackwardCtas + workers) * 2 * d * (int64_t)sizeof(float); }
 
-template <typename T, int V, int NC, bool INTER, bool GRAD>
+template <typename T, int V, int NC, bool INTER, bool GRAD, bool EXACT>
 cudaError_t start(const RopeArgs& a, int workers, int ctas, cudaStream_t st) {
   constexpr size_t smem = kWarps * Feed<T, V, NC, GRAD ? 2 : 1>::kWarpBytes;
-  cudaError_t e = smem > 32 * 1024 ? allow_smem<rope_kernel<T, V, NC, INTER, GRAD>>(smem) : cudaSuccess;
+  cudaError_t e = smem > 32 * 1024 ? allow_smem<rope_kernel<T, V, NC, INTER, GRAD, EXACT>>(smem) : cudaSuccess;
   if (e == cudaSuccess) {
-    rope_kernel<T, V, NC, INTER, GRAD><<<dim3(ctas, workers), kThreads, smem, st>>>(a);
+    rope_kernel<T, V, NC, INTER, GRAD, EXACT><<<dim3(ctas, workers), kThreads, smem, st>>>(a);
     e = cudaGetLastError();
   }
   return e;
 }
 template <typename T, int V, int NC>
 cudaError_t launch(const RopeArgs& a, int workers, int ctas, bool grad, bool inter, cudaStream_t st) {
-  if (grad) return inter ? start<T, V, NC, true, true>(a, workers, ctas, st) : start<T, V, NC, false, true>(a, workers, ctas, st);
-  return inter ? start<T, V, NC, true, false>(a, workers, ctas, st) : start<T, V, NC, false, false>(a, workers, ctas, st);
+  if constexpr (V >= 4) {
+    if ((a.lg & (a.lg - 1)) != 0) {
+      if (inter) return grad ? start<T, V, NC, true, true, true>(a, workers, ctas, st) : start<T, V, NC, true, false, true>(a, workers, ctas, st);
+      return grad ? start<T, V, NC, false, true, true>(a, workers, ctas, st) : start<T, V, NC, false, false, true>(a, workers, ctas, st);
+    }
+  }
+  if (inter) return grad ? start<T, V, NC, true, true, false>(a, workers, ctas, st) : start<T, V, NC, true, false, false>(a, workers, ctas, st);
+  return grad ? start<T, V, NC, false, true, false>(a, workers, ctas, st) : start<T, V, NC, false, false, false>(a, workers, ctas, st);
 }
 
 struct Mat { const char* name; const void* p; int64_t rows, width, ld; bool output; };
@@ -705,23 +733,41 @@ int run_rope(const fgd_qk_rope_args* b, bool backward, int device, void* stream)
     a.cos = static_cast<const float*>(b->cos.p); a.sin = static_cast<const float*>(b->sin.p); a.cos_ld = b->cos.ld; a.sin_ld = b->sin.ld;
     a.positions = has_positions ? b->positions : nullptr; a.position_bytes = b->position_bytes;
     a.rows = b->rows; a.table_rows = b->table_rows;
-    a.d = d; a.rot = rot; a.lg = l.lg; a.pairs = l.pairs;
-    a.gt = group_of(heads[0], heads[1], 32 / l.lg);
+    a.d = d; a.rot = rot; a.pairs = l.pairs;
     // Warps share a token's heads where that evens out the rounds of the SMs' warps over the tokens (a step for a batch, and two more for each token).
-    const int64_t tokens = 32 / l.lg / a.gt, warps = b->workers * ((b->rows + tokens - 1) / tokens);
     const int per_sm = ctas_of(l.vec, l.vec > 1 ? 1 : l.pairs <= 64 ? 2 : 4, sums);
-    int64_t least = 0;
-    for (int split = 1; split <= kWarps; split *= 2) {
-      const int64_t places = (int64_t)sm_count() * per_sm * kWarps, rounds = (warps * split + places - 1) / places;
-      const int64_t cost = rounds * ((heads[0] / a.gt + split - 1) / split + (heads[1] / a.gt + split - 1) / split + 2);
-      if (split == 1 || cost < least) { least = cost; a.split = split; }
+    struct Plan { int lg, gt, split; int64_t tokens; double steps; };
+    auto plan = [&](int lg) {
+      Plan p = {lg, group_of(heads[0], heads[1], 32 / lg), 1, 0, 0};
+      p.tokens = 32 / lg / p.gt;
+      const int64_t warps = b->workers * ((b->rows + p.tokens - 1) / p.tokens), places = (int64_t)sm_count() * per_sm * kWarps;
+      int64_t least = 0;
+      for (int split = 1; split <= kWarps; split *= 2) {
+        const int64_t rounds = (warps * split + places - 1) / places;
+        const int64_t batches = (heads[0] / p.gt + split - 1) / split + (heads[1] / p.gt + split - 1) / split + 2;
+        const double steps = batches * (warps * split > places ? (double)(warps * split) / (double)places : 1.);
+        if (split == 1 || rounds * batches < least) { least = rounds * batches; p.split = split; }
+        if (split == 1 || steps < p.steps) p.steps = steps;
+      }
+      return p;
+    };
+    Plan p = plan(l.lg);
+    // Heads of as many lanes as they have chunk pairs, instead of a power of two, where more of them fit a warp and that saves steps.  Chunks of 8 bytes are bound
+    // by instructions: 16384 tokens of 16 + 4 heads of 72, bf16, 38 and 61 us with 16 lanes, 29 and 49 with nine; rotation alone 28 and 23.  Of 16 bytes the rotation
+    // alone loses (32 + 32 heads of 80: 64 us with eight lanes, 69 with five: shorter pieces of memory), and with norms a third of the steps has to go:
+    // 16 + 4 heads of 80 30 and 51 us, 26 and 48; of 48 (four lanes or three) 33 us backward would become 40.  (What the estimate gets wrong: backward of
+    // 3000 tokens of 16 + 4 heads of 80, 18 us and 21.)
+    if (l.vec >= 4 && l.pairs <= 16 && 32 / l.pairs > 32 / l.lg) {
+      const Plan exact = plan(l.pairs);
+      if (exact.steps < (l.vec * bytes < 16 ? 1. : any_norm ? 0.68 : 0.) * p.steps) p = exact;
     }
+    a.lg = p.lg; a.gt = p.gt; a.split = p.split;
     for (int i = 0; i < 2; ++i) {
       RopeSide& side = a.side[i];
       side.batches = heads[i] / a.gt;
       for (RopeHeads* h : {&side.x, &side.y, &side.g}) h->step = h->hs * a.gt * a.split;
     }
-    c.ctas = ctas_for(per_sm, b->workers, b->rows * a.split, tokens);
+    c.ctas = ctas_for(per_sm, b->workers, b->rows * a.split, p.tokens);
     a.eps = (float)b->eps; a.inv_d = 1.f / (float)d; a.turn = backward ? -1.f : 1.f;
     const bool inter = b->interleaved != 0;
     auto by_vec = [&](auto zero) {

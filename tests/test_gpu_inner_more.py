@@ -121,6 +121,15 @@ def test_rope_many_tokens(norm):
     _rope_case(2, 9001, 3, 1, 64, 64, False, norm, "bf16", N=4000)
 
 
+@pytest.mark.parametrize("K,rows,hq,hk,d,rot,inter,norm,dtype", [
+    (2, 6001, 2, 1, 72, 72, False, "qk", "bf16"), (1, 12002, 2, 1, 72, 40, True, "q", "f16"), (1, 12001, 2, 1, 72, 72, True, "", "bf16"), (3, 3001, 6, 2, 40, 40, False, "qk", "bf16"),
+    (1, 30001, 2, 2, 24, 16, True, "qk", "f16"), (1, 9000, 16, 4, 80, 80, False, "qk", "bf16"), (2, 4501, 4, 4, 96, 96, True, "qk", "bf16"), (1, 5003, 6, 2, 80, 48, True, "qk", "f32"),
+    (5, 1001, 6, 0, 80, 80, False, "q", "f32"), (1, 9001, 4, 4, 96, 48, False, "k", "f16")])
+def test_rope_many_tokens_of_heads_of_any_number_of_lanes(K, rows, hq, hk, d, rot, inter, norm, dtype):
+    """As many lanes to a head as it has chunks, three to six heads to a warp: taken where there are more tokens than the GPU's warps."""
+    _rope_case(K, rows, hq, hk, d, rot, inter, norm, dtype, "fused" if K == 1 else "plain", N=300)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 def test_rotation_alone_is_the_plain_one_to_the_bit(dtype):
     """Without weights: the results and gradients of the rotation written out in fp32."""
