@@ -11,8 +11,8 @@
 //   joins  the pieces of the runs that cross chunks, which are few, eight warps to a run.
 // A few tokens need no sort: a warp looks through all of them for the one that its row of the table stands for, in one launch.
 // The order of every sum depends on the tokens alone.
-// 4 x 8192 tokens of 32000 rows, 2048 wide, bf16: 188 us, 94 % of the copy peak (sort 14, rows and zeros 168, joins 6); 65536 tokens of 50257, 1536 wide, f16:
-// 121 us (25, 84, 8).
+// 4 x 8192 tokens of 32000 rows, 2048 wide, bf16: 187 us, 95 % of the copy peak (sort 13, rows and zeros 168, joins 6); 65536 tokens of 50257, 1536 wide, f16:
+// 121 us (25, 84, 12).
 #include <cooperative_groups.h>
 
 #include <cmath>
