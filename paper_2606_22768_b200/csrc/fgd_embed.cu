@@ -66,6 +66,7 @@ template <typename T, bool ANY, bool SHORT>
 __global__ void __launch_bounds__(kThreads, SHORT ? 3 : ANY ? 4 : 5) embed_forward_kernel(const EmbedArgs a) {
   using S = Slab<T, ANY>;
   constexpr int V = S::V, ROWS = SHORT ? kSlabs : 1;
+  wait_for_previous();
   // the worker is the grid's second axis: 64-bit divisions would be a good part of the instructions
   const int64_t worker = blockIdx.y, t0 = ((int64_t)blockIdx.x * kWarps + threadIdx.x / 32) * ROWS;
   if (t0 >= a.rows) return;
@@ -639,9 +640,8 @@ cudaError_t forward(const EmbedArgs& a, int workers, cudaStream_t st) {
   // a warp goes through its whole row, unless there are few rows: then its parts go to several
   const int64_t parts = (slabs + kSlabs - 1) / kSlabs, cuts = (int64_t)sm_count() * 4 / (ctas * workers) + 1;
   const dim3 grid((unsigned)ctas, (unsigned)workers, (unsigned)(cuts < parts ? cuts : parts));
-  if (slabs == 1) embed_forward_kernel<T, ANY, true><<<grid, kThreads, 0, st>>>(a);
-  else embed_forward_kernel<T, ANY, false><<<grid, kThreads, 0, st>>>(a);
-  return cudaGetLastError();
+  // (starting while the kernel before it ends saves 0.2 to 0.5 us; the gradient's sort gains nothing by it)
+  return launch_early(slabs == 1 ? embed_forward_kernel<T, ANY, true> : embed_forward_kernel<T, ANY, false>, grid, kThreads, 0, st, a);
 }
 template <typename T, bool ANY>
 cudaError_t backward(const RowsArgs& r, cudaStream_t st) {

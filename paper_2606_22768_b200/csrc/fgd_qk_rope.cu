@@ -364,6 +364,7 @@ __global__ void __launch_bounds__(kThreads, ctas_of(V, NC, GRAD)) rope_kernel(co
   const int part = place % a.split;
   const int64_t base = worker * a.rows + mine;
   const Geometry<V, NC, INTER> geo(in_head, a);
+  wait_for_previous();
   if constexpr (GRAD) let_next_start();      // the sums' CTAs wait for this kernel's end on the SMs
   // The step that is fetched next, kDepth - 1 ahead: side, first token of the warp's group, batch, addresses.  (An address moves on by a constant
   // within a token; worked out anew in every step they were a third of the kernel's instructions.)
@@ -576,8 +577,8 @@ cudaError_t start(const RopeArgs& a, int workers, int ctas, cudaStream_t st) {
   constexpr size_t smem = kWarps * Feed<T, V, NC, GRAD ? 2 : 1>::kWarpBytes;
   cudaError_t e = smem > 32 * 1024 ? allow_smem<rope_kernel<T, V, NC, INTER, GRAD, EXACT>>(smem) : cudaSuccess;
   if (e == cudaSuccess) {
-    rope_kernel<T, V, NC, INTER, GRAD, EXACT><<<dim3(ctas, workers), kThreads, smem, st>>>(a);
-    e = cudaGetLastError();
+    // (starting while the kernel before it ends saves 0.2 to 0.6 us)
+    e = launch_early(rope_kernel<T, V, NC, INTER, GRAD, EXACT>, dim3(ctas, workers), kThreads, smem, st, a);
   }
   return e;
 }
