@@ -85,7 +85,8 @@ __device__ __forceinline__ uint32_t verdicts(uint32_t group, const RowWords& row
   return keep;
 }
 
-__device__ __forceinline__ uint64_t offset_of(const DropoutArgs& a) { return a.offset + (a.counter ? (uint64_t)__ldg(a.counter) : 0u); }
+// (volatile: not before the wait for the kernel that may have written it)
+__device__ __forceinline__ uint64_t offset_of(const DropoutArgs& a) { return a.offset + (a.counter ? (uint64_t)*(const volatile int64_t*)a.counter : 0u); }
 
 // A warp takes strips of kStrip x 32 chunks of 16 bytes of a row.  32768 x 4096 bf16: 86 us, 95 % of the copy peak (with one chunk a thread and nothing
 // shared between them 106 us: bound by the generator's instructions).
@@ -114,11 +115,11 @@ __device__ __forceinline__ void store_some(T* p, const ActPack<T, V>& y, int c, 
 template <typename T, bool INSIDE>
 __global__ void __launch_bounds__(kThreads) dropout_kernel(const DropoutArgs a) {
   constexpr int V = 16 / sizeof(T), kColumns = 32 * kStrip * V;
-  wait_for_previous();
+  const int cta = wait_for_previous((int)blockIdx.x);
   const uint64_t offset = offset_of(a);
   const int lane = threadIdx.x & 31, strips = (int)((a.width + (INSIDE ? V - 1 : 0) + kColumns - 1) / kColumns);
   const int64_t total = a.rows * strips, stride = (int64_t)gridDim.x * (kThreads / 32);
-  int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / 32;
+  int64_t i = ((int64_t)cta * kThreads + threadIdx.x) / 32;
   Walk w(i, stride, strips);
   for (; i < total; i += stride, w.next()) {
     const T* x = reinterpret_cast<const T*>(a.x) + w.row * a.ld_x;
@@ -171,14 +172,14 @@ __global__ void __launch_bounds__(kThreads) dropout_kernel(const DropoutArgs a) 
 template <typename T>
 __global__ void __launch_bounds__(kThreads) dropout_shifted_kernel(const DropoutArgs a) {
   constexpr int V = 16;
-  wait_for_previous();
+  const int cta = wait_for_previous((int)blockIdx.x);
   const uint64_t offset = offset_of(a);
   const int units = (int)((a.width + V - 1) / V);
   const int64_t total = a.rows * units, padded = (total + 31) / 32 * 32, stride = (int64_t)gridDim.x * kThreads;      // whole warps stay for the shuffles
   const T* x = reinterpret_cast<const T*>(a.x);
   const T* end = x + (a.rows - 1) * a.ld_x + a.width;
   T* out = reinterpret_cast<T*>(a.out);
-  int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  int64_t i = (int64_t)cta * kThreads + threadIdx.x;
   Walk w(i, stride, units);
   for (; i < padded; i += stride, w.next()) {
     const ShiftedUnit<V> u(w, i < total, a.width);
@@ -199,7 +200,7 @@ cudaError_t go(const DropoutArgs& a, int64_t threads, int waves, cudaStream_t st
     if (known) cached[dev] = fit;
   }
   const int64_t want = (threads + kThreads - 1) / kThreads, most = (int64_t)sm_count() * fit * waves;
-  // (starting while the kernel before it ends saves 0.4 to 0.7 us)
+  // (starting while the kernel before it ends saves 0.4 to 0.7 us, among other work 2)
   return launch_early(KERNEL, dim3((unsigned)(want < most ? want : most)), kThreads, 0, st, a);
 }
 

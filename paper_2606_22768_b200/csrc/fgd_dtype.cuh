@@ -159,6 +159,12 @@ inline int sm_count() {
 // once every CTA of that one has called let_next_start (or has ended); wait_for_previous then waits for its end and its writes.
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// The same, and `index`, known only then: no load whose address depends on it can be moved before the wait, not even one that the compiler takes for a load of
+// what never changes.
+__device__ __forceinline__ int wait_for_previous(int index) {
+  asm volatile("griddepcontrol.wait;" : "+r"(index) : : "memory");
+  return index;
+}
 template <typename... P, typename... A>
 cudaError_t launch_early(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, A&&... args) {
   cudaLaunchAttribute attr = {};

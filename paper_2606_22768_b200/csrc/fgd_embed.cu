@@ -66,9 +66,8 @@ template <typename T, bool ANY, bool SHORT>
 __global__ void __launch_bounds__(kThreads, SHORT ? 3 : ANY ? 4 : 5) embed_forward_kernel(const EmbedArgs a) {
   using S = Slab<T, ANY>;
   constexpr int V = S::V, ROWS = SHORT ? kSlabs : 1;
-  wait_for_previous();
   // the worker is the grid's second axis: 64-bit divisions would be a good part of the instructions
-  const int64_t worker = blockIdx.y, t0 = ((int64_t)blockIdx.x * kWarps + threadIdx.x / 32) * ROWS;
+  const int64_t worker = wait_for_previous((int)blockIdx.y), t0 = ((int64_t)blockIdx.x * kWarps + threadIdx.x / 32) * ROWS;
   if (t0 >= a.rows) return;
   const float* row[ROWS];
   float other[ROWS];           // of a token outside the vocabulary
@@ -143,7 +142,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortArgs
   asm volatile("barrier.cluster.arrive;" ::: "memory");      // its wait: before the first store to another CTA, which has to be there by then
   extern __shared__ __align__(16) unsigned char smem[];
   const int bins = 1 << a.bits, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = blockIdx.x % a.cluster;
-  const int64_t worker = blockIdx.x / a.cluster;
+  const int64_t worker = wait_for_previous((int)(blockIdx.x / a.cluster));
   uint32_t* hist = reinterpret_cast<uint32_t*>(smem);                       // [cluster][bins] of all CTAs' parts
   uint32_t* base = hist + a.cluster * bins;                                  // [bins] where the next key of a digit goes
   unsigned short* count = reinterpret_cast<unsigned short*>(base + bins);    // [warp][bins] of a tile
@@ -522,7 +521,7 @@ __global__ void __launch_bounds__(kThreads) embed_few_kernel(const FewArgs a) {
   __shared__ int lengths[kWarps];
   __shared__ __align__(16) float sums[kWarps][S::kColumns];
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
-  const int64_t worker = blockIdx.y, v0 = (int64_t)blockIdx.x * kWarps, v = v0 + warp;
+  const int64_t worker = wait_for_previous((int)blockIdx.y), v0 = (int64_t)blockIdx.x * kWarps, v = v0 + warp;
   for (int i = threadIdx.x; i < a.rows; i += kThreads) {
     const int64_t tok = a.tokens.at(worker, i);
     tokens[i] = tok >= 0 && tok < a.vocab ? (int)tok : -1;
@@ -640,7 +639,7 @@ cudaError_t forward(const EmbedArgs& a, int workers, cudaStream_t st) {
   // a warp goes through its whole row, unless there are few rows: then its parts go to several
   const int64_t parts = (slabs + kSlabs - 1) / kSlabs, cuts = (int64_t)sm_count() * 4 / (ctas * workers) + 1;
   const dim3 grid((unsigned)ctas, (unsigned)workers, (unsigned)(cuts < parts ? cuts : parts));
-  // (starting while the kernel before it ends saves 0.2 to 0.5 us; the gradient's sort gains nothing by it)
+  // (starting while the kernel before it ends saves 0.2 to 0.5 us, among other work 2)
   return launch_early(slabs == 1 ? embed_forward_kernel<T, ANY, true> : embed_forward_kernel<T, ANY, false>, grid, kThreads, 0, st, a);
 }
 template <typename T, bool ANY>
@@ -669,8 +668,7 @@ cudaError_t few(const FewArgs& f, int workers, cudaStream_t st) {
   a.slabs = (a.width + Slab<T, ANY>::kColumns - 1) / Slab<T, ANY>::kColumns;
   // every CTA looks through the tokens, so columns are cut only as far as the SMs would stay empty
   const int64_t ctas = (a.vocab + kWarps - 1) / kWarps, want = (int64_t)sm_count() * 4 / (ctas * workers) + 1;
-  embed_few_kernel<T, ANY><<<dim3((unsigned)ctas, workers, (unsigned)(want < a.slabs ? want : a.slabs)), kThreads, 0, st>>>(a);
-  return cudaGetLastError();
+  return launch_early(embed_few_kernel<T, ANY>, dim3((unsigned)ctas, workers, (unsigned)(want < a.slabs ? want : a.slabs)), kThreads, 0, st, a);
 }
 // CTAs of a cluster that sorts many tokens: sixteen where the device can place so many (of 65536 tokens 25 us, eight 35), which CUDA does not promise.
 cudaError_t cluster_size(int* size, size_t smem) {
@@ -705,17 +703,19 @@ cudaError_t sort(SortArgs& a, cudaStream_t st) {
   a.cluster = a.rows <= 4096 ? 4 : 8;
   if (e == cudaSuccess && a.rows > 16384) e = cluster_size(&a.cluster, most);
   if (e != cudaSuccess) return e;
-  cudaLaunchAttribute attr = {};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = a.cluster;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = a.cluster;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t c = {};
   c.gridDim = dim3((unsigned)(a.workers * a.cluster));
   c.blockDim = dim3(kSortThreads);
   c.dynamicSmemBytes = smem(a.cluster, a.bits);
   c.stream = st;
-  c.attrs = &attr;
-  c.numAttrs = 1;
+  c.attrs = attr;
+  c.numAttrs = 2;
   return cudaLaunchKernelEx(&c, embed_sort_kernel, a);
 }
 

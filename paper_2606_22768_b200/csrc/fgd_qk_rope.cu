@@ -355,16 +355,16 @@ __global__ void __launch_bounds__(kThreads, ctas_of(V, NC, GRAD)) rope_kernel(co
   using Ring = Feed<T, V, NC, N>;
   extern __shared__ __align__(16) unsigned char ring[];
   __shared__ float sums[GRAD ? 2 : 1][GRAD ? kWarps : 1][kMaxDim];
-  const int worker = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
   // (lanes behind the last head that fits have no channels)
   const bool extra = EXACT && lane >= 32 / a.lg * a.lg;
   const int group = extra ? 0 : lane / a.lg, in_head = extra ? a.pairs : lane % a.lg, sub = group % a.gt;
   const uint32_t tokens = 32 / a.lg / a.gt, mine = group / a.gt;      // tokens of a warp at once, this lane's among them
   const uint32_t rows = (uint32_t)a.rows, place = blockIdx.x * kWarps + warp, stride = gridDim.x * kWarps / a.split * tokens, first = place / a.split * tokens;
   const int part = place % a.split;
-  const int64_t base = worker * a.rows + mine;
   const Geometry<V, NC, INTER> geo(in_head, a);
-  wait_for_previous();
+  const int worker = wait_for_previous((int)blockIdx.y);
+  const int64_t base = worker * a.rows + mine;
   if constexpr (GRAD) let_next_start();      // the sums' CTAs wait for this kernel's end on the SMs
   // The step that is fetched next, kDepth - 1 ahead: side, first token of the warp's group, batch, addresses.  (An address moves on by a constant
   // within a token; worked out anew in every step they were a third of the kernel's instructions.)
@@ -577,7 +577,7 @@ cudaError_t start(const RopeArgs& a, int workers, int ctas, cudaStream_t st) {
   constexpr size_t smem = kWarps * Feed<T, V, NC, GRAD ? 2 : 1>::kWarpBytes;
   cudaError_t e = smem > 32 * 1024 ? allow_smem<rope_kernel<T, V, NC, INTER, GRAD, EXACT>>(smem) : cudaSuccess;
   if (e == cudaSuccess) {
-    // (starting while the kernel before it ends saves 0.2 to 0.6 us)
+    // (starting while the kernel before it ends saves 0.2 to 0.6 us, among other work 2)
     e = launch_early(rope_kernel<T, V, NC, INTER, GRAD, EXACT>, dim3(ctas, workers), kThreads, smem, st, a);
   }
   return e;
