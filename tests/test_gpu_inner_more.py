@@ -571,6 +571,39 @@ def test_bindings_refuse_on_the_gpu():
 
 
 # ------------------------------------------------------------------------------- streams and graphs
+def test_inputs_written_right_before():
+    """The kernels start before the one in front of them has ended; what it writes is what they read, the counter too."""
+    import paper_2606_22768_b200 as fgd
+    torch = _torch()
+    T, h, d, K, rows, V, W = 20000, 8, 64, 1, 8192, 5000, 512
+    given = [_randn((T, h, d), "f32", 0), 1.0 + _randn((1, d), "f32", 1, 0.1), torch.arange(T, device="cuda") % 300, _tables(300, d)[0], _randn((K, V, W), "f32", 2),
+             torch.from_numpy(_text(K, rows, V)).cuda(), torch.full((), 3, dtype=torch.int64, device="cuda")]
+    sin = _tables(300, d)[1]
+
+    def run(fresh):
+        q, w, pos, cos, table, tokens, counter = given
+        if fresh:      # each input is written by the kernel in front of the call
+            q, w, pos, cos, table, tokens, counter = (torch.zeros_like(t) for t in given)
+            for to, t in zip((w, pos, cos, q), (given[1], given[2], given[3], given[0])):
+                to.copy_(t)
+        qo, ko, e, dtable, dropped = torch.empty_like(q), torch.empty_like(q), torch.empty((K * rows, W), device="cuda"), torch.empty_like(given[4]), torch.empty((K * rows, W), device="cuda")
+        fgd.fgd_qk_rope_forward(q, q, w, w, cos, sin, pos, qo, ko)
+        if fresh:
+            table.copy_(given[4])
+            tokens.copy_(given[5])
+        fgd.fgd_embed_forward(tokens, table, e)
+        fgd.fgd_embed_backward(tokens, e, dtable)
+        if fresh:
+            counter.copy_(given[6])
+        fgd.fgd_dropout(e, dropped, 0.3, 1, 2, counter)
+        torch.cuda.synchronize()
+        return qo, ko, e, dtable, dropped
+
+    want = run(False)
+    for _ in range(20):
+        assert all(torch.equal(a, b) for a, b in zip(want, run(True)))
+
+
 @pytest.mark.parametrize("rows", [900, 5000, 17000])
 @pytest.mark.parametrize("given", [False, True])
 def test_on_streams_and_in_graphs(given, rows):
