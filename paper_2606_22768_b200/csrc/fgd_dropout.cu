@@ -137,14 +137,14 @@ __global__ void __launch_bounds__(kThreads) dropout_kernel(const DropoutArgs a) 
     if constexpr (INSIDE) {
       const int m = -before & 3;      // c0 - m is a multiple of 4 (-4 in a row's first chunk, where what is made of that group is not used)
       const int group = (c0 - m) >> 2, chunks = (width - c0 + lane * V + V - 1) / V;      // (of the row from this strip's first on: the same in all lanes)
-      uint32_t keep[kStrip + 1];
+      uint32_t keep[kStrip + 1];      // (also behind the row's last chunk where that is lane 31's: its last m columns belong to the group after its own)
 #pragma unroll
       for (int k = 0; k <= kStrip; ++k)
-        if (k * 32 < chunks || k == 0) keep[k] = k < kStrip ? verdicts<V>((uint32_t)(group + k * 8 * V), row, a) : verdicts<4>((uint32_t)(group + k * 8 * V), row, a);
+        if (k * 32 <= chunks) keep[k] = k < kStrip ? verdicts<V>((uint32_t)(group + k * 8 * V), row, a) : verdicts<4>((uint32_t)(group + k * 8 * V), row, a);
 #pragma unroll
       for (int k = 0; k < kStrip; ++k) {
         if (k * 32 >= chunks) break;
-        const uint32_t above = __shfl_down_sync(0xffffffffu, keep[k], 1), first = (k + 1) * 32 < chunks ? __shfl_sync(0xffffffffu, keep[k + 1], 0) : 0u;
+        const uint32_t above = __shfl_down_sync(0xffffffffu, keep[k], 1), first = (k + 1) * 32 <= chunks ? __shfl_sync(0xffffffffu, keep[k + 1], 0) : 0u;
         const uint32_t bits = (keep[k] | (lane == 31 ? first : above) << V) >> m;
         const int c = c0 + k * 32 * V;
         Vals<V> y = unpack<T, V>(raw[k]);

@@ -445,6 +445,44 @@ def test_dropout_mask_does_not_depend_on_the_layout():
         assert abs(same - 0.5) < 5 * 0.5 / (700 * 520) ** 0.5
 
 
+# Widths whose rows, with what the first 16-byte chunk has before them, are whole numbers of 32 chunks, and their neighbours.
+ENDS = [("f32", W) for W in (1148, 1149, 1150, 1151, 1152, 1279, 4095)] + [(t, W) for t in ("bf16", "f16") for W in (2296, 2297, 2298, 2299, 2301, 2302, 2303, 2304, 4095)]
+
+
+@pytest.mark.parametrize("dtype,W", ENDS)
+def test_dropout_rows_that_end_with_a_warps_last_chunk(dtype, W):
+    """Long rows that start anywhere in a 16-byte chunk, x and out alike: the last columns have verdicts of their own."""
+    import paper_2606_22768_b200 as fgd
+    torch = _torch()
+    R, seed, offset = 19, 0x1234567812345678, 2 ** 40 + 3
+    for lead in (0, 1, 3):
+        for ld in (W, W + 1):
+            x, out = (torch.empty((lead + R * ld,), dtype=_dt(dtype), device="cuda")[lead:].view(R, ld)[:, :W] for _ in range(2))
+            x.copy_(_randn((R, W), dtype, lead))
+            fgd.fgd_dropout(x, out, 0.0, seed, offset)
+            assert torch.equal(out, x), (lead, ld, "nothing is dropped where p is 0")
+            keeps = O.dropout_keeps(R, W, 0.4, seed, offset)
+            fgd.fgd_dropout(x, out, 0.4, seed, offset)
+            ref = np.where(keeps, _np(x) / 0.6, 0.0)
+            _near(out, ref, (U[dtype] + 3 * F32) * np.abs(ref) + TINY[dtype], f"out {lead} {ld}")
+            assert np.array_equal(_np(out) != 0, keeps & (_np(x) != 0)), (lead, ld)
+
+
+@pytest.mark.parametrize("dtype,W", ENDS)
+def test_dropout_mask_of_long_rows_does_not_depend_on_the_layout(dtype, W):
+    """Rows on the 16-byte boundaries (with columns behind them), rows that start anywhere in a chunk, and x and out at different places of one."""
+    import paper_2606_22768_b200 as fgd
+    torch = _torch()
+    R, wide = 19, -(-W // 8) * 8
+    masks = []
+    for width, ld, lead_x, lead_out in ((wide, wide, 0, 0), (W, W, 0, 0), (W, W, 1, 1), (W, W + 2, 3, 3), (W, W, 0, 1), (W, W + 1, 3, 2)):
+        x = torch.ones((lead_x + R * ld,), dtype=_dt(dtype), device="cuda")[lead_x:].view(R, ld)[:, :width]
+        out = torch.empty((lead_out + R * ld,), dtype=_dt(dtype), device="cuda")[lead_out:].view(R, ld)[:, :width]
+        fgd.fgd_dropout(x, out, 0.5, 5, 9)
+        masks.append(out[:, :W] != 0)
+    assert all(torch.equal(masks[0], m) for m in masks)
+
+
 @pytest.mark.parametrize("p", [0.0, 1e-3, 0.1, 0.5, 0.9, 1.0 - 2.0 ** -33])
 def test_dropout_rate(p):
     import paper_2606_22768_b200 as fgd
