@@ -76,8 +76,10 @@ class _Embedding(torch.autograd.Function):
 
 
 def embedding(tokens, table, scale: float = 1.0, dtype: torch.dtype = torch.bfloat16):
-    """scale * table[m, tokens[m]] of every worker m: tokens [K, rows] (below 0: padding, a row of zeros), table [K, V, W] fp32, which may be a column range
-    of the parameter matrix -> [K * rows, W]."""
+    """scale * table[m, tokens[m]] of every worker m: tokens [K, rows] (below 0: padding, a row of zeros; V or above: a row of NaN without a gradient) with any
+    strides, table [K, V, W] fp32, which may be a column range of the parameter matrix -> [K * rows, W]."""
+    if tokens.dim() == 2 and (tokens.stride(1) != 1 or tokens.stride(0) < tokens.shape[1]):      # transposed, expanded over the workers, windows of one text
+        tokens = tokens.contiguous()
     return _Embedding.apply(tokens, table, scale, dtype)
 
 

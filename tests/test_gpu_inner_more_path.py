@@ -252,3 +252,31 @@ def test_example_runs_with_norms_and_dropout():
     spec.loader.exec_module(ex)
     history = ex.main(["--rounds", "2", "--inner", "2", "--workers", "2", "--qk-norm", "--dropout", "0.1"])
     assert len(history) == 2 and all(np.isfinite(v) for row in history for v in row)
+
+
+@pytest.mark.parametrize("how", ["expanded", "transposed", "every second", "windows", "columns", "one worker", "int32"])
+def test_decoder_takes_tokens_of_any_strides(how):
+    """Logits and gradients are those of the same tokens laid out in rows."""
+    import paper_2606_22768_b200 as fgd
+    from paper_2606_22768_b200 import inner
+    torch = _torch()
+    cfg = inner.DecoderConfig()
+    K, lens = 1 if how == "one worker" else 3, [60, 4]
+    rows = sum(lens)
+    many = torch.randint(cfg.vocab, (K * rows * 2,), generator=torch.Generator().manual_seed(1)).cuda()
+    tokens = {"expanded": lambda: many[None, :rows].expand(K, -1), "transposed": lambda: many[:rows * K].view(rows, K).t(), "every second": lambda: many.view(K, 2 * rows)[:, ::2],
+              "windows": lambda: many.unfold(0, rows, 1)[:K], "columns": lambda: many.view(K, 2 * rows)[:, 5:5 + rows], "one worker": lambda: many[:rows].view(rows, 1).t(),
+              "int32": lambda: many[None, :rows].int().expand(K, -1)}[how]()
+    assert tokens.shape == (K, rows)
+    _, P = inner.param_layout(cfg)
+    theta = torch.zeros((K, P), device="cuda")
+    inner.init_params(theta, cfg, 0)
+    plan = fgd.AttnPlan(np.concatenate([[0], np.cumsum(lens * K)]))
+    positions = torch.cat([torch.arange(n) for n in lens * K]).cuda()
+    got = []
+    for t in (tokens, tokens.contiguous().clone()):
+        leaf = theta.clone().requires_grad_(True)
+        logits = inner.decoder_logits(leaf, t, plan, positions, cfg)
+        logits.float().square().sum().backward()
+        got.append((logits.detach(), leaf.grad))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
