@@ -376,12 +376,15 @@ class InnerSteps:
         self.m, self.v, self.t = torch.zeros_like(theta), torch.zeros_like(theta), 0
 
     def step(self, tokens, targets, plan: AttnPlan, positions) -> torch.Tensor:
-        """One step on a batch; returns the workers' losses before it.  Raises FgdError, with parameters and moments as they were, if a
-        device-side wait of the attention kernels gave up (it waits for the gradients to know)."""
+        """One step on a batch; returns the workers' losses before it.  With parameters and moments as they were it raises FgdError if a
+        device-side wait of the attention kernels gave up, and IndexError if a token is not in the vocabulary (it waits for the gradients to know)."""
+        highest = tokens.max() if tokens.numel() else None      # (rows of tokens beyond the vocabulary are NaN, and so would be the gradients)
         leaf = self.theta.detach().requires_grad_(True)
         losses = worker_losses(decoder_logits(leaf, tokens, plan, positions, self.cfg, draw=(self.seed, self.t)), targets)
         losses.sum().backward()      # (the workers share no parameter: every row gets its own worker's gradient)
         fgd_attn_status(plan)
+        if highest is not None and highest.item() >= self.cfg.vocab:
+            raise IndexError(f"a token is not in the vocabulary of {self.cfg.vocab}")
         with torch.no_grad():
             self.t += 1
             b1, b2 = self.betas

@@ -280,3 +280,32 @@ def test_decoder_takes_tokens_of_any_strides(how):
         logits.float().square().sum().backward()
         got.append((logits.detach(), leaf.grad))
     assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+
+
+@pytest.mark.parametrize("wrong", [256, 257, 2 ** 40])
+def test_inner_steps_refuse_tokens_beyond_the_vocabulary(wrong):
+    """Parameters, moments and the count of steps stay, and the next step is as if there had been none; padding is no such token."""
+    import paper_2606_22768_b200 as fgd
+    from paper_2606_22768_b200 import inner
+    torch = _torch()
+    cfg = inner.DecoderConfig(dropout=0.1)
+    K, lens = 2, [100, 28]
+    _, P = inner.param_layout(cfg)
+    theta = torch.zeros((K, P), device="cuda")
+    inner.init_params(theta, cfg, 0)
+    gen = torch.Generator().manual_seed(1)
+    tokens, targets = (torch.randint(cfg.vocab, (K, sum(lens)), generator=gen).cuda() for _ in range(2))
+    tokens[0, -3:] = targets[0, -3:] = -1
+    plan = fgd.AttnPlan(np.concatenate([[0], np.cumsum(lens * K)]))
+    positions = torch.cat([torch.arange(n) for n in lens * K]).cuda()
+    plain, steps = inner.InnerSteps(theta.clone(), cfg), inner.InnerSteps(theta.clone(), cfg)
+    plain.step(tokens, targets, plan, positions)
+    steps.step(tokens, targets, plan, positions)
+    keep = [t.clone() for t in (steps.theta, steps.m, steps.v)]
+    bad = tokens.clone()
+    bad[1, 5] = wrong
+    with pytest.raises(IndexError, match="vocabulary of 256"):
+        steps.step(bad, targets, plan, positions)
+    assert all(torch.equal(a, b) for a, b in zip(keep, (steps.theta, steps.m, steps.v))) and steps.t == 1
+    assert torch.equal(plain.step(tokens, targets, plan, positions), steps.step(tokens, targets, plan, positions))
+    assert torch.equal(plain.theta, steps.theta) and bool(steps.theta.isfinite().all())
