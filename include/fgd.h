@@ -437,7 +437,7 @@ int64_t fgd_qk_rope_workspace(int device, int workers, int head_dim);
  *   forward:  out = scale table[token], rounded once.  A token below 0 is padding, its row zero; one at vocab or above makes its row NaN.
  *   backward: dtable[v] = scale times the sum of dout over the tokens that are v (in fp32, in an order that depends on the tokens alone);
  *             every row of dtable is written, those of absent tokens with zero; tokens outside [0, vocab) have no part.
- * width <= 65536, vocab <= 2^30, workers <= FGD_MAX_K. */
+ * width <= 65536, vocab <= 2^30, workers <= FGD_MAX_K, scale finite in fp32. */
 int fgd_embed_forward(int device, int dtype, int workers, int64_t rows, int64_t vocab, int64_t width, const void* tokens, int token_bytes, int64_t ld_tokens,
                       const float* table, int64_t worker_stride, int64_t row_stride, double scale, void* out, int64_t ld_out, void* stream);
 int fgd_embed_backward(int device, int dtype, int workers, int64_t rows, int64_t vocab, int64_t width, const void* tokens, int token_bytes, int64_t ld_tokens,

@@ -592,7 +592,7 @@ int check_common(const char* who, int dtype, int workers, int64_t rows, int64_t 
     return op_fail(FGD_ERR_INVALID_ARG, "%s: workers=%d, rows=%lld, vocab=%lld, width=%lld out of range", who, workers, (long long)rows, (long long)vocab, (long long)width);
   if (width > kMaxWidth) return op_fail(FGD_ERR_UNSUPPORTED, "%s: width %lld above %lld", who, (long long)width, (long long)kMaxWidth);
   if (token_bytes != 4 && token_bytes != 8) return op_fail(FGD_ERR_INVALID_ARG, "%s: token_bytes %d", who, token_bytes);
-  if (!std::isfinite(scale)) return op_fail(FGD_ERR_INVALID_ARG, "%s: scale is not finite", who);
+  if (!std::isfinite((float)scale)) return op_fail(FGD_ERR_INVALID_ARG, "%s: scale is not finite in fp32", who);
   if (!table || (rows > 0 && (!tokens || !x))) return op_fail(FGD_ERR_INVALID_ARG, "%s: NULL pointer", who);
   if (rows > 0 && (ld_tokens < rows || ld_x < width)) return op_fail(FGD_ERR_INVALID_ARG, "%s: a row stride is below the row's width", who);
   if (row_stride < width || worker_stride < 0) return op_fail(FGD_ERR_INVALID_ARG, "%s: a stride of the table is below its row's width, or negative", who);

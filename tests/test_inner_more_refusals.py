@@ -94,6 +94,14 @@ def test_embed_refuses(backward, status, change):
     assert _embed(backward, **change) == status
 
 
+@pytest.mark.parametrize("backward", [False, True])
+@pytest.mark.parametrize("rows", [10, 1000])
+@pytest.mark.parametrize("scale", [1e39, -1e39, 3.4028236e38])
+def test_embed_refuses_scales_beyond_fp32(backward, rows, scale):
+    """Finite in 64 bits and infinite in the kernels, where padding and absent tokens would be 0 times infinity."""
+    assert _embed(backward, rows=rows, ld_tokens=rows, scale=scale) == INVALID
+
+
 @pytest.mark.parametrize("backward,status,change", [
     (False, ALIAS, dict(x=_at(0))), (True, INVALID, dict(worker_stride=3199)), (True, INVALID, dict(worker_stride=0)), (True, ALIAS, dict(table=_at(0))), (True, ALIAS, dict(table=_at(3) + 16)), (True, ALIAS, dict(x=_at(3))), (True, INVALID, dict(workspace=0)),
     (True, INVALID, dict(workspace=_at(3) + 8)), (True, INVALID, dict(workspace_bytes=100)), (True, ALIAS, dict(workspace=_at(0))),
