@@ -424,7 +424,7 @@ typedef struct {
   void* workspace;              /* backward with weights: device scratch */
   int64_t workspace_bytes;
 } fgd_qk_rope_args;
-/* head_dim <= 256, workers <= FGD_MAX_K, rotary_dim even.  Full speed: heads on 16-byte boundaries, rotary_dim / 2 and half of the other channels
+/* head_dim <= 256, workers <= FGD_MAX_K, rotary_dim even, eps >= 0 and finite in fp32.  Full speed: heads on 16-byte boundaries, rotary_dim / 2 and half of the other channels
  * multiples of 16 bytes, tables on 16-byte boundaries.  16-bit heads of which these are multiples of 8 or (to 128 channels) 4 bytes take 1.5 to 3 times
  * as long per byte, everything else, channel by channel, 5 to 7 times.  A workspace, here and below, belongs to one call at a time. */
 int fgd_qk_rope_forward(int device, const fgd_qk_rope_args* args, void* stream);

@@ -607,7 +607,7 @@ int run_rope(const fgd_qk_rope_args* b, bool backward, int device, void* stream)
   if (d > kMaxDim) return op_fail(FGD_ERR_UNSUPPORTED, "%s: head_dim %d above %d", who, d, kMaxDim);
   if (rot < 2 || rot % 2 != 0 || rot > d) return op_fail(FGD_ERR_INVALID_ARG, "%s: rotary_dim %d is not an even number up to head_dim", who, rot);
   if (b->position_bytes != 0 && b->position_bytes != 4 && b->position_bytes != 8) return op_fail(FGD_ERR_INVALID_ARG, "%s: position_bytes %d", who, b->position_bytes);
-  if (!std::isfinite(b->eps) || b->eps < 0) return op_fail(FGD_ERR_INVALID_ARG, "%s: eps is negative or not finite", who);
+  if (!std::isfinite((float)b->eps) || b->eps < 0) return op_fail(FGD_ERR_INVALID_ARG, "%s: eps is negative or not finite in fp32", who);
   const int64_t T = b->workers * b->rows;
   const bool use[2] = {true, b->n_k_heads > 0};
   const bool norm[2] = {b->w_q.p != nullptr, use[1] && b->w_k.p != nullptr}, any_norm = norm[0] || norm[1];

@@ -61,6 +61,13 @@ def test_rope_backward_refuses(status, change):
     assert _rope(True, **change) == status
 
 
+@pytest.mark.parametrize("backward", [False, True])
+@pytest.mark.parametrize("eps", [1e39, 3.4028236e38])
+def test_rope_refuses_eps_beyond_fp32(backward, eps):
+    """Finite in 64 bits and infinite in the kernels, where every norm would be zero."""
+    assert _rope(backward, eps=eps) == INVALID
+
+
 def test_rope_null():
     assert fgd._lib.fgd_qk_rope_forward(0, None, None) == INVALID and fgd._lib.fgd_qk_rope_backward(0, None, None) == INVALID
     for args in ((0, 64), (65, 64), (1, 0), (1, 257)):
