@@ -110,7 +110,9 @@ class _QkvRope(torch.autograd.Function):
 
 def qkv_rope(qkv, n_q: int, n_k: int, cos, sin, positions=None, w_q=None, w_k=None, eps: float = 1e-5, interleaved: bool = False):
     """(q, k, v) of a fused projection's output [T, n_q + n_k + values' heads, d]: q and k normalised per head (w_q, w_k [K, d]; None: not) and rotated by rows
-    ``positions`` (None: row t) of the tables cos and sin [N, r / 2]; v is a view of qkv."""
+    ``positions`` (None: row t) of the tables cos and sin [N, r / 2], which have no gradients; v is a view of qkv."""
+    if torch.is_grad_enabled() and (cos.requires_grad or sin.requires_grad):
+        raise ValueError("cos and sin have no gradients here: detach them")
     return _QkvRope.apply(qkv, w_q, w_k, cos, sin, positions, n_q, n_k, eps, interleaved)
 
 

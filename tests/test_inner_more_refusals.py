@@ -154,3 +154,15 @@ def test_bindings_refuse_cpu_tensors_and_wrong_shapes():
     with pytest.raises(TypeError):
         fgd.fgd_dropout(t, t, 0.1, 0)
     assert ctypes.sizeof(ctypes.c_int64) * 46 == fgd._ROPE_ARGS.size
+
+
+@pytest.mark.parametrize("which", ["cos", "sin"])
+def test_rotation_refuses_tables_that_ask_for_gradients(which):
+    """There are none: the result would be differentiated as if the tables were constants."""
+    torch = pytest.importorskip("torch")
+    from paper_2606_22768_b200 import inner
+    tables = {n: torch.zeros((4, 4), requires_grad=n == which) for n in ("cos", "sin")}
+    with pytest.raises(ValueError, match="no gradients"):
+        inner.qkv_rope(torch.zeros((4, 4, 8)), 2, 1, **tables)
+    with torch.no_grad(), pytest.raises(TypeError, match="CUDA"):      # (without one it goes on to the next check)
+        inner.qkv_rope(torch.zeros((4, 4, 8)), 2, 1, **tables)
