@@ -110,6 +110,34 @@ def test_rope_parts(norm, hk, positions):
     _rope_case(2, 30, 4, hk, 64, 64, False, norm, "bf16", positions=positions)
 
 
+@pytest.mark.parametrize("layout", ["plain", "fused", "head_major", "odd"])
+@pytest.mark.parametrize("K,rows,hq,hk,d,rot,inter,norm,dtype", [
+    (2, 37, 4, 2, 64, 64, False, "qk", "bf16"), (1, 9001, 6, 2, 128, 128, False, "qk", "bf16"), (1, 5003, 6, 2, 80, 48, True, "qk", "f32"), (3, 3001, 6, 2, 40, 40, False, "qk", "f16"),
+    (1, 301, 3, 1, 66, 66, False, "qk", "bf16"), (1, 1, 16, 4, 128, 128, True, "qk", "f32"), (2, 700, 4, 4, 72, 72, True, "q", "bf16"), (2, 700, 4, 4, 255, 128, False, "k", "f16")])
+def test_rope_gradients_in_place_of_what_they_come_from(K, rows, hq, hk, d, rot, inter, norm, dtype, layout):
+    """dq may be dq_out and dk dk_out with weights, too: the same bits as beside one another."""
+    import paper_2606_22768_b200 as fgd
+    torch = _torch()
+    T = K * rows
+    cos, sin = _tables(300, rot)
+    pos = (torch.arange(T, device="cuda") * 7 + 3) % 300
+    w = {n: 1.0 + _randn((K, d), "f32", i, 0.2) if n in norm else None for i, n in enumerate("qk")}
+    x, dy, dx = ({n: _layout(T, h, d, dtype, layout, fill=_randn((T, h, d), dtype, seed + h)) for n, h in (("q", hq), ("k", hk))} for seed in (10, 50, 90))
+
+    def run(dq, dk):
+        dw = {n: None if w[n] is None else torch.empty_like(w[n]) for n in "qk"}
+        fgd.fgd_qk_rope_backward(dy["q"][0], dy["k"][0], x["q"][0], x["k"][0], w["q"], w["k"], cos, sin, pos, dq, dk, dw["q"], dw["k"], 1e-5, inter)
+        return [t for t in dw.values() if t is not None]
+
+    apart = run(dx["q"][0], dx["k"][0])
+    inside = run(dy["q"][0], dy["k"][0])
+    assert all(torch.equal(a, b) for a, b in zip(apart, inside))
+    for n in "qk":
+        assert torch.equal(dx[n][0], dy[n][0]), "d" + n
+        if layout != "plain":
+            _untouched(*dy[n], "d" + n)
+
+
 @pytest.mark.parametrize("pad", [1, 4])
 def test_rope_table_strides(pad):
     _rope_case(1, 40, 4, 2, 128, 128, False, "qk", "bf16", pad=pad)
