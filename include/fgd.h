@@ -435,7 +435,8 @@ int64_t fgd_qk_rope_workspace(int device, int workers, int head_dim);
 /* Embeddings of K workers' tokens.  tokens: device int64 or int32 (token_bytes 8 or 4) [workers, rows], ld_tokens apart; table: fp32, row v of worker m at
  * table + m worker_stride + v row_stride, e.g. a column range of the flat [K, ld] parameter matrix; out, dout: [workers * rows, width] of `dtype`.
  *   forward:  out = scale table[token], rounded once.  A token below 0 is padding, its row zero; one at vocab or above makes its row NaN.
- *   backward: dtable[v] = scale times the sum of dout over the tokens that are v (in fp32, in an order that depends on the tokens alone);
+ *   backward: dtable[v] = scale times the sum of dout over the tokens that are v (in fp32, in an order that the tokens and the sizes - workers, rows, vocab,
+ *             width - decide alone);
  *             every row of dtable is written, those of absent tokens with zero; tokens outside [0, vocab) have no part.
  * width <= 65536, vocab <= 2^30, workers <= FGD_MAX_K, scale finite in fp32. */
 int fgd_embed_forward(int device, int dtype, int workers, int64_t rows, int64_t vocab, int64_t width, const void* tokens, int token_bytes, int64_t ld_tokens,
@@ -447,10 +448,10 @@ int fgd_embed_backward(int device, int dtype, int workers, int64_t rows, int64_t
 int64_t fgd_embed_workspace(int workers, int64_t rows, int64_t vocab, int64_t width);
 
 /* Dropout with a mask that is a function of (seed, offset, row, column) and is never stored; on the gradient it is its own backward pass.
- *   out[r][c] = x[r][c] / (1 - p) where word(r, c) >= round(p 2^32), else 0 (whatever x holds there)
+ *   out[r][c] = x[r][c] / (1 - p) where word(r, c) >= min(round(p 2^32), 2^32 - 1), else 0 (whatever x holds there)
  *   word(r, c): word c % 4 of Philox4x32 with seven rounds, counter (c / 4, r, low, high word of the offset), key (low, high word of the seed)
  * `counter`: device memory, added to the offset when the kernel runs (NULL: nothing), so that a captured call has another mask at every replay.
- * 0 <= p < 1; rows < 2^32, width < 2^31.  out may be x itself, and otherwise may not overlap it.  Any base and stride on element boundaries. */
+ * 0 <= p < 1; rows < 2^32, width < 2^31 - 4096.  out may be x itself, and otherwise may not overlap it.  Any base and stride on element boundaries. */
 int fgd_dropout(int device, int dtype, int64_t rows, int64_t width, const void* x, int64_t ld_x, void* out, int64_t ld_out, double p, uint64_t seed,
                 uint64_t offset, const int64_t* counter, void* stream);
 

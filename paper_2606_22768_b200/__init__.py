@@ -768,7 +768,8 @@ _NO_ROPE_GRADS, _NO_ROPE_OUTPUTS = (0,) * 18, (0,) * 6
 def _rope_usual(q, k, q_to, k_to, w_q, w_k, cos, sin, positions, eps, interleaved, x_q=None, x_k=None, dw_q=None, dw_k=None):
     """The arguments of a call as they usually are, checked; None where anything is not as usual: then the checks one by one say what is wrong, if it is.
     (Small calls are bound by what the host does: written out, this takes about 6 us of it where the checks one by one take 9.)  q, k go in and q_to, k_to come out,
-    gradients in a backward pass; x_q, x_k and dw_q, dw_k are then its q, k and the gradients of the weights."""
+    gradients in a backward pass; x_q, x_k and dw_q, dw_k are then its q, k and the gradients of the weights.  Calls without positions, as the decoder's, with weights
+    of one side, without keys, and backward passes without weights are not among them."""
     import torch
     if k is None or positions is None or (w_q is None) is not (w_k is None):
         return None

@@ -10,7 +10,7 @@
 //          absent tokens with zeros.
 //   joins  the pieces of the runs that cross chunks, which are few, eight warps to a run.
 // A few tokens need no sort: a warp looks through all of them for the one that its row of the table stands for, in one launch.
-// The order of every sum depends on the tokens alone.
+// The order of every sum depends on the tokens and the sizes alone: workers, rows, vocabulary and width say which kernels run and how long the chunks are.
 // 4 x 8192 tokens of 32000 rows, 2048 wide, bf16: 187 us, 95 % of the copy peak (sort 13, rows and zeros 168, joins 6); 65536 tokens of 50257, 1536 wide, f16:
 // 121 us (25, 84, 12).
 #include <cooperative_groups.h>
